@@ -272,6 +272,22 @@ xpipe_status xpipe_rule_step(xpipe_stage_t st, const xpipe_rule_hparams* rp, con
                              float* buf, float* sq, int32_t s_fwd_next, int32_t s_bwd_next,
                              int32_t emit_pred);
 
+/* Clipping of a stage's updates by the global norm of the gradients.  With
+ * norm_coef (device memory of the caller's, two fp32 values {norm, coefficient},
+ * used until this call is made again or the stage is destroyed) every later
+ * xpipe_adam_step, xpipe_rule_step and update of xpipe_stage_run multiplies the
+ * accumulated gradient by norm_coef[1], rounded to fp32, as it reads it.
+ *   max_norm > 0: the update first computes both values over the stage's own
+ *     accumulator, as xpipe_grad_norm does; workspace (device memory, 8-byte
+ *     aligned, at least xpipe_grad_norm_query's bytes for one tensor of the
+ *     stage's padded parameter count) is used by the updates.
+ *   max_norm = 0: the caller has written norm_coef on the stage's stream before
+ *     the update: a norm over several stages and tables (xpipe_grad_norm,
+ *     xpipe_clip_coef).  No workspace.
+ * norm_coef = NULL turns clipping off (the default). */
+xpipe_status xpipe_stage_set_clip(xpipe_stage_t st, double max_norm, float* norm_coef, void* workspace,
+                                  size_t workspace_bytes);
+
 xpipe_status xpipe_stage_destroy(xpipe_stage_t st);
 
 /* ---------------------------------------------------------------- partition
@@ -374,6 +390,131 @@ xpipe_status xpipe_rule_flat(float* W, float* buf, float* sq, float* m, float* v
                              const xpipe_rule_hparams* rp, const xpipe_hparams* hp, int32_t zero_grad,
                              float* pred_fwd, int32_t s_fwd, float* pred_bwd, int32_t s_bwd,
                              void* hip_stream);
+
+/* xpipe_adam_flat and xpipe_rule_flat on the gradient times norm_coef[1] (device,
+ * written on the same stream before by xpipe_grad_norm or xpipe_clip_coef; the
+ * product is rounded to fp32, G itself is not changed by it). */
+xpipe_status xpipe_adam_flat_clipped(float* W, float* m, float* v, float* G, int64_t n,
+                                     const xpipe_hparams* hp, int32_t zero_grad,
+                                     float* pred_fwd, int32_t s_fwd, float* pred_bwd, int32_t s_bwd,
+                                     const float* norm_coef, void* hip_stream);
+xpipe_status xpipe_rule_flat_clipped(float* W, float* buf, float* sq, float* m, float* v, float* G, int64_t n,
+                                     const xpipe_rule_hparams* rp, const xpipe_hparams* hp, int32_t zero_grad,
+                                     float* pred_fwd, int32_t s_fwd, float* pred_bwd, int32_t s_bwd,
+                                     const float* norm_coef, void* hip_stream);
+
+/* ---------------------------------------------------------------- gradient norm
+ * The global norm of the gradients over many tensors, for clipping (the
+ * accumulators of stages, linear layers and tables that one norm bounds).
+ *   sumsq = sum over all elements of g^2   (fp64)
+ *   norm = sqrt(sumsq);  coefficient = min(1, max_norm / (norm + 1e-6))
+ * A NaN anywhere makes both NaN; an infinity makes the norm infinite and the
+ * coefficient 0.  The order of the sums follows from the sizes and alignments
+ * alone, so a repeated call gives the same bits.  tensors: host array, read by
+ * the call itself; each tensor contiguous, aligned to its element, of dtype
+ * XPIPE_F32 or XPIPE_BF16 (one for all), n >= 0.  workspace: device memory,
+ * 8-byte aligned, of xpipe_grad_norm_query's bytes, free again once the call's
+ * work is done.  sumsq (device, fp64, may be NULL) receives the sum;
+ * norm_coef (device, two fp32, may be NULL) {norm, coefficient}.  max_norm > 0
+ * where norm_coef is given. */
+typedef struct {
+  const void* p;
+  int64_t n;
+} xpipe_tensor;
+xpipe_status xpipe_grad_norm_query(const xpipe_tensor* tensors, int32_t n_tensors, size_t* workspace_bytes);
+xpipe_status xpipe_grad_norm(const xpipe_tensor* tensors, int32_t n_tensors, int32_t dtype, double max_norm,
+                             double* sumsq, float* norm_coef, void* workspace, size_t workspace_bytes,
+                             void* hip_stream);
+/* The same from n sums of squares (device, fp64), added in order: a pipeline's
+ * stages each pass their own sumsq on and clip by the norm over all of them. */
+xpipe_status xpipe_clip_coef(const double* sumsq, int64_t n, double max_norm, float* norm_coef, void* hip_stream);
+
+/* ---------------------------------------------------------------- linear
+ * A linear layer outside a stage, with its bias, activation and residual in the
+ * product's epilogue, and its gradients: the layers of a network over tokens
+ * between its table (xpipe_embedding_fwd) and a stage.  W is the layer's weight
+ * in the storage dtype (for XPIPE_BF16 xpipe_predict_flat's out_bf16), bias its
+ * fp32 prediction.
+ *   forward:  z = x W^T + bias;  y = act(z) + residual
+ *   backward: dx = (dz W) act'(preact) + residual;  grad_W += dz^T x;  grad_b += sum of dz's rows
+ * As in a stage, a gradient buffer holds the gradient of the pre-activation:
+ * dz is the one of this layer's z, and the backward's act and preact are those
+ * of the layer whose output act(preact) is x (XPIPE_ACT_NONE: x is no
+ * activation's output), so that dx is that layer's dz.  The backward's residual
+ * is a gradient that reaches x another way (a skip connection's), added as it is.
+ * The activation's gradient where dy comes from elsewhere: xpipe_act_bwd.
+ * Products have fp32 sums (XPIPE_BF16: bf16 MFMA; XPIPE_F32: fp32 MFMA), the
+ * epilogue is computed in fp32, each stored value is rounded once (z_stored is
+ * rounded apart; y comes from the unrounded z).  A row's results depend on its
+ * own values alone; the order of the sums follows from sizes, strides and
+ * alignments, so a repeated call gives the same bits.
+ * Every matrix has contiguous rows, ld elements apart (ld >= its columns, at
+ * most XPIPE_LINEAR_MAX_LD), is aligned to its element, and may start anywhere;
+ * 16-byte aligned pointers with ld a multiple of 16 bytes are read and written
+ * without a copy.  rows >= 0 (0: nothing is done).  Outputs must not overlap
+ * inputs or one another; residual (and preact in the backward) alone may be the
+ * output's own buffer (same pointer and ld). */
+typedef enum { XPIPE_ACT_NONE = 0, XPIPE_ACT_RELU = 1,
+               XPIPE_ACT_GELU = 2,  /* z/2 (1 + erf(z / sqrt 2)) */
+               XPIPE_ACT_SILU = 3   /* z / (1 + exp(-z)) */
+} xpipe_act;
+#define XPIPE_LINEAR_MAX_LD ((int64_t)1 << 20)
+typedef struct {
+  int64_t rows;
+  int32_t cin, cout, dtype, act;
+  const void* x; int64_t ldx;            /* [rows][cin] */
+  const void* W; int64_t ldw;            /* [cout][cin] */
+  const float* bias;                     /* [cout], or NULL */
+  const void* residual; int64_t ldr;     /* [rows][cout], or NULL */
+  void* preact; int64_t ldz;             /* [rows][cout]: receives z, or NULL */
+  void* y; int64_t ldy;                  /* [rows][cout] */
+} xpipe_linear_fwd_args;
+typedef struct {
+  int64_t rows;
+  int32_t cin, cout, dtype, act;
+  const void* dz; int64_t lddz;          /* [rows][cout] */
+  const void* x; int64_t ldx;            /* [rows][cin]; may be NULL without grad_W and grad_b */
+  const void* W; int64_t ldw;            /* [cout][cin]; may be NULL without dx */
+  const void* preact; int64_t ldz;       /* [rows][cin]; NULL iff act is XPIPE_ACT_NONE or dx is NULL */
+  const void* residual; int64_t ldr;     /* [rows][cin], or NULL */
+  void* dx; int64_t lddx;                /* [rows][cin], or NULL */
+  float* grad_W;                         /* [cout][cin] contiguous, added to, or NULL */
+  float* grad_b;                         /* [cout], added to, or NULL (needs grad_W) */
+} xpipe_linear_bwd_args;
+/* Workspace of a call with these arguments (0 for most; it depends on sizes,
+ * strides and the pointers' alignment).  Host only. */
+xpipe_status xpipe_linear_fwd_query(const xpipe_linear_fwd_args* args, size_t* workspace_bytes);
+xpipe_status xpipe_linear_bwd_query(const xpipe_linear_bwd_args* args, size_t* workspace_bytes);
+/* workspace: device memory, 256-byte aligned, of at least the query's bytes, free
+ * again once the call's work is done (NULL where the query gives 0). */
+xpipe_status xpipe_linear_fwd(const xpipe_linear_fwd_args* args, void* workspace, size_t workspace_bytes,
+                              void* hip_stream);
+xpipe_status xpipe_linear_bwd(const xpipe_linear_bwd_args* args, void* workspace, size_t workspace_bytes,
+                              void* hip_stream);
+/* dz = dy act'(z), n contiguous elements of dtype (dz may be dy or z). */
+xpipe_status xpipe_act_bwd(const void* dy, const void* z, void* dz, int64_t n, int32_t act, int32_t dtype,
+                           void* hip_stream);
+
+/* ---------------------------------------------------------------- embedding
+ * The lookup of a token model's first stage and its table's gradient.
+ *   forward:  y[i] = scale * table[tokens[i]]
+ *   backward: grad[v] += scale * sum over i with tokens[i] = v of dy[i]
+ * table [vocab][dim], y and dy [n_tokens][dim] in the storage dtype, grad
+ * [vocab][dim] fp32, all contiguous; tokens int32 on the device.  A token
+ * outside [0, vocab) is padding: its row of y is zeros, its dy is not
+ * read.  y can be a stage's x, and dy its dx.  Products
+ * and sums are formed in fp64 and rounded once (a run of more than 8 (from
+ * 2048 tokens on 16, from 16384 on 64) equal tokens that passes a multiple of
+ * that many sorted positions has its parts' sums rounded to fp32 between).  The terms
+ * are added in the order of the positions, so a repeated call gives the same bits. */
+xpipe_status xpipe_embedding_fwd(const void* table, const int32_t* tokens, int64_t n_tokens, int32_t vocab, int32_t dim,
+                                 double scale, int32_t dtype, void* y, void* hip_stream);
+/* workspace: device memory, 256-byte aligned, of the query's bytes, free again
+ * once the call's work is done. */
+xpipe_status xpipe_embedding_bwd_query(int64_t n_tokens, int32_t vocab, int32_t dim, size_t* workspace_bytes);
+xpipe_status xpipe_embedding_bwd(const void* dy, const int32_t* tokens, int64_t n_tokens, int32_t vocab, int32_t dim,
+                                 double scale, int32_t dtype, float* grad, void* workspace, size_t workspace_bytes,
+                                 void* hip_stream);
 
 /* Optional per-kernel timing (measurement support, not part of the method):
  * while enabled, hipEvents bracket every kernel the stage launches on its

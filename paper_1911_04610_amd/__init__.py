@@ -9,8 +9,14 @@ Entry points (same names as the C ABI):
   xpipe_version_difference, xpipe_stage_query, Stage (xpipe_stage_create /
   _param_layout / _output_shape / xpipe_predict_weights / xpipe_stage_fwd /
   xpipe_stage_bwd / xpipe_adam_step / xpipe_rule_step / xpipe_stage_destroy /
-  timing / recorded passes / xpipe_stage_run), xpipe_schedule, xpipe_predict_flat,
-  xpipe_adam_flat, xpipe_rule_flat.
+  timing / recorded passes / xpipe_stage_run / xpipe_stage_set_clip), xpipe_schedule,
+  xpipe_predict_flat, xpipe_adam_flat, xpipe_rule_flat (with clip= their _clipped forms);
+  around a stage: xpipe_linear_fwd, xpipe_linear_bwd, xpipe_act_bwd,
+  xpipe_embedding_fwd, xpipe_embedding_bwd, xpipe_grad_norm (over a TensorList),
+  xpipe_clip_coef.
+The last group checks devices, types and shapes (ValueError), runs on its
+tensors' device (on `stream`, or that device's current stream) and allocates
+the workspace that a call needs from torch on that stream, unless it is given one.
 """
 from __future__ import annotations
 
@@ -28,6 +34,7 @@ FWD, BWD = 0, 1
 KEEP_PRED = 2
 PRED_EQ3, PRED_ADAMDIR, PRED_LITERAL, PRED_SMOOTHED = 0, 1, 2, 3
 RULE_MOMENTUM_SGD, RULE_RMSPROP = 1, 2
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
 ROUND_HALF_UP, ROUND_HALF_EVEN, ROUND_HALF_DOWN = 0, 1, 2
 KINDS = {"linear": 0, "conv": 1, "bn": 2, "relu": 3, "add": 4, "maxpool2": 5, "avgpool3": 6,
          "gap": 7, "concat": 8, "softmax_ce": 9, "maxpool3s2": 10}
@@ -67,6 +74,27 @@ class RunIO(ctypes.Structure):
 class RuleParams(ctypes.Structure):
     _fields_ = [("rule", ctypes.c_int32), ("lr", ctypes.c_double), ("momentum", ctypes.c_double),
                 ("weight_decay", ctypes.c_double), ("alpha", ctypes.c_double), ("eps", ctypes.c_double)]
+
+
+class TensorDesc(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("n", ctypes.c_int64)]
+
+
+class LinearFwdArgs(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cin", ctypes.c_int32), ("cout", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("act", ctypes.c_int32),
+                ("x", ctypes.c_void_p), ("ldx", ctypes.c_int64), ("W", ctypes.c_void_p), ("ldw", ctypes.c_int64),
+                ("bias", ctypes.c_void_p), ("residual", ctypes.c_void_p), ("ldr", ctypes.c_int64),
+                ("preact", ctypes.c_void_p), ("ldz", ctypes.c_int64), ("y", ctypes.c_void_p), ("ldy", ctypes.c_int64)]
+
+
+class LinearBwdArgs(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cin", ctypes.c_int32), ("cout", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("act", ctypes.c_int32),
+                ("dz", ctypes.c_void_p), ("lddz", ctypes.c_int64), ("x", ctypes.c_void_p), ("ldx", ctypes.c_int64),
+                ("W", ctypes.c_void_p), ("ldw", ctypes.c_int64), ("preact", ctypes.c_void_p), ("ldz", ctypes.c_int64),
+                ("residual", ctypes.c_void_p), ("ldr", ctypes.c_int64), ("dx", ctypes.c_void_p),
+                ("lddx", ctypes.c_int64), ("grad_W", ctypes.c_void_p), ("grad_b", ctypes.c_void_p)]
 
 
 @dataclasses.dataclass
@@ -125,6 +153,22 @@ _SIGS = {
     "xpipe_predict_flat": [_P, _P, _P, _P, _P, _I64, _I32, ctypes.POINTER(HParams), _P],
     "xpipe_adam_flat": [_P, _P, _P, _P, _I64, ctypes.POINTER(HParams), _I32, _P, _I32, _P, _I32,
                         _P],
+    "xpipe_adam_flat_clipped": [_P, _P, _P, _P, _I64, ctypes.POINTER(HParams), _I32, _P, _I32, _P, _I32,
+                                _P, _P],
+    "xpipe_rule_flat_clipped": [_P, _P, _P, _P, _P, _P, _I64, ctypes.POINTER(RuleParams),
+                                ctypes.POINTER(HParams), _I32, _P, _I32, _P, _I32, _P, _P],
+    "xpipe_stage_set_clip": [_P, ctypes.c_double, _P, _P, _SZ],
+    "xpipe_grad_norm_query": [_P, _I32, ctypes.POINTER(_SZ)],
+    "xpipe_grad_norm": [_P, _I32, _I32, ctypes.c_double, _P, _P, _P, _SZ, _P],
+    "xpipe_clip_coef": [_P, _I64, ctypes.c_double, _P, _P],
+    "xpipe_linear_fwd_query": [ctypes.POINTER(LinearFwdArgs), ctypes.POINTER(_SZ)],
+    "xpipe_linear_bwd_query": [ctypes.POINTER(LinearBwdArgs), ctypes.POINTER(_SZ)],
+    "xpipe_linear_fwd": [ctypes.POINTER(LinearFwdArgs), _P, _SZ, _P],
+    "xpipe_linear_bwd": [ctypes.POINTER(LinearBwdArgs), _P, _SZ, _P],
+    "xpipe_act_bwd": [_P, _P, _P, _I64, _I32, _I32, _P],
+    "xpipe_embedding_fwd": [_P, _P, _I64, _I32, _I32, ctypes.c_double, _I32, _P, _P],
+    "xpipe_embedding_bwd_query": [_I64, _I32, _I32, ctypes.POINTER(_SZ)],
+    "xpipe_embedding_bwd": [_P, _P, _I64, _I32, _I32, ctypes.c_double, _I32, _P, _P, _SZ, _P],
     "xpipe_probe_copy": [_P, _P, _I64, _P],
     "xpipe_probe_mfma": [_P, _I32, _I32, _P],
     "xpipe_probe_graph": [_P, _I32, _I32, _I32, _I32, ctypes.POINTER(ctypes.c_double), _P],
@@ -354,6 +398,23 @@ class Stage:
                                      ctypes.cast(ctypes.pointer(r), ctypes.c_void_p) if r is not None else None,
                                      _ptr(buf), _ptr(sq), int(draft)))
 
+    def xpipe_stage_set_clip(self, max_norm: float, norm_coef):
+        """Clip every later update by the global gradient norm.  norm_coef: fp32
+        device tensor of two elements {norm, coefficient} (None: off).  With
+        max_norm > 0 each update computes them over this stage's accumulator
+        (workspace allocated here); with 0 the caller writes them before the
+        update (xpipe_grad_norm over several buffers)."""
+        ws, size = None, _SZ(0)
+        if norm_coef is not None:
+            _check_norm_coef(norm_coef, self.grad.device)
+            if max_norm > 0:
+                import torch
+                one = TensorDesc(_ptr(self.grad), self.P)
+                _check(lib().xpipe_grad_norm_query(ctypes.byref(one), 1, ctypes.byref(size)))
+                ws = torch.empty(max(size.value, 8), dtype=torch.uint8, device=self.device)
+        _check(lib().xpipe_stage_set_clip(self._h, max_norm, _ptr(norm_coef), _ptr(ws), size.value))
+        self._clip = (norm_coef, ws)  # kept while the stage uses them
+
     def set_timing(self, enable: bool):
         _check(lib().xpipe_stage_set_timing(self._h, int(enable)))
 
@@ -411,8 +472,15 @@ def xpipe_schedule(size: int, T: int, rank: int, minibatches: int, rounding: int
 
 
 def xpipe_rule_flat(W, buf, sq, m, v, G, rule: Rule, hp: Hyper, t: int, zero_grad=True, pred_fwd=None,
-                    s_fwd=0, pred_bwd=None, s_bwd=0, stream=None):
+                    s_fwd=0, pred_bwd=None, s_bwd=0, stream=None, clip=None):
+    """clip: {norm, coefficient} of xpipe_grad_norm; the update reads G times the coefficient."""
     r, c = rule.c(), hp.c(t)
+    if clip is not None:
+        _check_norm_coef(clip, W.device)
+        _check(lib().xpipe_rule_flat_clipped(_ptr(W), _ptr(buf), _ptr(sq), _ptr(m), _ptr(v), _ptr(G), W.numel(),
+                                             ctypes.byref(r), ctypes.byref(c), int(zero_grad), _ptr(pred_fwd), s_fwd,
+                                             _ptr(pred_bwd), s_bwd, _ptr(clip), _stream_ptr(stream)))
+        return
     _check(lib().xpipe_rule_flat(_ptr(W), _ptr(buf), _ptr(sq), _ptr(m), _ptr(v), _ptr(G), W.numel(),
                                  ctypes.byref(r), ctypes.byref(c), int(zero_grad), _ptr(pred_fwd), s_fwd,
                                  _ptr(pred_bwd), s_bwd, _stream_ptr(stream)))
@@ -453,8 +521,253 @@ def xpipe_probe_stream(srcs, dsts, stream=None):
 
 
 def xpipe_adam_flat(W, m, v, G, hp: Hyper, t: int, zero_grad=True, pred_fwd=None, s_fwd=0,
-                    pred_bwd=None, s_bwd=0, stream=None):
+                    pred_bwd=None, s_bwd=0, stream=None, clip=None):
+    """clip: {norm, coefficient} of xpipe_grad_norm; the update reads G times the coefficient."""
     c = hp.c(t)
+    if clip is not None:
+        _check_norm_coef(clip, W.device)
+        _check(lib().xpipe_adam_flat_clipped(_ptr(W), _ptr(m), _ptr(v), _ptr(G), W.numel(), ctypes.byref(c),
+                                             int(zero_grad), _ptr(pred_fwd), s_fwd, _ptr(pred_bwd), s_bwd,
+                                             _ptr(clip), _stream_ptr(stream)))
+        return
     _check(lib().xpipe_adam_flat(_ptr(W), _ptr(m), _ptr(v), _ptr(G), W.numel(), ctypes.byref(c),
                                  int(zero_grad), _ptr(pred_fwd), s_fwd, _ptr(pred_bwd), s_bwd,
                                  _stream_ptr(stream)))
+
+
+# ---------------------------------------------------------------- operators around a stage
+def _need(ok, msg):
+    if not ok:
+        raise ValueError(msg)
+
+
+def _check_norm_coef(t, device):
+    import torch
+    _need(t.dtype == torch.float32 and t.numel() == 2 and t.is_contiguous() and t.device == device,
+          "{norm, coefficient}: two contiguous float32 elements on the gradients' device")
+
+
+def _dtype_of(t) -> int:
+    import torch
+    _need(t.dtype in (torch.bfloat16, torch.float32), f"bfloat16 or float32, not {t.dtype}")
+    return BF16 if t.dtype == torch.bfloat16 else F32
+
+
+def _matrix(name, t, like, shape):
+    """Row pitch (elements) of a 2-D tensor of `like`'s type and device with contiguous rows."""
+    _need(t.dtype == like.dtype and t.device == like.device, f"{name}: another type or device")
+    _need(tuple(t.shape) == tuple(shape), f"{name}: shape {tuple(t.shape)}, {tuple(shape)} expected")
+    if t.shape[0] <= 1:
+        _need(t.shape[1] <= 1 or t.stride(1) == 1, f"{name}: rows must be contiguous")
+        return t.shape[1]
+    _need((t.shape[1] <= 1 or t.stride(1) == 1) and t.stride(0) >= t.shape[1], f"{name}: rows must be contiguous")
+    return t.stride(0)
+
+
+def _vector(name, t, like, n):
+    import torch
+    _need(t.dtype == torch.float32 and t.device == like.device and t.is_contiguous() and t.numel() == n,
+          f"{name}: {n} contiguous float32 elements on the same device expected")
+
+
+class _On:
+    """Makes a tensor's device current for a call; gives the stream and the workspace there."""
+
+    def __init__(self, t, stream):
+        import torch
+        self.ctx = None
+        _need(t.is_cuda, "tensors must be on the GPU")
+        if t.device.index != torch.cuda.current_device():
+            self.ctx = torch.cuda.device(t.device)
+        self.device, self.stream = t.device, stream
+
+    def __enter__(self):
+        import torch
+        if self.ctx is not None:
+            self.ctx.__enter__()
+        if self.stream is not None and self.stream.device != self.device:
+            self.__exit__(None, None, None)
+            raise ValueError("the stream is another device's")
+        self.own_stream = self.stream is None
+        if self.own_stream:
+            self.stream = torch.cuda.current_stream()
+        self.ptr = self.stream.cuda_stream
+        return self
+
+    def workspace(self, need, given):
+        """(pointer, bytes, tensor to keep until the call returns)."""
+        import torch
+        if need == 0:
+            return None, 0, None
+        if given is not None:
+            _need(given.device == self.device and given.is_contiguous(), "workspace: contiguous, on the same device")
+            base, size = given.data_ptr(), given.numel() * given.element_size()
+            skip = -base % 256
+            return base + skip, max(0, size - skip), given
+        if self.own_stream:
+            ws = torch.empty(need + 256, dtype=torch.uint8, device=self.device)
+        else:  # the allocator then gives it out again in that stream's order
+            with torch.cuda.stream(self.stream):
+                ws = torch.empty(need + 256, dtype=torch.uint8, device=self.device)
+        skip = -ws.data_ptr() % 256
+        return ws.data_ptr() + skip, need, ws
+
+    def __exit__(self, *exc):
+        if self.ctx is not None:
+            self.ctx.__exit__(*exc)
+
+
+def _ld(a, name, t, like, shape, field):
+    if t is not None:
+        setattr(a, field[0], t.data_ptr())
+        setattr(a, field[1], _matrix(name, t, like, shape))
+
+
+def _linear_fwd_args(x, W, bias, y, act, residual, preact):
+    _need(x.dim() == 2 and W.dim() == 2 and W.shape[1] == x.shape[1], "x [rows, cin] and W [cout, cin] expected")
+    (rows, cin), cout = x.shape, W.shape[0]
+    a = LinearFwdArgs(rows=rows, cin=cin, cout=cout, dtype=_dtype_of(x), act=int(act))
+    _ld(a, "x", x, x, (rows, cin), ("x", "ldx"))
+    _ld(a, "W", W, x, (cout, cin), ("W", "ldw"))
+    _ld(a, "residual", residual, x, (rows, cout), ("residual", "ldr"))
+    _ld(a, "preact", preact, x, (rows, cout), ("preact", "ldz"))
+    _ld(a, "y", y, x, (rows, cout), ("y", "ldy"))
+    if bias is not None:
+        _vector("bias", bias, x, cout)
+        a.bias = bias.data_ptr()
+    return a
+
+
+def xpipe_linear_fwd(x, W, bias, y, act: int = ACT_NONE, residual=None, preact=None, workspace=None, stream=None):
+    """y = act(x W^T + bias) + residual; preact (optional) receives the
+    pre-activation.  Matrices of one type (bfloat16 or float32), their rows
+    contiguous; bias float32 or None.  residual may be y itself."""
+    a = _linear_fwd_args(x, W, bias, y, act, residual, preact)
+    with _On(x, stream) as on:
+        need = _SZ(0)
+        _check(lib().xpipe_linear_fwd_query(ctypes.byref(a), ctypes.byref(need)))
+        ptr, size, keep = on.workspace(need.value, workspace)
+        _check(lib().xpipe_linear_fwd(ctypes.byref(a), ptr, size, on.ptr))
+
+
+def xpipe_linear_bwd(dz, x, W, dx=None, grad_W=None, grad_b=None, act: int = ACT_NONE, preact=None, residual=None,
+                     workspace=None, stream=None):
+    """Gradients of a linear layer from dz, the gradient of its pre-activation:
+    dx = (dz W) act'(preact) + residual, grad_W += dz^T x, grad_b += dz's row sum
+    (float32), each optional.  act and preact are those of the layer whose output
+    x is, so dx is that layer's dz; residual is a gradient that reaches x another
+    way and may be dx itself."""
+    _need(dz.dim() == 2, "dz [rows, cout] expected")
+    given = x if x is not None else W
+    _need(given is not None and given.dim() == 2, "x or W expected")
+    (rows, cout), cin = dz.shape, given.shape[1]
+    a = LinearBwdArgs(rows=rows, cin=cin, cout=cout, dtype=_dtype_of(dz), act=int(act))
+    _ld(a, "dz", dz, dz, (rows, cout), ("dz", "lddz"))
+    _ld(a, "x", x, dz, (rows, cin), ("x", "ldx"))
+    _ld(a, "W", W, dz, (cout, cin), ("W", "ldw"))
+    _ld(a, "preact", preact, dz, (rows, cin), ("preact", "ldz"))
+    _ld(a, "residual", residual, dz, (rows, cin), ("residual", "ldr"))
+    _ld(a, "dx", dx, dz, (rows, cin), ("dx", "lddx"))
+    if grad_W is not None:
+        _vector("grad_W", grad_W, dz, cout * cin)
+        a.grad_W = grad_W.data_ptr()
+    if grad_b is not None:
+        _vector("grad_b", grad_b, dz, cout)
+        a.grad_b = grad_b.data_ptr()
+    with _On(dz, stream) as on:
+        need = _SZ(0)
+        _check(lib().xpipe_linear_bwd_query(ctypes.byref(a), ctypes.byref(need)))
+        ptr, size, keep = on.workspace(need.value, workspace)
+        _check(lib().xpipe_linear_bwd(ctypes.byref(a), ptr, size, on.ptr))
+
+
+def xpipe_act_bwd(dy, z, dz, act: int, stream=None):
+    """dz = dy act'(z): contiguous tensors of one type and shape (dz may be dy or z)."""
+    for t in (dy, z, dz):
+        _need(t.shape == dy.shape and t.dtype == dy.dtype and t.device == dy.device and t.is_contiguous(),
+              "contiguous tensors of one type, shape and device expected")
+    dtype = _dtype_of(dy)
+    with _On(dy, stream) as on:
+        _check(lib().xpipe_act_bwd(_ptr(dy), _ptr(z), _ptr(dz), dy.numel(), int(act), dtype, on.ptr))
+
+
+def _embedding_args(rows, name, tokens, like):
+    import torch
+    _need(tokens.dtype == torch.int32 and tokens.is_contiguous() and tokens.device == like.device,
+          "tokens: contiguous int32 on the same device expected")
+    _need(rows.dim() >= 1 and rows.is_contiguous() and rows.device == like.device and
+          rows.numel() == tokens.numel() * rows.shape[-1], f"{name}: contiguous [tokens, dim] expected")
+
+
+def xpipe_embedding_fwd(table, tokens, y, scale: float = 1.0, stream=None):
+    """y[i] = scale * table[tokens[i]] (zeros where a token is outside the table).
+    table [vocab, dim] and y [..., dim] of one type; tokens int32."""
+    _need(table.dim() == 2 and table.is_contiguous(), "table: contiguous [vocab, dim] expected")
+    _embedding_args(y, "y", tokens, table)
+    _need(y.dtype == table.dtype and y.shape[-1] == table.shape[1], "y: the table's type and columns expected")
+    dtype = _dtype_of(table)
+    with _On(table, stream) as on:
+        _check(lib().xpipe_embedding_fwd(_ptr(table), _ptr(tokens), tokens.numel(), table.shape[0], table.shape[1],
+                                         float(scale), dtype, _ptr(y), on.ptr))
+
+
+def xpipe_embedding_bwd(dy, tokens, grad, scale: float = 1.0, workspace=None, stream=None):
+    """grad[tokens[i]] += scale * dy[i], for the tokens inside the table.
+    grad: contiguous float32 [vocab, dim]; dy [..., dim]; tokens int32."""
+    import torch
+    _need(grad.dim() == 2 and grad.is_contiguous() and grad.dtype == torch.float32,
+          "grad: contiguous float32 [vocab, dim] expected")
+    _embedding_args(dy, "dy", tokens, grad)
+    _need(dy.shape[-1] == grad.shape[1], "dy: the table's columns expected")
+    dtype, (vocab, dim) = _dtype_of(dy), grad.shape
+    with _On(grad, stream) as on:
+        need = _SZ(0)
+        _check(lib().xpipe_embedding_bwd_query(tokens.numel(), vocab, dim, ctypes.byref(need)))
+        ptr, size, keep = on.workspace(need.value, workspace)
+        _check(lib().xpipe_embedding_bwd(_ptr(dy), _ptr(tokens), tokens.numel(), vocab, dim, float(scale), dtype,
+                                         _ptr(grad), ptr, size, on.ptr))
+
+
+class TensorList:
+    """Gradients that one norm is taken over: contiguous tensors of one type on
+    one device, kept (with their addresses and the call's workspace size) for
+    repeated xpipe_grad_norm calls."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        _need(len(self.tensors) > 0, "at least one tensor expected")
+        first = self.tensors[0]
+        self.device, self.dtype = first.device, _dtype_of(first)
+        for t in self.tensors:
+            _need(t.dtype == first.dtype and t.device == first.device and t.is_contiguous(),
+                  "contiguous tensors of one type on one device expected")
+        self.descs = (TensorDesc * len(self.tensors))(*[(t.data_ptr(), t.numel()) for t in self.tensors])
+        need = _SZ(0)
+        _check(lib().xpipe_grad_norm_query(self.descs, len(self.tensors), ctypes.byref(need)))
+        self.workspace_bytes = need.value
+
+
+def xpipe_grad_norm(tensors, max_norm: float, norm_coef=None, sumsq=None, workspace=None, stream=None):
+    """Global L2 norm over `tensors` (a TensorList, or an iterable of tensors):
+    norm_coef (float32, two elements) receives {norm, min(1, max_norm / (norm +
+    1e-6))}, sumsq (float64, one element) the sum of squares; either may be None."""
+    import torch
+    ts = tensors if isinstance(tensors, TensorList) else TensorList(tensors)
+    if norm_coef is not None:
+        _check_norm_coef(norm_coef, ts.device)
+    if sumsq is not None:
+        _need(sumsq.dtype == torch.float64 and sumsq.numel() == 1 and sumsq.device == ts.device,
+              "sumsq: one float64 element on the gradients' device expected")
+    with _On(ts.tensors[0], stream) as on:
+        ptr, size, keep = on.workspace(ts.workspace_bytes, workspace)
+        _check(lib().xpipe_grad_norm(ts.descs, len(ts.tensors), ts.dtype, float(max_norm), _ptr(sumsq),
+                                     _ptr(norm_coef), ptr, size, on.ptr))
+
+
+def xpipe_clip_coef(sumsq, max_norm: float, norm_coef, stream=None):
+    """{norm, coefficient} from float64 sums of squares (one per stage), added in order."""
+    import torch
+    _need(sumsq.dtype == torch.float64 and sumsq.is_contiguous(), "sumsq: contiguous float64 expected")
+    _check_norm_coef(norm_coef, sumsq.device)
+    with _On(sumsq, stream) as on:
+        _check(lib().xpipe_clip_coef(_ptr(sumsq), sumsq.numel(), float(max_norm), _ptr(norm_coef), on.ptr))

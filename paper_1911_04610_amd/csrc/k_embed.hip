@@ -1,0 +1,408 @@
+// Embedding lookup, and its gradient by sorted tokens.
+//
+// The gradient of a table row is the sum over the positions that hold its token.
+// The positions are sorted by token (stable, so a row's terms are added in the
+// order of their positions: the same bits every time, no atomics on sums), and
+// every row of dy is then read once.  Tokens outside [0, vocab) are padding:
+// zero rows forwards, nothing backwards; the sort puts them last, as `vocab`.
+#include "xp_device.h"
+#include "xp_lds.h"
+#include "xp_kernels.h"
+
+#include <algorithm>
+
+namespace xp {
+
+namespace {
+
+template <typename T> constexpr int CHUNK = 16 / (int)sizeof(T);
+
+int grid_of(int64_t items, int per) {
+  return (int)std::max<int64_t>(1, std::min<int64_t>((items + per - 1) / per, (int64_t)1 << 20));
+}
+
+template <typename T>
+XP_DEV void unpack(const u32x4_t& u, float (&v)[CHUNK<T>]) {
+#pragma unroll
+  for (int i = 0; i < CHUNK<T>; ++i) {
+    if constexpr (sizeof(T) == 4) v[i] = __uint_as_float(u[i]);
+    else v[i] = __uint_as_float(i & 1 ? u[i / 2] & 0xffff0000u : u[i / 2] << 16);
+  }
+}
+
+// ---------------------------------------------------------------- lookup
+// One 16-byte chunk of one position per thread (VEC), else one element.  The
+// product is formed in fp64 and rounded once.
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void k_embed_fwd(EmbedArgs a) {
+  constexpr int C = VEC ? CHUNK<T> : 1;
+  const int64_t cpr = a.dim / C, total = a.n * cpr;
+  const T* table = (const T*)a.table;
+  T* y = (T*)a.y;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / cpr, c = (i - r * cpr) * C;
+    const int t = a.tokens[r];
+    const bool live = t >= 0 && t < a.vocab;
+    if constexpr (VEC) {
+      u32x4_t u = {0u, 0u, 0u, 0u};
+      if (live) {
+        float v[C];
+        unpack<T>(*reinterpret_cast<const u32x4_t*>(table + (int64_t)t * a.dim + c), v);
+#pragma unroll
+        for (int q = 0; q < C; ++q) v[q] = (float)((double)v[q] * a.scale);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          if constexpr (sizeof(T) == 4) u[q] = __float_as_uint(v[q]);
+          else u[q] = f32x2_to_bf16x2(v[2 * q], v[2 * q + 1]);
+        }
+      }
+      *reinterpret_cast<u32x4_t*>(y + r * a.dim + c) = u;
+    } else {
+      std_(y + r * a.dim + c, live ? ldd(table + (int64_t)t * a.dim + c) * a.scale : 0.0);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- sort
+XP_DEV uint32_t sort_key(int t, int vocab) { return (uint32_t)t < (uint32_t)vocab ? (uint32_t)t : (uint32_t)vocab; }
+
+// Few positions: a position's place is the number of positions before it in the
+// order.  256 positions per workgroup, four threads each, over all keys.
+constexpr int RANK_MAX = 8192;
+__global__ __launch_bounds__(1024) void k_embed_rank(const int32_t* __restrict__ tokens, int n, int vocab,
+                                                      uint32_t* __restrict__ keys, uint32_t* __restrict__ pos) {
+  __shared__ __align__(16) uint32_t sk[RANK_MAX];
+  __shared__ int sums[4][256];
+  const int tid = threadIdx.x, part = tid >> 8, li = tid & 255;
+  const int pad = (n + 3) / 4 * 4;
+  for (int j = tid; j < pad; j += 1024) sk[j] = j < n ? sort_key(tokens[j], vocab) : ~0u;
+  __syncthreads();
+  const int i0 = blockIdx.x * 256, i = i0 + li;
+  const uint32_t key = i < n ? sk[i] : 0u;
+  int rank = 0;
+  // before the workgroup's own positions equal keys count, after them they do not
+  for (int j = part * 4; j < pad; j += 16) {
+    const u32x4_t k = *reinterpret_cast<const u32x4_t*>(sk + j);
+    if (j < i0) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) rank += k[q] <= key;
+    } else if (j >= i0 + 256) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) rank += k[q] < key;
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) rank += k[q] < key || (k[q] == key && j + q < i);
+    }
+  }
+  sums[part][li] = rank;
+  __syncthreads();
+  if (part == 0 && i < n) {
+    const int at = sums[0][li] + sums[1][li] + sums[2][li] + sums[3][li];
+    keys[at] = key;
+    pos[at] = (uint32_t)i;
+  }
+}
+
+// More positions: a stable radix sort, eight bits of the token at a time.  A
+// workgroup takes `per` consecutive positions (a multiple of 256), each of its
+// four waves a quarter of them.
+constexpr int RADIX = 256, SORT_BLOCKS = 256;
+XP_DEV uint32_t first_key(const uint32_t* keys, const int32_t* tokens, int vocab, int64_t i) {
+  return tokens ? sort_key(tokens[i], vocab) : keys[i];
+}
+
+__global__ __launch_bounds__(256) void k_embed_hist(const uint32_t* __restrict__ keys, const int32_t* __restrict__ tokens,
+                                                    int vocab, int64_t n, int64_t per, int shift,
+                                                    uint32_t* __restrict__ hist) {
+  __shared__ uint32_t cnt[RADIX];
+  const int tid = threadIdx.x;
+  cnt[tid] = 0;
+  __syncthreads();
+  const int64_t beg = blockIdx.x * per, end = min(n, beg + per);
+  for (int64_t i = beg + tid; i < end; i += 256)
+    atomicAdd(&cnt[(first_key(keys, tokens, vocab, i) >> shift) & (RADIX - 1)], 1u);  // a count: any order
+  __syncthreads();
+  hist[(int64_t)blockIdx.x * RADIX + tid] = cnt[tid];
+}
+
+__global__ __launch_bounds__(256) void k_embed_scatter(const uint32_t* __restrict__ keys, const int32_t* __restrict__ tokens,
+                                                       int vocab, const uint32_t* __restrict__ pos, int64_t n, int64_t per,
+                                                       int shift, const uint32_t* __restrict__ hist,
+                                                       uint32_t* __restrict__ keys_out, uint32_t* __restrict__ pos_out) {
+  __shared__ uint32_t off[4][RADIX];
+  __shared__ uint32_t wsum[4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) off[w][tid] = 0;
+  __syncthreads();
+  const int64_t beg = blockIdx.x * per + wave * (per / 4), end = min(n, beg + per / 4);
+  for (int64_t i = beg + lane; i < end; i += 64)
+    atomicAdd(&off[wave][(first_key(keys, tokens, vocab, i) >> shift) & (RADIX - 1)], 1u);
+  // of digit tid: how many positions all workgroups, and the ones before this one, hold
+  uint32_t all = 0, before = 0;
+#pragma unroll 8
+  for (int b = 0; b < (int)gridDim.x; ++b) {
+    const uint32_t h = hist[(int64_t)b * RADIX + tid];
+    all += h;
+    before += b < (int)blockIdx.x ? h : 0u;
+  }
+  uint32_t scan = all;  // inclusive over the wave's digits, then the waves
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t up = __shfl_up(scan, d, 64);
+    scan += lane >= d ? up : 0u;
+  }
+  if (lane == 63) wsum[wave] = scan;
+  __syncthreads();
+  uint32_t at = scan - all + before;
+  for (int w = 0; w < wave; ++w) at += wsum[w];
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const uint32_t c = off[w][tid];
+    off[w][tid] = at;
+    at += c;
+  }
+  __syncthreads();
+  // 64 positions at a time; the lanes of one digit take their places in lane order
+  volatile uint32_t* mine = off[wave];
+  for (int64_t i0 = beg; i0 < end; i0 += 64) {
+    const int64_t i = i0 + lane;
+    const bool live = i < end;
+    const uint32_t key = live ? first_key(keys, tokens, vocab, i) : 0u;
+    const int digit = (key >> shift) & (RADIX - 1);
+    uint64_t peers = __ballot(live);
+#pragma unroll
+    for (int b = 0; b < 8; ++b) {
+      const uint64_t m = __ballot((digit >> b) & 1);
+      peers &= (digit >> b) & 1 ? m : ~m;
+    }
+    const int rank = __popcll(peers & (((uint64_t)1 << lane) - 1));
+    if (live) {
+      const uint32_t to = mine[digit] + rank;
+      keys_out[to] = key;
+      pos_out[to] = tokens ? (uint32_t)i : pos[i];
+    }
+    __builtin_amdgcn_wave_barrier();
+    if (live && rank == 0) mine[digit] = mine[digit] + __popcll(peers);
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// ---------------------------------------------------------------- gradient
+// A wave takes `span` consecutive sorted positions and 64 chunks of columns, and
+// adds the rows of each run of equal tokens in fp64.  Runs inside the span go
+// straight into the accumulator; what a run has in this span that started before
+// it (part 0) or goes on behind it (part 1) is left as an fp32 partial for
+// k_embed_join; a run that does both is part 0.  Rows are taken GROUP at a
+// time, with the accumulators' rows that they end in, so that the loads of a
+// group are in flight together.
+constexpr int GROUP = 8;
+template <typename T, bool VEC>
+__global__ __launch_bounds__(64) void k_embed_bwd(EmbedArgs a, const uint32_t* __restrict__ keys,
+                                                  const uint32_t* __restrict__ pos, int span, float* __restrict__ part) {
+  constexpr int C = VEC ? CHUNK<T> : 1;
+  const int64_t beg = (int64_t)blockIdx.x * span, end = min(a.n, beg + span);
+  const int64_t col = ((int64_t)blockIdx.y * 64 + threadIdx.x) * C;
+  if (col >= a.dim) return;
+  const T* dy = (const T*)a.dy + col;
+  float* grad = a.grad + col;
+  double acc[C];
+#pragma unroll
+  for (int q = 0; q < C; ++q) acc[q] = 0.0;
+  bool head = beg > 0 && keys[beg - 1] == keys[beg];  // the present run started before the span
+  for (int64_t g = beg; g < end; g += GROUP) {
+    uint32_t key[GROUP];
+    bool last[GROUP], whole[GROUP];
+    float v[GROUP][C], o[GROUP][C];
+    bool h = head;
+#pragma unroll
+    for (int j = 0; j < GROUP; ++j) {
+      const int64_t i = g + j;
+      const bool in = i < end;
+      key[j] = in ? keys[i] : (uint32_t)a.vocab;
+      const bool live = in && key[j] < (uint32_t)a.vocab;
+      const bool more = i + 1 < a.n && keys[min(i + 1, a.n - 1)] == key[j];  // the run goes on behind i
+      last[j] = live && (!more || i + 1 == end);
+      whole[j] = last[j] && !more && !h;
+      if (in && !more) h = false;
+      if (!live) continue;
+      const T* row = dy + (int64_t)pos[i] * a.dim;
+      if constexpr (VEC) unpack<T>(*reinterpret_cast<const u32x4_t*>(row), v[j]);
+      else v[j][0] = (float)ldd(row);
+      if (whole[j]) {
+        const float* gr = grad + (int64_t)key[j] * a.dim;
+#pragma unroll
+        for (int q = 0; q < C; ++q) o[j][q] = gr[q];
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < GROUP; ++j) {
+      if (key[j] >= (uint32_t)a.vocab) continue;
+#pragma unroll
+      for (int q = 0; q < C; ++q) acc[q] += (double)v[j][q];
+      if (!last[j]) continue;
+      if (whole[j]) {
+        float* gr = grad + (int64_t)key[j] * a.dim;
+#pragma unroll
+        for (int q = 0; q < C; ++q) gr[q] = (float)((double)o[j][q] + a.scale * acc[q]);
+      } else {
+        // from before the span, or (whole runs aside) on behind it
+        float* p = part + ((int64_t)blockIdx.x * 2 + (head ? 0 : 1)) * a.dim + col;
+#pragma unroll
+        for (int q = 0; q < C; ++q) p[q] = (float)acc[q];
+      }
+      head = false;
+#pragma unroll
+      for (int q = 0; q < C; ++q) acc[q] = 0.0;
+    }
+  }
+}
+
+// The runs that pass a span's end: the span that a run starts in adds its
+// partials.  Eight groups of 128 threads (one column each) take consecutive
+// parts of the run's spans, and the groups are added in order.
+__global__ __launch_bounds__(1024) void k_embed_join(EmbedArgs a, const uint32_t* __restrict__ keys, int span,
+                                                      const float* __restrict__ part) {
+  __shared__ double sums[8][128];
+  const int64_t c = blockIdx.x, beg = c * span, next = beg + span;
+  if (next >= a.n) return;
+  const uint32_t key = keys[next - 1];
+  if (key >= (uint32_t)a.vocab || keys[next] != key) return;           // no run passes the end
+  if (beg > 0 && keys[beg] == key && keys[beg - 1] == key) return;      // it started before this span
+  const int64_t spans = (a.n + span - 1) / span;
+  // the run's last span: steps that double, then back
+  int64_t lo = c + 1, step = 1;
+  while (lo + step < spans && keys[(lo + step) * span] == key) {
+    lo += step;
+    step *= 2;
+  }
+  for (; step > 0; step /= 2)
+    if (lo + step < spans && keys[(lo + step) * span] == key) lo += step;
+  const int64_t cnt = lo - c;  // spans behind the first one
+  const int g = threadIdx.x >> 7, lc = threadIdx.x & 127;
+  const int64_t per = (cnt + 7) / 8, s0 = c + 1 + g * per, s1 = min(lo + 1, s0 + per);
+  for (int64_t col0 = (int64_t)blockIdx.y * 128; col0 < a.dim; col0 += (int64_t)gridDim.y * 128) {
+    const int64_t col = col0 + lc;
+    double t = 0.0;
+    if (col < a.dim) {
+      if (g == 0) t = (double)part[(c * 2 + 1) * a.dim + col];
+#pragma unroll 8
+      for (int64_t s = s0; s < s1; ++s) t += (double)part[s * 2 * a.dim + col];
+    }
+    sums[g][lc] = t;
+    __syncthreads();
+    if (g == 0 && col < a.dim) {
+#pragma unroll
+      for (int q = 1; q < 8; ++q) t += sums[q][lc];
+      float* o = a.grad + (int64_t)key * a.dim + col;
+      *o = (float)((double)*o + a.scale * t);
+    }
+    __syncthreads();
+  }
+}
+
+size_t up256(size_t b) { return (b + 255) / 256 * 256; }
+bool aligned(const void* p, int64_t dim, int chunk) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && dim % chunk == 0; }
+
+// sorted positions per wave of the gradient: enough waves for small calls, few partials for large ones
+int span_of(int64_t n) { return n >= 16384 ? 64 : n >= 2048 ? 16 : 8; }
+
+int64_t sort_per(int64_t n) { return std::max<int64_t>(1024, ((n + SORT_BLOCKS - 1) / SORT_BLOCKS + 255) / 256 * 256); }
+
+struct Layout {
+  size_t keys[2], pos[2], hist, part, bytes;
+};
+Layout layout(int64_t n, int64_t dim) {
+  Layout l{};
+  size_t off = 0;
+  auto take = [&](size_t b) {
+    const size_t at = off;
+    off += up256(b);
+    return at;
+  };
+  const int sides = n <= RANK_MAX ? 1 : 2;
+  for (int s = 0; s < sides; ++s) {
+    l.keys[s] = take((size_t)n * 4);
+    l.pos[s] = take((size_t)n * 4);
+  }
+  if (n > RANK_MAX) l.hist = take((size_t)SORT_BLOCKS * RADIX * 4);
+  l.part = take((size_t)((n + span_of(n) - 1) / span_of(n)) * 2 * dim * sizeof(float));
+  l.bytes = off;
+  return l;
+}
+
+}  // namespace
+
+hipError_t launch_embed_fwd(int dtype, const EmbedArgs& a, hipStream_t s) {
+  if (a.n <= 0 || a.dim <= 0) return hipSuccess;
+  const int es = dtype == DT_BF16 ? 2 : 4, chunk = 16 / es;
+  const bool vec = aligned(a.table, a.dim, chunk) && aligned(a.y, a.dim, chunk);
+  const dim3 grid(grid_of(a.n * (vec ? a.dim / chunk : a.dim), 256));
+  const double bytes = 2.0 * a.n * a.dim * es;
+  if (dtype == DT_BF16) {
+    if (vec) XP_LAUNCH("k_embed_fwd<bf16>", bytes, (k_embed_fwd<bf16_t, true>), grid, dim3(256), 0, s, a);
+    else XP_LAUNCH("k_embed_fwd<bf16>", bytes, (k_embed_fwd<bf16_t, false>), grid, dim3(256), 0, s, a);
+  } else {
+    if (vec) XP_LAUNCH("k_embed_fwd<f32>", bytes, (k_embed_fwd<float, true>), grid, dim3(256), 0, s, a);
+    else XP_LAUNCH("k_embed_fwd<f32>", bytes, (k_embed_fwd<float, false>), grid, dim3(256), 0, s, a);
+  }
+  return hipGetLastError();
+}
+
+size_t embed_bwd_bytes(int64_t n, int64_t dim) { return n <= 0 ? 0 : layout(n, dim).bytes; }
+
+hipError_t launch_embed_bwd(int dtype, const EmbedArgs& a, void* workspace, hipStream_t s) {
+  if (a.n <= 0 || a.dim <= 0) return hipSuccess;
+  char* ws = (char*)workspace;
+  const Layout l = layout(a.n, a.dim);
+  uint32_t *keys = (uint32_t*)(ws + l.keys[0]), *pos = (uint32_t*)(ws + l.pos[0]);
+  hipError_t e;
+  if (a.n <= RANK_MAX) {
+    XP_LAUNCH("k_embed_rank", 12.0 * a.n, k_embed_rank, dim3((unsigned)((a.n + 255) / 256)), dim3(1024), 0, s, a.tokens,
+              (int)a.n, a.vocab, keys, pos);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  } else {
+    int bits = 1;  // of the largest key, vocab
+    while ((int64_t)a.vocab >> bits) ++bits;
+    const int64_t per = sort_per(a.n);
+    const unsigned blocks = (unsigned)((a.n + per - 1) / per);
+    uint32_t* hist = (uint32_t*)(ws + l.hist);
+    int side = 0;
+    for (int shift = 0; shift < bits; shift += 8) {
+      const int32_t* tokens = shift == 0 ? a.tokens : nullptr;  // the first pass reads the tokens themselves
+      XP_LAUNCH("k_embed_hist", 4.0 * a.n, k_embed_hist, dim3(blocks), dim3(256), 0, s, keys, tokens, a.vocab, a.n, per,
+                shift, hist);
+      uint32_t *ko = (uint32_t*)(ws + l.keys[1 - side]), *po = (uint32_t*)(ws + l.pos[1 - side]);
+      XP_LAUNCH("k_embed_scatter", 16.0 * a.n, k_embed_scatter, dim3(blocks), dim3(256), 0, s, keys, tokens, a.vocab, pos,
+                a.n, per, shift, hist, ko, po);
+      e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      side = 1 - side;
+      keys = ko;
+      pos = po;
+    }
+  }
+  const int es = dtype == DT_BF16 ? 2 : 4, chunk = 16 / es, span = span_of(a.n);
+  // (the accumulator's rows need no alignment of their own: their elements are 4 bytes wide)
+  const bool vec = aligned(a.dy, a.dim, chunk);
+  const unsigned spans = (unsigned)((a.n + span - 1) / span);
+  const int64_t cols = vec ? a.dim / chunk : a.dim;
+  const dim3 grid(spans, (unsigned)((cols + 63) / 64));
+  float* part = (float*)(ws + l.part);
+  const double bytes = (double)a.n * a.dim * es;
+  if (dtype == DT_BF16) {
+    if (vec) XP_LAUNCH("k_embed_bwd<bf16>", bytes, (k_embed_bwd<bf16_t, true>), grid, dim3(64), 0, s, a, keys, pos, span, part);
+    else XP_LAUNCH("k_embed_bwd<bf16>", bytes, (k_embed_bwd<bf16_t, false>), grid, dim3(64), 0, s, a, keys, pos, span, part);
+  } else {
+    if (vec) XP_LAUNCH("k_embed_bwd<f32>", bytes, (k_embed_bwd<float, true>), grid, dim3(64), 0, s, a, keys, pos, span, part);
+    else XP_LAUNCH("k_embed_bwd<f32>", bytes, (k_embed_bwd<float, false>), grid, dim3(64), 0, s, a, keys, pos, span, part);
+  }
+  e = hipGetLastError();
+  if (e != hipSuccess || spans < 2) return e;
+  XP_LAUNCH("k_embed_join", 0.0, k_embed_join, dim3(spans - 1, (unsigned)std::min<int64_t>(8, (a.dim + 127) / 128)),
+            dim3(1024), 0, s, a, keys, span, part);
+  return hipGetLastError();
+}
+
+}  // namespace xp

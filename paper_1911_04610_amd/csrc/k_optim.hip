@@ -116,12 +116,24 @@ XP_DEV AdamElem adam1(float w, float m, float v, float g, const AdamCoef& a) {
   return AdamElem{(float)wn, (float)mn, (float)vn};
 }
 
+// The gradient times the clipping coefficient, rounded to fp32: what a pass that
+// scaled G in place would leave there (CLIP false: the gradient itself).
+template <bool CLIP>
+XP_DEV float clipped(float g, float coef) { return CLIP ? g * coef : g; }
+template <bool CLIP>
+XP_DEV float4 clipped(float4 g, float coef) {
+  return make_float4(clipped<CLIP>(g.x, coef), clipped<CLIP>(g.y, coef), clipped<CLIP>(g.z, coef), clipped<CLIP>(g.w, coef));
+}
+
+template <bool CLIP>
 __global__ __launch_bounds__(STREAM_BLOCK) void k_adam(float* __restrict__ W, float* __restrict__ m,
                                                float* __restrict__ v, float* __restrict__ G,
                                                int64_t n, AdamCoef a, int zero_grad,
                                                float* __restrict__ pf, bf16_t* __restrict__ pf_bf,
                                                PredCoef cf, float* __restrict__ pb,
-                                               bf16_t* __restrict__ pb_bf, PredCoef cb) {
+                                               bf16_t* __restrict__ pb_bf, PredCoef cb,
+                                               const float* __restrict__ clip) {
+  const float coef = CLIP ? *clip : 1.f;
   const int64_t nv = n >> 2;
   const int64_t stride = (int64_t)gridDim.x * blockDim.x;
   const bool shared = cf.c1 == cb.c1 && cf.c2 == cb.c2 && cf.eps == cb.eps && cf.kind == cb.kind;
@@ -130,7 +142,7 @@ __global__ __launch_bounds__(STREAM_BLOCK) void k_adam(float* __restrict__ W, fl
   float4* v4 = reinterpret_cast<float4*>(v);
   float4* G4 = reinterpret_cast<float4*>(G);
   for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < nv; i += stride) {
-    float4 w = ldnt(W4 + i), mm = ldnt(m4 + i), vv = ldnt(v4 + i), g = ldnt(G4 + i);
+    float4 w = ldnt(W4 + i), mm = ldnt(m4 + i), vv = ldnt(v4 + i), g = clipped<CLIP>(ldnt(G4 + i), coef);
     AdamElem e0 = adam1(w.x, mm.x, vv.x, g.x, a);
     AdamElem e1 = adam1(w.y, mm.y, vv.y, g.y, a);
     AdamElem e2 = adam1(w.z, mm.z, vv.z, g.z, a);
@@ -176,7 +188,7 @@ __global__ __launch_bounds__(STREAM_BLOCK) void k_adam(float* __restrict__ W, fl
   }
   int64_t t = (nv << 2) + (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
   if (t < n) {
-    AdamElem e = adam1(W[t], m[t], v[t], G[t], a);
+    AdamElem e = adam1(W[t], m[t], v[t], clipped<CLIP>(G[t], coef), a);
     W[t] = e.w;
     m[t] = e.m;
     v[t] = e.v;
@@ -221,15 +233,16 @@ XP_DEV RuleElem rule1(float w, float b, float q, float m, float v, float gr, con
   return RuleElem{(float)wn, (float)bn, (float)qn, (float)mn, (float)vn};
 }
 
-template <int RULE>
+template <int RULE, bool CLIP>
 __global__ __launch_bounds__(STREAM_BLOCK) void k_rule(float* __restrict__ W, float* __restrict__ B,
                                               float* __restrict__ Q, float* __restrict__ m,
                                               float* __restrict__ v, float* __restrict__ G, int64_t n,
                                               RuleCoef c, int zero_grad, float* __restrict__ pf,
                                               bf16_t* __restrict__ pf_bf, PredCoef cf,
                                               float* __restrict__ pb, bf16_t* __restrict__ pb_bf,
-                                              PredCoef cb) {
+                                              PredCoef cb, const float* __restrict__ clip) {
   constexpr bool RMS = RULE == RULE_RMSPROP;
+  const float coef = CLIP ? *clip : 1.f;
   const int64_t nv = n >> 2;
   const int64_t stride = (int64_t)gridDim.x * blockDim.x;
   float4* W4 = reinterpret_cast<float4*>(W);
@@ -270,7 +283,8 @@ __global__ __launch_bounds__(STREAM_BLOCK) void k_rule(float* __restrict__ W, fl
     }
   };
   for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < nv; i += stride) {
-    const float4 w = ldnt(W4 + i), b = ldnt(B4 + i), mm = ldnt(m4 + i), vv = ldnt(v4 + i), g = ldnt(G4 + i);
+    const float4 w = ldnt(W4 + i), b = ldnt(B4 + i), mm = ldnt(m4 + i), vv = ldnt(v4 + i),
+                 g = clipped<CLIP>(ldnt(G4 + i), coef);
     const float4 q = RMS ? ldnt(Q4 + i) : make_float4(0.f, 0.f, 0.f, 0.f);
     const RuleElem e[4] = {rule1<RULE>(w.x, b.x, q.x, mm.x, vv.x, g.x, c),
                            rule1<RULE>(w.y, b.y, q.y, mm.y, vv.y, g.y, c),
@@ -286,7 +300,7 @@ __global__ __launch_bounds__(STREAM_BLOCK) void k_rule(float* __restrict__ W, fl
   }
   const int64_t t = (nv << 2) + (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
   if (t < n) {
-    const RuleElem e = rule1<RULE>(W[t], B[t], RMS ? Q[t] : 0.f, m[t], v[t], G[t], c);
+    const RuleElem e = rule1<RULE>(W[t], B[t], RMS ? Q[t] : 0.f, m[t], v[t], clipped<CLIP>(G[t], coef), c);
     W[t] = e.w;
     B[t] = e.b;
     if (RMS) Q[t] = e.q;
@@ -330,28 +344,34 @@ hipError_t launch_predict(const float* W, const float* m, const float* v, float*
 
 hipError_t launch_adam(float* W, float* m, float* v, float* G, int64_t n, const AdamCoef& a,
                        int zero_grad, float* pf, bf16_t* pf_bf, const PredCoef& cf, float* pb,
-                       bf16_t* pb_bf, const PredCoef& cb, hipStream_t s) {
+                       bf16_t* pb_bf, const PredCoef& cb, hipStream_t s, const float* clip) {
   if (n <= 0) return hipSuccess;
   double bytes = (double)n * (28 + (zero_grad ? 4 : 0) + (pf ? 4 : 0) + (pb ? 4 : 0) +
                               (pf_bf ? 2 : 0) + (pb_bf ? 2 : 0));
-  XP_LAUNCH("k_adam", bytes, k_adam, dim3(stream_grid(n)), dim3(STREAM_BLOCK), 0, s, W, m, v, G, n, a, zero_grad,
-            pf, pf_bf, cf, pb, pb_bf, cb);
+  if (clip)
+    XP_LAUNCH("k_adam<clip>", bytes, k_adam<true>, dim3(stream_grid(n)), dim3(STREAM_BLOCK), 0, s, W, m, v, G, n, a,
+              zero_grad, pf, pf_bf, cf, pb, pb_bf, cb, clip);
+  else
+    XP_LAUNCH("k_adam", bytes, k_adam<false>, dim3(stream_grid(n)), dim3(STREAM_BLOCK), 0, s, W, m, v, G, n, a,
+              zero_grad, pf, pf_bf, cf, pb, pb_bf, cb, clip);
   return hipGetLastError();
 }
 
 hipError_t launch_rule(int rule, float* W, float* B, float* Q, float* m, float* v, float* G, int64_t n,
                        const RuleCoef& c, int zero_grad, float* pf, bf16_t* pf_bf, const PredCoef& cf,
-                       float* pb, bf16_t* pb_bf, const PredCoef& cb, hipStream_t s) {
+                       float* pb, bf16_t* pb_bf, const PredCoef& cb, hipStream_t s, const float* clip) {
   if (n <= 0) return hipSuccess;
   const bool rms = rule == RULE_RMSPROP;
   double bytes = (double)n * ((rms ? 44 : 36) + (zero_grad ? 4 : 0) + (pf ? 4 : 0) + (pb ? 4 : 0) +
                               (pf_bf ? 2 : 0) + (pb_bf ? 2 : 0));
-  if (rms)
-    XP_LAUNCH("k_rule<rmsprop>", bytes, k_rule<RULE_RMSPROP>, dim3(stream_grid(n)), dim3(STREAM_BLOCK), 0, s, W, B, Q,
-              m, v, G, n, c, zero_grad, pf, pf_bf, cf, pb, pb_bf, cb);
-  else
-    XP_LAUNCH("k_rule<momentum_sgd>", bytes, k_rule<RULE_MOMENTUM_SGD>, dim3(stream_grid(n)), dim3(STREAM_BLOCK), 0, s,
-              W, B, Q, m, v, G, n, c, zero_grad, pf, pf_bf, cf, pb, pb_bf, cb);
+  auto go = [&](auto kernel, const char* name) {
+    XP_LAUNCH(name, bytes, kernel, dim3(stream_grid(n)), dim3(STREAM_BLOCK), 0, s, W, B, Q, m, v, G, n, c, zero_grad, pf,
+              pf_bf, cf, pb, pb_bf, cb, clip);
+  };
+  if (rms && clip) go(k_rule<RULE_RMSPROP, true>, "k_rule<rmsprop,clip>");
+  else if (rms) go(k_rule<RULE_RMSPROP, false>, "k_rule<rmsprop>");
+  else if (clip) go(k_rule<RULE_MOMENTUM_SGD, true>, "k_rule<momentum_sgd,clip>");
+  else go(k_rule<RULE_MOMENTUM_SGD, false>, "k_rule<momentum_sgd>");
   return hipGetLastError();
 }
 

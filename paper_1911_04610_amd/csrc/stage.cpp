@@ -29,26 +29,20 @@
 #include <string>
 #include <vector>
 
-#include "../../include/xpipe.h"
-#include "xp_kernels.h"
+#include "xp_host.h"
 
 using namespace xp;
 
 namespace {
-
 thread_local std::string g_err;
+}
 
-xpipe_status fail(xpipe_status s, const std::string& msg) {
+xpipe_status xp::fail(xpipe_status s, const std::string& msg) {
   g_err = msg;
   return s;
 }
 
-#define XP_HIP(call)                                                                     \
-  do {                                                                                   \
-    hipError_t e_ = (call);                                                              \
-    if (e_ != hipSuccess)                                                                \
-      return fail(XPIPE_EHIP, std::string(#call) + ": " + hipGetErrorString(e_));        \
-  } while (0)
+namespace {
 
 constexpr int64_t PARAM_ALIGN = 64;  // elements
 constexpr size_t WS_ALIGN = 256;     // bytes
@@ -199,6 +193,11 @@ struct xpipe_stage {
   bool pred_valid[2] = {false, false};
   bool wd_valid = false;
   int64_t bwd_since_step = 0;
+  // clipping of the updates (xpipe_stage_set_clip): {norm, coefficient} on the
+  // device; with a positive clip_max the update computes them first
+  float* clip = nullptr;
+  double clip_max = 0.0;
+  double* clip_part = nullptr;
   // timing: hipEvents around every launch, aggregated per kernel
   struct Hook : xp::LaunchHook {
     xpipe_stage* st = nullptr;
@@ -1876,8 +1875,6 @@ xpipe_status refresh_flipped(xpipe_stage* st) {
   return XPIPE_OK;
 }
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
-
 void drop_graphs(xpipe_stage* st) {
   for (auto& g : st->pass_graphs) (void)hipGraphExecDestroy(g.exec);
   st->pass_graphs.clear();
@@ -2352,6 +2349,36 @@ xpipe_status xpipe_stage_set_graphs(xpipe_stage_t st, int32_t enable) {
   return XPIPE_OK;
 }
 
+xpipe_status xpipe_stage_set_clip(xpipe_stage_t st, double max_norm, float* norm_coef, void* workspace,
+                                  size_t workspace_bytes) {
+  if (!st) return fail(XPIPE_EINVAL, "null stage");
+  if (!norm_coef) {
+    st->clip = nullptr;
+    return XPIPE_OK;
+  }
+  if (!(max_norm >= 0)) return fail(XPIPE_EINVAL, "max_norm must be >= 0");
+  if ((reinterpret_cast<uintptr_t>(norm_coef) & 3) != 0) return fail(XPIPE_EINVAL, "norm_coef must be 4-byte aligned");
+  if (max_norm > 0) {
+    if (!workspace) return fail(XPIPE_EINVAL, "null workspace");
+    if ((reinterpret_cast<uintptr_t>(workspace) & 7) != 0) return fail(XPIPE_EINVAL, "workspace must be 8-byte aligned");
+    if (workspace_bytes < (size_t)norm_blocks(st->P) * sizeof(double)) return fail(XPIPE_EINVAL, "workspace too small");
+  }
+  st->clip = norm_coef;
+  st->clip_max = max_norm;
+  st->clip_part = (double*)workspace;
+  return XPIPE_OK;
+}
+
+// the coefficient that the update is to multiply the gradient by, or null; with
+// a norm of its own, enqueues it
+static xpipe_status stage_clip(xpipe_stage* st, const float** coef) {
+  *coef = nullptr;
+  if (!st->clip) return XPIPE_OK;
+  if (st->clip_max > 0) XP_HIP(grad_norm_flat(st->grad, st->P, st->clip_max, st->clip_part, st->clip, st->stream));
+  *coef = st->clip + 1;
+  return XPIPE_OK;
+}
+
 xpipe_status xpipe_adam_step(xpipe_stage_t st, const xpipe_hparams* hp, int32_t s_fwd_next,
                              int32_t s_bwd_next, int32_t emit_pred) {
   if (!st) return fail(XPIPE_EINVAL, "null stage");
@@ -2372,10 +2399,10 @@ xpipe_status xpipe_adam_step(xpipe_stage_t st, const xpipe_hparams* hp, int32_t 
     fb = (bf16_t*)(st->wws + st->bf_b_off);
   }
   if (emit_pred) XP_OK(wait_forwards(st));
-  {
-    XP_HIP(launch_adam(st->W, st->m, st->v, st->grad, st->P, a, 1, emit_pred ? st->wpf : nullptr, ff, cf,
-                       emit_pred ? st->wpb : nullptr, fb, cb, st->stream));
-  }
+  const float* clip;
+  XP_OK(stage_clip(st, &clip));
+  XP_HIP(launch_adam(st->W, st->m, st->v, st->grad, st->P, a, 1, emit_pred ? st->wpf : nullptr, ff, cf,
+                     emit_pred ? st->wpb : nullptr, fb, cb, st->stream, clip));
   st->bwd_since_step = 0;
   if (keep) return XPIPE_OK;  // the cached predictions (and what derives from them) stay
   st->pred_valid[0] = st->pred_valid[1] = emit_pred != 0;
@@ -2413,8 +2440,10 @@ xpipe_status xpipe_rule_step(xpipe_stage_t st, const xpipe_rule_hparams* rp, con
     fb = (bf16_t*)(st->wws + st->bf_b_off);
   }
   if (emit_pred) XP_OK(wait_forwards(st));
+  const float* clip;
+  XP_OK(stage_clip(st, &clip));
   XP_HIP(launch_rule(rp->rule, st->W, buf, sq, st->m, st->v, st->grad, st->P, rule_coef(rp, hp), 1,
-                     emit_pred ? st->wpf : nullptr, ff, cf, emit_pred ? st->wpb : nullptr, fb, cb, st->stream));
+                     emit_pred ? st->wpf : nullptr, ff, cf, emit_pred ? st->wpb : nullptr, fb, cb, st->stream, clip));
   st->bwd_since_step = 0;
   if (keep) return XPIPE_OK;
   st->pred_valid[0] = st->pred_valid[1] = emit_pred != 0;
@@ -2466,9 +2495,9 @@ xpipe_status xpipe_predict_flat(const float* W, const float* m, const float* v, 
   return XPIPE_OK;
 }
 
-xpipe_status xpipe_adam_flat(float* W, float* m, float* v, float* G, int64_t n, const xpipe_hparams* hp,
-                             int32_t zero_grad, float* pred_fwd, int32_t s_fwd, float* pred_bwd, int32_t s_bwd,
-                             void* hip_stream) {
+static xpipe_status adam_flat(float* W, float* m, float* v, float* G, int64_t n, const xpipe_hparams* hp,
+                              int32_t zero_grad, float* pred_fwd, int32_t s_fwd, float* pred_bwd, int32_t s_bwd,
+                              const float* norm_coef, void* hip_stream) {
   if (n < 0) return fail(XPIPE_EINVAL, "negative length");
   xpipe_status hs = check_hp(hp);
   if (hs != XPIPE_OK) return hs;
@@ -2479,14 +2508,28 @@ xpipe_status xpipe_adam_flat(float* W, float* m, float* v, float* G, int64_t n, 
       (pred_fwd && !aligned16(pred_fwd)) || (pred_bwd && !aligned16(pred_bwd)))
     return fail(XPIPE_EINVAL, "buffers must be 16-byte aligned");
   XP_HIP(launch_adam(W, m, v, G, n, adam_coef(hp), zero_grad, pred_fwd, nullptr, pred_coef(hp, hp->t + 1, s_fwd),
-                     pred_bwd, nullptr, pred_coef(hp, hp->t + 1, s_bwd), (hipStream_t)hip_stream));
+                     pred_bwd, nullptr, pred_coef(hp, hp->t + 1, s_bwd), (hipStream_t)hip_stream,
+                     norm_coef ? norm_coef + 1 : nullptr));
   return XPIPE_OK;
 }
 
-xpipe_status xpipe_rule_flat(float* W, float* buf, float* sq, float* m, float* v, float* G, int64_t n,
-                             const xpipe_rule_hparams* rp, const xpipe_hparams* hp, int32_t zero_grad,
-                             float* pred_fwd, int32_t s_fwd, float* pred_bwd, int32_t s_bwd,
+xpipe_status xpipe_adam_flat(float* W, float* m, float* v, float* G, int64_t n, const xpipe_hparams* hp,
+                             int32_t zero_grad, float* pred_fwd, int32_t s_fwd, float* pred_bwd, int32_t s_bwd,
                              void* hip_stream) {
+  return adam_flat(W, m, v, G, n, hp, zero_grad, pred_fwd, s_fwd, pred_bwd, s_bwd, nullptr, hip_stream);
+}
+
+xpipe_status xpipe_adam_flat_clipped(float* W, float* m, float* v, float* G, int64_t n, const xpipe_hparams* hp,
+                                     int32_t zero_grad, float* pred_fwd, int32_t s_fwd, float* pred_bwd,
+                                     int32_t s_bwd, const float* norm_coef, void* hip_stream) {
+  if (!norm_coef) return fail(XPIPE_EINVAL, "null norm_coef");
+  return adam_flat(W, m, v, G, n, hp, zero_grad, pred_fwd, s_fwd, pred_bwd, s_bwd, norm_coef, hip_stream);
+}
+
+static xpipe_status rule_flat(float* W, float* buf, float* sq, float* m, float* v, float* G, int64_t n,
+                              const xpipe_rule_hparams* rp, const xpipe_hparams* hp, int32_t zero_grad,
+                              float* pred_fwd, int32_t s_fwd, float* pred_bwd, int32_t s_bwd,
+                              const float* norm_coef, void* hip_stream) {
   if (n < 0) return fail(XPIPE_EINVAL, "negative length");
   xpipe_status hs = check_hp(hp);
   if (hs != XPIPE_OK) return hs;
@@ -2500,8 +2543,23 @@ xpipe_status xpipe_rule_flat(float* W, float* buf, float* sq, float* m, float* v
     return fail(XPIPE_EINVAL, "buffers must be 16-byte aligned");
   XP_HIP(launch_rule(rp->rule, W, buf, sq, m, v, G, n, rule_coef(rp, hp), zero_grad, pred_fwd, nullptr,
                      pred_coef(hp, hp->t + 1, s_fwd), pred_bwd, nullptr, pred_coef(hp, hp->t + 1, s_bwd),
-                     (hipStream_t)hip_stream));
+                     (hipStream_t)hip_stream, norm_coef ? norm_coef + 1 : nullptr));
   return XPIPE_OK;
+}
+
+xpipe_status xpipe_rule_flat(float* W, float* buf, float* sq, float* m, float* v, float* G, int64_t n,
+                             const xpipe_rule_hparams* rp, const xpipe_hparams* hp, int32_t zero_grad,
+                             float* pred_fwd, int32_t s_fwd, float* pred_bwd, int32_t s_bwd,
+                             void* hip_stream) {
+  return rule_flat(W, buf, sq, m, v, G, n, rp, hp, zero_grad, pred_fwd, s_fwd, pred_bwd, s_bwd, nullptr, hip_stream);
+}
+
+xpipe_status xpipe_rule_flat_clipped(float* W, float* buf, float* sq, float* m, float* v, float* G, int64_t n,
+                                     const xpipe_rule_hparams* rp, const xpipe_hparams* hp, int32_t zero_grad,
+                                     float* pred_fwd, int32_t s_fwd, float* pred_bwd, int32_t s_bwd,
+                                     const float* norm_coef, void* hip_stream) {
+  if (!norm_coef) return fail(XPIPE_EINVAL, "null norm_coef");
+  return rule_flat(W, buf, sq, m, v, G, n, rp, hp, zero_grad, pred_fwd, s_fwd, pred_bwd, s_bwd, norm_coef, hip_stream);
 }
 
 xpipe_status xpipe_probe_copy(const void* src, void* dst, int64_t bytes, void* hip_stream) {

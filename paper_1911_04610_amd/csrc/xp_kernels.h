@@ -60,10 +60,11 @@ hipError_t launch_predict(const float* W, const float* m, const float* v, float*
                           bf16_t* out_bf, int64_t n, const PredCoef& c, hipStream_t s);
 hipError_t launch_rule(int rule, float* W, float* B, float* Q, float* m, float* v, float* G, int64_t n,
                        const RuleCoef& c, int zero_grad, float* pf, bf16_t* pf_bf, const PredCoef& cf,
-                       float* pb, bf16_t* pb_bf, const PredCoef& cb, hipStream_t s);
+                       float* pb, bf16_t* pb_bf, const PredCoef& cb, hipStream_t s, const float* clip = nullptr);
+// clip (optional, device): the gradient is multiplied by *clip, rounded to fp32, before anything reads it
 hipError_t launch_adam(float* W, float* m, float* v, float* G, int64_t n, const AdamCoef& a,
                        int zero_grad, float* pf, bf16_t* pf_bf, const PredCoef& cf, float* pb,
-                       bf16_t* pb_bf, const PredCoef& cb, hipStream_t s);
+                       bf16_t* pb_bf, const PredCoef& cb, hipStream_t s, const float* clip = nullptr);
 
 // ---------------------------------------------------------------- weight gather
 // Copies nseg blocks of elements (storage dtype) back to back into dst: the
@@ -315,6 +316,75 @@ struct CeArgs {
   void* dz; int lddz;              // backward: dlogits (may be null)
 };
 hipError_t launch_softmax_ce(int dtype, const CeArgs& a, hipStream_t s);
+
+// ---------------------------------------------------------------- linear
+// One product of a linear layer outside a stage: P[m][n] = sum_k A(m, k) B(n, k)
+// with fp32 sums, then by `epi`:
+//   LIN_FWD   A = x [M][K], B = W [N][K]: z = P + bias; z_out = z (optional);
+//             y = act(z) + res (optional)
+//   LIN_DATA  A = dz [M][K], B(n, k) = W[k][n]: y = P act'(z_in) + res (optional);
+//             act LIN_NONE: no z_in
+//   LIN_GRAD  A(m, k) = dz[k][m], B(n, k) = x[k][n]: grad[m][n] += P (optional
+//             grad_b[m] += sum_k A(m, k)); grad has rows of N
+// Operands and y, z, res in the storage dtype, rows of lda, ldb, ... elements.
+enum { LIN_FWD = 0, LIN_DATA = 1, LIN_GRAD = 2 };
+enum { LIN_NONE = 0, LIN_RELU = 1, LIN_GELU = 2, LIN_SILU = 3 };
+struct LinearArgs {
+  int epi, act;
+  int64_t M;
+  int N, K;
+  const void* A; int64_t lda;
+  const void* B; int64_t ldb;
+  const float* bias;               // LIN_FWD, optional
+  const void* res; int64_t ldr;    // optional
+  const void* z_in; void* z_out; int64_t ldz;
+  void* y; int64_t ldy;
+  float* grad; float* grad_b;      // LIN_GRAD
+  // set by the launcher: the reduction's parts (kper indices each), their sums
+  // [splits][M][ldpart], and whether every row allows 16-byte accesses
+  int splits; int64_t kper; int64_t ldpart;
+  float* part; double* part_b;
+  int vec;
+};
+struct LinearPlan {
+  int bm, splits;
+  int64_t kper, ldpart;
+  bool pack_a, pack_b;
+  int a_cols, b_cols;
+  size_t a_off, b_off, part_off, part_b_off, bytes;  // in the workspace
+};
+LinearPlan linear_plan(int dtype, const LinearArgs& a);
+hipError_t launch_linear(int dtype, const LinearArgs& a, void* workspace, hipStream_t s);
+// dz = dy act'(z) over n elements
+hipError_t launch_act_bwd(int dtype, const void* dy, const void* z, void* dz, int64_t n, int act, hipStream_t s);
+
+// ---------------------------------------------------------------- embedding
+struct EmbedArgs {
+  int64_t n, dim;          // positions, columns
+  int vocab;
+  const int32_t* tokens;   // [n]; outside [0, vocab): padding
+  double scale;
+  const void* table; void* y;        // forward: y[i] = scale table[tokens[i]]
+  const void* dy; float* grad;       // backward: grad[tokens[i]] += scale dy[i]
+};
+hipError_t launch_embed_fwd(int dtype, const EmbedArgs& a, hipStream_t s);
+size_t embed_bwd_bytes(int64_t n, int64_t dim);
+hipError_t launch_embed_bwd(int dtype, const EmbedArgs& a, void* workspace, hipStream_t s);
+
+// ---------------------------------------------------------------- gradient norm
+// One launch takes up to NORM_BATCH tensors (their list travels as the kernel's
+// arguments, 3.9 KB): workgroups first[i] .. of tensor i, one partial sum each.
+constexpr int NORM_BATCH = 192;
+struct NormArgs {
+  int count;
+  const void* p[NORM_BATCH];
+  int64_t n[NORM_BATCH];
+  int first[NORM_BATCH];
+  double* part;
+};
+int64_t norm_blocks(int64_t n);
+hipError_t launch_grad_sumsq(int dtype, const NormArgs& a, int blocks, hipStream_t s);
+hipError_t launch_clip_coef(const double* part, int64_t n, double max_norm, double* sumsq, float* out, hipStream_t s);
 
 // ---------------------------------------------------------------- measurement probes
 hipError_t launch_probe_copy(const void* src, void* dst, int64_t bytes, hipStream_t s);

@@ -1,0 +1,818 @@
+"""GPU parity of the operators around a stage (linear layers with their
+epilogue and gradients, the embedding and its gradient, the gradient norm and
+the clipped updates) against their formulas in 64 bits, element by element.
+
+Bounds.  u = 2^-8 (bf16) or 2^-24 (fp32) is half a step of the stored type.  A
+sum of K fp32 products is off by at most (K + 1) 2^-23 times the sum of their
+magnitudes (2^-23 and not 2^-24 per addition: the matrix unit may truncate); the
+joined parts of a split reduction are among those K additions.  |gelu'| and
+|silu'| stay below 1.13, erf, exp and a quotient are taken as good to
+8 * 2^-24 of the values they make, and an added residual rounds once more."""
+import math
+
+import pytest
+
+import paper_1911_04610_amd as xp
+
+pytestmark = pytest.mark.gpu
+ACT = {"none": xp.ACT_NONE, "relu": xp.ACT_RELU, "gelu": xp.ACT_GELU, "silu": xp.ACT_SILU}
+E24, E23 = 2.0 ** -24, 2.0 ** -23
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def _dt(name):
+    torch = _torch()
+    return {"bf16": torch.bfloat16, "f32": torch.float32}[name]
+
+
+def _half_step(name):
+    return {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}[name]
+
+
+def _rows(g, rows, cols, dtype, pitch=0, scale=1.0, offset=0):
+    """[rows, cols] on the GPU, rows pitch elements further apart than long, starting offset elements into its buffer."""
+    torch = _torch()
+    buf = torch.randn(rows, cols + pitch, generator=g) * scale
+    return buf.to(dtype).cuda()[:, offset:offset + cols]
+
+
+def _gen(seed):
+    torch = _torch()
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return g
+
+
+def _act64(z, act):
+    torch = _torch()
+    if act == "relu":
+        return torch.relu(z)
+    if act == "gelu":
+        return z * 0.5 * (1 + torch.erf(z / math.sqrt(2)))
+    return z * torch.sigmoid(z) if act == "silu" else z
+
+
+def _slope64(z, act):
+    torch = _torch()
+    if act == "relu":
+        return (z > 0).double()
+    if act == "gelu":
+        return 0.5 * (1 + torch.erf(z / math.sqrt(2))) + z * torch.exp(-z * z / 2) / math.sqrt(2 * math.pi)
+    if act == "silu":
+        s = torch.sigmoid(z)
+        return s + z * s * (1 - s)
+    return torch.ones_like(z)
+
+
+def _close(got, want, tol, what):
+    got = got.double().cpu()
+    off = (got - want).abs()
+    assert bool((off <= tol).all()), f"{what}: {float((off - tol).max()):.3e} over its bound, at {int((off - tol).argmax())}"
+
+
+def _d(t):
+    return t.detach().cpu().double()
+
+
+# ---------------------------------------------------------------- linear
+def _check_fwd(x, W, b, r, y, z, act, dtype):
+    u, K = _half_step(dtype), x.shape[1]
+    X, V = _d(x), _d(W)
+    z64, mag = X @ V.t(), X.abs() @ V.abs().t()
+    if b is not None:
+        z64 = z64 + _d(b)
+        mag = mag + _d(b).abs()
+    dz = (K + 2) * E23 * mag
+    if z is not None:
+        _close(z, z64, u * (z64.abs() + dz) + dz, "preact")
+    y64 = _act64(z64, act)
+    dy = 1.13 * dz + (0 if act in ("none", "relu") else 16 * E24 * z64.abs())
+    if r is not None:
+        y64 = y64 + _d(r)
+        dy = dy + E24 * (y64.abs() + dy)
+    _close(y, y64, u * (y64.abs() + dy) + dy, "y")
+
+
+LINEAR = [  # rows, cin, cout
+    (1, 1, 1), (1, 4096, 128), (3, 7, 5), (5, 64, 64), (16, 256, 10), (17, 129, 130), (32, 256, 256), (64, 1000, 72),
+    (100, 2048, 200), (127, 65, 63), (128, 128, 128), (130, 260, 520), (257, 96, 300), (300, 8, 1000),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cin,cout", LINEAR)
+def test_linear_forward(rows, cin, cout, dtype):
+    torch = _torch()
+    dt, g = _dt(dtype), _gen(rows * 31 + cin * 7 + cout)
+    for k, act in enumerate(ACT):
+        pitch = (0, 5, 8, 64)[k]
+        x, W = _rows(g, rows, cin, dt, pitch), _rows(g, cout, cin, dt, (pitch * 3) % 16, cin ** -0.5)
+        b = torch.randn(cout, generator=g).cuda() if k != 1 else None
+        r = _rows(g, rows, cout, dt, pitch) if k != 2 else None
+        y, z = torch.full((rows, cout), 7.0, dtype=dt, device="cuda"), torch.empty(rows, cout, dtype=dt, device="cuda")
+        xp.xpipe_linear_fwd(x, W, b, y, act=ACT[act], residual=r, preact=z if k != 3 else None)
+        _check_fwd(x, W, b, r, y, z if k != 3 else None, act, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("offset", [0, 1, 2, 4, 8])
+def test_linear_forward_any_alignment(offset, dtype):
+    """Every matrix starts `offset` elements into its buffer; the columns around the output stay."""
+    torch = _torch()
+    dt, g = _dt(dtype), _gen(offset)
+    rows, cin, cout = 70, 136, 72
+    x = _rows(g, rows, cin, dt, 16, offset=offset)
+    W = _rows(g, cout, cin, dt, 16, 0.1, offset=offset)
+    r = _rows(g, rows, cout, dt, 16, offset=offset)
+    buf = torch.full((rows + 2, cout + 16), 3.0, dtype=dt, device="cuda")
+    y = buf[1:rows + 1, offset:offset + cout]
+    xp.xpipe_linear_fwd(x, W, None, y, act=xp.ACT_SILU, residual=r)
+    _check_fwd(x, W, None, r, y, None, "silu", dtype)
+    kept = torch.ones_like(buf, dtype=torch.bool)
+    kept[1:rows + 1, offset:offset + cout] = False
+    assert bool((buf[kept] == 3.0).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cin,cout", [(2000, 1024, 2048), (4096, 520, 3000), (40, 8192, 264), (513, 4096, 4100)])
+def test_linear_forward_large(rows, cin, cout, dtype):
+    torch = _torch()
+    dt, g = _dt(dtype), _gen(5)
+    x, W, b = _rows(g, rows, cin, dt), _rows(g, cout, cin, dt, scale=cin ** -0.5), torch.randn(cout, generator=g).cuda()
+    y = _rows(g, rows, cout, dt)
+    r = y.clone()
+    xp.xpipe_linear_fwd(x, W, b, y, act=xp.ACT_GELU, residual=y)  # the residual in place
+    pick = torch.randperm(rows, generator=g)[:200]
+    _check_fwd(x[pick.cuda()], W, b, r[pick.cuda()], y[pick.cuda()], None, "gelu", dtype)
+
+
+def _check_bwd(dz, x, W, dx, gW, gb, gW0, gb0, act, z, res, dtype):
+    u, rows, cout = _half_step(dtype), dz.shape[0], dz.shape[1]
+    G, X, V = _d(dz), _d(x), _d(W)
+    p, mag = G @ V, G.abs() @ V.abs()
+    dp = (cout + 1) * E23 * mag
+    s = _slope64(_d(z), act) if z is not None else _torch().ones_like(p)
+    want = p * s
+    tol = dp * 1.13 + (0 if act in ("none", "relu") else p.abs() * 16 * E24 * (1 + _d(z).abs()))
+    if res is not None:
+        want = want + _d(res)
+        tol = tol + E24 * (want.abs() + tol)
+    _close(dx, want, u * (want.abs() + tol) + tol, "dx")
+    w64, wmag = G.t() @ X, G.abs().t() @ X.abs()
+    _close(gW.view_as(w64), _d(gW0).view_as(w64) + w64, (rows + 2) * E23 * wmag + E24 * (_d(gW0).view_as(w64).abs() + wmag), "grad_W")
+    if gb is not None:
+        # 32 terms at a time in fp32, the rest in fp64
+        bmag = G.abs().sum(0)
+        _close(gb, _d(gb0) + G.sum(0), 32 * E24 * bmag + E24 * (_d(gb0).abs() + bmag), "grad_b")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cin,cout", LINEAR + [(1000, 96, 64), (2049, 30, 17)])
+def test_linear_backward(rows, cin, cout, dtype):
+    torch = _torch()
+    dt, g = _dt(dtype), _gen(rows + cin * 3 + cout * 5)
+    for k, act in enumerate(ACT):
+        pitch = (0, 3, 8, 64)[k]
+        dz, x = _rows(g, rows, cout, dt, pitch), _rows(g, rows, cin, dt, pitch)
+        W = _rows(g, cout, cin, dt, (pitch * 3) % 16, cout ** -0.5)
+        z = _rows(g, rows, cin, dt, pitch, 2.0) if act != "none" else None
+        res = _rows(g, rows, cin, dt, 0) if k % 2 else None
+        gW, gb = torch.randn(cout * cin, generator=g).cuda(), torch.randn(cout, generator=g).cuda()
+        gW0, gb0 = gW.clone(), gb.clone()
+        dx = torch.empty(rows, cin, dtype=dt, device="cuda")
+        xp.xpipe_linear_bwd(dz, x, W, dx, gW, gb if k != 2 else None, act=ACT[act], preact=z, residual=res)
+        _check_bwd(dz, x, W, dx, gW, gb if k != 2 else None, gW0, gb0, act, z, res, dtype)
+        if k == 2:
+            assert torch.equal(gb, gb0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_linear_backward_large(dtype):
+    torch = _torch()
+    dt, g = _dt(dtype), _gen(9)
+    rows, cin, cout = 3000, 1100, 2200
+    dz, x, W = _rows(g, rows, cout, dt), _rows(g, rows, cin, dt), _rows(g, cout, cin, dt, scale=cout ** -0.5)
+    z, dx = _rows(g, rows, cin, dt), torch.empty(rows, cin, dtype=dt, device="cuda")
+    gW, gb = torch.zeros(cout, cin, device="cuda"), torch.zeros(cout, device="cuda")
+    gW0, gb0 = gW.clone(), gb.clone()
+    xp.xpipe_linear_bwd(dz, x, W, dx, gW, gb, act=xp.ACT_SILU, preact=z)
+    _check_bwd(dz, x, W, dx, gW, gb, gW0, gb0, "silu", z, None, dtype)
+
+
+def test_linear_backward_parts_alone():
+    """dx without accumulators (and x), accumulators without dx (and W): the same bits as together."""
+    torch = _torch()
+    g = _gen(3)
+    dz, x, W = (_rows(g, 50, 40, torch.bfloat16), _rows(g, 50, 24, torch.bfloat16), _rows(g, 40, 24, torch.bfloat16))
+    dx, gW, gb = torch.empty(50, 24, dtype=torch.bfloat16, device="cuda"), torch.zeros(40, 24, device="cuda"), torch.zeros(40, device="cuda")
+    xp.xpipe_linear_bwd(dz, x, W, dx, gW, gb)
+    dx2, gW2, gb2 = torch.empty_like(dx), torch.zeros_like(gW), torch.zeros_like(gb)
+    xp.xpipe_linear_bwd(dz, None, W, dx2)
+    xp.xpipe_linear_bwd(dz, x, None, None, gW2, gb2)
+    assert torch.equal(dx, dx2) and torch.equal(gW, gW2) and torch.equal(gb, gb2)
+    xp.xpipe_linear_bwd(dz, x, None, None, gW2, gb2)  # added, not written
+    assert torch.equal(gW2, gW * 2) and torch.equal(gb2, gb * 2)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", list(ACT))
+def test_linear_gradient_against_differences(act, dtype):
+    """(f(x + h d) - f(x - h d)) / 2h for the chain act -> linear -> act in 64 bits
+    against the backward's dx (through xpipe_act_bwd) and accumulators.  The
+    difference's own error is h^2 / 6 times a third derivative of order 10, 1e-7 at
+    h = 1e-4; smooth points only (ReLU inputs away from 0 by more than h).  The
+    stored gradients are off by at most their half steps, along the way twice."""
+    torch = _torch()
+    dt, g = _dt(dtype), _gen(12)
+    rows, cin, cout = 9, 16, 24
+    zin = _rows(g, rows, cin, dt)
+    W, b = _rows(g, cout, cin, dt, scale=cin ** -0.5), torch.randn(cout, generator=g).cuda()
+    zin = torch.where(zin.abs() < 0.05, torch.full_like(zin, 0.125), zin).contiguous()
+    x, z = torch.empty(rows, cin, dtype=dt, device="cuda"), torch.empty(rows, cout, dtype=dt, device="cuda")
+    y = torch.empty_like(z)
+    x.copy_(_act64(zin.double(), act))
+    xp.xpipe_linear_fwd(x, W, b, y, act=ACT[act], preact=z)
+    dy = _rows(g, rows, cout, dt)
+    dz, dx = torch.empty_like(dy), torch.empty(rows, cin, dtype=dt, device="cuda")
+    xp.xpipe_act_bwd(dy, z, dz, ACT[act])
+    gW, gb = torch.zeros(cout, cin, device="cuda"), torch.zeros(cout, device="cuda")
+    xp.xpipe_linear_bwd(dz, x, W, dx, gW, gb, act=ACT[act], preact=zin if act != "none" else None)
+
+    Z, V, B, D, X = _d(zin), _d(W), _d(b), _d(dy), _d(x)
+    u, h = _half_step(dtype), 1e-4
+
+    def loss(zi, v, bb):  # x stored: the linear layer's inputs are what it read
+        return float((_act64((X + (_act64(zi, act) - _act64(Z, act))) @ v.t() + bb, act) * D).sum())
+
+    # ReLU outputs must not change sign under the step either
+    dirs = {"dx": torch.randn(rows, cin, generator=g).double() * 0.1, "gW": torch.randn(cout, cin, generator=g).double() * 0.1,
+            "gb": torch.randn(cout, generator=g).double() * 0.1}
+    got = {"dx": dx, "gW": gW, "gb": gb}
+    for name, d in dirs.items():
+        step = lambda s: loss(Z + s * d if name == "dx" else Z, V + s * d if name == "gW" else V, B + s * d if name == "gb" else B)
+        diff = (step(h) - step(-h)) / (2 * h)
+        inner = float((_d(got[name]).view_as(d) * d).sum())
+        # dz is stored (u), from a stored z (u |z| curvature 1.13 at most), then dx is (u); magnitudes of the sums
+        dzmag = D.abs() * 1.13 + D.abs() * 1.2 * _d(z).abs()
+        mag = {"dx": 1.13 * (dzmag @ V.abs()), "gW": dzmag.t() @ X.abs(), "gb": dzmag.sum(0)}[name]
+        mag = float((mag * d.abs()).sum())
+        assert abs(diff - inner) <= 3 * u * mag + 40 * E23 * mag + 1e-6 * (1 + abs(diff)), name
+
+
+def test_linear_rows_are_independent_and_non_finite_values_stay_in_their_rows():
+    torch = _torch()
+    g = _gen(4)
+    for dt in (torch.bfloat16, torch.float32):
+        x, W = _rows(g, 70, 72, dt), _rows(g, 40, 72, dt)
+        y0, y1 = torch.empty(70, 40, dtype=dt, device="cuda"), torch.empty(70, 40, dtype=dt, device="cuda")
+        xp.xpipe_linear_fwd(x, W, None, y0, act=xp.ACT_RELU)
+        bad = x.clone()
+        bad[3, 5], bad[40, 71] = float("nan"), float("inf")
+        xp.xpipe_linear_fwd(bad, W, None, y1, act=xp.ACT_RELU)
+        keep = torch.ones(70, dtype=torch.bool, device="cuda")
+        keep[3] = keep[40] = False
+        assert torch.equal(y0[keep], y1[keep]) and bool(torch.isnan(y1[3]).all())
+        want = torch.where(W[:, 71] > 0, float("inf"), 0.0).to(dt)
+        assert torch.equal(y1[40], want)
+        # values past a matrix's own columns are never taken in
+        wide = torch.full((70, 80), float("nan"), dtype=dt, device="cuda")
+        wide[:, :72] = x
+        xp.xpipe_linear_fwd(wide[:, :72], W, None, y1, act=xp.ACT_RELU)
+        assert torch.equal(y0, y1)
+
+
+def test_linear_repeats_bit_for_bit_and_takes_a_given_workspace_and_stream():
+    torch = _torch()
+    g = _gen(6)
+    x, W = _rows(g, 40, 4096, torch.bfloat16), _rows(g, 101, 4096, torch.bfloat16)
+    y = [torch.empty(40, 101, dtype=torch.bfloat16, device="cuda") for _ in range(3)]
+    xp.xpipe_linear_fwd(x, W, None, y[0])
+    xp.xpipe_linear_fwd(x, W, None, y[1], workspace=torch.empty(64 << 20, dtype=torch.uint8, device="cuda"))
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    xp.xpipe_linear_fwd(x, W, None, y[2], stream=s)
+    s.synchronize()
+    torch.cuda.synchronize()
+    assert torch.equal(y[0], y[1]) and torch.equal(y[0], y[2])
+
+
+def test_linear_zero_rows():
+    torch = _torch()
+    e = lambda *s: torch.empty(*s, dtype=torch.bfloat16, device="cuda")
+    gW = torch.ones(8, 16, device="cuda")
+    xp.xpipe_linear_fwd(e(0, 16), e(8, 16), None, e(0, 8))
+    xp.xpipe_linear_bwd(e(0, 8), e(0, 16), e(8, 16), e(0, 16), gW)
+    assert bool((gW == 1).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [1, 7, 8, 1000, 4099])
+def test_act_bwd(n, dtype):
+    torch = _torch()
+    dt, g = _dt(dtype), _gen(n)
+    for act in ACT:
+        dy, z = _rows(g, 1, n, dt)[0], _rows(g, 1, n, dt, scale=3.0)[0]
+        dz = torch.empty_like(dy)
+        xp.xpipe_act_bwd(dy, z, dz, ACT[act])
+        want = _d(dy) * _slope64(_d(z), act)
+        tol = _d(dy).abs() * 16 * E24 * (1 + _d(z).abs())
+        _close(dz, want, _half_step(dtype) * (want.abs() + tol) + tol, act)
+
+
+# ---------------------------------------------------------------- embedding
+def _tokens(g, n, vocab, kind):
+    torch = _torch()
+    if kind == "one":
+        t = torch.full((n,), vocab // 2)
+    elif kind == "zipf":
+        t = (torch.exp(torch.rand(n, generator=g, dtype=torch.float64) * math.log(vocab + 1)).long().clamp(1, vocab) - 1)
+    elif kind == "padded":
+        t = torch.randint(-2, vocab + 3, (n,), generator=g)
+    elif kind == "all_padding":
+        t = torch.full((n,), -1)
+    else:
+        t = torch.randint(0, vocab, (n,), generator=g)
+    return t.to(torch.int32).cuda()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,vocab,dim", [(0, 5, 8), (1, 1, 1), (5, 3, 7), (100, 50, 64), (33, 1000, 130), (4097, 300, 24), (1000, 70000, 256)])
+def test_embedding_forward(n, vocab, dim, dtype):
+    torch = _torch()
+    g = _gen(n + dim)
+    table = _rows(g, vocab, dim, _dt(dtype))
+    for kind in ("uniform", "padded"):
+        t = _tokens(g, n, vocab, kind)
+        y = torch.full((n, dim), 9.0, dtype=_dt(dtype), device="cuda")
+        xp.xpipe_embedding_fwd(table, t, y, scale=math.sqrt(dim))
+        live = (t >= 0) & (t < vocab)
+        want = (table.double()[t.long().clamp(0, vocab - 1)] * math.sqrt(dim)).float().to(_dt(dtype)) * live[:, None]
+        assert torch.equal(y, want)
+
+
+EMBED = [(1, 1, 1), (2, 1, 3), (7, 3, 5), (64, 10, 8), (256, 1000, 256), (2047, 50, 40), (2048, 50, 40), (2049, 7, 36),
+         (8191, 300, 16), (8192, 300, 16), (8193, 300, 16), (16383, 255, 8), (16384, 256, 8), (20000, 70000, 24), (50001, 65535, 12),
+         (40000, 3, 520)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,vocab,dim", EMBED)
+def test_embedding_backward(n, vocab, dim, dtype):
+    torch = _torch()
+    g = _gen(n * 3 + dim)
+    for kind in ("uniform", "zipf", "one", "padded", "all_padding"):
+        t, dy = _tokens(g, n, vocab, kind), _rows(g, n, dim, _dt(dtype))
+        grad = torch.randn(vocab, dim, generator=g).cuda()
+        before = grad.clone()
+        xp.xpipe_embedding_bwd(dy, t, grad, scale=0.75)
+        live = ((t >= 0) & (t < vocab)).cpu()
+        idx = t.cpu().long()[live]
+        want = _d(before).index_add_(0, idx, _d(dy)[live] * 0.75)
+        mag = torch.zeros(vocab, dim, dtype=torch.float64).index_add_(0, idx, _d(dy)[live].abs() * 0.75)
+        # rounded once, and the parts of a long run once each
+        _close(grad, want, (want.abs() + mag) * E24 * (1 + 1e-6), kind)
+        untouched = torch.ones(vocab, dtype=torch.bool)
+        untouched[idx] = False
+        assert torch.equal(grad.cpu()[untouched], before.cpu()[untouched])
+        again = before.clone()
+        xp.xpipe_embedding_bwd(dy, t, again, scale=0.75)
+        assert torch.equal(grad, again)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_embedding_unaligned_rows(dtype):
+    torch = _torch()
+    g, dt = _gen(8), _dt(dtype)
+    buf = _rows(g, 1, 1 + 30 * 16, dt)[0]
+    table, t = buf[1:].view(30, 16), _tokens(g, 90, 30, "padded")
+    ybuf = torch.full((1 + 90 * 16 + 8,), 5.0, dtype=dt, device="cuda")
+    y = ybuf[1:1 + 90 * 16].view(90, 16)
+    xp.xpipe_embedding_fwd(table, t, y)
+    live = (t >= 0) & (t < 30)
+    assert torch.equal(y, table[t.long().clamp(0, 29)] * live[:, None]) and float(ybuf[0]) == 5.0 and bool((ybuf[-8:] == 5.0).all())
+    gbuf = torch.zeros(1 + 30 * 16, device="cuda")
+    xp.xpipe_embedding_bwd(y, t, gbuf[1:].view(30, 16))
+    want = torch.zeros(30, 16, dtype=torch.float64).index_add_(0, t.cpu().long()[live.cpu()], _d(y)[live.cpu()])
+    mag = torch.zeros(30, 16, dtype=torch.float64).index_add_(0, t.cpu().long()[live.cpu()], _d(y)[live.cpu()].abs())
+    _close(gbuf[1:].view(30, 16), want, (want.abs() + mag) * E24 * (1 + 1e-6), "unaligned")
+
+
+def test_embedding_gradient_against_differences():
+    """The lookup is linear in the table, so a difference is exact up to rounding:
+    f(T + d) - f(T) in 64 bits against the gradient's inner product with d."""
+    torch = _torch()
+    g = _gen(10)
+    t, D = _tokens(g, 500, 40, "padded"), _rows(g, 500, 12, torch.float32)
+    grad = torch.zeros(40, 12, device="cuda")
+    xp.xpipe_embedding_bwd(D, t, grad, scale=1.5)
+    d = torch.randn(40, 12, generator=g).double()
+    live = ((t >= 0) & (t < 40)).cpu()
+    f = lambda tab: float((tab[t.cpu().long().clamp(0, 39)] * live[:, None] * 1.5 * _d(D)).sum())
+    base = torch.randn(40, 12, generator=g).double()
+    diff, inner = f(base + d) - f(base), float((_d(grad) * d).sum())
+    mag = float((_d(D).abs() * 1.5).sum()) * float(d.abs().max())
+    assert abs(diff - inner) <= 2 * E24 * mag
+
+
+def test_embedding_non_finite_rows_stay_in_their_tokens():
+    torch = _torch()
+    g = _gen(11)
+    t = _tokens(g, 300, 20, "padded")
+    dy = _rows(g, 300, 16, torch.float32)
+    pad = ~((t >= 0) & (t < 20))
+    dy[pad] = float("nan")  # padding is not read
+    dy[(t == 4).nonzero()[0]] = float("inf")
+    grad = torch.zeros(20, 16, device="cuda")
+    xp.xpipe_embedding_bwd(dy, t, grad)
+    ok = torch.ones(20, dtype=torch.bool, device="cuda")
+    ok[4] = False
+    assert bool(torch.isfinite(grad[ok]).all()) and bool(torch.isinf(grad[4]).all())
+
+
+# ---------------------------------------------------------------- norm and clipping
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("sizes", [[1], [0, 3, 0], [16384], [16385, 1, 2, 3, 16383], [5] * 500, [100003, 7, 65536] * 3])
+def test_grad_norm(sizes, dtype):
+    torch = _torch()
+    g = _gen(sum(sizes))
+    flat = torch.randn(sum(sizes) + len(sizes), generator=g).to(_dt(dtype)).cuda()
+    views, at = [], 0
+    for k, n in enumerate(sizes):  # cuts at any element
+        views.append(flat[at:at + n])
+        at += n + k % 2
+    want = math.sqrt(sum(float((_d(v) ** 2).sum()) for v in views))
+    out, sq = torch.zeros(2, device="cuda"), torch.zeros(1, dtype=torch.float64, device="cuda")
+    for max_norm in (0.5 * want, 2 * want + 1):
+        xp.xpipe_grad_norm(views, max_norm, out, sumsq=sq)
+        coef = min(1.0, max_norm / (want + 1e-6))
+        assert abs(float(sq) - want ** 2) <= 1e-12 * want ** 2
+        assert abs(float(out[0]) - want) <= 1.01 * E24 * want and abs(float(out[1]) - coef) <= 1.01 * E24 * coef
+        again = torch.zeros(2, device="cuda")
+        xp.xpipe_clip_coef(sq, max_norm, again)
+        assert torch.equal(again, out)
+        lst = xp.TensorList(views)
+        xp.xpipe_grad_norm(lst, max_norm, again)
+        assert torch.equal(again, out)
+
+
+def test_grad_norm_of_nothing_large_values_and_non_finite_ones():
+    torch = _torch()
+    out = torch.full((2,), 7.0, device="cuda")
+    xp.xpipe_grad_norm([torch.zeros(0, device="cuda")], 1.0, out)
+    assert out.tolist() == [0.0, 1.0]
+    xp.xpipe_grad_norm([torch.zeros(100, device="cuda")], 1.0, out)
+    assert out.tolist() == [0.0, 1.0]
+    big = torch.full((100,), 1e38, device="cuda")  # squares leave the range of fp32
+    xp.xpipe_grad_norm([big], 1.0, out)
+    assert float(out[0]) == float("inf") or abs(float(out[0]) / 1e39 - 1) < 1e-6
+    xp.xpipe_grad_norm([big[:1] * 1e-3], 1.0, out)
+    assert abs(float(out[0]) / 1e35 - 1) <= 2 * E24 and abs(float(out[1]) * 1e35 - 1) <= 1e-6
+    x = torch.ones(40000, device="cuda")
+    x[39999] = float("inf")
+    xp.xpipe_grad_norm([x], 1.0, out)
+    assert out.tolist() == [float("inf"), 0.0]
+    x[3] = float("nan")
+    xp.xpipe_grad_norm([x], 1.0, out)
+    assert bool(torch.isnan(out).all())
+
+
+def test_clip_coef_over_stages_is_the_norm_over_all_tensors():
+    torch = _torch()
+    g = _gen(2)
+    a, b = torch.randn(5000, generator=g).cuda(), torch.randn(333, generator=g).cuda()
+    parts = torch.zeros(2, dtype=torch.float64, device="cuda")
+    xp.xpipe_grad_norm([a], 1.0, sumsq=parts[0:1])
+    xp.xpipe_grad_norm([b], 1.0, sumsq=parts[1:2])
+    one, all_ = torch.zeros(2, device="cuda"), torch.zeros(2, device="cuda")
+    xp.xpipe_clip_coef(parts, 3.0, one)
+    xp.xpipe_grad_norm([a, b], 3.0, all_)
+    assert abs(float(one[0] - all_[0])) <= 2 * E24 * float(one[0]) and abs(float(one[1] - all_[1])) <= 2 * E24 * float(one[1])
+
+
+@pytest.mark.parametrize("n", [1, 3, 4, 1000, 70001])
+@pytest.mark.parametrize("rule", ["adam", "sgd", "rmsprop"])
+@pytest.mark.parametrize("max_norm", [0.01, 1e6])
+def test_clipped_update_is_the_update_of_the_scaled_gradient(rule, n, max_norm):
+    """Bit for bit, with both predictions and with the gradient zeroed or left."""
+    torch = _torch()
+    for zero in (True, False):
+        runs = []
+        for fused in (True, False):
+            g = _gen(n)
+            r = lambda s: (torch.randn(n, generator=g) * s).cuda()
+            W, m, v, G, buf, sq = r(1.0), r(1e-2), r(1e-2).abs(), r(1.0), r(1.0), r(1.0).abs()
+            pf, pb = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+            clip = torch.zeros(2, device="cuda")
+            xp.xpipe_grad_norm([G], max_norm, clip)
+            g0 = G.clone()
+            if not fused:
+                G.mul_(clip[1])
+            kw = dict(zero_grad=zero, pred_fwd=pf, s_fwd=2, pred_bwd=pb, s_bwd=1, clip=clip if fused else None)
+            if rule == "adam":
+                xp.xpipe_adam_flat(W, m, v, G, xp.Hyper(), 3, **kw)
+            else:
+                kind = xp.RULE_RMSPROP if rule == "rmsprop" else xp.RULE_MOMENTUM_SGD
+                xp.xpipe_rule_flat(W, buf, sq if rule == "rmsprop" else None, m, v, G, xp.Rule(kind, weight_decay=1e-3),
+                                   xp.Hyper(), 3, **kw)
+            if fused:
+                assert torch.equal(G, torch.zeros_like(G) if zero else g0)
+            runs.append((W, m, v, pf, pb, buf, sq))
+            assert (float(clip[1]) < 1) == (max_norm < 1)
+        for a, b in zip(*runs):
+            assert torch.equal(a, b)
+
+
+def _small_stage(dtype=None, seed=1, T=1, micro=16, cin=24, classes=10, **kw):
+    torch = _torch()
+    layers = [dict(kind="linear", inputs=[-1], cin=cin, cout=20, bias=True), dict(kind="relu", inputs=[0]),
+              dict(kind="linear", inputs=[1], cin=20, cout=classes, bias=True), dict(kind="softmax_ce", inputs=[2], classes=classes)]
+    st = xp.Stage(layers, micro, T, (cin,), xp.F32 if dtype is None else dtype, **kw)
+    g = _gen(seed)
+    for off, cnt in st.layout:
+        st.W[off:off + cnt] = (torch.randn(cnt, generator=g) * 0.3).cuda()
+    return st
+
+
+@pytest.mark.parametrize("rule", ["adam", "sgd", "rmsprop"])
+def test_stage_clips_its_updates(rule):
+    """With max_norm the stage computes norm and coefficient itself; with 0 it takes the caller's; off again: unclipped."""
+    torch = _torch()
+    g = _gen(4)
+    x, lab = torch.randn(16, 24, generator=g).cuda(), torch.randint(0, 10, (16,), generator=g).to(torch.int32).cuda()
+    hp = xp.Hyper()
+    out = {}
+    for mode in ("own", "given", "scaled", "off", "none"):
+        st = _small_stage()
+        clip, y = torch.zeros(2, device="cuda"), torch.empty(16, 10, device="cuda")
+        if mode in ("own", "off"):
+            st.xpipe_stage_set_clip(0.05, clip)
+        if mode == "off":
+            st.xpipe_stage_set_clip(0.0, None)
+        if mode == "given":
+            st.xpipe_stage_set_clip(0.0, clip)
+        buf, sq = torch.zeros_like(st.W), torch.zeros_like(st.W)
+        for t in range(3):
+            st.xpipe_predict_weights(xp.FWD, 1, hp, t)
+            st.xpipe_predict_weights(xp.BWD, 1, hp, t)
+            st.xpipe_stage_fwd(x, y, lab)
+            st.xpipe_stage_bwd(x, labels=lab)
+            if mode in ("given", "scaled"):
+                xp.xpipe_grad_norm([st.grad], 0.05, clip)
+            if mode == "scaled":
+                st.grad.mul_(clip[1])
+            if rule == "adam":
+                st.xpipe_adam_step(hp, t)
+            else:
+                kind = xp.RULE_RMSPROP if rule == "rmsprop" else xp.RULE_MOMENTUM_SGD
+                st.xpipe_rule_step(xp.Rule(kind), hp, t, buf, sq if rule == "rmsprop" else None)
+            assert not bool(st.grad.any())
+        out[mode] = [st.W.clone(), st.m.clone(), st.v.clone(), clip.clone()]
+        st.destroy()
+    for a, b in zip(out["own"], out["given"]):
+        assert torch.equal(a, b)
+    for a, b in zip(out["own"], out["scaled"]):
+        assert torch.equal(a, b)
+    for a, b in zip(out["off"][:3], out["none"][:3]):
+        assert torch.equal(a, b)
+    assert float(out["own"][3][1]) < 1 and not torch.equal(out["own"][1], out["none"][1])
+
+
+def test_stage_run_clips_every_update():
+    torch = _torch()
+    g = _gen(6)
+    T, minis = 2, 3
+    ev = xp.xpipe_schedule(1, T, 0, minis)
+    n = T * minis
+    x = [torch.randn(16, 24, generator=g).cuda() for _ in range(n)]
+    lab = [torch.randint(0, 10, (16,), generator=g).to(torch.int32).cuda() for _ in range(n)]
+    res = []
+    for how in ("run", "steps"):
+        st = _small_stage(T=T)
+        clip, hp = torch.zeros(2, device="cuda"), xp.Hyper()
+        st.xpipe_stage_set_clip(0.02, clip)
+        y = [torch.empty(16, 10, device="cuda") for _ in range(n)]
+        if how == "run":
+            st.xpipe_stage_run(ev, x, y, hp, 0, labels=lab)
+        else:
+            t = 0
+            for e in ev:
+                k = e.micro - 1
+                if e.bellwether:
+                    st.xpipe_predict_weights(e.kind, e.s_eq, hp, t)
+                if e.kind == xp.FWD:
+                    st.xpipe_stage_fwd(x[k], y[k], lab[k])
+                else:
+                    st.xpipe_stage_bwd(x[k], labels=lab[k])
+                    if e.update_after:
+                        st.xpipe_adam_step(hp, t, emit_pred=xp.KEEP_PRED)
+                        t += 1
+        res.append((st.W.clone(), st.m.clone(), clip.clone()))
+        st.destroy()
+    for a, b in zip(*res):
+        assert torch.equal(a, b)
+    assert float(res[0][2][1]) < 1
+
+
+# ---------------------------------------------------------------- together
+class _Net:
+    """table -> linear(gelu) -> linear + skip -> stage (linear, relu, linear, loss), clipped by one norm."""
+
+    def __init__(self, dtype, seed, vocab=50, dim=24, hidden=56, n=16, T=1):
+        torch = _torch()
+        g = _gen(seed)
+        self.n, self.dim, self.hidden, self.dt, self.scale = n, dim, hidden, _dt(dtype), math.sqrt(dim)
+        sizes = {"table": (vocab, dim), "W1": (hidden, dim), "b1": (hidden,), "W2": (dim, hidden), "b2": (dim,)}
+        self.off, at = {}, 0
+        for k, s in sizes.items():
+            self.off[k] = (at, s)
+            at += -(-math.prod(s) // 64) * 64
+        z = lambda: torch.zeros(at, device="cuda")
+        self.W, self.m, self.v, self.G, self.P, self.Pb = z(), z(), z(), z(), z(), torch.zeros(at, dtype=torch.bfloat16, device="cuda")
+        for k, s in sizes.items():
+            self.view(self.W, k).copy_((torch.randn(*s, generator=g) * 0.3).cuda())
+        self.stage = _small_stage(xp.F32 if dtype == "f32" else xp.BF16, seed + 1, T, n, dim)
+        self.clip, self.hp, self.t = torch.zeros(2, device="cuda"), xp.Hyper(lr=1e-2), 0
+        self.stage.xpipe_stage_set_clip(0.0, self.clip)
+        self.list = xp.TensorList([self.G, self.stage.grad])
+        e = lambda c: torch.empty(n, c, dtype=self.dt, device="cuda")
+        self.h0, self.z1, self.h1, self.h2, self.dh2, self.dz1, self.dh0 = e(dim), e(hidden), e(hidden), e(dim), e(dim), e(hidden), e(dim)
+        self.logits, self.loss = e(10), torch.zeros(1, device="cuda")
+
+    def view(self, buf, k):
+        at, s = self.off[k]
+        return buf[at:at + math.prod(s)].view(s)
+
+    def predict(self, s):
+        xp.xpipe_predict_flat(self.W, self.m, self.v, self.P, self.Pb, s, self.hp, self.t)
+
+    def weight(self, k):
+        return self.view(self.P if self.dt == _torch().float32 else self.Pb, k)
+
+    def step(self, tokens, labels, max_norm, s=1):
+        st = self.stage
+        self.predict(s)
+        st.xpipe_predict_weights(xp.FWD, s, self.hp, self.t)
+        st.xpipe_predict_weights(xp.BWD, s, self.hp, self.t)
+        self.passes(tokens, labels, max_norm)
+        xp.xpipe_adam_flat(self.W, self.m, self.v, self.G, self.hp, self.t, clip=self.clip)
+        st.xpipe_adam_step(self.hp, self.t)
+        self.t += 1
+
+    def passes(self, tokens, labels, max_norm):
+        st, w = self.stage, self.weight
+        xp.xpipe_embedding_fwd(w("table"), tokens, self.h0, scale=self.scale)
+        xp.xpipe_linear_fwd(self.h0, w("W1"), self.view(self.P, "b1"), self.h1, act=xp.ACT_GELU, preact=self.z1)
+        xp.xpipe_linear_fwd(self.h1, w("W2"), self.view(self.P, "b2"), self.h2, residual=self.h0)
+        st.xpipe_stage_fwd(self.h2, self.logits, labels, self.loss)
+        st.xpipe_stage_bwd(self.h2, labels=labels, dx=self.dh2)
+        xp.xpipe_linear_bwd(self.dh2, self.h1, w("W2"), self.dz1, self.view(self.G, "W2"), self.view(self.G, "b2"), act=xp.ACT_GELU,
+                            preact=self.z1)
+        xp.xpipe_linear_bwd(self.dz1, self.h0, w("W1"), self.dh0, self.view(self.G, "W1"), self.view(self.G, "b1"), residual=self.dh2)
+        xp.xpipe_embedding_bwd(self.dh0, tokens, self.view(self.G, "table"), scale=self.scale)
+        xp.xpipe_grad_norm(self.list, max_norm, self.clip)
+
+
+def _net64(net, tokens, labels, params, stage_params):
+    """Loss and gradients in 64 bits by automatic differentiation."""
+    torch = _torch()
+    P = {k: v.clone().requires_grad_() for k, v in params.items()}
+    S = [p.clone().requires_grad_() for p in stage_params]
+    live = (tokens >= 0).double()[:, None]
+    h0 = P["table"][tokens.clamp(min=0)] * net.scale * live
+    z1 = h0 @ P["W1"].t() + P["b1"]
+    h2 = _act64(z1, "gelu") @ P["W2"].t() + P["b2"] + h0
+    a = torch.relu(h2 @ S[0].view(20, -1).t() + S[1])
+    loss = torch.nn.functional.cross_entropy(a @ S[2].view(10, 20).t() + S[3], labels, reduction="sum") / len(labels)
+    loss.backward()
+    return loss.item(), {k: v.grad for k, v in P.items()}, [p.grad for p in S]
+
+
+@pytest.mark.parametrize("max_norm", [0.05, 1e6])
+def test_a_token_network_trains_together(max_norm):
+    """fp32 storage, three updates with predictions, against 64 bits.  The
+    chain is a few hundred fp32 operations deep at most on values of order 1, each
+    off by 2^-24, so gradients agree to well under 1e-4 of their norm (the bound
+    that the stage's own fp32 parity has); m is their decayed sum, and Adam's first
+    steps divide by their own size, which keeps relative errors as they are except
+    where a gradient is next to zero: W is compared by its movement's norm."""
+    torch = _torch()
+    net = _Net("f32", 3)
+    g = _gen(30)
+    names, lay = list(net.off), net.stage.layout
+    W = {k: _d(net.view(net.W, k)) for k in names}
+    S = [_d(net.stage.W[o:o + c]) for o, c in lay]
+    m = [torch.zeros_like(w) for w in list(W.values()) + S]
+    v = [torch.zeros_like(w) for w in m]
+    for t in range(3):
+        tok = torch.randint(0, 50, (16,), generator=g)
+        tok[5] = -1
+        lab = torch.randint(0, 10, (16,), generator=g)
+        params = list(W.values()) + S
+        if t > 0:  # Eq. 3 with s = 1
+            c1, c2 = 1 - 0.9 ** t, 1 - 0.999 ** t
+            params = [w - 1e-2 * (a / c1) / torch.sqrt(b / c2 + 1e-8) for w, a, b in zip(params, m, v)]
+        loss, gw, gs = _net64(net, tok, lab, dict(zip(names, params)), params[len(names):])
+        net.step(tok.to(torch.int32).cuda(), lab.to(torch.int32).cuda(), max_norm)
+        assert abs(float(net.loss) - loss) <= 1e-4 * abs(loss)
+        grads = list(gw.values()) + gs
+        norm = math.sqrt(sum(float((x * x).sum()) for x in grads))
+        coef = min(1.0, max_norm / (norm + 1e-6))
+        assert abs(float(net.clip[0]) - norm) <= 1e-4 * norm and abs(float(net.clip[1]) - coef) <= 1e-4 * coef
+        for i, x in enumerate(grads):
+            m[i] = 0.9 * m[i] + 0.1 * x * coef
+            v[i] = 0.999 * v[i] + 0.001 * (x * coef) ** 2
+            step = 1e-2 * (m[i] / (1 - 0.9 ** (t + 1))) / (torch.sqrt(v[i] / (1 - 0.999 ** (t + 1))) + 1e-8)
+            if i < len(names):
+                W[names[i]] = W[names[i]] - step
+            else:
+                S[i - len(names)] = S[i - len(names)] - step
+        got = [net.view(net.m, k) for k in names] + [net.stage.m[o:o + c] for o, c in lay]
+        for a, b in zip(got, m):
+            assert float((_d(a).view_as(b) - b).norm()) <= 1e-3 * float(b.norm()) + 1e-12
+    assert not bool(net.G.any()) and not bool(net.stage.grad.any())
+    net.stage.destroy()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_passes_captured_into_a_graph(dtype):
+    """Lookups, products, gradients, norm and clipped update recorded into one graph
+    and replayed on new inputs between eager work, against the eager calls, bit for bit."""
+    torch = _torch()
+    g = _gen(40)
+    n, vocab, dim, hidden = 9000, 500, 32, 72
+    dt = _dt(dtype)
+    table, W1, W2 = _rows(g, vocab, dim, dt), _rows(g, hidden, dim, dt, scale=0.2), _rows(g, dim, hidden, dt, scale=0.1)
+    b1 = torch.randn(hidden, generator=g).cuda()
+    e = lambda c: torch.empty(n, c, dtype=dt, device="cuda")
+    h0, z1, h1, h2, d1, d0 = e(dim), e(hidden), e(hidden), e(dim), e(hidden), e(dim)
+    tok, dy = torch.zeros(n, dtype=torch.int32, device="cuda"), e(dim)
+    f = lambda *s: torch.zeros(*s, device="cuda")
+    sizes = {"t": (vocab, dim), "W1": (hidden, dim), "b1": (hidden,), "W2": (dim, hidden)}
+    G = {k: f(*s) for k, s in sizes.items()}
+    lst, clip = xp.TensorList(G.values()), f(2)
+    Wt, m, v = f(vocab * dim), f(vocab * dim), f(vocab * dim)
+
+    def work():
+        for x in G.values():
+            x.zero_()
+        xp.xpipe_embedding_fwd(table, tok, h0, scale=2.0)
+        xp.xpipe_linear_fwd(h0, W1, b1, h1, act=xp.ACT_SILU, preact=z1)
+        xp.xpipe_linear_fwd(h1, W2, None, h2, residual=h0)
+        xp.xpipe_linear_bwd(dy, h1, W2, d1, G["W2"], None, act=xp.ACT_SILU, preact=z1)
+        xp.xpipe_linear_bwd(d1, h0, W1, d0, G["W1"], G["b1"], residual=dy)
+        xp.xpipe_embedding_bwd(d0, tok, G["t"], scale=2.0)
+        xp.xpipe_grad_norm(lst, 0.1, clip)
+        xp.xpipe_adam_flat(Wt, m, v, G["t"], xp.Hyper(), 5, zero_grad=False, clip=clip)
+
+    def new_inputs():
+        tok.copy_(_tokens(g, n, vocab, "zipf"))
+        dy.copy_(_rows(g, n, dim, dt))
+        for x in (Wt, m, v):
+            x.copy_(torch.rand(vocab * dim, generator=g).cuda())
+
+    new_inputs()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        work()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        work()
+    for _ in range(4):
+        new_inputs()
+        state = [x.clone() for x in (Wt, m, v)]
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [x.clone() for x in (h0, z1, h1, h2, d1, d0, clip, Wt, m, v, *G.values())]
+        for x, s in zip((Wt, m, v), state):
+            x.copy_(s)
+        work()
+        for a, b in zip(got, (h0, z1, h1, h2, d1, d0, clip, Wt, m, v, *G.values())):
+            assert torch.equal(a, b)
+
+
+def test_workloads_on_two_streams_at_once():
+    """Two calls in flight at the same time have workspaces of their own."""
+    torch = _torch()
+    g = _gen(50)
+    x, W = [_rows(g, 30, 4096, torch.bfloat16) for _ in range(2)], _rows(g, 333, 4096, torch.bfloat16)
+    t, dy = [_tokens(g, 9000, 100, "zipf") for _ in range(2)], [_rows(g, 9000, 64, torch.bfloat16) for _ in range(2)]
+    alone, both = [], []
+    for out, streams in ((alone, [None, None]), (both, [torch.cuda.Stream(), torch.cuda.Stream()])):
+        torch.cuda.synchronize()
+        for k in range(2):
+            y, grad = torch.empty(30, 333, dtype=torch.bfloat16, device="cuda"), torch.zeros(100, 64, device="cuda")
+            out.append((y, grad))
+        torch.cuda.synchronize()
+        for _ in range(5):
+            for k in range(2):
+                xp.xpipe_linear_fwd(x[k], W, None, out[k][0], stream=streams[k])
+                xp.xpipe_embedding_bwd(dy[k], t[k], out[k][1], stream=streams[k])
+        torch.cuda.synchronize()
+    for a, b in zip(alone, both):
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
