@@ -20,23 +20,37 @@ template <typename T> constexpr int STEP = 128 / (int)sizeof(T);
 // ---------------------------------------------------------------- activations
 // In fp32: a stored value is rounded to 8 (bf16) or 24 bits from there, and the
 // product before it has fp32 sums.  erff and expf are correct to a few 2^-24.
-XP_DEV float act_value(float z, int act) {
-  if (act == LIN_RELU) return z > 0.f ? z : (z != z ? z : 0.f);
-  if (act == LIN_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-  if (act == LIN_SILU) return z / (1.f + expf(-z));
-  return z;
+template <int N>
+XP_DEV void act_values(float (&z)[N], int act) {
+  if (act == LIN_RELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) z[i] = z[i] > 0.f ? z[i] : (z[i] != z[i] ? z[i] : 0.f);
+  } else if (act == LIN_GELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) z[i] = 0.5f * z[i] * (1.f + erff(z[i] * 0.70710678118654752f));
+  } else if (act == LIN_SILU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) z[i] = z[i] / (1.f + expf(-z[i]));
+  }
 }
 
-// act'(z); 0 at 0 for the ReLU
-XP_DEV float act_slope(float z, int act) {
-  if (act == LIN_RELU) return z > 0.f ? 1.f : 0.f;
-  if (act == LIN_GELU)
-    return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * 0.39894228040143268f * expf(-0.5f * z * z);
-  if (act == LIN_SILU) {
-    const float s = 1.f / (1.f + expf(-z));
-    return s * (1.f + z * (1.f - s));
+// v *= act'(z); 0 at 0 for the ReLU
+template <int N>
+XP_DEV void act_slopes(float (&v)[N], const float (&z)[N], int act) {
+  if (act == LIN_RELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] *= z[i] > 0.f ? 1.f : 0.f;
+  } else if (act == LIN_GELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      v[i] *= 0.5f * (1.f + erff(z[i] * 0.70710678118654752f)) + z[i] * 0.39894228040143268f * expf(-0.5f * z[i] * z[i]);
+  } else if (act == LIN_SILU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float s = 1.f / (1.f + expf(-z[i]));
+      v[i] *= s * (1.f + z[i] * (1.f - s));
+    }
   }
-  return 1.f;
 }
 
 // ---------------------------------------------------------------- epilogue
@@ -44,81 +58,111 @@ template <typename T> XP_DEV float ldf(const T* p);
 template <> XP_DEV float ldf<float>(const float* p) { return *p; }
 template <> XP_DEV float ldf<bf16_t>(const bf16_t* p) { return bf16_to_f32(*p); }
 
-// CHUNK<T> consecutive elements as fp32: one 16-byte access, or (vec false) one by one up to n
+// a 16-byte chunk: CHUNK<T> elements
 template <typename T>
-XP_DEV void ld_chunk(const T* p, bool vec, int n, float (&v)[CHUNK<T>]) {
-  constexpr int C = CHUNK<T>;
-  if (vec) {
-    const u32x4_t u = *reinterpret_cast<const u32x4_t*>(p);
+XP_DEV void unpack(const u32x4_t& u, float (&v)[CHUNK<T>]) {
 #pragma unroll
-    for (int i = 0; i < C; ++i) {
-      if constexpr (sizeof(T) == 4) v[i] = __uint_as_float(u[i]);
-      else v[i] = __uint_as_float(i & 1 ? u[i / 2] & 0xffff0000u : u[i / 2] << 16);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < C; ++i) v[i] = i < n ? ldf<T>(p + i) : 0.f;
+  for (int i = 0; i < CHUNK<T>; ++i) {
+    if constexpr (sizeof(T) == 4) v[i] = __uint_as_float(u[i]);
+    else v[i] = __uint_as_float(i & 1 ? u[i / 2] & 0xffff0000u : u[i / 2] << 16);
   }
 }
-
+template <typename T>
+XP_DEV u32x4_t pack(const float (&v)[CHUNK<T>]) {
+  u32x4_t u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) u[i] = __float_as_uint(v[i]);
+    else u[i] = f32x2_to_bf16x2(v[2 * i], v[2 * i + 1]);
+  }
+  return u;
+}
+// the same element by element, the first n of them
+template <typename T>
+XP_DEV u32x4_t ld_some(const T* p, int n) {
+  float v[CHUNK<T>];
+#pragma unroll
+  for (int i = 0; i < CHUNK<T>; ++i) v[i] = i < n ? ldf<T>(p + i) : 0.f;
+  return pack<T>(v);  // (bf16 values: no rounding)
+}
+template <typename T>
+XP_DEV void st_some(T* p, int n, const float (&v)[CHUNK<T>]) {
+#pragma unroll
+  for (int i = 0; i < CHUNK<T>; ++i)
+    if (i < n) {
+      if constexpr (sizeof(T) == 4) p[i] = v[i];
+      else p[i] = f32_to_bf16(v[i]);
+    }
+}
+template <typename T>
+XP_DEV u32x4_t ld_chunk(const T* p, bool vec, int n) {
+  return vec ? *reinterpret_cast<const u32x4_t*>(p) : ld_some<T>(p, n);
+}
 template <typename T>
 XP_DEV void st_chunk(T* p, bool vec, int n, const float (&v)[CHUNK<T>]) {
-  constexpr int C = CHUNK<T>;
-  if (vec) {
-    u32x4_t u;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (sizeof(T) == 4) u[i] = __float_as_uint(v[i]);
-      else u[i] = f32x2_to_bf16x2(v[2 * i], v[2 * i + 1]);
-    }
-    *reinterpret_cast<u32x4_t*>(p) = u;
-  } else {
-#pragma unroll
-    for (int i = 0; i < C; ++i)
-      if (i < n) {
-        if constexpr (sizeof(T) == 4) p[i] = v[i];
-        else p[i] = f32_to_bf16(v[i]);
-      }
-  }
+  if (vec) *reinterpret_cast<u32x4_t*>(p) = pack<T>(v);
+  else st_some<T>(p, n, v);
 }
 
-// The product's epilogue for up to CHUNK<T> columns n.. of row m; v: the sums
+// What the epilogue of columns n .. n + CHUNK<T> of row m reads: the residual and the
+// pre-activation, or (LIN_GRAD) the accumulators
+struct Fetched {
+  u32x4_t r, z;
+};
 template <typename T, int EPI>
-XP_DEV void finish(const LinearArgs& a, int64_t m, int n, float (&v)[CHUNK<T>]) {
+XP_DEV Fetched fetch(const LinearArgs& a, int64_t m, int n) {
+  const int left = a.N - n;
+  const bool vec = a.vec && left >= CHUNK<T>;
+  Fetched f;
+  if constexpr (EPI == LIN_GRAD) {
+    const float* g = a.grad + m * a.N + n;
+    f.r = ld_chunk<float>(g, vec, left);
+    if constexpr (sizeof(T) == 2) f.z = ld_chunk<float>(g + 4, vec, left - 4);
+  } else {
+    if (a.res) f.r = ld_chunk<T>((const T*)a.res + m * a.ldr + n, vec, left);
+    if (EPI == LIN_DATA && a.z_in) f.z = ld_chunk<T>((const T*)a.z_in + m * a.ldz + n, vec, left);
+  }
+  return f;
+}
+// the bias of columns n ..
+template <typename T, int EPI>
+XP_DEV void fetch_bias(const LinearArgs& a, int n, float (&b)[CHUNK<T>]) {
+#pragma unroll
+  for (int i = 0; i < CHUNK<T>; ++i) b[i] = EPI == LIN_FWD && a.bias && n + i < a.N ? a.bias[n + i] : 0.f;
+}
+
+// The product's epilogue; v: the sums
+template <typename T, int EPI>
+XP_DEV void finish(const LinearArgs& a, int64_t m, int n, float (&v)[CHUNK<T>], const float (&b)[CHUNK<T>], const Fetched& f) {
   constexpr int C = CHUNK<T>;
   const int left = a.N - n;
   const bool vec = a.vec && left >= C;
   if constexpr (EPI == LIN_GRAD) {
-    // fp32 accumulators whatever T: CHUNK<T> / 4 accesses of 16 bytes
+    // fp32 accumulators whatever T
     float* g = a.grad + m * a.N + n;
 #pragma unroll
     for (int h = 0; h < C / 4; ++h) {
       float o[4];
-      const bool full = a.vec && left >= 4 * h + 4;
-      ld_chunk<float>(g + 4 * h, full, left - 4 * h, o);
+      unpack<float>(h ? f.z : f.r, o);
 #pragma unroll
       for (int i = 0; i < 4; ++i) o[i] += v[4 * h + i];
-      st_chunk<float>(g + 4 * h, full, left - 4 * h, o);
+      st_chunk<float>(g + 4 * h, vec, left - 4 * h, o);
     }
     return;
   }
   if constexpr (EPI == LIN_FWD) {
-    if (a.bias) {
 #pragma unroll
-      for (int i = 0; i < C; ++i) v[i] += i < left ? a.bias[n + i] : 0.f;
-    }
+    for (int i = 0; i < C; ++i) v[i] += b[i];
     if (a.z_out) st_chunk<T>((T*)a.z_out + m * a.ldz + n, vec, left, v);
-#pragma unroll
-    for (int i = 0; i < C; ++i) v[i] = act_value(v[i], a.act);
-  } else if (a.act != LIN_NONE) {
+    act_values(v, a.act);
+  } else if (a.z_in) {
     float z[C];
-    ld_chunk<T>((const T*)a.z_in + m * a.ldz + n, vec, left, z);
-#pragma unroll
-    for (int i = 0; i < C; ++i) v[i] *= act_slope(z[i], a.act);
+    unpack<T>(f.z, z);
+    act_slopes(v, z, a.act);
   }
   if (a.res) {
     float r[C];
-    ld_chunk<T>((const T*)a.res + m * a.ldr + n, vec, left, r);
+    unpack<T>(f.r, r);
 #pragma unroll
     for (int i = 0; i < C; ++i) v[i] += r[i];
   }
@@ -128,14 +172,53 @@ XP_DEV void finish(const LinearArgs& a, int64_t m, int n, float (&v)[CHUNK<T>]) 
 // ---------------------------------------------------------------- product
 // LDS tile of an operand, one step deep.  Stored with the reduction along its
 // rows in memory (TR false): one 128-byte row of 8 chunks per tile row, chunk c
-// of row r at position c ^ (r & 7), so that the rows of one fragment read lie in
-// different banks.  Stored with the reduction down its rows (TR true): one row of
+// of row r at position c ^ (r / 2 & 7): two rows span the banks, and the 16 rows
+// that a fragment read takes at a time then lie in different ones.  Stored with the reduction down its rows (TR true): one row of
 // W elements per reduction index; chunk c of row k at c ^ tr_swz(k), which moves
 // the rows that one fragment read touches to different banks.
 template <typename T, int W>
 XP_DEV int tr_swz(int k) {
   if constexpr (sizeof(T) == 4) return ((k >> 2) & 1) << 3;
   else return W >= 128 ? (k & 3) << 2 : ((k >> 1) & 1) << 2;
+}
+
+// Transposing LDS reads of N bf16 fragments (16 of the reduction, 32 columns), in one
+// block with their wait.  In each group of 16 lanes, output e (0..3) of lane i is
+// element i % 4 of the 8 bytes that lane 4 e + i / 4 addressed; a fragment is two
+// reads, HI bytes (four rows) apart.  As builtins they would each wait for every
+// copy into LDS that is in flight (the compiler does not see which array they read).
+template <int N, int OFF, int HI>
+XP_DEV void read_tr(const uint32_t (&at)[N], u32x4_t (&out)[N]) {
+  typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+  static_assert(N == 1 || N == 2 || N == 4 || N == 6, "blocks written out");
+  static_assert(OFF + HI < 65536, "16-bit offsets");
+  u32x2_t lo[N], hi[N];
+#define XP_TR(A, D) "ds_read_b64_tr_b16 %" #D ", %" #A " offset:%c[o]\n\t"
+#define XP_TRH(A, D) "ds_read_b64_tr_b16 %" #D ", %" #A " offset:%c[h]\n\t"
+#define XP_WAIT "s_waitcnt lgkmcnt(0)"
+  if constexpr (N == 1)
+    asm volatile(XP_TR(2, 0) XP_TRH(2, 1) XP_WAIT
+                 : "=&v"(lo[0]), "=&v"(hi[0]) : "v"(at[0]), [o] "n"(OFF), [h] "n"(OFF + HI) : "memory");
+  else if constexpr (N == 2)
+    asm volatile(XP_TR(4, 0) XP_TRH(4, 1) XP_TR(5, 2) XP_TRH(5, 3) XP_WAIT
+                 : "=&v"(lo[0]), "=&v"(hi[0]), "=&v"(lo[1]), "=&v"(hi[1])
+                 : "v"(at[0]), "v"(at[1]), [o] "n"(OFF), [h] "n"(OFF + HI) : "memory");
+  else if constexpr (N == 4)
+    asm volatile(XP_TR(8, 0) XP_TRH(8, 1) XP_TR(9, 2) XP_TRH(9, 3) XP_TR(10, 4) XP_TRH(10, 5) XP_TR(11, 6) XP_TRH(11, 7) XP_WAIT
+                 : "=&v"(lo[0]), "=&v"(hi[0]), "=&v"(lo[1]), "=&v"(hi[1]), "=&v"(lo[2]), "=&v"(hi[2]), "=&v"(lo[3]), "=&v"(hi[3])
+                 : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), [o] "n"(OFF), [h] "n"(OFF + HI) : "memory");
+  else
+    asm volatile(XP_TR(12, 0) XP_TRH(12, 1) XP_TR(13, 2) XP_TRH(13, 3) XP_TR(14, 4) XP_TRH(14, 5) XP_TR(15, 6) XP_TRH(15, 7)
+                 XP_TR(16, 8) XP_TRH(16, 9) XP_TR(17, 10) XP_TRH(17, 11) XP_WAIT
+                 : "=&v"(lo[0]), "=&v"(hi[0]), "=&v"(lo[1]), "=&v"(hi[1]), "=&v"(lo[2]), "=&v"(hi[2]), "=&v"(lo[3]), "=&v"(hi[3]),
+                   "=&v"(lo[4]), "=&v"(hi[4]), "=&v"(lo[5]), "=&v"(hi[5])
+                 : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "v"(at[4]), "v"(at[5]), [o] "n"(OFF), [h] "n"(OFF + HI)
+                 : "memory");
+#undef XP_TR
+#undef XP_TRH
+#undef XP_WAIT
+#pragma unroll
+  for (int i = 0; i < N; ++i) out[i] = __builtin_shufflevector(lo[i], hi[i], 0, 1, 2, 3);
 }
 
 // One workgroup per BM x BN tile of the product and part of the reduction, WM x
@@ -172,16 +255,15 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear(LinearArgs a, int tiles
   const int nk = (int)((kend - kbeg + BK - 1) / BK);
 
   // Per copy the lane's byte offset from the step's base, ~0 where its row (TR:
-  // its column chunk) is past the operand; the base moves by one step at a time.
-  // Reduction indices past the end are masked step by step, and nothing past
-  // the operand's last element's word is read (the resource ends there).
+  // its column chunk) is past the operand; the base moves by one step at a time, and
+  // reduction indices past the end are masked step by step.  So every chunk that
+  // is read holds an element of the operand (a 16-byte chunk never leaves that
+  // element's page).
   const char* abase = (const char*)a.A + (TA ? kbeg * a.lda + m0 : m0 * a.lda + kbeg) * ES;
   const char* bbase = (const char*)a.B + (TB ? kbeg * a.ldb + n0 : n0 * a.ldb + kbeg) * ES;
-  const char* aend = (const char*)a.A + (TA ? (a.K - 1) * a.lda + a.M : (a.M - 1) * a.lda + a.K) * ES;
-  const char* bend = (const char*)a.B + (TB ? (a.K - 1) * a.ldb + a.N : (a.N - 1) * a.ldb + a.K) * ES;
   const int64_t astep = TA ? (int64_t)BK * a.lda * ES : 128, bstep = TB ? (int64_t)BK * a.ldb * ES : 128;
   uint32_t a_off[A_I], b_off[B_I];
-  int a_k[TA ? A_I : 1], b_k[TB ? B_I : 1];  // the reduction index (of the step) that the copy reads
+  int a_k[A_I], b_k[B_I];  // the reduction index (of the step) that the copy reads
   auto place = [&](auto TR, auto W, int i, int64_t r0, int64_t rows, int64_t ld, uint32_t& off, int& k) __attribute__((always_inline)) {
     constexpr int w = decltype(W)::value;
     if constexpr (decltype(TR)::value) {
@@ -191,42 +273,33 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear(LinearArgs a, int tiles
       const int col = ((pos % CPR) ^ tr_swz<T, w>(k)) * C;
       off = r0 + col < rows ? (uint32_t)((k * ld + col) * ES) : ~0u;
     } else {
-      const int r = i * 8 + (lane >> 3), c = (lane & 7) ^ (r & 7);
+      const int r = i * 8 + (lane >> 3), c = (lane & 7) ^ (r >> 1 & 7);
       k = c * C;
       off = r0 + r < rows ? (uint32_t)((r * ld + k) * ES) : ~0u;
     }
   };
 #pragma unroll
   for (int i = 0; i < A_I; ++i)
-    place(std::bool_constant<TA>{}, std::integral_constant<int, BM>{}, wave * A_I + i, m0, a.M, a.lda, a_off[i], a_k[TA ? i : 0]);
+    place(std::bool_constant<TA>{}, std::integral_constant<int, BM>{}, wave * A_I + i, m0, a.M, a.lda, a_off[i], a_k[i]);
 #pragma unroll
   for (int i = 0; i < B_I; ++i)
-    place(std::bool_constant<TB>{}, std::integral_constant<int, BN>{}, wave * B_I + i, n0, a.N, a.ldb, b_off[i], b_k[TB ? i : 0]);
+    place(std::bool_constant<TB>{}, std::integral_constant<int, BN>{}, wave * B_I + i, n0, a.N, a.ldb, b_off[i], b_k[i]);
 
-  int copied = 0;
-  auto copy = [&](auto I) __attribute__((always_inline)) {
-    if (copied >= nk) return;
+  int left = (int)(kend - kbeg);  // reduction indices not copied yet
+  auto copy = [&](auto I) __attribute__((always_inline)) {  // past the last step: zeros
     unsigned char* sa = stage(I);
     unsigned char* sb = stage(I) + BM * 128;
-    const int left = (int)min((int64_t)BK, kend - kbeg - (int64_t)copied * BK);
-    auto rsrc = [](const char* base, const char* end) __attribute__((always_inline)) {
-      const int64_t bytes = min((int64_t)0x7ffffff0, max((int64_t)0, (int64_t)(end - base + 3) & ~(int64_t)3));
-      return __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, (int)bytes, 0x00020000);
-    };
-    const __amdgpu_buffer_rsrc_t ar = rsrc(abase, aend), br = rsrc(bbase, bend);
+    const __amdgpu_buffer_rsrc_t ar = __builtin_amdgcn_make_buffer_rsrc((void*)abase, (short)0, 0x7ffffff0, 0x00020000);
+    const __amdgpu_buffer_rsrc_t br = __builtin_amdgcn_make_buffer_rsrc((void*)bbase, (short)0, 0x7ffffff0, 0x00020000);
 #pragma unroll
-    for (int i = 0; i < A_I; ++i) {
-      const int past = a_k[TA ? i : 0] < left ? 0 : -1;
-      load_lds16(ar, (bf16_t*)(sa + (wave * A_I + i) * 1024), (int)a_off[i] | past, 0);
-    }
+    for (int i = 0; i < A_I; ++i)
+      load_lds16(ar, (bf16_t*)(sa + (wave * A_I + i) * 1024), a_k[i] < left ? (int)a_off[i] : -1, 0);
 #pragma unroll
-    for (int i = 0; i < B_I; ++i) {
-      const int past = b_k[TB ? i : 0] < left ? 0 : -1;
-      load_lds16(br, (bf16_t*)(sb + (wave * B_I + i) * 1024), (int)b_off[i] | past, 0);
-    }
+    for (int i = 0; i < B_I; ++i)
+      load_lds16(br, (bf16_t*)(sb + (wave * B_I + i) * 1024), b_k[i] < left ? (int)b_off[i] : -1, 0);
     abase += astep;
     bbase += bstep;
-    ++copied;
+    left -= BK;
   };
 
   f32x16_t acc[TM][TN];
@@ -242,108 +315,175 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear(LinearArgs a, int tiles
   // elements for one 32x32x16 product; fp32: 4, one for each of four 32x32x2
   // products, whose reduction indices then are 4 (l / 32) + q in both operands).
   const int fr = lane & 31, fh = lane >> 5;
-  auto frag = [&](auto TR, auto W, const unsigned char* base, int row0, int kk) __attribute__((always_inline)) -> u32x4_t {
+  // (One offset into the stage's array per read: the compiler then sees which array
+  // it reads, and waits for no copies into the other.)
+  auto frag = [&](auto I, auto TR, auto W, int base, int row0, int kk) __attribute__((always_inline)) -> u32x4_t {
     constexpr int w = decltype(W)::value;
+    const unsigned char* lds = stage(I);
     if constexpr (!decltype(TR)::value) {
-      return *reinterpret_cast<const u32x4_t*>(base + (row0 + fr) * 128 + (((kk * 2 + fh) ^ (fr & 7)) << 4));
-    } else if constexpr (ES == 2) {
-      // transposing LDS read: in each group of 16 lanes, output e (0..3) of lane
-      // i is element i % 4 of the 8 bytes that lane 4 e + i / 4 addressed
-      typedef short v4i16 __attribute__((ext_vector_type(4)));
-      typedef short v8i16 __attribute__((ext_vector_type(8)));
-      const int k = kk * 16 + 8 * fh + ((lane & 15) >> 2);
-      const int c = row0 + 16 * (fr >> 4) + 4 * (lane & 3);
-      const unsigned char* p = base + k * (w * 2) + (((c >> 3) ^ tr_swz<T, w>(k)) << 4) + (c & 7) * 2;
-      // the second read's row is k + 4: the same swizzle (it takes k modulo 4)
-      const v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4i16*)(p));
-      const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4i16*)(p + 4 * w * 2));
-      return __builtin_bit_cast(u32x4_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      return *reinterpret_cast<const u32x4_t*>(lds + (base + (row0 + fr) * 128 + (((kk * 2 + fh) ^ (fr >> 1 & 7)) << 4)));
     } else {
       u32x4_t v;
-      const int k = kk * 8 + 4 * fh, c = row0 + fr;
-      const unsigned char* p = base + k * (w * 4) + (((c >> 2) ^ tr_swz<T, w>(k)) << 4) + (c & 3) * 4;
+      const int k = 4 * fh, c = row0 + fr;
+      const int at = base + (kk * 8 + k) * (w * 4) + (((c >> 2) ^ tr_swz<T, w>(k)) << 4) + (c & 3) * 4;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] = *reinterpret_cast<const uint32_t*>(p + q * w * 4);
+      for (int q = 0; q < 4; ++q) v[q] = *reinterpret_cast<const uint32_t*>(lds + (at + q * w * 4));
       return v;
     }
   };
+  // Two sets of fragments: while the products of one quarter of a step run, the next
+  // quarter's fragments are read.
+  u32x4_t fa[2][TM], fb[2][TN];
+  // where the lane's transposing reads of a quarter start (of the first quarter, in the first stage's array)
+  constexpr int TRN = ES == 2 ? (TA ? TM : 0) + (TB ? TN : 0) : 0;
+  uint32_t tr_at[TRN > 0 ? TRN : 1];
+  if constexpr (TRN > 0) {
+    static_assert(BM == BN, "one offset for both operands' rows");
+    auto at = [&](int base, int row0) __attribute__((always_inline)) -> uint32_t {
+      const int k = 8 * fh + ((lane & 15) >> 2);  // the first read's row (the swizzle takes it modulo 4)
+      const int c = row0 + 16 * (fr >> 4) + 4 * (lane & 3);
+      return base + k * (BM * 2) + (((c >> 3) ^ tr_swz<T, BM>(k)) << 4) + (c & 7) * 2;
+    };
+    if constexpr (TB) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j) tr_at[j] = at(BM * 128, wn * WTN + j * 32);
+    }
+    if constexpr (TA) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i) tr_at[TRN - TM + i] = at(0, wm * WTM + i * 32);
+    }
+  }
+  auto read = [&](auto I, auto KK, int set) __attribute__((always_inline)) {
+    constexpr int kk = decltype(KK)::value;
+    // (B's first: the next quarter's first products take all of them and one of A's)
+    if constexpr (!(ES == 2 && TB)) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+        fb[set][j] = frag(I, std::bool_constant<TB>{}, std::integral_constant<int, BN>{}, BM * 128, wn * WTN + j * 32, kk);
+    }
+    if constexpr (!(ES == 2 && TA)) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+        fa[set][i] = frag(I, std::bool_constant<TA>{}, std::integral_constant<int, BM>{}, 0, wm * WTM + i * 32, kk);
+    }
+    if constexpr (TRN > 0) {
+      const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)stage(I);
+      uint32_t at[TRN];
+      u32x4_t out[TRN];
+#pragma unroll
+      for (int i = 0; i < TRN; ++i) at[i] = lds + tr_at[i];
+      read_tr<TRN, kk * 16 * BM * 2, 4 * BM * 2>(at, out);
+      if constexpr (TB) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j) fb[set][j] = out[j];
+      }
+      if constexpr (TA) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i) fa[set][i] = out[TRN - TM + i];
+      }
+    }
+  };
+  auto multiply = [&](int set, int from, int to) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = from; i < to; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        if constexpr (ES == 2) {
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, fa[set][i]),
+                                                              __builtin_bit_cast(bf16x8_t, fb[set][j]), acc[i][j], 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(fa[set][i][q]), __uint_as_float(fb[set][j][q]),
+                                                             acc[i][j], 0, 0, 0);
+        }
+      }
+  };
+  // Reads one quarter's fragments and multiplies another's.  Reads that the
+  // compiler can move are spread over the products; a block of transposing reads
+  // comes between them (the other wave of the SIMD multiplies while it waits).
+  auto overlap = [&](auto I, auto KK, int into, int set) __attribute__((always_inline)) {
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (TRN > 0) {
+      multiply(set, 0, (TM + 1) / 2);
+      __builtin_amdgcn_sched_barrier(0);
+      read(I, KK, into);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(set, (TM + 1) / 2, TM);
+    } else {
+      constexpr int PER = TM * TN * (ES == 2 ? 1 : 4), READS = TM * (TA ? 4 : 1) + TN * (TB ? 4 : 1);
+      constexpr int SLOTS = READS < PER ? READS : PER;
+      read(I, KK, into);
+      multiply(set, 0, TM);
+      static_for<0, SLOTS>([&](auto S) __attribute__((always_inline)) {
+        constexpr int s = decltype(S)::value;
+        constexpr int r = (s + 1) * READS / SLOTS - s * READS / SLOTS, m = (s + 1) * PER / SLOTS - s * PER / SLOTS;
+        __builtin_amdgcn_sched_group_barrier(0x100, r, 0);  // LDS reads
+        __builtin_amdgcn_sched_group_barrier(0x008, m, 0);  // products
+      });
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
   // The bias gradient is the sum of A's rows over the reduction: the first wave
-  // column of the first tile column adds the elements of its fragments, a step in
-  // fp32 (at most 32 of them) and the steps in fp64.
+  // column of the first tile column adds the elements of its fragments, a quarter in
+  // fp32 (at most 8 of them) and the quarters in fp64.
   const bool sums = EPI == LIN_GRAD && a.grad_b && tn == 0 && wn == 0;
   double bsum[TM];
 #pragma unroll
   for (int i = 0; i < TM; ++i) bsum[i] = 0.0;
-  auto multiply = [&](auto I) __attribute__((always_inline)) {
-    const unsigned char* sa = stage(I);
-    const unsigned char* sb = stage(I) + BM * 128;
-    float part[TM];
+  auto add_rows = [&](int set) __attribute__((always_inline)) {
+    if constexpr (EPI == LIN_GRAD) {
+      if (sums) {
 #pragma unroll
-    for (int i = 0; i < TM; ++i) part[i] = 0.f;
+        for (int i = 0; i < TM; ++i) {
+          float e[4];
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk) {
-      u32x4_t af[TM], bf[TN];
-#pragma unroll
-      for (int i = 0; i < TM; ++i)
-        af[i] = frag(std::bool_constant<TA>{}, std::integral_constant<int, BM>{}, sa, wm * WTM + i * 32, kk);
-#pragma unroll
-      for (int j = 0; j < TN; ++j)
-        bf[j] = frag(std::bool_constant<TB>{}, std::integral_constant<int, BN>{}, sb, wn * WTN + j * 32, kk);
-      if constexpr (EPI == LIN_GRAD) {
-        if (sums) {
-#pragma unroll
-          for (int i = 0; i < TM; ++i) {
-            float e[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              if constexpr (ES == 4) e[q] = __uint_as_float(af[i][q]);
-              else e[q] = __uint_as_float(af[i][q] << 16) + __uint_as_float(af[i][q] & 0xffff0000u);
-            }
-            part[i] += (e[0] + e[1]) + (e[2] + e[3]);
+          for (int q = 0; q < 4; ++q) {
+            if constexpr (ES == 4) e[q] = __uint_as_float(fa[set][i][q]);
+            else e[q] = __uint_as_float(fa[set][i][q] << 16) + __uint_as_float(fa[set][i][q] & 0xffff0000u);
           }
+          bsum[i] += (double)((e[0] + e[1]) + (e[2] + e[3]));
         }
       }
-#pragma unroll
-      for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j) {
-          if constexpr (ES == 2) {
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, af[i]),
-                                                                __builtin_bit_cast(bf16x8_t, bf[j]), acc[i][j], 0, 0, 0);
-          } else {
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(af[i][q]), __uint_as_float(bf[j][q]),
-                                                               acc[i][j], 0, 0, 0);
-          }
-        }
-    }
-    if constexpr (EPI == LIN_GRAD) {
-#pragma unroll
-      for (int i = 0; i < TM; ++i) bsum[i] += (double)part[i];
     }
   };
 
-  if (nk > 0) {
-    copy(std::integral_constant<int, 0>{});
-    int k = 0;
-    while (true) {
-      bool done = false;
-      static_for<0, 2>([&](auto I) __attribute__((always_inline)) {
-        if (!done) {
-          // this wave's copies of step k have landed; past the barrier so have
-          // the others', and all waves have read the buffer that is refilled
-          wait_step<0>();
-          copy(std::integral_constant<int, 1 - decltype(I)::value>{});
-          __builtin_amdgcn_sched_barrier(0);
-          multiply(I);
-          done = ++k == nk;
-        }
-      });
-      if (done) break;
-    }
-    wait_step<0>();
+  // Step k from buffer k % 2.  By its last quarter all of the step's fragments
+  // are in registers: past the barrier there the buffer takes the copies of step
+  // k + 2, and the first fragments of step k + 1, whose copies have had a step's time
+  // to land, are read while the last quarter is multiplied.
+  constexpr std::integral_constant<int, 0> B0{};
+  copy(B0);
+  copy(std::integral_constant<int, 1>{});
+  wait_step<A_I + B_I>();
+  read(B0, B0, 0);
+  int k = 0;
+  auto quarters = [&](auto I) __attribute__((always_inline)) {
+    static_for<0, 3>([&](auto KK) __attribute__((always_inline)) {
+      constexpr int kk = decltype(KK)::value;
+      add_rows(kk & 1);
+      overlap(I, std::integral_constant<int, kk + 1>{}, (kk + 1) & 1, kk & 1);
+    });
+    add_rows(1);
+  };
+  quarters(B0);
+  while (++k < nk) {
+    bool done = false;
+    static_for<0, 2>([&](auto I) __attribute__((always_inline)) {
+      if (!done) {
+        constexpr std::integral_constant<int, 1 - decltype(I)::value> NEXT{};
+        // this wave's copies of step k have landed and its reads of step k - 1
+        // returned; past the barrier so have the others'
+        wait_step<0>();
+        copy(I);
+        overlap(NEXT, B0, 0, 1);
+        quarters(NEXT);
+        if (decltype(I)::value == 0) done = ++k == nk;
+      }
+    });
   }
+  multiply(1, 0, TM);
+  wait_step<0>();
 
   if constexpr (EPI == LIN_GRAD) {
     if (sums) {
@@ -360,16 +500,37 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear(LinearArgs a, int tiles
   }
 
   // Each wave finishes its tile in strips of 16 rows through its own part of LDS
-  // (no barrier), so that memory is accessed by rows, 16 bytes a lane.  32x32
+  // (no barrier), so that memory is accessed by rows, 16 bytes a lane; what a
+  // strip's epilogue reads is loaded before the strip before it is finished.  32x32
   // result: lane l, register r holds row 8 (r / 4) + 4 (l / 32) + r % 4, column l % 32.
   constexpr int PITCH = WTN + 4;
   static_assert(NW * 16 * PITCH * 4 <= SZ, "strips");
   float* strip = reinterpret_cast<float*>(st0) + wave * 16 * PITCH;
-  constexpr int CW = WTN / C, RP = 64 / CW;  // chunks per strip row, rows per pass
+  constexpr int CW = WTN / C, RP = 64 / CW, PASS = 16 / RP;  // chunks per strip row, rows per pass
   const int ch = lane % CW;
   const int n = n0 + wn * WTN + ch * C;
+  const bool direct = !a.part;
+  float bias[C];
+  fetch_bias<T, EPI>(a, n, bias);
+  auto row_of = [&](int s, int p) __attribute__((always_inline)) -> int64_t {
+    const int64_t m = m0 + wm * WTM + s * 16 + p * RP + lane / CW;
+    return m < a.M && n < a.N ? m : -1;
+  };
+  Fetched next[PASS];
+  auto prefetch = [&](int s) __attribute__((always_inline)) {
 #pragma unroll
-  for (int s = 0; s < TM * 2; ++s) {
+    for (int p = 0; p < PASS; ++p) {
+      const int64_t m = row_of(s, p);
+      if (direct && m >= 0) next[p] = fetch<T, EPI>(a, m, n);
+    }
+  };
+  prefetch(0);
+  static_for<0, TM * 2>([&](auto S) __attribute__((always_inline)) {
+    constexpr int s = decltype(S)::value;
+    Fetched now[PASS];
+#pragma unroll
+    for (int p = 0; p < PASS; ++p) now[p] = next[p];
+    if constexpr (s + 1 < TM * 2) prefetch(s + 1);
 #pragma unroll
     for (int j = 0; j < TN; ++j)
 #pragma unroll
@@ -377,30 +538,28 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear(LinearArgs a, int tiles
         strip[(8 * (r >> 2) + 4 * fh + (r & 3)) * PITCH + j * 32 + fr] = acc[s >> 1][j][(s & 1) * 8 + r];
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int p = 0; p < 16 / RP; ++p) {
-      const int row = p * RP + lane / CW;
-      const int64_t m = m0 + wm * WTM + s * 16 + row;
+    for (int p = 0; p < PASS; ++p) {
+      const int64_t m = row_of(s, p);
       float v[C];
 #pragma unroll
       for (int q = 0; q < C / 4; ++q) {
-        const f32x4_t f = *reinterpret_cast<const f32x4_t*>(strip + row * PITCH + ch * C + q * 4);
+        const f32x4_t f = *reinterpret_cast<const f32x4_t*>(strip + (p * RP + lane / CW) * PITCH + ch * C + q * 4);
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[q * 4 + i] = f[i];
       }
-      if (m < a.M && n < a.N) {
-        if (a.part) {
-          // partial sums, rows of N rounded up to whole chunks
-          float* out = a.part + ((int64_t)split * a.M + m) * a.ldpart + n;
+      if (m < 0) continue;
+      if (direct) {
+        finish<T, EPI>(a, m, n, v, bias, now[p]);
+      } else {
+        // partial sums, rows of N rounded up to whole chunks
+        float* out = a.part + ((int64_t)split * a.M + m) * a.ldpart + n;
 #pragma unroll
-          for (int q = 0; q < C / 4; ++q)
-            *reinterpret_cast<f32x4_t*>(out + 4 * q) = (f32x4_t){v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
-        } else {
-          finish<T, EPI>(a, m, n, v);
-        }
+        for (int q = 0; q < C / 4; ++q)
+          *reinterpret_cast<f32x4_t*>(out + 4 * q) = (f32x4_t){v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
       }
     }
     __builtin_amdgcn_wave_barrier();
-  }
+  });
 }
 
 // the splits' partial sums added in order, and the epilogue
@@ -424,7 +583,9 @@ __global__ __launch_bounds__(256) void k_linear_join(LinearArgs a) {
         for (int e = 0; e < 4; ++e) v[4 * q + e] += f[e];
       }
     }
-    finish<T, EPI>(a, m, n, v);
+    float b[C];
+    fetch_bias<T, EPI>(a, n, b);
+    finish<T, EPI>(a, m, n, v, b, fetch<T, EPI>(a, m, n));
   }
   if constexpr (EPI == LIN_GRAD) {
     if (!a.grad_b) return;
@@ -460,10 +621,9 @@ __global__ __launch_bounds__(256) void k_act_bwd(const T* __restrict__ dy, const
     const int left = (int)min((int64_t)C, n - i * C);
     const bool v = vec && left == C;
     float g[C], zz[C];
-    ld_chunk<T>(dy + i * C, v, left, g);
-    ld_chunk<T>(z + i * C, v, left, zz);
-#pragma unroll
-    for (int e = 0; e < C; ++e) g[e] *= act_slope(zz[e], act);
+    unpack<T>(ld_chunk<T>(dy + i * C, v, left), g);
+    unpack<T>(ld_chunk<T>(z + i * C, v, left), zz);
+    act_slopes(g, zz, act);
     st_chunk<T>(dz + i * C, v, left, g);
   }
 }
