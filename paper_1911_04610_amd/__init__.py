@@ -406,7 +406,7 @@ class Stage:
         update (xpipe_grad_norm over several buffers)."""
         ws, size = None, _SZ(0)
         if norm_coef is not None:
-            _check_norm_coef(norm_coef, self.grad.device)
+            _check_norm_coef(norm_coef, self.grad.get_device())
             if max_norm > 0:
                 import torch
                 one = TensorDesc(_ptr(self.grad), self.P)
@@ -476,7 +476,7 @@ def xpipe_rule_flat(W, buf, sq, m, v, G, rule: Rule, hp: Hyper, t: int, zero_gra
     """clip: {norm, coefficient} of xpipe_grad_norm; the update reads G times the coefficient."""
     r, c = rule.c(), hp.c(t)
     if clip is not None:
-        _check_norm_coef(clip, W.device)
+        _check_norm_coef(clip, W.get_device())
         _check(lib().xpipe_rule_flat_clipped(_ptr(W), _ptr(buf), _ptr(sq), _ptr(m), _ptr(v), _ptr(G), W.numel(),
                                              ctypes.byref(r), ctypes.byref(c), int(zero_grad), _ptr(pred_fwd), s_fwd,
                                              _ptr(pred_bwd), s_bwd, _ptr(clip), _stream_ptr(stream)))
@@ -525,7 +525,7 @@ def xpipe_adam_flat(W, m, v, G, hp: Hyper, t: int, zero_grad=True, pred_fwd=None
     """clip: {norm, coefficient} of xpipe_grad_norm; the update reads G times the coefficient."""
     c = hp.c(t)
     if clip is not None:
-        _check_norm_coef(clip, W.device)
+        _check_norm_coef(clip, W.get_device())
         _check(lib().xpipe_adam_flat_clipped(_ptr(W), _ptr(m), _ptr(v), _ptr(G), W.numel(), ctypes.byref(c),
                                              int(zero_grad), _ptr(pred_fwd), s_fwd, _ptr(pred_bwd), s_bwd,
                                              _ptr(clip), _stream_ptr(stream)))
@@ -536,118 +536,103 @@ def xpipe_adam_flat(W, m, v, G, hp: Hyper, t: int, zero_grad=True, pred_fwd=None
 
 
 # ---------------------------------------------------------------- operators around a stage
-def _need(ok, msg):
-    if not ok:
-        raise ValueError(msg)
-
-
-def _check_norm_coef(t, device):
+# (checks come as `if`s, so that a message is only made where one fails: a small
+# call's time is the host's)
+def _check_norm_coef(t, dev: int):
     import torch
-    _need(t.dtype == torch.float32 and t.numel() == 2 and t.is_contiguous() and t.device == device,
-          "{norm, coefficient}: two contiguous float32 elements on the gradients' device")
+    if t.dtype is not torch.float32 or t.numel() != 2 or not t.is_contiguous() or t.get_device() != dev:
+        raise ValueError("{norm, coefficient}: two contiguous float32 elements on the gradients' device expected")
 
 
 def _dtype_of(t) -> int:
     import torch
-    _need(t.dtype in (torch.bfloat16, torch.float32), f"bfloat16 or float32, not {t.dtype}")
-    return BF16 if t.dtype == torch.bfloat16 else F32
+    if t.dtype is torch.bfloat16:
+        return BF16
+    if t.dtype is torch.float32:
+        return F32
+    raise ValueError(f"bfloat16 or float32 expected, not {t.dtype}")
 
 
-def _matrix(name, t, like, shape):
-    """Row pitch (elements) of a 2-D tensor of `like`'s type and device with contiguous rows."""
-    _need(t.dtype == like.dtype and t.device == like.device, f"{name}: another type or device")
-    _need(tuple(t.shape) == tuple(shape), f"{name}: shape {tuple(t.shape)}, {tuple(shape)} expected")
-    if t.shape[0] <= 1:
-        _need(t.shape[1] <= 1 or t.stride(1) == 1, f"{name}: rows must be contiguous")
-        return t.shape[1]
-    _need((t.shape[1] <= 1 or t.stride(1) == 1) and t.stride(0) >= t.shape[1], f"{name}: rows must be contiguous")
-    return t.stride(0)
+def _matrix(name, t, like, rows, cols):
+    """(pointer, row pitch in elements) of a [rows, cols] tensor of `like`'s type and device, its rows contiguous."""
+    if t is None:
+        return None, 0
+    if t.dtype is not like.dtype or t.get_device() != like.get_device():
+        raise ValueError(f"{name}: another type or device")
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, ({rows}, {cols}) expected")
+    ld, inner = t.stride()
+    if rows <= 1:
+        ld = cols
+    if ld < cols or (inner != 1 and cols > 1):
+        raise ValueError(f"{name}: rows must be contiguous")
+    return t.data_ptr(), ld
 
 
 def _vector(name, t, like, n):
     import torch
-    _need(t.dtype == torch.float32 and t.device == like.device and t.is_contiguous() and t.numel() == n,
-          f"{name}: {n} contiguous float32 elements on the same device expected")
+    if t is None:
+        return None
+    if t.dtype is not torch.float32 or t.get_device() != like.get_device() or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name}: {n} contiguous float32 elements on the same device expected")
+    return t.data_ptr()
 
 
-class _On:
-    """Makes a tensor's device current for a call; gives the stream and the workspace there."""
-
-    def __init__(self, t, stream):
-        import torch
-        self.ctx = None
-        _need(t.is_cuda, "tensors must be on the GPU")
-        if t.device.index != torch.cuda.current_device():
-            self.ctx = torch.cuda.device(t.device)
-        self.device, self.stream = t.device, stream
-
-    def __enter__(self):
-        import torch
-        if self.ctx is not None:
-            self.ctx.__enter__()
-        if self.stream is not None and self.stream.device != self.device:
-            self.__exit__(None, None, None)
-            raise ValueError("the stream is another device's")
-        self.own_stream = self.stream is None
-        if self.own_stream:
-            self.stream = torch.cuda.current_stream()
-        self.ptr = self.stream.cuda_stream
-        return self
-
-    def workspace(self, need, given):
-        """(pointer, bytes, tensor to keep until the call returns)."""
-        import torch
-        if need == 0:
-            return None, 0, None
-        if given is not None:
-            _need(given.device == self.device and given.is_contiguous(), "workspace: contiguous, on the same device")
-            base, size = given.data_ptr(), given.numel() * given.element_size()
-            skip = -base % 256
-            return base + skip, max(0, size - skip), given
-        if self.own_stream:
-            ws = torch.empty(need + 256, dtype=torch.uint8, device=self.device)
-        else:  # the allocator then gives it out again in that stream's order
-            with torch.cuda.stream(self.stream):
-                ws = torch.empty(need + 256, dtype=torch.uint8, device=self.device)
-        skip = -ws.data_ptr() % 256
-        return ws.data_ptr() + skip, need, ws
-
-    def __exit__(self, *exc):
-        if self.ctx is not None:
-            self.ctx.__exit__(*exc)
+def _elsewhere(t) -> bool:
+    """True where the tensor's GPU is not the current one; raises for a CPU tensor."""
+    import torch
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError("tensors on the GPU expected")
+    return dev != torch.cuda.current_device()
 
 
-def _ld(a, name, t, like, shape, field):
-    if t is not None:
-        setattr(a, field[0], t.data_ptr())
-        setattr(a, field[1], _matrix(name, t, like, shape))
+def _raw_stream(t, stream):
+    """The HIP stream of a call on t's device (the current one): `stream`, or the device's current stream."""
+    import torch
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(t.get_device())
+    if stream.device.index != t.get_device():
+        raise ValueError("the stream is another device's")
+    return stream.cuda_stream
 
 
-def _linear_fwd_args(x, W, bias, y, act, residual, preact):
-    _need(x.dim() == 2 and W.dim() == 2 and W.shape[1] == x.shape[1], "x [rows, cin] and W [cout, cin] expected")
-    (rows, cin), cout = x.shape, W.shape[0]
-    a = LinearFwdArgs(rows=rows, cin=cin, cout=cout, dtype=_dtype_of(x), act=int(act))
-    _ld(a, "x", x, x, (rows, cin), ("x", "ldx"))
-    _ld(a, "W", W, x, (cout, cin), ("W", "ldw"))
-    _ld(a, "residual", residual, x, (rows, cout), ("residual", "ldr"))
-    _ld(a, "preact", preact, x, (rows, cout), ("preact", "ldz"))
-    _ld(a, "y", y, x, (rows, cout), ("y", "ldy"))
-    if bias is not None:
-        _vector("bias", bias, x, cout)
-        a.bias = bias.data_ptr()
-    return a
+def _workspace(need, given, t, stream):
+    """(pointer, bytes, tensor to hold during the call) of a 256-byte aligned workspace."""
+    import torch
+    if need == 0:
+        return None, 0, None
+    if given is not None:
+        if given.get_device() != t.get_device() or not given.is_contiguous():
+            raise ValueError("workspace: contiguous, on the same device expected")
+        skip = -given.data_ptr() % 256
+        return given.data_ptr() + skip, max(0, given.numel() * given.element_size() - skip), given
+    if stream is None:
+        ws = torch.empty(need + 256, dtype=torch.uint8, device=t.device)
+    else:  # the allocator then gives it out again in that stream's order
+        with torch.cuda.stream(stream):
+            ws = torch.empty(need + 256, dtype=torch.uint8, device=t.device)
+    return ws.data_ptr() + -ws.data_ptr() % 256, need, ws
 
 
 def xpipe_linear_fwd(x, W, bias, y, act: int = ACT_NONE, residual=None, preact=None, workspace=None, stream=None):
     """y = act(x W^T + bias) + residual; preact (optional) receives the
     pre-activation.  Matrices of one type (bfloat16 or float32), their rows
     contiguous; bias float32 or None.  residual may be y itself."""
-    a = _linear_fwd_args(x, W, bias, y, act, residual, preact)
-    with _On(x, stream) as on:
-        need = _SZ(0)
-        _check(lib().xpipe_linear_fwd_query(ctypes.byref(a), ctypes.byref(need)))
-        ptr, size, keep = on.workspace(need.value, workspace)
-        _check(lib().xpipe_linear_fwd(ctypes.byref(a), ptr, size, on.ptr))
+    import torch
+    if _elsewhere(x):
+        with torch.cuda.device(x.device):
+            return xpipe_linear_fwd(x, W, bias, y, act, residual, preact, workspace, stream)
+    if x.dim() != 2 or W.dim() != 2:
+        raise ValueError("x [rows, cin] and W [cout, cin] expected")
+    (rows, cin), cout = x.shape, W.shape[0]
+    a = LinearFwdArgs(rows, cin, cout, _dtype_of(x), act, *_matrix("x", x, x, rows, cin), *_matrix("W", W, x, cout, cin),
+                      _vector("bias", bias, x, cout), *_matrix("residual", residual, x, rows, cout),
+                      *_matrix("preact", preact, x, rows, cout), *_matrix("y", y, x, rows, cout))
+    L, need, ref = lib(), _SZ(), ctypes.byref(a)
+    _check(L.xpipe_linear_fwd_query(ref, ctypes.byref(need)))
+    ptr, size, keep = _workspace(need.value, workspace, x, stream)
+    _check(L.xpipe_linear_fwd(ref, ptr, size, _raw_stream(x, stream)))
 
 
 def xpipe_linear_bwd(dz, x, W, dx=None, grad_W=None, grad_b=None, act: int = ACT_NONE, preact=None, residual=None,
@@ -657,75 +642,79 @@ def xpipe_linear_bwd(dz, x, W, dx=None, grad_W=None, grad_b=None, act: int = ACT
     (float32), each optional.  act and preact are those of the layer whose output
     x is, so dx is that layer's dz; residual is a gradient that reaches x another
     way and may be dx itself."""
-    _need(dz.dim() == 2, "dz [rows, cout] expected")
+    import torch
+    if _elsewhere(dz):
+        with torch.cuda.device(dz.device):
+            return xpipe_linear_bwd(dz, x, W, dx, grad_W, grad_b, act, preact, residual, workspace, stream)
     given = x if x is not None else W
-    _need(given is not None and given.dim() == 2, "x or W expected")
+    if dz.dim() != 2 or given is None or given.dim() != 2:
+        raise ValueError("dz [rows, cout], and x [rows, cin] or W [cout, cin] expected")
     (rows, cout), cin = dz.shape, given.shape[1]
-    a = LinearBwdArgs(rows=rows, cin=cin, cout=cout, dtype=_dtype_of(dz), act=int(act))
-    _ld(a, "dz", dz, dz, (rows, cout), ("dz", "lddz"))
-    _ld(a, "x", x, dz, (rows, cin), ("x", "ldx"))
-    _ld(a, "W", W, dz, (cout, cin), ("W", "ldw"))
-    _ld(a, "preact", preact, dz, (rows, cin), ("preact", "ldz"))
-    _ld(a, "residual", residual, dz, (rows, cin), ("residual", "ldr"))
-    _ld(a, "dx", dx, dz, (rows, cin), ("dx", "lddx"))
-    if grad_W is not None:
-        _vector("grad_W", grad_W, dz, cout * cin)
-        a.grad_W = grad_W.data_ptr()
-    if grad_b is not None:
-        _vector("grad_b", grad_b, dz, cout)
-        a.grad_b = grad_b.data_ptr()
-    with _On(dz, stream) as on:
-        need = _SZ(0)
-        _check(lib().xpipe_linear_bwd_query(ctypes.byref(a), ctypes.byref(need)))
-        ptr, size, keep = on.workspace(need.value, workspace)
-        _check(lib().xpipe_linear_bwd(ctypes.byref(a), ptr, size, on.ptr))
+    a = LinearBwdArgs(rows, cin, cout, _dtype_of(dz), act, *_matrix("dz", dz, dz, rows, cout),
+                      *_matrix("x", x, dz, rows, cin), *_matrix("W", W, dz, cout, cin),
+                      *_matrix("preact", preact, dz, rows, cin), *_matrix("residual", residual, dz, rows, cin),
+                      *_matrix("dx", dx, dz, rows, cin), _vector("grad_W", grad_W, dz, cout * cin),
+                      _vector("grad_b", grad_b, dz, cout))
+    L, need, ref = lib(), _SZ(), ctypes.byref(a)
+    _check(L.xpipe_linear_bwd_query(ref, ctypes.byref(need)))
+    ptr, size, keep = _workspace(need.value, workspace, dz, stream)
+    _check(L.xpipe_linear_bwd(ref, ptr, size, _raw_stream(dz, stream)))
 
 
 def xpipe_act_bwd(dy, z, dz, act: int, stream=None):
     """dz = dy act'(z): contiguous tensors of one type and shape (dz may be dy or z)."""
-    for t in (dy, z, dz):
-        _need(t.shape == dy.shape and t.dtype == dy.dtype and t.device == dy.device and t.is_contiguous(),
-              "contiguous tensors of one type, shape and device expected")
-    dtype = _dtype_of(dy)
-    with _On(dy, stream) as on:
-        _check(lib().xpipe_act_bwd(_ptr(dy), _ptr(z), _ptr(dz), dy.numel(), int(act), dtype, on.ptr))
-
-
-def _embedding_args(rows, name, tokens, like):
     import torch
-    _need(tokens.dtype == torch.int32 and tokens.is_contiguous() and tokens.device == like.device,
-          "tokens: contiguous int32 on the same device expected")
-    _need(rows.dim() >= 1 and rows.is_contiguous() and rows.device == like.device and
-          rows.numel() == tokens.numel() * rows.shape[-1], f"{name}: contiguous [tokens, dim] expected")
+    for t in (dy, z, dz):
+        if t.shape != dy.shape or t.dtype is not dy.dtype or t.get_device() != dy.get_device() or not t.is_contiguous():
+            raise ValueError("contiguous tensors of one type, shape and device expected")
+    if _elsewhere(dy):
+        with torch.cuda.device(dy.device):
+            return xpipe_act_bwd(dy, z, dz, act, stream)
+    _check(lib().xpipe_act_bwd(dy.data_ptr(), z.data_ptr(), dz.data_ptr(), dy.numel(), act, _dtype_of(dy),
+                               _raw_stream(dy, stream)))
+
+
+def _check_embedding(rows, name, tokens, table):
+    import torch
+    if table.dim() != 2 or not table.is_contiguous():
+        raise ValueError("table and grad: contiguous [vocab, dim] expected")
+    if tokens.dtype is not torch.int32 or not tokens.is_contiguous() or tokens.get_device() != table.get_device():
+        raise ValueError("tokens: contiguous int32 on the same device expected")
+    if (rows.dim() < 1 or not rows.is_contiguous() or rows.get_device() != table.get_device() or
+            rows.shape[-1] != table.shape[1] or rows.numel() != tokens.numel() * table.shape[1]):
+        raise ValueError(f"{name}: contiguous [tokens, dim] on the same device expected")
 
 
 def xpipe_embedding_fwd(table, tokens, y, scale: float = 1.0, stream=None):
     """y[i] = scale * table[tokens[i]] (zeros where a token is outside the table).
     table [vocab, dim] and y [..., dim] of one type; tokens int32."""
-    _need(table.dim() == 2 and table.is_contiguous(), "table: contiguous [vocab, dim] expected")
-    _embedding_args(y, "y", tokens, table)
-    _need(y.dtype == table.dtype and y.shape[-1] == table.shape[1], "y: the table's type and columns expected")
-    dtype = _dtype_of(table)
-    with _On(table, stream) as on:
-        _check(lib().xpipe_embedding_fwd(_ptr(table), _ptr(tokens), tokens.numel(), table.shape[0], table.shape[1],
-                                         float(scale), dtype, _ptr(y), on.ptr))
+    import torch
+    if _elsewhere(table):
+        with torch.cuda.device(table.device):
+            return xpipe_embedding_fwd(table, tokens, y, scale, stream)
+    _check_embedding(y, "y", tokens, table)
+    if y.dtype is not table.dtype:
+        raise ValueError("y: the table's type expected")
+    vocab, dim = table.shape
+    _check(lib().xpipe_embedding_fwd(table.data_ptr(), tokens.data_ptr(), tokens.numel(), vocab, dim, scale,
+                                     _dtype_of(table), y.data_ptr(), _raw_stream(table, stream)))
 
 
 def xpipe_embedding_bwd(dy, tokens, grad, scale: float = 1.0, workspace=None, stream=None):
     """grad[tokens[i]] += scale * dy[i], for the tokens inside the table.
     grad: contiguous float32 [vocab, dim]; dy [..., dim]; tokens int32."""
     import torch
-    _need(grad.dim() == 2 and grad.is_contiguous() and grad.dtype == torch.float32,
-          "grad: contiguous float32 [vocab, dim] expected")
-    _embedding_args(dy, "dy", tokens, grad)
-    _need(dy.shape[-1] == grad.shape[1], "dy: the table's columns expected")
-    dtype, (vocab, dim) = _dtype_of(dy), grad.shape
-    with _On(grad, stream) as on:
-        need = _SZ(0)
-        _check(lib().xpipe_embedding_bwd_query(tokens.numel(), vocab, dim, ctypes.byref(need)))
-        ptr, size, keep = on.workspace(need.value, workspace)
-        _check(lib().xpipe_embedding_bwd(_ptr(dy), _ptr(tokens), tokens.numel(), vocab, dim, float(scale), dtype,
-                                         _ptr(grad), ptr, size, on.ptr))
+    if _elsewhere(grad):
+        with torch.cuda.device(grad.device):
+            return xpipe_embedding_bwd(dy, tokens, grad, scale, workspace, stream)
+    _check_embedding(dy, "dy", tokens, grad)
+    if grad.dtype is not torch.float32:
+        raise ValueError("grad: float32 expected")
+    L, need, n, (vocab, dim) = lib(), _SZ(), tokens.numel(), grad.shape
+    _check(L.xpipe_embedding_bwd_query(n, vocab, dim, ctypes.byref(need)))
+    ptr, size, keep = _workspace(need.value, workspace, grad, stream)
+    _check(L.xpipe_embedding_bwd(dy.data_ptr(), tokens.data_ptr(), n, vocab, dim, scale, _dtype_of(dy), grad.data_ptr(),
+                                 ptr, size, _raw_stream(grad, stream)))
 
 
 class TensorList:
@@ -735,14 +724,15 @@ class TensorList:
 
     def __init__(self, tensors):
         self.tensors = list(tensors)
-        _need(len(self.tensors) > 0, "at least one tensor expected")
+        if not self.tensors:
+            raise ValueError("at least one tensor expected")
         first = self.tensors[0]
-        self.device, self.dtype = first.device, _dtype_of(first)
+        self.dtype = _dtype_of(first)
         for t in self.tensors:
-            _need(t.dtype == first.dtype and t.device == first.device and t.is_contiguous(),
-                  "contiguous tensors of one type on one device expected")
+            if t.dtype is not first.dtype or t.get_device() != first.get_device() or not t.is_contiguous():
+                raise ValueError("contiguous tensors of one type on one device expected")
         self.descs = (TensorDesc * len(self.tensors))(*[(t.data_ptr(), t.numel()) for t in self.tensors])
-        need = _SZ(0)
+        need = _SZ()
         _check(lib().xpipe_grad_norm_query(self.descs, len(self.tensors), ctypes.byref(need)))
         self.workspace_bytes = need.value
 
@@ -753,21 +743,28 @@ def xpipe_grad_norm(tensors, max_norm: float, norm_coef=None, sumsq=None, worksp
     1e-6))}, sumsq (float64, one element) the sum of squares; either may be None."""
     import torch
     ts = tensors if isinstance(tensors, TensorList) else TensorList(tensors)
+    t = ts.tensors[0]
+    if _elsewhere(t):
+        with torch.cuda.device(t.device):
+            return xpipe_grad_norm(ts, max_norm, norm_coef, sumsq, workspace, stream)
     if norm_coef is not None:
-        _check_norm_coef(norm_coef, ts.device)
-    if sumsq is not None:
-        _need(sumsq.dtype == torch.float64 and sumsq.numel() == 1 and sumsq.device == ts.device,
-              "sumsq: one float64 element on the gradients' device expected")
-    with _On(ts.tensors[0], stream) as on:
-        ptr, size, keep = on.workspace(ts.workspace_bytes, workspace)
-        _check(lib().xpipe_grad_norm(ts.descs, len(ts.tensors), ts.dtype, float(max_norm), _ptr(sumsq),
-                                     _ptr(norm_coef), ptr, size, on.ptr))
+        _check_norm_coef(norm_coef, t.get_device())
+    if sumsq is not None and (sumsq.dtype is not torch.float64 or sumsq.numel() != 1 or
+                              sumsq.get_device() != t.get_device()):
+        raise ValueError("sumsq: one float64 element on the gradients' device expected")
+    ptr, size, keep = _workspace(ts.workspace_bytes, workspace, t, stream)
+    _check(lib().xpipe_grad_norm(ts.descs, len(ts.tensors), ts.dtype, max_norm, _ptr(sumsq), _ptr(norm_coef), ptr, size,
+                                 _raw_stream(t, stream)))
 
 
 def xpipe_clip_coef(sumsq, max_norm: float, norm_coef, stream=None):
     """{norm, coefficient} from float64 sums of squares (one per stage), added in order."""
     import torch
-    _need(sumsq.dtype == torch.float64 and sumsq.is_contiguous(), "sumsq: contiguous float64 expected")
-    _check_norm_coef(norm_coef, sumsq.device)
-    with _On(sumsq, stream) as on:
-        _check(lib().xpipe_clip_coef(_ptr(sumsq), sumsq.numel(), float(max_norm), _ptr(norm_coef), on.ptr))
+    if _elsewhere(sumsq):
+        with torch.cuda.device(sumsq.device):
+            return xpipe_clip_coef(sumsq, max_norm, norm_coef, stream)
+    if sumsq.dtype is not torch.float64 or not sumsq.is_contiguous():
+        raise ValueError("sumsq: contiguous float64 expected")
+    _check_norm_coef(norm_coef, sumsq.get_device())
+    _check(lib().xpipe_clip_coef(sumsq.data_ptr(), sumsq.numel(), max_norm, norm_coef.data_ptr(),
+                                 _raw_stream(sumsq, stream)))
