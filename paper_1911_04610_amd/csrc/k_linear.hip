@@ -77,7 +77,7 @@ XP_DEV u32x4_t pack(const float (&v)[CHUNK<T>]) {
   }
   return u;
 }
-// the same element by element, the first n of them
+// the first n of a chunk's elements, one by one
 template <typename T>
 XP_DEV u32x4_t ld_some(const T* p, int n) {
   float v[CHUNK<T>];
@@ -94,15 +94,45 @@ XP_DEV void st_some(T* p, int n, const float (&v)[CHUNK<T>]) {
       else p[i] = f32_to_bf16(v[i]);
     }
 }
+// a chunk with n elements left in its row: vec, aligned (whole chunks only); else of any alignment
 template <typename T>
 XP_DEV u32x4_t ld_chunk(const T* p, bool vec, int n) {
-  return vec ? *reinterpret_cast<const u32x4_t*>(p) : ld_some<T>(p, n);
+  if (vec) return *reinterpret_cast<const u32x4_t*>(p);
+  if (n < CHUNK<T>) return ld_some<T>(p, n);
+  u32x4_t u;
+  __builtin_memcpy(&u, p, 16);
+  return u;
 }
 template <typename T>
 XP_DEV void st_chunk(T* p, bool vec, int n, const float (&v)[CHUNK<T>]) {
-  if (vec) *reinterpret_cast<u32x4_t*>(p) = pack<T>(v);
-  else st_some<T>(p, n, v);
+  if (vec) {
+    *reinterpret_cast<u32x4_t*>(p) = pack<T>(v);
+  } else if (n < CHUNK<T>) {
+    st_some<T>(p, n, v);
+  } else {
+    const u32x4_t u = pack<T>(v);
+    __builtin_memcpy(p, &u, 16);
+  }
 }
+
+// The arguments with the epilogue's pointers moved to row m0 and column n0, and N the
+// columns from there: rows and offsets below then are 32 bits wide (256 rows at most,
+// XPIPE_LINEAR_MAX_LD elements apart).
+template <typename T>
+XP_DEV LinearArgs from(LinearArgs a, int64_t m0, int n0) {
+  const auto move = [&](const void* p, int64_t ld) __attribute__((always_inline)) -> void* {
+    return p ? (void*)((T*)p + m0 * ld + n0) : nullptr;
+  };
+  a.res = move(a.res, a.ldr);
+  a.z_in = move(a.z_in, a.ldz);
+  a.z_out = move(a.z_out, a.ldz);
+  a.y = move(a.y, a.ldy);
+  if (a.grad) a.grad += m0 * a.ldg + n0;
+  if (a.bias) a.bias += n0;
+  a.N -= n0;
+  return a;
+}
+XP_DEV uint32_t at(int row, int64_t ld, int n) { return (uint32_t)row * (uint32_t)ld + (uint32_t)n; }
 
 // What the epilogue of columns n .. n + CHUNK<T> of row m reads: the residual and the
 // pre-activation, or (LIN_GRAD) the accumulators
@@ -110,17 +140,17 @@ struct Fetched {
   u32x4_t r, z;
 };
 template <typename T, int EPI>
-XP_DEV Fetched fetch(const LinearArgs& a, int64_t m, int n) {
+XP_DEV Fetched fetch(const LinearArgs& a, int m, int n) {
   const int left = a.N - n;
   const bool vec = a.vec && left >= CHUNK<T>;
   Fetched f;
   if constexpr (EPI == LIN_GRAD) {
-    const float* g = a.grad + m * a.N + n;
+    const float* g = a.grad + at(m, a.ldg, n);
     f.r = ld_chunk<float>(g, vec, left);
     if constexpr (sizeof(T) == 2) f.z = ld_chunk<float>(g + 4, vec, left - 4);
   } else {
-    if (a.res) f.r = ld_chunk<T>((const T*)a.res + m * a.ldr + n, vec, left);
-    if (EPI == LIN_DATA && a.z_in) f.z = ld_chunk<T>((const T*)a.z_in + m * a.ldz + n, vec, left);
+    if (a.res) f.r = ld_chunk<T>((const T*)a.res + at(m, a.ldr, n), vec, left);
+    if (EPI == LIN_DATA && a.z_in) f.z = ld_chunk<T>((const T*)a.z_in + at(m, a.ldz, n), vec, left);
   }
   return f;
 }
@@ -133,13 +163,13 @@ XP_DEV void fetch_bias(const LinearArgs& a, int n, float (&b)[CHUNK<T>]) {
 
 // The product's epilogue; v: the sums
 template <typename T, int EPI>
-XP_DEV void finish(const LinearArgs& a, int64_t m, int n, float (&v)[CHUNK<T>], const float (&b)[CHUNK<T>], const Fetched& f) {
+XP_DEV void finish(const LinearArgs& a, int m, int n, float (&v)[CHUNK<T>], const float (&b)[CHUNK<T>], const Fetched& f) {
   constexpr int C = CHUNK<T>;
   const int left = a.N - n;
   const bool vec = a.vec && left >= C;
   if constexpr (EPI == LIN_GRAD) {
     // fp32 accumulators whatever T
-    float* g = a.grad + m * a.N + n;
+    float* g = a.grad + at(m, a.ldg, n);
 #pragma unroll
     for (int h = 0; h < C / 4; ++h) {
       float o[4];
@@ -153,7 +183,7 @@ XP_DEV void finish(const LinearArgs& a, int64_t m, int n, float (&v)[CHUNK<T>], 
   if constexpr (EPI == LIN_FWD) {
 #pragma unroll
     for (int i = 0; i < C; ++i) v[i] += b[i];
-    if (a.z_out) st_chunk<T>((T*)a.z_out + m * a.ldz + n, vec, left, v);
+    if (a.z_out) st_chunk<T>((T*)a.z_out + at(m, a.ldz, n), vec, left, v);
     act_values(v, a.act);
   } else if (a.z_in) {
     float z[C];
@@ -166,7 +196,27 @@ XP_DEV void finish(const LinearArgs& a, int64_t m, int n, float (&v)[CHUNK<T>], 
 #pragma unroll
     for (int i = 0; i < C; ++i) v[i] += r[i];
   }
-  st_chunk<T>((T*)a.y + m * a.ldy + n, vec, left, v);
+  st_chunk<T>((T*)a.y + at(m, a.ldy, n), vec, left, v);
+}
+
+// The same for one element of a forward: what it reads, and its end
+struct Fetched1 {
+  float r, b;
+};
+template <typename T>
+XP_DEV Fetched1 fetch1(const LinearArgs& a, int m, int n) {
+  return Fetched1{a.res ? ldf<T>((const T*)a.res + at(m, a.ldr, n)) : 0.f, a.bias ? a.bias[n] : 0.f};
+}
+template <typename T>
+XP_DEV void finish1(const LinearArgs& a, int m, int n, float sum, const Fetched1& f) {
+  const auto st = [&](void* p, int64_t ld, float v) __attribute__((always_inline)) {
+    if constexpr (sizeof(T) == 4) ((float*)p)[at(m, ld, n)] = v;
+    else ((bf16_t*)p)[at(m, ld, n)] = f32_to_bf16(v);
+  };
+  float v[1] = {sum + f.b};
+  if (a.z_out) st(a.z_out, a.ldz, v[0]);
+  act_values(v, a.act);
+  st(a.y, a.ldy, a.res ? v[0] + f.r : v[0]);
 }
 
 // ---------------------------------------------------------------- product
@@ -221,11 +271,39 @@ XP_DEV void read_tr(const uint32_t (&at)[N], u32x4_t (&out)[N]) {
   for (int i = 0; i < N; ++i) out[i] = __builtin_shufflevector(lo[i], hi[i], 0, 1, 2, 3);
 }
 
+// The same for fp32: of N columns (a lane each) four rows, PITCH bytes apart.
+template <int N, int OFF, int PITCH>
+XP_DEV void read_col(const uint32_t (&at)[N], u32x4_t (&out)[N]) {
+  static_assert(N == 1 || N == 2 || N == 4, "blocks written out");
+  static_assert(OFF + 3 * PITCH < 65536, "16-bit offsets");
+  uint32_t v[4 * N];
+#define XP_C4(A, D0, D1, D2, D3)                                                                        \
+  "ds_read_b32 %" #D0 ", %" #A " offset:%c[p0]\n\tds_read_b32 %" #D1 ", %" #A " offset:%c[p1]\n\t"      \
+  "ds_read_b32 %" #D2 ", %" #A " offset:%c[p2]\n\tds_read_b32 %" #D3 ", %" #A " offset:%c[p3]\n\t"
+#define XP_O4(I) "=&v"(v[4 * I]), "=&v"(v[4 * I + 1]), "=&v"(v[4 * I + 2]), "=&v"(v[4 * I + 3])
+#define XP_OFFS [p0] "n"(OFF), [p1] "n"(OFF + PITCH), [p2] "n"(OFF + 2 * PITCH), [p3] "n"(OFF + 3 * PITCH)
+#define XP_WAIT "s_waitcnt lgkmcnt(0)"
+  if constexpr (N == 1)
+    asm volatile(XP_C4(4, 0, 1, 2, 3) XP_WAIT : XP_O4(0) : "v"(at[0]), XP_OFFS : "memory");
+  else if constexpr (N == 2)
+    asm volatile(XP_C4(8, 0, 1, 2, 3) XP_C4(9, 4, 5, 6, 7) XP_WAIT : XP_O4(0), XP_O4(1) : "v"(at[0]), "v"(at[1]), XP_OFFS : "memory");
+  else
+    asm volatile(XP_C4(16, 0, 1, 2, 3) XP_C4(17, 4, 5, 6, 7) XP_C4(18, 8, 9, 10, 11) XP_C4(19, 12, 13, 14, 15) XP_WAIT
+                 : XP_O4(0), XP_O4(1), XP_O4(2), XP_O4(3)
+                 : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), XP_OFFS : "memory");
+#undef XP_C4
+#undef XP_O4
+#undef XP_OFFS
+#undef XP_WAIT
+#pragma unroll
+  for (int i = 0; i < N; ++i) out[i] = (u32x4_t){v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
+}
+
 // One workgroup per BM x BN tile of the product and part of the reduction, WM x
 // WN waves of 32x32 MFMA results.  Both operands are copied from memory
-// straight into LDS, one step (128 bytes of the reduction) at a time, with two
-// buffers: one step is in flight while one is multiplied.
-template <typename T, int BM, int BN, int WM, int WN, bool TA, bool TB, int EPI>
+// straight into LDS, one step (128 bytes of the reduction) at a time, with NS
+// buffers: NS - 1 steps are in flight while one is multiplied.
+template <typename T, int BM, int BN, int WM, int WN, int NS, bool TA, bool TB, int EPI>
 __global__ __launch_bounds__(WM * WN * 64) void k_linear(LinearArgs a, int tiles_m, int tiles_n) {
   constexpr int NW = WM * WN, ES = (int)sizeof(T), C = CHUNK<T>, BK = STEP<T>;
   constexpr int WTM = BM / WM, WTN = BN / WN, TM = WTM / 32, TN = WTN / 32;
@@ -235,9 +313,15 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear(LinearArgs a, int tiles
   constexpr int SZ = (BM + BN) * 128;
   __shared__ __align__(16) unsigned char st0[SZ];
   __shared__ __align__(16) unsigned char st1[SZ];
+  __shared__ __align__(16) unsigned char st2[NS > 2 ? SZ : 16];
+  __shared__ __align__(16) unsigned char st3[NS > 3 ? SZ : 16];
+  static_assert(NS >= 2 && NS <= 4, "stages");
   auto stage = [&](auto I) __attribute__((always_inline)) -> unsigned char* {
-    if constexpr (decltype(I)::value == 0) return st0;
-    else return st1;
+    constexpr int i = decltype(I)::value;
+    if constexpr (i == 0) return st0;
+    else if constexpr (i == 1) return st1;
+    else if constexpr (i == 2) return st2;
+    else return st3;
   };
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / WN, wn = wave % WN;
@@ -245,8 +329,8 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear(LinearArgs a, int tiles
   // tile order: runs of 8 tile rows, so that the tiles that one XCD holds at a
   // time share rows of both operands in its L2
   const int lin = xcd_tile(blockIdx.x, gridDim.x);
-  const int split = lin / (tiles_m * tiles_n), t = lin - split * tiles_m * tiles_n;
-  const int grp = t / (8 * tiles_n), gm = min(8, tiles_m - grp * 8), in = t - grp * 8 * tiles_n;
+  const int split = lin / (tiles_m * tiles_n), tile = lin - split * tiles_m * tiles_n;
+  const int grp = tile / (8 * tiles_n), gm = min(8, tiles_m - grp * 8), in = tile - grp * 8 * tiles_n;
   const int tm = grp * 8 + in % gm, tn = in / gm;
   const int64_t m0 = (int64_t)tm * BM;
   const int n0 = tn * BN;
@@ -257,7 +341,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear(LinearArgs a, int tiles
   // Per copy the lane's byte offset from the step's base, ~0 where its row (TR:
   // its column chunk) is past the operand; the base moves by one step at a time, and
   // reduction indices past the end are masked step by step.  So every chunk that
-  // is read holds an element of the operand (a 16-byte chunk never leaves that
+  // is copied holds an element of the operand (a 16-byte chunk never leaves that
   // element's page).
   const char* abase = (const char*)a.A + (TA ? kbeg * a.lda + m0 : m0 * a.lda + kbeg) * ES;
   const char* bbase = (const char*)a.B + (TB ? kbeg * a.ldb + n0 : n0 * a.ldb + kbeg) * ES;
@@ -316,33 +400,23 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear(LinearArgs a, int tiles
   // products, whose reduction indices then are 4 (l / 32) + q in both operands).
   const int fr = lane & 31, fh = lane >> 5;
   // (One offset into the stage's array per read: the compiler then sees which array
-  // it reads, and waits for no copies into the other.)
-  auto frag = [&](auto I, auto TR, auto W, int base, int row0, int kk) __attribute__((always_inline)) -> u32x4_t {
-    constexpr int w = decltype(W)::value;
-    const unsigned char* lds = stage(I);
-    if constexpr (!decltype(TR)::value) {
-      return *reinterpret_cast<const u32x4_t*>(lds + (base + (row0 + fr) * 128 + (((kk * 2 + fh) ^ (fr >> 1 & 7)) << 4)));
-    } else {
-      u32x4_t v;
-      const int k = 4 * fh, c = row0 + fr;
-      const int at = base + (kk * 8 + k) * (w * 4) + (((c >> 2) ^ tr_swz<T, w>(k)) << 4) + (c & 3) * 4;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] = *reinterpret_cast<const uint32_t*>(lds + (at + q * w * 4));
-      return v;
-    }
+  // it reads, and waits for no copies into the others.)
+  auto frag = [&](auto I, int base, int row0, int kk) __attribute__((always_inline)) -> u32x4_t {
+    return *reinterpret_cast<const u32x4_t*>(stage(I) + (base + (row0 + fr) * 128 + (((kk * 2 + fh) ^ (fr >> 1 & 7)) << 4)));
   };
   // Two sets of fragments: while the products of one quarter of a step run, the next
   // quarter's fragments are read.
   u32x4_t fa[2][TM], fb[2][TN];
-  // where the lane's transposing reads of a quarter start (of the first quarter, in the first stage's array)
-  constexpr int TRN = ES == 2 ? (TA ? TM : 0) + (TB ? TN : 0) : 0;
+  // where the lane's reads of columns start (in the first quarter, from the stage's array on)
+  constexpr int TRN = (TA ? TM : 0) + (TB ? TN : 0);
   uint32_t tr_at[TRN > 0 ? TRN : 1];
   if constexpr (TRN > 0) {
     static_assert(BM == BN, "one offset for both operands' rows");
     auto at = [&](int base, int row0) __attribute__((always_inline)) -> uint32_t {
-      const int k = 8 * fh + ((lane & 15) >> 2);  // the first read's row (the swizzle takes it modulo 4)
-      const int c = row0 + 16 * (fr >> 4) + 4 * (lane & 3);
-      return base + k * (BM * 2) + (((c >> 3) ^ tr_swz<T, BM>(k)) << 4) + (c & 7) * 2;
+      // the first read's row (the swizzle is the same for all of the lane's rows) and column
+      const int k = ES == 2 ? 8 * fh + ((lane & 15) >> 2) : 4 * fh;
+      const int c = ES == 2 ? row0 + 16 * (fr >> 4) + 4 * (lane & 3) : row0 + fr;
+      return base + k * (BM * ES) + (((c / C) ^ tr_swz<T, BM>(k)) << 4) + c % C * ES;
     };
     if constexpr (TB) {
 #pragma unroll
@@ -356,15 +430,13 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear(LinearArgs a, int tiles
   auto read = [&](auto I, auto KK, int set) __attribute__((always_inline)) {
     constexpr int kk = decltype(KK)::value;
     // (B's first: the next quarter's first products take all of them and one of A's)
-    if constexpr (!(ES == 2 && TB)) {
+    if constexpr (!TB) {
 #pragma unroll
-      for (int j = 0; j < TN; ++j)
-        fb[set][j] = frag(I, std::bool_constant<TB>{}, std::integral_constant<int, BN>{}, BM * 128, wn * WTN + j * 32, kk);
+      for (int j = 0; j < TN; ++j) fb[set][j] = frag(I, BM * 128, wn * WTN + j * 32, kk);
     }
-    if constexpr (!(ES == 2 && TA)) {
+    if constexpr (!TA) {
 #pragma unroll
-      for (int i = 0; i < TM; ++i)
-        fa[set][i] = frag(I, std::bool_constant<TA>{}, std::integral_constant<int, BM>{}, 0, wm * WTM + i * 32, kk);
+      for (int i = 0; i < TM; ++i) fa[set][i] = frag(I, 0, wm * WTM + i * 32, kk);
     }
     if constexpr (TRN > 0) {
       const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)stage(I);
@@ -372,7 +444,8 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear(LinearArgs a, int tiles
       u32x4_t out[TRN];
 #pragma unroll
       for (int i = 0; i < TRN; ++i) at[i] = lds + tr_at[i];
-      read_tr<TRN, kk * 16 * BM * 2, 4 * BM * 2>(at, out);
+      if constexpr (ES == 2) read_tr<TRN, kk * 16 * BM * 2, 4 * BM * 2>(at, out);
+      else read_col<TRN, kk * 8 * BM * 4, BM * 4>(at, out);
       if constexpr (TB) {
 #pragma unroll
         for (int j = 0; j < TN; ++j) fb[set][j] = out[j];
@@ -400,7 +473,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear(LinearArgs a, int tiles
       }
   };
   // Reads one quarter's fragments and multiplies another's.  Reads that the
-  // compiler can move are spread over the products; a block of transposing reads
+  // compiler can move are spread over the products; a block of column reads
   // comes between them (the other wave of the SIMD multiplies while it waits).
   auto overlap = [&](auto I, auto KK, int into, int set) __attribute__((always_inline)) {
     __builtin_amdgcn_sched_barrier(0);
@@ -411,7 +484,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear(LinearArgs a, int tiles
       __builtin_amdgcn_sched_barrier(0);
       multiply(set, (TM + 1) / 2, TM);
     } else {
-      constexpr int PER = TM * TN * (ES == 2 ? 1 : 4), READS = TM * (TA ? 4 : 1) + TN * (TB ? 4 : 1);
+      constexpr int PER = TM * TN * (ES == 2 ? 1 : 4), READS = TM + TN;
       constexpr int SLOTS = READS < PER ? READS : PER;
       read(I, KK, into);
       multiply(set, 0, TM);
@@ -448,14 +521,13 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear(LinearArgs a, int tiles
     }
   };
 
-  // Step k from buffer k % 2.  By its last quarter all of the step's fragments
+  // Step k from buffer k % NS.  By its last quarter all of the step's fragments
   // are in registers: past the barrier there the buffer takes the copies of step
-  // k + 2, and the first fragments of step k + 1, whose copies have had a step's time
-  // to land, are read while the last quarter is multiplied.
+  // k + NS, and the first fragments of step k + 1, whose copies have had NS - 1 steps'
+  // time to land, are read while the last quarter is multiplied.
   constexpr std::integral_constant<int, 0> B0{};
-  copy(B0);
-  copy(std::integral_constant<int, 1>{});
-  wait_step<A_I + B_I>();
+  static_for<0, NS>([&](auto I) __attribute__((always_inline)) { copy(I); });
+  wait_step<(NS - 1) * (A_I + B_I)>();
   read(B0, B0, 0);
   int k = 0;
   auto quarters = [&](auto I) __attribute__((always_inline)) {
@@ -467,18 +539,18 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear(LinearArgs a, int tiles
     add_rows(1);
   };
   quarters(B0);
-  while (++k < nk) {
-    bool done = false;
-    static_for<0, 2>([&](auto I) __attribute__((always_inline)) {
-      if (!done) {
-        constexpr std::integral_constant<int, 1 - decltype(I)::value> NEXT{};
+  bool more = ++k < nk;
+  while (more) {
+    static_for<0, NS>([&](auto I) __attribute__((always_inline)) {
+      if (more) {
+        constexpr std::integral_constant<int, (decltype(I)::value + 1) % NS> NEXT{};
         // this wave's copies of step k have landed and its reads of step k - 1
         // returned; past the barrier so have the others'
-        wait_step<0>();
+        wait_step<(NS - 2) * (A_I + B_I)>();
         copy(I);
         overlap(NEXT, B0, 0, 1);
         quarters(NEXT);
-        if (decltype(I)::value == 0) done = ++k == nk;
+        more = ++k < nk;
       }
     });
   }
@@ -506,22 +578,28 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear(LinearArgs a, int tiles
   constexpr int PITCH = WTN + 4;
   static_assert(NW * 16 * PITCH * 4 <= SZ, "strips");
   float* strip = reinterpret_cast<float*>(st0) + wave * 16 * PITCH;
-  constexpr int CW = WTN / C, RP = 64 / CW, PASS = 16 / RP;  // chunks per strip row, rows per pass
-  const int ch = lane % CW;
-  const int n = n0 + wn * WTN + ch * C;
+  const int64_t rows = a.M - m0;  // of the tile and below
+  const LinearArgs t = from<T>(a, m0, n0);
+  auto to_strip = [&](auto S) __attribute__((always_inline)) {
+    constexpr int s = decltype(S)::value;
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int r = 0; r < 8; ++r)
+        strip[(8 * (r >> 2) + 4 * fh + (r & 3)) * PITCH + j * 32 + fr] = acc[s >> 1][j][(s & 1) * 8 + r];
+    __builtin_amdgcn_wave_barrier();
+  };
+  constexpr int CW = WTN / C, RP = 64 / CW, PASS = 16 / RP;  // chunks per strip row, rows per part
+  const int ch = lane % CW, c = wn * WTN + ch * C, lr = wm * WTM + lane / CW;
   const bool direct = !a.part;
   float bias[C];
-  fetch_bias<T, EPI>(a, n, bias);
-  auto row_of = [&](int s, int p) __attribute__((always_inline)) -> int64_t {
-    const int64_t m = m0 + wm * WTM + s * 16 + p * RP + lane / CW;
-    return m < a.M && n < a.N ? m : -1;
-  };
+  fetch_bias<T, EPI>(t, c, bias);
   Fetched next[PASS];
   auto prefetch = [&](int s) __attribute__((always_inline)) {
 #pragma unroll
     for (int p = 0; p < PASS; ++p) {
-      const int64_t m = row_of(s, p);
-      if (direct && m >= 0) next[p] = fetch<T, EPI>(a, m, n);
+      const int row = lr + s * 16 + p * RP;
+      if (direct && row < rows && c < t.N) next[p] = fetch<T, EPI>(t, row, c);
     }
   };
   prefetch(0);
@@ -531,28 +609,23 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear(LinearArgs a, int tiles
 #pragma unroll
     for (int p = 0; p < PASS; ++p) now[p] = next[p];
     if constexpr (s + 1 < TM * 2) prefetch(s + 1);
-#pragma unroll
-    for (int j = 0; j < TN; ++j)
-#pragma unroll
-      for (int r = 0; r < 8; ++r)
-        strip[(8 * (r >> 2) + 4 * fh + (r & 3)) * PITCH + j * 32 + fr] = acc[s >> 1][j][(s & 1) * 8 + r];
-    __builtin_amdgcn_wave_barrier();
+    to_strip(S);
 #pragma unroll
     for (int p = 0; p < PASS; ++p) {
-      const int64_t m = row_of(s, p);
+      const int row = lr + s * 16 + p * RP;
       float v[C];
 #pragma unroll
       for (int q = 0; q < C / 4; ++q) {
-        const f32x4_t f = *reinterpret_cast<const f32x4_t*>(strip + (p * RP + lane / CW) * PITCH + ch * C + q * 4);
+        const f32x4_t g = *reinterpret_cast<const f32x4_t*>(strip + (p * RP + lane / CW) * PITCH + ch * C + q * 4);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[q * 4 + i] = f[i];
+        for (int i = 0; i < 4; ++i) v[q * 4 + i] = g[i];
       }
-      if (m < 0) continue;
+      if (row >= rows || c >= t.N) continue;
       if (direct) {
-        finish<T, EPI>(a, m, n, v, bias, now[p]);
+        finish<T, EPI>(t, row, c, v, bias, now[p]);
       } else {
         // partial sums, rows of N rounded up to whole chunks
-        float* out = a.part + ((int64_t)split * a.M + m) * a.ldpart + n;
+        float* out = a.part + ((int64_t)split * a.M + m0 + row) * a.ldpart + n0 + c;
 #pragma unroll
         for (int q = 0; q < C / 4; ++q)
           *reinterpret_cast<f32x4_t*>(out + 4 * q) = (f32x4_t){v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
@@ -571,21 +644,23 @@ __global__ __launch_bounds__(256) void k_linear_join(LinearArgs a) {
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
     const int64_t m = i / cpr;
     const int n = (int)(i - m * cpr) * C;
-    float v[C];
+    const LinearArgs t = from<T>(a, m, 0);
+    const Fetched f = fetch<T, EPI>(t, 0, n);
+    float v[C], b[C];
+    fetch_bias<T, EPI>(t, n, b);
 #pragma unroll
     for (int q = 0; q < C; ++q) v[q] = 0.f;
     const float* p = a.part + m * a.ldpart + n;
+#pragma unroll 4
     for (int s = 0; s < a.splits; ++s, p += a.M * a.ldpart) {
 #pragma unroll
       for (int q = 0; q < C / 4; ++q) {
-        const f32x4_t f = *reinterpret_cast<const f32x4_t*>(p + 4 * q);
+        const f32x4_t g = *reinterpret_cast<const f32x4_t*>(p + 4 * q);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[4 * q + e] += f[e];
+        for (int e = 0; e < 4; ++e) v[4 * q + e] += g[e];
       }
     }
-    float b[C];
-    fetch_bias<T, EPI>(a, n, b);
-    finish<T, EPI>(a, m, n, v, b, fetch<T, EPI>(a, m, n));
+    finish<T, EPI>(t, 0, n, v, b, f);
   }
   if constexpr (EPI == LIN_GRAD) {
     if (!a.grad_b) return;
@@ -597,17 +672,161 @@ __global__ __launch_bounds__(256) void k_linear_join(LinearArgs a) {
   }
 }
 
-// ---------------------------------------------------------------- packing
-// Rows whose chunks do not start at multiples of 16 bytes, or end inside a
-// chunk of the reduction, are copied to rows of whole chunks, zeros behind.
+// The first n >= 1 of CHUNK<T> elements at p, of any alignment, zeros behind them: made
+// from the aligned 16 bytes that the first lies in and, where they reach past
+// those, the next.
 template <typename T>
-__global__ __launch_bounds__(256) void k_linear_pack(const T* __restrict__ src, int64_t ld, int64_t rows, int cols,
-                                                     T* __restrict__ dst, int cols_out) {
-  const int64_t total = rows * cols_out;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / cols_out;
-    const int c = (int)(i - r * cols_out);
-    dst[i] = c < cols ? src[r * ld + c] : T(0);
+XP_DEV u32x4_t ld_any(const char* p, int n) {
+  const int bytes = min(n, CHUNK<T>) * (int)sizeof(T);
+  const int mis = (int)(reinterpret_cast<uintptr_t>(p) & 15);
+  const u32x4_t* q = reinterpret_cast<const u32x4_t*>(p - mis);
+  const u32x4_t lo = q[0];
+  u32x4_t hi = {0u, 0u, 0u, 0u};
+  if (mis + bytes > 16) hi = q[1];
+  uint32_t w[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+  if (mis & 8) {
+#pragma unroll
+    for (int e = 0; e < 6; ++e) w[e] = w[e + 2];
+  }
+  if (mis & 4) {
+#pragma unroll
+    for (int e = 0; e < 5; ++e) w[e] = w[e + 1];
+  }
+  if (mis & 2) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = __funnelshift_r(w[e], w[e + 1], 16);
+  }
+  u32x4_t out;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int have = bytes - 4 * e;
+    out[e] = have >= 4 ? w[e] : have == 2 ? w[e] & 0xffffu : 0u;
+  }
+  return out;
+}
+
+// ---------------------------------------------------------------- few rows
+// The forward of up to 16 MT rows: bound by reading W once, so every wave streams
+// its part of the reduction of 16 rows of W from memory straight into registers
+// (16x16 products, W the columns, the rows of x the rows, empty ones zeros).
+// The eight waves of a workgroup take the reduction's 128-byte steps in turn and
+// add their results through LDS in the order of the waves: no workspace, one launch.
+// ANY: operands of any alignment.
+constexpr int FEW_WAVES = 8, FEW_STEPS = 4;  // steps in flight per wave
+template <typename T, int MT, bool ANY>
+__global__ __launch_bounds__(FEW_WAVES * 64) void k_linear_few(LinearArgs a) {
+  constexpr int C = CHUNK<T>, ES = (int)sizeof(T), BK = STEP<T>;
+  constexpr int EACH = (MT * 256 + FEW_WAVES * 64 - 1) / (FEW_WAVES * 64);  // results per thread
+  __shared__ float red[FEW_WAVES][MT][256];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n0 = blockIdx.x * 16, fr = lane & 15, fg = lane >> 4;
+  const LinearArgs t = from<T>(a, 0, n0);
+  auto result = [&](int e, int& m, int& n) __attribute__((always_inline)) -> bool {
+    const int i = e * FEW_WAVES * 64 + tid;
+    m = i / 16;
+    n = i % 16;
+    return i < MT * 256 && m < a.M && n < t.N;
+  };
+  Fetched1 f[EACH];
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) {
+    int m, n;
+    if (result(e, m, n)) f[e] = fetch1<T>(t, m, n);
+  }
+  const char* xr[MT];  // the lane's rows (null: none)
+#pragma unroll
+  for (int i = 0; i < MT; ++i) xr[i] = i * 16 + fr < a.M ? (const char*)a.A + (i * 16 + fr) * a.lda * ES : nullptr;
+  const char* wr = n0 + fr < a.N ? (const char*)a.B + (int64_t)(n0 + fr) * a.ldb * ES : nullptr;
+  auto chunk = [&](const char* row, int k) __attribute__((always_inline)) -> u32x4_t {
+    const int n = a.K - k;
+    u32x4_t u = {0u, 0u, 0u, 0u};
+    if (row && n > 0) {
+      if constexpr (ANY) u = ld_any<T>(row + (int64_t)k * ES, n);
+      else u = *reinterpret_cast<const u32x4_t*>(row + (int64_t)k * ES);  // (K is whole chunks)
+    }
+    return u;
+  };
+  f32x4_t acc[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) acc[i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+  const int steps = (a.K + BK - 1) / BK;
+  for (int s0 = wave; s0 < steps; s0 += FEW_WAVES * FEW_STEPS) {
+    // 16 x 16 x (4 chunks): lane l holds row l % 16 and chunk l / 16, in both operands
+    u32x4_t x[FEW_STEPS][2][MT], w[FEW_STEPS][2];
+#pragma unroll
+    for (int u = 0; u < FEW_STEPS; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int k = (s0 + u * FEW_WAVES) * BK + (h * 4 + fg) * C;
+        w[u][h] = chunk(wr, k);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) x[u][h][i] = chunk(xr[i], k);
+      }
+#pragma unroll
+    for (int u = 0; u < FEW_STEPS; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          if constexpr (ES == 2) {
+            acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x[u][h][i]),
+                                                             __builtin_bit_cast(bf16x8_t, w[u][h]), acc[i], 0, 0, 0);
+          } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              acc[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x[u][h][i][q]), __uint_as_float(w[u][h][q]),
+                                                            acc[i], 0, 0, 0);
+          }
+        }
+  }
+  // 16x16 result: lane l, register r holds row 4 (l / 16) + r, column l % 16
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) red[wave][i][(4 * fg + r) * 16 + fr] = acc[i][r];
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) {
+    int m, n;
+    if (!result(e, m, n)) continue;
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < FEW_WAVES; ++w) v += red[w][m >> 4][(m & 15) * 16 + n];
+    finish1<T>(t, m, n, v, f[e]);
+  }
+}
+
+// ---------------------------------------------------------------- packing
+// Operands whose rows do not start at multiples of 16 bytes, or end inside a
+// chunk of the reduction, are copied to rows of whole chunks (zeros behind the
+// columns), all of a call's in one launch.  Loads of 16 unaligned bytes straight
+// into the products took four times an aligned product's time (2001x2001x2001 98 us, packed 38, aligned 25).
+struct PackArgs {
+  int count;
+  const void* src[3];
+  void* dst[3];
+  int64_t ld[3], rows[3];           // source pitch (elements), rows
+  int cols[3], per_row[3], log[3];  // columns, chunks per packed row, log2 of the lanes that take a row
+  int first[3], blocks;             // first workgroup, and their number
+};
+template <typename T>
+__global__ __launch_bounds__(256) void k_linear_pack(PackArgs a) {
+  constexpr int C = CHUNK<T>, ES = (int)sizeof(T);
+  int m = 0;
+#pragma unroll
+  for (int q = 1; q < 3; ++q)
+    if (q < a.count && (int)blockIdx.x >= a.first[q]) m = q;
+  // 2^log lanes take a row
+  const int log = a.log[m], per = a.per_row[m], cols = a.cols[m];
+  const int64_t r = ((int64_t)((int)blockIdx.x - a.first[m]) * 256 + threadIdx.x) >> log;
+  if (r >= a.rows[m]) return;
+  const char* row = (const char*)a.src[m] + r * a.ld[m] * ES;
+  u32x4_t* dst = reinterpret_cast<u32x4_t*>(a.dst[m]) + r * per;
+#pragma unroll 2
+  for (int j = threadIdx.x & ((1 << log) - 1); j < per; j += 1 << log) {
+    const int c = j * C, n = min(C, cols - c);
+    const char* p = row + (int64_t)c * ES;
+    dst[j] = ld_any<T>(p, n);
   }
 }
 
@@ -631,25 +850,48 @@ __global__ __launch_bounds__(256) void k_act_bwd(const T* __restrict__ dy, const
 int grid_of(int64_t items) { return (int)std::max<int64_t>(1, std::min<int64_t>((items + 255) / 256, 1 << 16)); }
 
 // ---------------------------------------------------------------- plan
-struct Tile {
-  int bm, bn;
+// What a launch costs, in us, fitted to 500 timed products of 76 shapes (MI355X; a
+// step is 128 bytes of the reduction): per step and workgroup alone on its CU, per
+// step of two that share a CU (one 256x256 tile fills it), and the rest of a
+// workgroup (prologue and epilogue).  Products of up to a few workgroups per CU
+// are bound by the length of their chains, not by rates.  The choice by these
+// costs was on average 3% (bf16) and 1% (fp32) slower than the fastest of all
+// tiles and splits timed: e.g. 512x1024x4096 64x64 9.2 us, 128x128 13.2, 64x64
+// in two splits 24; 4096x2048x4096 256x256 68, 128x128 73; weight gradient
+// 8192x1024x1024 128x128 in eight splits 36, in one 66.
+struct TileCost {
+  int tile;
+  double alone, pair, alone_rest, pair_rest;
 };
+constexpr TileCost COST_BF16[] = {{64, 0.29, 0.41, 2.1, 2.1}, {128, 0.63, 0.93, 3.1, 5.8}, {256, 1.46, 2.92, 8.2, 16.4}};
+constexpr TileCost COST_F32[] = {{64, 0.56, 1.05, 0.0, 1.3}, {128, 2.0, 3.7, 3.5, 3.9}};
+// the join of splits: its launch, and the partial sums' traffic per MB of fp32 results
+constexpr double JOIN_US = 4.6, JOIN_US_PER_MB = 0.134;
+constexpr int MAX_SPLITS = 16;
 
-// tile and splits of a product of M x N results over K
-void pick(int dtype, int64_t M, int N, int K, Tile* t, int* splits) {
-  const int bk = dtype == DT_BF16 ? STEP<bf16_t> : STEP<float>;
-  const int64_t big = ((M + 255) / 256) * ((N + 255) / 256), mid = ((M + 127) / 128) * ((N + 127) / 128);
-  if (dtype == DT_BF16 && big >= 192) *t = Tile{256, 256};
-  else if (mid >= 128) *t = Tile{128, 128};
-  else *t = Tile{64, 64};
-  const int64_t tiles = ((M + t->bm - 1) / t->bm) * ((N + t->bn - 1) / t->bn);
-  const int steps = (K + bk - 1) / bk;
-  int64_t s = 1;
-  if (tiles < 256) s = std::min<int64_t>(512 / tiles, steps / 4);
-  *splits = (int)std::max<int64_t>(1, s);
+void pick(int dtype, int64_t M, int N, int64_t steps, int* tile, int* splits) {
+  const TileCost* cost = dtype == DT_BF16 ? COST_BF16 : COST_F32;
+  const int tiles = dtype == DT_BF16 ? 3 : 2;
+  double best = 0.0;
+  *tile = 0;
+  for (int i = 0; i < tiles; ++i) {
+    const int b = cost[i].tile;
+    const int64_t count = ((M + b - 1) / b) * ((N + b - 1) / b);
+    for (int s = 1; s <= MAX_SPLITS && (s == 1 || 2 * s <= steps); s *= 2) {
+      const int64_t per = (steps + s - 1) / s, blocks = (count * ((steps + per - 1) / per) + 255) / 256;
+      double t = (double)(blocks / 2) * (cost[i].pair * per + cost[i].pair_rest) +
+                 (double)(blocks % 2) * (cost[i].alone * per + cost[i].alone_rest);
+      if (s > 1) t += JOIN_US + JOIN_US_PER_MB * 4e-6 * (double)M * N * (2 * s + 1);
+      if (*tile == 0 || t < best) {
+        best = t;
+        *tile = b;
+        *splits = s;
+      }
+    }
+  }
 }
 
-template <typename T, int BM, int BN, int WM, int WN, bool TA, bool TB, int EPI>
+template <typename T, int BM, int BN, int WM, int WN, int NS, bool TA, bool TB, int EPI>
 hipError_t go(const LinearArgs& a, hipStream_t s) {
   const int64_t tm = (a.M + BM - 1) / BM, tn = (a.N + BN - 1) / BN;
   static const struct Name {
@@ -657,8 +899,8 @@ hipError_t go(const LinearArgs& a, hipStream_t s) {
     Name() { snprintf(s, sizeof s, "k_linear<%s,%d,%d,%s>", sizeof(T) == 2 ? "bf16" : "f32", BM, BN,
                       EPI == LIN_FWD ? "fwd" : EPI == LIN_DATA ? "data" : "grad"); }
   } name;
-  XP_LAUNCH(name.s, 2.0 * a.M * a.N * a.K, (k_linear<T, BM, BN, WM, WN, TA, TB, EPI>), dim3((unsigned)(tm * tn * a.splits)),
-            dim3(WM * WN * 64), 0, s, a, (int)tm, (int)tn);
+  XP_LAUNCH(name.s, 2.0 * a.M * a.N * a.K, (k_linear<T, BM, BN, WM, WN, NS, TA, TB, EPI>),
+            dim3((unsigned)(tm * tn * a.splits)), dim3(WM * WN * 64), 0, s, a, (int)tm, (int)tn);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.part) return e;
   XP_LAUNCH("k_linear_join", 4.0 * a.M * a.N * a.splits, (k_linear_join<T, EPI>),
@@ -666,107 +908,163 @@ hipError_t go(const LinearArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+// Buffers: two for 128x128 tiles (two workgroups per CU; four buffers and one
+// workgroup were 0 to 5% slower), four for 64x64 (products of a few workgroups
+// per CU: 5 to 15% over two).
 template <typename T, bool TA, bool TB, int EPI>
-hipError_t by_tile(const LinearArgs& a, const Tile& t, hipStream_t s) {
+hipError_t by_tile(const LinearArgs& a, int tile, hipStream_t s) {
   if constexpr (sizeof(T) == 2) {
-    if (t.bm == 256) return go<T, 256, 256, 2, 4, TA, TB, EPI>(a, s);
+    if (tile == 256) return go<T, 256, 256, 2, 4, 2, TA, TB, EPI>(a, s);
   }
-  if (t.bm == 128) return go<T, 128, 128, 2, 2, TA, TB, EPI>(a, s);
-  return go<T, 64, 64, 2, 2, TA, TB, EPI>(a, s);
+  if (tile == 128) return go<T, 128, 128, 2, 2, 2, TA, TB, EPI>(a, s);
+  return go<T, 64, 64, 2, 2, 4, TA, TB, EPI>(a, s);
 }
 
 template <typename T>
-hipError_t by_kind(const LinearArgs& a, const Tile& t, hipStream_t s) {
-  if (a.epi == LIN_FWD) return by_tile<T, false, false, LIN_FWD>(a, t, s);
-  if (a.epi == LIN_DATA) return by_tile<T, false, true, LIN_DATA>(a, t, s);
-  return by_tile<T, true, true, LIN_GRAD>(a, t, s);
+hipError_t by_kind(const LinearArgs& a, int tile, hipStream_t s) {
+  if (a.epi == LIN_FWD) return by_tile<T, false, false, LIN_FWD>(a, tile, s);
+  if (a.epi == LIN_DATA) return by_tile<T, false, true, LIN_DATA>(a, tile, s);
+  return by_tile<T, true, true, LIN_GRAD>(a, tile, s);
+}
+
+// The forwards that k_linear_few takes: up to 32 rows (us, MI355X, tiles in brackets:
+// bf16 1x4096x4096 7.1 (12.4), 16x4096x4096 9.7 (13.0), 32x4096x4096 13.3 (14.0),
+// 16x999x1333 8.1 (13.1); 64 rows 21.2 (15.5); fp32 1x4096x4096 17.1 (25.0), 16 rows
+// 20.7 (25.1)), but not a long reduction for a few columns, whose workgroups
+// leave most CUs idle (16x16384x64 29.6 (13.4)).
+bool takes_few(const LinearArgs& a, int64_t steps) {
+  return a.epi == LIN_FWD && a.M <= 32 && (a.N >= 1024 || steps <= 3 * FEW_WAVES * FEW_STEPS);
+}
+template <typename T, int MT, bool ANY>
+hipError_t go_few(const LinearArgs& a, hipStream_t s) {
+  XP_LAUNCH(sizeof(T) == 2 ? "k_linear_few<bf16>" : "k_linear_few<f32>", 2.0 * a.M * a.N * a.K, (k_linear_few<T, MT, ANY>),
+            dim3((unsigned)((a.N + 15) / 16)), dim3(FEW_WAVES * 64), 0, s, a);
+  return hipGetLastError();
+}
+template <typename T>
+hipError_t few(const LinearArgs& a, bool any, hipStream_t s) {
+  if (a.M <= 16) return any ? go_few<T, 1, true>(a, s) : go_few<T, 1, false>(a, s);
+  return any ? go_few<T, 2, true>(a, s) : go_few<T, 2, false>(a, s);
 }
 
 bool chunked(const void* p, int64_t ld, int chunk) {
   return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld % chunk == 0;
 }
 
-size_t up256(size_t b) { return (b + 255) / 256 * 256; }
-
-}  // namespace
-
-// Where the operands and the results lie: what a call needs of its workspace.
-LinearPlan linear_plan(int dtype, const LinearArgs& a) {
-  LinearPlan p{};
-  const int es = dtype == DT_BF16 ? 2 : 4, chunk = 16 / es;
-  const bool ta = a.epi == LIN_GRAD, tb = a.epi != LIN_FWD;
-  // a reduction along the rows has to end with a chunk
-  p.pack_a = !chunked(a.A, a.lda, chunk) || (!ta && a.K % chunk != 0);
-  p.pack_b = !chunked(a.B, a.ldb, chunk) || (!tb && a.K % chunk != 0);
-  auto cols = [&](bool tr, int64_t n) { return (tr ? n : (int64_t)a.K + chunk - 1) / chunk * chunk; };
-  p.a_cols = (int)(ta ? (a.M + chunk - 1) / chunk * chunk : cols(false, 0));
-  p.b_cols = (int)(tb ? ((int64_t)a.N + chunk - 1) / chunk * chunk : cols(false, 0));
-  Tile t;
-  pick(dtype, a.M, a.N, a.K, &t, &p.splits);
-  p.bm = t.bm;
-  const int bk = 128 / es;
+struct Plan {
+  int tile, splits;
+  int64_t kper, ldpart;
+  size_t part_b, bytes;  // offset of the bias gradient's partial sums, workspace
+};
+Plan plan(int dtype, const LinearArgs& a) {
+  Plan p{};
+  const int bk = dtype == DT_BF16 ? STEP<bf16_t> : STEP<float>;
   const int64_t steps = ((int64_t)a.K + bk - 1) / bk;
+  pick(dtype, a.M, a.N, steps, &p.tile, &p.splits);
   p.kper = (steps + p.splits - 1) / p.splits * bk;
   p.splits = (int)(((int64_t)a.K + p.kper - 1) / p.kper);  // those that hold something
+  if (p.splits == 1) return p;
   p.ldpart = (a.N + 7) / 8 * 8;
-  size_t off = 0;
-  if (p.pack_a) {
-    p.a_off = off;
-    off += up256((size_t)(ta ? a.K : a.M) * p.a_cols * es);
-  }
-  if (p.pack_b) {
-    p.b_off = off;
-    off += up256((size_t)(tb ? a.K : a.N) * p.b_cols * es);
-  }
-  if (p.splits > 1) {
-    p.part_off = off;
-    off += up256((size_t)p.splits * a.M * p.ldpart * sizeof(float));
-    p.part_b_off = off;
-    if (a.grad_b) off += up256((size_t)p.splits * a.M * sizeof(double));
-  }
-  p.bytes = off;
+  p.part_b = ((size_t)p.splits * a.M * p.ldpart * sizeof(float) + 255) / 256 * 256;
+  p.bytes = p.part_b + (a.grad_b ? (size_t)p.splits * a.M * sizeof(double) : 0);
   return p;
 }
 
-hipError_t launch_linear(int dtype, const LinearArgs& in, void* workspace, hipStream_t s) {
-  if (in.M <= 0 || in.N <= 0) return hipSuccess;
-  LinearArgs a = in;
-  const LinearPlan p = linear_plan(dtype, a);
+}  // namespace
+
+// A call's products with their packed operands: where those lie in the workspace
+// (before the partial sums, which the products use one after the other).
+namespace {
+struct Call {
+  LinearArgs p[2];
+  PackArgs pack;
+  size_t parts, bytes;
+  bool few;
+};
+Call lay_out(int dtype, const LinearArgs* in, int n, char* ws) {
+  Call c{};
   const int es = dtype == DT_BF16 ? 2 : 4, chunk = 16 / es;
-  const bool ta = a.epi == LIN_GRAD, tb = a.epi != LIN_FWD;
-  char* ws = (char*)workspace;
-  auto pack = [&](const void*& ptr, int64_t& ld, int64_t rows, int cols, int cols_out, size_t off) -> hipError_t {
-    void* dst = ws + off;
-    const double bytes = (double)rows * (cols + cols_out) * es;
-    if (dtype == DT_BF16)
-      XP_LAUNCH("k_linear_pack<bf16>", bytes, k_linear_pack<bf16_t>, dim3(grid_of(rows * cols_out)), dim3(256), 0, s,
-                (const bf16_t*)ptr, ld, rows, cols, (bf16_t*)dst, cols_out);
-    else
-      XP_LAUNCH("k_linear_pack<f32>", bytes, k_linear_pack<float>, dim3(grid_of(rows * cols_out)), dim3(256), 0, s,
-                (const float*)ptr, ld, rows, cols, (float*)dst, cols_out);
-    ptr = dst;
-    ld = cols_out;
-    return hipGetLastError();
+  c.few = in[0].M > 0 && takes_few(in[0], ((int64_t)in[0].K + 8 * chunk - 1) / (8 * chunk));
+  if (c.few) {
+    c.p[0] = in[0];
+    return c;
+  }
+  auto operand = [&](const void*& ptr, int64_t& ld, int64_t rows, int cols, bool must) {
+    PackArgs& k = c.pack;
+    int at = 0;
+    while (at < k.count && !(k.src[at] == ptr && k.ld[at] == ld && k.cols[at] == cols && k.rows[at] == rows)) ++at;
+    if (at == k.count) {
+      if (!must) return;
+      k.rows[at] = rows;
+      k.src[at] = ptr;
+      k.ld[at] = ld;
+      k.cols[at] = cols;
+      k.per_row[at] = (cols + chunk - 1) / chunk;
+      while (k.log[at] < 8 && 1 << k.log[at] < k.per_row[at]) ++k.log[at];
+      k.first[at] = k.blocks;
+      k.blocks += (int)(((rows << k.log[at]) + 255) / 256);
+      k.dst[at] = ws + c.bytes;
+      c.bytes += ((size_t)rows * k.per_row[at] * 16 + 255) / 256 * 256;
+      ++k.count;
+    }
+    ptr = k.dst[at];
+    ld = (int64_t)k.per_row[at] * chunk;
   };
-  if (p.pack_a) {
-    hipError_t e = pack(a.A, a.lda, ta ? a.K : a.M, ta ? (int)a.M : a.K, p.a_cols, p.a_off);
+  for (int i = 0; i < n; ++i) {
+    LinearArgs& a = c.p[i];
+    a = in[i];
+    if (a.M <= 0) continue;
+    const bool ta = a.epi == LIN_GRAD, tb = a.epi != LIN_FWD, tail = a.K % chunk != 0;
+    // a reduction along an operand's rows has to end with a chunk
+    operand(a.A, a.lda, ta ? a.K : a.M, ta ? (int)a.M : a.K, !chunked(a.A, a.lda, chunk) || (!ta && tail));
+    operand(a.B, a.ldb, tb ? a.K : a.N, tb ? a.N : a.K, !chunked(a.B, a.ldb, chunk) || (!tb && tail));
+  }
+  c.parts = c.bytes;
+  size_t parts = 0;
+  for (int i = 0; i < n; ++i)
+    if (c.p[i].M > 0) parts = std::max(parts, plan(dtype, c.p[i]).bytes);
+  c.bytes += parts;
+  return c;
+}
+}  // namespace
+
+size_t linear_bytes(int dtype, const LinearArgs* products, int n) { return lay_out(dtype, products, n, nullptr).bytes; }
+
+hipError_t launch_linear(int dtype, const LinearArgs* products, int n, void* workspace, hipStream_t s) {
+  const Call c = lay_out(dtype, products, n, (char*)workspace);
+  const int chunk = dtype == DT_BF16 ? CHUNK<bf16_t> : CHUNK<float>;
+  if (c.few) {
+    const LinearArgs& a = c.p[0];
+    const bool any = !chunked(a.A, a.lda, chunk) || !chunked(a.B, a.ldb, chunk) || a.K % chunk != 0;
+    return dtype == DT_BF16 ? few<bf16_t>(a, any, s) : few<float>(a, any, s);
+  }
+  if (c.pack.count > 0) {
+    const dim3 grid((unsigned)c.pack.blocks);
+    const double bytes = 2.0 * c.parts;
+    if (dtype == DT_BF16) XP_LAUNCH("k_linear_pack<bf16>", bytes, k_linear_pack<bf16_t>, grid, dim3(256), 0, s, c.pack);
+    else XP_LAUNCH("k_linear_pack<f32>", bytes, k_linear_pack<float>, grid, dim3(256), 0, s, c.pack);
+    hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (p.pack_b) {
-    hipError_t e = pack(a.B, a.ldb, tb ? a.K : a.N, tb ? a.N : a.K, p.b_cols, p.b_off);
+  for (int i = 0; i < n; ++i) {
+    LinearArgs a = c.p[i];
+    if (a.M <= 0) continue;
+    const Plan p = plan(dtype, a);
+    a.splits = p.splits;
+    a.kper = p.kper;
+    a.ldpart = p.ldpart;
+    a.ldg = a.N;
+    char* parts = (char*)workspace + c.parts;
+    a.part = p.splits > 1 ? (float*)parts : nullptr;
+    a.part_b = p.splits > 1 ? (double*)(parts + p.part_b) : nullptr;
+    a.vec = a.epi == LIN_GRAD
+                ? chunked(a.grad, a.N, 4)
+                : chunked(a.y, a.ldy, chunk) && (!a.res || chunked(a.res, a.ldr, chunk)) &&
+                      (!a.z_in || chunked(a.z_in, a.ldz, chunk)) && (!a.z_out || chunked(a.z_out, a.ldz, chunk));
+    hipError_t e = dtype == DT_BF16 ? by_kind<bf16_t>(a, p.tile, s) : by_kind<float>(a, p.tile, s);
     if (e != hipSuccess) return e;
   }
-  a.splits = p.splits;
-  a.kper = p.kper;
-  a.ldpart = p.ldpart;
-  a.part = p.splits > 1 ? (float*)(ws + p.part_off) : nullptr;
-  a.part_b = p.splits > 1 ? (double*)(ws + p.part_b_off) : nullptr;
-  a.vec = a.epi == LIN_GRAD
-              ? chunked(a.grad, a.N, 4)
-              : chunked(a.y, a.ldy, chunk) && (!a.res || chunked(a.res, a.ldr, chunk)) &&
-                    (!a.z_in || chunked(a.z_in, a.ldz, chunk)) && (!a.z_out || chunked(a.z_out, a.ldz, chunk));
-  const Tile t{p.bm, p.bm};
-  return dtype == DT_BF16 ? by_kind<bf16_t>(a, t, s) : by_kind<float>(a, t, s);
+  return hipSuccess;
 }
 
 hipError_t launch_act_bwd(int dtype, const void* dy, const void* z, void* dz, int64_t n, int act, hipStream_t s) {

@@ -86,7 +86,8 @@ xpipe_status fwd_product(const xpipe_linear_fwd_args* q, LinearArgs* a) {
 }
 
 // the backward's two products (M = 0 for one that is not asked for)
-xpipe_status bwd_products(const xpipe_linear_bwd_args* q, LinearArgs* data, LinearArgs* grad) {
+xpipe_status bwd_products(const xpipe_linear_bwd_args* q, LinearArgs (&p)[2]) {
+  LinearArgs *data = &p[0], *grad = &p[1];
   if (!q) return fail(XPIPE_EINVAL, "null arguments");
   XP_TRY(check_sizes(q->rows, q->cin, q->cout, q->dtype, q->act));
   *data = LinearArgs{};
@@ -255,19 +256,15 @@ xpipe_status xpipe_linear_fwd_query(const xpipe_linear_fwd_args* args, size_t* w
   if (!workspace_bytes) return fail(XPIPE_EINVAL, "null output");
   LinearArgs a;
   XP_TRY(fwd_product(args, &a));
-  *workspace_bytes = a.M > 0 ? linear_plan(args->dtype, a).bytes : 0;
+  *workspace_bytes = linear_bytes(args->dtype, &a, 1);
   return XPIPE_OK;
 }
 
 xpipe_status xpipe_linear_bwd_query(const xpipe_linear_bwd_args* args, size_t* workspace_bytes) {
   if (!workspace_bytes) return fail(XPIPE_EINVAL, "null output");
-  LinearArgs d, g;
-  XP_TRY(bwd_products(args, &d, &g));
-  // one after the other: they share the workspace
-  size_t need = 0;
-  if (d.M > 0) need = linear_plan(args->dtype, d).bytes;
-  if (g.M > 0) need = std::max(need, linear_plan(args->dtype, g).bytes);
-  *workspace_bytes = need;
+  LinearArgs p[2];
+  XP_TRY(bwd_products(args, p));
+  *workspace_bytes = linear_bytes(args->dtype, p, 2);
   return XPIPE_OK;
 }
 
@@ -276,20 +273,17 @@ xpipe_status xpipe_linear_fwd(const xpipe_linear_fwd_args* args, void* workspace
   LinearArgs a;
   XP_TRY(fwd_product(args, &a));
   if (a.M == 0) return XPIPE_OK;
-  XP_TRY(check_workspace(workspace, workspace_bytes, linear_plan(args->dtype, a).bytes));
-  XP_HIP(launch_linear(args->dtype, a, workspace, (hipStream_t)hip_stream));
+  XP_TRY(check_workspace(workspace, workspace_bytes, linear_bytes(args->dtype, &a, 1)));
+  XP_HIP(launch_linear(args->dtype, &a, 1, workspace, (hipStream_t)hip_stream));
   return XPIPE_OK;
 }
 
 xpipe_status xpipe_linear_bwd(const xpipe_linear_bwd_args* args, void* workspace, size_t workspace_bytes,
                               void* hip_stream) {
-  LinearArgs d, g;
-  size_t need = 0;
-  XP_TRY(bwd_products(args, &d, &g));
-  XP_TRY(xpipe_linear_bwd_query(args, &need));
-  XP_TRY(check_workspace(workspace, workspace_bytes, need));
-  if (d.M > 0) XP_HIP(launch_linear(args->dtype, d, workspace, (hipStream_t)hip_stream));
-  if (g.M > 0) XP_HIP(launch_linear(args->dtype, g, workspace, (hipStream_t)hip_stream));
+  LinearArgs p[2];
+  XP_TRY(bwd_products(args, p));
+  XP_TRY(check_workspace(workspace, workspace_bytes, linear_bytes(args->dtype, p, 2)));
+  XP_HIP(launch_linear(args->dtype, p, 2, workspace, (hipStream_t)hip_stream));
   return XPIPE_OK;
 }
 

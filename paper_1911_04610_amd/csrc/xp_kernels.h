@@ -341,20 +341,15 @@ struct LinearArgs {
   void* y; int64_t ldy;
   float* grad; float* grad_b;      // LIN_GRAD
   // set by the launcher: the reduction's parts (kper indices each), their sums
-  // [splits][M][ldpart], and whether every row allows 16-byte accesses
-  int splits; int64_t kper; int64_t ldpart;
+  // [splits][M][ldpart], the pitch of grad's rows, and whether every row allows
+  // 16-byte accesses
+  int splits; int64_t kper; int64_t ldpart, ldg;
   float* part; double* part_b;
   int vec;
 };
-struct LinearPlan {
-  int bm, splits;
-  int64_t kper, ldpart;
-  bool pack_a, pack_b;
-  int a_cols, b_cols;
-  size_t a_off, b_off, part_off, part_b_off, bytes;  // in the workspace
-};
-LinearPlan linear_plan(int dtype, const LinearArgs& a);
-hipError_t launch_linear(int dtype, const LinearArgs& a, void* workspace, hipStream_t s);
+// a call's products (M = 0: left out), one after the other, and their workspace
+size_t linear_bytes(int dtype, const LinearArgs* products, int n);
+hipError_t launch_linear(int dtype, const LinearArgs* products, int n, void* workspace, hipStream_t s);
 // dz = dy act'(z) over n elements
 hipError_t launch_act_bwd(int dtype, const void* dy, const void* z, void* dz, int64_t n, int act, hipStream_t s);
 
