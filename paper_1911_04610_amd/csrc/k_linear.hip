@@ -299,22 +299,21 @@ XP_DEV void read_col(const uint32_t (&at)[N], u32x4_t (&out)[N]) {
   for (int i = 0; i < N; ++i) out[i] = (u32x4_t){v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
 }
 
+// bytes of a step's two tiles
+template <int BM, int BN> constexpr int STAGE = (BM + BN) * 128;
+
 // One workgroup per BM x BN tile of the product and part of the reduction, WM x
 // WN waves of 32x32 MFMA results.  Both operands are copied from memory
 // straight into LDS, one step (128 bytes of the reduction) at a time, with NS
 // buffers: NS - 1 steps are in flight while one is multiplied.
 template <typename T, int BM, int BN, int WM, int WN, int NS, bool TA, bool TB, int EPI>
-__global__ __launch_bounds__(WM * WN * 64) void k_linear(LinearArgs a, int tiles_m, int tiles_n) {
+XP_DEV void linear_tile(const LinearArgs& a, int tiles_m, int tiles_n, int lin, unsigned char* st0, unsigned char* st1,
+                        unsigned char* st2, unsigned char* st3) {
   constexpr int NW = WM * WN, ES = (int)sizeof(T), C = CHUNK<T>, BK = STEP<T>;
   constexpr int WTM = BM / WM, WTN = BN / WN, TM = WTM / 32, TN = WTN / 32;
   static_assert(WTM % 32 == 0 && WTN % 32 == 0, "wave tile");
   constexpr int A_I = BM / 8 / NW, B_I = BN / 8 / NW;  // copies of 1 KB per wave and step
   static_assert(A_I * NW * 8 == BM && B_I * NW * 8 == BN, "whole copies per wave");
-  constexpr int SZ = (BM + BN) * 128;
-  __shared__ __align__(16) unsigned char st0[SZ];
-  __shared__ __align__(16) unsigned char st1[SZ];
-  __shared__ __align__(16) unsigned char st2[NS > 2 ? SZ : 16];
-  __shared__ __align__(16) unsigned char st3[NS > 3 ? SZ : 16];
   static_assert(NS >= 2 && NS <= 4, "stages");
   auto stage = [&](auto I) __attribute__((always_inline)) -> unsigned char* {
     constexpr int i = decltype(I)::value;
@@ -328,7 +327,6 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear(LinearArgs a, int tiles
 
   // tile order: runs of 8 tile rows, so that the tiles that one XCD holds at a
   // time share rows of both operands in its L2
-  const int lin = xcd_tile(blockIdx.x, gridDim.x);
   const int split = lin / (tiles_m * tiles_n), tile = lin - split * tiles_m * tiles_n;
   const int grp = tile / (8 * tiles_n), gm = min(8, tiles_m - grp * 8), in = tile - grp * 8 * tiles_n;
   const int tm = grp * 8 + in % gm, tn = in / gm;
@@ -576,7 +574,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear(LinearArgs a, int tiles
   // strip's epilogue reads is loaded before the strip before it is finished.  32x32
   // result: lane l, register r holds row 8 (r / 4) + 4 (l / 32) + r % 4, column l % 32.
   constexpr int PITCH = WTN + 4;
-  static_assert(NW * 16 * PITCH * 4 <= SZ, "strips");
+  static_assert(NW * 16 * PITCH * 4 <= STAGE<BM, BN>, "strips");
   float* strip = reinterpret_cast<float*>(st0) + wave * 16 * PITCH;
   const int64_t rows = a.M - m0;  // of the tile and below
   const LinearArgs t = from<T>(a, m0, n0);
@@ -633,6 +631,34 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear(LinearArgs a, int tiles
     }
     __builtin_amdgcn_wave_barrier();
   });
+}
+
+// (separate arrays: see frag)
+#define XP_STAGES(BM, BN, NS)                                                   \
+  __shared__ __align__(16) unsigned char st0[STAGE<BM, BN>];                    \
+  __shared__ __align__(16) unsigned char st1[STAGE<BM, BN>];                    \
+  __shared__ __align__(16) unsigned char st2[NS > 2 ? STAGE<BM, BN> : 16];      \
+  __shared__ __align__(16) unsigned char st3[NS > 3 ? STAGE<BM, BN> : 16]
+
+template <typename T, int BM, int BN, int WM, int WN, int NS, bool TA, bool TB, int EPI>
+__global__ __launch_bounds__(WM * WN * 64) void k_linear(LinearArgs a, int tiles_m, int tiles_n) {
+  XP_STAGES(BM, BN, NS);
+  linear_tile<T, BM, BN, WM, WN, NS, TA, TB, EPI>(a, tiles_m, tiles_n, xcd_tile(blockIdx.x, gridDim.x), st0, st1, st2, st3);
+}
+
+// Both products of a backward in one launch: the first `first` workgroups are the
+// data gradient's.  They depend on nothing of each other's, and small ones alone
+// leave most of the GPU idle.
+template <typename T, int B, int NS>
+__global__ __launch_bounds__(256) void k_linear_bwd(LinearArgs d, int tiles_md, int tiles_nd, int first, LinearArgs g,
+                                                    int tiles_mg, int tiles_ng) {
+  XP_STAGES(B, B, NS);
+  const int b = blockIdx.x;
+  if (b < first)
+    linear_tile<T, B, B, 2, 2, NS, false, true, LIN_DATA>(d, tiles_md, tiles_nd, xcd_tile(b, first), st0, st1, st2, st3);
+  else
+    linear_tile<T, B, B, 2, 2, NS, true, true, LIN_GRAD>(g, tiles_mg, tiles_ng, xcd_tile(b - first, gridDim.x - first), st0,
+                                                         st1, st2, st3);
 }
 
 // the splits' partial sums added in order, and the epilogue
@@ -891,6 +917,13 @@ void pick(int dtype, int64_t M, int N, int64_t steps, int* tile, int* splits) {
   }
 }
 
+template <typename T, int EPI>
+hipError_t join(const LinearArgs& a, hipStream_t s) {
+  XP_LAUNCH("k_linear_join", 4.0 * a.M * a.N * a.splits, (k_linear_join<T, EPI>),
+            dim3(grid_of(a.M * ((a.N + CHUNK<T> - 1) / CHUNK<T>))), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
 template <typename T, int BM, int BN, int WM, int WN, int NS, bool TA, bool TB, int EPI>
 hipError_t go(const LinearArgs& a, hipStream_t s) {
   const int64_t tm = (a.M + BM - 1) / BM, tn = (a.N + BN - 1) / BN;
@@ -902,22 +935,42 @@ hipError_t go(const LinearArgs& a, hipStream_t s) {
   XP_LAUNCH(name.s, 2.0 * a.M * a.N * a.K, (k_linear<T, BM, BN, WM, WN, NS, TA, TB, EPI>),
             dim3((unsigned)(tm * tn * a.splits)), dim3(WM * WN * 64), 0, s, a, (int)tm, (int)tn);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !a.part) return e;
-  XP_LAUNCH("k_linear_join", 4.0 * a.M * a.N * a.splits, (k_linear_join<T, EPI>),
-            dim3(grid_of(a.M * ((a.N + CHUNK<T> - 1) / CHUNK<T>))), dim3(256), 0, s, a);
-  return hipGetLastError();
+  return e != hipSuccess || !a.part ? e : join<T, EPI>(a, s);
+}
+
+template <typename T, int B, int NS>
+hipError_t go_bwd(const LinearArgs& d, const LinearArgs& g, hipStream_t s) {
+  const int64_t tmd = (d.M + B - 1) / B, tnd = (d.N + B - 1) / B, tmg = (g.M + B - 1) / B, tng = (g.N + B - 1) / B;
+  const int64_t first = tmd * tnd * d.splits;
+  static const struct Name {
+    char s[64];
+    Name() { snprintf(s, sizeof s, "k_linear_bwd<%s,%d>", sizeof(T) == 2 ? "bf16" : "f32", B); }
+  } name;
+  XP_LAUNCH(name.s, 2.0 * d.M * d.N * d.K + 2.0 * g.M * g.N * g.K, (k_linear_bwd<T, B, NS>),
+            dim3((unsigned)(first + tmg * tng * g.splits)), dim3(256), 0, s, d, (int)tmd, (int)tnd, (int)first, g, (int)tmg,
+            (int)tng);
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess && d.part) e = join<T, LIN_DATA>(d, s);
+  if (e == hipSuccess && g.part) e = join<T, LIN_GRAD>(g, s);
+  return e;
 }
 
 // Buffers: two for 128x128 tiles (two workgroups per CU; four buffers and one
 // workgroup were 0 to 5% slower), four for 64x64 (products of a few workgroups
 // per CU: 5 to 15% over two).
+constexpr int NS_128 = 2, NS_64 = 4;
 template <typename T, bool TA, bool TB, int EPI>
 hipError_t by_tile(const LinearArgs& a, int tile, hipStream_t s) {
   if constexpr (sizeof(T) == 2) {
     if (tile == 256) return go<T, 256, 256, 2, 4, 2, TA, TB, EPI>(a, s);
   }
-  if (tile == 128) return go<T, 128, 128, 2, 2, 2, TA, TB, EPI>(a, s);
-  return go<T, 64, 64, 2, 2, 4, TA, TB, EPI>(a, s);
+  if (tile == 128) return go<T, 128, 128, 2, 2, NS_128, TA, TB, EPI>(a, s);
+  return go<T, 64, 64, 2, 2, NS_64, TA, TB, EPI>(a, s);
+}
+
+template <typename T>
+hipError_t both(const LinearArgs& d, const LinearArgs& g, int tile, hipStream_t s) {
+  return tile == 128 ? go_bwd<T, 128, NS_128>(d, g, s) : go_bwd<T, 64, NS_64>(d, g, s);
 }
 
 template <typename T>
@@ -972,13 +1025,13 @@ Plan plan(int dtype, const LinearArgs& a) {
 
 }  // namespace
 
-// A call's products with their packed operands: where those lie in the workspace
-// (before the partial sums, which the products use one after the other).
+// A call's products with their packed operands: where those and the products' partial
+// sums lie in the workspace.
 namespace {
 struct Call {
   LinearArgs p[2];
   PackArgs pack;
-  size_t parts, bytes;
+  size_t parts[2], bytes;
   bool few;
 };
 Call lay_out(int dtype, const LinearArgs* in, int n, char* ws) {
@@ -1019,11 +1072,10 @@ Call lay_out(int dtype, const LinearArgs* in, int n, char* ws) {
     operand(a.A, a.lda, ta ? a.K : a.M, ta ? (int)a.M : a.K, !chunked(a.A, a.lda, chunk) || (!ta && tail));
     operand(a.B, a.ldb, tb ? a.K : a.N, tb ? a.N : a.K, !chunked(a.B, a.ldb, chunk) || (!tb && tail));
   }
-  c.parts = c.bytes;
-  size_t parts = 0;
-  for (int i = 0; i < n; ++i)
-    if (c.p[i].M > 0) parts = std::max(parts, plan(dtype, c.p[i]).bytes);
-  c.bytes += parts;
+  for (int i = 0; i < n; ++i) {
+    c.parts[i] = c.bytes;
+    if (c.p[i].M > 0) c.bytes += (plan(dtype, c.p[i]).bytes + 255) / 256 * 256;
+  }
   return c;
 }
 }  // namespace
@@ -1040,28 +1092,38 @@ hipError_t launch_linear(int dtype, const LinearArgs* products, int n, void* wor
   }
   if (c.pack.count > 0) {
     const dim3 grid((unsigned)c.pack.blocks);
-    const double bytes = 2.0 * c.parts;
+    const double bytes = 2.0 * c.parts[0];
     if (dtype == DT_BF16) XP_LAUNCH("k_linear_pack<bf16>", bytes, k_linear_pack<bf16_t>, grid, dim3(256), 0, s, c.pack);
     else XP_LAUNCH("k_linear_pack<f32>", bytes, k_linear_pack<float>, grid, dim3(256), 0, s, c.pack);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
+  LinearArgs a[2];
+  int tile[2] = {0, 0};
   for (int i = 0; i < n; ++i) {
-    LinearArgs a = c.p[i];
-    if (a.M <= 0) continue;
-    const Plan p = plan(dtype, a);
-    a.splits = p.splits;
-    a.kper = p.kper;
-    a.ldpart = p.ldpart;
-    a.ldg = a.N;
-    char* parts = (char*)workspace + c.parts;
-    a.part = p.splits > 1 ? (float*)parts : nullptr;
-    a.part_b = p.splits > 1 ? (double*)(parts + p.part_b) : nullptr;
-    a.vec = a.epi == LIN_GRAD
-                ? chunked(a.grad, a.N, 4)
-                : chunked(a.y, a.ldy, chunk) && (!a.res || chunked(a.res, a.ldr, chunk)) &&
-                      (!a.z_in || chunked(a.z_in, a.ldz, chunk)) && (!a.z_out || chunked(a.z_out, a.ldz, chunk));
-    hipError_t e = dtype == DT_BF16 ? by_kind<bf16_t>(a, p.tile, s) : by_kind<float>(a, p.tile, s);
+    if (c.p[i].M <= 0) continue;
+    LinearArgs& q = a[i];
+    q = c.p[i];
+    const Plan p = plan(dtype, q);
+    char* parts = (char*)workspace + c.parts[i];
+    tile[i] = p.tile;
+    q.splits = p.splits;
+    q.kper = p.kper;
+    q.ldpart = p.ldpart;
+    q.ldg = q.N;
+    q.part = p.splits > 1 ? (float*)parts : nullptr;
+    q.part_b = p.splits > 1 ? (double*)(parts + p.part_b) : nullptr;
+    q.vec = q.epi == LIN_GRAD
+                ? chunked(q.grad, q.N, 4)
+                : chunked(q.y, q.ldy, chunk) && (!q.res || chunked(q.res, q.ldr, chunk)) &&
+                      (!q.z_in || chunked(q.z_in, q.ldz, chunk)) && (!q.z_out || chunked(q.z_out, q.ldz, chunk));
+  }
+  // (256x256 tiles fill the GPU by themselves)
+  if (tile[0] == tile[1] && tile[0] > 0 && tile[0] <= 128)
+    return dtype == DT_BF16 ? both<bf16_t>(a[0], a[1], tile[0], s) : both<float>(a[0], a[1], tile[0], s);
+  for (int i = 0; i < n; ++i) {
+    if (tile[i] == 0) continue;
+    hipError_t e = dtype == DT_BF16 ? by_kind<bf16_t>(a[i], tile[i], s) : by_kind<float>(a[i], tile[i], s);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;

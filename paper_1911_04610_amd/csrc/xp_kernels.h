@@ -347,7 +347,8 @@ struct LinearArgs {
   float* part; double* part_b;
   int vec;
 };
-// a call's products (M = 0: left out), one after the other, and their workspace
+// a call's products (a forward; a backward's data and weight gradient, M = 0: left
+// out) and their workspace
 size_t linear_bytes(int dtype, const LinearArgs* products, int n);
 hipError_t launch_linear(int dtype, const LinearArgs* products, int n, void* workspace, hipStream_t s);
 // dz = dy act'(z) over n elements
