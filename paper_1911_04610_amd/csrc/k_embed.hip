@@ -67,26 +67,29 @@ __global__ __launch_bounds__(256) void k_embed_fwd(EmbedArgs a) {
 XP_DEV uint32_t sort_key(int t, int vocab) { return (uint32_t)t < (uint32_t)vocab ? (uint32_t)t : (uint32_t)vocab; }
 
 // Few positions: a position's place is the number of positions before it in the
-// order.  256 positions per workgroup, four threads each, over all keys.
+// order.  64 positions per workgroup, a lane of each wave; the sixteen waves go
+// through all keys, every sixteenth four of them each.  (8192 keys in 128
+// workgroups take as long as the radix sort's four launches.)
 constexpr int RANK_MAX = 8192;
 __global__ __launch_bounds__(1024) void k_embed_rank(const int32_t* __restrict__ tokens, int n, int vocab,
                                                       uint32_t* __restrict__ keys, uint32_t* __restrict__ pos) {
   __shared__ __align__(16) uint32_t sk[RANK_MAX];
-  __shared__ int sums[4][256];
-  const int tid = threadIdx.x, part = tid >> 8, li = tid & 255;
+  __shared__ int sums[16][64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int pad = (n + 3) / 4 * 4;
   for (int j = tid; j < pad; j += 1024) sk[j] = j < n ? sort_key(tokens[j], vocab) : ~0u;
   __syncthreads();
-  const int i0 = blockIdx.x * 256, i = i0 + li;
+  const int i0 = blockIdx.x * 64, i = i0 + lane;
   const uint32_t key = i < n ? sk[i] : 0u;
   int rank = 0;
   // before the workgroup's own positions equal keys count, after them they do not
-  for (int j = part * 4; j < pad; j += 16) {
+#pragma unroll 4
+  for (int j = wave * 4; j < pad; j += 64) {
     const u32x4_t k = *reinterpret_cast<const u32x4_t*>(sk + j);
     if (j < i0) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) rank += k[q] <= key;
-    } else if (j >= i0 + 256) {
+    } else if (j >= i0 + 64) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) rank += k[q] < key;
     } else {
@@ -94,10 +97,12 @@ __global__ __launch_bounds__(1024) void k_embed_rank(const int32_t* __restrict__
       for (int q = 0; q < 4; ++q) rank += k[q] < key || (k[q] == key && j + q < i);
     }
   }
-  sums[part][li] = rank;
+  sums[wave][lane] = rank;
   __syncthreads();
-  if (part == 0 && i < n) {
-    const int at = sums[0][li] + sums[1][li] + sums[2][li] + sums[3][li];
+  if (wave == 0 && i < n) {
+    int at = 0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) at += sums[w][lane];
     keys[at] = key;
     pos[at] = (uint32_t)i;
   }
@@ -130,6 +135,7 @@ __global__ __launch_bounds__(256) void k_embed_scatter(const uint32_t* __restric
                                                        int shift, const uint32_t* __restrict__ hist,
                                                        uint32_t* __restrict__ keys_out, uint32_t* __restrict__ pos_out) {
   __shared__ uint32_t off[4][RADIX];
+  __shared__ __align__(16) uint32_t sums[4][2][RADIX];
   __shared__ uint32_t wsum[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
 #pragma unroll
@@ -138,13 +144,25 @@ __global__ __launch_bounds__(256) void k_embed_scatter(const uint32_t* __restric
   const int64_t beg = blockIdx.x * per + wave * (per / 4), end = min(n, beg + per / 4);
   for (int64_t i = beg + lane; i < end; i += 64)
     atomicAdd(&off[wave][(first_key(keys, tokens, vocab, i) >> shift) & (RADIX - 1)], 1u);
-  // of digit tid: how many positions all workgroups, and the ones before this one, hold
-  uint32_t all = 0, before = 0;
-#pragma unroll 8
-  for (int b = 0; b < (int)gridDim.x; ++b) {
-    const uint32_t h = hist[(int64_t)b * RADIX + tid];
-    all += h;
-    before += b < (int)blockIdx.x ? h : 0u;
+  // how many positions all workgroups, and the ones before this one, hold of each
+  // digit: a wave adds every fourth workgroup's counts, a lane four digits
+  {
+    u32x4_t sa = {0u, 0u, 0u, 0u}, sb = {0u, 0u, 0u, 0u};
+#pragma unroll 16
+    for (int b = wave; b < (int)gridDim.x; b += 4) {
+      const u32x4_t h = *reinterpret_cast<const u32x4_t*>(hist + (int64_t)b * RADIX + lane * 4);
+      sa += h;
+      sb += b < (int)blockIdx.x ? h : (u32x4_t){0u, 0u, 0u, 0u};
+    }
+    *reinterpret_cast<u32x4_t*>(&sums[wave][0][lane * 4]) = sa;
+    *reinterpret_cast<u32x4_t*>(&sums[wave][1][lane * 4]) = sb;
+  }
+  __syncthreads();
+  uint32_t all = 0, before = 0;  // of digit tid
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    all += sums[w][0][tid];
+    before += sums[w][1][tid];
   }
   uint32_t scan = all;  // inclusive over the wave's digits, then the waves
 #pragma unroll
@@ -196,7 +214,7 @@ __global__ __launch_bounds__(256) void k_embed_scatter(const uint32_t* __restric
 // k_embed_join; a run that does both is part 0.  Rows are taken GROUP at a
 // time, with the accumulators' rows that they end in, so that the loads of a
 // group are in flight together.
-constexpr int GROUP = 8;
+constexpr int GROUP = 4;
 template <typename T, bool VEC>
 __global__ __launch_bounds__(64) void k_embed_bwd(EmbedArgs a, const uint32_t* __restrict__ keys,
                                                   const uint32_t* __restrict__ pos, int span, float* __restrict__ part) {
@@ -213,7 +231,8 @@ __global__ __launch_bounds__(64) void k_embed_bwd(EmbedArgs a, const uint32_t* _
   for (int64_t g = beg; g < end; g += GROUP) {
     uint32_t key[GROUP];
     bool last[GROUP], whole[GROUP];
-    float v[GROUP][C], o[GROUP][C];
+    u32x4_t v[GROUP];  // (not VEC: one element)
+    float o[GROUP][C];
     bool h = head;
 #pragma unroll
     for (int j = 0; j < GROUP; ++j) {
@@ -227,8 +246,8 @@ __global__ __launch_bounds__(64) void k_embed_bwd(EmbedArgs a, const uint32_t* _
       if (in && !more) h = false;
       if (!live) continue;
       const T* row = dy + (int64_t)pos[i] * a.dim;
-      if constexpr (VEC) unpack<T>(*reinterpret_cast<const u32x4_t*>(row), v[j]);
-      else v[j][0] = (float)ldd(row);
+      if constexpr (VEC) v[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(row));
+      else v[j][0] = __float_as_uint((float)ldd(row));
       if (whole[j]) {
         const float* gr = grad + (int64_t)key[j] * a.dim;
 #pragma unroll
@@ -238,8 +257,14 @@ __global__ __launch_bounds__(64) void k_embed_bwd(EmbedArgs a, const uint32_t* _
 #pragma unroll
     for (int j = 0; j < GROUP; ++j) {
       if (key[j] >= (uint32_t)a.vocab) continue;
+      if constexpr (VEC) {
+        float e[C];
+        unpack<T>(v[j], e);
 #pragma unroll
-      for (int q = 0; q < C; ++q) acc[q] += (double)v[j][q];
+        for (int q = 0; q < C; ++q) acc[q] += (double)e[q];
+      } else {
+        acc[0] += (double)__uint_as_float(v[j][0]);
+      }
       if (!last[j]) continue;
       if (whole[j]) {
         float* gr = grad + (int64_t)key[j] * a.dim;
@@ -259,16 +284,17 @@ __global__ __launch_bounds__(64) void k_embed_bwd(EmbedArgs a, const uint32_t* _
 }
 
 // The runs that pass a span's end: the span that a run starts in adds its
-// partials.  Eight groups of 128 threads (one column each) take consecutive
-// parts of the run's spans, and the groups are added in order.
-__global__ __launch_bounds__(1024) void k_embed_join(EmbedArgs a, const uint32_t* __restrict__ keys, int span,
-                                                      const float* __restrict__ part) {
-  __shared__ double sums[8][128];
+// partials.  Four waves take consecutive parts of the run's spans, 64 JOIN_COLS
+// columns each, and their sums are added in order.
+constexpr int JOIN_COLS = 4;
+__global__ __launch_bounds__(256) void k_embed_join(EmbedArgs a, const uint32_t* __restrict__ keys, int span,
+                                                     const float* __restrict__ part) {
+  __shared__ double sums[3][64][JOIN_COLS];
   const int64_t c = blockIdx.x, beg = c * span, next = beg + span;
   if (next >= a.n) return;
-  const uint32_t key = keys[next - 1];
-  if (key >= (uint32_t)a.vocab || keys[next] != key) return;           // no run passes the end
-  if (beg > 0 && keys[beg] == key && keys[beg - 1] == key) return;      // it started before this span
+  const uint32_t key = keys[next - 1], kn = keys[next], kb = keys[beg], kp = keys[beg > 0 ? beg - 1 : 0];
+  if (key >= (uint32_t)a.vocab || kn != key) return;  // no run passes the end
+  if (beg > 0 && kb == key && kp == key) return;       // it started before this span
   const int64_t spans = (a.n + span - 1) / span;
   // the run's last span: steps that double, then back
   int64_t lo = c + 1, step = 1;
@@ -279,33 +305,139 @@ __global__ __launch_bounds__(1024) void k_embed_join(EmbedArgs a, const uint32_t
   for (; step > 0; step /= 2)
     if (lo + step < spans && keys[(lo + step) * span] == key) lo += step;
   const int64_t cnt = lo - c;  // spans behind the first one
-  const int g = threadIdx.x >> 7, lc = threadIdx.x & 127;
-  const int64_t per = (cnt + 7) / 8, s0 = c + 1 + g * per, s1 = min(lo + 1, s0 + per);
-  for (int64_t col0 = (int64_t)blockIdx.y * 128; col0 < a.dim; col0 += (int64_t)gridDim.y * 128) {
-    const int64_t col = col0 + lc;
-    double t = 0.0;
-    if (col < a.dim) {
-      if (g == 0) t = (double)part[(c * 2 + 1) * a.dim + col];
-#pragma unroll 8
-      for (int64_t s = s0; s < s1; ++s) t += (double)part[s * 2 * a.dim + col];
-    }
-    sums[g][lc] = t;
-    __syncthreads();
-    if (g == 0 && col < a.dim) {
+  const int g = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int64_t per = max((int64_t)4, (cnt + 3) / 4), s0 = c + 1 + g * per, s1 = min(lo + 1, s0 + per);
+  for (int64_t col = ((int64_t)blockIdx.y * 64 + lane) * JOIN_COLS; col - lane * JOIN_COLS < a.dim;
+       col += (int64_t)gridDim.y * 64 * JOIN_COLS) {
+    const int cols = (int)max((int64_t)0, min((int64_t)JOIN_COLS, a.dim - col));
+    const bool vec = cols == JOIN_COLS && a.dim % JOIN_COLS == 0;  // (the partials' rows are 16-byte aligned then)
+    double t[JOIN_COLS];
 #pragma unroll
-      for (int q = 1; q < 8; ++q) t += sums[q][lc];
-      float* o = a.grad + (int64_t)key * a.dim + col;
-      *o = (float)((double)*o + a.scale * t);
+    for (int q = 0; q < JOIN_COLS; ++q) t[q] = 0.0;
+    auto add = [&](const float* p) __attribute__((always_inline)) {
+      if (vec) {
+        const f32x4_t v = *reinterpret_cast<const f32x4_t*>(p);
+#pragma unroll
+        for (int q = 0; q < JOIN_COLS; ++q) t[q] += (double)v[q];
+      } else {
+#pragma unroll
+        for (int q = 0; q < JOIN_COLS; ++q)
+          if (q < cols) t[q] += (double)p[q];
+      }
+    };
+    if (g == 0) add(part + (c * 2 + 1) * a.dim + col);
+#pragma unroll 8
+    for (int64_t s = s0; s < s1; ++s) add(part + s * 2 * a.dim + col);
+    if (g > 0) {
+#pragma unroll
+      for (int q = 0; q < JOIN_COLS; ++q) sums[g - 1][lane][q] = t[q];
     }
     __syncthreads();
+    if (g == 0) {
+      float* o = a.grad + (int64_t)key * a.dim + col;
+#pragma unroll
+      for (int q = 0; q < JOIN_COLS; ++q) {
+        if (q >= cols) continue;
+        const double v = ((t[q] + sums[0][lane][q]) + sums[1][lane][q]) + sums[2][lane][q];
+        o[q] = (float)((double)o[q] + a.scale * v);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// ---------------------------------------------------------------- few positions
+// Without a sort: the workgroup of the first position that holds a token adds all
+// of its positions' rows, 64 chunks of columns a wave, each of its four waves a
+// consecutive part of them; the others find an earlier one and end.  One launch.
+constexpr int SMALL_MAX = 1024;
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void k_embed_bwd_small(EmbedArgs a) {
+  constexpr int C = VEC ? CHUNK<T> : 1;
+  __shared__ uint64_t mask[SMALL_MAX / 64];
+  __shared__ int list[SMALL_MAX];
+  __shared__ double sums[3][64][C];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = blockIdx.x;
+  const int t = a.tokens[i], n = (int)a.n;
+  if (t < 0 || t >= a.vocab) return;
+#pragma unroll
+  for (int q = 0; q < SMALL_MAX / 256; ++q) {
+    const int j = q * 256 + tid;
+    const uint64_t m = __ballot(j < n && a.tokens[min(j, n - 1)] == t);
+    if (lane == 0) mask[q * 4 + wave] = m;
+  }
+  __syncthreads();
+  // the token's positions in order, and whether i is the first
+  int count = 0;
+  bool first = true;
+#pragma unroll
+  for (int w = 0; w < SMALL_MAX / 64; ++w) {
+    const uint64_t m = mask[w];
+    const uint64_t low = i >= (w + 1) * 64 ? ~(uint64_t)0 : i <= w * 64 ? 0 : ((uint64_t)1 << (i - w * 64)) - 1;
+    first = first && (m & low) == 0;
+    if (w % 4 == wave && (m >> lane & 1))
+      list[count + __popcll(m & (((uint64_t)1 << lane) - 1))] = w * 64 + lane;
+    count += __popcll(m);
+  }
+  if (!first) return;
+  __syncthreads();
+  const int per = max(8, (count + 3) / 4), s0 = min(count, wave * per), s1 = min(count, s0 + per);
+  const int64_t col = ((int64_t)blockIdx.y * 64 + lane) * C;
+  const bool live = col < a.dim;
+  double acc[C];
+#pragma unroll
+  for (int q = 0; q < C; ++q) acc[q] = 0.0;
+  float* o = a.grad + (int64_t)t * a.dim + col;
+  float old[C];
+  if (live && wave == 0) {
+#pragma unroll
+    for (int q = 0; q < C; ++q) old[q] = o[q];
+  }
+  if (live) {
+    const T* dy = (const T*)a.dy + col;
+#pragma unroll 8
+    for (int s = s0; s < s1; ++s) {
+      const T* row = dy + (int64_t)list[s] * a.dim;
+      if constexpr (VEC) {
+        float e[C];
+        unpack<T>(*reinterpret_cast<const u32x4_t*>(row), e);
+#pragma unroll
+        for (int q = 0; q < C; ++q) acc[q] += (double)e[q];
+      } else {
+        acc[0] += ldd(row);
+      }
+    }
+  }
+  if (count > per) {  // (the same for the whole workgroup)
+    if (wave > 0) {
+#pragma unroll
+      for (int q = 0; q < C; ++q) sums[wave - 1][lane][q] = acc[q];
+    }
+    __syncthreads();
+    if (wave == 0) {
+#pragma unroll
+      for (int w = 0; w < 3; ++w)
+#pragma unroll
+        for (int q = 0; q < C; ++q) acc[q] += sums[w][lane][q];
+    }
+  }
+  if (live && wave == 0) {
+#pragma unroll
+    for (int q = 0; q < C; ++q) o[q] = (float)((double)old[q] + a.scale * acc[q]);
   }
 }
 
 size_t up256(size_t b) { return (b + 255) / 256 * 256; }
 bool aligned(const void* p, int64_t dim, int chunk) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && dim % chunk == 0; }
 
-// sorted positions per wave of the gradient: enough waves for small calls, few partials for large ones
-int span_of(int64_t n) { return n >= 16384 ? 64 : n >= 2048 ? 16 : 8; }
+// sorted positions per wave of the gradient: as many as leave some 4096 waves (the
+// fewer spans, the fewer partials), 8 to 64
+int span_of(int64_t n, int64_t dim) {
+  const int64_t waves = n * ((dim + 511) / 512);
+  int span = 8;
+  while (span < 64 && waves > (int64_t)4096 * span) span *= 2;
+  return span;
+}
 
 int64_t sort_per(int64_t n) { return std::max<int64_t>(1024, ((n + SORT_BLOCKS - 1) / SORT_BLOCKS + 255) / 256 * 256); }
 
@@ -326,7 +458,7 @@ Layout layout(int64_t n, int64_t dim) {
     l.pos[s] = take((size_t)n * 4);
   }
   if (n > RANK_MAX) l.hist = take((size_t)SORT_BLOCKS * RADIX * 4);
-  l.part = take((size_t)((n + span_of(n) - 1) / span_of(n)) * 2 * dim * sizeof(float));
+  l.part = take((size_t)((n + span_of(n, dim) - 1) / span_of(n, dim)) * 2 * dim * sizeof(float));
   l.bytes = off;
   return l;
 }
@@ -349,16 +481,32 @@ hipError_t launch_embed_fwd(int dtype, const EmbedArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-size_t embed_bwd_bytes(int64_t n, int64_t dim) { return n <= 0 ? 0 : layout(n, dim).bytes; }
+size_t embed_bwd_bytes(int64_t n, int64_t dim) { return n <= SMALL_MAX ? 0 : layout(n, dim).bytes; }
 
 hipError_t launch_embed_bwd(int dtype, const EmbedArgs& a, void* workspace, hipStream_t s) {
   if (a.n <= 0 || a.dim <= 0) return hipSuccess;
+  const int es = dtype == DT_BF16 ? 2 : 4, chunk = 16 / es;
+  // (the accumulator's rows need no alignment of their own: their elements are 4 bytes wide)
+  const bool vec = aligned(a.dy, a.dim, chunk);
+  const double bytes = (double)a.n * a.dim * es;
+  const unsigned col_blocks = (unsigned)(((vec ? a.dim / chunk : a.dim) + 63) / 64);
+  if (a.n <= SMALL_MAX) {
+    const dim3 grid((unsigned)a.n, col_blocks);
+    if (dtype == DT_BF16) {
+      if (vec) XP_LAUNCH("k_embed_bwd_small<bf16>", bytes, (k_embed_bwd_small<bf16_t, true>), grid, dim3(256), 0, s, a);
+      else XP_LAUNCH("k_embed_bwd_small<bf16>", bytes, (k_embed_bwd_small<bf16_t, false>), grid, dim3(256), 0, s, a);
+    } else {
+      if (vec) XP_LAUNCH("k_embed_bwd_small<f32>", bytes, (k_embed_bwd_small<float, true>), grid, dim3(256), 0, s, a);
+      else XP_LAUNCH("k_embed_bwd_small<f32>", bytes, (k_embed_bwd_small<float, false>), grid, dim3(256), 0, s, a);
+    }
+    return hipGetLastError();
+  }
   char* ws = (char*)workspace;
   const Layout l = layout(a.n, a.dim);
   uint32_t *keys = (uint32_t*)(ws + l.keys[0]), *pos = (uint32_t*)(ws + l.pos[0]);
   hipError_t e;
   if (a.n <= RANK_MAX) {
-    XP_LAUNCH("k_embed_rank", 12.0 * a.n, k_embed_rank, dim3((unsigned)((a.n + 255) / 256)), dim3(1024), 0, s, a.tokens,
+    XP_LAUNCH("k_embed_rank", 12.0 * a.n, k_embed_rank, dim3((unsigned)((a.n + 63) / 64)), dim3(1024), 0, s, a.tokens,
               (int)a.n, a.vocab, keys, pos);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -383,14 +531,10 @@ hipError_t launch_embed_bwd(int dtype, const EmbedArgs& a, void* workspace, hipS
       pos = po;
     }
   }
-  const int es = dtype == DT_BF16 ? 2 : 4, chunk = 16 / es, span = span_of(a.n);
-  // (the accumulator's rows need no alignment of their own: their elements are 4 bytes wide)
-  const bool vec = aligned(a.dy, a.dim, chunk);
+  const int span = span_of(a.n, a.dim);
   const unsigned spans = (unsigned)((a.n + span - 1) / span);
-  const int64_t cols = vec ? a.dim / chunk : a.dim;
-  const dim3 grid(spans, (unsigned)((cols + 63) / 64));
+  const dim3 grid(spans, col_blocks);
   float* part = (float*)(ws + l.part);
-  const double bytes = (double)a.n * a.dim * es;
   if (dtype == DT_BF16) {
     if (vec) XP_LAUNCH("k_embed_bwd<bf16>", bytes, (k_embed_bwd<bf16_t, true>), grid, dim3(64), 0, s, a, keys, pos, span, part);
     else XP_LAUNCH("k_embed_bwd<bf16>", bytes, (k_embed_bwd<bf16_t, false>), grid, dim3(64), 0, s, a, keys, pos, span, part);
@@ -400,8 +544,8 @@ hipError_t launch_embed_bwd(int dtype, const EmbedArgs& a, void* workspace, hipS
   }
   e = hipGetLastError();
   if (e != hipSuccess || spans < 2) return e;
-  XP_LAUNCH("k_embed_join", 0.0, k_embed_join, dim3(spans - 1, (unsigned)std::min<int64_t>(8, (a.dim + 127) / 128)),
-            dim3(1024), 0, s, a, keys, span, part);
+  XP_LAUNCH("k_embed_join", 0.0, k_embed_join, dim3(spans - 1, (unsigned)std::min<int64_t>(16, (a.dim + 64 * JOIN_COLS - 1) / (64 * JOIN_COLS))),
+            dim3(256), 0, s, a, keys, span, part);
   return hipGetLastError();
 }
 
