@@ -413,8 +413,8 @@ xpipe_status xpipe_rule_flat_clipped(float* W, float* buf, float* sq, float* m, 
  * alone, so a repeated call gives the same bits.  tensors: host array, read by
  * the call itself; each tensor contiguous, aligned to its element, of dtype
  * XPIPE_F32 or XPIPE_BF16 (one for all), n >= 0.  workspace: device memory,
- * 8-byte aligned, of xpipe_grad_norm_query's bytes, free again once the call's
- * work is done.  sumsq (device, fp64, may be NULL) receives the sum;
+ * 8-byte aligned, of xpipe_grad_norm_query's bytes (0 for small lists), free
+ * again once the call's work is done.  sumsq (device, fp64, may be NULL) receives the sum;
  * norm_coef (device, two fp32, may be NULL) {norm, coefficient}.  max_norm > 0
  * where norm_coef is given. */
 typedef struct {

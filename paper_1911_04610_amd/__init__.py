@@ -23,6 +23,7 @@ from __future__ import annotations
 import ctypes
 import dataclasses
 import os
+import struct
 from typing import List, Optional, Sequence
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -124,6 +125,7 @@ class Hyper:
 
 
 _lib = None
+_torch = None  # set with the library
 _P = ctypes.c_void_p
 _I32, _I64, _SZ = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
 
@@ -161,10 +163,10 @@ _SIGS = {
     "xpipe_grad_norm_query": [_P, _I32, ctypes.POINTER(_SZ)],
     "xpipe_grad_norm": [_P, _I32, _I32, ctypes.c_double, _P, _P, _P, _SZ, _P],
     "xpipe_clip_coef": [_P, _I64, ctypes.c_double, _P, _P],
-    "xpipe_linear_fwd_query": [ctypes.POINTER(LinearFwdArgs), ctypes.POINTER(_SZ)],
-    "xpipe_linear_bwd_query": [ctypes.POINTER(LinearBwdArgs), ctypes.POINTER(_SZ)],
-    "xpipe_linear_fwd": [ctypes.POINTER(LinearFwdArgs), _P, _SZ, _P],
-    "xpipe_linear_bwd": [ctypes.POINTER(LinearBwdArgs), _P, _SZ, _P],
+    "xpipe_linear_fwd_query": [_P, ctypes.POINTER(_SZ)],  # _P: LinearFwdArgs / LinearBwdArgs
+    "xpipe_linear_bwd_query": [_P, ctypes.POINTER(_SZ)],
+    "xpipe_linear_fwd": [_P, _P, _SZ, _P],
+    "xpipe_linear_bwd": [_P, _P, _SZ, _P],
     "xpipe_act_bwd": [_P, _P, _P, _I64, _I32, _I32, _P],
     "xpipe_embedding_fwd": [_P, _P, _I64, _I32, _I32, ctypes.c_double, _I32, _P, _P],
     "xpipe_embedding_bwd_query": [_I64, _I32, _I32, ctypes.POINTER(_SZ)],
@@ -185,7 +187,7 @@ _SIGS = {
 
 def lib() -> ctypes.CDLL:
     """The loaded libxpipe.so; raises if it has not been built."""
-    global _lib
+    global _lib, _torch
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise ImportError(f"{LIB_PATH} is missing: build it with "
@@ -195,7 +197,7 @@ def lib() -> ctypes.CDLL:
         # ships its own copy of the runtime; loaded after the library, it would
         # come in as a second runtime with its own device contexts.  Importing
         # torch first makes the library bind to torch's copy.
-        import torch  # noqa: F401
+        import torch
         L = ctypes.CDLL(LIB_PATH)
         for name, args in _SIGS.items():
             f = getattr(L, name)
@@ -203,6 +205,7 @@ def lib() -> ctypes.CDLL:
             f.restype = ctypes.c_int
         L.xpipe_last_error.argtypes = []
         L.xpipe_last_error.restype = ctypes.c_char_p
+        _torch = torch
         _lib = L
     return _lib
 
@@ -263,6 +266,8 @@ def _ptr(t) -> Optional[int]:
 
 def _stream_ptr(stream) -> Optional[int]:
     import torch
+    if stream is None and torch.cuda.is_initialized():
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     s = stream if stream is not None else torch.cuda.current_stream()
     return s.cuda_stream
 
@@ -536,30 +541,29 @@ def xpipe_adam_flat(W, m, v, G, hp: Hyper, t: int, zero_grad=True, pred_fwd=None
 
 
 # ---------------------------------------------------------------- operators around a stage
-# (checks come as `if`s, so that a message is only made where one fails: a small
-# call's time is the host's)
+# A small call's time is the host's: checks are `if`s, so that a message is only made
+# where one fails, and a tensor is asked for each property once.
 def _check_norm_coef(t, dev: int):
-    import torch
-    if t.dtype is not torch.float32 or t.numel() != 2 or not t.is_contiguous() or t.get_device() != dev:
+    lib()
+    if t.dtype is not _torch.float32 or t.numel() != 2 or not t.is_contiguous() or t.get_device() != dev:
         raise ValueError("{norm, coefficient}: two contiguous float32 elements on the gradients' device expected")
 
 
 def _dtype_of(t) -> int:
-    import torch
-    if t.dtype is torch.bfloat16:
+    if t.dtype is _torch.bfloat16:
         return BF16
-    if t.dtype is torch.float32:
+    if t.dtype is _torch.float32:
         return F32
     raise ValueError(f"bfloat16 or float32 expected, not {t.dtype}")
 
 
-def _matrix(name, t, like, rows, cols):
-    """(pointer, row pitch in elements) of a [rows, cols] tensor of `like`'s type and device, its rows contiguous."""
+def _matrix(name, t, dtype, dev, rows, cols):
+    """(pointer, row pitch in elements) of a [rows, cols] tensor of that type and device, its rows contiguous."""
     if t is None:
-        return None, 0
-    if t.dtype is not like.dtype or t.get_device() != like.get_device():
+        return 0, 0
+    if t.dtype is not dtype or t.get_device() != dev:
         raise ValueError(f"{name}: another type or device")
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+    if t.shape != (rows, cols):
         raise ValueError(f"{name}: shape {tuple(t.shape)}, ({rows}, {cols}) expected")
     ld, inner = t.stride()
     if rows <= 1:
@@ -569,37 +573,33 @@ def _matrix(name, t, like, rows, cols):
     return t.data_ptr(), ld
 
 
-def _vector(name, t, like, n):
-    import torch
+def _vector(name, t, dev, n):
     if t is None:
-        return None
-    if t.dtype is not torch.float32 or t.get_device() != like.get_device() or t.numel() != n or not t.is_contiguous():
+        return 0
+    if t.dtype is not _torch.float32 or t.get_device() != dev or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{name}: {n} contiguous float32 elements on the same device expected")
     return t.data_ptr()
 
 
-def _elsewhere(t) -> bool:
-    """True where the tensor's GPU is not the current one; raises for a CPU tensor."""
-    import torch
+def _device_of(t):
+    """(index of the tensor's GPU, whether it is the current one); raises for a CPU tensor."""
     dev = t.get_device()
     if dev < 0:
         raise ValueError("tensors on the GPU expected")
-    return dev != torch.cuda.current_device()
+    return dev, dev == _torch._C._cuda_getDevice()
 
 
-def _raw_stream(t, stream):
-    """The HIP stream of a call on t's device (the current one): `stream`, or the device's current stream."""
-    import torch
+def _raw_stream(dev, stream):
+    """The HIP stream of a call on GPU dev (the current one): `stream`, or the device's current stream."""
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(t.get_device())
-    if stream.device.index != t.get_device():
+        return _torch._C._cuda_getCurrentRawStream(dev)
+    if stream.device.index != dev:
         raise ValueError("the stream is another device's")
     return stream.cuda_stream
 
 
 def _workspace(need, given, t, stream):
     """(pointer, bytes, tensor to hold during the call) of a 256-byte aligned workspace."""
-    import torch
     if need == 0:
         return None, 0, None
     if given is not None:
@@ -608,31 +608,40 @@ def _workspace(need, given, t, stream):
         skip = -given.data_ptr() % 256
         return given.data_ptr() + skip, max(0, given.numel() * given.element_size() - skip), given
     if stream is None:
-        ws = torch.empty(need + 256, dtype=torch.uint8, device=t.device)
+        ws = _torch.empty(need + 256, dtype=_torch.uint8, device=t.device)
     else:  # the allocator then gives it out again in that stream's order
-        with torch.cuda.stream(stream):
-            ws = torch.empty(need + 256, dtype=torch.uint8, device=t.device)
-    return ws.data_ptr() + -ws.data_ptr() % 256, need, ws
+        with _torch.cuda.stream(stream):
+            ws = _torch.empty(need + 256, dtype=_torch.uint8, device=t.device)
+    ptr = ws.data_ptr()
+    return ptr + -ptr % 256, need, ws
+
+
+# LinearFwdArgs and LinearBwdArgs as struct formats: packing is a quarter of a
+# ctypes structure's time
+_FWD_FORMAT, _BWD_FORMAT = struct.Struct("qiiiiPqPqPPqPqPq"), struct.Struct("qiiiiPqPqPqPqPqPqPP")
+assert _FWD_FORMAT.size == ctypes.sizeof(LinearFwdArgs) and _BWD_FORMAT.size == ctypes.sizeof(LinearBwdArgs)
 
 
 def xpipe_linear_fwd(x, W, bias, y, act: int = ACT_NONE, residual=None, preact=None, workspace=None, stream=None):
     """y = act(x W^T + bias) + residual; preact (optional) receives the
     pre-activation.  Matrices of one type (bfloat16 or float32), their rows
     contiguous; bias float32 or None.  residual may be y itself."""
-    import torch
-    if _elsewhere(x):
-        with torch.cuda.device(x.device):
+    L = lib()
+    dev, here = _device_of(x)
+    if not here:
+        with _torch.cuda.device(dev):
             return xpipe_linear_fwd(x, W, bias, y, act, residual, preact, workspace, stream)
     if x.dim() != 2 or W.dim() != 2:
         raise ValueError("x [rows, cin] and W [cout, cin] expected")
-    (rows, cin), cout = x.shape, W.shape[0]
-    a = LinearFwdArgs(rows, cin, cout, _dtype_of(x), act, *_matrix("x", x, x, rows, cin), *_matrix("W", W, x, cout, cin),
-                      _vector("bias", bias, x, cout), *_matrix("residual", residual, x, rows, cout),
-                      *_matrix("preact", preact, x, rows, cout), *_matrix("y", y, x, rows, cout))
-    L, need, ref = lib(), _SZ(), ctypes.byref(a)
-    _check(L.xpipe_linear_fwd_query(ref, ctypes.byref(need)))
+    (rows, cin), cout, dt = x.shape, W.shape[0], x.dtype
+    a = _FWD_FORMAT.pack(rows, cin, cout, _dtype_of(x), act, *_matrix("x", x, dt, dev, rows, cin),
+                         *_matrix("W", W, dt, dev, cout, cin), _vector("bias", bias, dev, cout),
+                         *_matrix("residual", residual, dt, dev, rows, cout), *_matrix("preact", preact, dt, dev, rows, cout),
+                         *_matrix("y", y, dt, dev, rows, cout))
+    need = _SZ()
+    _check(L.xpipe_linear_fwd_query(a, ctypes.byref(need)))
     ptr, size, keep = _workspace(need.value, workspace, x, stream)
-    _check(L.xpipe_linear_fwd(ref, ptr, size, _raw_stream(x, stream)))
+    _check(L.xpipe_linear_fwd(a, ptr, size, _raw_stream(dev, stream)))
 
 
 def xpipe_linear_bwd(dz, x, W, dx=None, grad_W=None, grad_b=None, act: int = ACT_NONE, preact=None, residual=None,
@@ -642,79 +651,84 @@ def xpipe_linear_bwd(dz, x, W, dx=None, grad_W=None, grad_b=None, act: int = ACT
     (float32), each optional.  act and preact are those of the layer whose output
     x is, so dx is that layer's dz; residual is a gradient that reaches x another
     way and may be dx itself."""
-    import torch
-    if _elsewhere(dz):
-        with torch.cuda.device(dz.device):
+    L = lib()
+    dev, here = _device_of(dz)
+    if not here:
+        with _torch.cuda.device(dev):
             return xpipe_linear_bwd(dz, x, W, dx, grad_W, grad_b, act, preact, residual, workspace, stream)
     given = x if x is not None else W
     if dz.dim() != 2 or given is None or given.dim() != 2:
         raise ValueError("dz [rows, cout], and x [rows, cin] or W [cout, cin] expected")
-    (rows, cout), cin = dz.shape, given.shape[1]
-    a = LinearBwdArgs(rows, cin, cout, _dtype_of(dz), act, *_matrix("dz", dz, dz, rows, cout),
-                      *_matrix("x", x, dz, rows, cin), *_matrix("W", W, dz, cout, cin),
-                      *_matrix("preact", preact, dz, rows, cin), *_matrix("residual", residual, dz, rows, cin),
-                      *_matrix("dx", dx, dz, rows, cin), _vector("grad_W", grad_W, dz, cout * cin),
-                      _vector("grad_b", grad_b, dz, cout))
-    L, need, ref = lib(), _SZ(), ctypes.byref(a)
-    _check(L.xpipe_linear_bwd_query(ref, ctypes.byref(need)))
+    (rows, cout), cin, dt = dz.shape, given.shape[1], dz.dtype
+    a = _BWD_FORMAT.pack(rows, cin, cout, _dtype_of(dz), act, *_matrix("dz", dz, dt, dev, rows, cout),
+                         *_matrix("x", x, dt, dev, rows, cin), *_matrix("W", W, dt, dev, cout, cin),
+                         *_matrix("preact", preact, dt, dev, rows, cin), *_matrix("residual", residual, dt, dev, rows, cin),
+                         *_matrix("dx", dx, dt, dev, rows, cin), _vector("grad_W", grad_W, dev, cout * cin),
+                         _vector("grad_b", grad_b, dev, cout))
+    need = _SZ()
+    _check(L.xpipe_linear_bwd_query(a, ctypes.byref(need)))
     ptr, size, keep = _workspace(need.value, workspace, dz, stream)
-    _check(L.xpipe_linear_bwd(ref, ptr, size, _raw_stream(dz, stream)))
+    _check(L.xpipe_linear_bwd(a, ptr, size, _raw_stream(dev, stream)))
 
 
 def xpipe_act_bwd(dy, z, dz, act: int, stream=None):
     """dz = dy act'(z): contiguous tensors of one type and shape (dz may be dy or z)."""
-    import torch
+    L = lib()
+    dev, here = _device_of(dy)
     for t in (dy, z, dz):
-        if t.shape != dy.shape or t.dtype is not dy.dtype or t.get_device() != dy.get_device() or not t.is_contiguous():
+        if t.shape != dy.shape or t.dtype is not dy.dtype or t.get_device() != dev or not t.is_contiguous():
             raise ValueError("contiguous tensors of one type, shape and device expected")
-    if _elsewhere(dy):
-        with torch.cuda.device(dy.device):
+    if not here:
+        with _torch.cuda.device(dev):
             return xpipe_act_bwd(dy, z, dz, act, stream)
-    _check(lib().xpipe_act_bwd(dy.data_ptr(), z.data_ptr(), dz.data_ptr(), dy.numel(), act, _dtype_of(dy),
-                               _raw_stream(dy, stream)))
+    _check(L.xpipe_act_bwd(dy.data_ptr(), z.data_ptr(), dz.data_ptr(), dy.numel(), act, _dtype_of(dy),
+                           _raw_stream(dev, stream)))
 
 
-def _check_embedding(rows, name, tokens, table):
-    import torch
+def _check_embedding(rows, name, tokens, table, dev):
+    """(vocab, dim, number of tokens)"""
     if table.dim() != 2 or not table.is_contiguous():
         raise ValueError("table and grad: contiguous [vocab, dim] expected")
-    if tokens.dtype is not torch.int32 or not tokens.is_contiguous() or tokens.get_device() != table.get_device():
+    (vocab, dim), n = table.shape, tokens.numel()
+    if tokens.dtype is not _torch.int32 or not tokens.is_contiguous() or tokens.get_device() != dev:
         raise ValueError("tokens: contiguous int32 on the same device expected")
-    if (rows.dim() < 1 or not rows.is_contiguous() or rows.get_device() != table.get_device() or
-            rows.shape[-1] != table.shape[1] or rows.numel() != tokens.numel() * table.shape[1]):
+    if (rows.dim() < 1 or not rows.is_contiguous() or rows.get_device() != dev or rows.shape[-1] != dim or
+            rows.numel() != n * dim):
         raise ValueError(f"{name}: contiguous [tokens, dim] on the same device expected")
+    return vocab, dim, n
 
 
 def xpipe_embedding_fwd(table, tokens, y, scale: float = 1.0, stream=None):
     """y[i] = scale * table[tokens[i]] (zeros where a token is outside the table).
     table [vocab, dim] and y [..., dim] of one type; tokens int32."""
-    import torch
-    if _elsewhere(table):
-        with torch.cuda.device(table.device):
+    L = lib()
+    dev, here = _device_of(table)
+    if not here:
+        with _torch.cuda.device(dev):
             return xpipe_embedding_fwd(table, tokens, y, scale, stream)
-    _check_embedding(y, "y", tokens, table)
+    vocab, dim, n = _check_embedding(y, "y", tokens, table, dev)
     if y.dtype is not table.dtype:
         raise ValueError("y: the table's type expected")
-    vocab, dim = table.shape
-    _check(lib().xpipe_embedding_fwd(table.data_ptr(), tokens.data_ptr(), tokens.numel(), vocab, dim, scale,
-                                     _dtype_of(table), y.data_ptr(), _raw_stream(table, stream)))
+    _check(L.xpipe_embedding_fwd(table.data_ptr(), tokens.data_ptr(), n, vocab, dim, scale, _dtype_of(table), y.data_ptr(),
+                                 _raw_stream(dev, stream)))
 
 
 def xpipe_embedding_bwd(dy, tokens, grad, scale: float = 1.0, workspace=None, stream=None):
     """grad[tokens[i]] += scale * dy[i], for the tokens inside the table.
     grad: contiguous float32 [vocab, dim]; dy [..., dim]; tokens int32."""
-    import torch
-    if _elsewhere(grad):
-        with torch.cuda.device(grad.device):
+    L = lib()
+    dev, here = _device_of(grad)
+    if not here:
+        with _torch.cuda.device(dev):
             return xpipe_embedding_bwd(dy, tokens, grad, scale, workspace, stream)
-    _check_embedding(dy, "dy", tokens, grad)
-    if grad.dtype is not torch.float32:
+    vocab, dim, n = _check_embedding(dy, "dy", tokens, grad, dev)
+    if grad.dtype is not _torch.float32:
         raise ValueError("grad: float32 expected")
-    L, need, n, (vocab, dim) = lib(), _SZ(), tokens.numel(), grad.shape
+    need = _SZ()
     _check(L.xpipe_embedding_bwd_query(n, vocab, dim, ctypes.byref(need)))
     ptr, size, keep = _workspace(need.value, workspace, grad, stream)
     _check(L.xpipe_embedding_bwd(dy.data_ptr(), tokens.data_ptr(), n, vocab, dim, scale, _dtype_of(dy), grad.data_ptr(),
-                                 ptr, size, _raw_stream(grad, stream)))
+                                 ptr, size, _raw_stream(dev, stream)))
 
 
 class TensorList:
@@ -723,6 +737,7 @@ class TensorList:
     repeated xpipe_grad_norm calls."""
 
     def __init__(self, tensors):
+        L = lib()
         self.tensors = list(tensors)
         if not self.tensors:
             raise ValueError("at least one tensor expected")
@@ -733,7 +748,7 @@ class TensorList:
                 raise ValueError("contiguous tensors of one type on one device expected")
         self.descs = (TensorDesc * len(self.tensors))(*[(t.data_ptr(), t.numel()) for t in self.tensors])
         need = _SZ()
-        _check(lib().xpipe_grad_norm_query(self.descs, len(self.tensors), ctypes.byref(need)))
+        _check(L.xpipe_grad_norm_query(self.descs, len(self.tensors), ctypes.byref(need)))
         self.workspace_bytes = need.value
 
 
@@ -741,30 +756,30 @@ def xpipe_grad_norm(tensors, max_norm: float, norm_coef=None, sumsq=None, worksp
     """Global L2 norm over `tensors` (a TensorList, or an iterable of tensors):
     norm_coef (float32, two elements) receives {norm, min(1, max_norm / (norm +
     1e-6))}, sumsq (float64, one element) the sum of squares; either may be None."""
-    import torch
+    L = lib()
     ts = tensors if isinstance(tensors, TensorList) else TensorList(tensors)
     t = ts.tensors[0]
-    if _elsewhere(t):
-        with torch.cuda.device(t.device):
+    dev, here = _device_of(t)
+    if not here:
+        with _torch.cuda.device(dev):
             return xpipe_grad_norm(ts, max_norm, norm_coef, sumsq, workspace, stream)
     if norm_coef is not None:
-        _check_norm_coef(norm_coef, t.get_device())
-    if sumsq is not None and (sumsq.dtype is not torch.float64 or sumsq.numel() != 1 or
-                              sumsq.get_device() != t.get_device()):
+        _check_norm_coef(norm_coef, dev)
+    if sumsq is not None and (sumsq.dtype is not _torch.float64 or sumsq.numel() != 1 or sumsq.get_device() != dev):
         raise ValueError("sumsq: one float64 element on the gradients' device expected")
     ptr, size, keep = _workspace(ts.workspace_bytes, workspace, t, stream)
-    _check(lib().xpipe_grad_norm(ts.descs, len(ts.tensors), ts.dtype, max_norm, _ptr(sumsq), _ptr(norm_coef), ptr, size,
-                                 _raw_stream(t, stream)))
+    _check(L.xpipe_grad_norm(ts.descs, len(ts.tensors), ts.dtype, max_norm, _ptr(sumsq), _ptr(norm_coef), ptr, size,
+                             _raw_stream(dev, stream)))
 
 
 def xpipe_clip_coef(sumsq, max_norm: float, norm_coef, stream=None):
     """{norm, coefficient} from float64 sums of squares (one per stage), added in order."""
-    import torch
-    if _elsewhere(sumsq):
-        with torch.cuda.device(sumsq.device):
+    L = lib()
+    dev, here = _device_of(sumsq)
+    if not here:
+        with _torch.cuda.device(dev):
             return xpipe_clip_coef(sumsq, max_norm, norm_coef, stream)
-    if sumsq.dtype is not torch.float64 or not sumsq.is_contiguous():
+    if sumsq.dtype is not _torch.float64 or not sumsq.is_contiguous():
         raise ValueError("sumsq: contiguous float64 expected")
-    _check_norm_coef(norm_coef, sumsq.get_device())
-    _check(lib().xpipe_clip_coef(sumsq.data_ptr(), sumsq.numel(), max_norm, norm_coef.data_ptr(),
-                                 _raw_stream(sumsq, stream)))
+    _check_norm_coef(norm_coef, dev)
+    _check(L.xpipe_clip_coef(sumsq.data_ptr(), sumsq.numel(), max_norm, norm_coef.data_ptr(), _raw_stream(dev, stream)))

@@ -159,31 +159,65 @@ xpipe_status check_embedding(const void* rows, const char* name, const int32_t* 
   return XPIPE_OK;
 }
 
+// partial sums that a norm over the tensors leaves in its workspace (0: small, none)
 xpipe_status check_tensors(const xpipe_tensor* t, int32_t n, int64_t* blocks) {
   if (n < 0 || (n > 0 && !t)) return fail(XPIPE_EINVAL, "bad tensor list");
-  int64_t b = 0;
+  int64_t b = 0, units = 0;
   for (int32_t i = 0; i < n; ++i) {
     if (t[i].n < 0) return fail(XPIPE_EINVAL, "negative length");
     if (t[i].n > 0 && !t[i].p) return fail(XPIPE_EINVAL, "null tensor");
     if (t[i].n >= (int64_t)1 << 40) return fail(XPIPE_EUNSUPPORTED, "a tensor of 2^40 elements or more");
     b += norm_blocks(t[i].n);
+    units += (t[i].n + NORM_SMALL_PER - 1) / NORM_SMALL_PER;
   }
-  *blocks = b;
+  *blocks = units <= NORM_SMALL_UNITS ? 0 : b;
   return XPIPE_OK;
 }
 
 }  // namespace
 
-hipError_t xp::grad_norm_flat(const float* g, int64_t n, double max_norm, double* part, float* norm_coef, hipStream_t s) {
+hipError_t xp::grad_norm(const xpipe_tensor* tensors, int32_t n, int32_t dtype, double max_norm, double* sumsq,
+                         float* norm_coef, double* part, int64_t blocks, hipStream_t s) {
   NormArgs a{};
-  a.count = 1;
-  a.p[0] = g;
-  a.n[0] = n;
+  if (blocks == 0) {  // (at most NORM_SMALL_UNITS tensors hold something)
+    int units = 0;
+    for (int32_t i = 0; i < n; ++i) {
+      if (tensors[i].n == 0) continue;
+      a.p[a.count] = tensors[i].p;
+      a.n[a.count] = tensors[i].n;
+      a.first[a.count++] = units;
+      units += (int)((tensors[i].n + NORM_SMALL_PER - 1) / NORM_SMALL_PER);
+    }
+    return launch_grad_norm_small(dtype, a, units, max_norm, sumsq, norm_coef, s);
+  }
   a.part = part;
-  const int64_t blocks = norm_blocks(n);
-  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-  hipError_t e = launch_grad_sumsq(DT_F32, a, (int)blocks, s);
-  return e != hipSuccess ? e : launch_clip_coef(part, blocks, max_norm, nullptr, norm_coef, s);
+  int64_t first = 0;
+  auto flush = [&]() -> hipError_t {
+    hipError_t e = launch_grad_sumsq(dtype, a, (int)first, s);
+    a.part += first;
+    a.count = 0;
+    first = 0;
+    return e;
+  };
+  // tensors in batches of NORM_BATCH, long ones in pieces of 2^30 elements (whole
+  // workgroups: norm_blocks counts the same partial sums)
+  constexpr int64_t PIECE = (int64_t)1 << 30, MOST = (int64_t)1 << 30;
+  for (int32_t i = 0; i < n; ++i) {
+    const char* p = (const char*)tensors[i].p;
+    for (int64_t left = tensors[i].n; left > 0; left -= PIECE, p += PIECE * esize(dtype)) {
+      const int64_t take = std::min(left, PIECE);
+      if (a.count == NORM_BATCH || first + norm_blocks(take) > MOST) {
+        hipError_t e = flush();
+        if (e != hipSuccess) return e;
+      }
+      a.p[a.count] = p;
+      a.n[a.count] = take;
+      a.first[a.count++] = (int)first;
+      first += norm_blocks(take);
+    }
+  }
+  hipError_t e = flush();
+  return e != hipSuccess ? e : launch_clip_coef(part, blocks, max_norm, sumsq, norm_coef, s);
 }
 
 extern "C" {
@@ -212,33 +246,7 @@ xpipe_status xpipe_grad_norm(const xpipe_tensor* tensors, int32_t n_tensors, int
     if (workspace_bytes < (size_t)blocks * sizeof(double)) return fail(XPIPE_EINVAL, "workspace too small");
     if (!at_multiple(workspace, 8)) return fail(XPIPE_EINVAL, "workspace must be 8-byte aligned");
   }
-  hipStream_t s = (hipStream_t)hip_stream;
-  NormArgs a{};
-  a.part = (double*)workspace;
-  int64_t first = 0;
-  auto flush = [&]() -> hipError_t {
-    hipError_t e = launch_grad_sumsq(dtype, a, (int)first, s);
-    a.part += first;
-    a.count = 0;
-    first = 0;
-    return e;
-  };
-  // tensors in batches of NORM_BATCH, long ones in pieces of 2^30 elements (whole
-  // workgroups: norm_blocks counts the same partial sums)
-  constexpr int64_t PIECE = (int64_t)1 << 30, MOST = (int64_t)1 << 30;
-  for (int32_t i = 0; i < n_tensors; ++i) {
-    const char* p = (const char*)tensors[i].p;
-    for (int64_t left = tensors[i].n; left > 0; left -= PIECE, p += PIECE * esize(dtype)) {
-      const int64_t take = std::min(left, PIECE);
-      if (a.count == NORM_BATCH || first + norm_blocks(take) > MOST) XP_HIP(flush());
-      a.p[a.count] = p;
-      a.n[a.count] = take;
-      a.first[a.count++] = (int)first;
-      first += norm_blocks(take);
-    }
-  }
-  if (a.count > 0) XP_HIP(flush());
-  XP_HIP(launch_clip_coef((const double*)workspace, blocks, max_norm, sumsq, norm_coef, s));
+  XP_HIP(grad_norm(tensors, n_tensors, dtype, max_norm, sumsq, norm_coef, (double*)workspace, blocks, (hipStream_t)hip_stream));
   return XPIPE_OK;
 }
 

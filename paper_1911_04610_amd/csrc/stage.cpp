@@ -198,6 +198,7 @@ struct xpipe_stage {
   float* clip = nullptr;
   double clip_max = 0.0;
   double* clip_part = nullptr;
+  int64_t clip_blocks = 0;
   // timing: hipEvents around every launch, aggregated per kernel
   struct Hook : xp::LaunchHook {
     xpipe_stage* st = nullptr;
@@ -2358,11 +2359,15 @@ xpipe_status xpipe_stage_set_clip(xpipe_stage_t st, double max_norm, float* norm
   }
   if (!(max_norm >= 0)) return fail(XPIPE_EINVAL, "max_norm must be >= 0");
   if ((reinterpret_cast<uintptr_t>(norm_coef) & 3) != 0) return fail(XPIPE_EINVAL, "norm_coef must be 4-byte aligned");
+  const xpipe_tensor own = {st->grad, st->P};
+  size_t need = 0;
   if (max_norm > 0) {
-    if (!workspace) return fail(XPIPE_EINVAL, "null workspace");
+    XP_OK(xpipe_grad_norm_query(&own, 1, &need));
+    if (need > 0 && !workspace) return fail(XPIPE_EINVAL, "null workspace");
     if ((reinterpret_cast<uintptr_t>(workspace) & 7) != 0) return fail(XPIPE_EINVAL, "workspace must be 8-byte aligned");
-    if (workspace_bytes < (size_t)norm_blocks(st->P) * sizeof(double)) return fail(XPIPE_EINVAL, "workspace too small");
+    if (workspace_bytes < need) return fail(XPIPE_EINVAL, "workspace too small");
   }
+  st->clip_blocks = (int64_t)(need / sizeof(double));
   st->clip = norm_coef;
   st->clip_max = max_norm;
   st->clip_part = (double*)workspace;
@@ -2374,7 +2379,10 @@ xpipe_status xpipe_stage_set_clip(xpipe_stage_t st, double max_norm, float* norm
 static xpipe_status stage_clip(xpipe_stage* st, const float** coef) {
   *coef = nullptr;
   if (!st->clip) return XPIPE_OK;
-  if (st->clip_max > 0) XP_HIP(grad_norm_flat(st->grad, st->P, st->clip_max, st->clip_part, st->clip, st->stream));
+  if (st->clip_max > 0) {
+    const xpipe_tensor own = {st->grad, st->P};
+    XP_HIP(grad_norm(&own, 1, XPIPE_F32, st->clip_max, nullptr, st->clip, st->clip_part, st->clip_blocks, st->stream));
+  }
   *coef = st->clip + 1;
   return XPIPE_OK;
 }

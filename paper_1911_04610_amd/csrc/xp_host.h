@@ -22,7 +22,9 @@ xpipe_status fail(xpipe_status s, const std::string& msg);
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-// the two launches of xpipe_grad_norm over one fp32 tensor (part: norm_blocks(n) doubles)
-hipError_t grad_norm_flat(const float* g, int64_t n, double max_norm, double* part, float* norm_coef, hipStream_t s);
+// xpipe_grad_norm's launches, for checked arguments; part: its workspace, of `blocks`
+// doubles (0: one launch and no workspace)
+hipError_t grad_norm(const xpipe_tensor* tensors, int32_t n, int32_t dtype, double max_norm, double* sumsq, float* norm_coef,
+                     double* part, int64_t blocks, hipStream_t s);
 
 }  // namespace xp

@@ -379,6 +379,10 @@ struct NormArgs {
   double* part;
 };
 int64_t norm_blocks(int64_t n);
+// the whole norm in one workgroup (first counts units of NORM_SMALL_PER elements)
+constexpr int NORM_SMALL_PER = 1024, NORM_SMALL_UNITS = 32;
+hipError_t launch_grad_norm_small(int dtype, const NormArgs& a, int units, double max_norm, double* sumsq, float* out,
+                                  hipStream_t s);
 hipError_t launch_grad_sumsq(int dtype, const NormArgs& a, int blocks, hipStream_t s);
 hipError_t launch_clip_coef(const double* part, int64_t n, double max_norm, double* sumsq, float* out, hipStream_t s);
 
