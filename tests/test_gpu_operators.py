@@ -300,6 +300,99 @@ def test_linear_repeats_bit_for_bit_and_takes_a_given_workspace_and_stream():
     assert torch.equal(y[0], y[1]) and torch.equal(y[0], y[2])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cin,cout", [(33, 2100, 40), (40, 4099, 261), (64, 8192, 8), (4097, 513, 4001)])
+def test_linear_forward_splits_and_large_tiles(rows, cin, cout, dtype):
+    """Long reductions for few results (split and joined), and results that fill the
+    GPU with its largest tiles, with every part of the epilogue and rows of any pitch."""
+    torch = _torch()
+    dt, g = _dt(dtype), _gen(rows + cout)
+    for pitch in (0, 3, 8):
+        x, W = _rows(g, rows, cin, dt, pitch), _rows(g, cout, cin, dt, pitch, cin ** -0.5)
+        b, r = torch.randn(cout, generator=g).cuda(), _rows(g, rows, cout, dt, pitch)
+        y, z = _rows(g, rows, cout, dt, pitch), _rows(g, rows, cout, dt, pitch)
+        xp.xpipe_linear_fwd(x, W, b, y, act=xp.ACT_SILU, residual=r, preact=z)
+        pick = torch.randperm(rows, generator=g)[:150].cuda()
+        _check_fwd(x[pick], W, b, r[pick], y[pick], z[pick], "silu", dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cin,cout", [(5000, 33, 17), (9001, 64, 130), (600, 4099, 2050), (2100, 2000, 1500)])
+def test_linear_backward_splits_and_large_tiles(rows, cin, cout, dtype):
+    torch = _torch()
+    dt, g = _dt(dtype), _gen(rows + cin)
+    dz, x = _rows(g, rows, cout, dt), _rows(g, rows, cin, dt)
+    W, z = _rows(g, cout, cin, dt, scale=cout ** -0.5), _rows(g, rows, cin, dt, 8)
+    res = _rows(g, rows, cin, dt)
+    dx = res.clone()  # the residual in place
+    gW, gb = torch.randn(cout * cin, generator=g).cuda(), torch.randn(cout, generator=g).cuda()
+    gW0, gb0 = gW.clone(), gb.clone()
+    xp.xpipe_linear_bwd(dz, x, W, dx, gW, gb, act=xp.ACT_GELU, preact=z, residual=dx)
+    _check_bwd(dz, x, W, dx, gW, gb, gW0, gb0, "gelu", z, res, dtype)
+    again, gW2, gb2 = res.clone(), gW0.clone(), gb0.clone()
+    xp.xpipe_linear_bwd(dz, x, W, again, gW2, gb2, act=xp.ACT_GELU, preact=z, residual=again)
+    assert torch.equal(dx, again) and torch.equal(gW, gW2) and torch.equal(gb, gb2)
+
+
+def test_linear_offsets_past_32_bits():
+    """Rows of x, dz, y and dx 8192 elements apart in buffers of over 4 GiB: the last rows' results, and the gradient sums."""
+    torch = _torch()
+    rows, ld, cin, cout = 300001, 8192, 24, 16
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    xb, yb = torch.empty(rows, ld, dtype=torch.bfloat16, device="cuda"), torch.empty(rows, ld, dtype=torch.bfloat16, device="cuda")
+    assert xb.numel() * 2 > 1 << 32
+    x, y, dx, dz = xb[:, :cin], yb[:, :cout], yb[:, 64:64 + cin], xb[:, 64:64 + cout]
+    x.copy_(torch.randn(rows, cin, generator=g, device="cuda"))
+    dz.copy_(torch.randn(rows, cout, generator=g, device="cuda"))
+    W = torch.randn(cout, cin, generator=g, device="cuda").to(torch.bfloat16)
+    gW, gb = torch.zeros(cout, cin, device="cuda"), torch.zeros(cout, device="cuda")
+    xp.xpipe_linear_fwd(x, W, None, y)
+    xp.xpipe_linear_bwd(dz, x, W, dx, gW, gb)
+    for at in (0, 131071, 262144, rows - 40):
+        _check_fwd(x[at:at + 40], W, None, None, y[at:at + 40], None, "none", "bf16")
+        want, mag = _d(dz[at:at + 40]) @ _d(W), _d(dz[at:at + 40]).abs() @ _d(W).abs()
+        tol = (cout + 1) * E23 * mag
+        _close(dx[at:at + 40], want, 2.0 ** -8 * (want.abs() + tol) + tol, "dx")
+    G, X = dz.double().cpu(), x.double().cpu()
+    _close(gW, G.t() @ X, (rows + 2) * E23 * (G.abs().t() @ X.abs()), "grad_W")
+    _close(gb, G.sum(0), 33 * E24 * G.abs().sum(0), "grad_b")
+
+
+def test_embedding_offsets_past_32_bits():
+    torch = _torch()
+    vocab, dim, n = 600001, 4096, 3000
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    table = torch.empty(vocab, dim, dtype=torch.bfloat16, device="cuda")
+    t = torch.randint(vocab - 1500, vocab, (n,), generator=g, device="cuda", dtype=torch.int32)
+    t[0] = 0
+    table[t.long()] = torch.randn(n, dim, generator=g, device="cuda").to(torch.bfloat16)
+    y = torch.empty(n, dim, dtype=torch.bfloat16, device="cuda")
+    xp.xpipe_embedding_fwd(table, t, y)
+    assert torch.equal(y, table[t.long()])
+    del table
+    grad = torch.zeros(vocab, dim, device="cuda")
+    assert grad.numel() > 1 << 31
+    xp.xpipe_embedding_bwd(y, t, grad)
+    used = torch.unique(t.long())
+    want = torch.zeros(len(used), dim, dtype=torch.float64, device="cuda").index_add_(0, torch.searchsorted(used, t.long()), y.double())
+    mag = torch.zeros_like(want).index_add_(0, torch.searchsorted(used, t.long()), y.double().abs())
+    assert bool(((grad[used].double() - want).abs() <= (want.abs() + mag) * E24 * (1 + 1e-6)).all())
+    assert not bool(grad[1:vocab - 1500].any())
+
+
+def test_grad_norm_of_more_elements_than_32_bits_count():
+    torch = _torch()
+    n = (1 << 31) + 7
+    x = torch.zeros(n, device="cuda")
+    x[:3], x[(1 << 30) - 1:(1 << 30) + 2], x[n - 2:] = 2.0, 3.0, 5.0
+    out = torch.zeros(2, device="cuda")
+    xp.xpipe_grad_norm([x], 1.0, out)
+    want = math.sqrt(3 * 4 + 3 * 9 + 2 * 25)
+    assert abs(float(out[0]) - want) <= 1.01 * E24 * want
+
+
 def test_linear_zero_rows():
     torch = _torch()
     e = lambda *s: torch.empty(*s, dtype=torch.bfloat16, device="cuda")
@@ -354,7 +447,7 @@ def test_embedding_forward(n, vocab, dim, dtype):
         assert torch.equal(y, want)
 
 
-EMBED = [(1, 1, 1), (2, 1, 3), (7, 3, 5), (64, 10, 8), (256, 1000, 256), (2047, 50, 40), (2048, 50, 40), (2049, 7, 36),
+EMBED = [(1023, 20, 8), (1024, 7, 36), (1025, 7, 36), (1, 1, 1), (2, 1, 3), (7, 3, 5), (64, 10, 8), (256, 1000, 256), (2047, 50, 40), (2048, 50, 40), (2049, 7, 36),
          (8191, 300, 16), (8192, 300, 16), (8193, 300, 16), (16383, 255, 8), (16384, 256, 8), (20000, 70000, 24), (50001, 65535, 12),
          (40000, 3, 520)]
 
@@ -579,6 +672,59 @@ def test_stage_clips_its_updates(rule):
     for a, b in zip(out["off"][:3], out["none"][:3]):
         assert torch.equal(a, b)
     assert float(out["own"][3][1]) < 1 and not torch.equal(out["own"][1], out["none"][1])
+
+
+def test_operator_refusals_on_the_gpu():
+    torch = _torch()
+    z = lambda *s, dtype=torch.bfloat16: torch.zeros(*s, dtype=dtype, device="cuda")
+    x, W, y = z(4, 16), z(8, 16), z(4, 8)
+    for bad in (lambda: xp.xpipe_linear_fwd(x, W, None, z(4, 9)), lambda: xp.xpipe_linear_fwd(x, W, None, z(4, 8, dtype=torch.float32)),
+                lambda: xp.xpipe_linear_fwd(z(16, 4).t(), W, None, y), lambda: xp.xpipe_linear_fwd(x, z(16, 8).t(), None, y),
+                lambda: xp.xpipe_linear_fwd(x, W, z(8), y), lambda: xp.xpipe_linear_fwd(x, W.cpu(), None, y),
+                lambda: xp.xpipe_linear_fwd(x.half(), W.half(), None, y.half()), lambda: xp.xpipe_linear_fwd(x[0], W, None, y),
+                lambda: xp.xpipe_linear_bwd(y, x, W, z(4, 16), z(8, 16)), lambda: xp.xpipe_linear_bwd(y, x, None, None, z(100, dtype=torch.float32)),
+                lambda: xp.xpipe_embedding_fwd(W, z(4, dtype=torch.int64), z(4, 16)), lambda: xp.xpipe_embedding_fwd(W, z(4, dtype=torch.int32), z(4, 8)),
+                lambda: xp.xpipe_embedding_bwd(x, z(4, dtype=torch.int32), z(8, 16)), lambda: xp.xpipe_grad_norm([x], 1.0, z(3, dtype=torch.float32)),
+                lambda: xp.xpipe_adam_flat(x, x, x, x, xp.Hyper(), 0, clip=z(1, dtype=torch.float32))):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: xp.xpipe_linear_fwd(x, W, None, y, act=7), lambda: xp.xpipe_linear_fwd(x, W, None, x[:, :8]),
+                lambda: xp.xpipe_linear_bwd(y, x, W, z(4, 16), act=xp.ACT_GELU), lambda: xp.xpipe_grad_norm([x], 0.0, z(2, dtype=torch.float32)),
+                lambda: xp.xpipe_linear_fwd(z(100, 99), z(8, 99), None, z(100, 8), workspace=z(64))):
+        with pytest.raises(xp.XPipeError):
+            bad()
+    st = _small_stage()
+    L, ok = xp.lib(), torch.zeros(2, device="cuda")
+    assert L.xpipe_stage_set_clip(st._h, -1.0, ok.data_ptr(), None, 0) == xp.EINVAL
+    assert L.xpipe_stage_set_clip(st._h, float("nan"), ok.data_ptr(), None, 0) == xp.EINVAL
+    assert L.xpipe_stage_set_clip(st._h, 0.0, ok.data_ptr() + 2, None, 0) == xp.EINVAL
+    st.destroy()
+    big = _small_stage(cin=2048)
+    assert big.P > 32768 and L.xpipe_stage_set_clip(big._h, 1.0, ok.data_ptr(), None, 0) == xp.EINVAL
+    big.destroy()
+
+
+def test_stage_clips_with_a_workspace():
+    """A stage of more elements than one workgroup's norm takes, against the norm over its accumulator and the caller's coefficient."""
+    torch = _torch()
+    g = _gen(14)
+    x, lab = torch.randn(16, 2048, generator=g).cuda(), torch.randint(0, 10, (16,), generator=g).to(torch.int32).cuda()
+    out = []
+    for own in (True, False):
+        st, clip, y, hp = _small_stage(cin=2048), torch.zeros(2, device="cuda"), torch.empty(16, 10, device="cuda"), xp.Hyper()
+        st.xpipe_stage_set_clip(0.05 if own else 0.0, clip)
+        st.xpipe_predict_weights(xp.FWD, 0, hp, 0)
+        st.xpipe_predict_weights(xp.BWD, 0, hp, 0)
+        st.xpipe_stage_fwd(x, y, lab)
+        st.xpipe_stage_bwd(x, labels=lab)
+        if not own:
+            xp.xpipe_grad_norm([st.grad], 0.05, clip)
+        st.xpipe_adam_step(hp, 0, 1, 1, True)
+        out.append((st.W.clone(), st.m.clone(), st.w_pred_fwd.clone(), clip.clone()))
+        st.destroy()
+    for a, b in zip(*out):
+        assert torch.equal(a, b)
+    assert float(out[0][3][1]) < 1
 
 
 def test_stage_run_clips_every_update():
