@@ -767,12 +767,12 @@ XP_DEV u32x4_t ld_any(const char* p, int n) {
 }
 
 // ---------------------------------------------------------------- few rows
-// The forward of up to 16 MT rows: bound by reading W once, so every wave streams
-// its part of the reduction of 16 rows of W from memory straight into registers
-// (16x16 products, W the columns, the rows of x the rows, empty ones zeros).
-// The eight waves of a workgroup take the reduction's 128-byte steps in turn and
-// add their results through LDS in the order of the waves: no workspace, one launch.
-// ANY: operands of any alignment.
+// The forward of a few rows, 16 MT of them per workgroup: bound by reading W once, so
+// every wave streams its part of the reduction of 16 rows of W from memory
+// straight into registers (16x16 products, W the columns, the rows of x the rows,
+// empty ones zeros).  The eight waves of a workgroup take the reduction's 128-byte
+// steps in turn and add their results through LDS in the order of the waves: no
+// workspace, one launch.  ANY: operands of any alignment.
 constexpr int FEW_WAVES = 8, FEW_STEPS = 4;  // steps in flight per wave
 template <typename T, int MT, bool ANY>
 __global__ __launch_bounds__(FEW_WAVES * 64) void k_linear_few(LinearArgs a) {
@@ -781,12 +781,14 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_linear_few(LinearArgs a) {
   __shared__ float red[FEW_WAVES][MT][256];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n0 = blockIdx.x * 16, fr = lane & 15, fg = lane >> 4;
-  const LinearArgs t = from<T>(a, 0, n0);
+  const int64_t m0 = (int64_t)blockIdx.y * (16 * MT);
+  const int rows = (int)min((int64_t)(16 * MT), a.M - m0);
+  const LinearArgs t = from<T>(a, m0, n0);
   auto result = [&](int e, int& m, int& n) __attribute__((always_inline)) -> bool {
     const int i = e * FEW_WAVES * 64 + tid;
     m = i / 16;
     n = i % 16;
-    return i < MT * 256 && m < a.M && n < t.N;
+    return i < MT * 256 && m < rows && n < t.N;
   };
   Fetched1 f[EACH];
 #pragma unroll
@@ -796,7 +798,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_linear_few(LinearArgs a) {
   }
   const char* xr[MT];  // the lane's rows (null: none)
 #pragma unroll
-  for (int i = 0; i < MT; ++i) xr[i] = i * 16 + fr < a.M ? (const char*)a.A + (i * 16 + fr) * a.lda * ES : nullptr;
+  for (int i = 0; i < MT; ++i) xr[i] = i * 16 + fr < rows ? (const char*)a.A + (m0 + i * 16 + fr) * a.lda * ES : nullptr;
   const char* wr = n0 + fr < a.N ? (const char*)a.B + (int64_t)(n0 + fr) * a.ldb * ES : nullptr;
   auto chunk = [&](const char* row, int k) __attribute__((always_inline)) -> u32x4_t {
     const int n = a.K - k;
@@ -930,7 +932,7 @@ constexpr TileCost COST_F32[] = {{64, 0.56, 1.05, 0.0, 1.3}, {128, 2.0, 3.7, 3.5
 constexpr double JOIN_US = 4.6, JOIN_US_PER_MB = 0.134;
 constexpr int MAX_SPLITS = 16;
 
-void pick(int dtype, int64_t M, int N, int64_t steps, int* tile, int* splits) {
+double pick(int dtype, int64_t M, int N, int64_t steps, int* tile, int* splits) {
   const TileCost* cost = dtype == DT_BF16 ? COST_BF16 : COST_F32;
   const int tiles = dtype == DT_BF16 ? 3 : 2;
   double best = 0.0;
@@ -950,6 +952,7 @@ void pick(int dtype, int64_t M, int N, int64_t steps, int* tile, int* splits) {
       }
     }
   }
+  return best;
 }
 
 template <typename T, int EPI>
@@ -1015,18 +1018,31 @@ hipError_t by_kind(const LinearArgs& a, int tile, hipStream_t s) {
   return by_tile<T, true, true, LIN_GRAD>(a, tile, s);
 }
 
-// The forwards that k_linear_few takes: up to 32 rows (us, MI355X, tiles in brackets:
+// The forwards that k_linear_few takes.  Up to 32 rows (us, MI355X, tiles in brackets:
 // bf16 1x4096x4096 7.1 (12.4), 16x4096x4096 9.7 (13.0), 32x4096x4096 13.3 (14.0),
 // 16x999x1333 8.1 (13.1); 64 rows 21.2 (15.5); fp32 1x4096x4096 17.1 (25.0), 16 rows
 // 20.7 (25.1)), but not a long reduction for a few columns, whose workgroups
-// leave most CUs idle (16x16384x64 29.6 (13.4)).
-bool takes_few(const LinearArgs& a, int64_t steps) {
-  return a.epi == LIN_FWD && a.M <= 32 && (a.N >= 1024 || steps <= 3 * FEW_WAVES * FEW_STEPS);
+// leave most CUs idle (16x16384x64 29.6 (13.4)).  And more rows whose operands would
+// have to be packed, where that and the tiles cost more: sets of four
+// workgroups per CU, in each of which the waves take 32 steps at a time, and what all
+// of them read from L2 (137x57x128 7.8 (12.4), 300x300x300 8.2 (14.5), 2000x100x100
+// 9.2 (12.4); 500x4097x100 30.6 (18.0), which stays with the tiles).
+constexpr double PACK_US = 6.0, FEW_US = 2.0, FEW_ROUND_US = 8.0, FEW_MB_PER_US = 8.0;
+bool takes_few(const LinearArgs& a, int es, bool any, double tiles_us) {
+  if (a.epi != LIN_FWD) return false;
+  const int64_t steps = ((int64_t)a.K * es + 127) / 128, round = FEW_WAVES * FEW_STEPS;
+  if (a.M <= 32) return a.N >= 1024 || steps <= 3 * round;
+  if (!any) return false;
+  const int64_t groups = (a.M + 31) / 32 * ((a.N + 15) / 16);
+  if ((a.M + 31) / 32 > 65535) return false;
+  const double us = (double)((groups + 1023) / 1024) * (FEW_US + FEW_ROUND_US * (double)steps / round) +
+                    (double)groups * 48.0 * a.K * es * 1e-6 / FEW_MB_PER_US;
+  return us < tiles_us + PACK_US;
 }
 template <typename T, int MT, bool ANY>
 hipError_t go_few(const LinearArgs& a, hipStream_t s) {
   XP_LAUNCH(sizeof(T) == 2 ? "k_linear_few<bf16>" : "k_linear_few<f32>", 2.0 * a.M * a.N * a.K, (k_linear_few<T, MT, ANY>),
-            dim3((unsigned)((a.N + 15) / 16)), dim3(FEW_WAVES * 64), 0, s, a);
+            dim3((unsigned)((a.N + 15) / 16), (unsigned)((a.M + 16 * MT - 1) / (16 * MT))), dim3(FEW_WAVES * 64), 0, s, a);
   return hipGetLastError();
 }
 template <typename T>
@@ -1039,8 +1055,14 @@ bool chunked(const void* p, int64_t ld, int chunk) {
   return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld % chunk == 0;
 }
 
+// a forward's operands: a reduction along their rows has to end with a chunk
+bool unaligned(const LinearArgs& a, int chunk) {
+  return !chunked(a.A, a.lda, chunk) || !chunked(a.B, a.ldb, chunk) || a.K % chunk != 0;
+}
+
 struct Plan {
   int tile, splits;
+  double us;
   int64_t kper, ldpart;
   size_t part_b, bytes;  // offset of the bias gradient's partial sums, workspace
 };
@@ -1048,7 +1070,7 @@ Plan plan(int dtype, const LinearArgs& a) {
   Plan p{};
   const int bk = dtype == DT_BF16 ? STEP<bf16_t> : STEP<float>;
   const int64_t steps = ((int64_t)a.K + bk - 1) / bk;
-  pick(dtype, a.M, a.N, steps, &p.tile, &p.splits);
+  p.us = pick(dtype, a.M, a.N, steps, &p.tile, &p.splits);
   p.kper = (steps + p.splits - 1) / p.splits * bk;
   p.splits = (int)(((int64_t)a.K + p.kper - 1) / p.kper);  // those that hold something
   if (p.splits == 1) return p;
@@ -1072,7 +1094,7 @@ struct Call {
 Call lay_out(int dtype, const LinearArgs* in, int n, char* ws) {
   Call c{};
   const int es = dtype == DT_BF16 ? 2 : 4, chunk = 16 / es;
-  c.few = in[0].M > 0 && takes_few(in[0], ((int64_t)in[0].K + 8 * chunk - 1) / (8 * chunk));
+  c.few = in[0].M > 0 && takes_few(in[0], es, unaligned(in[0], chunk), plan(dtype, in[0]).us);
   if (c.few) {
     c.p[0] = in[0];
     return c;
@@ -1122,7 +1144,7 @@ hipError_t launch_linear(int dtype, const LinearArgs* products, int n, void* wor
   const int chunk = dtype == DT_BF16 ? CHUNK<bf16_t> : CHUNK<float>;
   if (c.few) {
     const LinearArgs& a = c.p[0];
-    const bool any = !chunked(a.A, a.lda, chunk) || !chunked(a.B, a.ldb, chunk) || a.K % chunk != 0;
+    const bool any = unaligned(a, chunk);
     return dtype == DT_BF16 ? few<bf16_t>(a, any, s) : few<float>(a, any, s);
   }
   if (c.pack.count > 0) {

@@ -690,7 +690,7 @@ def test_operator_refusals_on_the_gpu():
             bad()
     for bad in (lambda: xp.xpipe_linear_fwd(x, W, None, y, act=7), lambda: xp.xpipe_linear_fwd(x, W, None, x[:, :8]),
                 lambda: xp.xpipe_linear_bwd(y, x, W, z(4, 16), act=xp.ACT_GELU), lambda: xp.xpipe_grad_norm([x], 0.0, z(2, dtype=torch.float32)),
-                lambda: xp.xpipe_linear_fwd(z(100, 99), z(8, 99), None, z(100, 8), workspace=z(64))):
+                lambda: xp.xpipe_linear_bwd(z(100, 8), z(100, 99), z(8, 99), z(100, 99), workspace=z(64))):
         with pytest.raises(xp.XPipeError):
             bad()
     st = _small_stage()

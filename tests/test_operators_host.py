@@ -71,22 +71,28 @@ def test_linear_null_arguments_and_workspaces():
     for q, f in ((L.xpipe_linear_fwd_query, L.xpipe_linear_fwd), (L.xpipe_linear_bwd_query, L.xpipe_linear_bwd)):
         assert q(None, ctypes.byref(need)) == xp.EINVAL and f(None, None, 0, None) == xp.EINVAL
     assert L.xpipe_linear_fwd_query(ctypes.byref(_fwd()), None) == xp.EINVAL
-    # a call that packs an operand: rows of 99 elements
-    a = _fwd(rows=100, cin=99, ldx=99, ldw=99)
+    # a backward always packs operands that chunks of 16 bytes do not fit: rows of 99 elements
+    a = _bwd(rows=100, cin=99, ldx=99, ldw=99, lddx=99)
     st, size = _query(a)
     assert st == xp.OK and size >= 100 * 104 * 2 + 32 * 104 * 2
     for ws, n in ((None, size), (P, size - 1), (P + 128, size)):
-        assert L.xpipe_linear_fwd(ctypes.byref(a), ws, n, None) == xp.EINVAL
+        assert L.xpipe_linear_bwd(ctypes.byref(a), ws, n, None) == xp.EINVAL
+    # and so does a forward of many results
+    a = _fwd(rows=4096, cin=99, cout=4096, ldx=99, ldw=99, ldy=4096)
+    st, size = _query(a)
+    assert st == xp.OK and size >= 2 * 4096 * 104 * 2
+    assert L.xpipe_linear_fwd(ctypes.byref(a), P, size - 1, None) == xp.EINVAL
 
 
 def test_linear_query_follows_alignment_and_splits():
     assert _query(_fwd()) == (xp.OK, 0) and _query(_bwd()) == (xp.OK, 0)
     assert _query(_fwd(rows=4096, cin=4096, cout=4096, ldx=4096, ldw=4096, ldy=4096)) == (xp.OK, 0)
-    # up to 32 rows nothing is packed; from 33 on operands that chunks of 16 bytes do not fit are
+    # up to 32 rows nothing is packed; operands of many results that chunks of 16 bytes do not fit are
     odd = dict(cin=65, ldx=65, ldw=65)
-    assert _query(_fwd(rows=32, **odd)) == (xp.OK, 0) and _query(_fwd(rows=33, **odd))[1] > 0
-    assert _query(_fwd(rows=40, x=P + 2))[1] > 0 and _query(_fwd(rows=40, ldx=68))[1] > 0
-    assert _query(_fwd(rows=40, y=3 * P + 2)) == (xp.OK, 0)  # results need no alignment
+    many = dict(rows=4096, cout=4096, ldy=4096)
+    assert _query(_fwd(rows=32, **odd)) == (xp.OK, 0) and _query(_fwd(**many, **odd))[1] > 0
+    assert _query(_fwd(x=P + 2, **many))[1] > 0 and _query(_fwd(ldx=68, **many))[1] > 0
+    assert _query(_fwd(**many)) == (xp.OK, 0) and _query(_fwd(y=3 * P + 2, **many)) == (xp.OK, 0)  # results need no alignment
     # a long reduction for few results is split, and its parts' sums need memory
     long = _bwd(rows=16384, lddz=32, ldx=64)
     st, size = _query(long)
