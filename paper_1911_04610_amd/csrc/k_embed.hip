@@ -67,29 +67,29 @@ __global__ __launch_bounds__(256) void k_embed_fwd(EmbedArgs a) {
 XP_DEV uint32_t sort_key(int t, int vocab) { return (uint32_t)t < (uint32_t)vocab ? (uint32_t)t : (uint32_t)vocab; }
 
 // Few positions: a position's place is the number of positions before it in the
-// order.  64 positions per workgroup, a lane of each wave; the sixteen waves go
-// through all keys, every sixteenth four of them each.  (8192 keys in 128
-// workgroups take as long as the radix sort's four launches.)
-constexpr int RANK_MAX = 8192;
+// order.  Sixteen positions per workgroup; the sixteen waves go through all keys in
+// LDS, and each quarter of a wave takes every fourth four of the wave's own.
+constexpr int RANK_MAX = 8192, RANK_POS = 16;
 __global__ __launch_bounds__(1024) void k_embed_rank(const int32_t* __restrict__ tokens, int n, int vocab,
                                                       uint32_t* __restrict__ keys, uint32_t* __restrict__ pos) {
   __shared__ __align__(16) uint32_t sk[RANK_MAX];
   __shared__ int sums[16][64];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int pad = (n + 3) / 4 * 4;
+  const int pad = (n + 15) / 16 * 16;
   for (int j = tid; j < pad; j += 1024) sk[j] = j < n ? sort_key(tokens[j], vocab) : ~0u;
   __syncthreads();
-  const int i0 = blockIdx.x * 64, i = i0 + lane;
+  const int i0 = blockIdx.x * RANK_POS, i = i0 + (lane & 15);
   const uint32_t key = i < n ? sk[i] : 0u;
   int rank = 0;
   // before the workgroup's own positions equal keys count, after them they do not
 #pragma unroll 4
-  for (int j = wave * 4; j < pad; j += 64) {
+  for (int j0 = wave * 16; j0 < pad; j0 += 256) {
+    const int j = j0 + (lane >> 4) * 4;
     const u32x4_t k = *reinterpret_cast<const u32x4_t*>(sk + j);
-    if (j < i0) {
+    if (j0 < i0) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) rank += k[q] <= key;
-    } else if (j >= i0 + 64) {
+    } else if (j0 > i0) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) rank += k[q] < key;
     } else {
@@ -99,12 +99,16 @@ __global__ __launch_bounds__(1024) void k_embed_rank(const int32_t* __restrict__
   }
   sums[wave][lane] = rank;
   __syncthreads();
-  if (wave == 0 && i < n) {
+  if (wave == 0) {
     int at = 0;
 #pragma unroll
     for (int w = 0; w < 16; ++w) at += sums[w][lane];
-    keys[at] = key;
-    pos[at] = (uint32_t)i;
+    at += __shfl_xor(at, 16, 64);
+    at += __shfl_xor(at, 32, 64);
+    if (lane < RANK_POS && i < n) {
+      keys[at] = key;
+      pos[at] = (uint32_t)i;
+    }
   }
 }
 
@@ -284,29 +288,33 @@ __global__ __launch_bounds__(64) void k_embed_bwd(EmbedArgs a, const uint32_t* _
 }
 
 // The runs that pass a span's end: the span that a run starts in adds its
-// partials.  Four waves take consecutive parts of the run's spans, 64 JOIN_COLS
+// partials.  JOIN_WAVES waves take consecutive parts of the run's spans, 64 JOIN_COLS
 // columns each, and their sums are added in order.
-constexpr int JOIN_COLS = 4;
-__global__ __launch_bounds__(256) void k_embed_join(EmbedArgs a, const uint32_t* __restrict__ keys, int span,
+constexpr int JOIN_COLS = 4, JOIN_WAVES = 4;
+__global__ __launch_bounds__(64 * JOIN_WAVES) void k_embed_join(EmbedArgs a, const uint32_t* __restrict__ keys, int span,
                                                      const float* __restrict__ part) {
-  __shared__ double sums[3][64][JOIN_COLS];
+  __shared__ double sums[JOIN_WAVES - 1][64][JOIN_COLS];
   const int64_t c = blockIdx.x, beg = c * span, next = beg + span;
   if (next >= a.n) return;
   const uint32_t key = keys[next - 1], kn = keys[next], kb = keys[beg], kp = keys[beg > 0 ? beg - 1 : 0];
   if (key >= (uint32_t)a.vocab || kn != key) return;  // no run passes the end
   if (beg > 0 && kb == key && kp == key) return;       // it started before this span
   const int64_t spans = (a.n + span - 1) / span;
-  // the run's last span: steps that double, then back
-  int64_t lo = c + 1, step = 1;
-  while (lo + step < spans && keys[(lo + step) * span] == key) {
-    lo += step;
-    step *= 2;
-  }
-  for (; step > 0; step /= 2)
-    if (lo + step < spans && keys[(lo + step) * span] == key) lo += step;
+  // the run's last span: the next as many as there are threads are looked at together, then, of a longer run,
+  // every stride-th of those behind
+  int64_t lo = c;
+  auto look = [&](int64_t stride) __attribute__((always_inline)) {
+    const int64_t at = lo + (threadIdx.x + 1) * stride;
+    const int more = __syncthreads_count(at < spans && keys[at * span] == key);
+    lo += more * stride;
+    return more;
+  };
+  if (look(1) == 64 * JOIN_WAVES)
+    for (int64_t stride = (int64_t)1 << 24; stride > 0; stride >>= 8)
+      if (lo + stride < spans) look(stride);
   const int64_t cnt = lo - c;  // spans behind the first one
   const int g = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t per = max((int64_t)4, (cnt + 3) / 4), s0 = c + 1 + g * per, s1 = min(lo + 1, s0 + per);
+  const int64_t per = max((int64_t)4, (cnt + JOIN_WAVES - 1) / JOIN_WAVES), s0 = c + 1 + g * per, s1 = min(lo + 1, s0 + per);
   for (int64_t col = ((int64_t)blockIdx.y * 64 + lane) * JOIN_COLS; col - lane * JOIN_COLS < a.dim;
        col += (int64_t)gridDim.y * 64 * JOIN_COLS) {
     const int cols = (int)max((int64_t)0, min((int64_t)JOIN_COLS, a.dim - col));
@@ -326,7 +334,7 @@ __global__ __launch_bounds__(256) void k_embed_join(EmbedArgs a, const uint32_t*
       }
     };
     if (g == 0) add(part + (c * 2 + 1) * a.dim + col);
-#pragma unroll 8
+#pragma unroll 16
     for (int64_t s = s0; s < s1; ++s) add(part + s * 2 * a.dim + col);
     if (g > 0) {
 #pragma unroll
@@ -338,7 +346,9 @@ __global__ __launch_bounds__(256) void k_embed_join(EmbedArgs a, const uint32_t*
 #pragma unroll
       for (int q = 0; q < JOIN_COLS; ++q) {
         if (q >= cols) continue;
-        const double v = ((t[q] + sums[0][lane][q]) + sums[1][lane][q]) + sums[2][lane][q];
+        double v = t[q];
+#pragma unroll
+        for (int w = 0; w < JOIN_WAVES - 1; ++w) v += sums[w][lane][q];
         o[q] = (float)((double)o[q] + a.scale * v);
       }
     }
@@ -430,12 +440,12 @@ __global__ __launch_bounds__(256) void k_embed_bwd_small(EmbedArgs a) {
 size_t up256(size_t b) { return (b + 255) / 256 * 256; }
 bool aligned(const void* p, int64_t dim, int chunk) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && dim % chunk == 0; }
 
-// sorted positions per wave of the gradient: as many as leave some 4096 waves (the
+// sorted positions per wave of the gradient: as many as leave some 2048 waves (the
 // fewer spans, the fewer partials), 8 to 64
 int span_of(int64_t n, int64_t dim) {
   const int64_t waves = n * ((dim + 511) / 512);
   int span = 8;
-  while (span < 64 && waves > (int64_t)4096 * span) span *= 2;
+  while (span < 64 && waves > (int64_t)2048 * span) span *= 2;
   return span;
 }
 
@@ -506,7 +516,7 @@ hipError_t launch_embed_bwd(int dtype, const EmbedArgs& a, void* workspace, hipS
   uint32_t *keys = (uint32_t*)(ws + l.keys[0]), *pos = (uint32_t*)(ws + l.pos[0]);
   hipError_t e;
   if (a.n <= RANK_MAX) {
-    XP_LAUNCH("k_embed_rank", 12.0 * a.n, k_embed_rank, dim3((unsigned)((a.n + 63) / 64)), dim3(1024), 0, s, a.tokens,
+    XP_LAUNCH("k_embed_rank", 12.0 * a.n, k_embed_rank, dim3((unsigned)((a.n + RANK_POS - 1) / RANK_POS)), dim3(1024), 0, s, a.tokens,
               (int)a.n, a.vocab, keys, pos);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -545,7 +555,7 @@ hipError_t launch_embed_bwd(int dtype, const EmbedArgs& a, void* workspace, hipS
   e = hipGetLastError();
   if (e != hipSuccess || spans < 2) return e;
   XP_LAUNCH("k_embed_join", 0.0, k_embed_join, dim3(spans - 1, (unsigned)std::min<int64_t>(16, (a.dim + 64 * JOIN_COLS - 1) / (64 * JOIN_COLS))),
-            dim3(256), 0, s, a, keys, span, part);
+            dim3(64 * JOIN_WAVES), 0, s, a, keys, span, part);
   return hipGetLastError();
 }
 
