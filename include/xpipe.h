@@ -502,11 +502,11 @@ xpipe_status xpipe_act_bwd(const void* dy, const void* z, void* dz, int64_t n, i
  * table [vocab][dim], y and dy [n_tokens][dim] in the storage dtype, grad
  * [vocab][dim] fp32, all contiguous; tokens int32 on the device.  A token
  * outside [0, vocab) is padding: its row of y is zeros, its dy is not
- * read.  y can be a stage's x, and dy its dx.  Products
- * and sums are formed in fp64 and rounded once (from 1025 tokens on, a
+ * read.  y can be a stage's x, and dy its dx.  Products and sums are formed in
+ * fp64 and rounded once to fp32 (y in bf16: from there; from 1025 tokens on, a
  * run of equal tokens in the sorted order is added in parts of up to 64, whose
- * sums are rounded to fp32).  The order of the terms
- * follows from tokens and sizes, so a repeated call gives the same bits. */
+ * sums are rounded to fp32).  The order of the terms follows from tokens and
+ * sizes, so a repeated call gives the same bits. */
 xpipe_status xpipe_embedding_fwd(const void* table, const int32_t* tokens, int64_t n_tokens, int32_t vocab, int32_t dim,
                                  double scale, int32_t dtype, void* y, void* hip_stream);
 /* workspace: device memory, 256-byte aligned, of the query's bytes, free again

@@ -289,6 +289,7 @@ class Stage:
         self.P, ws = xpipe_stage_query(layers, micro_batch, in_shape, dtype)
         self.ws_bytes = ws
         self.fwd_workspace = self.fwd_stream = None
+        self._clip = self._clip_ws = None
         f32 = dict(dtype=torch.float32, device=self.device)
         self.W = torch.zeros(self.P, **f32)
         self.m = torch.zeros(self.P, **f32)
@@ -413,12 +414,14 @@ class Stage:
         if norm_coef is not None:
             _check_norm_coef(norm_coef, self.grad.get_device())
             if max_norm > 0:
-                import torch
                 one = TensorDesc(_ptr(self.grad), self.P)
                 _check(lib().xpipe_grad_norm_query(ctypes.byref(one), 1, ctypes.byref(size)))
-                ws = torch.empty(max(size.value, 8), dtype=torch.uint8, device=self.device)
+                if self._clip_ws is None:  # kept from then on: updates in flight may use it
+                    with _torch.cuda.stream(self.stream):
+                        self._clip_ws = _torch.empty(max(size.value, 8), dtype=_torch.uint8, device=self.device)
+                ws = self._clip_ws
         _check(lib().xpipe_stage_set_clip(self._h, max_norm, _ptr(norm_coef), _ptr(ws), size.value))
-        self._clip = (norm_coef, ws)  # kept while the stage uses them
+        self._clip = norm_coef  # kept while the stage uses it
 
     def set_timing(self, enable: bool):
         _check(lib().xpipe_stage_set_timing(self._h, int(enable)))
@@ -733,12 +736,16 @@ def xpipe_embedding_bwd(dy, tokens, grad, scale: float = 1.0, workspace=None, st
 
 class TensorList:
     """Gradients that one norm is taken over: contiguous tensors of one type on
-    one device, kept (with their addresses and the call's workspace size) for
-    repeated xpipe_grad_norm calls."""
+    one device, kept with their descriptors for repeated xpipe_grad_norm calls.
+    A call looks at the tensors' addresses and sizes again: one whose storage was
+    exchanged in between is read where it is now."""
 
     def __init__(self, tensors):
-        L = lib()
         self.tensors = list(tensors)
+        self._describe()
+
+    def _describe(self):
+        L = lib()
         if not self.tensors:
             raise ValueError("at least one tensor expected")
         first = self.tensors[0]
@@ -746,10 +753,18 @@ class TensorList:
         for t in self.tensors:
             if t.dtype is not first.dtype or t.get_device() != first.get_device() or not t.is_contiguous():
                 raise ValueError("contiguous tensors of one type on one device expected")
-        self.descs = (TensorDesc * len(self.tensors))(*[(t.data_ptr(), t.numel()) for t in self.tensors])
+        self.places = self._places()
+        self.descs = (TensorDesc * len(self.tensors))(*self.places)
         need = _SZ()
         _check(L.xpipe_grad_norm_query(self.descs, len(self.tensors), ctypes.byref(need)))
         self.workspace_bytes = need.value
+
+    def _places(self):
+        return [(t.data_ptr(), t.numel()) for t in self.tensors]
+
+    def refresh(self):
+        if self._places() != self.places:
+            self._describe()
 
 
 def xpipe_grad_norm(tensors, max_norm: float, norm_coef=None, sumsq=None, workspace=None, stream=None):
@@ -757,7 +772,11 @@ def xpipe_grad_norm(tensors, max_norm: float, norm_coef=None, sumsq=None, worksp
     norm_coef (float32, two elements) receives {norm, min(1, max_norm / (norm +
     1e-6))}, sumsq (float64, one element) the sum of squares; either may be None."""
     L = lib()
-    ts = tensors if isinstance(tensors, TensorList) else TensorList(tensors)
+    if isinstance(tensors, TensorList):
+        ts = tensors
+        ts.refresh()
+    else:
+        ts = TensorList(tensors)
     t = ts.tensors[0]
     dev, here = _device_of(t)
     if not here:

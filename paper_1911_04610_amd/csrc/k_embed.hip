@@ -32,7 +32,7 @@ XP_DEV void unpack(const u32x4_t& u, float (&v)[CHUNK<T>]) {
 
 // ---------------------------------------------------------------- lookup
 // One 16-byte chunk of one position per thread (VEC), else one element.  The
-// product is formed in fp64 and rounded once.
+// product is formed in fp64 and rounded to fp32 (for bf16, from there).
 template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void k_embed_fwd(EmbedArgs a) {
   constexpr int C = VEC ? CHUNK<T> : 1;

@@ -51,12 +51,13 @@ XP_DEV void act_values(float (&z)[N], int act) {
   }
 }
 
-// v *= act'(z); 0 at 0 for the ReLU
+// v *= act'(z); 0 at 0 for the ReLU, and then 0 whatever v (an infinite gradient of a
+// dead unit is none)
 template <int N>
 XP_DEV void act_slopes(float (&v)[N], const float (&z)[N], int act) {
   if (act == LIN_RELU) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] *= z[i] > 0.f ? 1.f : 0.f;
+    for (int i = 0; i < N; ++i) v[i] = z[i] > 0.f ? v[i] : 0.f;
   } else if (act == LIN_GELU) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -942,6 +943,7 @@ double pick(int dtype, int64_t M, int N, int64_t steps, int* tile, int* splits) 
     const int64_t count = ((M + b - 1) / b) * ((N + b - 1) / b);
     for (int s = 1; s <= MAX_SPLITS && (s == 1 || 2 * s <= steps); s *= 2) {
       const int64_t per = (steps + s - 1) / s, blocks = (count * ((steps + per - 1) / per) + 255) / 256;
+      if (blocks >= 1 << 15 && i + 1 < tiles) continue;  // a launch has fewer than 2^32 threads
       double t = (double)(blocks / 2) * (cost[i].pair * per + cost[i].pair_rest) +
                  (double)(blocks % 2) * (cost[i].alone * per + cost[i].alone_rest);
       if (s > 1) t += JOIN_US + JOIN_US_PER_MB * 4e-6 * (double)M * N * (2 * s + 1);
@@ -1110,7 +1112,8 @@ Call lay_out(int dtype, const LinearArgs* in, int n, char* ws) {
       k.ld[at] = ld;
       k.cols[at] = cols;
       k.per_row[at] = (cols + chunk - 1) / chunk;
-      while (k.log[at] < 8 && 1 << k.log[at] < k.per_row[at]) ++k.log[at];
+      // (a launch has fewer than 2^32 threads)
+      while (k.log[at] < 8 && 1 << k.log[at] < k.per_row[at] && rows << k.log[at] < (int64_t)1 << 29) ++k.log[at];
       k.first[at] = k.blocks;
       k.blocks += (int)(((rows << k.log[at]) + 255) / 256);
       k.dst[at] = ws + c.bytes;

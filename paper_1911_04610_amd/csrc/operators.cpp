@@ -63,7 +63,7 @@ xpipe_status fwd_product(const xpipe_linear_fwd_args* q, LinearArgs* a) {
   if (q->preact) XP_TRY(check_matrix("preact", q->preact, q->ldz, q->cout, es));
   if (q->bias && !at_multiple(q->bias, 4)) return fail(XPIPE_EINVAL, "bias is not aligned to its element");
   if (q->y == q->x || q->y == q->W || q->y == (const void*)q->bias || (q->preact && (q->preact == q->y || q->preact == q->x ||
-      q->preact == q->W || q->preact == q->residual)))
+      q->preact == q->W || q->preact == q->residual || q->preact == (const void*)q->bias)))
     return fail(XPIPE_EINVAL, "an output is an input's or another output's buffer");
   if (q->y == q->residual && q->ldy != q->ldr) return fail(XPIPE_EINVAL, "residual in y's buffer with another ld");
   a->epi = LIN_FWD;

@@ -2530,7 +2530,8 @@ xpipe_status xpipe_adam_flat(float* W, float* m, float* v, float* G, int64_t n, 
 xpipe_status xpipe_adam_flat_clipped(float* W, float* m, float* v, float* G, int64_t n, const xpipe_hparams* hp,
                                      int32_t zero_grad, float* pred_fwd, int32_t s_fwd, float* pred_bwd,
                                      int32_t s_bwd, const float* norm_coef, void* hip_stream) {
-  if (!norm_coef) return fail(XPIPE_EINVAL, "null norm_coef");
+  if (!norm_coef || (reinterpret_cast<uintptr_t>(norm_coef) & 3) != 0)
+    return fail(XPIPE_EINVAL, "norm_coef must be present and 4-byte aligned");
   return adam_flat(W, m, v, G, n, hp, zero_grad, pred_fwd, s_fwd, pred_bwd, s_bwd, norm_coef, hip_stream);
 }
 
@@ -2566,7 +2567,8 @@ xpipe_status xpipe_rule_flat_clipped(float* W, float* buf, float* sq, float* m, 
                                      const xpipe_rule_hparams* rp, const xpipe_hparams* hp, int32_t zero_grad,
                                      float* pred_fwd, int32_t s_fwd, float* pred_bwd, int32_t s_bwd,
                                      const float* norm_coef, void* hip_stream) {
-  if (!norm_coef) return fail(XPIPE_EINVAL, "null norm_coef");
+  if (!norm_coef || (reinterpret_cast<uintptr_t>(norm_coef) & 3) != 0)
+    return fail(XPIPE_EINVAL, "norm_coef must be present and 4-byte aligned");
   return rule_flat(W, buf, sq, m, v, G, n, rp, hp, zero_grad, pred_fwd, s_fwd, pred_bwd, s_bwd, norm_coef, hip_stream);
 }
 

@@ -526,6 +526,25 @@ def test_embedding_non_finite_rows_stay_in_their_tokens():
     assert bool(torch.isfinite(grad[ok]).all()) and bool(torch.isinf(grad[4]).all())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_relu_gradient_of_a_dead_unit_is_zero(dtype):
+    """Whatever arrives there: infinities and NaN stay out of the units whose pre-activation is not positive."""
+    torch = _torch()
+    dt = _dt(dtype)
+    z = torch.tensor([-1.0, 0.0, 2.0, -3.0, 5.0, -0.0, 1.0, -9.0] * 5, dtype=dt, device="cuda")
+    dy = torch.tensor([float("inf"), float("nan"), 3.0, float("-inf"), float("inf"), float("nan"), -2.0, 4.0] * 5, dtype=dt, device="cuda")
+    dz = torch.empty_like(z)
+    xp.xpipe_act_bwd(dy, z, dz, xp.ACT_RELU)
+    assert torch.equal(dz, torch.where(z > 0, dy, torch.zeros_like(dy)))
+    # through a layer: row 1 of dz is infinite, so its dx is at the live units alone
+    W, g2 = torch.ones(8, 40, dtype=dt, device="cuda"), torch.ones(3, 8, dtype=dt, device="cuda")
+    g2[1] = float("inf")
+    pre, dx = z.repeat(3, 1).contiguous(), torch.empty(3, 40, dtype=dt, device="cuda")
+    xp.xpipe_linear_bwd(g2, None, W, dx, act=xp.ACT_RELU, preact=pre)
+    full = torch.tensor([8.0, float("inf"), 8.0], dtype=dt, device="cuda")[:, None].expand(3, 40)
+    assert torch.equal(dx, torch.where(pre > 0, full, torch.zeros_like(dx)))
+
+
 # ---------------------------------------------------------------- norm and clipping
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("sizes", [[1], [0, 3, 0], [16384], [16385, 1, 2, 3, 16383], [5] * 500, [100003, 7, 65536] * 3])
@@ -550,6 +569,17 @@ def test_grad_norm(sizes, dtype):
         lst = xp.TensorList(views)
         xp.xpipe_grad_norm(lst, max_norm, again)
         assert torch.equal(again, out)
+
+
+def test_grad_norm_follows_a_tensor_whose_storage_was_exchanged():
+    torch = _torch()
+    a, b, out = torch.ones(100, device="cuda"), torch.full((50000,), 2.0, device="cuda"), torch.zeros(2, device="cuda")
+    lst = xp.TensorList([a])
+    xp.xpipe_grad_norm(lst, 1.0, out)
+    assert float(out[0]) == 10.0
+    a.data = b  # (other place, size and workspace)
+    xp.xpipe_grad_norm(lst, 1.0, out)
+    assert abs(float(out[0]) - math.sqrt(200000.0)) <= 1.01 * E24 * math.sqrt(200000.0)
 
 
 def test_grad_norm_of_nothing_large_values_and_non_finite_ones():

@@ -42,7 +42,7 @@ def _refused(a, status=xp.EINVAL):
     dict(rows=-1), dict(cin=0), dict(cout=0), dict(cin=-3), dict(dtype=2), dict(dtype=-1), dict(act=4), dict(act=-1),
     dict(x=None), dict(W=None), dict(y=None), dict(x=P + 1), dict(W=P + 1), dict(y=P + 1), dict(ldx=63), dict(ldw=0), dict(ldy=31),
     dict(ldx=-64), dict(residual=4 * P, ldr=31), dict(preact=4 * P, ldz=31), dict(bias=4 * P + 2), dict(y=P), dict(y=2 * P),
-    dict(preact=3 * P, ldz=32), dict(preact=P, ldz=64), dict(residual=3 * P, ldr=40), dict(residual=5 * P, ldr=32, preact=5 * P, ldz=32),
+    dict(preact=3 * P, ldz=32), dict(preact=P, ldz=64), dict(preact=6 * P, ldz=32, bias=6 * P), dict(residual=3 * P, ldr=40), dict(residual=5 * P, ldr=32, preact=5 * P, ldz=32),
     dict(y=7 * P, bias=7 * P), dict(dtype=xp.F32, x=P + 2),
 ])
 def test_linear_forward_refusals(kw):
@@ -178,7 +178,7 @@ def test_clipped_update_refusals():
     rule = lambda clip, W=P: L.xpipe_rule_flat_clipped(W, 2 * P, None, 3 * P, 4 * P, 5 * P, 8, ctypes.byref(rp), ctypes.byref(hp), 1,
                                                        None, 0, None, 0, clip, None)
     for f in (adam, rule):
-        assert f(None) == xp.EINVAL and f(6 * P, W=None) == xp.EINVAL and f(6 * P, W=P + 4) == xp.EINVAL
+        assert f(None) == xp.EINVAL and f(6 * P + 2) == xp.EINVAL and f(6 * P, W=None) == xp.EINVAL and f(6 * P, W=P + 4) == xp.EINVAL
     assert L.xpipe_stage_set_clip(None, 1.0, P, None, 0) == xp.EINVAL
 
 
@@ -197,6 +197,11 @@ def test_binding_refuses_cpu_tensors_and_mixed_arguments():
         xp.xpipe_embedding_bwd(t(3, 8), t(3, dtype=torch.int32), t(4, 8))
     with pytest.raises(ValueError):
         xp.xpipe_grad_norm([t(5)], 1.0, t(2))
+    lst, swapped = xp.TensorList([t(3), t(70000)]), t(90000)
+    assert lst.workspace_bytes == 6 * 8
+    lst.tensors[1].data = swapped
+    lst.refresh()  # read where it is now, with the workspace that its size needs
+    assert (lst.descs[1].p, lst.descs[1].n, lst.workspace_bytes) == (swapped.data_ptr(), 90000, 7 * 8)
     with pytest.raises(ValueError):
         xp.TensorList([])
     with pytest.raises(ValueError):
