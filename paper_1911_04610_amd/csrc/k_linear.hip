@@ -683,18 +683,18 @@ __global__ __launch_bounds__(WM * WN * 64) void k_linear(LinearArgs a, int tiles
 }
 
 // Both products of a backward in one launch: the first `first` workgroups are the
-// data gradient's.  They depend on nothing of each other's, and small ones alone
-// leave most of the GPU idle.
+// data gradient's (grad_first: the weight gradient's).  They depend on nothing of each
+// other's, and small ones alone leave most of the GPU idle.
 template <typename T, int B, int NS>
-__global__ __launch_bounds__(256) void k_linear_bwd(LinearArgs d, int tiles_md, int tiles_nd, int first, LinearArgs g,
-                                                    int tiles_mg, int tiles_ng) {
+__global__ __launch_bounds__(256) void k_linear_bwd(LinearArgs d, int tiles_md, int tiles_nd, int first, int grad_first,
+                                                    LinearArgs g, int tiles_mg, int tiles_ng) {
   XP_STAGES(B, B, NS);
   const int b = blockIdx.x;
-  if (b < first)
-    linear_tile<T, B, B, 2, 2, NS, false, true, LIN_DATA>(d, tiles_md, tiles_nd, xcd_tile(b, first), st0, st1, st2, st3);
+  const int t = b < first ? xcd_tile(b, first) : xcd_tile(b - first, gridDim.x - first);
+  if ((b < first) != (grad_first != 0))
+    linear_tile<T, B, B, 2, 2, NS, false, true, LIN_DATA>(d, tiles_md, tiles_nd, t, st0, st1, st2, st3);
   else
-    linear_tile<T, B, B, 2, 2, NS, true, true, LIN_GRAD>(g, tiles_mg, tiles_ng, xcd_tile(b - first, gridDim.x - first), st0,
-                                                         st1, st2, st3);
+    linear_tile<T, B, B, 2, 2, NS, true, true, LIN_GRAD>(g, tiles_mg, tiles_ng, t, st0, st1, st2, st3);
 }
 
 // the splits' partial sums added in order, and the epilogue
@@ -981,36 +981,46 @@ hipError_t go(const LinearArgs& a, hipStream_t s) {
 template <typename T, int B, int NS>
 hipError_t go_bwd(const LinearArgs& d, const LinearArgs& g, hipStream_t s) {
   const int64_t tmd = (d.M + B - 1) / B, tnd = (d.N + B - 1) / B, tmg = (g.M + B - 1) / B, tng = (g.N + B - 1) / B;
-  const int64_t first = tmd * tnd * d.splits;
+  // the product with more of the reduction per workgroup first: at the end the short ones fill the CUs evenly
+  const int64_t nd = tmd * tnd * d.splits, ng = tmg * tng * g.splits;
+  const bool grad_first = g.kper > d.kper;
   static const struct Name {
     char s[64];
     Name() { snprintf(s, sizeof s, "k_linear_bwd<%s,%d>", sizeof(T) == 2 ? "bf16" : "f32", B); }
   } name;
   XP_LAUNCH(name.s, 2.0 * d.M * d.N * d.K + 2.0 * g.M * g.N * g.K, (k_linear_bwd<T, B, NS>),
-            dim3((unsigned)(first + tmg * tng * g.splits)), dim3(256), 0, s, d, (int)tmd, (int)tnd, (int)first, g, (int)tmg,
-            (int)tng);
+            dim3((unsigned)(nd + ng)), dim3(256), 0, s, d, (int)tmd, (int)tnd, (int)(grad_first ? ng : nd), (int)grad_first,
+            g, (int)tmg, (int)tng);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && d.part) e = join<T, LIN_DATA>(d, s);
   if (e == hipSuccess && g.part) e = join<T, LIN_GRAD>(g, s);
   return e;
 }
 
-// Buffers: two for 128x128 tiles (two workgroups per CU; four buffers and one
-// workgroup were 0 to 5% slower), four for 64x64 (products of a few workgroups
-// per CU: 5 to 15% over two).
-constexpr int NS_128 = 2, NS_64 = 4;
+// Buffers: two, which leaves room for two 128x128 or five 64x64 tiles on a CU.
+// 128x128: four buffers and one tile were 0 to 5% slower.  64x64 in bf16: with up to
+// two tiles per CU and more than a few steps there is nothing else to hide the copies'
+// time behind, and four are faster (over 200 timed products: 16 to 32 steps 1.10 to
+// 1.20 of four's time with two, more steps 1.26 to 1.32; up to 8 steps the same; more
+// than two tiles per CU 0.86 to 0.97).
+constexpr int NS_128 = 2;
+template <typename T>
+bool deep(int64_t groups, int64_t k) { return sizeof(T) == 2 && groups <= 512 && k > 8 * STEP<T>; }
 template <typename T, bool TA, bool TB, int EPI>
 hipError_t by_tile(const LinearArgs& a, int tile, hipStream_t s) {
   if constexpr (sizeof(T) == 2) {
     if (tile == 256) return go<T, 256, 256, 2, 4, 2, TA, TB, EPI>(a, s);
   }
   if (tile == 128) return go<T, 128, 128, 2, 2, NS_128, TA, TB, EPI>(a, s);
-  return go<T, 64, 64, 2, 2, NS_64, TA, TB, EPI>(a, s);
+  if constexpr (sizeof(T) == 2) {
+    if (deep<T>((a.M + 63) / 64 * ((a.N + 63) / 64) * a.splits, a.kper)) return go<T, 64, 64, 2, 2, 4, TA, TB, EPI>(a, s);
+  }
+  return go<T, 64, 64, 2, 2, 2, TA, TB, EPI>(a, s);
 }
 
 template <typename T>
 hipError_t both(const LinearArgs& d, const LinearArgs& g, int tile, hipStream_t s) {
-  return tile == 128 ? go_bwd<T, 128, NS_128>(d, g, s) : go_bwd<T, 64, NS_64>(d, g, s);
+  return tile == 128 ? go_bwd<T, 128, NS_128>(d, g, s) : go_bwd<T, 64, 2>(d, g, s);
 }
 
 template <typename T>
