@@ -67,7 +67,7 @@ def kernel_key(name):
     launch names: no namespaces or arguments, storage types as bf16 / f32, and
     without the template arguments only the compiler's name shows (the general
     GEMM's gather mode, named by the library only when not 0; the row kernels'
-    rows per trip; the pools' channels per thread)."""
+    rows per trip; the pools' channels per thread; whether an update clips)."""
     import re
     n = name.replace("(anonymous namespace)::", "").split("(")[0].replace("void ", "").replace("xp::", "")
     n = n.replace("unsigned short", "bf16").replace(" ", "")
@@ -76,6 +76,7 @@ def kernel_key(name):
     if m:
         gm = int(m.group(2))
         n = "k_conv_gemm<" + m.group(1) + ("" if gm == 0 else "," + ("strided", "strided_dgrad")[gm - 1]) + ">"
+    n = {"k_adam<false>": "k_adam", "k_adam<true>": "k_adam<clip>"}.get(n, n)
     return re.sub(r"^(k_bn_apply_v|k_bn_bwd_v|k_maxpool3s2_fwd|k_maxpool3s2_bwd)<(bf16|f32),\d+>$",
                   r"\1<\2>", n)
 

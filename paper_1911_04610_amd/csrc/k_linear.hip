@@ -1030,26 +1030,51 @@ hipError_t by_kind(const LinearArgs& a, int tile, hipStream_t s) {
   return by_tile<T, true, true, LIN_GRAD>(a, tile, s);
 }
 
-// The forwards that k_linear_few takes.  Up to 32 rows (us, MI355X, tiles in brackets:
-// bf16 1x4096x4096 7.1 (12.4), 16x4096x4096 9.7 (13.0), 32x4096x4096 13.3 (14.0),
-// 16x999x1333 8.1 (13.1); 64 rows 21.2 (15.5); fp32 1x4096x4096 17.1 (25.0), 16 rows
-// 20.7 (25.1)), but not a long reduction for a few columns, whose workgroups
-// leave most CUs idle (16x16384x64 29.6 (13.4)).  And more rows whose operands would
-// have to be packed, where that and the tiles cost more: sets of four
-// workgroups per CU, in each of which the waves take 32 steps at a time, and what all
-// of them read from L2 (137x57x128 7.8 (12.4), 300x300x300 8.2 (14.5), 2000x100x100
-// 9.2 (12.4); 500x4097x100 30.6 (18.0), which stays with the tiles).
-constexpr double PACK_US = 6.0, FEW_US = 2.0, FEW_ROUND_US = 8.0, FEW_MB_PER_US = 8.0;
-bool takes_few(const LinearArgs& a, int es, bool any, double tiles_us) {
-  if (a.epi != LIN_FWD) return false;
-  const int64_t steps = ((int64_t)a.K * es + 127) / 128, round = FEW_WAVES * FEW_STEPS;
-  if (a.M <= 32) return a.N >= 1024 || steps <= 3 * round;
-  if (!any) return false;
-  const int64_t groups = (a.M + 31) / 32 * ((a.N + 15) / 16);
-  if ((a.M + 31) / 32 > 65535) return false;
-  const double us = (double)((groups + 1023) / 1024) * (FEW_US + FEW_ROUND_US * (double)steps / round) +
-                    (double)groups * 48.0 * a.K * es * 1e-6 / FEW_MB_PER_US;
-  return us < tiles_us + PACK_US;
+struct Plan {
+  int tile, splits;
+  double us;
+  int64_t kper, ldpart;
+  size_t part_b, bytes;  // offset of the bias gradient's partial sums, workspace
+};
+Plan plan(int dtype, const LinearArgs& a) {
+  Plan p{};
+  const int bk = dtype == DT_BF16 ? STEP<bf16_t> : STEP<float>;
+  const int64_t steps = ((int64_t)a.K + bk - 1) / bk;
+  p.us = pick(dtype, a.M, a.N, steps, &p.tile, &p.splits);
+  p.kper = (steps + p.splits - 1) / p.splits * bk;
+  p.splits = (int)(((int64_t)a.K + p.kper - 1) / p.kper);  // those that hold something
+  if (p.splits == 1) return p;
+  p.ldpart = (a.N + 7) / 8 * 8;
+  p.part_b = ((size_t)p.splits * a.M * p.ldpart * sizeof(float) + 255) / 256 * 256;
+  p.bytes = p.part_b + (a.grad_b ? (size_t)p.splits * a.M * sizeof(double) : 0);
+  return p;
+}
+
+// The forwards that k_linear_few takes: those for which it costs less than the
+// tiles (and, where operands are not aligned, packing them).  Its cost, in us: sets of
+// four workgroups per CU, in each of which the waves take 32 steps at a time, with a
+// time for them that grows with the rows; what the workgroups read through L2 (both
+// twice where chunks are put together from two; half as much again where rows cross
+// cache lines); W from memory.  A call's host
+// time is a floor under both sides: one launch, or two and a workspace.
+// Measured, tiles in brackets: bf16 1x4096x4096 7.6 (13.3), 16x4096x4096 10.0 (13.2),
+// 32x4096x4096 13.6 (14.8), 16x8192x2048 16.6 (13.7), 32x8192x8192 45.5 (26.3),
+// 1x8192x8192 26.4 (25.1); fp32 1x8192x8192 53 (72), 32x8192x8192 111 (77);
+// with packing 137x57x128 7.8 (12.4), 300x300x300 8.2 (14.5), 500x4097x100 30.6 (18.0),
+// fp32 777x1030x515 53.5 (25.6).
+constexpr double FEW_US = 2.0, FEW_ROUND_US = 2.3, FEW_ROW_US = 0.1, FEW_L2_MB_PER_US = 8.8, FEW_W_MB_PER_US = 5.3;
+constexpr double PACK_US = 6.0, ONE_LAUNCH_US = 7.5, TWO_LAUNCHES_US = 13.0;
+bool takes_few(const LinearArgs& a, int es, bool any, const Plan& tiles) {
+  if (a.epi != LIN_FWD || (!any && a.M > 32) || (a.M + 31) / 32 > 65535) return false;
+  const double steps = ((int64_t)a.K * es + 127) / 128, groups = (double)((a.M + 31) / 32) * ((a.N + 15) / 16);
+  const double rows = a.M <= 16 ? (double)a.M : 32.0, row_mb = (double)a.K * es * 1e-6, twice = any ? 2.0 : 1.0;
+  const double lines = any ? 2.0 : (a.lda * es | a.ldb * es) % 128 ? 1.5 : 1.0;
+  const double chain = (FEW_US + steps / (FEW_WAVES * FEW_STEPS) * (FEW_ROUND_US + FEW_ROW_US * rows) * twice) *
+                       (double)(((int64_t)groups + 1023) / 1024);
+  const double read = FEW_US + std::max(groups * (16.0 + rows) * row_mb * lines / FEW_L2_MB_PER_US, a.N * row_mb / FEW_W_MB_PER_US);
+  const bool two = any || tiles.splits > 1;
+  return std::max({chain, read, ONE_LAUNCH_US}) <=
+         std::max(tiles.us + (any ? PACK_US : 0.0), two ? TWO_LAUNCHES_US : ONE_LAUNCH_US);
 }
 template <typename T, int MT, bool ANY>
 hipError_t go_few(const LinearArgs& a, hipStream_t s) {
@@ -1072,26 +1097,6 @@ bool unaligned(const LinearArgs& a, int chunk) {
   return !chunked(a.A, a.lda, chunk) || !chunked(a.B, a.ldb, chunk) || a.K % chunk != 0;
 }
 
-struct Plan {
-  int tile, splits;
-  double us;
-  int64_t kper, ldpart;
-  size_t part_b, bytes;  // offset of the bias gradient's partial sums, workspace
-};
-Plan plan(int dtype, const LinearArgs& a) {
-  Plan p{};
-  const int bk = dtype == DT_BF16 ? STEP<bf16_t> : STEP<float>;
-  const int64_t steps = ((int64_t)a.K + bk - 1) / bk;
-  p.us = pick(dtype, a.M, a.N, steps, &p.tile, &p.splits);
-  p.kper = (steps + p.splits - 1) / p.splits * bk;
-  p.splits = (int)(((int64_t)a.K + p.kper - 1) / p.kper);  // those that hold something
-  if (p.splits == 1) return p;
-  p.ldpart = (a.N + 7) / 8 * 8;
-  p.part_b = ((size_t)p.splits * a.M * p.ldpart * sizeof(float) + 255) / 256 * 256;
-  p.bytes = p.part_b + (a.grad_b ? (size_t)p.splits * a.M * sizeof(double) : 0);
-  return p;
-}
-
 }  // namespace
 
 // A call's products with their packed operands: where those and the products' partial
@@ -1106,7 +1111,7 @@ struct Call {
 Call lay_out(int dtype, const LinearArgs* in, int n, char* ws) {
   Call c{};
   const int es = dtype == DT_BF16 ? 2 : 4, chunk = 16 / es;
-  c.few = in[0].M > 0 && takes_few(in[0], es, unaligned(in[0], chunk), plan(dtype, in[0]).us);
+  c.few = in[0].M > 0 && takes_few(in[0], es, unaligned(in[0], chunk), plan(dtype, in[0]));
   if (c.few) {
     c.p[0] = in[0];
     return c;
