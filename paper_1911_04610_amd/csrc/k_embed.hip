@@ -32,7 +32,9 @@ XP_DEV void unpack(const u32x4_t& u, float (&v)[CHUNK<T>]) {
 
 // ---------------------------------------------------------------- lookup
 // One 16-byte chunk of one position per thread (VEC), else one element.  The
-// product is formed in fp64 and rounded to fp32 (for bf16, from there).
+// product is formed in fp64 and rounded to fp32 (for bf16, from there).  Bound by
+// memory: 65536 rows of 2048 bf16 103 us, 16384 of 4096 43 us, 5.2 and 6.3 TB/s read and
+// written.
 template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void k_embed_fwd(EmbedArgs a) {
   constexpr int C = VEC ? CHUNK<T> : 1;
@@ -68,7 +70,9 @@ XP_DEV uint32_t sort_key(int t, int vocab) { return (uint32_t)t < (uint32_t)voca
 
 // Few positions: a position's place is the number of positions before it in the
 // order.  Sixteen positions per workgroup; the sixteen waves go through all keys in
-// LDS, and each quarter of a wave takes every fourth four of the wave's own.
+// LDS, and each quarter of a wave takes every fourth four of the wave's own.  Bound by
+// the LDS reads: 8192 keys 8 to 10 us (64 positions per workgroup, all lanes reading the same
+// key, 20; the radix sort's four launches 23).
 constexpr int RANK_MAX = 8192, RANK_POS = 16;
 __global__ __launch_bounds__(1024) void k_embed_rank(const int32_t* __restrict__ tokens, int n, int vocab,
                                                       uint32_t* __restrict__ keys, uint32_t* __restrict__ pos) {
@@ -217,7 +221,8 @@ __global__ __launch_bounds__(256) void k_embed_scatter(const uint32_t* __restric
 // it (part 0) or goes on behind it (part 1) is left as an fp32 partial for
 // k_embed_join; a run that does both is part 0.  Rows are taken GROUP at a
 // time, with the accumulators' rows that they end in, so that the loads of a
-// group are in flight together.
+// group are in flight together.  Bound by memory: 65536 rows of 2048 bf16 into a table
+// of 50000 111 to 120 us, 4.4 to 4.7 TB/s of rows and accumulators.
 constexpr int GROUP = 4;
 template <typename T, bool VEC>
 __global__ __launch_bounds__(64) void k_embed_bwd(EmbedArgs a, const uint32_t* __restrict__ keys,
@@ -289,7 +294,9 @@ __global__ __launch_bounds__(64) void k_embed_bwd(EmbedArgs a, const uint32_t* _
 
 // The runs that pass a span's end: the span that a run starts in adds its
 // partials.  JOIN_WAVES waves take consecutive parts of the run's spans, 64 JOIN_COLS
-// columns each, and their sums are added in order.
+// columns each, and their sums are added in order.  Most workgroups find no run to
+// join and end: eight waves each were 10 us slower for 65536 positions, and one
+// wave 9, where the four take 17 (and the longest run bounds it).
 constexpr int JOIN_COLS = 4, JOIN_WAVES = 4;
 __global__ __launch_bounds__(64 * JOIN_WAVES) void k_embed_join(EmbedArgs a, const uint32_t* __restrict__ keys, int span,
                                                      const float* __restrict__ part) {
@@ -359,7 +366,9 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void k_embed_join(EmbedArgs a, con
 // ---------------------------------------------------------------- few positions
 // Without a sort: the workgroup of the first position that holds a token adds all
 // of its positions' rows, 64 chunks of columns a wave, each of its four waves a
-// consecutive part of them; the others find an earlier one and end.  One launch.
+// consecutive part of them; the others find an earlier one and end.  One launch: 1024
+// positions of 1024 bf16 10.6 us, 1025 sorted 15.5; every workgroup reads all tokens, so
+// the sort takes over there.  256 positions of 256 fp32 4.4 us, its launch.
 constexpr int SMALL_MAX = 1024;
 template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void k_embed_bwd_small(EmbedArgs a) {
