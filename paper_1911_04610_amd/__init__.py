@@ -693,6 +693,8 @@ def _check_embedding(rows, name, tokens, table, dev):
     if table.dim() != 2 or not table.is_contiguous():
         raise ValueError("table and grad: contiguous [vocab, dim] expected")
     (vocab, dim), n = table.shape, tokens.numel()
+    if vocab >= 1 << 31 or dim >= 1 << 31:  # (ctypes would cut them to 32 bits)
+        raise ValueError("table and grad: 2^31 rows or columns or more")
     if tokens.dtype is not _torch.int32 or not tokens.is_contiguous() or tokens.get_device() != dev:
         raise ValueError("tokens: contiguous int32 on the same device expected")
     if (rows.dim() < 1 or not rows.is_contiguous() or rows.get_device() != dev or rows.shape[-1] != dim or

@@ -208,3 +208,14 @@ def test_binding_refuses_cpu_tensors_and_mixed_arguments():
         xp.TensorList([t(3), t(3, dtype=torch.bfloat16)])
     with pytest.raises(ValueError):
         xp.TensorList([t(3, 4).t()])
+
+
+def test_binding_refuses_tables_that_32_bits_cannot_count():
+    import torch
+    meta = lambda *s, dtype=torch.bfloat16: torch.empty(*s, dtype=dtype, device="meta")
+    tokens = meta(3, dtype=torch.int32)
+    assert xp._check_embedding(meta(3, 8), "y", tokens, meta(70000, 8), -1) == (70000, 8, 3)
+    with pytest.raises(ValueError):  # (cut to 32 bits: a table of five rows)
+        xp._check_embedding(meta(3, 1), "y", tokens, meta((1 << 32) + 5, 1), -1)
+    with pytest.raises(ValueError):
+        xp._check_embedding(meta(3, 1 << 31), "y", tokens, meta(2, 1 << 31), -1)
