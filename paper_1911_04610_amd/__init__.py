@@ -300,6 +300,8 @@ class Stage:
         self._h = _P()
         H, W, C = _hwc(in_shape)
         self._descs = layer_descs(layers)
+        # what the stage runs on, whatever stream is current later
+        self._run_stream = stream if stream is not None else torch.cuda.current_stream()
         if static_workspace:
             self.workspace = None
             _check(lib().xpipe_stage_create_static(self._descs, len(layers), micro_batch, T, H, W, C,
@@ -413,11 +415,13 @@ class Stage:
         ws, size = None, _SZ(0)
         if norm_coef is not None:
             _check_norm_coef(norm_coef, self.grad.get_device())
+            # the stage's stream writes and reads it: given out again only behind the updates in flight
+            norm_coef.record_stream(self._run_stream)
             if max_norm > 0:
                 one = TensorDesc(_ptr(self.grad), self.P)
                 _check(lib().xpipe_grad_norm_query(ctypes.byref(one), 1, ctypes.byref(size)))
                 if self._clip_ws is None:  # kept from then on: updates in flight may use it
-                    with _torch.cuda.stream(self.stream):
+                    with _torch.cuda.stream(self._run_stream):
                         self._clip_ws = _torch.empty(max(size.value, 8), dtype=_torch.uint8, device=self.device)
                 ws = self._clip_ws
         _check(lib().xpipe_stage_set_clip(self._h, max_norm, _ptr(norm_coef), _ptr(ws), size.value))

@@ -992,3 +992,35 @@ def test_workloads_on_two_streams_at_once():
         torch.cuda.synchronize()
     for a, b in zip(alone, both):
         assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_stage_updates_in_flight_keep_the_clip_that_was_replaced():
+    """{norm, coefficient} dropped by its caller and replaced while updates on the stage's own stream
+    still use it: the allocator gives its memory out again only behind them."""
+    torch = _torch()
+    hp, s = xp.Hyper(), torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        st = _small_stage()  # (runs on the stream that is current here)
+    x, lab = torch.randn(16, 24, generator=_gen(4)).cuda(), torch.zeros(16, dtype=torch.int32, device="cuda")
+    y = torch.empty(16, 10, device="cuda")
+    clip = torch.zeros(2, device="cuda")
+    at = clip.data_ptr()
+    torch.cuda.synchronize()
+    big = torch.empty(1 << 28, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        for _ in range(20):
+            big.fill_(1.0)  # some ms of work ahead of the update
+        st.xpipe_stage_set_clip(0.05, clip)
+        st.xpipe_predict_weights(xp.FWD, 1, hp, 0)
+        st.xpipe_predict_weights(xp.BWD, 1, hp, 0)
+        st.xpipe_stage_fwd(x, y, lab)
+        st.xpipe_stage_bwd(x, labels=lab)
+        st.xpipe_adam_step(hp, 0)
+    st.xpipe_stage_set_clip(0.0, None)
+    del clip
+    others = [torch.full((2,), 3.0, device="cuda") for _ in range(64)]
+    inside = [o for o in others if o.data_ptr() == at]
+    torch.cuda.synchronize()
+    assert not inside and all(o.tolist() == [3.0, 3.0] for o in others)
+    st.destroy()
