@@ -416,7 +416,8 @@ xpipe_status xpipe_rule_flat_clipped(float* W, float* buf, float* sq, float* m, 
  * 8-byte aligned, of xpipe_grad_norm_query's bytes (0 for small lists), free
  * again once the call's work is done.  sumsq (device, fp64, may be NULL) receives the sum;
  * norm_coef (device, two fp32, may be NULL) {norm, coefficient}.  max_norm > 0
- * where norm_coef is given. */
+ * where norm_coef is given; an infinite max_norm clips nothing (coefficient 1, of
+ * an infinite norm NaN). */
 typedef struct {
   const void* p;
   int64_t n;
@@ -502,7 +503,7 @@ xpipe_status xpipe_act_bwd(const void* dy, const void* z, void* dz, int64_t n, i
  * table [vocab][dim], y and dy [n_tokens][dim] in the storage dtype, grad
  * [vocab][dim] fp32, all contiguous; tokens int32 on the device.  A token
  * outside [0, vocab) is padding: its row of y is zeros, its dy is not
- * read.  y can be a stage's x, and dy its dx.  Products and sums are formed in
+ * read.  Outputs must not overlap inputs.  y can be a stage's x, and dy its dx.  Products and sums are formed in
  * fp64 and rounded once to fp32 (y in bf16: from there; from 1025 tokens on, a
  * run of equal tokens in the sorted order is added in parts of up to 64, whose
  * sums are rounded to fp32).  The order of the terms follows from tokens and
