@@ -1064,28 +1064,33 @@ Plan plan(int dtype, const LinearArgs& a) {
 // The forwards that k_linear_few takes: those for which it costs less than the
 // tiles (and, where operands are not aligned, packing them).  Its cost, in us: sets of
 // four workgroups per CU, in each of which the waves take 32 steps at a time, with a
-// time for them that grows with the rows; what the workgroups read through L2 (both
-// twice where chunks are put together from two; half as much again where rows cross
-// cache lines); W from memory.  A call's host
+// time for them that grows with the rows; what the workgroups read through L2 (twice
+// where chunks are put together from two; half as much again where rows cross
+// cache lines); W from memory.  Packing reads and writes both operands.  A call's host
 // time is a floor under both sides: one launch, or two and a workspace.
 // Measured, tiles in brackets: bf16 1x4096x4096 7.6 (13.3), 16x4096x4096 10.0 (13.2),
 // 32x4096x4096 13.6 (14.8), 16x8192x2048 16.6 (13.7), 32x8192x8192 45.5 (26.3),
 // 1x8192x8192 26.4 (25.1); fp32 1x8192x8192 53 (72), 32x8192x8192 111 (77);
 // with packing 137x57x128 7.8 (12.4), 300x300x300 8.2 (14.5), 500x4097x100 30.6 (18.0),
-// fp32 777x1030x515 53.5 (25.6).
+// fp32 777x1030x515 53.5 (25.6); bf16 16x1003x16384 18 (24), 24x1003x16384 37 (25),
+// 8x4099x2048 19 (21), 8x4099x8192 29 (42), 8x12815x2048 67 (38), 8x12815x16384 172 (258),
+// fp32 8x4099x2048 40 (32), 8x12815x16384 333 (554).
 constexpr double FEW_US = 2.0, FEW_ROUND_US = 2.3, FEW_ROW_US = 0.1, FEW_L2_MB_PER_US = 8.8, FEW_W_MB_PER_US = 5.3;
-constexpr double PACK_US = 6.0, ONE_LAUNCH_US = 7.5, TWO_LAUNCHES_US = 13.0;
+constexpr double FEW_ANY_SET_US[2] = {9.5, 11.0}, FEW_ANY_ROWS[2] = {13.0, 42.0};  // up to 16 rows, 32
+constexpr double PACK_US = 6.0, PACK_MB_PER_US = 5.0, ONE_LAUNCH_US = 7.5, TWO_LAUNCHES_US = 13.0;
 bool takes_few(const LinearArgs& a, int es, bool any, const Plan& tiles) {
   if (a.epi != LIN_FWD || (!any && a.M > 32) || (a.M + 31) / 32 > 65535) return false;
   const double steps = ((int64_t)a.K * es + 127) / 128, groups = (double)((a.M + 31) / 32) * ((a.N + 15) / 16);
-  const double rows = a.M <= 16 ? (double)a.M : 32.0, row_mb = (double)a.K * es * 1e-6, twice = any ? 2.0 : 1.0;
+  const double rows = any ? FEW_ANY_ROWS[a.M > 16] : a.M <= 16 ? (double)a.M : 32.0, row_mb = (double)a.K * es * 1e-6;
+  const double set = any ? FEW_ANY_SET_US[a.M > 16] : FEW_ROUND_US + FEW_ROW_US * rows;
   const double lines = any ? 2.0 : (a.lda * es | a.ldb * es) % 128 ? 1.5 : 1.0;
-  const double chain = (FEW_US + steps / (FEW_WAVES * FEW_STEPS) * (FEW_ROUND_US + FEW_ROW_US * rows) * twice) *
-                       (double)(((int64_t)groups + 1023) / 1024);
+  const double chain = (FEW_US + steps / (FEW_WAVES * FEW_STEPS) * set) * (double)(((int64_t)groups + 1023) / 1024);
   const double read = FEW_US + std::max(groups * (16.0 + rows) * row_mb * lines / FEW_L2_MB_PER_US, a.N * row_mb / FEW_W_MB_PER_US);
+  // packing: both operands (of few rows nearly all is W), read and written
+  const double pack = any ? PACK_US + 2.0 * (double)(a.M + a.N) * row_mb / PACK_MB_PER_US : 0.0;
   const bool two = any || tiles.splits > 1;
   return std::max({chain, read, ONE_LAUNCH_US}) <=
-         std::max(tiles.us + (any ? PACK_US : 0.0), two ? TWO_LAUNCHES_US : ONE_LAUNCH_US);
+         std::max(tiles.us + pack, two ? TWO_LAUNCHES_US : ONE_LAUNCH_US);
 }
 template <typename T, int MT, bool ANY>
 hipError_t go_few(const LinearArgs& a, hipStream_t s) {
