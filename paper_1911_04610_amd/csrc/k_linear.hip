@@ -1076,7 +1076,7 @@ Plan plan(int dtype, const LinearArgs& a) {
 // 8x4099x2048 19 (21), 8x4099x8192 29 (42), 8x12815x2048 67 (38), 8x12815x16384 172 (258),
 // fp32 8x4099x2048 40 (32), 8x12815x16384 333 (554).
 constexpr double FEW_US = 2.0, FEW_ROUND_US = 2.3, FEW_ROW_US = 0.1, FEW_L2_MB_PER_US = 8.8, FEW_W_MB_PER_US = 5.3;
-constexpr double FEW_ANY_SET_US[2] = {9.5, 11.0}, FEW_ANY_ROWS[2] = {13.0, 42.0};  // up to 16 rows, 32
+constexpr double FEW_ANY_SET_US[2] = {9.5, 11.0}, FEW_ANY_ROWS[2] = {13.0, 48.0};  // up to 16 rows, 32
 constexpr double PACK_US = 6.0, PACK_MB_PER_US = 5.0, ONE_LAUNCH_US = 7.5, TWO_LAUNCHES_US = 13.0;
 bool takes_few(const LinearArgs& a, int es, bool any, const Plan& tiles) {
   if (a.epi != LIN_FWD || (!any && a.M > 32) || (a.M + 31) / 32 > 65535) return false;
