@@ -20,21 +20,36 @@ template <typename T> constexpr int STEP = 128 / (int)sizeof(T);
 // ---------------------------------------------------------------- activations
 // In fp32: a stored value is rounded to 8 (bf16) or 24 bits from there, and the
 // product before it has fp32 sums.  The exponential and the reciprocal are the
-// hardware's (good to 2^-23, the former times the argument's size).  The normal
-// distribution function is Abramowitz and Stegun's 7.1.26, off by at most 7.5e-8 of
-// 1, which shares its exponential with the density in GELU's slope (both gradients of
-// 8192x8192x2048 behind a GELU 639 us with erff and expf, 569 so).
+// hardware's (good to 2^-23, the former times the argument's size), but for GELU's
+// exponential in fp32 storage, which is expf.  The normal distribution function shares
+// its exponential with the density in GELU's slope: Phi(-a) = exp(-a^2 / 2) t P(t) with
+// t = 1 / (1 + p a), where
+//   fp32 storage: P has nine terms, fitted here for the least relative error over
+//     0 <= a <= 14.5 (below, Phi leaves fp32): good to 8 * 2^-24 of itself, rounding
+//     included, in the far tail too (xpipe_act_bwd of 2^26 elements 137 us, as ReLU; with
+//     erfcf 155).
+//   bf16 storage: Abramowitz and Stegun's 7.1.26, off by at most 7.5e-8 of 1 (both
+//     gradients of 8192x8192x2048 behind a GELU 639 us with erff and expf, 569 so).
+template <typename T>
 XP_DEV float normal_cdf(float z, float& e) {  // and e = exp(-z^2 / 2)
-  const float x = fabsf(z) * 0.70710678118654752f;
-  e = __expf(-x * x);
-  const float t = __builtin_amdgcn_rcpf(1.f + 0.3275911f * x);
-  const float q = t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
-  const float tail = 0.5f * q * e;
+  float tail;
+  if constexpr (sizeof(T) == 4) {
+    e = expf(-0.5f * z * z);
+    const float t = __builtin_amdgcn_rcpf(1.f + 0.28f * fabsf(z));
+    tail = e * t * (0.111689358f + t * (0.111959679f + t * (0.101177704f + t * (0.0911249906f + t * (0.0554682483f +
+                   t * (0.0176901268f + t * (0.0725002237f + t * (-0.0846662747f + t * 0.0230559717f))))))));
+  } else {
+    const float x = fabsf(z) * 0.70710678118654752f;
+    e = __expf(-x * x);
+    const float t = __builtin_amdgcn_rcpf(1.f + 0.3275911f * x);
+    const float q = t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+    tail = 0.5f * q * e;
+  }
   return z >= 0.f ? 1.f - tail : tail;
 }
 XP_DEV float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
 
-template <int N>
+template <typename T, int N>
 XP_DEV void act_values(float (&z)[N], int act) {
   if (act == LIN_RELU) {
 #pragma unroll
@@ -43,7 +58,7 @@ XP_DEV void act_values(float (&z)[N], int act) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       float e;
-      z[i] *= normal_cdf(z[i], e);
+      z[i] *= normal_cdf<T>(z[i], e);
     }
   } else if (act == LIN_SILU) {
 #pragma unroll
@@ -53,7 +68,7 @@ XP_DEV void act_values(float (&z)[N], int act) {
 
 // v *= act'(z); 0 at 0 for the ReLU, and then 0 whatever v (an infinite gradient of a
 // dead unit is none)
-template <int N>
+template <typename T, int N>
 XP_DEV void act_slopes(float (&v)[N], const float (&z)[N], int act) {
   if (act == LIN_RELU) {
 #pragma unroll
@@ -62,7 +77,7 @@ XP_DEV void act_slopes(float (&v)[N], const float (&z)[N], int act) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       float e;
-      const float c = normal_cdf(z[i], e);
+      const float c = normal_cdf<T>(z[i], e);
       v[i] *= c + z[i] * 0.39894228040143268f * e;
     }
   } else if (act == LIN_SILU) {
@@ -205,11 +220,11 @@ XP_DEV void finish(const LinearArgs& a, int m, int n, float (&v)[CHUNK<T>], cons
 #pragma unroll
     for (int i = 0; i < C; ++i) v[i] += b[i];
     if (a.z_out) st_chunk<T>((T*)a.z_out + at(m, a.ldz, n), vec, left, v);
-    act_values(v, a.act);
+    act_values<T>(v, a.act);
   } else if (a.z_in) {
     float z[C];
     unpack<T>(f.z, z);
-    act_slopes(v, z, a.act);
+    act_slopes<T>(v, z, a.act);
   }
   if (a.res) {
     float r[C];
@@ -236,7 +251,7 @@ XP_DEV void finish1(const LinearArgs& a, int m, int n, float sum, const Fetched1
   };
   float v[1] = {sum + f.b};
   if (a.z_out) st(a.z_out, a.ldz, v[0]);
-  act_values(v, a.act);
+  act_values<T>(v, a.act);
   st(a.y, a.ldy, a.res ? v[0] + f.r : v[0]);
 }
 
@@ -905,7 +920,7 @@ __global__ __launch_bounds__(256) void k_linear_pack(PackArgs a) {
 }
 
 // ---------------------------------------------------------------- activation gradient
-// Bound by memory: 2^26 bf16 elements behind a GELU 70 us, 5.8 TB/s.
+// Bound by memory: 2^26 elements behind a GELU 70 us in bf16, 5.8 TB/s, 137 in fp32, 5.9.
 template <typename T>
 __global__ __launch_bounds__(256) void k_act_bwd(const T* __restrict__ dy, const T* __restrict__ z, T* __restrict__ dz,
                                                  int64_t n, int act, int vec) {
@@ -917,7 +932,7 @@ __global__ __launch_bounds__(256) void k_act_bwd(const T* __restrict__ dy, const
     float g[C], zz[C];
     unpack<T>(ld_chunk<T>(dy + i * C, v, left), g);
     unpack<T>(ld_chunk<T>(z + i * C, v, left), zz);
-    act_slopes(g, zz, act);
+    act_slopes<T>(g, zz, act);
     st_chunk<T>(dz + i * C, v, left, g);
   }
 }

@@ -1024,3 +1024,41 @@ def test_stage_updates_in_flight_keep_the_clip_that_was_replaced():
     torch.cuda.synchronize()
     assert not inside and all(o.tolist() == [3.0, 3.0] for o in others)
     st.destroy()
+
+
+# ---------------------------------------------------------------- activations, value by value
+def _gelu_args(g):
+    torch = _torch()
+    return torch.cat([torch.linspace(-12, 12, 4801), torch.randn(6000, generator=g), torch.tensor([0.0, -0.0])])
+
+
+def _phi64(z):
+    torch = _torch()
+    return torch.special.erfc(-z / math.sqrt(2)) / 2
+
+
+def test_gelu_of_fp32_storage_is_good_to_fp32():
+    """Each value relative to itself, in the lower tail too.  Phi(-a) = erfc(a / sqrt 2) / 2
+    falls as exp(-a^2 / 2): an argument off by 1.5 * 2^-24 of itself (constant and
+    product) is raised by at most z^2 + 1; the functions behind it are taken as good to
+    16 ulp for Phi and 3 for the exponential (32 and 6 of 2^-24), the density's argument
+    to 2^-24 of z^2 / 2, and every product and sum rounds once."""
+    torch = _torch()
+    z = _gelu_args(_gen(21))
+    z64 = z.double()
+    P, zphi = _phi64(z64), z64 * torch.exp(-z64 * z64 / 2) / math.sqrt(2 * math.pi)
+    cdf = P * (1.5 * (z64 * z64 + 1) + 33) * E24
+    n = len(z)
+    y = torch.empty(n, 1, device="cuda")
+    xp.xpipe_linear_fwd(z[:, None].cuda(), torch.ones(1, 1, device="cuda"), None, y, act=xp.ACT_GELU)
+    _close(y[:, 0], z64 * P, z64.abs() * (cdf + P * E24), "value")
+    for dy in (torch.ones(n), torch.randn(n, generator=_gen(22))):
+        dz = torch.empty(n, device="cuda")
+        xp.xpipe_act_bwd(dy.cuda(), z.cuda(), dz, xp.ACT_GELU)
+        s = P + zphi
+        tol = cdf + zphi.abs() * (z64 * z64 / 2 + 9) * E24 + s.abs() * E24
+        _close(dz, dy.double() * s, dy.double().abs() * (tol + s.abs() * E24), "slope")
+    # the same slope behind a product
+    W, dx = torch.ones(1, 1, device="cuda"), torch.empty(n, 1, device="cuda")
+    xp.xpipe_linear_bwd(dy[:, None].cuda(), None, W, dx, act=xp.ACT_GELU, preact=z[:, None].cuda())
+    _close(dx[:, 0], dy.double() * s, dy.double().abs() * (tol + s.abs() * E24), "dx")
