@@ -28,8 +28,9 @@ template <typename T> constexpr int STEP = 128 / (int)sizeof(T);
 //     0 <= a <= 14.5 (below, Phi leaves fp32): good to 8 * 2^-24 of itself, rounding
 //     included, in the far tail too (xpipe_act_bwd of 2^26 elements 137 us, as ReLU; with
 //     erfcf 155).
-//   bf16 storage: Abramowitz and Stegun's 7.1.26, off by at most 7.5e-8 of 1 (both
-//     gradients of 8192x8192x2048 behind a GELU 639 us with erff and expf, 569 so).
+//   bf16 storage: six terms, fitted to 5e-8 of 1 and to 2^-11 of Phi itself, an eighth of
+//     bf16's half step, where that is less (both gradients of 8192x8192x2048 behind a GELU
+//     639 us with erff and expf, 570 so).
 template <typename T>
 XP_DEV float normal_cdf(float z, float& e) {  // and e = exp(-z^2 / 2)
   float tail;
@@ -39,11 +40,10 @@ XP_DEV float normal_cdf(float z, float& e) {  // and e = exp(-z^2 / 2)
     tail = e * t * (0.111689358f + t * (0.111959679f + t * (0.101177704f + t * (0.0911249906f + t * (0.0554682483f +
                    t * (0.0176901268f + t * (0.0725002237f + t * (-0.0846662747f + t * 0.0230559717f))))))));
   } else {
-    const float x = fabsf(z) * 0.70710678118654752f;
-    e = __expf(-x * x);
-    const float t = __builtin_amdgcn_rcpf(1.f + 0.3275911f * x);
-    const float q = t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
-    tail = 0.5f * q * e;
+    e = __expf(-0.5f * z * z);
+    const float t = __builtin_amdgcn_rcpf(1.f + 0.29f * fabsf(z));
+    tail = e * t * (0.116616427f + t * (0.102033926f + t * (0.176945863f + t * (-0.0907976066f + t * (0.283885533f -
+                   t * 0.0886841861f)))));
   }
   return z >= 0.f ? 1.f - tail : tail;
 }

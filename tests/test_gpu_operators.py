@@ -1062,3 +1062,22 @@ def test_gelu_of_fp32_storage_is_good_to_fp32():
     W, dx = torch.ones(1, 1, device="cuda"), torch.empty(n, 1, device="cuda")
     xp.xpipe_linear_bwd(dy[:, None].cuda(), None, W, dx, act=xp.ACT_GELU, preact=z[:, None].cuda())
     _close(dx[:, 0], dy.double() * s, dy.double().abs() * (tol + s.abs() * E24), "dx")
+
+
+def test_gelu_of_bf16_storage_in_the_lower_tail():
+    """The fit is good to 2^-11 of Phi, an eighth of the stored value's half step; the
+    exponential's argument is off by 1.5 * 2^-24 of z^2 / 2 <= 72, under 2^-17."""
+    torch = _torch()
+    z = torch.cat([torch.linspace(-12, 12, 4801), torch.randn(6000, generator=_gen(23))]).bfloat16()
+    z64 = z.double()
+    P = _phi64(z64)
+    tol = 2.0 ** -11 + 2.0 ** -17 + 4 * E24
+    y = torch.empty(len(z), 1, dtype=torch.bfloat16, device="cuda")
+    xp.xpipe_linear_fwd(z[:, None].cuda(), torch.ones(1, 1, dtype=torch.bfloat16, device="cuda"), None, y, act=xp.ACT_GELU)
+    want = z64 * P
+    _close(y[:, 0], want, want.abs() * (tol + 2.0 ** -8 * (1 + tol)), "value")
+    dz, dy = torch.empty(len(z), dtype=torch.bfloat16, device="cuda"), torch.ones(len(z), dtype=torch.bfloat16)
+    xp.xpipe_act_bwd(dy.cuda(), z.cuda(), dz, xp.ACT_GELU)
+    zphi = z64 * torch.exp(-z64 * z64 / 2) / math.sqrt(2 * math.pi)
+    off = (P + zphi.abs()) * tol
+    _close(dz, P + zphi, off + 2.0 ** -8 * ((P + zphi).abs() + off), "slope")
