@@ -1081,3 +1081,23 @@ def test_gelu_of_bf16_storage_in_the_lower_tail():
     zphi = z64 * torch.exp(-z64 * z64 / 2) / math.sqrt(2 * math.pi)
     off = (P + zphi.abs()) * tol
     _close(dz, P + zphi, off + 2.0 ** -8 * ((P + zphi).abs() + off), "slope")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,offset", [(1, 0), (4096, 0), (4103, 0), (4103, 1), (70001, 3)])
+def test_act_bwd_in_place(n, offset, dtype):
+    """dz in dy's or z's buffer: the bits of a call with a buffer of its own, and nothing around it."""
+    torch = _torch()
+    g = _gen(n + offset)
+    wide = lambda: torch.randn(n + 16, generator=g).to(_dt(dtype)).cuda()
+    for act in ACT.values():
+        dy, z = wide(), wide()
+        cut = lambda t: t[offset:offset + n]
+        want = torch.empty(n, dtype=dy.dtype, device="cuda")
+        xp.xpipe_act_bwd(cut(dy), cut(z), want, act)
+        for which in (0, 1):
+            both = [dy.clone(), z.clone()]
+            xp.xpipe_act_bwd(cut(both[0]), cut(both[1]), cut(both[which]), act)
+            assert torch.equal(cut(both[which]), want) and torch.equal(both[1 - which], (dy, z)[1 - which])
+            assert torch.equal(both[which][:offset], (dy, z)[which][:offset])
+            assert torch.equal(both[which][offset + n:], (dy, z)[which][offset + n:])
