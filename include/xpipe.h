@@ -510,8 +510,9 @@ xpipe_status xpipe_act_bwd(const void* dy, const void* z, void* dz, int64_t n, i
  * sizes, so a repeated call gives the same bits. */
 xpipe_status xpipe_embedding_fwd(const void* table, const int32_t* tokens, int64_t n_tokens, int32_t vocab, int32_t dim,
                                  double scale, int32_t dtype, void* y, void* hip_stream);
-/* workspace: device memory, 256-byte aligned, of the query's bytes, free again
- * once the call's work is done. */
+/* Calls and query take fewer than 2^30 tokens and vocabulary entries and at most
+ * 2^20 columns (more: XPIPE_EUNSUPPORTED).  workspace: device memory, 256-byte
+ * aligned, of the query's bytes, free again once the call's work is done. */
 xpipe_status xpipe_embedding_bwd_query(int64_t n_tokens, int32_t vocab, int32_t dim, size_t* workspace_bytes);
 xpipe_status xpipe_embedding_bwd(const void* dy, const int32_t* tokens, int64_t n_tokens, int32_t vocab, int32_t dim,
                                  double scale, int32_t dtype, float* grad, void* workspace, size_t workspace_bytes,

@@ -144,13 +144,18 @@ xpipe_status bwd_products(const xpipe_linear_bwd_args* q, LinearArgs (&p)[2]) {
   return XPIPE_OK;
 }
 
-xpipe_status check_embedding(const void* rows, const char* name, const int32_t* tokens, int64_t n, int32_t vocab,
-                             int32_t dim, double scale, int32_t dtype) {
+xpipe_status check_embedding_sizes(int64_t n, int32_t vocab, int32_t dim) {
   if (n < 0 || vocab < 1 || dim < 1) return fail(XPIPE_EINVAL, "n_tokens must be >= 0, vocab and dim >= 1");
-  if (!known_dtype(dtype)) return fail(XPIPE_EINVAL, "unknown dtype");
-  if (!std::isfinite(scale)) return fail(XPIPE_EINVAL, "scale must be finite");
   if (n >= (int64_t)1 << 30 || vocab >= 1 << 30 || dim > 1 << 20)
     return fail(XPIPE_EUNSUPPORTED, "2^30 tokens or vocabulary entries or more, or more than 2^20 columns");
+  return XPIPE_OK;
+}
+
+xpipe_status check_embedding(const void* rows, const char* name, const int32_t* tokens, int64_t n, int32_t vocab,
+                             int32_t dim, double scale, int32_t dtype) {
+  if (!known_dtype(dtype)) return fail(XPIPE_EINVAL, "unknown dtype");
+  if (!std::isfinite(scale)) return fail(XPIPE_EINVAL, "scale must be finite");
+  XP_TRY(check_embedding_sizes(n, vocab, dim));
   if (n == 0) return XPIPE_OK;
   if (!rows) return fail(XPIPE_EINVAL, std::string("null ") + name);
   if (!tokens) return fail(XPIPE_EINVAL, "null tokens");
@@ -330,7 +335,7 @@ xpipe_status xpipe_embedding_fwd(const void* table, const int32_t* tokens, int64
 
 xpipe_status xpipe_embedding_bwd_query(int64_t n_tokens, int32_t vocab, int32_t dim, size_t* workspace_bytes) {
   if (!workspace_bytes) return fail(XPIPE_EINVAL, "null output");
-  if (n_tokens < 0 || vocab < 1 || dim < 1) return fail(XPIPE_EINVAL, "n_tokens must be >= 0, vocab and dim >= 1");
+  XP_TRY(check_embedding_sizes(n_tokens, vocab, dim));
   *workspace_bytes = embed_bwd_bytes(n_tokens, dim);
   return XPIPE_OK;
 }

@@ -219,3 +219,14 @@ def test_binding_refuses_tables_that_32_bits_cannot_count():
         xp._check_embedding(meta(3, 1), "y", tokens, meta((1 << 32) + 5, 1), -1)
     with pytest.raises(ValueError):
         xp._check_embedding(meta(3, 1 << 31), "y", tokens, meta(2, 1 << 31), -1)
+
+
+def test_embedding_query_refuses_what_the_call_refuses():
+    L, need = xp.lib(), ctypes.c_size_t(77)
+    q = lambda *a: L.xpipe_embedding_bwd_query(*a, ctypes.byref(need))
+    for sizes in ((1 << 30, 10, 8), (1 << 60, 10, 8), ((1 << 63) - 1, 1, 1), (4, 1 << 30, 8), (4, 10, (1 << 20) + 1)):
+        assert q(*sizes) == xp.EUNSUPPORTED and need.value == 77, sizes
+        assert L.xpipe_embedding_bwd(P, 2 * P, *sizes, 1.0, xp.BF16, 3 * P, 4 * P, 1 << 62, None) == xp.EUNSUPPORTED
+    # the largest that both take: keys and positions twice, and two rows of partial sums for every 64 positions
+    n, dim = (1 << 30) - 1, 1 << 20
+    assert q(n, (1 << 30) - 1, dim) == xp.OK and need.value >= 16 * n + 8 * (n // 64) * dim
