@@ -426,8 +426,9 @@ xpipe_status xpipe_grad_norm_query(const xpipe_tensor* tensors, int32_t n_tensor
 xpipe_status xpipe_grad_norm(const xpipe_tensor* tensors, int32_t n_tensors, int32_t dtype, double max_norm,
                              double* sumsq, float* norm_coef, void* workspace, size_t workspace_bytes,
                              void* hip_stream);
-/* The same from n sums of squares (device, fp64), added in order: a pipeline's
- * stages each pass their own sumsq on and clip by the norm over all of them. */
+/* The same from n sums of squares (device, fp64), added in fp64 in an order that n
+ * alone decides (not that from the first to the last): a pipeline's stages each pass
+ * their own sumsq on and clip by the norm over all of them. */
 xpipe_status xpipe_clip_coef(const double* sumsq, int64_t n, double max_norm, float* norm_coef, void* hip_stream);
 
 /* ---------------------------------------------------------------- linear

@@ -798,7 +798,7 @@ def xpipe_grad_norm(tensors, max_norm: float, norm_coef=None, sumsq=None, worksp
 
 
 def xpipe_clip_coef(sumsq, max_norm: float, norm_coef, stream=None):
-    """{norm, coefficient} from float64 sums of squares (one per stage), added in order."""
+    """{norm, coefficient} from float64 sums of squares (one per stage), added in an order that their number decides."""
     L = lib()
     dev, here = _device_of(sumsq)
     if not here:

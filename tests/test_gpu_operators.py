@@ -1101,3 +1101,18 @@ def test_act_bwd_in_place(n, offset, dtype):
             assert torch.equal(cut(both[which]), want) and torch.equal(both[1 - which], (dy, z)[1 - which])
             assert torch.equal(both[which][:offset], (dy, z)[which][:offset])
             assert torch.equal(both[which][offset + n:], (dy, z)[which][offset + n:])
+
+
+@pytest.mark.parametrize("n", [0, 1, 3, 64, 65, 1024, 1025, 5000])
+def test_clip_coef_of_any_number_of_sums(n):
+    """fp64 additions in whatever order are off by n 2^-53 of the sum at most; the results round to fp32 once."""
+    torch = _torch()
+    parts = torch.rand(n, generator=_gen(n), dtype=torch.float64) * torch.logspace(-3, 3, n, dtype=torch.float64)
+    norm = math.sqrt(math.fsum(parts.tolist()))
+    coef = min(1.0, 0.5 / (norm + 1e-6))
+    out = [torch.full((2,), 7.0, device="cuda") for _ in range(2)]
+    for o in out:
+        xp.xpipe_clip_coef(parts.cuda(), 0.5, o)
+    tol = E24 + n * 2.0 ** -53
+    assert abs(float(out[0][0]) - norm) <= tol * norm and abs(float(out[0][1]) - coef) <= tol * coef
+    assert torch.equal(out[0], out[1])
