@@ -1116,3 +1116,58 @@ def test_clip_coef_of_any_number_of_sums(n):
     tol = E24 + n * 2.0 ** -53
     assert abs(float(out[0][0]) - norm) <= tol * norm and abs(float(out[0][1]) - coef) <= tol * coef
     assert torch.equal(out[0], out[1])
+
+
+def _difference_case(act, dtype):
+    """A chain act -> linear -> act with its stored inputs, its loss in 64 bits, and for each
+    gradient the direction of its own signs: no cancellation hides an error there."""
+    torch = _torch()
+    dt, g = _dt(dtype), _gen(60 + ACT[act])
+    rows, cin, cout = 9, 16, 24
+    r = lambda *s: torch.randn(*s, generator=g)
+    zin = r(rows, cin)
+    zin = torch.where(zin.abs() < 0.05, torch.full_like(zin, 0.125), zin).to(dt)
+    W, b, dy = (r(cout, cin) * cin ** -0.5).to(dt), r(cout), r(rows, cout).to(dt)
+    x = _act64(zin.double(), act).to(dt)
+    Z, V, B, D, X = zin.double(), W.double(), b.double(), dy.double(), x.double()
+    z64 = X @ V.t() + B
+
+    def loss(zi, v, bb):  # x is stored: the layer's input is what it reads, moved as its pre-activation moves it
+        return float((_act64((X + (_act64(zi, act) - _act64(Z, act))) @ v.t() + bb, act) * D).sum())
+
+    G = D * _slope64(z64, act)
+    want = {"dx": (G @ V) * _slope64(Z, act), "gW": G.t() @ X, "gb": G.sum(0)}
+    h, diff = 1e-4, {}
+    for name, w in want.items():
+        d = torch.sign(w) * 0.1
+        step = lambda s: loss(Z + s * d if name == "dx" else Z, V + s * d if name == "gW" else V, B + s * d if name == "gb" else B)
+        diff[name] = (step(h) - step(-h)) / (2 * h)
+    # dz is stored (u), from a stored z (u |z| times the slope's slope, at most 0.8), then dx is (u); u |dz| |V| is
+    # the sum's share of the former two.  Products and slopes in fp32: 40 * 2^-23 of the same magnitudes.
+    u = _half_step(dtype)
+    curve = 0.0 if act in ("none", "relu") else 0.8
+    dzoff = (G.abs() + D.abs() * curve * z64.abs()) * (u + u * u) + 40 * E23 * D.abs() * 1.13
+    off = {"dx": (dzoff @ V.abs()) * 1.13 + u * want["dx"].abs() * (1 + u) + 40 * E23 * 1.13 * (G.abs() @ V.abs()),
+           "gW": dzoff.t() @ X.abs() + 40 * E23 * (G.abs().t() @ X.abs()), "gb": dzoff.sum(0) + 40 * E23 * G.abs().sum(0)}
+    tol = {k: 0.1 * float(v.sum()) + 1e-6 * (1 + abs(diff[k])) for k, v in off.items()}
+    return zin, x, W, b, dy, want, diff, tol
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", list(ACT))
+def test_linear_gradient_against_differences_along_its_signs(act, dtype):
+    """Along the gradient's own signs the difference is several times its bound, so that a
+    missing, halved or turned gradient fails."""
+    torch = _torch()
+    zin, x, W, b, dy, want, diff, tol = _difference_case(act, dtype)
+    c = lambda t: t.cuda()
+    z, y = torch.empty_like(c(dy)), torch.empty_like(c(dy))
+    xp.xpipe_linear_fwd(c(x), c(W), c(b), y, act=ACT[act], preact=z)
+    dz, dx = torch.empty_like(z), torch.empty_like(c(x))
+    xp.xpipe_act_bwd(c(dy), z, dz, ACT[act])
+    gW, gb = torch.zeros(W.shape, device="cuda"), torch.zeros(b.shape, device="cuda")
+    xp.xpipe_linear_bwd(dz, c(x), c(W), dx, gW, gb, act=ACT[act], preact=c(zin) if act != "none" else None)
+    for name, got in (("dx", dx), ("gW", gW), ("gb", gb)):
+        inner = 0.1 * float((_d(got) * torch.sign(want[name])).sum())
+        assert diff[name] > 4 * tol[name], name  # (so 0, half of it and its negative are outside)
+        assert abs(diff[name] - inner) <= tol[name], f"{name}: {diff[name]} by difference, {inner}"
