@@ -1171,3 +1171,99 @@ def test_linear_gradient_against_differences_along_its_signs(act, dtype):
         inner = 0.1 * float((_d(got) * torch.sign(want[name])).sum())
         assert diff[name] > 4 * tol[name], name  # (so 0, half of it and its negative are outside)
         assert abs(diff[name] - inner) <= tol[name], f"{name}: {diff[name]} by difference, {inner}"
+
+
+# The tiles (and splits) that the launcher's costs give the data and the weight gradient:
+BACKWARD_TILES = [
+    ("bf16", 2056, 4104, 40),   # data 256, weights 64 in splits
+    ("bf16", 2050, 4100, 40),   # the same from packed operands
+    ("bf16", 130, 6000, 8200),  # data 256 in splits, weights 256
+    ("bf16", 8200, 130, 6000),  # data 64, weights 256 in splits
+    ("bf16", 130, 1500, 6000),  # data 128 in splits, weights 256
+    ("bf16", 6000, 136, 1504),  # data 64, weights 128 in splits
+    ("bf16", 130, 12300, 40),   # data 128, weights 64
+    ("bf16", 40, 136, 12304),   # data 64 in splits, weights 128
+    ("bf16", 136, 12304, 136),  # both 128 in one launch
+    ("bf16", 264, 777, 6000),   # and the data gradient split
+    ("bf16", 6000, 776, 264),   # the weights' split
+    ("bf16", 6000, 136, 6000),  # both split
+    ("bf16", 1504, 40, 1504),   # both 64 and split
+    ("f32", 1500, 4100, 40),    # data 128, weights 64 in splits
+    ("f32", 520, 1500, 6000),   # data 128 in splits, weights 64
+    ("f32", 40, 1500, 4100),    # data 64 in splits, weights 128
+    ("f32", 6000, 1500, 520),   # data 64, weights 128 in splits
+    ("f32", 520, 6000, 520),    # both 128 in one launch
+    ("f32", 6000, 520, 1500),   # and the weights' split
+    ("f32", 1500, 521, 6001),   # the data gradient split, from packed operands
+]
+
+
+@pytest.mark.parametrize("dtype,rows,cin,cout", BACKWARD_TILES)
+def test_linear_backward_on_every_tile(dtype, rows, cin, cout):
+    torch = _torch()
+    dt, g = _dt(dtype), _gen(rows + cin + cout)
+    dz, x, W = _rows(g, rows, cout, dt), _rows(g, rows, cin, dt), _rows(g, cout, cin, dt, scale=cout ** -0.5)
+    z, res, dx = _rows(g, rows, cin, dt), _rows(g, rows, cin, dt), torch.empty(rows, cin, dtype=dt, device="cuda")
+    gW, gb = torch.randn(cout * cin, generator=g).cuda(), torch.randn(cout, generator=g).cuda()
+    gW0, gb0 = gW.clone(), gb.clone()
+    xp.xpipe_linear_bwd(dz, x, W, dx, gW, gb, act=xp.ACT_GELU, preact=z, residual=res)
+    _check_bwd(dz, x, W, dx, gW, gb, gW0, gb0, "gelu", z, res, dtype)
+    again, gW2, gb2 = torch.empty_like(dx), gW0.clone(), gb0.clone()
+    xp.xpipe_linear_bwd(dz, x, W, again, gW2, gb2, act=xp.ACT_GELU, preact=z, residual=res)
+    assert torch.equal(dx, again) and torch.equal(gW, gW2) and torch.equal(gb, gb2)
+
+
+FORWARD_TILES = [("bf16", 2056, 40, 4104), ("bf16", 130, 8200, 6000), ("bf16", 136, 40, 12304), ("bf16", 136, 6000, 1504),
+                 ("bf16", 40, 1504, 40), ("f32", 1500, 40, 4100), ("f32", 520, 6000, 1500), ("f32", 40, 520, 40)]
+
+
+@pytest.mark.parametrize("dtype,rows,cin,cout", FORWARD_TILES)  # 256, split, 128, split, (64 or few rows); 128, split, (64 or few rows)
+def test_linear_forward_on_every_tile(dtype, rows, cin, cout):
+    torch = _torch()
+    dt, g = _dt(dtype), _gen(rows + cin + cout)
+    x, W, b = _rows(g, rows, cin, dt), _rows(g, cout, cin, dt, scale=cin ** -0.5), torch.randn(cout, generator=g).cuda()
+    r, y, z = _rows(g, rows, cout, dt), torch.empty(rows, cout, dtype=dt, device="cuda"), torch.empty(rows, cout, dtype=dt, device="cuda")
+    xp.xpipe_linear_fwd(x, W, b, y, act=xp.ACT_GELU, residual=r, preact=z)
+    _check_fwd(x, W, b, r, y, z, "gelu", dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols,long", [(140, 136, 300), (140, 136, 4104), (504, 4096, 1024)])  # two buffers, splits, four buffers
+def test_linear_products_alone_on_small_tiles(rows, cols, long, dtype):
+    torch = _torch()
+    dt, g, u = _dt(dtype), _gen(long), _half_step(dtype)
+    a, b = _rows(g, rows, long, dt), _rows(g, cols, long, dt, scale=long ** -0.5)
+    y, z = torch.empty(rows, cols, dtype=dt, device="cuda"), torch.empty(rows, cols, dtype=dt, device="cuda")
+    xp.xpipe_linear_fwd(a, b, None, y, act=xp.ACT_SILU, preact=z)
+    _check_fwd(a, b, None, None, y, z, "silu", dtype)
+    bt = b.t().contiguous()
+    xp.xpipe_linear_bwd(a, None, bt, y)
+    want, mag = _d(a) @ _d(bt), _d(a).abs() @ _d(bt).abs()
+    tol = (long + 1) * E23 * mag
+    _close(y, want, u * (want.abs() + tol) + tol, "dx")
+    at, gW, gb = a.t().contiguous(), torch.zeros(rows, cols, device="cuda"), torch.zeros(rows, device="cuda")
+    xp.xpipe_linear_bwd(at, bt, None, None, gW, gb)
+    _close(gW, want, (long + 2) * E23 * mag + E24 * mag, "grad_W")
+    _close(gb, _d(at).sum(0), 33 * E24 * _d(at).abs().sum(0), "grad_b")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,dim", [(1500, 4100), (2050, 8200)])
+def test_embedding_gradient_of_wide_rows(n, dim, dtype):
+    """Rows of more columns than one pass of the join's workgroups takes, one token in most positions."""
+    torch = _torch()
+    g = _gen(n)
+    t = _tokens(g, n, 40, "uniform")
+    t[torch.rand(n, generator=g).cuda() < 0.8] = 7
+    t[::97] = -1
+    dy, grad = _rows(g, n, dim, _dt(dtype)), torch.randn(40, dim, generator=g).cuda()
+    before = grad.clone()
+    xp.xpipe_embedding_bwd(dy, t, grad, scale=0.5)
+    live = (t >= 0).cpu()
+    idx = t.cpu().long()[live]
+    want = _d(before).index_add_(0, idx, _d(dy)[live] * 0.5)
+    mag = torch.zeros(40, dim, dtype=torch.float64).index_add_(0, idx, _d(dy)[live].abs() * 0.5)
+    _close(grad, want, (want.abs() + mag) * E24 * (1 + 1e-6), "grad")
+    again = before.clone()
+    xp.xpipe_embedding_bwd(dy, t, again, scale=0.5)
+    assert torch.equal(grad, again)
