@@ -25,12 +25,12 @@ template <typename T> constexpr int STEP = 128 / (int)sizeof(T);
 // its exponential with the density in GELU's slope: Phi(-a) = exp(-a^2 / 2) t P(t) with
 // t = 1 / (1 + p a), where
 //   fp32 storage: P has nine terms, fitted here for the least relative error over
-//     0 <= a <= 14.5 (below, Phi leaves fp32): good to 8 * 2^-24 of itself, rounding
-//     included, in the far tail too (xpipe_act_bwd of 2^26 elements 137 us, as ReLU; with
-//     erfcf 155).
+//     0 <= a <= 14.5 (beyond, Phi leaves fp32): good to 8 * 2^-24 of itself, rounding
+//     included, and the exponential's argument to a^2 / 2 of them, in the far tail too
+//     (xpipe_act_bwd of 2^26 elements 137 us, as ReLU; with erfcf 155).
 //   bf16 storage: six terms, fitted to 5e-8 of 1 and to 2^-11 of Phi itself, an eighth of
 //     bf16's half step, where that is less (both gradients of 8192x8192x2048 behind a GELU
-//     639 us with erff and expf, 570 so).
+//     639 us with erff and expf, 559 so).
 template <typename T>
 XP_DEV float normal_cdf(float z, float& e) {  // and e = exp(-z^2 / 2)
   float tail;
@@ -342,13 +342,15 @@ template <int BM, int BN> constexpr int STAGE = (BM + BN) * 128;
 // WN waves of 32x32 MFMA results.  Both operands are copied from memory
 // straight into LDS, one step (128 bytes of the reduction) at a time, with NS
 // buffers: NS - 1 steps are in flight while one is multiplied.
-// Measured (256x256 tiles): forward 8192x16384x4096 0.86 to 0.93 ms, 1.2 to 1.3
-// PFLOP/s (the library's plain product 0.72 ms), 8192x8192x8192 0.86 ms (0.85 ms);
-// bound by the matrix units, busy for two thirds of the cycles at the 1.7 GHz or so
-// that power leaves them there.  8192x8192x2048 dx 238 us, behind a GELU 285: the
-// epilogue's own traffic, which nothing overlaps with one tile on a CU (128x128
-// tiles, two on a CU, 289 and 319).  fp32 8192x8192x8192 7.5 ms, 146 TFLOP/s (154 the
-// library's): the fp32 matrix rate.
+// Measured (256x256 tiles, the library's plain product in turn on the same card in
+// brackets): forward 8192x16384x4096 0.83 ms (0.68), 1.33 PFLOP/s (1.61); 8192x8192x8192 0.82
+// (0.67).  By counters the matrix units are busy for two thirds of the cycles, at the
+// 1.7 GHz that power leaves: the last third is the waves' wait for each step's barrier,
+// copies and fragments (0.38 of their cycles), which one tile of two waves per SIMD does not
+// cover.  8192x8192x2048 dx 233 us (222), behind a GELU 286: the epilogue's own
+// traffic, which nothing overlaps with one tile on a CU (128x128 tiles, two on a CU, 289
+// and 319); weight gradient 252 (237).  fp32 8192x8192x8192 7.4 ms, 148 TFLOP/s (154);
+// 4096x4096x2048 dx and weight gradient 0.49 ms each, 140 (149): the fp32 matrix rate.
 template <typename T, int BM, int BN, int WM, int WN, int NS, bool TA, bool TB, int EPI>
 XP_DEV void linear_tile(const LinearArgs& a, int tiles_m, int tiles_n, int lin, unsigned char* st0, unsigned char* st1,
                         unsigned char* st2, unsigned char* st3) {
@@ -795,8 +797,8 @@ XP_DEV u32x4_t ld_any(const char* p, int n) {
 // straight into registers (16x16 products, W the columns, the rows of x the rows,
 // empty ones zeros).  The eight waves of a workgroup take the reduction's 128-byte
 // steps in turn and add their results through LDS in the order of the waves: no
-// workspace, one launch.  ANY: operands of any alignment.  bf16 1x4096x4096 6.2 us,
-// 5.4 TB/s of W.
+// workspace, one launch.  ANY: operands of any alignment.  bf16 1x4096x4096 7.1 to 7.8
+// us, 4.3 to 4.7 TB/s of W.
 constexpr int FEW_WAVES = 8, FEW_STEPS = 4;  // steps in flight per wave
 template <typename T, int MT, bool ANY>
 __global__ __launch_bounds__(FEW_WAVES * 64) void k_linear_few(LinearArgs a) {
@@ -896,8 +898,8 @@ struct PackArgs {
   int cols[3], per_row[3], log[3];  // columns, chunks per packed row, log2 of the lanes that take a row
   int first[3], blocks;             // first workgroup, and their number
 };
-// Bound by its launch at the sizes where it counts (1001x999x1333 backward, 9 MB read
-// and written: 5 to 7 us).
+// Bound by its launch at the sizes where it counts (1001x999x1333 backward, 15 MB read
+// and written: 6.3 to 8.1 us).
 template <typename T>
 __global__ __launch_bounds__(256) void k_linear_pack(PackArgs a) {
   constexpr int C = CHUNK<T>, ES = (int)sizeof(T);
@@ -1090,6 +1092,8 @@ Plan plan(int dtype, const LinearArgs& a) {
 // fp32 777x1030x515 53.5 (25.6); bf16 16x1003x16384 18 (24), 24x1003x16384 37 (25),
 // 8x4099x2048 19 (21), 8x4099x8192 29 (42), 8x12815x2048 67 (38), 8x12815x16384 172 (258),
 // fp32 8x4099x2048 40 (32), 8x12815x16384 333 (554).
+// Next to where both sides cost the same the estimates (off by up to 10% each) choose
+// wrongly: bf16 8x12815x4096 is taken at 68 (59), 32x4096x4096 left at 14.8 for 13.6.
 constexpr double FEW_US = 2.0, FEW_ROUND_US = 2.3, FEW_ROW_US = 0.1, FEW_L2_MB_PER_US = 8.8, FEW_W_MB_PER_US = 5.3;
 constexpr double FEW_ANY_SET_US[2] = {9.5, 11.0}, FEW_ANY_ROWS[2] = {13.0, 48.0};  // up to 16 rows, 32
 constexpr double PACK_US = 6.0, PACK_MB_PER_US = 5.0, ONE_LAUNCH_US = 7.5, TWO_LAUNCHES_US = 13.0;
