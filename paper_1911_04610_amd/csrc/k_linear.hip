@@ -19,10 +19,10 @@ template <typename T> constexpr int STEP = 128 / (int)sizeof(T);
 
 // ---------------------------------------------------------------- activations
 // In fp32: a stored value is rounded to 8 (bf16) or 24 bits from there, and the
-// product before it has fp32 sums.  The exponential and the reciprocal are the
-// hardware's (good to 2^-23, the former times the argument's size), but for GELU's
-// exponential in fp32 storage, which is expf.  The normal distribution function shares
-// its exponential with the density in GELU's slope: Phi(-a) = exp(-a^2 / 2) t P(t) with
+// product before it has fp32 sums.  The reciprocal is the hardware's (good to 2^-23), and
+// so is the exponential in bf16 storage (2^-23 times the argument's size); in fp32 it
+// is expf, good to as much of itself whatever the argument.  The normal distribution
+// function shares its exponential with the density in GELU's slope: Phi(-a) = exp(-a^2 / 2) t P(t) with
 // t = 1 / (1 + p a), where
 //   fp32 storage: P has nine terms, fitted here for the least relative error over
 //     0 <= a <= 14.5 (beyond, Phi leaves fp32): good to 8 * 2^-24 of itself, rounding
@@ -47,7 +47,8 @@ XP_DEV float normal_cdf(float z, float& e) {  // and e = exp(-z^2 / 2)
   }
   return z >= 0.f ? 1.f - tail : tail;
 }
-XP_DEV float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
+template <typename T>
+XP_DEV float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + (sizeof(T) == 4 ? expf(-z) : __expf(-z))); }
 
 template <typename T, int N>
 XP_DEV void act_values(float (&z)[N], int act) {
@@ -62,7 +63,7 @@ XP_DEV void act_values(float (&z)[N], int act) {
     }
   } else if (act == LIN_SILU) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) z[i] *= sigmoid(z[i]);
+    for (int i = 0; i < N; ++i) z[i] *= sigmoid<T>(z[i]);
   }
 }
 
@@ -83,7 +84,7 @@ XP_DEV void act_slopes(float (&v)[N], const float (&z)[N], int act) {
   } else if (act == LIN_SILU) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const float s = sigmoid(z[i]);
+      const float s = sigmoid<T>(z[i]);
       v[i] *= s * (1.f + z[i] * (1.f - s));
     }
   }

@@ -1267,3 +1267,22 @@ def test_embedding_gradient_of_wide_rows(n, dim, dtype):
     again = before.clone()
     xp.xpipe_embedding_bwd(dy, t, again, scale=0.5)
     assert torch.equal(grad, again)
+
+
+def test_silu_of_fp32_storage_is_good_to_fp32():
+    """Each value relative to itself: the exponential is taken as good to 3 ulp (6 of 2^-24), the
+    reciprocal to 1 (2), the sum and every product and difference round once."""
+    torch = _torch()
+    z = torch.cat([torch.linspace(-80, 80, 16001), torch.randn(6000, generator=_gen(24)), torch.tensor([0.0, -0.0])])
+    z64, n = z.double(), len(z)
+    s = torch.sigmoid(z64)
+    y = torch.empty(n, 1, device="cuda")
+    xp.xpipe_linear_fwd(z[:, None].cuda(), torch.ones(1, 1, device="cuda"), None, y, act=xp.ACT_SILU)
+    off = 9 * E24  # of the sigmoid
+    _close(y[:, 0], z64 * s, z64.abs() * s * (off + E24) * (1 + off), "value")
+    dz = torch.empty(n, device="cuda")
+    xp.xpipe_act_bwd(torch.ones(n).cuda(), z.cuda(), dz, xp.ACT_SILU)
+    rest = s * off + 2 * E24 * (1 - s)  # off 1 - s
+    inner = 1 + z64 * (1 - s)
+    tol = s * (z64.abs() * (rest + E24 * (1 - s)) + inner.abs() * E24) + s * inner.abs() * (off + E24)
+    _close(dz, s * inner, tol * (1 + 1e-5) + E24 * (s * inner).abs(), "slope")
