@@ -180,10 +180,9 @@ def prepare(case, seed):
         for name in ("q_len", "k_len", "prefix", "doc", "bias", "gbias"):
             d.setdefault(name, None)
         B, nq, nk, H, K, D = (case[k] for k in ("batch", "nq", "nk", "heads", "kv_heads", "dim"))
-        out = dict(o=empty(B, nq, H, D), lse=empty(B, H, nq, dtype=torch.float32))
+        out = dict(o=empty(B, nq, H, D), stats=empty(B, H, nq, 2, dtype=torch.float32))
         if op == "attn_train":
-            out.update(dq=empty(B, nq, H, D), dk=empty(B, nk, K, D), dv=empty(B, nk, K, D),
-                       o32=empty(B, nq, H, D, dtype=torch.float32) if case["dtype"] == "bf16" else None)
+            out.update(dq=empty(B, nq, H, D), dk=empty(B, nk, K, D), dv=empty(B, nk, K, D))
     return dict(case=dict(case), **d, **out)
 
 
@@ -308,9 +307,8 @@ def _own(s):
     if op == "attn":
         xp.xpipe_attention_fwd(s["q"], s["k"], s["v"], s["o"], **how)
         return {"o": s["o"]}
-    xp.xpipe_attention_fwd(s["q"], s["k"], s["v"], s["o"], lse=s["lse"], o32=s["o32"], **how)
-    xp.xpipe_attention_bwd(s["do"], s["q"], s["k"], s["v"], s["o"] if s["o32"] is None else s["o32"], s["lse"], s["dq"],
-                           s["dk"], s["dv"], s["gbias"], **how)
+    xp.xpipe_attention_fwd(s["q"], s["k"], s["v"], s["o"], stats=s["stats"], **how)
+    xp.xpipe_attention_bwd(s["do"], s["q"], s["k"], s["v"], s["o"], s["stats"], s["dq"], s["dk"], s["dv"], s["gbias"], **how)
     out = {"o": s["o"], "dq": s["dq"], "dk": s["dk"], "dv": s["dv"]}
     return dict(out, gbias=s["gbias"]) if c["bias"] else out
 
