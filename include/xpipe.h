@@ -519,6 +519,132 @@ xpipe_status xpipe_embedding_bwd(const void* dy, const int32_t* tokens, int64_t 
                                  double scale, int32_t dtype, float* grad, void* workspace, size_t workspace_bytes,
                                  void* hip_stream);
 
+/* ---------------------------------------------------------------- RMS norm
+ * The norm in front of a token network's layers, with the skip connection's
+ * addition before it, and its gradients.
+ *   forward:  h = x + residual;  n = 1 / sqrt(mean(h^2) + eps);  y = h n weight
+ *   backward: g = dy weight;  dx = n (g - h n^2 mean(g h)) + residual;
+ *             grad_weight += sum over rows of dy h n
+ * sum receives h (for the next skip connection and the backward); the backward's
+ * residual is the gradient that reaches h another way (the skip connection's), and its
+ * dx is the gradient of both x and the forward's residual.  weight is the fp32
+ * prediction.  A row's sums are fp64, the rest fp32, each stored value is rounded
+ * once (sum is rounded apart; y comes from the unrounded h).  A row's results
+ * depend on its own values alone, and the order of grad_weight's sum on the sizes alone.
+ * Matrices as for the linear layers; dim at most 32768 (more: XPIPE_EUNSUPPORTED);
+ * eps > 0; rows >= 0 (0: nothing is done).  y and sum may each be x's or residual's
+ * buffer (same pointer and ld), dx may be dy's, h's or residual's; outputs must not
+ * overlap inputs otherwise, nor one another. */
+typedef struct {
+  int64_t rows;
+  int32_t dim, dtype;
+  double eps;
+  const void* x; int64_t ldx;            /* [rows][dim] */
+  const void* residual; int64_t ldr;     /* [rows][dim], or NULL */
+  const float* weight;                   /* [dim] */
+  void* sum; int64_t lds;                /* [rows][dim]: receives h, or NULL */
+  void* y; int64_t ldy;                  /* [rows][dim] */
+} xpipe_rmsnorm_fwd_args;
+typedef struct {
+  int64_t rows;
+  int32_t dim, dtype;
+  double eps;
+  const void* dy; int64_t lddy;          /* [rows][dim] */
+  const void* h; int64_t ldh;            /* [rows][dim] */
+  const float* weight;                   /* [dim] */
+  const void* residual; int64_t ldr;     /* [rows][dim], or NULL */
+  void* dx; int64_t lddx;                /* [rows][dim], or NULL */
+  float* grad_weight;                    /* [dim], added to, or NULL */
+} xpipe_rmsnorm_bwd_args;
+xpipe_status xpipe_rmsnorm_fwd(const xpipe_rmsnorm_fwd_args* args, void* hip_stream);
+/* workspace: device memory, 256-byte aligned, of the query's bytes, free again once
+ * the call's work is done (NULL where the query gives 0). */
+xpipe_status xpipe_rmsnorm_bwd_query(const xpipe_rmsnorm_bwd_args* args, size_t* workspace_bytes);
+xpipe_status xpipe_rmsnorm_bwd(const xpipe_rmsnorm_bwd_args* args, void* workspace, size_t workspace_bytes,
+                               void* hip_stream);
+
+/* ---------------------------------------------------------------- relative position bias
+ * A learned bias of attention's scores by the distance between key and query, one
+ * value for each of `buckets` ranges of distances and each head.
+ *   forward:  bias[h][max_distance + d] = table[bucket(d)][h],  d = -max_distance .. max_distance
+ *   backward: grad_table[b][h] += sum over d with bucket(d) = b of dbias[h][max_distance + d]
+ * d is the key's position less the query's; bias is what xpipe_attention_fwd reads
+ * with bias_range = max_distance (which takes further distances as the furthest), dbias
+ * what xpipe_attention_bwd adds up.  Buckets of a distance a = |d|, n of them (all of them
+ * for keys before the query, those after it counting as a = 0; with bidirectional != 0
+ * half of them, the upper half for d > 0): a < n / 2 has its own, and further ones share
+ * n / 2 + floor(log(a / (n / 2)) / log(max_distance / (n / 2)) (n - n / 2)), at most n - 1, a
+ * distance on a border belonging to the bucket that begins there.  All buffers fp32,
+ * contiguous, not overlapping; n >= 2, max_distance > n / 2.  At most 1024 buckets, 4096
+ * heads and a distance of 2^20 (more: XPIPE_EUNSUPPORTED).  Sums are fp64, in an order that
+ * the sizes decide. */
+xpipe_status xpipe_relbias_fwd(const float* table, int32_t buckets, int32_t heads, int32_t max_distance, int32_t bidirectional,
+                               float* bias, void* hip_stream);
+xpipe_status xpipe_relbias_bwd(const float* dbias, int32_t buckets, int32_t heads, int32_t max_distance, int32_t bidirectional,
+                               float* grad_table, void* hip_stream);
+
+/* ---------------------------------------------------------------- attention
+ * Attention of a token network, forward (for training, for whole texts and for
+ * single new tokens over the keys and values kept so far) and its gradients.  For query
+ * i of a head (key head = head / (heads / kv_heads)) and the keys j that it sees:
+ *   x = scale q_i . k_j;  s = cap tanh(x / cap) (cap 0: x) + bias[head][clamp(j - pos_i)]
+ *   P = softmax of s over j;  o_i = sum of P v_j
+ * Positions: key j is at j, query i at i + k_len - q_len: the queries are the last of the
+ * sequence.  A query sees the keys j
+ *   j < k_len[b];  with causal: j <= pos_i, or j < prefix[b];  with documents: of its own
+ *   (q_doc[b][i] = k_doc[b][j], and not negative).
+ * Rows that see nothing (also those behind q_len, and of a negative document) give zeros,
+ * in o and in every gradient; keys and values behind k_len or of a negative document,
+ * and queries and gradients behind q_len or of a negative document, are not used,
+ * whatever they hold.  (Another value that is not finite can also reach rows that do not see it,
+ * those of the same tile: 0 times it is a NaN.)  A -inf in bias masks; a row of which every score is -inf sees nothing.
+ * Types: as the linear layers' (products with fp32 sums; in XPIPE_BF16 P and the score
+ * gradients are rounded to bf16 as operands of the second products); scores, maxima and
+ * sums are fp32, and the order of the sums follows from the sizes and lengths alone.
+ * Layout: [batch][token][head][head_dim], contiguous only in head_dim, aligned to their
+ * element, strides in elements: >= 0 for inputs (0 shares them), and such that no two
+ * elements fall together for outputs; the token's at most XPIPE_ATTENTION_MAX_STRIDE.
+ * head_dim 1 .. 128, batch * heads * (nq / 128 + 1) and the same of keys below 2^27, nq and nk below 2^24,
+ * bias_range 1 .. 2^20 (beyond: XPIPE_EUNSUPPORTED).  Lengths outside 0 .. nq, 0 .. nk are taken as
+ * the nearest of them.  Outputs must not overlap inputs nor one another. */
+#define XPIPE_ATTENTION_MAX_STRIDE ((int64_t)1 << 22)
+typedef struct {
+  const void* p;
+  int64_t batch, token, head;            /* strides */
+} xpipe_heads;
+typedef struct {
+  int32_t batch, nq, nk, heads, kv_heads, head_dim, dtype;
+  int32_t causal, bias_range;
+  double scale, cap;                     /* scale > 0; cap >= 0 */
+  xpipe_heads q, k, v;
+  const int32_t* q_len;                  /* [batch] on the device, or NULL: nq */
+  const int32_t* k_len;                  /* [batch], or NULL: nk */
+  const int32_t* prefix;                 /* [batch], or NULL; needs causal */
+  const int32_t* q_doc;                  /* [batch][nq], or NULL */
+  const int32_t* k_doc;                  /* [batch][nk]; both or none */
+  const float* bias;                     /* [heads][2 bias_range + 1], or NULL */
+} xpipe_attention_inputs;
+typedef struct {
+  xpipe_attention_inputs in;
+  xpipe_heads o;                         /* written */
+  float* stats;                          /* [batch][heads][nq][2]: largest score, sum of exp(score - largest); or NULL */
+} xpipe_attention_fwd_args;
+/* The backward takes the forward's inputs, its o and its stats.  (dq reads do . o from the
+ * rounded o; dk, dv and grad_bias use the same sum as P dP, in fp32.) */
+typedef struct {
+  xpipe_attention_inputs in;
+  xpipe_heads dout, o;
+  const float* stats;
+  xpipe_heads dq, dk, dv;                /* written */
+  float* grad_bias;                      /* [heads][2 bias_range + 1], added to, or NULL */
+} xpipe_attention_bwd_args;
+xpipe_status xpipe_attention_fwd_query(const xpipe_attention_fwd_args* args, size_t* workspace_bytes);
+xpipe_status xpipe_attention_bwd_query(const xpipe_attention_bwd_args* args, size_t* workspace_bytes);
+/* workspace: device memory, 256-byte aligned, of at least the query's bytes, free
+ * again once the call's work is done (NULL where the query gives 0). */
+xpipe_status xpipe_attention_fwd(const xpipe_attention_fwd_args* args, void* workspace, size_t workspace_bytes, void* hip_stream);
+xpipe_status xpipe_attention_bwd(const xpipe_attention_bwd_args* args, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Optional per-kernel timing (measurement support, not part of the method):
  * while enabled, hipEvents bracket every kernel the stage launches on its
  * stream.  xpipe_stage_timing_count waits for the recorded launches and

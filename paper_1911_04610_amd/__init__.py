@@ -13,7 +13,8 @@ Entry points (same names as the C ABI):
   xpipe_predict_flat, xpipe_adam_flat, xpipe_rule_flat (with clip= their _clipped forms);
   around a stage: xpipe_linear_fwd, xpipe_linear_bwd, xpipe_act_bwd,
   xpipe_embedding_fwd, xpipe_embedding_bwd, xpipe_grad_norm (over a TensorList),
-  xpipe_clip_coef.
+  xpipe_clip_coef, xpipe_rmsnorm_fwd, xpipe_rmsnorm_bwd, xpipe_relbias_fwd,
+  xpipe_relbias_bwd, xpipe_attention_fwd, xpipe_attention_bwd.
 The last group checks devices, types and shapes (ValueError), runs on its
 tensors' device (on `stream`, or that device's current stream) and allocates
 the workspace that a call needs from torch on that stream, unless it is given one.
@@ -98,6 +99,39 @@ class LinearBwdArgs(ctypes.Structure):
                 ("lddx", ctypes.c_int64), ("grad_W", ctypes.c_void_p), ("grad_b", ctypes.c_void_p)]
 
 
+class RmsnormFwdArgs(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("eps", ctypes.c_double),
+                ("x", ctypes.c_void_p), ("ldx", ctypes.c_int64), ("residual", ctypes.c_void_p), ("ldr", ctypes.c_int64),
+                ("weight", ctypes.c_void_p), ("sum", ctypes.c_void_p), ("lds", ctypes.c_int64),
+                ("y", ctypes.c_void_p), ("ldy", ctypes.c_int64)]
+
+
+class RmsnormBwdArgs(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("eps", ctypes.c_double),
+                ("dy", ctypes.c_void_p), ("lddy", ctypes.c_int64), ("h", ctypes.c_void_p), ("ldh", ctypes.c_int64),
+                ("weight", ctypes.c_void_p), ("residual", ctypes.c_void_p), ("ldr", ctypes.c_int64),
+                ("dx", ctypes.c_void_p), ("lddx", ctypes.c_int64), ("grad_weight", ctypes.c_void_p)]
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("batch", ctypes.c_int64), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class AttentionInputs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "nq", "nk", "heads", "kv_heads", "head_dim", "dtype", "causal", "bias_range")] + \
+               [("scale", ctypes.c_double), ("cap", ctypes.c_double), ("q", Heads), ("k", Heads), ("v", Heads)] + \
+               [(n, ctypes.c_void_p) for n in ("q_len", "k_len", "prefix", "q_doc", "k_doc", "bias")]
+
+
+class AttentionFwdArgs(ctypes.Structure):
+    _fields_ = [("in_", AttentionInputs), ("o", Heads), ("stats", ctypes.c_void_p)]
+
+
+class AttentionBwdArgs(ctypes.Structure):
+    _fields_ = [("in_", AttentionInputs), ("dout", Heads), ("o", Heads), ("stats", ctypes.c_void_p),
+                ("dq", Heads), ("dk", Heads), ("dv", Heads), ("grad_bias", ctypes.c_void_p)]
+
+
 @dataclasses.dataclass
 class Rule:
     """Update rule besides Adam (xpipe_rule_hparams)."""
@@ -171,6 +205,15 @@ _SIGS = {
     "xpipe_embedding_fwd": [_P, _P, _I64, _I32, _I32, ctypes.c_double, _I32, _P, _P],
     "xpipe_embedding_bwd_query": [_I64, _I32, _I32, ctypes.POINTER(_SZ)],
     "xpipe_embedding_bwd": [_P, _P, _I64, _I32, _I32, ctypes.c_double, _I32, _P, _P, _SZ, _P],
+    "xpipe_rmsnorm_fwd": [_P, _P],
+    "xpipe_rmsnorm_bwd_query": [_P, ctypes.POINTER(_SZ)],
+    "xpipe_rmsnorm_bwd": [_P, _P, _SZ, _P],
+    "xpipe_relbias_fwd": [_P, _I32, _I32, _I32, _I32, _P, _P],
+    "xpipe_relbias_bwd": [_P, _I32, _I32, _I32, _I32, _P, _P],
+    "xpipe_attention_fwd_query": [_P, ctypes.POINTER(_SZ)],
+    "xpipe_attention_bwd_query": [_P, ctypes.POINTER(_SZ)],
+    "xpipe_attention_fwd": [_P, _P, _SZ, _P],
+    "xpipe_attention_bwd": [_P, _P, _SZ, _P],
     "xpipe_probe_copy": [_P, _P, _I64, _P],
     "xpipe_probe_mfma": [_P, _I32, _I32, _P],
     "xpipe_probe_graph": [_P, _I32, _I32, _I32, _I32, ctypes.POINTER(ctypes.c_double), _P],
@@ -808,3 +851,192 @@ def xpipe_clip_coef(sumsq, max_norm: float, norm_coef, stream=None):
         raise ValueError("sumsq: contiguous float64 expected")
     _check_norm_coef(norm_coef, dev)
     _check(L.xpipe_clip_coef(sumsq.data_ptr(), sumsq.numel(), max_norm, norm_coef.data_ptr(), _raw_stream(dev, stream)))
+
+
+_RMS_FWD_FORMAT, _RMS_BWD_FORMAT = struct.Struct("qiidPqPqPPqPq"), struct.Struct("qiidPqPqPPqPqP")
+assert _RMS_FWD_FORMAT.size == ctypes.sizeof(RmsnormFwdArgs) and _RMS_BWD_FORMAT.size == ctypes.sizeof(RmsnormBwdArgs)
+
+
+def xpipe_rmsnorm_fwd(x, weight, y, eps: float = 1e-6, residual=None, sum=None, stream=None):
+    """h = x + residual; y = h / sqrt(mean(h^2) + eps) * weight; sum (optional)
+    receives h.  Matrices [rows, dim] of one type, their rows contiguous; weight
+    float32.  y and sum may each be x or residual itself."""
+    L = lib()
+    dev, here = _device_of(x)
+    if not here:
+        with _torch.cuda.device(dev):
+            return xpipe_rmsnorm_fwd(x, weight, y, eps, residual, sum, stream)
+    if x.dim() != 2:
+        raise ValueError("x [rows, dim] expected")
+    (rows, dim), dt = x.shape, x.dtype
+    a = _RMS_FWD_FORMAT.pack(rows, dim, _dtype_of(x), eps, *_matrix("x", x, dt, dev, rows, dim),
+                             *_matrix("residual", residual, dt, dev, rows, dim), _vector("weight", weight, dev, dim),
+                             *_matrix("sum", sum, dt, dev, rows, dim), *_matrix("y", y, dt, dev, rows, dim))
+    _check(L.xpipe_rmsnorm_fwd(a, _raw_stream(dev, stream)))
+
+
+def xpipe_rmsnorm_bwd(dy, h, weight, dx=None, grad_weight=None, eps: float = 1e-6, residual=None, workspace=None, stream=None):
+    """Gradients of the norm from dy and h (the forward's sum): dx, plus residual (a
+    gradient that reaches h another way), and grad_weight (float32, added to), each
+    optional.  dx may be dy, h or residual itself."""
+    L = lib()
+    dev, here = _device_of(dy)
+    if not here:
+        with _torch.cuda.device(dev):
+            return xpipe_rmsnorm_bwd(dy, h, weight, dx, grad_weight, eps, residual, workspace, stream)
+    if dy.dim() != 2:
+        raise ValueError("dy [rows, dim] expected")
+    (rows, dim), dt = dy.shape, dy.dtype
+    a = _RMS_BWD_FORMAT.pack(rows, dim, _dtype_of(dy), eps, *_matrix("dy", dy, dt, dev, rows, dim), *_matrix("h", h, dt, dev, rows, dim),
+                             _vector("weight", weight, dev, dim), *_matrix("residual", residual, dt, dev, rows, dim),
+                             *_matrix("dx", dx, dt, dev, rows, dim), _vector("grad_weight", grad_weight, dev, dim))
+    need = _SZ()
+    _check(L.xpipe_rmsnorm_bwd_query(a, ctypes.byref(need)))
+    ptr, size, keep = _workspace(need.value, workspace, dy, stream)
+    _check(L.xpipe_rmsnorm_bwd(a, ptr, size, _raw_stream(dev, stream)))
+
+
+def _relbias(table, name, values, dev):
+    """(buckets, heads, max_distance) of a [buckets, heads] table and its [heads, 2 max_distance + 1] values."""
+    for t in (table, values):
+        if t.dtype is not _torch.float32 or t.dim() != 2 or not t.is_contiguous() or t.get_device() != dev:
+            raise ValueError("contiguous float32 matrices on one device expected")
+    (buckets, heads), (rows, width) = table.shape, values.shape
+    if rows != heads or width % 2 != 1:
+        raise ValueError(f"{name}: [heads, 2 max_distance + 1] expected")
+    if max(buckets, heads, width) >= 1 << 31:  # (ctypes would cut them to 32 bits)
+        raise ValueError("2^31 rows or columns or more")
+    return buckets, heads, width // 2
+
+
+def xpipe_relbias_fwd(table, bias, bidirectional: bool = True, stream=None):
+    """bias[h, max_distance + d] = table[bucket(d), h] for the distances d (key position
+    less query position) from -max_distance to max_distance, bias's width deciding
+    max_distance.  table [buckets, heads] and bias float32."""
+    L = lib()
+    dev, here = _device_of(table)
+    if not here:
+        with _torch.cuda.device(dev):
+            return xpipe_relbias_fwd(table, bias, bidirectional, stream)
+    buckets, heads, far = _relbias(table, "bias", bias, dev)
+    _check(L.xpipe_relbias_fwd(table.data_ptr(), buckets, heads, far, bool(bidirectional), bias.data_ptr(), _raw_stream(dev, stream)))
+
+
+def xpipe_relbias_bwd(dbias, grad_table, bidirectional: bool = True, stream=None):
+    """grad_table[b, h] += the sum of dbias[h] over the distances of bucket b."""
+    L = lib()
+    dev, here = _device_of(dbias)
+    if not here:
+        with _torch.cuda.device(dev):
+            return xpipe_relbias_bwd(dbias, grad_table, bidirectional, stream)
+    buckets, heads, far = _relbias(grad_table, "dbias", dbias, dev)
+    _check(L.xpipe_relbias_bwd(dbias.data_ptr(), buckets, heads, far, bool(bidirectional), grad_table.data_ptr(), _raw_stream(dev, stream)))
+
+
+_HEADS = "Pqqq"
+_ATTN_IN = "9i4xdd" + 3 * _HEADS + "6P"
+_ATTN_FWD_FORMAT = struct.Struct("@" + _ATTN_IN + _HEADS + "P")
+_ATTN_BWD_FORMAT = struct.Struct("@" + _ATTN_IN + 2 * _HEADS + "P" + 3 * _HEADS + "P")
+assert _ATTN_FWD_FORMAT.size == ctypes.sizeof(AttentionFwdArgs) and _ATTN_BWD_FORMAT.size == ctypes.sizeof(AttentionBwdArgs)
+
+
+def _heads(name, t, dtype, dev, shape):
+    """(pointer, strides of batch, token and head) of a [batch, tokens, heads, dim] tensor, dim contiguous."""
+    if t.dtype is not dtype or t.get_device() != dev:
+        raise ValueError(f"{name}: another type or device")
+    if t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, {tuple(shape)} expected")
+    b, n, h, d = t.stride()
+    if d != 1 and shape[3] > 1:
+        raise ValueError(f"{name}: contiguous in its last dimension expected")
+    return t.data_ptr(), b, n, h
+
+
+def _ints(name, t, dev, shape):
+    if t is None:
+        return 0
+    if t.dtype is not _torch.int32 or t.get_device() != dev or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous int32 {tuple(shape)} on the same device expected")
+    return t.data_ptr()
+
+
+def _floats(name, t, dev, shape):
+    if t is None:
+        return 0
+    if t.dtype is not _torch.float32 or t.get_device() != dev or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous float32 {tuple(shape)} on the same device expected")
+    return t.data_ptr()
+
+
+def _attention_inputs(q, k, v, dev, scale, causal, cap, bias, q_len, k_len, prefix, q_doc, k_doc):
+    """xpipe_attention_inputs as _ATTN_IN's values."""
+    if q.dim() != 4 or k.dim() != 4:
+        raise ValueError("q [batch, nq, heads, dim], k and v [batch, nk, kv_heads, dim] expected")
+    (batch, nq, heads, dim), dt = q.shape, q.dtype
+    nk, kv_heads = k.shape[1], k.shape[2]
+    kv = (batch, nk, kv_heads, dim)
+    reach = 0
+    if bias is not None:
+        if bias.dim() != 2 or bias.shape[1] % 2 != 1:
+            raise ValueError("bias: [heads, 2 range + 1] expected")
+        reach = bias.shape[1] // 2
+    if max(batch, nq, nk, heads, kv_heads, dim, reach) >= 1 << 31:
+        raise ValueError("a size of 2^31 or more")
+    return (batch, nq, nk, heads, kv_heads, dim, _dtype_of(q), bool(causal), reach, dim ** -0.5 if scale is None and dim else scale or 0.0, cap,
+            *_heads("q", q, dt, dev, q.shape), *_heads("k", k, dt, dev, kv), *_heads("v", v, dt, dev, kv),
+            _ints("q_len", q_len, dev, (batch,)), _ints("k_len", k_len, dev, (batch,)), _ints("prefix", prefix, dev, (batch,)),
+            _ints("q_doc", q_doc, dev, (batch, nq)), _ints("k_doc", k_doc, dev, (batch, nk)),
+            0 if bias is None else _floats("bias", bias, dev, (heads, 2 * reach + 1)))
+
+
+def xpipe_attention_fwd(q, k, v, o, scale: Optional[float] = None, causal: bool = False, cap: float = 0.0, bias=None, q_len=None,
+                        k_len=None, prefix=None, q_doc=None, k_doc=None, stats=None, workspace=None, stream=None):
+    """o = softmax(scores) v per head; scores = cap tanh(scale q.k / cap) + bias.
+    q and o [batch, nq, heads, dim], k and v [batch, nk, kv_heads, dim] of one type, contiguous
+    in dim; scale: dim^-0.5 unless given; cap 0: none; bias float32 [heads, 2 range + 1] by
+    distance (key less query position; further ones as the furthest).  q_len, k_len,
+    prefix: int32 [batch]; q_doc, k_doc: int32 documents of the tokens.  The queries are
+    the last q_len of a sequence of k_len tokens.  stats (for the
+    backward): float32 [batch, heads, nq, 2]."""
+    L = lib()
+    dev, here = _device_of(q)
+    if not here:
+        with _torch.cuda.device(dev):
+            return xpipe_attention_fwd(q, k, v, o, scale, causal, cap, bias, q_len, k_len, prefix, q_doc, k_doc, stats, workspace, stream)
+    given = _attention_inputs(q, k, v, dev, scale, causal, cap, bias, q_len, k_len, prefix, q_doc, k_doc)
+    batch, nq, heads, _ = q.shape
+    a = _ATTN_FWD_FORMAT.pack(*given, *_heads("o", o, q.dtype, dev, q.shape),
+                              _floats("stats", stats, dev, (batch, heads, nq, 2)))
+    need = _SZ()
+    _check(L.xpipe_attention_fwd_query(a, ctypes.byref(need)))
+    ptr, size, keep = _workspace(need.value, workspace, q, stream)
+    _check(L.xpipe_attention_fwd(a, ptr, size, _raw_stream(dev, stream)))
+
+
+def xpipe_attention_bwd(dout, q, k, v, o, stats, dq, dk, dv, grad_bias=None, scale: Optional[float] = None, causal: bool = False,
+                        cap: float = 0.0, bias=None, q_len=None, k_len=None, prefix=None, q_doc=None, k_doc=None, workspace=None,
+                        stream=None):
+    """Gradients of attention from dout: dq, dk, dv (written, types and shapes as q, k,
+    v), and grad_bias (float32 like bias, added to).  The forward's other arguments
+    as they were; o and stats are what it wrote."""
+    L = lib()
+    dev, here = _device_of(q)
+    if not here:
+        with _torch.cuda.device(dev):
+            return xpipe_attention_bwd(dout, q, k, v, o, stats, dq, dk, dv, grad_bias, scale, causal, cap, bias, q_len, k_len, prefix, q_doc,
+                                       k_doc, workspace, stream)
+    given = _attention_inputs(q, k, v, dev, scale, causal, cap, bias, q_len, k_len, prefix, q_doc, k_doc)
+    batch, nq, heads, _ = q.shape
+    dt = q.dtype
+    if stats is None:
+        raise ValueError("stats: the forward's expected")
+    if grad_bias is not None and bias is None:
+        raise ValueError("grad_bias without bias")
+    a = _ATTN_BWD_FORMAT.pack(*given, *_heads("dout", dout, dt, dev, q.shape), *_heads("o", o, dt, dev, q.shape),
+                              _floats("stats", stats, dev, (batch, heads, nq, 2)), *_heads("dq", dq, dt, dev, q.shape),
+                              *_heads("dk", dk, dt, dev, k.shape), *_heads("dv", dv, dt, dev, k.shape),
+                              0 if grad_bias is None else _floats("grad_bias", grad_bias, dev, bias.shape))
+    need = _SZ()
+    _check(L.xpipe_attention_bwd_query(a, ctypes.byref(need)))
+    ptr, size, keep = _workspace(need.value, workspace, q, stream)
+    _check(L.xpipe_attention_bwd(a, ptr, size, _raw_stream(dev, stream)))

@@ -14,7 +14,8 @@ INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 OUT = os.path.join(HERE, "libxpipe.so")
 BUILD = os.path.join(HERE, "_build")
 SOURCES = ["k_optim.hip", "k_gemm.hip", "k_conv.hip", "k_wgrad.hip", "k_image.hip", "k_elem.hip",
-           "k_linear.hip", "k_embed.hip", "k_norm.hip", "stage.cpp", "operators.cpp"]
+           "k_linear.hip", "k_embed.hip", "k_norm.hip", "k_rmsnorm.hip", "k_relbias.hip", "k_attn.hip",
+           "stage.cpp", "operators.cpp", "attention.cpp"]
 ARCH = "gfx950"
 
 

@@ -1,0 +1,104 @@
+// The learned relative position bias: a table of one value per bucket and head,
+// spread over distances (key position - query position) for attention to read,
+// and its gradient.
+//
+// A distance a >= 0 lies in one of n buckets: below n / 2 each has its own, beyond
+// they grow with the logarithm, bucket n / 2 + floor(log(2 a / n) / log(2 far / n) (n - n / 2)),
+// the last one from there on.  In fp64; a distance on a border belongs to the bucket that
+// starts there (the quotient is raised by 1e-10, which is less than the least that whole
+// distances up to 2^20 miss a border by).
+#include "xp_device.h"
+#include "xp_kernels.h"
+
+namespace xp {
+
+namespace {
+
+struct Buckets {
+  int n, half;      // of one direction; those of single distances
+  double scale;     // (n - half) / log(far / half)
+  int both, far;
+};
+
+XP_DEV int bucket_of(const Buckets& b, int away) {
+  if (away < b.half) return away;
+  const int k = (int)(log((double)away / b.half) * b.scale + 1e-10);
+  return min(b.n - 1, b.half + k);
+}
+XP_DEV int bucket_at(const Buckets& b, int d) {  // d: key position - query position
+  if (!b.both) return bucket_of(b, max(-d, 0));
+  return d > 0 ? b.n + bucket_of(b, d) : bucket_of(b, -d);
+}
+
+// A thread takes one distance and up to 16 heads: the logarithm costs more than the heads'
+// values do.
+constexpr int HEADS_PER = 16;
+
+__global__ __launch_bounds__(256) void k_relbias_fwd(const float* __restrict__ table, Buckets b, int heads, float* __restrict__ bias) {
+  const int x = blockIdx.x * 256 + threadIdx.x, width = 2 * b.far + 1;
+  if (x >= width) return;
+  const float* row = table + (int64_t)bucket_at(b, x - b.far) * heads;
+  const int h0 = blockIdx.y * HEADS_PER, h1 = min(heads, h0 + HEADS_PER);
+  for (int h = h0; h < h1; ++h) bias[(int64_t)h * width + x] = row[h];
+}
+
+// the first distance 0 .. far in bucket k or a later one; far + 1 if none
+XP_DEV int first_of(const Buckets& b, int k) {
+  int lo = 0, hi = b.far + 1;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (bucket_of(b, mid) >= k) hi = mid;
+    else lo = mid + 1;
+  }
+  return lo;
+}
+
+// One workgroup per bucket and head: the bucket's distances are one run of the head's row.
+__global__ __launch_bounds__(256) void k_relbias_bwd(const float* __restrict__ dbias, Buckets b, int heads, float* __restrict__ grad) {
+  __shared__ double sh[4];
+  const int k = blockIdx.x, h = blockIdx.y, side = b.both && k >= b.n, kk = side ? k - b.n : k;
+  const float* row = dbias + (int64_t)h * (2 * b.far + 1) + b.far;
+  const int lo = first_of(b, kk), hi = first_of(b, kk + 1);  // distances [lo, hi)
+  double s = 0.0;
+  if (side) {
+    for (int d = max(lo, 1) + (int)threadIdx.x; d < hi; d += 256) s += row[d];
+  } else {
+    for (int d = lo + (int)threadIdx.x; d < hi; d += 256) s += row[-d];
+    if (!b.both && kk == 0)  // keys behind the query count as distance 0
+      for (int d = 1 + threadIdx.x; d <= b.far; d += 256) s += row[d];
+  }
+  s = wave_sum(s);
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    float* g = grad + (int64_t)k * heads + h;
+    *g = (float)((double)*g + ((sh[0] + sh[1]) + (sh[2] + sh[3])));
+  }
+}
+
+Buckets describe(const RelBiasArgs& a) {
+  Buckets b{};
+  b.both = a.both;
+  b.n = a.both ? a.buckets / 2 : a.buckets;
+  b.half = b.n / 2;
+  b.far = a.far;
+  b.scale = (b.n - b.half) / log((double)a.far / b.half);
+  return b;
+}
+
+}  // namespace
+
+hipError_t launch_relbias_fwd(const RelBiasArgs& a, hipStream_t s) {
+  const int width = 2 * a.far + 1;
+  XP_LAUNCH("k_relbias_fwd", 4.0 * width * a.heads, k_relbias_fwd, dim3((width + 255) / 256, (a.heads + HEADS_PER - 1) / HEADS_PER),
+            dim3(256), 0, s, a.table, describe(a), a.heads, a.bias);
+  return hipGetLastError();
+}
+
+hipError_t launch_relbias_bwd(const RelBiasArgs& a, hipStream_t s) {
+  XP_LAUNCH("k_relbias_bwd", 4.0 * (2 * a.far + 1) * a.heads, k_relbias_bwd, dim3(a.buckets, a.heads), dim3(256), 0, s, a.dbias,
+            describe(a), a.heads, a.grad);
+  return hipGetLastError();
+}
+
+}  // namespace xp

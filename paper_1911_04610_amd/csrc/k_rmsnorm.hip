@@ -1,0 +1,302 @@
+// Root-mean-square norm of a token network's rows with the skip connection's
+// addition in front, and its gradients.
+//
+//   forward:  h = x + residual;  n = 1 / sqrt(mean(h^2) + eps);  y = h n w
+//   backward: g = dy w;  dx = n (g - h n^2 mean(g h)) + residual;  grad_w += sum over rows of dy h n
+//
+// Bandwidth-bound: a row is read once and held in the registers of the G threads
+// that share it (E elements each), the sums go over those threads.  Sums over a
+// row are fp64 (squares of fp32 values neither overflow nor lose bits there), the
+// rest is fp32, each stored value is rounded once.
+#include "xp_device.h"
+#include "xp_lds.h"
+#include "xp_kernels.h"
+
+#include <algorithm>
+
+namespace xp {
+
+namespace {
+
+template <typename T> constexpr int CHUNK = 16 / (int)sizeof(T);
+
+// n elements (more than CHUNK: a whole chunk) from p on, which may start anywhere; zeros behind them
+template <typename T>
+XP_DEV void ld_elems(const T* p, int n, float* v) {
+  if (n >= CHUNK<T>) {
+    u32x4_t u;
+    __builtin_memcpy(&u, p, 16);
+#pragma unroll
+    for (int i = 0; i < CHUNK<T>; ++i) {
+      if constexpr (sizeof(T) == 4) v[i] = __uint_as_float(u[i]);
+      else v[i] = __uint_as_float(i & 1 ? u[i / 2] & 0xffff0000u : u[i / 2] << 16);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < CHUNK<T>; ++i) v[i] = i < n ? (float)ldd(p + i) : 0.f;
+  }
+}
+template <typename T>
+XP_DEV void st_elems(T* p, int n, const float* v) {
+  if (n >= CHUNK<T>) {
+    u32x4_t u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 4) u[i] = __float_as_uint(v[i]);
+      else u[i] = f32x2_to_bf16x2(v[2 * i], v[2 * i + 1]);
+    }
+    __builtin_memcpy(p, &u, 16);
+  } else {
+#pragma unroll
+    for (int i = 0; i < CHUNK<T>; ++i)
+      if (i < n) std_(p + i, (double)v[i]);
+  }
+}
+
+// Threads of a workgroup, and the rows that they hold at a time.
+template <int G> constexpr int THREADS = G < 256 ? 256 : G;
+template <int G> constexpr int ROWS = THREADS<G> / G;
+
+// Sums of N values over a row's G threads, in all of them.  sh: two sets of N x 16
+// doubles, used in turn (so that one barrier a row is enough).
+template <int G, int N>
+XP_DEV void row_sums(double (&v)[N], double (*sh)[16], int turn) {
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int off = (G < 64 ? G : 64) / 2; off > 0; off >>= 1) v[i] += __shfl_xor(v[i], off, 64);
+  if constexpr (G > 64) {
+    double(*s)[16] = sh + turn * N;
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+      for (int i = 0; i < N; ++i) s[i][threadIdx.x >> 6] = v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      v[i] = 0.0;
+      for (int w = 0; w < G / 64; ++w) v[i] += s[i][w];
+    }
+  }
+}
+
+// No __restrict__: sum and y may be x's or residual's buffer (every element is read
+// by the thread that writes it, before).
+template <typename T, int G, int E>
+__global__ __launch_bounds__(THREADS<G>) void k_rms_fwd(RmsArgs a) {
+  constexpr int C = CHUNK<T>, V = E / C;
+  __shared__ double sh[2][16];
+  const int lt = threadIdx.x % G;
+  float w[E];
+#pragma unroll
+  for (int j = 0; j < V; ++j) ld_elems(a.w + (lt + j * G) * C, min(4, a.dim - (lt + j * G) * C), w + j * C);
+  if constexpr (C == 8)
+#pragma unroll
+    for (int j = 0; j < V; ++j) ld_elems(a.w + (lt + j * G) * C + 4, min(4, a.dim - (lt + j * G) * C - 4), w + j * C + 4);
+  int turn = 0;
+  // (workgroup-uniform where the sums need a barrier: ROWS is 1 there)
+  for (int64_t row = (int64_t)blockIdx.x * ROWS<G> + threadIdx.x / G; row < a.rows; row += (int64_t)gridDim.x * ROWS<G>) {
+    float h[E];
+    double ss[1] = {0.0};
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const int at = (lt + j * G) * C;
+      ld_elems((const T*)a.x + row * a.ldx + at, a.dim - at, h + j * C);
+    }
+    if (a.res) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const int at = (lt + j * G) * C;
+        float r[C];
+        ld_elems((const T*)a.res + row * a.ldr + at, a.dim - at, r);
+#pragma unroll
+        for (int i = 0; i < C; ++i) h[j * C + i] += r[i];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < E; ++i) ss[0] += (double)h[i] * h[i];
+    row_sums<G, 1>(ss, sh, turn);
+    turn ^= 1;
+    const float n = (float)(1.0 / sqrt(ss[0] / a.dim + a.eps));
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const int at = (lt + j * G) * C;
+      if (a.out) st_elems((T*)a.out + row * a.ldo + at, a.dim - at, h + j * C);
+      float y[C];
+#pragma unroll
+      for (int i = 0; i < C; ++i) y[i] = h[j * C + i] * n * w[j * C + i];
+      st_elems((T*)a.y + row * a.ldy + at, a.dim - at, y);
+    }
+  }
+}
+
+// One workgroup's rows: their dx, and its part of grad_w: the sum of its rows' terms in
+// fp32 (at most a few hundred of them), over the ROWS rows at a time in LDS.  The parts
+// are added in fp64 by k_rms_join; a single workgroup adds its own.
+template <typename T, int G, int E>
+__global__ __launch_bounds__(THREADS<G>) void k_rms_bwd(RmsArgs a) {
+  constexpr int C = CHUNK<T>, V = E / C;
+  __shared__ double sh[4][16];
+  __shared__ float gsum[ROWS<G> > 1 ? G * E * ROWS<G> : 1];
+  const int lt = threadIdx.x % G;
+  float acc[E];
+#pragma unroll
+  for (int i = 0; i < E; ++i) acc[i] = 0.f;
+  int turn = 0;
+  for (int64_t row = (int64_t)blockIdx.x * ROWS<G> + threadIdx.x / G; row < a.rows; row += (int64_t)gridDim.x * ROWS<G>) {
+    float h[E], dy[E];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const int at = (lt + j * G) * C;
+      ld_elems((const T*)a.x + row * a.ldx + at, a.dim - at, h + j * C);
+      ld_elems((const T*)a.dy + row * a.lddy + at, a.dim - at, dy + j * C);
+    }
+    double s[2] = {0.0, 0.0};
+    auto weight = [&](int j, float* w) __attribute__((always_inline)) {
+      const int at = (lt + j * G) * C;
+#pragma unroll
+      for (int p = 0; p < C; p += 4) ld_elems(a.w + at + p, min(4, a.dim - at - p), w + p);
+    };
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      float w[C];
+      weight(j, w);
+#pragma unroll
+      for (int i = 0; i < C; ++i) {
+        const int e = j * C + i;
+        s[0] += (double)h[e] * h[e];
+        s[1] += (double)(dy[e] * w[i]) * h[e];
+      }
+    }
+    row_sums<G, 2>(s, sh, turn);
+    turn ^= 1;
+    const double nd = 1.0 / sqrt(s[0] / a.dim + a.eps);
+    const float n = (float)nd, c = (float)(nd * nd * s[1] / a.dim);
+#pragma unroll
+    for (int i = 0; i < E; ++i) acc[i] += dy[i] * (h[i] * n);
+    if (a.y) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const int at = (lt + j * G) * C;
+        float w[C], r[C], dx[C];
+        weight(j, w);
+        if (a.res) ld_elems((const T*)a.res + row * a.ldr + at, a.dim - at, r);
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+          dx[i] = n * (dy[j * C + i] * w[i] - h[j * C + i] * c);
+          if (a.res) dx[i] += r[i];
+        }
+        st_elems((T*)a.y + row * a.ldy + at, a.dim - at, dx);
+      }
+    }
+  }
+  if (!a.grad) return;
+  if constexpr (ROWS<G> > 1) {
+    const int grp = threadIdx.x / G;
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+#pragma unroll
+      for (int i = 0; i < C; ++i) gsum[grp * (G * E) + (lt + j * G) * C + i] = acc[j * C + i];
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.dim; c += THREADS<G>) {
+      float t = 0.f;
+      for (int r = 0; r < ROWS<G>; ++r) t += gsum[r * (G * E) + c];
+      if (gridDim.x == 1) a.grad[c] += t;
+      else a.part[(int64_t)blockIdx.x * a.dim + c] = t;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+#pragma unroll
+      for (int i = 0; i < C; ++i) {
+        const int c = (lt + j * G) * C + i;
+        if (c < a.dim) {
+          if (gridDim.x == 1) a.grad[c] += acc[j * C + i];
+          else a.part[(int64_t)blockIdx.x * a.dim + c] = acc[j * C + i];
+        }
+      }
+  }
+}
+
+// grad[c] += sum of n parts, 16 columns and 16 runs of parts a workgroup
+__global__ __launch_bounds__(256) void k_rms_join(const float* __restrict__ part, int n, int dim, float* __restrict__ grad) {
+  __shared__ double sh[16][17];
+  const int c = threadIdx.x & 15, r = threadIdx.x >> 4;
+  const int col = blockIdx.x * 16 + c;
+  double s = 0.0;
+  if (col < dim) {
+#pragma unroll 8
+    for (int i = r; i < n; i += 16) s += (double)part[(int64_t)i * dim + col];
+  }
+  sh[r][c] = s;
+  __syncthreads();
+  if (r == 0 && col < dim) {
+    s = 0.0;
+    for (int i = 0; i < 16; ++i) s += sh[i][c];
+    grad[col] = (float)((double)grad[col] + s);
+  }
+}
+
+// calls f(threads a row, elements a thread) for rows of dim elements
+template <typename F>
+void by_size(int dim, F&& f) {
+  using std::integral_constant;
+  if (dim <= 64) f(integral_constant<int, 8>{}, integral_constant<int, 8>{});
+  else if (dim <= 512) f(integral_constant<int, 64>{}, integral_constant<int, 8>{});
+  else if (dim <= 1024) f(integral_constant<int, 64>{}, integral_constant<int, 16>{});
+  else if (dim <= 2048) f(integral_constant<int, 64>{}, integral_constant<int, 32>{});
+  else if (dim <= 4096) f(integral_constant<int, 256>{}, integral_constant<int, 16>{});
+  else if (dim <= 8192) f(integral_constant<int, 256>{}, integral_constant<int, 32>{});
+  else if (dim <= 16384) f(integral_constant<int, 1024>{}, integral_constant<int, 16>{});
+  else f(integral_constant<int, 1024>{}, integral_constant<int, 32>{});
+}
+
+template <int G>
+int bwd_blocks(int64_t rows) { return (int)std::min<int64_t>((rows + ROWS<G> - 1) / ROWS<G>, G >= 1024 ? 256 : 512); }
+
+template <typename T>
+hipError_t fwd(const RmsArgs& a, hipStream_t s) {
+  by_size(a.dim, [&](auto G, auto E) {
+    constexpr int g = decltype(G)::value, e = decltype(E)::value;
+    const int blocks = (int)std::min<int64_t>((a.rows + ROWS<g> - 1) / ROWS<g>, g >= 1024 ? 512 : 2048);
+    const double bytes = (double)sizeof(T) * a.rows * a.dim * (2 + (a.res != nullptr) + (a.out != nullptr));
+    XP_LAUNCH(sizeof(T) == 2 ? "k_rms_fwd<bf16>" : "k_rms_fwd<f32>", bytes, (k_rms_fwd<T, g, e>), dim3(blocks),
+              dim3(THREADS<g>), 0, s, a);
+  });
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t bwd(RmsArgs a, void* workspace, hipStream_t s) {
+  a.part = (float*)workspace;
+  by_size(a.dim, [&](auto G, auto E) {
+    constexpr int g = decltype(G)::value, e = decltype(E)::value;
+    const int blocks = bwd_blocks<g>(a.rows);
+    const double bytes = (double)sizeof(T) * a.rows * a.dim * (2 + (a.y != nullptr) + (a.res != nullptr));
+    XP_LAUNCH(sizeof(T) == 2 ? "k_rms_bwd<bf16>" : "k_rms_bwd<f32>", bytes, (k_rms_bwd<T, g, e>), dim3(blocks),
+              dim3(THREADS<g>), 0, s, a);
+    if (a.grad && blocks > 1)
+      XP_LAUNCH("k_rms_join", 4.0 * blocks * a.dim, k_rms_join, dim3((a.dim + 15) / 16), dim3(256), 0, s, a.part, blocks, a.dim, a.grad);
+  });
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rms_fwd(int dtype, const RmsArgs& a, hipStream_t s) {
+  return dtype == DT_BF16 ? fwd<bf16_t>(a, s) : fwd<float>(a, s);
+}
+
+size_t rms_bwd_bytes(int64_t rows, int dim) {
+  size_t n = 0;
+  by_size(dim, [&](auto G, auto) {
+    const int blocks = bwd_blocks<decltype(G)::value>(rows);
+    n = blocks > 1 ? (size_t)blocks * dim * sizeof(float) : 0;
+  });
+  return n;
+}
+
+hipError_t launch_rms_bwd(int dtype, const RmsArgs& a, void* workspace, hipStream_t s) {
+  return dtype == DT_BF16 ? bwd<bf16_t>(a, workspace, s) : bwd<float>(a, workspace, s);
+}
+
+}  // namespace xp

@@ -10,11 +10,6 @@ using namespace xp;
 
 namespace {
 
-bool known_dtype(int32_t d) { return d == XPIPE_F32 || d == XPIPE_BF16; }
-int esize(int32_t dtype) { return dtype == XPIPE_BF16 ? 2 : 4; }
-
-bool at_multiple(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
-
 // a matrix argument: present, aligned to its element, rows at least as far apart as long
 xpipe_status check_matrix(const char* name, const void* p, int64_t ld, int64_t cols, int es) {
   if (!p) return fail(XPIPE_EINVAL, std::string("null ") + name);
@@ -32,20 +27,6 @@ xpipe_status check_sizes(int64_t rows, int32_t cin, int32_t cout, int32_t dtype,
   // (a launch's tiles are counted in 32 bits)
   if (rows >= (int64_t)1 << 30 || rows / 64 * (std::max(cin, cout) / 64) >= (int64_t)1 << 30)
     return fail(XPIPE_EUNSUPPORTED, "2^30 rows or 2^42 results or more");
-  return XPIPE_OK;
-}
-
-#define XP_TRY(call)                        \
-  do {                                      \
-    xpipe_status r_ = (call);               \
-    if (r_ != XPIPE_OK) return r_;          \
-  } while (0)
-
-xpipe_status check_workspace(const void* ws, size_t bytes, size_t need) {
-  if (need == 0) return XPIPE_OK;
-  if (!ws) return fail(XPIPE_EINVAL, "null workspace");
-  if (bytes < need) return fail(XPIPE_EINVAL, "workspace too small");
-  if (!at_multiple(ws, 256)) return fail(XPIPE_EINVAL, "workspace must be 256-byte aligned");
   return XPIPE_OK;
 }
 
@@ -176,6 +157,95 @@ xpipe_status check_tensors(const xpipe_tensor* t, int32_t n, int64_t* blocks) {
     units += (t[i].n + NORM_SMALL_PER - 1) / NORM_SMALL_PER;
   }
   *blocks = units <= NORM_SMALL_UNITS ? 0 : b;
+  return XPIPE_OK;
+}
+
+// a norm's rows; `rows` = 0 leaves the matrices unchecked
+xpipe_status check_rms(int64_t rows, int32_t dim, int32_t dtype, double eps, const float* weight) {
+  if (rows < 0 || dim < 1) return fail(XPIPE_EINVAL, "rows must be >= 0, dim >= 1");
+  if (!known_dtype(dtype)) return fail(XPIPE_EINVAL, "unknown dtype");
+  if (!(eps > 0) || !std::isfinite(eps)) return fail(XPIPE_EINVAL, "eps must be > 0 and finite");
+  if (dim > RMS_MAX_DIM || rows >= (int64_t)1 << 40) return fail(XPIPE_EUNSUPPORTED, "more than 32768 columns, or 2^40 rows or more");
+  if (rows == 0) return XPIPE_OK;
+  if (!weight) return fail(XPIPE_EINVAL, "null weight");
+  if (!at_multiple(weight, 4)) return fail(XPIPE_EINVAL, "weight is not aligned to its element");
+  return XPIPE_OK;
+}
+
+// an output that may be an input's buffer, rows alike
+bool same_rows(const void* p, int64_t ld, const void* q, int64_t ldq) { return p != q || ld == ldq; }
+
+xpipe_status rms_fwd_args(const xpipe_rmsnorm_fwd_args* q, RmsArgs* a) {
+  if (!q) return fail(XPIPE_EINVAL, "null arguments");
+  XP_TRY(check_rms(q->rows, q->dim, q->dtype, q->eps, q->weight));
+  *a = RmsArgs{};
+  if (q->rows == 0) return XPIPE_OK;
+  const int es = esize(q->dtype);
+  XP_TRY(check_matrix("x", q->x, q->ldx, q->dim, es));
+  XP_TRY(check_matrix("y", q->y, q->ldy, q->dim, es));
+  if (q->residual) XP_TRY(check_matrix("residual", q->residual, q->ldr, q->dim, es));
+  if (q->sum) XP_TRY(check_matrix("sum", q->sum, q->lds, q->dim, es));
+  if (q->y == q->sum || q->y == (const void*)q->weight || q->sum == (const void*)q->weight)
+    return fail(XPIPE_EINVAL, "an output is the weight's or the other output's buffer");
+  if (!same_rows(q->y, q->ldy, q->x, q->ldx) || !same_rows(q->y, q->ldy, q->residual, q->ldr) ||
+      (q->sum && (!same_rows(q->sum, q->lds, q->x, q->ldx) || !same_rows(q->sum, q->lds, q->residual, q->ldr))))
+    return fail(XPIPE_EINVAL, "an output in an input's buffer with another ld");
+  a->rows = q->rows;
+  a->dim = q->dim;
+  a->eps = q->eps;
+  a->w = q->weight;
+  a->x = q->x;
+  a->ldx = q->ldx;
+  a->res = q->residual;
+  a->ldr = q->ldr;
+  a->out = q->sum;
+  a->ldo = q->lds;
+  a->y = q->y;
+  a->ldy = q->ldy;
+  return XPIPE_OK;
+}
+
+xpipe_status rms_bwd_args(const xpipe_rmsnorm_bwd_args* q, RmsArgs* a) {
+  if (!q) return fail(XPIPE_EINVAL, "null arguments");
+  XP_TRY(check_rms(q->rows, q->dim, q->dtype, q->eps, q->weight));
+  *a = RmsArgs{};
+  if (q->rows == 0 || (!q->dx && !q->grad_weight)) return XPIPE_OK;
+  const int es = esize(q->dtype);
+  XP_TRY(check_matrix("dy", q->dy, q->lddy, q->dim, es));
+  XP_TRY(check_matrix("h", q->h, q->ldh, q->dim, es));
+  if (q->residual) XP_TRY(check_matrix("residual", q->residual, q->ldr, q->dim, es));
+  if (q->dx) XP_TRY(check_matrix("dx", q->dx, q->lddx, q->dim, es));
+  if (!at_multiple(q->grad_weight, 4)) return fail(XPIPE_EINVAL, "grad_weight is not aligned to its element");
+  if (q->dx && (q->dx == (const void*)q->weight || !same_rows(q->dx, q->lddx, q->dy, q->lddy) ||
+                !same_rows(q->dx, q->lddx, q->h, q->ldh) || !same_rows(q->dx, q->lddx, q->residual, q->ldr)))
+    return fail(XPIPE_EINVAL, "dx is the weight's buffer, or an input's with another ld");
+  const void* g = q->grad_weight;
+  if (g && (g == q->dy || g == q->h || g == q->residual || g == q->dx || g == (const void*)q->weight))
+    return fail(XPIPE_EINVAL, "grad_weight is another argument's buffer");
+  a->rows = q->rows;
+  a->dim = q->dim;
+  a->eps = q->eps;
+  a->w = q->weight;
+  a->dy = q->dy;
+  a->lddy = q->lddy;
+  a->x = q->h;
+  a->ldx = q->ldh;
+  a->res = q->residual;
+  a->ldr = q->ldr;
+  a->y = q->dx;
+  a->ldy = q->lddx;
+  a->grad = q->grad_weight;
+  return XPIPE_OK;
+}
+
+xpipe_status check_relbias(int32_t buckets, int32_t heads, int32_t max_distance, int32_t bidirectional) {
+  if (heads < 1) return fail(XPIPE_EINVAL, "heads must be >= 1");
+  if (bidirectional && buckets % 2 != 0) return fail(XPIPE_EINVAL, "buckets of two directions must be even");
+  const int32_t n = bidirectional ? buckets / 2 : buckets;
+  if (n < 2) return fail(XPIPE_EINVAL, "at least 2 buckets in each direction");
+  if (max_distance <= n / 2) return fail(XPIPE_EINVAL, "max_distance must exceed half of a direction's buckets");
+  if (buckets > 1024 || heads > 4096 || max_distance > 1 << 20)
+    return fail(XPIPE_EUNSUPPORTED, "more than 1024 buckets, 4096 heads or a distance of 2^20");
   return XPIPE_OK;
 }
 
@@ -359,6 +429,65 @@ xpipe_status xpipe_embedding_bwd(const void* dy, const int32_t* tokens, int64_t 
   a.dy = dy;
   a.grad = grad;
   XP_HIP(launch_embed_bwd(dtype, a, workspace, (hipStream_t)hip_stream));
+  return XPIPE_OK;
+}
+
+xpipe_status xpipe_rmsnorm_fwd(const xpipe_rmsnorm_fwd_args* args, void* hip_stream) {
+  RmsArgs a;
+  XP_TRY(rms_fwd_args(args, &a));
+  if (a.rows == 0) return XPIPE_OK;
+  XP_HIP(launch_rms_fwd(args->dtype, a, (hipStream_t)hip_stream));
+  return XPIPE_OK;
+}
+
+xpipe_status xpipe_rmsnorm_bwd_query(const xpipe_rmsnorm_bwd_args* args, size_t* workspace_bytes) {
+  if (!workspace_bytes) return fail(XPIPE_EINVAL, "null output");
+  RmsArgs a;
+  XP_TRY(rms_bwd_args(args, &a));
+  *workspace_bytes = a.rows > 0 && a.grad ? rms_bwd_bytes(a.rows, a.dim) : 0;
+  return XPIPE_OK;
+}
+
+xpipe_status xpipe_rmsnorm_bwd(const xpipe_rmsnorm_bwd_args* args, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  RmsArgs a;
+  XP_TRY(rms_bwd_args(args, &a));
+  if (a.rows == 0) return XPIPE_OK;
+  XP_TRY(check_workspace(workspace, workspace_bytes, a.grad ? rms_bwd_bytes(a.rows, a.dim) : 0));
+  XP_HIP(launch_rms_bwd(args->dtype, a, workspace, (hipStream_t)hip_stream));
+  return XPIPE_OK;
+}
+
+xpipe_status xpipe_relbias_fwd(const float* table, int32_t buckets, int32_t heads, int32_t max_distance, int32_t bidirectional,
+                               float* bias, void* hip_stream) {
+  XP_TRY(check_relbias(buckets, heads, max_distance, bidirectional));
+  if (!table || !bias) return fail(XPIPE_EINVAL, "null buffer");
+  if (!at_multiple(table, 4) || !at_multiple(bias, 4)) return fail(XPIPE_EINVAL, "a buffer is not aligned to its element");
+  if (table == bias) return fail(XPIPE_EINVAL, "bias is the table's buffer");
+  RelBiasArgs a{};
+  a.buckets = buckets;
+  a.heads = heads;
+  a.far = max_distance;
+  a.both = bidirectional != 0;
+  a.table = table;
+  a.bias = bias;
+  XP_HIP(launch_relbias_fwd(a, (hipStream_t)hip_stream));
+  return XPIPE_OK;
+}
+
+xpipe_status xpipe_relbias_bwd(const float* dbias, int32_t buckets, int32_t heads, int32_t max_distance, int32_t bidirectional,
+                               float* grad_table, void* hip_stream) {
+  XP_TRY(check_relbias(buckets, heads, max_distance, bidirectional));
+  if (!dbias || !grad_table) return fail(XPIPE_EINVAL, "null buffer");
+  if (!at_multiple(dbias, 4) || !at_multiple(grad_table, 4)) return fail(XPIPE_EINVAL, "a buffer is not aligned to its element");
+  if (dbias == grad_table) return fail(XPIPE_EINVAL, "grad_table is dbias's buffer");
+  RelBiasArgs a{};
+  a.buckets = buckets;
+  a.heads = heads;
+  a.far = max_distance;
+  a.both = bidirectional != 0;
+  a.dbias = dbias;
+  a.grad = grad_table;
+  XP_HIP(launch_relbias_bwd(a, (hipStream_t)hip_stream));
   return XPIPE_OK;
 }
 

@@ -386,6 +386,67 @@ hipError_t launch_grad_norm_small(int dtype, const NormArgs& a, int units, doubl
 hipError_t launch_grad_sumsq(int dtype, const NormArgs& a, int blocks, hipStream_t s);
 hipError_t launch_clip_coef(const double* part, int64_t n, double max_norm, double* sumsq, float* out, hipStream_t s);
 
+// ---------------------------------------------------------------- RMS norm
+// Rows of dim elements in the storage dtype, ld.. elements apart; sums as k_rmsnorm.hip says.
+constexpr int RMS_MAX_DIM = 32768;
+struct RmsArgs {
+  int64_t rows;
+  int dim;
+  double eps;
+  const float* w;
+  const void* x; int64_t ldx;        // forward: x; backward: h
+  const void* dy; int64_t lddy;      // backward
+  const void* res; int64_t ldr;      // optional: added to x, or to dx
+  void* out; int64_t ldo;            // forward, optional: x + res
+  void* y; int64_t ldy;              // y; backward: dx (optional)
+  float* grad;                       // backward, optional: added to
+  float* part;                       // set by the launcher
+};
+hipError_t launch_rms_fwd(int dtype, const RmsArgs& a, hipStream_t s);
+size_t rms_bwd_bytes(int64_t rows, int dim);
+hipError_t launch_rms_bwd(int dtype, const RmsArgs& a, void* workspace, hipStream_t s);
+
+// ---------------------------------------------------------------- relative position bias
+struct RelBiasArgs {
+  int buckets, heads, far, both;
+  const float* table; float* bias;   // [buckets][heads] -> [heads][2 far + 1]
+  const float* dbias; float* grad;   // [heads][2 far + 1], added to [buckets][heads]
+};
+hipError_t launch_relbias_fwd(const RelBiasArgs& a, hipStream_t s);
+hipError_t launch_relbias_bwd(const RelBiasArgs& a, hipStream_t s);
+
+// ---------------------------------------------------------------- attention
+// k_attn.hip has the formulas.  A matrix is [batch][token][head][dim] in the storage
+// dtype, with these strides in elements (dim's is 1).
+struct AttnMat {
+  const void* p;
+  int64_t b, t, h;
+};
+constexpr int ATTN_MAX_DIM = 128;
+struct AttnArgs {
+  int batch, nq, nk, heads, kv_heads, dim, causal, range;
+  float scale, cap;                  // cap 0: none
+  AttnMat q, k, v;
+  AttnMat o;                         // forward: written; backward: the forward's
+  AttnMat dout, dq, dk, dv;          // backward
+  const int32_t *q_len, *k_len, *prefix;   // [batch], optional
+  const int32_t *q_doc, *k_doc;            // [batch][nq], [batch][nk], both or none
+  const float* bias;                 // [heads][2 range + 1], optional
+  float* grad_bias;                  // backward, optional: added to
+  float* stats;                      // [batch][heads][nq][2]: largest score, sum of exp(score - largest)
+  // set by the launcher: query rows of how many heads a workgroup holds together, parts
+  // of the keys and their results, documents of each tile, sums of P dP, sums of score
+  // gradients along diagonals
+  int pk, splits, near;
+  float *part_o, *part_ml;
+  int4 *k_tab, *q_tab;
+  float *delta, *diag, *tail;
+};
+size_t attn_fwd_bytes(int dtype, const AttnArgs& a);
+size_t attn_bwd_bytes(int dtype, const AttnArgs& a);
+hipError_t launch_attn_fwd(int dtype, AttnArgs a, void* workspace, hipStream_t s);
+hipError_t launch_attn_bwd(int dtype, AttnArgs a, void* workspace, hipStream_t s);
+
 // ---------------------------------------------------------------- measurement probes
 hipError_t launch_probe_copy(const void* src, void* dst, int64_t bytes, hipStream_t s);
 hipError_t launch_probe_mfma(float* out, int waves, int iters, hipStream_t s);
