@@ -32,8 +32,12 @@ constexpr int ROWS = 128;  // query rows (dk, dv: keys) of a workgroup: 4 waves 
 constexpr int QT = 32;     // queries of a step of k_attn_dkv
 
 template <typename T> constexpr int CHUNK = 16 / (int)sizeof(T);
-// keys of a step
+// keys of a step of the forward, and of k_attn_dq
 template <typename T> constexpr int BN = sizeof(T) == 2 ? 64 : 32;
+template <typename T, int DP> constexpr int BN_DQ = sizeof(T) == 2 && DP == 64 ? 64 : 32;
+// waves of a SIMD that a kernel's registers leave room for: 512 of them a lane, one wave
+// where both operands' columns and the results need more than 256
+template <typename T, int DP> constexpr int WAVES = sizeof(T) == 4 && DP == 128 ? 1 : 2;
 
 // ---------------------------------------------------------------- tiles in LDS
 // Rows of DP elements, chunk c of row r at position c ^ swz(r).  Read along rows, 16
@@ -45,6 +49,14 @@ XP_DEV int swz(int r) {
   if constexpr (sizeof(T) == 4) return ((r >> 2) & 1) << 3 | ((r >> 3) & 1) << 2 | (r & 3);
   else if constexpr (DP == 128) return (r & 3) << 2 | ((r >> 2) & 3);
   else return ((r >> 1) & 1) << 2 | ((r >> 2) & 3);
+}
+
+// The same value, of which the compiler knows nothing: what is computed from it is computed
+// where it stands.  (Every lane's place in every tile would otherwise be computed ahead of the
+// loops and kept in registers that the operands need.)
+XP_DEV int fresh(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
 }
 
 // n of a chunk's elements (more: all) from p on, which may start anywhere; zeros behind them
@@ -79,31 +91,41 @@ XP_DEV void widen(const u32x4_t& u, float (&v)[CHUNK<T>]) {
 }
 
 // N rows of DP elements on their way from memory to LDS: loaded a step ahead into
-// registers, stored when the step before is done.
+// registers, stored when the step before is done.  Rows are 16-byte aligned, of `dim`
+// elements in whole chunks; a chunk that is not to be read has an offset past the buffer's
+// end, which loads zeros.
 template <typename T, int DP, int N>
 struct Stager {
   static constexpr int CPR = DP / CHUNK<T>, STEP = 256 / CPR, PER = N / STEP;
   static_assert(N % STEP == 0 && PER >= 1, "whole passes");
   u32x4_t r[PER];
-  // rows [row0, row0 + N); zeros from limit on, behind dim, and where doc is negative
-  XP_DEV void load(const T* base, int64_t stride, int row0, int limit, int dim, const int32_t* doc) {
+  int off;  // of the lane's chunk in the first rows, in bytes; negative behind dim
+  int step;
+  XP_DEV Stager(int64_t stride, int dim) {
     const int c = threadIdx.x % CPR, at = threadIdx.x / CPR;
-    const T* p = base + (int64_t)row0 * stride + c * CHUNK<T>;
-    if (row0 + N <= limit && dim == DP && !doc) {
+    off = c * CHUNK<T> < dim ? (int)((at * stride + c * CHUNK<T>) * (int64_t)sizeof(T)) : -1;
+    step = (int)(STEP * stride * (int64_t)sizeof(T));
+  }
+  // rows from p on; zeros from the limit-th on, and where doc is negative
+  XP_DEV void load(const T* p, int limit, const int32_t* doc) {
+    const int off = fresh(this->off);
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)p, (short)0, 0x7ffffff0, 0x00020000);
+    if (limit >= N && !doc) {
 #pragma unroll
-      for (int i = 0; i < PER; ++i) __builtin_memcpy(&r[i], p + (int64_t)(at + i * STEP) * stride, 16);
+      for (int i = 0; i < PER; ++i) r[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, off < 0 ? off : off + i * step, 0, 0);
     } else {
+      const int at = fresh(threadIdx.x) / CPR;
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
-        const int row = row0 + at + i * STEP;
-        r[i] = (u32x4_t){0, 0, 0, 0};
-        if (row < limit && c * CHUNK<T> < dim && !(doc && doc[row] < 0))
-          r[i] = ld_chunk(p + (int64_t)(at + i * STEP) * stride, dim - c * CHUNK<T>);
+        const int row = at + i * STEP;
+        bool use = off >= 0 && row < limit;
+        if (doc && use) use = doc[row] >= 0;
+        r[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, use ? off + i * step : -1, 0, 0);
       }
     }
   }
   XP_DEV void store(T* lds) const {
-    const int c = threadIdx.x % CPR, at = threadIdx.x / CPR;
+    const int tid = fresh(threadIdx.x), c = tid & (CPR - 1), at = (tid & 255) / CPR;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int row = at + i * STEP;
@@ -119,8 +141,23 @@ XP_DEV void ld_column(const T* row, bool valid, int dim, u32x4_t (&f)[DP / CHUNK
 #pragma unroll
   for (int s = 0; s < DP / CHUNK<T> / 2; ++s) {
     const int at = (2 * s + h) * CHUNK<T>;
-    f[s] = (u32x4_t){0, 0, 0, 0};
-    if (valid && at < dim) f[s] = ld_chunk(row + at, dim - at);
+    u32x4_t u = {0, 0, 0, 0};
+    if (valid && at < dim) u = *reinterpret_cast<const u32x4_t*>(row + at);
+    f[s] = u;
+  }
+}
+
+// [batch][token][head][dim] with any strides to contiguous rows of ldim elements, zeros behind dim
+template <typename T>
+__global__ __launch_bounds__(256) void k_attn_pack(AttnMat from, T* __restrict__ to, int64_t rows, int tokens, int heads, int dim, int ldim) {
+  const int per = ldim / CHUNK<T>;
+  const int64_t n = rows * per;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int64_t row = i / per;
+    const int c = (int)(i % per) * CHUNK<T>, h = (int)(row % heads), t = (int)(row / heads % tokens);
+    const int64_t b = row / heads / tokens;
+    const T* p = (const T*)from.p + b * from.b + t * from.t + h * from.h + c;
+    *reinterpret_cast<u32x4_t*>(to + i * CHUNK<T>) = ld_chunk(p, dim - c);
   }
 }
 
@@ -139,33 +176,43 @@ XP_DEV f32x16_t mma(const u32x4_t& a, const u32x4_t& b, f32x16_t c) {
 // Row of a block that register r of a result holds: 8 (r / 4) + 4 (lane / 32) + r % 4.
 XP_DEV int row_of(int r) { return 8 * (r >> 2) + 4 * ((threadIdx.x >> 5) & 1) + (r & 3); }
 
-// 32 rows of a tile times the lanes' columns
-template <typename T, int DP>
-XP_DEV f32x16_t rows_times(const T* tile, const u32x4_t (&col)[DP / CHUNK<T> / 2]) {
-  const int r = threadIdx.x & 31, h = (threadIdx.x >> 5) & 1;
-  f32x16_t c;
+// 32 rows of a tile times the lanes' N columns
+template <typename T, int DP, int N>
+XP_DEV void rows_times(const T* tile, const u32x4_t (&col)[N][DP / CHUNK<T> / 2], f32x16_t (&out)[N]) {
+  const int lane = fresh(threadIdx.x), r = lane & 31, h = (lane >> 5) & 1;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) c[i] = 0.f;
+  for (int c = 0; c < N; ++c)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) out[c][i] = 0.f;
 #pragma unroll
   for (int s = 0; s < DP / CHUNK<T> / 2; ++s) {
     const u32x4_t a = *reinterpret_cast<const u32x4_t*>(tile + r * DP + (((2 * s + h) ^ swz<T, DP>(r)) * CHUNK<T>));
-    c = mma<T>(a, col[s], c);
+#pragma unroll
+    for (int c = 0; c < N; ++c) out[c] = mma<T>(a, col[c][s], out[c]);
   }
-  return c;
+}
+template <typename T, int DP>
+XP_DEV f32x16_t rows_times(const T* tile, const u32x4_t (&col)[DP / CHUNK<T> / 2]) {
+  const auto& one = reinterpret_cast<const u32x4_t(&)[1][DP / CHUNK<T> / 2]>(col);
+  f32x16_t out[1];
+  rows_times<T, DP, 1>(tile, one, out);
+  return out[0];
 }
 
-// acc[d][lane's column] += sum over the 32 rows of tile[row][d] w[row]
-template <typename T, int DP>
-XP_DEV void add_transposed(f32x16_t (&acc)[DP / 32], const T* tile, const float (&w)[16]) {
-  const int lane = threadIdx.x & 63, h = lane >> 5;
+// acc[c][d][lane's column] += sum over the 32 rows of tile[row][d] w[c][row]
+template <typename T, int DP, int N>
+XP_DEV void add_transposed(f32x16_t (&acc)[N][DP / 32], const T* tile, const float (&w)[N][16]) {
+  const int lane = fresh(threadIdx.x) & 63, h = lane >> 5;
   if constexpr (sizeof(T) == 2) {
     typedef short v4i16 __attribute__((ext_vector_type(4)));
     const int p = (lane & 15) >> 2;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      u32x4_t f;
+      u32x4_t f[N];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) f[i] = f32x2_to_bf16x2(w[8 * b + 2 * i], w[8 * b + 2 * i + 1]);
+      for (int c = 0; c < N; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[c][i] = f32x2_to_bf16x2(w[c][8 * b + 2 * i], w[c][8 * b + 2 * i + 1]);
 #pragma unroll
       for (int d = 0; d < DP / 32; ++d) {
         const int chunk = d * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
@@ -176,21 +223,28 @@ XP_DEV void add_transposed(f32x16_t (&acc)[DP / 32], const T* tile, const float 
           part[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4i16*)(
               tile + row * DP + ((chunk ^ swz<T, DP>(row)) * 8) + 4 * (lane & 1)));
         }
-        acc[d] = mma<T>(__builtin_bit_cast(u32x4_t, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7)), f, acc[d]);
+        const u32x4_t x = __builtin_bit_cast(u32x4_t, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+        for (int c = 0; c < N; ++c) acc[c][d] = mma<T>(x, f[c], acc[c][d]);
       }
     }
   } else {
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const int row = row_of(r);
+      const int row = 8 * (r >> 2) + 4 * h + (r & 3);
 #pragma unroll
       for (int d = 0; d < DP / 32; ++d) {
         const int col = d * 32 + (lane & 31);
-        const float a = tile[row * DP + (((col >> 2) ^ swz<T, DP>(row)) << 2) + (col & 3)];
-        acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w[r], acc[d], 0, 0, 0);
+        const float x = tile[row * DP + (((col >> 2) ^ swz<T, DP>(row)) << 2) + (col & 3)];
+#pragma unroll
+        for (int c = 0; c < N; ++c) acc[c][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, w[c][r], acc[c][d], 0, 0, 0);
       }
     }
   }
+}
+template <typename T, int DP>
+XP_DEV void add_transposed(f32x16_t (&acc)[DP / 32], const T* tile, const float (&w)[16]) {
+  add_transposed<T, DP, 1>(reinterpret_cast<f32x16_t(&)[1][DP / 32]>(acc), tile, reinterpret_cast<const float(&)[1][16]>(w));
 }
 
 // The lane's column of a result [DP][32], times f, to a row of dim elements in memory.
@@ -218,6 +272,10 @@ XP_DEV void st_column(T* row, int dim, const f32x16_t (&acc)[DP / 32], float f) 
       }
     }
 }
+
+// Nothing moves over this line: without it the compiler starts the next product's reads so
+// early that the registers do not hold them.
+XP_DEV void phase() { __builtin_amdgcn_sched_barrier(0); }
 
 // ---------------------------------------------------------------- halves and waves
 // the larger, and the sum, of a value in lanes l and l ^ 32
@@ -273,7 +331,7 @@ struct Walk {
   }
 };
 
-// {smallest, largest document, whether the tile holds several or padding} of each tile
+// {smallest, largest document, whether the tile holds several or padding, whether padding} of each tile
 __global__ __launch_bounds__(64) void k_attn_docs(const int32_t* __restrict__ doc, const int32_t* __restrict__ len, int n, int tile,
                                                    int4* __restrict__ tab) {
   const int b = blockIdx.y, limit = len ? min(max(len[b], 0), n) : n;
@@ -286,15 +344,21 @@ __global__ __launch_bounds__(64) void k_attn_docs(const int32_t* __restrict__ do
     hi = max(hi, __shfl_xor(hi, o, 64));
   }
   const bool pad = __any((int)threadIdx.x < tile && d < 0);
-  if (threadIdx.x == 0) tab[(int64_t)b * gridDim.x + blockIdx.x] = make_int4(lo, hi < 0 ? -1 : hi, lo != hi || pad, 0);
+  if (threadIdx.x == 0) tab[(int64_t)b * gridDim.x + blockIdx.x] = make_int4(lo, hi < 0 ? -1 : hi, lo != hi || pad, pad);
 }
 
 // smallest and largest document over a workgroup's rows, and over the wave's; negative ones do not count
 struct DocRange { int lo, hi, wlo, whi; };
-XP_DEV DocRange doc_range(int doc, int (*sh)[2]) {
+template <int N>
+XP_DEV DocRange doc_range(const int (&doc)[N], int (*sh)[2]) {
   DocRange d;
-  d.wlo = doc >= 0 ? doc : INT_MAX;
-  d.whi = doc >= 0 ? doc : -1;
+  d.wlo = INT_MAX;
+  d.whi = -1;
+#pragma unroll
+  for (int c = 0; c < N; ++c) {
+    d.wlo = min(d.wlo, doc[c] >= 0 ? doc[c] : INT_MAX);
+    d.whi = max(d.whi, doc[c]);
+  }
   for (int o = 32; o > 0; o >>= 1) {
     d.wlo = min(d.wlo, __shfl_xor(d.wlo, o, 64));
     d.whi = max(d.whi, __shfl_xor(d.whi, o, 64));
@@ -381,16 +445,20 @@ XP_DEV void scores(f32x16_t& s, const AttnArgs& a, const Bias& bias, int dist, i
 }
 
 // ---------------------------------------------------------------- forward
-// One workgroup per 128 query rows of a head (with pk > 1: of the pk heads that share
-// keys, row r being query r / pk of head r % pk), and part of the keys.
-template <typename T, int DP, bool GEN>
-__global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs a) {
-  constexpr int KEYS = BN<T>, NB = KEYS / 32;
+// One workgroup per 4 waves of 32 QB query rows of a head (with pk > 1: of the pk heads that
+// share keys, row r being query r / pk of head r % pk), and part of the keys.
+//
+// The largest score enters the exponentials only when it has grown by more than 8 (base 2)
+// since it last did: P is then at most 2^8, the sums stay in fp32's range, and the results
+// are rarely multiplied.
+template <typename T, int DP, bool GEN, int QB>
+__global__ __launch_bounds__(256, QB == 2 && DP == 128 ? 1 : (WAVES<T, DP>)) void k_attn_fwd(AttnArgs a) {
+  constexpr int KEYS = BN<T>, NB = KEYS / 32, WAVE = 32 * QB, GROUP = 4 * WAVE;
   __shared__ T sk[2][KEYS * DP], sv[2][KEYS * DP];
   __shared__ int sdoc[2][KEYS];
   __shared__ int sh[4][2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int rows = a.nq * a.pk, blocks = (rows + ROWS - 1) / ROWS, units = a.heads / a.pk;
+  const int rows = a.nq * a.pk, blocks = (rows + GROUP - 1) / GROUP, units = a.heads / a.pk;
   int id = xcd_tile(blockIdx.x, gridDim.x);
   const int split = id % a.splits;
   id /= a.splits;
@@ -400,48 +468,58 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs a) {
   const int kvh = unit * a.pk / (a.heads / a.kv_heads);
   const Seq seq(a, b);
 
-  const int row = blk * ROWS + wave * 32 + (lane & 31);
-  const int i = row / a.pk, head = unit * a.pk + row % a.pk;
-  const bool in = row < rows, live = in && i < seq.ql;
-  const int doc = a.q_doc ? (live ? a.q_doc[(int64_t)b * a.nq + i] : -1) : 0;
-  const int kend = live && doc >= 0 ? seq.kend(i) : 0, pos = i + seq.off;
   // limits of the workgroup's and the wave's rows (of those that count)
-  const int last = min((min(rows, (blk + 1) * ROWS) - 1) / a.pk, seq.ql - 1), first = blk * ROWS / a.pk;
+  const int last = min((min(rows, (blk + 1) * GROUP) - 1) / a.pk, seq.ql - 1), first = blk * GROUP / a.pk;
   const int kmax = first <= last ? seq.kend(last) : 0;
-  const int wfirst = (blk * ROWS + wave * 32) / a.pk, wlast = min((blk * ROWS + wave * 32 + 31) / a.pk, min(a.nq, seq.ql) - 1);
+  const int row0 = blk * GROUP + wave * WAVE;
+  const int wfirst = row0 / a.pk, wlast = min((row0 + WAVE - 1) / a.pk, min(a.nq, seq.ql) - 1);
   const int wmax = wfirst <= wlast ? seq.kend(wlast) : 0, wmin = wfirst <= wlast ? seq.kend(wfirst) : 0;
-  DocRange docs = {0, 0, 0, 0};
-  if (a.q_doc) docs = doc_range(doc, sh);
 
-  u32x4_t q[DP / CHUNK<T> / 2];
-  ld_column<T, DP>((const T*)a.q.p + b * a.q.b + (int64_t)i * a.q.t + head * a.q.h, live, a.dim, q);
+  int doc[QB], kend[QB], pos[QB], head[QB];
+  u32x4_t q[QB][DP / CHUNK<T> / 2];
+#pragma unroll
+  for (int c = 0; c < QB; ++c) {
+    const int row = row0 + c * 32 + (lane & 31), i = row / a.pk;
+    const bool live = row < rows && i < seq.ql;
+    head[c] = unit * a.pk + row % a.pk;
+    doc[c] = a.q_doc ? (live ? a.q_doc[(int64_t)b * a.nq + i] : -1) : 0;
+    kend[c] = live && doc[c] >= 0 ? seq.kend(i) : 0;
+    pos[c] = i + seq.off;
+    ld_column<T, DP>((const T*)a.q.p + b * a.q.b + (int64_t)i * a.q.t + head[c] * a.q.h, live, a.ldim, q[c]);
+  }
+  DocRange docs = {0, 0, 0, 0};
+  if (a.q_doc) docs = doc_range<QB>(doc, sh);
   const T* kp = (const T*)a.k.p + b * a.k.b + kvh * a.k.h;
   const T* vp = (const T*)a.v.p + b * a.v.b + kvh * a.v.h;
   const int32_t* kdoc = a.k_doc ? a.k_doc + (int64_t)b * a.nk : nullptr;
-  const Bias bias(a, in ? head : 0);
 
   const int tiles = (kmax + KEYS - 1) / KEYS, per = (tiles + a.splits - 1) / a.splits;
   const int tab_tiles = (a.nk + KEYS - 1) / KEYS;
   Walk walk(a.k_tab ? a.k_tab + (int64_t)b * tab_tiles : nullptr, min(tiles, (split + 1) * per), docs.lo, docs.hi);
 
-  // m: the largest of the products (GEN: of the scores) so far; l: this lane's part of the sum
+  // m: the largest of the products (GEN: of the scores) so far, base: the one in the
+  // exponentials; l: this lane's part of the sum
   const float c1 = GEN ? LOG2E : a.scale * LOG2E;
-  float m = NEG_INF, l = 0.f;
-  f32x16_t acc[DP / 32];
+  float m[QB], base[QB], l[QB];
+  f32x16_t acc[QB][DP / 32];
 #pragma unroll
-  for (int d = 0; d < DP / 32; ++d)
+  for (int c = 0; c < QB; ++c) {
+    m[c] = base[c] = NEG_INF;
+    l[c] = 0.f;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[c][d][r] = 0.f;
+  }
 
-  Stager<T, DP, KEYS> ks, vs;
+  Stager<T, DP, KEYS> ks(a.k.t, a.ldim), vs(a.v.t, a.ldim);
   int dreg = -1;
   auto load = [&](int t) __attribute__((always_inline)) {
-    ks.load(kp, a.k.t, t * KEYS, seq.kl, a.dim, kdoc);
-    vs.load(vp, a.v.t, t * KEYS, seq.kl, a.dim, kdoc);
-    if (kdoc && threadIdx.x < KEYS) {
-      const int j = t * KEYS + (int)threadIdx.x;
-      dreg = j < seq.kl ? kdoc[j] : -1;
-    }
+    const int j0 = t * KEYS;
+    const int32_t* pad = kdoc && walk.tab[t].w ? kdoc + j0 : nullptr;
+    ks.load(kp + (int64_t)j0 * a.k.t, seq.kl - j0, pad);
+    vs.load(vp + (int64_t)j0 * a.v.t, seq.kl - j0, pad);
+    if (kdoc && threadIdx.x < KEYS) dreg = j0 + (int)threadIdx.x < seq.kl ? kdoc[j0 + threadIdx.x] : -1;
   };
   auto store = [&](int buf) __attribute__((always_inline)) {
     ks.store(sk[buf]);
@@ -464,49 +542,62 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs a) {
       mixed = e.z || docs.wlo != docs.whi;
     }
     if (!skip) {
-      f32x16_t s[NB];
-#pragma unroll
-      for (int n = 0; n < NB; ++n) s[n] = rows_times<T, DP>(sk[buf] + n * 32 * DP, q);
-      if constexpr (GEN) {
-        float none[16];
-#pragma unroll
-        for (int n = 0; n < NB; ++n) {
-          const int k0 = t * KEYS + n * 32;
-          scores<true, false>(s[n], a, bias, k0 - pos, k0 - wlast - seq.off, k0 + 31 - wfirst - seq.off, none);
-        }
-      }
-      if (mixed || (t + 1) * KEYS > wmin) {
-#pragma unroll
-        for (int n = 0; n < NB; ++n) {
-          const uint32_t hide = hidden(t * KEYS + n * 32, kend, kdoc ? sdoc[buf] + n * 32 : nullptr, doc);
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[n][r] = hide >> r & 1 ? NEG_INF : s[n][r];
-        }
-      }
-      float top = s[0][0];
-#pragma unroll
-      for (int n = 0; n < NB; ++n)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[n][r]);
-      const float mn = fmaxf(m, both_max(top)), base = mn == NEG_INF ? 0.f : mn;
-      const float keep = exp2_((m - base) * c1);
-      m = mn;
-      l *= keep;
-      if (__any(keep != 1.f)) {
-#pragma unroll
-        for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) acc[d][r] *= keep;
-      }
+      const bool masked = mixed || (t + 1) * KEYS > wmin;
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
-        float p[16];
+        const int k0 = t * KEYS + n * 32;
+        f32x16_t s[QB];
+        rows_times<T, DP, QB>(sk[buf] + n * 32 * DP, q, s);
+        phase();
+        if constexpr (GEN) {
+          float none[16];
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          p[r] = GEN ? exp2_((s[n][r] - base) * c1) : exp2_(s[n][r] * c1 - base * c1);
-          l += p[r];
+          for (int c = 0; c < QB; ++c) {
+            const Bias bias(a, min(head[c], a.heads - 1));
+            scores<true, false>(s[c], a, bias, k0 - pos[c], k0 - wlast - seq.off, k0 + 31 - wfirst - seq.off, none);
+          }
         }
-        add_transposed<T, DP>(acc, sv[buf] + n * 32 * DP, p);
+        if (masked) {
+#pragma unroll
+          for (int c = 0; c < QB; ++c) {
+            const uint32_t hide = hidden(k0, kend[c], kdoc ? sdoc[buf] + n * 32 : nullptr, doc[c]);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[c][r] = hide >> r & 1 ? NEG_INF : s[c][r];
+          }
+        }
+        bool grown = false;
+#pragma unroll
+        for (int c = 0; c < QB; ++c) {
+          float top = s[c][0];
+#pragma unroll
+          for (int r = 1; r < 16; ++r) top = fmaxf(top, s[c][r]);
+          m[c] = fmaxf(m[c], both_max(top));
+          grown = grown || (m[c] - base[c]) * c1 > 8.f;  // (from -inf on: infinite; while there is no key: NaN)
+        }
+        if (__any(grown)) {
+#pragma unroll
+          for (int c = 0; c < QB; ++c) {
+            const float keep = m[c] == NEG_INF ? 1.f : exp2_((base[c] - m[c]) * c1);
+            base[c] = m[c];
+            l[c] *= keep;
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) acc[c][d][r] *= keep;
+          }
+        }
+        float p[QB][16];
+#pragma unroll
+        for (int c = 0; c < QB; ++c) {
+          const float off = base[c] == NEG_INF ? 0.f : base[c], bc = off * c1;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            p[c][r] = GEN ? exp2_((s[c][r] - off) * c1) : exp2_(s[c][r] * c1 - bc);
+            l[c] += p[c][r];
+          }
+        }
+        add_transposed<T, DP, QB>(acc, sv[buf] + n * 32 * DP, p);
+        phase();
       }
     }
     buf ^= 1;
@@ -514,37 +605,36 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnArgs a) {
     t = tn;
   }
 
-  l = both_sum(l);
-  if (kend == 0) {
-    m = NEG_INF;
-    l = 0.f;
-  }
-  if (!in) return;
-  const float ms = GEN ? m : m * a.scale;
-  if (a.splits > 1) {
-    const int64_t r = ((int64_t)split * a.batch + b) * a.heads * a.nq + (int64_t)head * a.nq + i;
-    if (lane < 32) {
-      a.part_ml[2 * r] = ms;
-      a.part_ml[2 * r + 1] = l;
+#pragma unroll
+  for (int c = 0; c < QB; ++c) {
+    const int row = row0 + c * 32 + (lane & 31), i = row / a.pk;
+    // (a NaN among the scores leaves l NaN, and the row NaN)
+    const float sum = both_sum(l[c]);
+    const bool none = kend[c] == 0 || sum == 0.f;
+    const float ms = none ? NEG_INF : GEN ? m[c] : m[c] * a.scale, ls = none ? 0.f : sum * exp2_((base[c] - m[c]) * c1);
+    if (row >= rows) continue;
+    if (a.splits > 1) {
+      // (o's part belongs to `base`; a sum of zero leaves it unwritten)
+      const int64_t r = ((int64_t)split * a.batch + b) * a.heads * a.nq + (int64_t)head[c] * a.nq + i;
+      if (lane < 32) {
+        a.part_ml[2 * r] = ms;
+        a.part_ml[2 * r + 1] = ls;
+      }
+      st_column<float, DP>(a.part_o + r * DP, none ? 0 : DP, acc[c], exp2_((base[c] - m[c]) * c1));
+      continue;
     }
-    st_column<float, DP>(a.part_o + r * DP, l > 0.f ? DP : 0, acc, 1.f);
-    return;
-  }
-  if (a.stats && lane < 32) {
-    float* st = a.stats + 2 * (((int64_t)b * a.heads + head) * a.nq + i);
-    st[0] = ms;
-    st[1] = l;
-  }
-  // (a NaN among the scores leaves l NaN, and the row NaN)
-  const bool none = l == 0.f;
-  if (none) {
+    if (a.stats && lane < 32) {
+      float* st = a.stats + 2 * (((int64_t)b * a.heads + head[c]) * a.nq + i);
+      st[0] = ms;
+      st[1] = ls;
+    }
+    if (none)
 #pragma unroll
-    for (int d = 0; d < DP / 32; ++d)
+      for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
+        for (int r = 0; r < 16; ++r) acc[c][d][r] = 0.f;
+    st_column<T, DP>((T*)a.o.p + b * a.o.b + (int64_t)i * a.o.t + head[c] * a.o.h, a.dim, acc[c], none ? 0.f : 1.f / sum);
   }
-  const float f = none ? 0.f : 1.f / l;
-  st_column<T, DP>((T*)a.o.p + b * a.o.b + (int64_t)i * a.o.t + head * a.o.h, a.dim, acc, f);
 }
 
 // The parts of the keys joined: one wave per query row.
@@ -581,19 +671,24 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
 }
 
 // ---------------------------------------------------------------- statistics of a row
-// P = exp2(score' - row.a) row.b with score' in units of log 2 (without GEN: the product times
-// scale log2(e), and row.a has the sum in it).  A row without keys gives 0.
+// P = exp2(score' - row.a) with score' in units of log 2, where row.a has the sum's logarithm
+// in it; GEN (a bias can be as large as fp32 goes): exp2((score - row.a) log2(e) - row.b) with
+// the sum's logarithm apart.  A row without keys gives 0.
 struct RowStat { float a, b; };
 template <bool GEN>
 XP_DEV RowStat row_stat(float m, float l) {
   if (l == 0.f) return {__builtin_inff(), 0.f};
-  if constexpr (GEN) return {m, 1.f / l};
-  else return {m * LOG2E + __builtin_amdgcn_logf(l), 1.f};
+  const float log2l = __builtin_amdgcn_logf(l);
+  if constexpr (GEN) return {m, log2l};
+  else return {m * LOG2E + log2l, 0.f};
 }
 template <bool GEN>
-XP_DEV float weight(float s, RowStat st, float c1) {
-  return GEN ? exp2_((s - st.a) * LOG2E) * st.b : exp2_(s * c1 - st.a);
+XP_DEV float weight(float s, float a, float b, float c1) {
+  return GEN ? exp2_((s - a) * LOG2E - b) : exp2_(s * c1 - a);
 }
+// What k_attn_dkv needs of 32 query rows: row.a, row.b, sum of P dP, kend, document, 32 each, and
+// room up to ROW_INFO floats.
+constexpr int ROW_INFO = 256;
 
 // Blocks of 32 keys (from key kw on) by 32 queries that hold a distance within the bias's
 // range: the first one's index, of at most near_blocks().
@@ -605,8 +700,8 @@ XP_DEV int first_near(const AttnArgs& a, const Seq& seq, int kw) { return max(0,
 // sum as P dP in fp32, which the loop makes by the way, is what k_attn_dkv reads: bias
 // gradients are fp32, and a rounded o would show in their sums.
 template <typename T, int DP, bool GEN>
-__global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs a) {
-  constexpr int KEYS = BN<T>, NB = KEYS / 32;
+__global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dq(AttnArgs a) {
+  constexpr int KEYS = BN_DQ<T, DP>, NB = KEYS / 32;
   __shared__ T sk[2][KEYS * DP], sv[2][KEYS * DP];
   __shared__ int sdoc[2][KEYS];
   __shared__ int sh[4][2];
@@ -628,12 +723,12 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs a) {
   const int wfirst = first + wave * 32, wlast = min(wfirst + 31, last);
   const int wmax = wfirst <= wlast ? seq.kend(wlast) : 0, wmin = wfirst <= wlast ? seq.kend(wfirst) : 0;
   DocRange docs = {0, 0, 0, 0};
-  if (a.q_doc) docs = doc_range(doc, sh);
+  if (a.q_doc) docs = doc_range<1>({doc}, sh);
 
   u32x4_t q[DP / CHUNK<T> / 2], g[DP / CHUNK<T> / 2];
   const bool use = live && doc >= 0;
-  ld_column<T, DP>((const T*)a.q.p + b * a.q.b + (int64_t)i * a.q.t + head * a.q.h, use, a.dim, q);
-  ld_column<T, DP>((const T*)a.dout.p + b * a.dout.b + (int64_t)i * a.dout.t + head * a.dout.h, use, a.dim, g);
+  ld_column<T, DP>((const T*)a.q.p + b * a.q.b + (int64_t)i * a.q.t + head * a.q.h, use, a.ldim, q);
+  ld_column<T, DP>((const T*)a.dout.p + b * a.dout.b + (int64_t)i * a.dout.t + head * a.dout.h, use, a.ldim, g);
   const int64_t srow = ((int64_t)b * a.heads + head) * a.nq + i;
   float delta = 0.f;
   RowStat st = {__builtin_inff(), 0.f};
@@ -669,15 +764,14 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs a) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
 
-  Stager<T, DP, KEYS> ks, vs;
+  Stager<T, DP, KEYS> ks(a.k.t, a.ldim), vs(a.v.t, a.ldim);
   int dreg = -1;
   auto load = [&](int t) __attribute__((always_inline)) {
-    ks.load(kp, a.k.t, t * KEYS, seq.kl, a.dim, kdoc);
-    vs.load(vp, a.v.t, t * KEYS, seq.kl, a.dim, kdoc);
-    if (kdoc && threadIdx.x < KEYS) {
-      const int j = t * KEYS + (int)threadIdx.x;
-      dreg = j < seq.kl ? kdoc[j] : -1;
-    }
+    const int j0 = t * KEYS;
+    const int32_t* pad = kdoc && walk.tab[t].w ? kdoc + j0 : nullptr;
+    ks.load(kp + (int64_t)j0 * a.k.t, seq.kl - j0, pad);
+    vs.load(vp + (int64_t)j0 * a.v.t, seq.kl - j0, pad);
+    if (kdoc && threadIdx.x < KEYS) dreg = j0 + (int)threadIdx.x < seq.kl ? kdoc[j0 + threadIdx.x] : -1;
   };
   auto store = [&](int buf) __attribute__((always_inline)) {
     ks.store(sk[buf]);
@@ -704,12 +798,14 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs a) {
       for (int n = 0; n < NB; ++n) {
         const int k0 = t * KEYS + n * 32;
         f32x16_t s = rows_times<T, DP>(sk[buf] + n * 32 * DP, q);
+        phase();
         const f32x16_t dp = rows_times<T, DP>(sv[buf] + n * 32 * DP, g);
+        phase();
         float slope[16], ds[16];
         if constexpr (GEN)
           scores<true, true>(s, a, bias, k0 - pos, k0 - wlast - seq.off, k0 + 31 - wfirst - seq.off, slope);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) ds[r] = weight<GEN>(s[r], st, c1);
+        for (int r = 0; r < 16; ++r) ds[r] = weight<GEN>(s[r], st.a, st.b, c1);
         if (mixed || k0 + 32 > wmin) {
           const uint32_t hide = hidden(k0, kend, kdoc ? sdoc[buf] + n * 32 : nullptr, doc);
 #pragma unroll
@@ -724,7 +820,9 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs a) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) ds[r] *= slope[r];
         }
+        phase();
         add_transposed<T, DP>(acc, sk[buf] + n * 32 * DP, ds);
+        phase();
       }
     }
     buf ^= 1;
@@ -732,7 +830,14 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(AttnArgs a) {
     t = tn;
   }
   exact = both_sum(exact);
-  if (in && lane < 32) a.delta[srow] = exact;
+  if (lane < 32) {
+    float* row = a.rows + (((int64_t)b * a.heads + head) * (blocks * 4) + blk * 4 + wave) * ROW_INFO + lane;
+    row[0] = st.a;
+    row[32] = st.b;
+    row[64] = exact;
+    row[96] = __int_as_float(kend);
+    row[128] = __int_as_float(doc);
+  }
   if (in) st_column<T, DP>((T*)a.dq.p + b * a.dq.b + (int64_t)i * a.dq.t + head * a.dq.h, a.dim, acc, a.scale);
 }
 
@@ -774,10 +879,9 @@ __global__ __launch_bounds__(256) void k_attn_dbias(AttnArgs a) {
 // the sums of dS along the diagonals of each block of 32 x 32 near the diagonal, and over
 // the blocks beyond the bias's range on either side.
 template <typename T, int DP, bool GEN, int WHAT>
-__global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs a) {
+__global__ __launch_bounds__(256, GEN && DP == 128 ? 1 : (WAVES<T, DP>)) void k_attn_dkv(AttnArgs a) {
   __shared__ T sq[2][QT * DP], sg[2][QT * DP];
-  __shared__ float sa[2][QT], sb[2][QT], sd[2][QT];
-  __shared__ int send[2][QT], sdoc[2][QT];
+  __shared__ float srow[2][5 * QT];
   __shared__ int sh[4][2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int blocks = (a.nk + ROWS - 1) / ROWS, group = a.heads / a.kv_heads;
@@ -792,14 +896,14 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs a) {
   DocRange docs = {0, 0, 0, 0};
   bool pad = false;
   if (a.k_doc) {
-    docs = doc_range(doc, sh);
+    docs = doc_range<1>({doc}, sh);
     pad = __any(doc < 0);
   }
   u32x4_t kc[DP / CHUNK<T> / 2], vc[DP / CHUNK<T> / 2];
   const bool use = j < seq.kl && doc >= 0;
-  ld_column<T, DP>((const T*)a.k.p + b * a.k.b + (int64_t)j * a.k.t + kvh * a.k.h, use, a.dim, kc);
+  ld_column<T, DP>((const T*)a.k.p + b * a.k.b + (int64_t)j * a.k.t + kvh * a.k.h, use, a.ldim, kc);
   if constexpr (WHAT & 2)
-    ld_column<T, DP>((const T*)a.v.p + b * a.v.b + (int64_t)j * a.v.t + kvh * a.v.h, use, a.dim, vc);
+    ld_column<T, DP>((const T*)a.v.p + b * a.v.b + (int64_t)j * a.v.t + kvh * a.v.h, use, a.ldim, vc);
   const int32_t* qdoc = a.q_doc ? a.q_doc + (int64_t)b * a.nq : nullptr;
 
   // queries that see a key of the workgroup: those with kend > k0, from the first such on
@@ -831,37 +935,20 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs a) {
       if (lane < 2) a.tail[2 * w + lane] = 0.f;
     }
 
-  Stager<T, DP, QT> qs, gs;
-  float ra = 0.f, rb = 0.f, rd = 0.f;
-  int rend = 0, rdoc = -1;
+  Stager<T, DP, QT> qs(a.q.t, a.ldim), gs(a.dout.t, a.ldim);
+  const int row_tiles = (a.nq + ROWS - 1) / ROWS * 4;
+  float rreg = 0.f;
   auto load = [&](int t, int head) __attribute__((always_inline)) {
-    qs.load((const T*)a.q.p + b * a.q.b + head * a.q.h, a.q.t, t * QT, seq.ql, a.dim, qdoc);
-    gs.load((const T*)a.dout.p + b * a.dout.b + head * a.dout.h, a.dout.t, t * QT, seq.ql, a.dim, qdoc);
-    if (threadIdx.x < QT) {
-      const int i = t * QT + (int)threadIdx.x;
-      rdoc = qdoc ? (i < seq.ql ? qdoc[i] : -1) : 0;
-      rend = i < seq.ql && rdoc >= 0 ? seq.kend(i) : 0;
-      RowStat st = {__builtin_inff(), 0.f};
-      rd = 0.f;
-      if (rend > 0) {
-        const int64_t srow = ((int64_t)b * a.heads + head) * a.nq + i;
-        st = row_stat<GEN>(a.stats[2 * srow], a.stats[2 * srow + 1]);
-        rd = a.delta[srow];
-      }
-      ra = st.a;
-      rb = st.b;
-    }
+    const int i0 = t * QT;
+    const int32_t* pads = qdoc && walk.tab[t].w ? qdoc + i0 : nullptr;
+    qs.load((const T*)a.q.p + b * a.q.b + head * a.q.h + i0 * a.q.t, seq.ql - i0, pads);
+    gs.load((const T*)a.dout.p + b * a.dout.b + head * a.dout.h + i0 * a.dout.t, seq.ql - i0, pads);
+    if (threadIdx.x < 5 * QT) rreg = a.rows[(((int64_t)b * a.heads + head) * row_tiles + t) * ROW_INFO + threadIdx.x];
   };
   auto store = [&](int buf) __attribute__((always_inline)) {
     qs.store(sq[buf]);
     gs.store(sg[buf]);
-    if (threadIdx.x < QT) {
-      sa[buf][threadIdx.x] = ra;
-      sb[buf][threadIdx.x] = rb;
-      sd[buf][threadIdx.x] = rd;
-      send[buf][threadIdx.x] = rend;
-      sdoc[buf][threadIdx.x] = rdoc;
-    }
+    if (threadIdx.x < 5 * QT) srow[buf][threadIdx.x] = rreg;
   };
   int g = 0, t = walk.next(t0), buf = 0;
   const int t_first = t;
@@ -888,6 +975,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs a) {
     if (!skip) {
       const int head = kvh * group + g;
       f32x16_t s = rows_times<T, DP>(sq[buf], kc);
+      phase();
       float p[16], slope[16];
       if constexpr (GEN) {
         const Bias bias(a, head);
@@ -895,20 +983,25 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs a) {
         scores<false, true>(s, a, bias, dist, kw - i1 - seq.off, kw + 31 - i0 - seq.off, slope);
       }
 #pragma unroll
-      for (int r = 0; r < 16; ++r) p[r] = weight<GEN>(s[r], {sa[buf][row_of(r)], sb[buf][row_of(r)]}, c1);
+      for (int r = 0; r < 16; ++r) p[r] = weight<GEN>(s[r], srow[buf][row_of(r)], GEN ? srow[buf][32 + row_of(r)] : 0.f, c1);
       const bool masked = mixed || i0 + QT > seq.ql || seq.kend(i0) < kw + 32;
       if (masked) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) p[r] = j >= send[buf][row_of(r)] ? 0.f : p[r];
+        for (int r = 0; r < 16; ++r) p[r] = j >= __float_as_int(srow[buf][96 + row_of(r)]) ? 0.f : p[r];
         if (qdoc)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) p[r] = sdoc[buf][row_of(r)] != doc ? 0.f : p[r];
+          for (int r = 0; r < 16; ++r) p[r] = __float_as_int(srow[buf][128 + row_of(r)]) != doc ? 0.f : p[r];
       }
-      if constexpr (WHAT & 1) add_transposed<T, DP>(dv, sg[buf], p);
+      if constexpr (WHAT & 1) {
+        phase();
+        add_transposed<T, DP>(dv, sg[buf], p);
+        phase();
+      }
       if constexpr (WHAT & 2) {
         const f32x16_t dp = rows_times<T, DP>(sg[buf], vc);
+        phase();
 #pragma unroll
-        for (int r = 0; r < 16; ++r) p[r] *= dp[r] - sd[buf][row_of(r)];
+        for (int r = 0; r < 16; ++r) p[r] *= dp[r] - srow[buf][64 + row_of(r)];
         if (diag) {
           const int dlow = kw - i0 - 31 - seq.off;  // the block's smallest distance
           if (dlow + 62 <= -a.range || dlow >= a.range) {
@@ -943,6 +1036,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dkv(AttnArgs a) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) p[r] *= slope[r];
         }
+        phase();
         add_transposed<T, DP>(dk, sq[buf], p);
       }
     }
@@ -973,6 +1067,7 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 int padded_dim(int dim) { return dim <= 64 ? 64 : 128; }
 int keys_of(int dtype) { return dtype == DT_BF16 ? BN<bf16_t> : BN<float>; }
+int dq_keys_of(int dtype, const AttnArgs& a) { return dtype == DT_BF16 && a.dim <= 64 ? BN_DQ<bf16_t, 64> : 32; }
 
 // Few query rows: those of the heads that share keys go into one workgroup, which then reads
 // the keys once for all of them.
@@ -990,13 +1085,36 @@ int parts(int dtype, const AttnArgs& a) {
   return (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(512, groups), steps / 4));
 }
 
+// whether the forward's waves take 64 query rows each
+bool wide(const AttnArgs& a) {
+  return a.splits == 1 && ceil_div((int64_t)a.nq * a.pk, 2 * ROWS) * (a.heads / a.pk) * a.batch >= 256;
+}
+
 // blocks of 32 queries that hold distances within the range, of 32 keys
 int near_blocks(const AttnArgs& a) { return (int)std::min<int64_t>(ceil_div(a.nq, 32), ceil_div(2 * (int64_t)a.range + 62, 32) + 1); }
 
+// Inputs whose rows are not whole, aligned chunks of 16 bytes are copied to such ones first:
+// the kernels read nothing else.  Places the copy at `at` in the workspace, with `from` what is to
+// be copied (p null: nothing), and returns the workspace's new end.
+size_t lay_packed(int dtype, AttnArgs& a, AttnMat& m, int64_t tokens, int64_t heads, char* base, size_t at, AttnMat& from) {
+  const int es = dtype == DT_BF16 ? 2 : 4, chunk = 16 / es;
+  a.ldim = (a.dim + chunk - 1) / chunk * chunk;
+  from = AttnMat{};
+  const int64_t n = a.batch * tokens * heads;
+  if (n == 0) return at;
+  auto odd = [&](int64_t stride, int64_t count) { return count > 1 && stride % chunk != 0; };
+  if (a.ldim == a.dim && (reinterpret_cast<uintptr_t>(m.p) & 15) == 0 && !odd(m.b, a.batch) && !odd(m.t, tokens) && !odd(m.h, heads)) return at;
+  from = m;
+  m = AttnMat{base ? base + at : nullptr, tokens * heads * a.ldim, heads * a.ldim, a.ldim};
+  return at + round256((size_t)n * a.ldim * es);
+}
+
 // The workspace's pieces; sets their pointers where base is given.
-size_t lay_fwd(int dtype, AttnArgs& a, char* base) {
+size_t lay_fwd(int dtype, AttnArgs& a, char* base, AttnMat* from) {
   size_t n = 0;
   auto take = [&](size_t bytes) { size_t at = n; n += round256(bytes); return base ? base + at : nullptr; };
+  AttnMat* m[3] = {&a.q, &a.k, &a.v};
+  for (int i = 0; i < 3; ++i) n = lay_packed(dtype, a, *m[i], i ? a.nk : a.nq, i ? a.kv_heads : a.heads, base, n, from[i]);
   a.pk = rows_packed(a);
   a.splits = parts(dtype, a);
   const int64_t rows = (int64_t)a.batch * a.heads * a.nq;
@@ -1007,12 +1125,17 @@ size_t lay_fwd(int dtype, AttnArgs& a, char* base) {
   if (a.k_doc) a.k_tab = (int4*)take((size_t)a.batch * ceil_div(a.nk, keys_of(dtype)) * sizeof(int4));
   return n;
 }
-size_t lay_bwd(int dtype, AttnArgs& a, char* base) {
+size_t lay_bwd(int dtype, AttnArgs& a, char* base, AttnMat* from) {
   size_t n = 0;
   auto take = [&](size_t bytes) { size_t at = n; n += round256(bytes); return base ? base + at : nullptr; };
-  a.delta = (float*)take((size_t)a.batch * a.heads * a.nq * 4);
+  AttnMat* m[4] = {&a.q, &a.k, &a.v, &a.dout};
+  for (int i = 0; i < 4; ++i) {
+    const bool keys = i == 1 || i == 2;
+    n = lay_packed(dtype, a, *m[i], keys ? a.nk : a.nq, keys ? a.kv_heads : a.heads, base, n, from[i]);
+  }
+  a.rows = (float*)take((size_t)a.batch * a.heads * ceil_div(a.nq, ROWS) * 4 * ROW_INFO * 4);
   if (a.k_doc) {
-    a.k_tab = (int4*)take((size_t)a.batch * ceil_div(a.nk, keys_of(dtype)) * sizeof(int4));
+    a.k_tab = (int4*)take((size_t)a.batch * ceil_div(a.nk, dq_keys_of(dtype, a)) * sizeof(int4));
     a.q_tab = (int4*)take((size_t)a.batch * ceil_div(a.nq, QT) * sizeof(int4));
   }
   if (a.grad_bias) {
@@ -1032,11 +1155,30 @@ void launch_docs(const int32_t* doc, const int32_t* len, int n, int batch, int t
   XP_LAUNCH("k_attn_docs", 4.0 * batch * n, k_attn_docs, dim3((unsigned)ceil_div(n, tile), batch), dim3(64), 0, s, doc, len, n, tile, tab);
 }
 
+void launch_pack(int dtype, const AttnArgs& a, const AttnMat& from, const AttnMat& to, int64_t tokens, int64_t heads, hipStream_t s) {
+  if (!from.p) return;
+  const int64_t rows = (int64_t)a.batch * tokens * heads, n = rows * a.ldim;
+  const unsigned blocks = (unsigned)std::min<int64_t>(ceil_div(n, 256 * 8), 4096);
+  if (dtype == DT_BF16)
+    XP_LAUNCH("k_attn_pack<bf16>", 4.0 * n, k_attn_pack<bf16_t>, dim3(blocks), dim3(256), 0, s, from, (bf16_t*)to.p, rows, (int)tokens, (int)heads, a.dim, a.ldim);
+  else
+    XP_LAUNCH("k_attn_pack<f32>", 8.0 * n, k_attn_pack<float>, dim3(blocks), dim3(256), 0, s, from, (float*)to.p, rows, (int)tokens, (int)heads, a.dim, a.ldim);
+}
+
 template <typename T, int DP, bool GEN>
 void fwd(const AttnArgs& a, hipStream_t s) {
   const double flops = 4.0 * a.batch * a.heads * a.nq * (double)a.nk * a.dim;
-  const int64_t groups = ceil_div((int64_t)a.nq * a.pk, ROWS) * (a.heads / a.pk) * a.batch * a.splits;
-  XP_LAUNCH(sizeof(T) == 2 ? "k_attn_fwd<bf16>" : "k_attn_fwd<f32>", flops, (k_attn_fwd<T, DP, GEN>), dim3((unsigned)groups), dim3(256), 0, s, a);
+  auto run = [&](auto qb) {
+    constexpr int QB = decltype(qb)::value;
+    const int64_t groups = ceil_div((int64_t)a.nq * a.pk, ROWS * QB) * (a.heads / a.pk) * a.batch * a.splits;
+    XP_LAUNCH(sizeof(T) == 2 ? "k_attn_fwd<bf16>" : "k_attn_fwd<f32>", flops, (k_attn_fwd<T, DP, GEN, QB>), dim3((unsigned)groups), dim3(256), 0, s, a);
+  };
+  if constexpr (sizeof(T) == 2) {
+    if (wide(a)) run(std::integral_constant<int, 2>{});
+    else run(std::integral_constant<int, 1>{});
+  } else {
+    run(std::integral_constant<int, 1>{});
+  }
   if (a.splits > 1) {
     const int64_t rows = (int64_t)a.batch * a.heads * a.nq;
     XP_LAUNCH("k_attn_join", 4.0 * rows * a.splits * DP, (k_attn_join<T, DP>), dim3((unsigned)ceil_div(rows, 4)), dim3(256), 0, s, a);
@@ -1082,25 +1224,36 @@ void by_kind(int dtype, const AttnArgs& a, F&& f) {
 
 size_t attn_fwd_bytes(int dtype, const AttnArgs& a) {
   AttnArgs c = a;
-  return lay_fwd(dtype, c, nullptr);
+  AttnMat from[3];
+  return lay_fwd(dtype, c, nullptr, from);
 }
 size_t attn_bwd_bytes(int dtype, const AttnArgs& a) {
   AttnArgs c = a;
-  return lay_bwd(dtype, c, nullptr);
+  AttnMat from[4];
+  return lay_bwd(dtype, c, nullptr, from);
 }
 
 hipError_t launch_attn_fwd(int dtype, AttnArgs a, void* workspace, hipStream_t s) {
-  lay_fwd(dtype, a, (char*)workspace);
+  AttnMat from[3];
+  lay_fwd(dtype, a, (char*)workspace, from);
+  launch_pack(dtype, a, from[0], a.q, a.nq, a.heads, s);
+  launch_pack(dtype, a, from[1], a.k, a.nk, a.kv_heads, s);
+  launch_pack(dtype, a, from[2], a.v, a.nk, a.kv_heads, s);
   if (a.k_doc) launch_docs(a.k_doc, a.k_len, a.nk, a.batch, keys_of(dtype), a.k_tab, s);
   by_kind(dtype, a, [&](auto t, auto d, auto g) { fwd<decltype(t), decltype(d)::value, decltype(g)::value>(a, s); });
   return hipGetLastError();
 }
 
 hipError_t launch_attn_bwd(int dtype, AttnArgs a, void* workspace, hipStream_t s) {
+  AttnMat from[4];
   a.pk = a.splits = 1;
-  lay_bwd(dtype, a, (char*)workspace);
+  lay_bwd(dtype, a, (char*)workspace, from);
+  launch_pack(dtype, a, from[0], a.q, a.nq, a.heads, s);
+  launch_pack(dtype, a, from[1], a.k, a.nk, a.kv_heads, s);
+  launch_pack(dtype, a, from[2], a.v, a.nk, a.kv_heads, s);
+  launch_pack(dtype, a, from[3], a.dout, a.nq, a.heads, s);
   if (a.k_doc) {
-    launch_docs(a.k_doc, a.k_len, a.nk, a.batch, keys_of(dtype), a.k_tab, s);
+    launch_docs(a.k_doc, a.k_len, a.nk, a.batch, dq_keys_of(dtype, a), a.k_tab, s);
     launch_docs(a.q_doc, a.q_len, a.nq, a.batch, QT, a.q_tab, s);
   }
   by_kind(dtype, a, [&](auto t, auto d, auto g) { bwd<decltype(t), decltype(d)::value, decltype(g)::value>(a, s); });

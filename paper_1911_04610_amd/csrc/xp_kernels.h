@@ -435,12 +435,12 @@ struct AttnArgs {
   float* grad_bias;                  // backward, optional: added to
   float* stats;                      // [batch][heads][nq][2]: largest score, sum of exp(score - largest)
   // set by the launcher: query rows of how many heads a workgroup holds together, parts
-  // of the keys and their results, documents of each tile, sums of P dP, sums of score
+  // of the keys and their results, documents of each tile, what the gradients need of each query row, sums of score
   // gradients along diagonals
-  int pk, splits, near;
+  int pk, splits, near, ldim;        // ldim: dim in whole chunks of 16 bytes
   float *part_o, *part_ml;
   int4 *k_tab, *q_tab;
-  float *delta, *diag, *tail;
+  float *rows, *diag, *tail;
 };
 size_t attn_fwd_bytes(int dtype, const AttnArgs& a);
 size_t attn_bwd_bytes(int dtype, const AttnArgs& a);
