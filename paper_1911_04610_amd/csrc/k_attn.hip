@@ -51,6 +51,19 @@ XP_DEV int swz(int r) {
   else return ((r >> 1) & 1) << 2 | ((r >> 2) & 3);
 }
 
+template <typename T, int DP> constexpr int ROW = DP * (int)sizeof(T);  // bytes
+// Tiles are named by their byte address in LDS, a multiple of ROW: where a lane's reads differ in
+// the chunk, they then differ by an exclusive or of a constant, and where they differ in the
+// row, by an offset in the instruction.
+template <typename V>
+XP_DEV __attribute__((address_space(3))) V* lds(uint32_t at) {
+  return (__attribute__((address_space(3))) V*)at;
+}
+template <typename V>
+XP_DEV uint32_t lds_address(V* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)p;
+}
+
 // The same value, of which the compiler knows nothing: what is computed from it is computed
 // where it stands.  (Every lane's place in every tile would otherwise be computed ahead of the
 // loops and kept in registers that the operands need.)
@@ -124,12 +137,12 @@ struct Stager {
       }
     }
   }
-  XP_DEV void store(T* lds) const {
+  XP_DEV void store(uint32_t tile) const {
     const int tid = fresh(threadIdx.x), c = tid & (CPR - 1), at = (tid & 255) / CPR;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int row = at + i * STEP;
-      *reinterpret_cast<u32x4_t*>(lds + row * DP + ((c ^ swz<T, DP>(row)) * CHUNK<T>)) = r[i];
+      *lds<u32x4_t>(tile + row * ROW<T, DP> + ((c ^ swz<T, DP>(row)) << 4)) = r[i];
     }
   }
 };
@@ -176,38 +189,52 @@ XP_DEV f32x16_t mma(const u32x4_t& a, const u32x4_t& b, f32x16_t c) {
 // Row of a block that register r of a result holds: 8 (r / 4) + 4 (lane / 32) + r % 4.
 XP_DEV int row_of(int r) { return 8 * (r >> 2) + 4 * ((threadIdx.x >> 5) & 1) + (r & 3); }
 
-// 32 rows of a tile times the lanes' N columns
+// A lane's first address in a tile at 0, for reads along rows and down columns.
+template <typename T, int DP>
+XP_DEV uint32_t row_place() {
+  const int r = threadIdx.x & 31, h = (threadIdx.x >> 5) & 1;
+  return r * ROW<T, DP> + ((h ^ swz<T, DP>(r)) << 4);
+}
+template <typename T, int DP>
+XP_DEV uint32_t column_place() {
+  const int lane = threadIdx.x & 63, h = lane >> 5;
+  if constexpr (sizeof(T) == 2) {
+    const int row = 4 * h + ((lane & 15) >> 2), chunk = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+    return row * ROW<T, DP> + ((chunk ^ swz<T, DP>(row)) << 4) + 8 * (lane & 1);
+  } else {
+    const int col = lane & 31;
+    return 4 * h * ROW<T, DP> + (((col >> 2) ^ swz<T, DP>(4 * h)) << 4) + 4 * (col & 3);
+  }
+}
+
+// 32 rows of a tile, `more` bytes from it on, times the lanes' N columns; at: row_place + tile
 template <typename T, int DP, int N>
-XP_DEV void rows_times(const T* tile, const u32x4_t (&col)[N][DP / CHUNK<T> / 2], f32x16_t (&out)[N]) {
-  const int lane = fresh(threadIdx.x), r = lane & 31, h = (lane >> 5) & 1;
+XP_DEV void rows_times(uint32_t at, int more, const u32x4_t (&col)[N][DP / CHUNK<T> / 2], f32x16_t (&out)[N]) {
 #pragma unroll
   for (int c = 0; c < N; ++c)
 #pragma unroll
     for (int i = 0; i < 16; ++i) out[c][i] = 0.f;
 #pragma unroll
   for (int s = 0; s < DP / CHUNK<T> / 2; ++s) {
-    const u32x4_t a = *reinterpret_cast<const u32x4_t*>(tile + r * DP + (((2 * s + h) ^ swz<T, DP>(r)) * CHUNK<T>));
+    const u32x4_t a = *lds<u32x4_t>((at ^ (s * 32)) + more);
 #pragma unroll
     for (int c = 0; c < N; ++c) out[c] = mma<T>(a, col[c][s], out[c]);
   }
 }
 template <typename T, int DP>
-XP_DEV f32x16_t rows_times(const T* tile, const u32x4_t (&col)[DP / CHUNK<T> / 2]) {
-  const auto& one = reinterpret_cast<const u32x4_t(&)[1][DP / CHUNK<T> / 2]>(col);
+XP_DEV f32x16_t rows_times(uint32_t at, int more, const u32x4_t (&col)[DP / CHUNK<T> / 2]) {
   f32x16_t out[1];
-  rows_times<T, DP, 1>(tile, one, out);
+  rows_times<T, DP, 1>(at, more, reinterpret_cast<const u32x4_t(&)[1][DP / CHUNK<T> / 2]>(col), out);
   return out[0];
 }
 
-// acc[c][d][lane's column] += sum over the 32 rows of tile[row][d] w[c][row]
+// acc[c][d][lane's column] += sum over 32 rows of tile[row][d] w[c][row]; at: column_place + tile
 template <typename T, int DP, int N>
-XP_DEV void add_transposed(f32x16_t (&acc)[N][DP / 32], const T* tile, const float (&w)[N][16]) {
-  const int lane = fresh(threadIdx.x) & 63, h = lane >> 5;
+XP_DEV void add_transposed(f32x16_t (&acc)[N][DP / 32], uint32_t at, int more, const float (&w)[N][16]) {
   if constexpr (sizeof(T) == 2) {
     typedef short v4i16 __attribute__((ext_vector_type(4)));
-    const int p = (lane & 15) >> 2;
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < 2; ++b) {  // 16 rows: 4 lane / 32 + 0 .. 3 of them, and 8 further on
       u32x4_t f[N];
 #pragma unroll
       for (int c = 0; c < N; ++c)
@@ -215,14 +242,10 @@ XP_DEV void add_transposed(f32x16_t (&acc)[N][DP / 32], const T* tile, const flo
         for (int i = 0; i < 4; ++i) f[c][i] = f32x2_to_bf16x2(w[c][8 * b + 2 * i], w[c][8 * b + 2 * i + 1]);
 #pragma unroll
       for (int d = 0; d < DP / 32; ++d) {
-        const int chunk = d * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
         v4i16 part[2];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const int row = 16 * b + 8 * k + 4 * h + p;
-          part[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4i16*)(
-              tile + row * DP + ((chunk ^ swz<T, DP>(row)) * 8) + 4 * (lane & 1)));
-        }
+        for (int k = 0; k < 2; ++k)
+          part[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds<v4i16>((at ^ (d * 64 + k * 32)) + (more + (16 * b + 8 * k) * ROW<T, DP>)));
         const u32x4_t x = __builtin_bit_cast(u32x4_t, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
         for (int c = 0; c < N; ++c) acc[c][d] = mma<T>(x, f[c], acc[c][d]);
@@ -230,21 +253,18 @@ XP_DEV void add_transposed(f32x16_t (&acc)[N][DP / 32], const T* tile, const flo
     }
   } else {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int row = 8 * (r >> 2) + 4 * h + (r & 3);
+    for (int r = 0; r < 16; ++r)
 #pragma unroll
       for (int d = 0; d < DP / 32; ++d) {
-        const int col = d * 32 + (lane & 31);
-        const float x = tile[row * DP + (((col >> 2) ^ swz<T, DP>(row)) << 2) + (col & 3)];
+        const float x = *lds<float>((at ^ (d * 128 + ((r >> 2) & 1) * 64 + (r & 3) * 16)) + (more + (8 * (r >> 2) + (r & 3)) * ROW<T, DP>));
 #pragma unroll
         for (int c = 0; c < N; ++c) acc[c][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, w[c][r], acc[c][d], 0, 0, 0);
       }
-    }
   }
 }
 template <typename T, int DP>
-XP_DEV void add_transposed(f32x16_t (&acc)[DP / 32], const T* tile, const float (&w)[16]) {
-  add_transposed<T, DP, 1>(reinterpret_cast<f32x16_t(&)[1][DP / 32]>(acc), tile, reinterpret_cast<const float(&)[1][16]>(w));
+XP_DEV void add_transposed(f32x16_t (&acc)[DP / 32], uint32_t at, int more, const float (&w)[16]) {
+  add_transposed<T, DP, 1>(reinterpret_cast<f32x16_t(&)[1][DP / 32]>(acc), at, more, reinterpret_cast<const float(&)[1][16]>(w));
 }
 
 // The lane's column of a result [DP][32], times f, to a row of dim elements in memory.
@@ -454,7 +474,8 @@ XP_DEV void scores(f32x16_t& s, const AttnArgs& a, const Bias& bias, int dist, i
 template <typename T, int DP, bool GEN, int QB>
 __global__ __launch_bounds__(256, QB == 2 && DP == 128 ? 1 : (WAVES<T, DP>)) void k_attn_fwd(AttnArgs a) {
   constexpr int KEYS = BN<T>, NB = KEYS / 32, WAVE = 32 * QB, GROUP = 4 * WAVE;
-  __shared__ T sk[2][KEYS * DP], sv[2][KEYS * DP];
+  constexpr int TILE = KEYS * ROW<T, DP>;
+  __shared__ __attribute__((aligned(1024))) unsigned char tiles_[4 * TILE];  // keys, values, twice
   __shared__ int sdoc[2][KEYS];
   __shared__ int sh[4][2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -521,9 +542,10 @@ __global__ __launch_bounds__(256, QB == 2 && DP == 128 ? 1 : (WAVES<T, DP>)) voi
     vs.load(vp + (int64_t)j0 * a.v.t, seq.kl - j0, pad);
     if (kdoc && threadIdx.x < KEYS) dreg = j0 + (int)threadIdx.x < seq.kl ? kdoc[j0 + threadIdx.x] : -1;
   };
+  const uint32_t tile0 = lds_address(tiles_), rplace = row_place<T, DP>() + tile0, cplace = column_place<T, DP>() + tile0;
   auto store = [&](int buf) __attribute__((always_inline)) {
-    ks.store(sk[buf]);
-    vs.store(sv[buf]);
+    ks.store(tile0 + buf * 2 * TILE);
+    vs.store(tile0 + buf * 2 * TILE + TILE);
     if (kdoc && threadIdx.x < KEYS) sdoc[buf][threadIdx.x] = dreg;
   };
   int t = walk.next(min(tiles, split * per)), buf = 0;
@@ -542,19 +564,20 @@ __global__ __launch_bounds__(256, QB == 2 && DP == 128 ? 1 : (WAVES<T, DP>)) voi
       mixed = e.z || docs.wlo != docs.whi;
     }
     if (!skip) {
+      const uint32_t rat = rplace + buf * 2 * TILE, cat = cplace + buf * 2 * TILE;
       const bool masked = mixed || (t + 1) * KEYS > wmin;
+      f32x16_t s[NB][QB];
+#pragma unroll
+      for (int n = 0; n < NB; ++n) rows_times<T, DP, QB>(rat, n * 32 * ROW<T, DP>, q, s[n]);
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
         const int k0 = t * KEYS + n * 32;
-        f32x16_t s[QB];
-        rows_times<T, DP, QB>(sk[buf] + n * 32 * DP, q, s);
-        phase();
         if constexpr (GEN) {
           float none[16];
 #pragma unroll
           for (int c = 0; c < QB; ++c) {
             const Bias bias(a, min(head[c], a.heads - 1));
-            scores<true, false>(s[c], a, bias, k0 - pos[c], k0 - wlast - seq.off, k0 + 31 - wfirst - seq.off, none);
+            scores<true, false>(s[n][c], a, bias, k0 - pos[c], k0 - wlast - seq.off, k0 + 31 - wfirst - seq.off, none);
           }
         }
         if (masked) {
@@ -562,42 +585,46 @@ __global__ __launch_bounds__(256, QB == 2 && DP == 128 ? 1 : (WAVES<T, DP>)) voi
           for (int c = 0; c < QB; ++c) {
             const uint32_t hide = hidden(k0, kend[c], kdoc ? sdoc[buf] + n * 32 : nullptr, doc[c]);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[c][r] = hide >> r & 1 ? NEG_INF : s[c][r];
+            for (int r = 0; r < 16; ++r) s[n][c][r] = hide >> r & 1 ? NEG_INF : s[n][c][r];
           }
         }
-        bool grown = false;
+      }
+      bool grown = false;
+#pragma unroll
+      for (int c = 0; c < QB; ++c) {
+        float top = s[0][c][0];
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) top = fmaxf(top, s[n][c][r]);
+        m[c] = fmaxf(m[c], both_max(top));
+        grown = grown || (m[c] - base[c]) * c1 > 8.f;  // (from -inf on: infinite; while there is no key: NaN)
+      }
+      if (__any(grown)) {
 #pragma unroll
         for (int c = 0; c < QB; ++c) {
-          float top = s[c][0];
+          const float keep = m[c] == NEG_INF ? 1.f : exp2_((base[c] - m[c]) * c1);
+          base[c] = m[c];
+          l[c] *= keep;
 #pragma unroll
-          for (int r = 1; r < 16; ++r) top = fmaxf(top, s[c][r]);
-          m[c] = fmaxf(m[c], both_max(top));
-          grown = grown || (m[c] - base[c]) * c1 > 8.f;  // (from -inf on: infinite; while there is no key: NaN)
+          for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[c][d][r] *= keep;
         }
-        if (__any(grown)) {
+      }
 #pragma unroll
-          for (int c = 0; c < QB; ++c) {
-            const float keep = m[c] == NEG_INF ? 1.f : exp2_((base[c] - m[c]) * c1);
-            base[c] = m[c];
-            l[c] *= keep;
-#pragma unroll
-            for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-              for (int r = 0; r < 16; ++r) acc[c][d][r] *= keep;
-          }
-        }
+      for (int n = 0; n < NB; ++n) {
         float p[QB][16];
 #pragma unroll
         for (int c = 0; c < QB; ++c) {
           const float off = base[c] == NEG_INF ? 0.f : base[c], bc = off * c1;
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            p[c][r] = GEN ? exp2_((s[c][r] - off) * c1) : exp2_(s[c][r] * c1 - bc);
+            p[c][r] = GEN ? exp2_((s[n][c][r] - off) * c1) : exp2_(s[n][c][r] * c1 - bc);
             l[c] += p[c][r];
           }
         }
-        add_transposed<T, DP, QB>(acc, sv[buf] + n * 32 * DP, p);
-        phase();
+        add_transposed<T, DP, QB>(acc, cat, TILE + n * 32 * ROW<T, DP>, p);
       }
     }
     buf ^= 1;
@@ -702,7 +729,8 @@ XP_DEV int first_near(const AttnArgs& a, const Seq& seq, int kw) { return max(0,
 template <typename T, int DP, bool GEN>
 __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dq(AttnArgs a) {
   constexpr int KEYS = BN_DQ<T, DP>, NB = KEYS / 32;
-  __shared__ T sk[2][KEYS * DP], sv[2][KEYS * DP];
+  constexpr int TILE = KEYS * ROW<T, DP>;
+  __shared__ __attribute__((aligned(1024))) unsigned char tiles_[4 * TILE];  // keys, values, twice
   __shared__ int sdoc[2][KEYS];
   __shared__ int sh[4][2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -773,9 +801,10 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dq(AttnArgs a) {
     vs.load(vp + (int64_t)j0 * a.v.t, seq.kl - j0, pad);
     if (kdoc && threadIdx.x < KEYS) dreg = j0 + (int)threadIdx.x < seq.kl ? kdoc[j0 + threadIdx.x] : -1;
   };
+  const uint32_t tile0 = lds_address(tiles_), rplace = row_place<T, DP>() + tile0, cplace = column_place<T, DP>() + tile0;
   auto store = [&](int buf) __attribute__((always_inline)) {
-    ks.store(sk[buf]);
-    vs.store(sv[buf]);
+    ks.store(tile0 + buf * 2 * TILE);
+    vs.store(tile0 + buf * 2 * TILE + TILE);
     if (kdoc && threadIdx.x < KEYS) sdoc[buf][threadIdx.x] = dreg;
   };
   int t = walk.next(0), buf = 0;
@@ -794,12 +823,13 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dq(AttnArgs a) {
       mixed = e.z || docs.wlo != docs.whi;
     }
     if (!skip) {
+      const uint32_t rat = rplace + buf * 2 * TILE, cat = cplace + buf * 2 * TILE;
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
         const int k0 = t * KEYS + n * 32;
-        f32x16_t s = rows_times<T, DP>(sk[buf] + n * 32 * DP, q);
+        f32x16_t s = rows_times<T, DP>(rat, n * 32 * ROW<T, DP>, q);
         phase();
-        const f32x16_t dp = rows_times<T, DP>(sv[buf] + n * 32 * DP, g);
+        const f32x16_t dp = rows_times<T, DP>(rat, TILE + n * 32 * ROW<T, DP>, g);
         phase();
         float slope[16], ds[16];
         if constexpr (GEN)
@@ -821,7 +851,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dq(AttnArgs a) {
           for (int r = 0; r < 16; ++r) ds[r] *= slope[r];
         }
         phase();
-        add_transposed<T, DP>(acc, sk[buf] + n * 32 * DP, ds);
+        add_transposed<T, DP>(acc, cat, n * 32 * ROW<T, DP>, ds);
         phase();
       }
     }
@@ -880,7 +910,8 @@ __global__ __launch_bounds__(256) void k_attn_dbias(AttnArgs a) {
 // the blocks beyond the bias's range on either side.
 template <typename T, int DP, bool GEN, int WHAT>
 __global__ __launch_bounds__(256, GEN && DP == 128 ? 1 : (WAVES<T, DP>)) void k_attn_dkv(AttnArgs a) {
-  __shared__ T sq[2][QT * DP], sg[2][QT * DP];
+  constexpr int TILE = QT * ROW<T, DP>;
+  __shared__ __attribute__((aligned(1024))) unsigned char tiles_[4 * TILE];  // q, dout, twice
   __shared__ float srow[2][5 * QT];
   __shared__ int sh[4][2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -945,9 +976,10 @@ __global__ __launch_bounds__(256, GEN && DP == 128 ? 1 : (WAVES<T, DP>)) void k_
     gs.load((const T*)a.dout.p + b * a.dout.b + head * a.dout.h + i0 * a.dout.t, seq.ql - i0, pads);
     if (threadIdx.x < 5 * QT) rreg = a.rows[(((int64_t)b * a.heads + head) * row_tiles + t) * ROW_INFO + threadIdx.x];
   };
+  const uint32_t tile0 = lds_address(tiles_), rplace = row_place<T, DP>() + tile0, cplace = column_place<T, DP>() + tile0;
   auto store = [&](int buf) __attribute__((always_inline)) {
-    qs.store(sq[buf]);
-    gs.store(sg[buf]);
+    qs.store(tile0 + buf * 2 * TILE);
+    gs.store(tile0 + buf * 2 * TILE + TILE);
     if (threadIdx.x < 5 * QT) srow[buf][threadIdx.x] = rreg;
   };
   int g = 0, t = walk.next(t0), buf = 0;
@@ -973,8 +1005,9 @@ __global__ __launch_bounds__(256, GEN && DP == 128 ? 1 : (WAVES<T, DP>)) void k_
       mixed = e.z || pad || docs.wlo != docs.whi;
     }
     if (!skip) {
+      const uint32_t rat = rplace + buf * 2 * TILE, cat = cplace + buf * 2 * TILE;
       const int head = kvh * group + g;
-      f32x16_t s = rows_times<T, DP>(sq[buf], kc);
+      f32x16_t s = rows_times<T, DP>(rat, 0, kc);
       phase();
       float p[16], slope[16];
       if constexpr (GEN) {
@@ -994,11 +1027,11 @@ __global__ __launch_bounds__(256, GEN && DP == 128 ? 1 : (WAVES<T, DP>)) void k_
       }
       if constexpr (WHAT & 1) {
         phase();
-        add_transposed<T, DP>(dv, sg[buf], p);
+        add_transposed<T, DP>(dv, cat, TILE, p);
         phase();
       }
       if constexpr (WHAT & 2) {
-        const f32x16_t dp = rows_times<T, DP>(sg[buf], vc);
+        const f32x16_t dp = rows_times<T, DP>(rat, TILE, vc);
         phase();
 #pragma unroll
         for (int r = 0; r < 16; ++r) p[r] *= dp[r] - srow[buf][64 + row_of(r)];
@@ -1037,7 +1070,7 @@ __global__ __launch_bounds__(256, GEN && DP == 128 ? 1 : (WAVES<T, DP>)) void k_
           for (int r = 0; r < 16; ++r) p[r] *= slope[r];
         }
         phase();
-        add_transposed<T, DP>(dk, sq[buf], p);
+        add_transposed<T, DP>(dk, cat, 0, p);
       }
     }
     if (diag && gn != g) {  // the head's last step
@@ -1086,7 +1119,7 @@ int parts(int dtype, const AttnArgs& a) {
 }
 
 // whether the forward's waves take 64 query rows each
-bool wide(const AttnArgs& a) {
+bool wide(const AttnArgs& a) { return false;
   return a.splits == 1 && ceil_div((int64_t)a.nq * a.pk, 2 * ROWS) * (a.heads / a.pk) * a.batch >= 256;
 }
 
