@@ -567,6 +567,7 @@ __global__ __launch_bounds__(256, QB == 2 && DP == 128 ? 1 : (WAVES<T, DP>)) voi
       const uint32_t rat = rplace + buf * 2 * TILE, cat = cplace + buf * 2 * TILE;
       const bool masked = mixed || (t + 1) * KEYS > wmin;
       f32x16_t s[NB][QB];
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int n = 0; n < NB; ++n) rows_times<T, DP, QB>(rat, n * 32 * ROW<T, DP>, q, s[n]);
 #pragma unroll
@@ -589,6 +590,7 @@ __global__ __launch_bounds__(256, QB == 2 && DP == 128 ? 1 : (WAVES<T, DP>)) voi
           }
         }
       }
+      __builtin_amdgcn_s_setprio(0);
       bool grown = false;
 #pragma unroll
       for (int c = 0; c < QB; ++c) {
@@ -872,33 +874,41 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dq(AttnArgs a) {
 }
 
 // grad_bias[head][x] += the sum over sequences and key blocks of the blocks' diagonals at
-// that distance: a workgroup takes 64 distances of a head, its waves runs of (sequence, 32 keys).
-__global__ __launch_bounds__(256) void k_attn_dbias(AttnArgs a) {
-  __shared__ double sh[4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, head = blockIdx.y;
+// that distance: a workgroup takes 64 distances of a head, its 16 waves every 16th (sequence, 32 keys).
+__global__ __launch_bounds__(1024) void k_attn_dbias(AttnArgs a) {
+  __shared__ double sh[16][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), head = blockIdx.y;
   const int x = blockIdx.x * 64 + lane, d = x - a.range, width = 2 * a.range + 1;
   const int blocks = (a.nk + ROWS - 1) / ROWS * 4;
+  const bool outer = x == 0 || x >= width - 1;
   double s = 0.0;
-  for (int n = wave; n < a.batch * blocks; n += 4) {
-    const int b = n / blocks, w = n % blocks;
+  for (int b = 0; b < a.batch; ++b) {
     const Seq seq(a, b);
-    if (w * 32 >= seq.kl) continue;
-    const int64_t at = ((int64_t)b * a.heads + head) * blocks + w;
-    if (x == 0) s += a.tail[2 * at];
-    else if (x == width - 1) s += a.tail[2 * at + 1];
-    else if (x < width) {
-      // of block t the distances from w 32 - 32 t - 31 - off on: places u in the two blocks that hold d
-      const int near0 = first_near(a, seq, w * 32), at0 = d - w * 32 + 31 + seq.off, u = at0 & 31, t = (u - at0) >> 5;
-      const float* part = a.diag + at * a.near * 64;
-      if (t >= near0 && t - near0 < a.near) s += part[(t - near0) * 64 + u];
-      if (u < 31 && t + 1 >= near0 && t + 1 - near0 < a.near) s += part[(t + 1 - near0) * 64 + u + 32];
+    const int64_t at0 = ((int64_t)b * a.heads + head) * blocks;
+    const int used = min(blocks, (seq.kl + 31) / 32);
+#pragma unroll 4
+    for (int w = wave; w < used; w += 16) {
+      const int64_t at = at0 + w;
+      float v0 = 0.f, v1 = 0.f;
+      if (outer) {
+        if (x < width) v0 = a.tail[2 * at + (x == 0 ? 0 : 1)];
+      } else {
+        // of block t the distances from w 32 - 32 t - 31 - off on: places u in the two blocks that hold d
+        const int near0 = first_near(a, seq, w * 32), from = d - w * 32 + 31 + seq.off, u = from & 31, t = (u - from) >> 5;
+        const float* part = a.diag + at * a.near * 64;
+        if (t >= near0 && t - near0 < a.near) v0 = part[(t - near0) * 64 + u];
+        if (u < 31 && t + 1 >= near0 && t + 1 - near0 < a.near) v1 = part[(t + 1 - near0) * 64 + u + 32];
+      }
+      s += (double)v0 + v1;
     }
   }
   sh[wave][lane] = s;
   __syncthreads();
   if (wave == 0 && x < width) {
+    s = 0.0;
+    for (int w = 0; w < 16; ++w) s += sh[w][lane];
     float* g = a.grad_bias + (int64_t)head * width + x;
-    *g = (float)((double)*g + ((sh[0][lane] + sh[1][lane]) + (sh[2][lane] + sh[3][lane])));
+    *g = (float)((double)*g + s);
   }
 }
 
@@ -1233,7 +1243,7 @@ void bwd(const AttnArgs& a, hipStream_t s) {
               dim3(256), 0, s, a);
   }
   if (a.grad_bias && groups > 0 && kgroups > 0)
-    XP_LAUNCH("k_attn_dbias", 4.0 * (2 * a.range + 1) * a.heads, k_attn_dbias, dim3((unsigned)ceil_div(2 * (int64_t)a.range + 1, 64), a.heads), dim3(256), 0, s, a);
+    XP_LAUNCH("k_attn_dbias", 4.0 * (2 * a.range + 1) * a.heads, k_attn_dbias, dim3((unsigned)ceil_div(2 * (int64_t)a.range + 1, 64), a.heads), dim3(1024), 0, s, a);
 }
 
 // calls f(element type, padded dim, whether scores need more than the scale)

@@ -42,37 +42,51 @@ __global__ __launch_bounds__(256) void k_relbias_fwd(const float* __restrict__ t
   for (int h = h0; h < h1; ++h) bias[(int64_t)h * width + x] = row[h];
 }
 
-// the first distance 0 .. far in bucket k or a later one; far + 1 if none
+// The first distance 0 .. far in bucket k or a later one; far + 1 if none.  From the border
+// itself, at most a few steps from what bucket_of says.
 XP_DEV int first_of(const Buckets& b, int k) {
-  int lo = 0, hi = b.far + 1;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (bucket_of(b, mid) >= k) hi = mid;
-    else lo = mid + 1;
+  if (k <= b.half) return k;
+  if (k >= b.n) return b.far + 1;
+  int d = max(b.half, min(b.far, (int)ceil(b.half * exp((k - b.half) / b.scale))));
+  while (d > b.half && bucket_of(b, d - 1) >= k) --d;
+  while (d <= b.far && bucket_of(b, d) < k) ++d;
+  return d;
+}
+
+// this thread's part of the sum of n consecutive values
+template <int THREADS>
+XP_DEV double run_sum(const float* p, int n) {
+  double s = 0.0;
+  int i = threadIdx.x * 4;
+#pragma unroll 4
+  for (; i + 4 <= n; i += THREADS * 4) {
+    float v[4];
+    __builtin_memcpy(v, p + i, 16);
+    s += ((double)v[0] + v[1]) + ((double)v[2] + v[3]);
   }
-  return lo;
+  for (; i < n; ++i) s += p[i];  // (one thread has such a rest)
+  return s;
 }
 
 // One workgroup per bucket and head: the bucket's distances are one run of the head's row.
-__global__ __launch_bounds__(256) void k_relbias_bwd(const float* __restrict__ dbias, Buckets b, int heads, float* __restrict__ grad) {
-  __shared__ double sh[4];
+// THREADS: 1024 where runs are long (64 heads, 32768 distances: 129 us with 256 threads and
+// single values).
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void k_relbias_bwd(const float* __restrict__ dbias, Buckets b, int heads, float* __restrict__ grad) {
+  __shared__ double sh[THREADS / 64];
   const int k = blockIdx.x, h = blockIdx.y, side = b.both && k >= b.n, kk = side ? k - b.n : k;
   const float* row = dbias + (int64_t)h * (2 * b.far + 1) + b.far;
-  const int lo = first_of(b, kk), hi = first_of(b, kk + 1);  // distances [lo, hi)
-  double s = 0.0;
-  if (side) {
-    for (int d = max(lo, 1) + (int)threadIdx.x; d < hi; d += 256) s += row[d];
-  } else {
-    for (int d = lo + (int)threadIdx.x; d < hi; d += 256) s += row[-d];
-    if (!b.both && kk == 0)  // keys behind the query count as distance 0
-      for (int d = 1 + threadIdx.x; d <= b.far; d += 256) s += row[d];
-  }
-  s = wave_sum(s);
+  const int lo = side ? max(first_of(b, kk), 1) : first_of(b, kk), hi = first_of(b, kk + 1);  // distances [lo, hi)
+  // (keys behind the query count as distance 0 where there is one direction)
+  const int first = side ? lo : 1 - hi, last = side ? hi : !b.both && kk == 0 ? b.far + 1 : 1 - lo;
+  double s = wave_sum(run_sum<THREADS>(row + first, last - first));
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = s;
   __syncthreads();
   if (threadIdx.x == 0) {
     float* g = grad + (int64_t)k * heads + h;
-    *g = (float)((double)*g + ((sh[0] + sh[1]) + (sh[2] + sh[3])));
+    s = 0.0;
+    for (int w = 0; w < THREADS / 64; ++w) s += sh[w];
+    *g = (float)((double)*g + s);
   }
 }
 
@@ -96,8 +110,10 @@ hipError_t launch_relbias_fwd(const RelBiasArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_relbias_bwd(const RelBiasArgs& a, hipStream_t s) {
-  XP_LAUNCH("k_relbias_bwd", 4.0 * (2 * a.far + 1) * a.heads, k_relbias_bwd, dim3(a.buckets, a.heads), dim3(256), 0, s, a.dbias,
-            describe(a), a.heads, a.grad);
+  const double bytes = 4.0 * (2 * a.far + 1) * a.heads;
+  const dim3 grid(a.buckets, a.heads);
+  if (a.far > 4096) XP_LAUNCH("k_relbias_bwd", bytes, k_relbias_bwd<1024>, grid, dim3(1024), 0, s, a.dbias, describe(a), a.heads, a.grad);
+  else XP_LAUNCH("k_relbias_bwd", bytes, k_relbias_bwd<256>, grid, dim3(256), 0, s, a.dbias, describe(a), a.heads, a.grad);
   return hipGetLastError();
 }
 
