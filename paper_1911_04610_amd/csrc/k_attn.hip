@@ -26,7 +26,7 @@ namespace xp {
 
 namespace {
 
-constexpr float LOG2E = 1.44269504088896340736f;
+constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 constexpr float NEG_INF = -__builtin_inff();
 constexpr int ROWS = 128;  // query rows (dk, dv: keys) of a workgroup: 4 waves of 32
 constexpr int QT = 32;     // queries of a step of k_attn_dkv
@@ -160,17 +160,26 @@ XP_DEV void ld_column(const T* row, bool valid, int dim, u32x4_t (&f)[DP / CHUNK
   }
 }
 
-// [batch][token][head][dim] with any strides to contiguous rows of ldim elements, zeros behind dim
+// [batch][token][head][dim] with any strides to contiguous rows of ldim elements, zeros behind
+// dim: all that a call has of these, one blockIdx.y each
+struct PackArgs {
+  AttnMat from[4];
+  void* to[4];
+  int64_t rows[4];
+  int tokens[4], heads[4];
+  int dim, ldim;
+};
 template <typename T>
-__global__ __launch_bounds__(256) void k_attn_pack(AttnMat from, T* __restrict__ to, int64_t rows, int tokens, int heads, int dim, int ldim) {
-  const int per = ldim / CHUNK<T>;
-  const int64_t n = rows * per;
+__global__ __launch_bounds__(256) void k_attn_pack(PackArgs a) {
+  const int m = blockIdx.y, per = a.ldim / CHUNK<T>;
+  const AttnMat from = a.from[m];
+  const int64_t n = a.rows[m] * per;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
     const int64_t row = i / per;
-    const int c = (int)(i % per) * CHUNK<T>, h = (int)(row % heads), t = (int)(row / heads % tokens);
-    const int64_t b = row / heads / tokens;
+    const int c = (int)(i % per) * CHUNK<T>, h = (int)(row % a.heads[m]), t = (int)(row / a.heads[m] % a.tokens[m]);
+    const int64_t b = row / a.heads[m] / a.tokens[m];
     const T* p = (const T*)from.p + b * from.b + t * from.t + h * from.h + c;
-    *reinterpret_cast<u32x4_t*>(to + i * CHUNK<T>) = ld_chunk(p, dim - c);
+    *reinterpret_cast<u32x4_t*>((T*)a.to[m] + i * CHUNK<T>) = ld_chunk(p, a.dim - c);
   }
 }
 
@@ -207,48 +216,50 @@ XP_DEV uint32_t column_place() {
   }
 }
 
-// 32 rows of a tile, `more` bytes from it on, times the lanes' N columns; at: row_place + tile
-template <typename T, int DP, int N>
-XP_DEV void rows_times(uint32_t at, int more, const u32x4_t (&col)[N][DP / CHUNK<T> / 2], f32x16_t (&out)[N]) {
-#pragma unroll
-  for (int c = 0; c < N; ++c)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) out[c][i] = 0.f;
-#pragma unroll
-  for (int s = 0; s < DP / CHUNK<T> / 2; ++s) {
-    const u32x4_t a = *lds<u32x4_t>((at ^ (s * 32)) + more);
-#pragma unroll
-    for (int c = 0; c < N; ++c) out[c] = mma<T>(a, col[c][s], out[c]);
-  }
-}
+// 32 rows of a tile, `more` bytes from it on, times the lanes' columns; at: row_place + tile
 template <typename T, int DP>
 XP_DEV f32x16_t rows_times(uint32_t at, int more, const u32x4_t (&col)[DP / CHUNK<T> / 2]) {
-  f32x16_t out[1];
-  rows_times<T, DP, 1>(at, more, reinterpret_cast<const u32x4_t(&)[1][DP / CHUNK<T> / 2]>(col), out);
-  return out[0];
+  f32x16_t c;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) c[i] = 0.f;
+#pragma unroll
+  for (int s = 0; s < DP / CHUNK<T> / 2; ++s) {
+    const u32x4_t row = *lds<u32x4_t>((at ^ (s * 32)) + more);
+    c = mma<T>(row, col[s], c);
+  }
+  return c;
+}
+// the same with the columns in LDS too, rows of another tile
+template <typename T, int DP>
+XP_DEV f32x16_t rows_times(uint32_t at, int more, uint32_t col) {
+  f32x16_t c;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) c[i] = 0.f;
+#pragma unroll
+  for (int s = 0; s < DP / CHUNK<T> / 2; ++s) {
+    const u32x4_t row = *lds<u32x4_t>((at ^ (s * 32)) + more), mine = *lds<u32x4_t>(col ^ (s * 32));
+    c = mma<T>(row, mine, c);
+  }
+  return c;
 }
 
-// acc[c][d][lane's column] += sum over 32 rows of tile[row][d] w[c][row]; at: column_place + tile
-template <typename T, int DP, int N>
-XP_DEV void add_transposed(f32x16_t (&acc)[N][DP / 32], uint32_t at, int more, const float (&w)[N][16]) {
+// acc[d][lane's column] += sum over 32 rows of tile[row][d] w[row]; at: column_place + tile
+template <typename T, int DP>
+XP_DEV void add_transposed(f32x16_t (&acc)[DP / 32], uint32_t at, int more, const float (&w)[16]) {
   if constexpr (sizeof(T) == 2) {
     typedef short v4i16 __attribute__((ext_vector_type(4)));
 #pragma unroll
     for (int b = 0; b < 2; ++b) {  // 16 rows: 4 lane / 32 + 0 .. 3 of them, and 8 further on
-      u32x4_t f[N];
+      u32x4_t f;
 #pragma unroll
-      for (int c = 0; c < N; ++c)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) f[c][i] = f32x2_to_bf16x2(w[c][8 * b + 2 * i], w[c][8 * b + 2 * i + 1]);
+      for (int i = 0; i < 4; ++i) f[i] = f32x2_to_bf16x2(w[8 * b + 2 * i], w[8 * b + 2 * i + 1]);
 #pragma unroll
       for (int d = 0; d < DP / 32; ++d) {
         v4i16 part[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k)
           part[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds<v4i16>((at ^ (d * 64 + k * 32)) + (more + (16 * b + 8 * k) * ROW<T, DP>)));
-        const u32x4_t x = __builtin_bit_cast(u32x4_t, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-        for (int c = 0; c < N; ++c) acc[c][d] = mma<T>(x, f[c], acc[c][d]);
+        acc[d] = mma<T>(__builtin_bit_cast(u32x4_t, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7)), f, acc[d]);
       }
     }
   } else {
@@ -257,14 +268,9 @@ XP_DEV void add_transposed(f32x16_t (&acc)[N][DP / 32], uint32_t at, int more, c
 #pragma unroll
       for (int d = 0; d < DP / 32; ++d) {
         const float x = *lds<float>((at ^ (d * 128 + ((r >> 2) & 1) * 64 + (r & 3) * 16)) + (more + (8 * (r >> 2) + (r & 3)) * ROW<T, DP>));
-#pragma unroll
-        for (int c = 0; c < N; ++c) acc[c][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, w[c][r], acc[c][d], 0, 0, 0);
+        acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, w[r], acc[d], 0, 0, 0);
       }
   }
-}
-template <typename T, int DP>
-XP_DEV void add_transposed(f32x16_t (&acc)[DP / 32], uint32_t at, int more, const float (&w)[16]) {
-  add_transposed<T, DP, 1>(reinterpret_cast<f32x16_t(&)[1][DP / 32]>(acc), at, more, reinterpret_cast<const float(&)[1][16]>(w));
 }
 
 // The lane's column of a result [DP][32], times f, to a row of dim elements in memory.
@@ -369,16 +375,10 @@ __global__ __launch_bounds__(64) void k_attn_docs(const int32_t* __restrict__ do
 
 // smallest and largest document over a workgroup's rows, and over the wave's; negative ones do not count
 struct DocRange { int lo, hi, wlo, whi; };
-template <int N>
-XP_DEV DocRange doc_range(const int (&doc)[N], int (*sh)[2]) {
+XP_DEV DocRange doc_range(int doc, int (*sh)[2]) {
   DocRange d;
-  d.wlo = INT_MAX;
-  d.whi = -1;
-#pragma unroll
-  for (int c = 0; c < N; ++c) {
-    d.wlo = min(d.wlo, doc[c] >= 0 ? doc[c] : INT_MAX);
-    d.whi = max(d.whi, doc[c]);
-  }
+  d.wlo = doc >= 0 ? doc : INT_MAX;
+  d.whi = doc >= 0 ? doc : -1;
   for (int o = 32; o > 0; o >>= 1) {
     d.wlo = min(d.wlo, __shfl_xor(d.wlo, o, 64));
     d.whi = max(d.whi, __shfl_xor(d.whi, o, 64));
@@ -409,77 +409,83 @@ XP_DEV uint32_t hidden(int k0, int kend, const int* docs, int doc) {
 }
 
 // ---------------------------------------------------------------- scores
-// cap tanh(x / cap) for u = x / cap: |error| of the tanh below 2^-23 (1 - e is exact to half a
-// step of 1); slope: its derivative, 4 e / (1 + e)^2
-XP_DEV float capped(float u, float cap, float& slope) {
-  const float e = exp2_(-2.f * LOG2E * fabsf(u)), r = __builtin_amdgcn_rcpf(1.f + e);
-  slope = 4.f * e * r * r;
-  return cap * copysignf((1.f - e) * r, u);
+// What the scores are, and in which units a kernel holds them:
+//   PLAIN  scale q.k; held as the products q.k (c1 = scale log2(e) comes in with the exponential)
+//   CAP    cap tanh(scale q.k / cap), in units of log 2
+//   BIAS   those or scale q.k, plus a bias, in their own units: a bias may be as low as fp32 goes,
+//          where a change of units would leave fp32
+enum { PLAIN = 0, CAP = 1, BIAS = 2 };
+// exp(score - base); c1: as above
+template <int MODE>
+XP_DEV float exp_of(float s, float base, float c1) {
+  if constexpr (MODE == PLAIN) return exp2_(s * c1 - base * c1);
+  else if constexpr (MODE == CAP) return exp2_(s - base);
+  else return exp2_((s - base) * LOG2E);
 }
+// a difference of scores in units of log 2, and a score in its own
+template <int MODE>
+XP_DEV float log2_of(float d, float c1) { return MODE == PLAIN ? d * c1 : MODE == CAP ? d : d * LOG2E; }
+template <int MODE>
+XP_DEV float score_of(float s, float scale) { return MODE == PLAIN ? s * scale : MODE == CAP ? s * LN2 : s; }
 
-// The bias of a head for a lane, by distance; the two ends stand for all further ones.
-struct Bias {
-  const float* at;  // distance 0
-  int range;
-  float left, right;
-  XP_DEV Bias(const AttnArgs& a, int head) {
-    range = a.range;
-    at = a.bias ? a.bias + (int64_t)head * (2 * range + 1) + range : nullptr;
-    left = at ? at[-range] : 0.f;
-    right = at ? at[range] : 0.f;
-  }
-  XP_DEV float get(int d) const { return at[min(max(d, -range), range)]; }
-};
-
-// Scores of a 32 x 32 block in place from its products (GEN; otherwise they stay products).
-// KEYS: the rows are keys and the lane a query, dist = first key - the query's position;
-// otherwise the lane is a key and dist = key - the first query's position.  dmin, dmax: the
-// distances that the block holds.  slope: of the cap, 1 without one.
-template <bool KEYS, bool SLOPE>
-XP_DEV void scores(f32x16_t& s, const AttnArgs& a, const Bias& bias, int dist, int dmin, int dmax, float (&slope)[16]) {
-  if (a.cap > 0.f) {
-    const float f = a.scale / a.cap;
+// Scores of a block of 32 x 32 from its products.  tanh(u) = 1 - 2 r with r = 1 / (1 + exp(2 u)),
+// off by at most 2^-23 of 1 (three roundings of values up to 1, the hardware's exponential and
+// reciprocal), its slope 4 r (1 - r); slope: of the cap (1 without one).  at(r): the bias of register r.
+template <int MODE, bool SLOPE, typename F>
+XP_DEV void scores(f32x16_t& s, const AttnArgs& a, float (&slope)[16], F&& at) {
+  if (MODE == CAP || (MODE == BIAS && a.cap > 0.f)) {
+    const float k = 2.f * LOG2E * a.scale / a.cap, top = MODE == CAP ? a.cap * LOG2E : a.cap;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      float c;
-      s[r] = capped(s[r] * f, a.cap, c);
-      if constexpr (SLOPE) slope[r] = c;
+      const float q = __builtin_amdgcn_rcpf(1.f + exp2_(s[r] * k));
+      s[r] = top - 2.f * top * q;
+      if constexpr (SLOPE) slope[r] = 4.f * q - 4.f * q * q;
     }
-  } else {
+  } else if constexpr (MODE == BIAS) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       s[r] *= a.scale;
       if constexpr (SLOPE) slope[r] = 1.f;
     }
   }
-  if (bias.at) {
-    if (dmin >= bias.range || dmax <= -bias.range) {
-      const float c = dmin >= bias.range ? bias.right : bias.left;
+  if constexpr (MODE == BIAS) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] += c;
-    } else {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] += bias.get(KEYS ? dist + row_of(r) : dist - row_of(r));
-    }
+    for (int r = 0; r < 16; ++r) s[r] += at(r);
   }
 }
 
+// A head's bias around a tile: WIDTH distances from `low` on, a step ahead like the tiles, in
+// LDS (reads from memory among the products would wait for the tiles in flight as well).
+template <int WIDTH>
+struct BiasWindow {
+  static_assert(WIDTH <= 256, "one each thread");
+  float reg;
+  XP_DEV void load(const AttnArgs& a, int head, int low) {
+    if (threadIdx.x < WIDTH)
+      reg = a.bias[(int64_t)head * (2 * a.range + 1) + a.range + min(max(low + (int)threadIdx.x, -a.range), a.range)];
+  }
+  XP_DEV void store(float* sh) const {
+    if (threadIdx.x < WIDTH) sh[threadIdx.x] = reg;
+  }
+};
+
 // ---------------------------------------------------------------- forward
-// One workgroup per 4 waves of 32 QB query rows of a head (with pk > 1: of the pk heads that
-// share keys, row r being query r / pk of head r % pk), and part of the keys.
+// One workgroup per 128 query rows of a head (with pk > 1: of the pk heads that share keys,
+// row r being query r / pk of head r % pk), and part of the keys.
 //
 // The largest score enters the exponentials only when it has grown by more than 8 (base 2)
 // since it last did: P is then at most 2^8, the sums stay in fp32's range, and the results
 // are rarely multiplied.
-template <typename T, int DP, bool GEN, int QB>
-__global__ __launch_bounds__(256, QB == 2 && DP == 128 ? 1 : (WAVES<T, DP>)) void k_attn_fwd(AttnArgs a) {
-  constexpr int KEYS = BN<T>, NB = KEYS / 32, WAVE = 32 * QB, GROUP = 4 * WAVE;
+template <typename T, int DP, int MODE>
+__global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_fwd(AttnArgs a) {
+  constexpr int KEYS = BN<T>, NB = KEYS / 32;
   constexpr int TILE = KEYS * ROW<T, DP>;
   __shared__ __attribute__((aligned(1024))) unsigned char tiles_[4 * TILE];  // keys, values, twice
+  __shared__ float sbias[2][MODE == BIAS ? ROWS + KEYS : 1];
   __shared__ int sdoc[2][KEYS];
   __shared__ int sh[4][2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int rows = a.nq * a.pk, blocks = (rows + GROUP - 1) / GROUP, units = a.heads / a.pk;
+  const int rows = a.nq * a.pk, blocks = (rows + ROWS - 1) / ROWS, units = a.heads / a.pk;
   int id = xcd_tile(blockIdx.x, gridDim.x);
   const int split = id % a.splits;
   id /= a.splits;
@@ -490,26 +496,20 @@ __global__ __launch_bounds__(256, QB == 2 && DP == 128 ? 1 : (WAVES<T, DP>)) voi
   const Seq seq(a, b);
 
   // limits of the workgroup's and the wave's rows (of those that count)
-  const int last = min((min(rows, (blk + 1) * GROUP) - 1) / a.pk, seq.ql - 1), first = blk * GROUP / a.pk;
+  const int last = min((min(rows, (blk + 1) * ROWS) - 1) / a.pk, seq.ql - 1), first = blk * ROWS / a.pk;
   const int kmax = first <= last ? seq.kend(last) : 0;
-  const int row0 = blk * GROUP + wave * WAVE;
-  const int wfirst = row0 / a.pk, wlast = min((row0 + WAVE - 1) / a.pk, min(a.nq, seq.ql) - 1);
+  const int row0 = blk * ROWS + wave * 32;
+  const int wfirst = row0 / a.pk, wlast = min((row0 + 31) / a.pk, min(a.nq, seq.ql) - 1);
   const int wmax = wfirst <= wlast ? seq.kend(wlast) : 0, wmin = wfirst <= wlast ? seq.kend(wfirst) : 0;
 
-  int doc[QB], kend[QB], pos[QB], head[QB];
-  u32x4_t q[QB][DP / CHUNK<T> / 2];
-#pragma unroll
-  for (int c = 0; c < QB; ++c) {
-    const int row = row0 + c * 32 + (lane & 31), i = row / a.pk;
-    const bool live = row < rows && i < seq.ql;
-    head[c] = unit * a.pk + row % a.pk;
-    doc[c] = a.q_doc ? (live ? a.q_doc[(int64_t)b * a.nq + i] : -1) : 0;
-    kend[c] = live && doc[c] >= 0 ? seq.kend(i) : 0;
-    pos[c] = i + seq.off;
-    ld_column<T, DP>((const T*)a.q.p + b * a.q.b + (int64_t)i * a.q.t + head[c] * a.q.h, live, a.ldim, q[c]);
-  }
+  const int row = row0 + (lane & 31), i = row / a.pk, head = unit * a.pk + row % a.pk;
+  const bool in = row < rows, live = in && i < seq.ql;
+  const int doc = a.q_doc ? (live ? a.q_doc[(int64_t)b * a.nq + i] : -1) : 0;
+  const int kend = live && doc >= 0 ? seq.kend(i) : 0;
+  u32x4_t q[DP / CHUNK<T> / 2];
+  ld_column<T, DP>((const T*)a.q.p + b * a.q.b + (int64_t)i * a.q.t + head * a.q.h, live, a.ldim, q);
   DocRange docs = {0, 0, 0, 0};
-  if (a.q_doc) docs = doc_range<QB>(doc, sh);
+  if (a.q_doc) docs = doc_range(doc, sh);
   const T* kp = (const T*)a.k.p + b * a.k.b + kvh * a.k.h;
   const T* vp = (const T*)a.v.p + b * a.v.b + kvh * a.v.h;
   const int32_t* kdoc = a.k_doc ? a.k_doc + (int64_t)b * a.nk : nullptr;
@@ -518,34 +518,32 @@ __global__ __launch_bounds__(256, QB == 2 && DP == 128 ? 1 : (WAVES<T, DP>)) voi
   const int tab_tiles = (a.nk + KEYS - 1) / KEYS;
   Walk walk(a.k_tab ? a.k_tab + (int64_t)b * tab_tiles : nullptr, min(tiles, (split + 1) * per), docs.lo, docs.hi);
 
-  // m: the largest of the products (GEN: of the scores) so far, base: the one in the
-  // exponentials; l: this lane's part of the sum
-  const float c1 = GEN ? LOG2E : a.scale * LOG2E;
-  float m[QB], base[QB], l[QB];
-  f32x16_t acc[QB][DP / 32];
+  // m: the largest score so far, base: the one in the exponentials; l: this lane's part of the sum
+  const float c1 = a.scale * LOG2E;
+  float m = NEG_INF, base = NEG_INF, l = 0.f;
+  f32x16_t acc[DP / 32];
 #pragma unroll
-  for (int c = 0; c < QB; ++c) {
-    m[c] = base[c] = NEG_INF;
-    l[c] = 0.f;
+  for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
-    for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[c][d][r] = 0.f;
-  }
+    for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
 
   Stager<T, DP, KEYS> ks(a.k.t, a.ldim), vs(a.v.t, a.ldim);
+  BiasWindow<ROWS + KEYS> window;
+  const int low = -(first + ROWS - 1) - seq.off;  // the window's smallest distance, of tile 0
   int dreg = -1;
   auto load = [&](int t) __attribute__((always_inline)) {
     const int j0 = t * KEYS;
     const int32_t* pad = kdoc && walk.tab[t].w ? kdoc + j0 : nullptr;
     ks.load(kp + (int64_t)j0 * a.k.t, seq.kl - j0, pad);
     vs.load(vp + (int64_t)j0 * a.v.t, seq.kl - j0, pad);
+    if (MODE == BIAS && a.pk == 1) window.load(a, unit, low + j0);
     if (kdoc && threadIdx.x < KEYS) dreg = j0 + (int)threadIdx.x < seq.kl ? kdoc[j0 + threadIdx.x] : -1;
   };
   const uint32_t tile0 = lds_address(tiles_), rplace = row_place<T, DP>() + tile0, cplace = column_place<T, DP>() + tile0;
   auto store = [&](int buf) __attribute__((always_inline)) {
     ks.store(tile0 + buf * 2 * TILE);
     vs.store(tile0 + buf * 2 * TILE + TILE);
+    if (MODE == BIAS && a.pk == 1) window.store(sbias[buf]);
     if (kdoc && threadIdx.x < KEYS) sdoc[buf][threadIdx.x] = dreg;
   };
   int t = walk.next(min(tiles, split * per)), buf = 0;
@@ -565,68 +563,60 @@ __global__ __launch_bounds__(256, QB == 2 && DP == 128 ? 1 : (WAVES<T, DP>)) voi
     }
     if (!skip) {
       const uint32_t rat = rplace + buf * 2 * TILE, cat = cplace + buf * 2 * TILE;
-      const bool masked = mixed || (t + 1) * KEYS > wmin;
-      f32x16_t s[NB][QB];
+      f32x16_t s[NB];
+      // (the other wave of the SIMD has its exponentials then)
       __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-      for (int n = 0; n < NB; ++n) rows_times<T, DP, QB>(rat, n * 32 * ROW<T, DP>, q, s[n]);
-#pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        const int k0 = t * KEYS + n * 32;
-        if constexpr (GEN) {
-          float none[16];
-#pragma unroll
-          for (int c = 0; c < QB; ++c) {
-            const Bias bias(a, min(head[c], a.heads - 1));
-            scores<true, false>(s[n][c], a, bias, k0 - pos[c], k0 - wlast - seq.off, k0 + 31 - wfirst - seq.off, none);
-          }
-        }
-        if (masked) {
-#pragma unroll
-          for (int c = 0; c < QB; ++c) {
-            const uint32_t hide = hidden(k0, kend[c], kdoc ? sdoc[buf] + n * 32 : nullptr, doc[c]);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[n][c][r] = hide >> r & 1 ? NEG_INF : s[n][c][r];
-          }
-        }
-      }
+      for (int n = 0; n < NB; ++n) s[n] = rows_times<T, DP>(rat, n * 32 * ROW<T, DP>, q);
       __builtin_amdgcn_s_setprio(0);
-      bool grown = false;
+      if constexpr (MODE != PLAIN) {
+        float none[16];
+        if (MODE == BIAS && a.pk > 1) {
+          const float* mine = a.bias + (int64_t)min(head, a.heads - 1) * (2 * a.range + 1) + a.range;
+          const int d0 = t * KEYS - i - seq.off;
 #pragma unroll
-      for (int c = 0; c < QB; ++c) {
-        float top = s[0][c][0];
+          for (int n = 0; n < NB; ++n)
+            scores<MODE, false>(s[n], a, none, [&](int r) { return mine[min(max(d0 + n * 32 + row_of(r), -a.range), a.range)]; });
+        } else {
+          const float* mine = sbias[buf] + ROWS - 1 - (row - blk * ROWS) + 4 * (lane >> 5);
 #pragma unroll
-        for (int n = 0; n < NB; ++n)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) top = fmaxf(top, s[n][c][r]);
-        m[c] = fmaxf(m[c], both_max(top));
-        grown = grown || (m[c] - base[c]) * c1 > 8.f;  // (from -inf on: infinite; while there is no key: NaN)
-      }
-      if (__any(grown)) {
-#pragma unroll
-        for (int c = 0; c < QB; ++c) {
-          const float keep = m[c] == NEG_INF ? 1.f : exp2_((base[c] - m[c]) * c1);
-          base[c] = m[c];
-          l[c] *= keep;
-#pragma unroll
-          for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[c][d][r] *= keep;
+          for (int n = 0; n < NB; ++n)
+            scores<MODE, false>(s[n], a, none, [&](int r) { return mine[n * 32 + 8 * (r >> 2) + (r & 3)]; });
         }
       }
+      if (mixed || (t + 1) * KEYS > wmin) {
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+          const uint32_t hide = hidden(t * KEYS + n * 32, kend, kdoc ? sdoc[buf] + n * 32 : nullptr, doc);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[n][r] = hide >> r & 1 ? NEG_INF : s[n][r];
+        }
+      }
+      float top = s[0][0];
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[n][r]);
+      m = fmaxf(m, both_max(top));
+      if (__any(log2_of<MODE>(m - base, c1) > 8.f)) {  // (from -inf on: infinite; while there is no key: NaN)
+        const float keep = m == NEG_INF ? 1.f : exp2_(log2_of<MODE>(base - m, c1));
+        base = m;
+        l *= keep;
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[d][r] *= keep;
+      }
+      const float off = base == NEG_INF ? 0.f : base;
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
-        float p[QB][16];
+        float p[16];
 #pragma unroll
-        for (int c = 0; c < QB; ++c) {
-          const float off = base[c] == NEG_INF ? 0.f : base[c], bc = off * c1;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            p[c][r] = GEN ? exp2_((s[n][c][r] - off) * c1) : exp2_(s[n][c][r] * c1 - bc);
-            l[c] += p[c][r];
-          }
+        for (int r = 0; r < 16; ++r) {
+          p[r] = exp_of<MODE>(s[n][r], off, c1);
+          l += p[r];
         }
-        add_transposed<T, DP, QB>(acc, cat, TILE + n * 32 * ROW<T, DP>, p);
+        add_transposed<T, DP>(acc, cat, TILE + n * 32 * ROW<T, DP>, p);
       }
     }
     buf ^= 1;
@@ -634,36 +624,32 @@ __global__ __launch_bounds__(256, QB == 2 && DP == 128 ? 1 : (WAVES<T, DP>)) voi
     t = tn;
   }
 
-#pragma unroll
-  for (int c = 0; c < QB; ++c) {
-    const int row = row0 + c * 32 + (lane & 31), i = row / a.pk;
-    // (a NaN among the scores leaves l NaN, and the row NaN)
-    const float sum = both_sum(l[c]);
-    const bool none = kend[c] == 0 || sum == 0.f;
-    const float ms = none ? NEG_INF : GEN ? m[c] : m[c] * a.scale, ls = none ? 0.f : sum * exp2_((base[c] - m[c]) * c1);
-    if (row >= rows) continue;
-    if (a.splits > 1) {
-      // (o's part belongs to `base`; a sum of zero leaves it unwritten)
-      const int64_t r = ((int64_t)split * a.batch + b) * a.heads * a.nq + (int64_t)head[c] * a.nq + i;
-      if (lane < 32) {
-        a.part_ml[2 * r] = ms;
-        a.part_ml[2 * r + 1] = ls;
-      }
-      st_column<float, DP>(a.part_o + r * DP, none ? 0 : DP, acc[c], exp2_((base[c] - m[c]) * c1));
-      continue;
+  if (!in) return;
+  // (a NaN among the scores leaves l NaN, and the row NaN)
+  const float sum = both_sum(l);
+  const bool none = kend == 0 || sum == 0.f;
+  const float fit = exp2_(log2_of<MODE>(base - m, c1));  // (o and l belong to `base`)
+  const float ms = none ? NEG_INF : score_of<MODE>(m, a.scale), ls = none ? 0.f : sum * fit;
+  if (a.splits > 1) {  // (a sum of zero leaves the part of o unwritten)
+    const int64_t r = ((int64_t)split * a.batch + b) * a.heads * a.nq + (int64_t)head * a.nq + i;
+    if (lane < 32) {
+      a.part_ml[2 * r] = ms;
+      a.part_ml[2 * r + 1] = ls;
     }
-    if (a.stats && lane < 32) {
-      float* st = a.stats + 2 * (((int64_t)b * a.heads + head[c]) * a.nq + i);
-      st[0] = ms;
-      st[1] = ls;
-    }
-    if (none)
-#pragma unroll
-      for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[c][d][r] = 0.f;
-    st_column<T, DP>((T*)a.o.p + b * a.o.b + (int64_t)i * a.o.t + head[c] * a.o.h, a.dim, acc[c], none ? 0.f : 1.f / sum);
+    st_column<float, DP>(a.part_o + r * DP, none ? 0 : DP, acc, fit);
+    return;
   }
+  if (a.stats && lane < 32) {
+    float* st = a.stats + 2 * (((int64_t)b * a.heads + head) * a.nq + i);
+    st[0] = ms;
+    st[1] = ls;
+  }
+  if (none)
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
+  st_column<T, DP>((T*)a.o.p + b * a.o.b + (int64_t)i * a.o.t + head * a.o.h, a.dim, acc, none ? 0.f : 1.f / sum);
 }
 
 // The parts of the keys joined: one wave per query row.
@@ -700,20 +686,22 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
 }
 
 // ---------------------------------------------------------------- statistics of a row
-// P = exp2(score' - row.a) with score' in units of log 2, where row.a has the sum's logarithm
-// in it; GEN (a bias can be as large as fp32 goes): exp2((score - row.a) log2(e) - row.b) with
-// the sum's logarithm apart.  A row without keys gives 0.
+// P = exp2(score - row.a) with the score in units of log 2, where row.a has the sum's logarithm in
+// it; BIAS: exp2((score - row.a) log2(e) - row.b) with the sum's logarithm apart.  A row without
+// keys gives 0.
 struct RowStat { float a, b; };
-template <bool GEN>
+template <int MODE>
 XP_DEV RowStat row_stat(float m, float l) {
   if (l == 0.f) return {__builtin_inff(), 0.f};
   const float log2l = __builtin_amdgcn_logf(l);
-  if constexpr (GEN) return {m, log2l};
+  if constexpr (MODE == BIAS) return {m, log2l};
   else return {m * LOG2E + log2l, 0.f};
 }
-template <bool GEN>
+template <int MODE>
 XP_DEV float weight(float s, float a, float b, float c1) {
-  return GEN ? exp2_((s - a) * LOG2E - b) : exp2_(s * c1 - a);
+  if constexpr (MODE == PLAIN) return exp2_(s * c1 - a);
+  else if constexpr (MODE == CAP) return exp2_(s - a);
+  else return exp2_((s - a) * LOG2E - b);
 }
 // What k_attn_dkv needs of 32 query rows: row.a, row.b, sum of P dP, kend, document, 32 each, and
 // room up to ROW_INFO floats.
@@ -728,11 +716,12 @@ XP_DEV int first_near(const AttnArgs& a, const Seq& seq, int kw) { return max(0,
 // dq += dX K.  do . o comes from the stored o here (rounded, as dq itself will be); the same
 // sum as P dP in fp32, which the loop makes by the way, is what k_attn_dkv reads: bias
 // gradients are fp32, and a rounded o would show in their sums.
-template <typename T, int DP, bool GEN>
+template <typename T, int DP, int MODE>
 __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dq(AttnArgs a) {
   constexpr int KEYS = BN_DQ<T, DP>, NB = KEYS / 32;
   constexpr int TILE = KEYS * ROW<T, DP>;
   __shared__ __attribute__((aligned(1024))) unsigned char tiles_[4 * TILE];  // keys, values, twice
+  __shared__ float sbias[2][MODE == BIAS ? ROWS + KEYS : 1];
   __shared__ int sdoc[2][KEYS];
   __shared__ int sh[4][2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -747,13 +736,13 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dq(AttnArgs a) {
   const int i = blk * ROWS + wave * 32 + (lane & 31);
   const bool in = i < a.nq, live = in && i < seq.ql;
   const int doc = a.q_doc ? (live ? a.q_doc[(int64_t)b * a.nq + i] : -1) : 0;
-  const int kend = live && doc >= 0 ? seq.kend(i) : 0, pos = i + seq.off;
+  const int kend = live && doc >= 0 ? seq.kend(i) : 0;
   const int last = min((blk + 1) * ROWS, min(a.nq, seq.ql)) - 1, first = blk * ROWS;
   const int kmax = first <= last ? seq.kend(last) : 0;
   const int wfirst = first + wave * 32, wlast = min(wfirst + 31, last);
   const int wmax = wfirst <= wlast ? seq.kend(wlast) : 0, wmin = wfirst <= wlast ? seq.kend(wfirst) : 0;
   DocRange docs = {0, 0, 0, 0};
-  if (a.q_doc) docs = doc_range<1>({doc}, sh);
+  if (a.q_doc) docs = doc_range(doc, sh);
 
   u32x4_t q[DP / CHUNK<T> / 2], g[DP / CHUNK<T> / 2];
   const bool use = live && doc >= 0;
@@ -775,7 +764,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dq(AttnArgs a) {
         for (int e = 0; e < CHUNK<T>; ++e) delta += x[e] * y[e];
       }
     }
-    st = row_stat<GEN>(a.stats[2 * srow], a.stats[2 * srow + 1]);
+    st = row_stat<MODE>(a.stats[2 * srow], a.stats[2 * srow + 1]);
   }
   delta = both_sum(delta);
   float exact = 0.f;
@@ -783,7 +772,6 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dq(AttnArgs a) {
   const T* kp = (const T*)a.k.p + b * a.k.b + kvh * a.k.h;
   const T* vp = (const T*)a.v.p + b * a.v.b + kvh * a.v.h;
   const int32_t* kdoc = a.k_doc ? a.k_doc + (int64_t)b * a.nk : nullptr;
-  const Bias bias(a, head);
 
   const int tiles = (kmax + KEYS - 1) / KEYS, tab_tiles = (a.nk + KEYS - 1) / KEYS;
   Walk walk(a.k_tab ? a.k_tab + (int64_t)b * tab_tiles : nullptr, tiles, docs.lo, docs.hi);
@@ -795,18 +783,22 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dq(AttnArgs a) {
     for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
 
   Stager<T, DP, KEYS> ks(a.k.t, a.ldim), vs(a.v.t, a.ldim);
+  BiasWindow<ROWS + KEYS> window;
+  const int low = -(first + ROWS - 1) - seq.off;  // the window's smallest distance, of tile 0
   int dreg = -1;
   auto load = [&](int t) __attribute__((always_inline)) {
     const int j0 = t * KEYS;
     const int32_t* pad = kdoc && walk.tab[t].w ? kdoc + j0 : nullptr;
     ks.load(kp + (int64_t)j0 * a.k.t, seq.kl - j0, pad);
     vs.load(vp + (int64_t)j0 * a.v.t, seq.kl - j0, pad);
+    if constexpr (MODE == BIAS) window.load(a, head, low + j0);
     if (kdoc && threadIdx.x < KEYS) dreg = j0 + (int)threadIdx.x < seq.kl ? kdoc[j0 + threadIdx.x] : -1;
   };
   const uint32_t tile0 = lds_address(tiles_), rplace = row_place<T, DP>() + tile0, cplace = column_place<T, DP>() + tile0;
   auto store = [&](int buf) __attribute__((always_inline)) {
     ks.store(tile0 + buf * 2 * TILE);
     vs.store(tile0 + buf * 2 * TILE + TILE);
+    if constexpr (MODE == BIAS) window.store(sbias[buf]);
     if (kdoc && threadIdx.x < KEYS) sdoc[buf][threadIdx.x] = dreg;
   };
   int t = walk.next(0), buf = 0;
@@ -834,10 +826,12 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dq(AttnArgs a) {
         const f32x16_t dp = rows_times<T, DP>(rat, TILE + n * 32 * ROW<T, DP>, g);
         phase();
         float slope[16], ds[16];
-        if constexpr (GEN)
-          scores<true, true>(s, a, bias, k0 - pos, k0 - wlast - seq.off, k0 + 31 - wfirst - seq.off, slope);
+        if constexpr (MODE != PLAIN) {
+          const float* mine = sbias[buf] + ROWS - 1 - (wave * 32 + (lane & 31)) + 4 * (lane >> 5) + n * 32;
+          scores<MODE, true>(s, a, slope, [&](int r) { return mine[8 * (r >> 2) + (r & 3)]; });
+        }
 #pragma unroll
-        for (int r = 0; r < 16; ++r) ds[r] = weight<GEN>(s[r], st.a, st.b, c1);
+        for (int r = 0; r < 16; ++r) ds[r] = weight<MODE>(s[r], st.a, st.b, c1);
         if (mixed || k0 + 32 > wmin) {
           const uint32_t hide = hidden(k0, kend, kdoc ? sdoc[buf] + n * 32 : nullptr, doc);
 #pragma unroll
@@ -848,7 +842,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dq(AttnArgs a) {
           exact += ds[r] * dp[r];
           ds[r] *= dp[r] - delta;
         }
-        if constexpr (GEN) {
+        if constexpr (MODE != PLAIN) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) ds[r] *= slope[r];
         }
@@ -918,15 +912,23 @@ __global__ __launch_bounds__(1024) void k_attn_dbias(AttnArgs a) {
 // 128: both sums and both operands would not fit a lane's registers).  With grad_bias also
 // the sums of dS along the diagonals of each block of 32 x 32 near the diagonal, and over
 // the blocks beyond the bias's range on either side.
-template <typename T, int DP, bool GEN, int WHAT>
-__global__ __launch_bounds__(256, GEN && DP == 128 ? 1 : (WAVES<T, DP>)) void k_attn_dkv(AttnArgs a) {
+//
+// A launch may be cut over the heads that share keys and over the queries (few keys would not
+// fill the card): each part then leaves its sums in fp32, which k_attn_dkv_join adds.
+// bf16 rows of 128: the values' columns stay in LDS, for 32 registers less.
+template <typename T, int DP, int MODE, int WHAT>
+__global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dkv(AttnArgs a) {
   constexpr int TILE = QT * ROW<T, DP>;
-  __shared__ __attribute__((aligned(1024))) unsigned char tiles_[4 * TILE];  // q, dout, twice
+  constexpr bool V_LDS = sizeof(T) == 2 && DP == 128;
+  __shared__ __attribute__((aligned(1024))) unsigned char tiles_[4 * TILE + (V_LDS ? ROWS * ROW<T, DP> : 0)];  // q, dout, twice; values
+  __shared__ float sbias[2][MODE == BIAS ? ROWS + QT : 1];
   __shared__ float srow[2][5 * QT];
   __shared__ int sh[4][2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int blocks = (a.nk + ROWS - 1) / ROWS, group = a.heads / a.kv_heads;
   int id = xcd_tile(blockIdx.x, gridDim.x);
+  const int parts = a.head_parts * a.q_parts, part = id % parts;
+  id /= parts;
   const int blk = id % blocks;  // (causal: the first keys have the most queries)
   id /= blocks;
   const int kvh = id % a.kv_heads, b = id / a.kv_heads;
@@ -937,13 +939,19 @@ __global__ __launch_bounds__(256, GEN && DP == 128 ? 1 : (WAVES<T, DP>)) void k_
   DocRange docs = {0, 0, 0, 0};
   bool pad = false;
   if (a.k_doc) {
-    docs = doc_range<1>({doc}, sh);
+    docs = doc_range(doc, sh);
     pad = __any(doc < 0);
   }
-  u32x4_t kc[DP / CHUNK<T> / 2], vc[DP / CHUNK<T> / 2];
+  const uint32_t tile0 = lds_address(tiles_), rplace = row_place<T, DP>() + tile0, cplace = column_place<T, DP>() + tile0;
+  const uint32_t vplace = rplace + 4 * TILE + wave * 32 * ROW<T, DP>;
+  u32x4_t kc[DP / CHUNK<T> / 2], vc[V_LDS ? 1 : DP / CHUNK<T> / 2];
   const bool use = j < seq.kl && doc >= 0;
   ld_column<T, DP>((const T*)a.k.p + b * a.k.b + (int64_t)j * a.k.t + kvh * a.k.h, use, a.ldim, kc);
-  if constexpr (WHAT & 2)
+  if constexpr (V_LDS) {
+    Stager<T, DP, ROWS> all(a.v.t, a.ldim);
+    all.load((const T*)a.v.p + b * a.v.b + kvh * a.v.h + k0 * a.v.t, seq.kl - k0, a.k_doc ? a.k_doc + (int64_t)b * a.nk + k0 : nullptr);
+    all.store(tile0 + 4 * TILE);
+  } else if constexpr (WHAT & 2)
     ld_column<T, DP>((const T*)a.v.p + b * a.v.b + (int64_t)j * a.v.t + kvh * a.v.h, use, a.ldim, vc);
   const int32_t* qdoc = a.q_doc ? a.q_doc + (int64_t)b * a.nq : nullptr;
 
@@ -951,6 +959,10 @@ __global__ __launch_bounds__(256, GEN && DP == 128 ? 1 : (WAVES<T, DP>)) void k_
   int tiles = (seq.ql + QT - 1) / QT, t0 = 0;
   if (k0 >= seq.kl) tiles = 0;
   else if (seq.causal && seq.prefix <= k0) t0 = min(tiles, max(0, k0 - seq.off) / QT);
+  const int h0 = kvh * group + part % a.head_parts * (group / a.head_parts), h1 = h0 + group / a.head_parts;
+  const int per = (tiles - t0 + a.q_parts - 1) / a.q_parts;
+  t0 = min(tiles, t0 + part / a.head_parts * per);
+  tiles = min(tiles, t0 + per);
   const int tab_tiles = (a.nq + QT - 1) / QT;
   Walk walk(a.q_tab ? a.q_tab + (int64_t)b * tab_tiles : nullptr, tiles, docs.lo, docs.hi);
 
@@ -965,12 +977,12 @@ __global__ __launch_bounds__(256, GEN && DP == 128 ? 1 : (WAVES<T, DP>)) void k_
     for (int r = 0; r < 16; ++r) d[r] = 0.f;
   const float c1 = a.scale * LOG2E;
 
-  const bool diag = GEN && (WHAT & 2) && a.grad_bias;
+  const bool diag = MODE == BIAS && (WHAT & 2) && a.grad_bias;
   float left = 0.f, right = 0.f;
   const int near0 = first_near(a, seq, kw);
   const int64_t wblock = blk * 4 + wave, wblocks = blocks * 4;
   if (diag)  // blocks that no step reaches
-    for (int h = kvh * group; h < (kvh + 1) * group; ++h) {
+    for (int h = h0; h < h1; ++h) {
       const int64_t w = ((int64_t)b * a.heads + h) * wblocks + wblock;
       for (int n = 0; n < a.near; ++n) a.diag[(w * a.near + n) * 64 + lane] = 0.f;
       if (lane < 2) a.tail[2 * w + lane] = 0.f;
@@ -978,34 +990,37 @@ __global__ __launch_bounds__(256, GEN && DP == 128 ? 1 : (WAVES<T, DP>)) void k_
 
   Stager<T, DP, QT> qs(a.q.t, a.ldim), gs(a.dout.t, a.ldim);
   const int row_tiles = (a.nq + ROWS - 1) / ROWS * 4;
+  BiasWindow<ROWS + QT> window;
+  const int low = k0 - (QT - 1) - seq.off;  // the window's smallest distance, of tile 0
   float rreg = 0.f;
   auto load = [&](int t, int head) __attribute__((always_inline)) {
     const int i0 = t * QT;
     const int32_t* pads = qdoc && walk.tab[t].w ? qdoc + i0 : nullptr;
     qs.load((const T*)a.q.p + b * a.q.b + head * a.q.h + i0 * a.q.t, seq.ql - i0, pads);
     gs.load((const T*)a.dout.p + b * a.dout.b + head * a.dout.h + i0 * a.dout.t, seq.ql - i0, pads);
+    if constexpr (MODE == BIAS) window.load(a, head, low - i0);
     if (threadIdx.x < 5 * QT) rreg = a.rows[(((int64_t)b * a.heads + head) * row_tiles + t) * ROW_INFO + threadIdx.x];
   };
-  const uint32_t tile0 = lds_address(tiles_), rplace = row_place<T, DP>() + tile0, cplace = column_place<T, DP>() + tile0;
   auto store = [&](int buf) __attribute__((always_inline)) {
     qs.store(tile0 + buf * 2 * TILE);
     gs.store(tile0 + buf * 2 * TILE + TILE);
+    if constexpr (MODE == BIAS) window.store(sbias[buf]);
     if (threadIdx.x < 5 * QT) srow[buf][threadIdx.x] = rreg;
   };
-  int g = 0, t = walk.next(t0), buf = 0;
+  int head = h0, t = walk.next(t0), buf = 0;
   const int t_first = t;
   const bool any = t < walk.end;
   if (any) {
-    load(t, kvh * group);
+    load(t, h0);
     store(0);
   }
-  while (any && g < group) {
-    int tn = walk.next(t + 1), gn = g;
+  while (any && head < h1) {
+    int tn = walk.next(t + 1), hn = head;
     if (tn >= walk.end) {
       tn = t_first;
-      ++gn;
+      ++hn;
     }
-    if (gn < group) load(tn, kvh * group + gn);
+    if (hn < h1) load(tn, hn);
     __syncthreads();
     const int i0 = t * QT, i1 = min(i0 + QT, seq.ql) - 1;
     bool mixed = false, skip = seq.kend(i1) <= kw;
@@ -1016,17 +1031,15 @@ __global__ __launch_bounds__(256, GEN && DP == 128 ? 1 : (WAVES<T, DP>)) void k_
     }
     if (!skip) {
       const uint32_t rat = rplace + buf * 2 * TILE, cat = cplace + buf * 2 * TILE;
-      const int head = kvh * group + g;
       f32x16_t s = rows_times<T, DP>(rat, 0, kc);
       phase();
       float p[16], slope[16];
-      if constexpr (GEN) {
-        const Bias bias(a, head);
-        const int dist = j - i0 - seq.off;
-        scores<false, true>(s, a, bias, dist, kw - i1 - seq.off, kw + 31 - i0 - seq.off, slope);
+      if constexpr (MODE != PLAIN) {  // (register r's place in the window: key - query + 31)
+        const float* mine = sbias[buf] + (j - k0) + 4 - 4 * (lane >> 5);
+        scores<MODE, (WHAT & 2) != 0>(s, a, slope, [&](int r) { return mine[27 - 8 * (r >> 2) - (r & 3)]; });
       }
 #pragma unroll
-      for (int r = 0; r < 16; ++r) p[r] = weight<GEN>(s[r], srow[buf][row_of(r)], GEN ? srow[buf][32 + row_of(r)] : 0.f, c1);
+      for (int r = 0; r < 16; ++r) p[r] = weight<MODE>(s[r], srow[buf][row_of(r)], MODE == BIAS ? srow[buf][32 + row_of(r)] : 0.f, c1);
       const bool masked = mixed || i0 + QT > seq.ql || seq.kend(i0) < kw + 32;
       if (masked) {
 #pragma unroll
@@ -1041,7 +1054,9 @@ __global__ __launch_bounds__(256, GEN && DP == 128 ? 1 : (WAVES<T, DP>)) void k_
         phase();
       }
       if constexpr (WHAT & 2) {
-        const f32x16_t dp = rows_times<T, DP>(rat, TILE, vc);
+        f32x16_t dp;
+        if constexpr (V_LDS) dp = rows_times<T, DP>(rat, TILE, (uint32_t)fresh(vplace));
+        else dp = rows_times<T, DP>(rat, TILE, vc);
         phase();
 #pragma unroll
         for (int r = 0; r < 16; ++r) p[r] *= dp[r] - srow[buf][64 + row_of(r)];
@@ -1075,7 +1090,7 @@ __global__ __launch_bounds__(256, GEN && DP == 128 ? 1 : (WAVES<T, DP>)) void k_
             a.diag[(w * a.near + (t - near0)) * 64 + lane] = outer ? 0.f : lo;
           }
         }
-        if constexpr (GEN) {
+        if constexpr (MODE != PLAIN) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) p[r] *= slope[r];
         }
@@ -1083,26 +1098,54 @@ __global__ __launch_bounds__(256, GEN && DP == 128 ? 1 : (WAVES<T, DP>)) void k_
         add_transposed<T, DP>(dk, cat, 0, p);
       }
     }
-    if (diag && gn != g) {  // the head's last step
+    if (diag && hn != head) {  // the head's last step
       for (int o = 32; o > 0; o >>= 1) {
         left += __shfl_xor(left, o, 64);
         right += __shfl_xor(right, o, 64);
       }
       if (lane == 0) {
-        float* w = a.tail + 2 * (((int64_t)b * a.heads + kvh * group + g) * wblocks + wblock);
+        float* w = a.tail + 2 * (((int64_t)b * a.heads + head) * wblocks + wblock);
         w[0] = left;
         w[1] = right;
       }
       left = right = 0.f;
     }
     buf ^= 1;
-    if (gn < group) store(buf);
+    if (hn < h1) store(buf);
     t = tn;
-    g = gn;
+    head = hn;
   }
   if (!in) return;
+  if (parts > 1) {
+    float* to = a.part_kv + ((((int64_t)part * a.batch + b) * a.nk + j) * a.kv_heads + kvh) * (2 * DP);
+    if constexpr (WHAT & 2) st_column<float, DP>(to, DP, dk, a.scale);
+    if constexpr (WHAT & 1) st_column<float, DP>(to + DP, DP, dv, 1.f);
+    return;
+  }
   if constexpr (WHAT & 1) st_column<T, DP>((T*)a.dv.p + b * a.dv.b + (int64_t)j * a.dv.t + kvh * a.dv.h, a.dim, dv, 1.f);
   if constexpr (WHAT & 2) st_column<T, DP>((T*)a.dk.p + b * a.dk.b + (int64_t)j * a.dk.t + kvh * a.dk.h, a.dim, dk, a.scale);
+}
+
+// The parts' sums of dk and dv added, in their order.
+template <typename T, int DP>
+__global__ __launch_bounds__(256) void k_attn_dkv_join(AttnArgs a) {
+  const int64_t rows = (int64_t)a.batch * a.nk * a.kv_heads, r = (int64_t)blockIdx.x * (256 / (DP / 2)) + threadIdx.x / (DP / 2);
+  if (r >= rows) return;
+  const int at = threadIdx.x % (DP / 2) * 4, d = at % DP;  // dk's and dv's columns side by side
+  const int parts = a.head_parts * a.q_parts;
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int p = 0; p < parts; ++p) {
+    const f32x4_t v = *reinterpret_cast<const f32x4_t*>(a.part_kv + (p * rows + r) * (2 * DP) + at);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] += v[i];
+  }
+  const int kvh = (int)(r % a.kv_heads), j = (int)(r / a.kv_heads % a.nk), b = (int)(r / a.kv_heads / a.nk);
+  const AttnMat& m = at < DP ? a.dk : a.dv;
+  T* to = (T*)m.p + b * m.b + (int64_t)j * m.t + kvh * m.h + d;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (d + i < a.dim) std_(to + i, (double)s[i]);
 }
 
 // ---------------------------------------------------------------- launches
@@ -1128,13 +1171,21 @@ int parts(int dtype, const AttnArgs& a) {
   return (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(512, groups), steps / 4));
 }
 
-// whether the forward's waves take 64 query rows each
-bool wide(const AttnArgs& a) { return false;
-  return a.splits == 1 && ceil_div((int64_t)a.nq * a.pk, 2 * ROWS) * (a.heads / a.pk) * a.batch >= 256;
-}
-
 // blocks of 32 queries that hold distances within the range, of 32 keys
 int near_blocks(const AttnArgs& a) { return (int)std::min<int64_t>(ceil_div(a.nq, 32), ceil_div(2 * (int64_t)a.range + 62, 32) + 1); }
+
+// Parts of k_attn_dkv where its blocks of keys do not fill the card twice over: heads that share
+// keys first, then runs of at least 8 steps of queries (with grad_bias heads alone: the
+// blocks' diagonals are laid out for one run).
+void cut_dkv(AttnArgs& a, int64_t kgroups) {
+  const int group = a.heads / a.kv_heads;
+  a.head_parts = a.q_parts = 1;
+  if (kgroups == 0) return;
+  for (int d = 1; d <= group && kgroups * a.head_parts < 512; ++d)
+    if (group % d == 0) a.head_parts = d;
+  const int64_t groups = kgroups * a.head_parts;
+  if (!a.grad_bias && groups < 512) a.q_parts = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(512, groups), ceil_div(a.nq, QT) / 8));
+}
 
 // Inputs whose rows are not whole, aligned chunks of 16 bytes are copied to such ones first:
 // the kernels read nothing else.  Places the copy at `at` in the workspace, with `from` what is to
@@ -1176,6 +1227,10 @@ size_t lay_bwd(int dtype, AttnArgs& a, char* base, AttnMat* from) {
     const bool keys = i == 1 || i == 2;
     n = lay_packed(dtype, a, *m[i], keys ? a.nk : a.nq, keys ? a.kv_heads : a.heads, base, n, from[i]);
   }
+  const int64_t kgroups = ceil_div(a.nk, ROWS) * a.kv_heads * a.batch;
+  cut_dkv(a, kgroups);
+  if (a.head_parts * a.q_parts > 1)
+    a.part_kv = (float*)take((size_t)a.batch * a.nk * a.kv_heads * a.head_parts * a.q_parts * 2 * padded_dim(a.dim) * 4);
   a.rows = (float*)take((size_t)a.batch * a.heads * ceil_div(a.nq, ROWS) * 4 * ROW_INFO * 4);
   if (a.k_doc) {
     a.k_tab = (int4*)take((size_t)a.batch * ceil_div(a.nk, dq_keys_of(dtype, a)) * sizeof(int4));
@@ -1190,70 +1245,76 @@ size_t lay_bwd(int dtype, AttnArgs& a, char* base, AttnMat* from) {
   return n;
 }
 
-bool general(const AttnArgs& a) { return a.bias || a.cap > 0.f; }
-
 // documents of the tiles of keys, and of queries
 void launch_docs(const int32_t* doc, const int32_t* len, int n, int batch, int tile, int4* tab, hipStream_t s) {
   if (n == 0) return;
   XP_LAUNCH("k_attn_docs", 4.0 * batch * n, k_attn_docs, dim3((unsigned)ceil_div(n, tile), batch), dim3(64), 0, s, doc, len, n, tile, tab);
 }
 
-void launch_pack(int dtype, const AttnArgs& a, const AttnMat& from, const AttnMat& to, int64_t tokens, int64_t heads, hipStream_t s) {
-  if (!from.p) return;
-  const int64_t rows = (int64_t)a.batch * tokens * heads, n = rows * a.ldim;
-  const unsigned blocks = (unsigned)std::min<int64_t>(ceil_div(n, 256 * 8), 4096);
-  if (dtype == DT_BF16)
-    XP_LAUNCH("k_attn_pack<bf16>", 4.0 * n, k_attn_pack<bf16_t>, dim3(blocks), dim3(256), 0, s, from, (bf16_t*)to.p, rows, (int)tokens, (int)heads, a.dim, a.ldim);
-  else
-    XP_LAUNCH("k_attn_pack<f32>", 8.0 * n, k_attn_pack<float>, dim3(blocks), dim3(256), 0, s, from, (float*)to.p, rows, (int)tokens, (int)heads, a.dim, a.ldim);
+void launch_pack(int dtype, const AttnArgs& a, const AttnMat* from, const AttnMat* const* to, int n, hipStream_t s) {
+  PackArgs p{};
+  p.dim = a.dim;
+  p.ldim = a.ldim;
+  int count = 0;
+  int64_t most = 0;
+  for (int i = 0; i < n; ++i) {
+    if (!from[i].p) continue;
+    const bool keys = i == 1 || i == 2;
+    p.from[count] = from[i];
+    p.to[count] = (void*)to[i]->p;
+    p.tokens[count] = keys ? a.nk : a.nq;
+    p.heads[count] = keys ? a.kv_heads : a.heads;
+    p.rows[count] = (int64_t)a.batch * p.tokens[count] * p.heads[count];
+    most = std::max(most, p.rows[count++]);
+  }
+  if (count == 0) return;
+  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(most * a.ldim, 256 * 8), 4096), count);
+  if (dtype == DT_BF16) XP_LAUNCH("k_attn_pack<bf16>", 4.0 * most * count * a.ldim, k_attn_pack<bf16_t>, grid, dim3(256), 0, s, p);
+  else XP_LAUNCH("k_attn_pack<f32>", 8.0 * most * count * a.ldim, k_attn_pack<float>, grid, dim3(256), 0, s, p);
 }
 
-template <typename T, int DP, bool GEN>
+template <typename T, int DP, int MODE>
 void fwd(const AttnArgs& a, hipStream_t s) {
   const double flops = 4.0 * a.batch * a.heads * a.nq * (double)a.nk * a.dim;
-  auto run = [&](auto qb) {
-    constexpr int QB = decltype(qb)::value;
-    const int64_t groups = ceil_div((int64_t)a.nq * a.pk, ROWS * QB) * (a.heads / a.pk) * a.batch * a.splits;
-    XP_LAUNCH(sizeof(T) == 2 ? "k_attn_fwd<bf16>" : "k_attn_fwd<f32>", flops, (k_attn_fwd<T, DP, GEN, QB>), dim3((unsigned)groups), dim3(256), 0, s, a);
-  };
-  if constexpr (sizeof(T) == 2) {
-    if (wide(a)) run(std::integral_constant<int, 2>{});
-    else run(std::integral_constant<int, 1>{});
-  } else {
-    run(std::integral_constant<int, 1>{});
-  }
+  const int64_t groups = ceil_div((int64_t)a.nq * a.pk, ROWS) * (a.heads / a.pk) * a.batch * a.splits;
+  XP_LAUNCH(sizeof(T) == 2 ? "k_attn_fwd<bf16>" : "k_attn_fwd<f32>", flops, (k_attn_fwd<T, DP, MODE>), dim3((unsigned)groups), dim3(256), 0, s, a);
   if (a.splits > 1) {
     const int64_t rows = (int64_t)a.batch * a.heads * a.nq;
     XP_LAUNCH("k_attn_join", 4.0 * rows * a.splits * DP, (k_attn_join<T, DP>), dim3((unsigned)ceil_div(rows, 4)), dim3(256), 0, s, a);
   }
 }
 
-template <typename T, int DP, bool GEN>
+template <typename T, int DP, int MODE>
 void bwd(const AttnArgs& a, hipStream_t s) {
   const double pairs = (double)a.batch * a.heads * a.nq * a.nk;
-  const int64_t groups = ceil_div(a.nq, ROWS) * a.heads * a.batch, kgroups = ceil_div(a.nk, ROWS) * a.kv_heads * a.batch;
+  const int64_t parts = (int64_t)a.head_parts * a.q_parts;
+  const int64_t groups = ceil_div(a.nq, ROWS) * a.heads * a.batch, kgroups = ceil_div(a.nk, ROWS) * a.kv_heads * a.batch * parts;
   if (groups > 0)
-    XP_LAUNCH(sizeof(T) == 2 ? "k_attn_dq<bf16>" : "k_attn_dq<f32>", 6 * pairs * a.dim, (k_attn_dq<T, DP, GEN>), dim3((unsigned)groups), dim3(256), 0, s, a);
-  if (kgroups == 0) {
-  } else if constexpr (sizeof(T) == 4 && DP == 128) {
-    XP_LAUNCH("k_attn_dv<f32>", 4 * pairs * a.dim, (k_attn_dkv<T, DP, GEN, 1>), dim3((unsigned)kgroups), dim3(256), 0, s, a);
-    XP_LAUNCH("k_attn_dk<f32>", 6 * pairs * a.dim, (k_attn_dkv<T, DP, GEN, 2>), dim3((unsigned)kgroups), dim3(256), 0, s, a);
+    XP_LAUNCH(sizeof(T) == 2 ? "k_attn_dq<bf16>" : "k_attn_dq<f32>", 6 * pairs * a.dim, (k_attn_dq<T, DP, MODE>), dim3((unsigned)groups), dim3(256), 0, s, a);
+  if (kgroups == 0) return;
+  if constexpr (sizeof(T) == 4 && DP == 128) {
+    XP_LAUNCH("k_attn_dv<f32>", 4 * pairs * a.dim, (k_attn_dkv<T, DP, MODE, 1>), dim3((unsigned)kgroups), dim3(256), 0, s, a);
+    XP_LAUNCH("k_attn_dk<f32>", 6 * pairs * a.dim, (k_attn_dkv<T, DP, MODE, 2>), dim3((unsigned)kgroups), dim3(256), 0, s, a);
   } else {
-    XP_LAUNCH(sizeof(T) == 2 ? "k_attn_dkv<bf16>" : "k_attn_dkv<f32>", 8 * pairs * a.dim, (k_attn_dkv<T, DP, GEN, 3>), dim3((unsigned)kgroups),
+    XP_LAUNCH(sizeof(T) == 2 ? "k_attn_dkv<bf16>" : "k_attn_dkv<f32>", 8 * pairs * a.dim, (k_attn_dkv<T, DP, MODE, 3>), dim3((unsigned)kgroups),
               dim3(256), 0, s, a);
   }
-  if (a.grad_bias && groups > 0 && kgroups > 0)
+  if (parts > 1) {
+    const int64_t rows = (int64_t)a.batch * a.nk * a.kv_heads;
+    XP_LAUNCH("k_attn_dkv_join", 8.0 * rows * parts * DP, (k_attn_dkv_join<T, DP>), dim3((unsigned)ceil_div(rows, 512 / DP)), dim3(256), 0, s, a);
+  }
+  if (a.grad_bias && groups > 0)
     XP_LAUNCH("k_attn_dbias", 4.0 * (2 * a.range + 1) * a.heads, k_attn_dbias, dim3((unsigned)ceil_div(2 * (int64_t)a.range + 1, 64), a.heads), dim3(1024), 0, s, a);
 }
 
-// calls f(element type, padded dim, whether scores need more than the scale)
+// calls f(element type, padded dim, kind of scores)
 template <typename F>
 void by_kind(int dtype, const AttnArgs& a, F&& f) {
-  using std::bool_constant;
   using std::integral_constant;
   auto with = [&](auto t, auto d) {
-    if (general(a)) f(t, d, bool_constant<true>{});
-    else f(t, d, bool_constant<false>{});
+    if (a.bias) f(t, d, integral_constant<int, BIAS>{});
+    else if (a.cap > 0.f) f(t, d, integral_constant<int, CAP>{});
+    else f(t, d, integral_constant<int, PLAIN>{});
   };
   auto dims = [&](auto t) {
     if (a.dim <= 64) with(t, integral_constant<int, 64>{});
@@ -1279,9 +1340,8 @@ size_t attn_bwd_bytes(int dtype, const AttnArgs& a) {
 hipError_t launch_attn_fwd(int dtype, AttnArgs a, void* workspace, hipStream_t s) {
   AttnMat from[3];
   lay_fwd(dtype, a, (char*)workspace, from);
-  launch_pack(dtype, a, from[0], a.q, a.nq, a.heads, s);
-  launch_pack(dtype, a, from[1], a.k, a.nk, a.kv_heads, s);
-  launch_pack(dtype, a, from[2], a.v, a.nk, a.kv_heads, s);
+  const AttnMat* const to[3] = {&a.q, &a.k, &a.v};
+  launch_pack(dtype, a, from, to, 3, s);
   if (a.k_doc) launch_docs(a.k_doc, a.k_len, a.nk, a.batch, keys_of(dtype), a.k_tab, s);
   by_kind(dtype, a, [&](auto t, auto d, auto g) { fwd<decltype(t), decltype(d)::value, decltype(g)::value>(a, s); });
   return hipGetLastError();
@@ -1291,10 +1351,8 @@ hipError_t launch_attn_bwd(int dtype, AttnArgs a, void* workspace, hipStream_t s
   AttnMat from[4];
   a.pk = a.splits = 1;
   lay_bwd(dtype, a, (char*)workspace, from);
-  launch_pack(dtype, a, from[0], a.q, a.nq, a.heads, s);
-  launch_pack(dtype, a, from[1], a.k, a.nk, a.kv_heads, s);
-  launch_pack(dtype, a, from[2], a.v, a.nk, a.kv_heads, s);
-  launch_pack(dtype, a, from[3], a.dout, a.nq, a.heads, s);
+  const AttnMat* const to[4] = {&a.q, &a.k, &a.v, &a.dout};
+  launch_pack(dtype, a, from, to, 4, s);
   if (a.k_doc) {
     launch_docs(a.k_doc, a.k_len, a.nk, a.batch, dq_keys_of(dtype, a), a.k_tab, s);
     launch_docs(a.q_doc, a.q_len, a.nq, a.batch, QT, a.q_tab, s);

@@ -438,7 +438,8 @@ struct AttnArgs {
   // of the keys and their results, documents of each tile, what the gradients need of each query row, sums of score
   // gradients along diagonals
   int pk, splits, near, ldim;        // ldim: dim in whole chunks of 16 bytes
-  float *part_o, *part_ml;
+  int head_parts, q_parts;           // of k_attn_dkv
+  float *part_o, *part_ml, *part_kv;
   int4 *k_tab, *q_tab;
   float *rows, *diag, *tail;
 };
