@@ -627,7 +627,8 @@ typedef struct {
 typedef struct {
   xpipe_attention_inputs in;
   xpipe_heads o;                         /* written */
-  float* stats;                          /* [batch][heads][nq][2]: largest score, sum of exp(score - largest); or NULL */
+  float* stats;                          /* [batch][heads][nq][2]: the largest score times log2(e), and the sum
+                                          * of exp(score - largest): -inf and 0 where nothing is seen; or NULL */
 } xpipe_attention_fwd_args;
 /* The backward takes the forward's inputs, its o and its stats.  (dq reads do . o from the
  * rounded o; dk, dv and grad_bias use the same sum as P dP, in fp32.) */

@@ -997,7 +997,8 @@ def xpipe_attention_fwd(q, k, v, o, scale: Optional[float] = None, causal: bool 
     distance (key less query position; further ones as the furthest).  q_len, k_len,
     prefix: int32 [batch]; q_doc, k_doc: int32 documents of the tokens.  The queries are
     the last q_len of a sequence of k_len tokens.  stats (for the
-    backward): float32 [batch, heads, nq, 2]."""
+    backward): float32 [batch, heads, nq, 2], the largest score times log2(e) and the
+    sum of exp(score - largest)."""
     L = lib()
     dev, here = _device_of(q)
     if not here:

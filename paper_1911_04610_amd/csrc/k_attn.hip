@@ -26,7 +26,7 @@ namespace xp {
 
 namespace {
 
-constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
+constexpr float LOG2E = 1.44269504088896340736f;
 constexpr float NEG_INF = -__builtin_inff();
 constexpr int ROWS = 128;  // query rows (dk, dv: keys) of a workgroup: 4 waves of 32
 constexpr int QT = 32;     // queries of a step of k_attn_dkv
@@ -395,38 +395,37 @@ XP_DEV DocRange doc_range(int doc, int (*sh)[2]) {
   return d;
 }
 
-// The keys of a lane's block of 32 (from k0 on) that its query does not see, a bit for each
-// register.  (Bits and selects: an element of a vector assigned under "a || b" is
-// lost in places with this compiler.)
-XP_DEV uint32_t hidden(int k0, int kend, const int* docs, int doc) {
-  uint32_t m = 0;
+// `none` in the place of keys that a lane's query does not see, of a block of 32 from k0 on: those
+// from kend on, and (docs given) those of other documents.  (Selects, one condition at a time:
+// an element of a vector assigned under "a || b" is lost in places with this compiler.)
+template <typename V>
+XP_DEV void hide_from(V& s, int left, float none) {  // left: kend - k0
+  left -= 4 * ((threadIdx.x >> 5) & 1);
 #pragma unroll
-  for (int r = 0; r < 16; ++r) m |= (uint32_t)(k0 + row_of(r) >= kend) << r;
-  if (docs)
+  for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + (r & 3) >= left ? none : s[r];
+}
+template <typename V>
+XP_DEV void hide_others(V& s, const int* docs, int doc, float none) {
+  docs += 4 * ((threadIdx.x >> 5) & 1);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) m |= (uint32_t)(docs[row_of(r)] != doc) << r;
-  return m;
+  for (int r = 0; r < 16; ++r) s[r] = docs[8 * (r >> 2) + (r & 3)] != doc ? none : s[r];
 }
 
 // ---------------------------------------------------------------- scores
-// What the scores are, and in which units a kernel holds them:
+// What the scores are, in units of log 2 (the exponential's):
 //   PLAIN  scale q.k; held as the products q.k (c1 = scale log2(e) comes in with the exponential)
-//   CAP    cap tanh(scale q.k / cap), in units of log 2
-//   BIAS   those or scale q.k, plus a bias, in their own units: a bias may be as low as fp32 goes,
-//          where a change of units would leave fp32
+//   CAP    cap tanh(scale q.k / cap)
+//   BIAS   those or scale q.k, plus a bias
 enum { PLAIN = 0, CAP = 1, BIAS = 2 };
 // exp(score - base); c1: as above
 template <int MODE>
 XP_DEV float exp_of(float s, float base, float c1) {
   if constexpr (MODE == PLAIN) return exp2_(s * c1 - base * c1);
-  else if constexpr (MODE == CAP) return exp2_(s - base);
-  else return exp2_((s - base) * LOG2E);
+  else return exp2_(s - base);
 }
-// a difference of scores in units of log 2, and a score in its own
+// a score, or a difference of two, in units of log 2
 template <int MODE>
-XP_DEV float log2_of(float d, float c1) { return MODE == PLAIN ? d * c1 : MODE == CAP ? d : d * LOG2E; }
-template <int MODE>
-XP_DEV float score_of(float s, float scale) { return MODE == PLAIN ? s * scale : MODE == CAP ? s * LN2 : s; }
+XP_DEV float log2_of(float d, float c1) { return MODE == PLAIN ? d * c1 : d; }
 
 // Scores of a block of 32 x 32 from its products.  tanh(u) = 1 - 2 r with r = 1 / (1 + exp(2 u)),
 // off by at most 2^-23 of 1 (three roundings of values up to 1, the hardware's exponential and
@@ -434,24 +433,31 @@ XP_DEV float score_of(float s, float scale) { return MODE == PLAIN ? s * scale :
 template <int MODE, bool SLOPE, typename F>
 XP_DEV void scores(f32x16_t& s, const AttnArgs& a, float (&slope)[16], F&& at) {
   if (MODE == CAP || (MODE == BIAS && a.cap > 0.f)) {
-    const float k = 2.f * LOG2E * a.scale / a.cap, top = MODE == CAP ? a.cap * LOG2E : a.cap;
+    const float k = 2.f * LOG2E * a.scale / a.cap, top = a.cap * LOG2E;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const float q = __builtin_amdgcn_rcpf(1.f + exp2_(s[r] * k));
       s[r] = top - 2.f * top * q;
       if constexpr (SLOPE) slope[r] = 4.f * q - 4.f * q * q;
     }
+    if constexpr (MODE == BIAS)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] += at(r);
   } else if constexpr (MODE == BIAS) {
+    const float c1 = a.scale * LOG2E;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      s[r] *= a.scale;
+      s[r] = s[r] * c1 + at(r);
       if constexpr (SLOPE) slope[r] = 1.f;
     }
   }
-  if constexpr (MODE == BIAS) {
-#pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] += at(r);
-  }
+}
+
+// A bias in units of log 2.  The lowest and highest values of fp32 stay finite: a row that holds
+// nothing else keeps its softmax of equal scores.
+XP_DEV float log2_bias(float v) {
+  const float most = 3.402823466e38f, u = v * LOG2E;
+  return fabsf(v) <= most ? fminf(fmaxf(u, -most), most) : u;
 }
 
 // A head's bias around a tile: WIDTH distances from `low` on, a step ahead like the tiles, in
@@ -465,7 +471,7 @@ struct BiasWindow {
       reg = a.bias[(int64_t)head * (2 * a.range + 1) + a.range + min(max(low + (int)threadIdx.x, -a.range), a.range)];
   }
   XP_DEV void store(float* sh) const {
-    if (threadIdx.x < WIDTH) sh[threadIdx.x] = reg;
+    if (threadIdx.x < WIDTH) sh[threadIdx.x] = log2_bias(reg);
   }
 };
 
@@ -576,7 +582,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_fwd(AttnArgs a) {
           const int d0 = t * KEYS - i - seq.off;
 #pragma unroll
           for (int n = 0; n < NB; ++n)
-            scores<MODE, false>(s[n], a, none, [&](int r) { return mine[min(max(d0 + n * 32 + row_of(r), -a.range), a.range)]; });
+            scores<MODE, false>(s[n], a, none, [&](int r) { return log2_bias(mine[min(max(d0 + n * 32 + row_of(r), -a.range), a.range)]); });
         } else {
           const float* mine = sbias[buf] + ROWS - 1 - (row - blk * ROWS) + 4 * (lane >> 5);
 #pragma unroll
@@ -584,14 +590,12 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_fwd(AttnArgs a) {
             scores<MODE, false>(s[n], a, none, [&](int r) { return mine[n * 32 + 8 * (r >> 2) + (r & 3)]; });
         }
       }
-      if (mixed || (t + 1) * KEYS > wmin) {
+      if ((t + 1) * KEYS > wmin)
 #pragma unroll
-        for (int n = 0; n < NB; ++n) {
-          const uint32_t hide = hidden(t * KEYS + n * 32, kend, kdoc ? sdoc[buf] + n * 32 : nullptr, doc);
+        for (int n = 0; n < NB; ++n) hide_from(s[n], kend - t * KEYS - n * 32, NEG_INF);
+      if (mixed)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[n][r] = hide >> r & 1 ? NEG_INF : s[n][r];
-        }
-      }
+        for (int n = 0; n < NB; ++n) hide_others(s[n], sdoc[buf] + n * 32, doc, NEG_INF);
       float top = s[0][0];
 #pragma unroll
       for (int n = 0; n < NB; ++n)
@@ -629,7 +633,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_fwd(AttnArgs a) {
   const float sum = both_sum(l);
   const bool none = kend == 0 || sum == 0.f;
   const float fit = exp2_(log2_of<MODE>(base - m, c1));  // (o and l belong to `base`)
-  const float ms = none ? NEG_INF : score_of<MODE>(m, a.scale), ls = none ? 0.f : sum * fit;
+  const float ms = none ? NEG_INF : log2_of<MODE>(m, c1), ls = none ? 0.f : sum * fit;
   if (a.splits > 1) {  // (a sum of zero leaves the part of o unwritten)
     const int64_t r = ((int64_t)split * a.batch + b) * a.heads * a.nq + (int64_t)head * a.nq + i;
     if (lane < 32) {
@@ -652,26 +656,32 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_fwd(AttnArgs a) {
   st_column<T, DP>((T*)a.o.p + b * a.o.b + (int64_t)i * a.o.t + head * a.o.h, a.dim, acc, none ? 0.f : 1.f / sum);
 }
 
-// The parts of the keys joined: one wave per query row.
+// The parts of the keys joined: one wave per query row, a lane a part for the sums.
+constexpr int MOST_SPLITS = 64;
 template <typename T, int DP>
 __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
   const int lane = threadIdx.x & 63;
   const int64_t rows = (int64_t)a.batch * a.heads * a.nq, r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (r >= rows) return;
   const int i = (int)(r % a.nq), head = (int)(r / a.nq % a.heads), b = (int)(r / a.nq / a.heads);
-  float m = NEG_INF;
-  for (int p = 0; p < a.splits; ++p) m = fmaxf(m, a.part_ml[2 * (p * rows + r)]);
-  const float base = m == NEG_INF ? 0.f : m;
-  float l = 0.f, o[DP / 64];
+  const bool has = lane < a.splits;
+  const float mp = has ? a.part_ml[2 * (lane * rows + r)] : NEG_INF, lp = has ? a.part_ml[2 * (lane * rows + r) + 1] : 0.f;
+  float m = mp;
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  const float w = lp == 0.f ? 0.f : exp2_(mp - m);
+  float l = lp * w;
+  for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
+  float o[DP / 64];
 #pragma unroll
   for (int d = 0; d < DP / 64; ++d) o[d] = 0.f;
-  for (int p = 0; p < a.splits; ++p) {
-    const float lp = a.part_ml[2 * (p * rows + r) + 1];
-    if (lp == 0.f) continue;  // (its part of o was not written)
-    const float w = exp2_((a.part_ml[2 * (p * rows + r)] - base) * LOG2E);
-    l += lp * w;
+#pragma unroll 8
+  for (int p = 0; p < a.splits; ++p) {  // (a part whose sum is zero was not written; of one that is NaN, l is)
+    const float wp = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), p));
 #pragma unroll
-    for (int d = 0; d < DP / 64; ++d) o[d] += w * (lp == lp ? a.part_o[(p * rows + r) * DP + d * 64 + lane] : lp);
+    for (int d = 0; d < DP / 64; ++d) {
+      const float v = a.part_o[(p * rows + r) * DP + d * 64 + lane];
+      o[d] += wp > 0.f ? wp * v : 0.f;
+    }
   }
   if (a.stats && lane == 0) {
     a.stats[2 * r] = m;
@@ -686,22 +696,21 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
 }
 
 // ---------------------------------------------------------------- statistics of a row
-// P = exp2(score - row.a) with the score in units of log 2, where row.a has the sum's logarithm in
-// it; BIAS: exp2((score - row.a) log2(e) - row.b) with the sum's logarithm apart.  A row without
-// keys gives 0.
+// P = exp2(score - row.a), where row.a has the sum's logarithm in it; BIAS (whose scores may be so
+// large that it would be lost there): exp2(score - row.a - row.b).  A row without keys gives 0.
 struct RowStat { float a, b; };
 template <int MODE>
 XP_DEV RowStat row_stat(float m, float l) {
   if (l == 0.f) return {__builtin_inff(), 0.f};
   const float log2l = __builtin_amdgcn_logf(l);
   if constexpr (MODE == BIAS) return {m, log2l};
-  else return {m * LOG2E + log2l, 0.f};
+  else return {m + log2l, 0.f};
 }
 template <int MODE>
 XP_DEV float weight(float s, float a, float b, float c1) {
   if constexpr (MODE == PLAIN) return exp2_(s * c1 - a);
   else if constexpr (MODE == CAP) return exp2_(s - a);
-  else return exp2_((s - a) * LOG2E - b);
+  else return exp2_((s - a) - b);
 }
 // What k_attn_dkv needs of 32 query rows: row.a, row.b, sum of P dP, kend, document, 32 each, and
 // room up to ROW_INFO floats.
@@ -832,11 +841,8 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dq(AttnArgs a) {
         }
 #pragma unroll
         for (int r = 0; r < 16; ++r) ds[r] = weight<MODE>(s[r], st.a, st.b, c1);
-        if (mixed || k0 + 32 > wmin) {
-          const uint32_t hide = hidden(k0, kend, kdoc ? sdoc[buf] + n * 32 : nullptr, doc);
-#pragma unroll
-          for (int r = 0; r < 16; ++r) ds[r] = hide >> r & 1 ? 0.f : ds[r];
-        }
+        if (k0 + 32 > wmin) hide_from(ds, kend - k0, 0.f);
+        if (mixed) hide_others(ds, sdoc[buf] + n * 32, doc, 0.f);
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           exact += ds[r] * dp[r];
@@ -1040,14 +1046,12 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dkv(AttnArgs a) {
       }
 #pragma unroll
       for (int r = 0; r < 16; ++r) p[r] = weight<MODE>(s[r], srow[buf][row_of(r)], MODE == BIAS ? srow[buf][32 + row_of(r)] : 0.f, c1);
-      const bool masked = mixed || i0 + QT > seq.ql || seq.kend(i0) < kw + 32;
-      if (masked) {
+      if (i0 + QT > seq.ql || seq.kend(i0) < kw + 32)
 #pragma unroll
         for (int r = 0; r < 16; ++r) p[r] = j >= __float_as_int(srow[buf][96 + row_of(r)]) ? 0.f : p[r];
-        if (qdoc)
+      if (mixed)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) p[r] = __float_as_int(srow[buf][128 + row_of(r)]) != doc ? 0.f : p[r];
-      }
+        for (int r = 0; r < 16; ++r) p[r] = __float_as_int(srow[buf][128 + row_of(r)]) != doc ? 0.f : p[r];
       if constexpr (WHAT & 1) {
         phase();
         add_transposed<T, DP>(dv, cat, TILE, p);
@@ -1163,12 +1167,15 @@ int rows_packed(const AttnArgs& a) {
 }
 
 // Parts of the keys where the rows alone do not fill the card (two workgroups a CU): at
-// least 4 steps each.
+// least 4 steps each.  Up to 32 rows a workgroup (a generation step) four times as many: what the
+// parts leave is little then, and sequences of different lengths even out (8 of 16384 to
+// 32768 tokens, 8 key heads of 128: 160 us with 512 workgroups).
 int parts(int dtype, const AttnArgs& a) {
   const int pk = rows_packed(a);
   const int64_t groups = ceil_div((int64_t)a.nq * pk, ROWS) * (a.heads / pk) * a.batch, steps = ceil_div(a.nk, keys_of(dtype));
   if (groups == 0 || groups >= 256) return 1;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(512, groups), steps / 4));
+  const int64_t want = (int64_t)a.nq * pk <= 32 ? 2048 : 512;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({ceil_div(want, groups), steps / 4, MOST_SPLITS}));
 }
 
 // blocks of 32 queries that hold distances within the range, of 32 keys

@@ -68,25 +68,41 @@ XP_DEV double run_sum(const float* p, int n) {
   return s;
 }
 
-// One workgroup per bucket and head: the bucket's distances are one run of the head's row.
-// THREADS: 1024 where runs are long (64 heads, 32768 distances: 129 us with 256 threads and
-// single values).
+// One workgroup per bucket and 4 heads: the bucket's distances are one run of each head's row.
+// Finding its ends costs as much as a short run, so one wave does it for all of them.
+// THREADS: 1024 where runs are long.
+constexpr int RUNS = 4;
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void k_relbias_bwd(const float* __restrict__ dbias, Buckets b, int heads, float* __restrict__ grad) {
-  __shared__ double sh[THREADS / 64];
-  const int k = blockIdx.x, h = blockIdx.y, side = b.both && k >= b.n, kk = side ? k - b.n : k;
-  const float* row = dbias + (int64_t)h * (2 * b.far + 1) + b.far;
-  const int lo = side ? max(first_of(b, kk), 1) : first_of(b, kk), hi = first_of(b, kk + 1);  // distances [lo, hi)
+  __shared__ double sh[RUNS][THREADS / 64];
+  __shared__ int ends[2];
+  const int k = blockIdx.x, side = b.both && k >= b.n, kk = side ? k - b.n : k, h0 = blockIdx.y * RUNS;
+  if (threadIdx.x < 64) {
+    const int d = first_of(b, kk + (threadIdx.x & 1));  // the bucket's distances: [ends[0], ends[1])
+    if (threadIdx.x < 2) ends[threadIdx.x] = d;
+  }
+  __syncthreads();
+  const int lo = side ? max(ends[0], 1) : ends[0], hi = ends[1];
   // (keys behind the query count as distance 0 where there is one direction)
   const int first = side ? lo : 1 - hi, last = side ? hi : !b.both && kk == 0 ? b.far + 1 : 1 - lo;
-  double s = wave_sum(run_sum<THREADS>(row + first, last - first));
-  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = s;
+  double s[RUNS];
+#pragma unroll
+  for (int i = 0; i < RUNS; ++i) {
+    const float* row = dbias + (int64_t)min(h0 + i, heads - 1) * (2 * b.far + 1) + b.far;
+    s[i] = run_sum<THREADS>(row + first, last - first);
+  }
+#pragma unroll
+  for (int i = 0; i < RUNS; ++i) {
+    s[i] = wave_sum(s[i]);
+    if ((threadIdx.x & 63) == 0) sh[i][threadIdx.x >> 6] = s[i];
+  }
   __syncthreads();
-  if (threadIdx.x == 0) {
+  const int h = h0 + threadIdx.x;
+  if (threadIdx.x < RUNS && h < heads) {
     float* g = grad + (int64_t)k * heads + h;
-    s = 0.0;
-    for (int w = 0; w < THREADS / 64; ++w) s += sh[w];
-    *g = (float)((double)*g + s);
+    double t = 0.0;
+    for (int w = 0; w < THREADS / 64; ++w) t += sh[threadIdx.x][w];
+    *g = (float)((double)*g + t);
   }
 }
 
@@ -111,7 +127,7 @@ hipError_t launch_relbias_fwd(const RelBiasArgs& a, hipStream_t s) {
 
 hipError_t launch_relbias_bwd(const RelBiasArgs& a, hipStream_t s) {
   const double bytes = 4.0 * (2 * a.far + 1) * a.heads;
-  const dim3 grid(a.buckets, a.heads);
+  const dim3 grid(a.buckets, (a.heads + RUNS - 1) / RUNS);
   if (a.far > 4096) XP_LAUNCH("k_relbias_bwd", bytes, k_relbias_bwd<1024>, grid, dim3(1024), 0, s, a.dbias, describe(a), a.heads, a.grad);
   else XP_LAUNCH("k_relbias_bwd", bytes, k_relbias_bwd<256>, grid, dim3(256), 0, s, a.dbias, describe(a), a.heads, a.grad);
   return hipGetLastError();

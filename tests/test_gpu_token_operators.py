@@ -360,7 +360,7 @@ class Case:
         value, tol = want["o"]
         _close(o.permute(0, 2, 1, 3), value, tol, "o")
         seen = want["l"][..., 0] > 0
-        m, l = _d(stats[..., 0]), _d(stats[..., 1])
+        m, l = _d(stats[..., 0]) * math.log(2), _d(stats[..., 1])
         assert torch.equal(l > 0, seen) and bool((m[~seen] == -math.inf).all()) and bool((o.permute(0, 2, 1, 3).cpu()[~seen] == 0).all())
         top, base, eps = want["m"]
         lse = (top[..., 0] + want["l"][..., 0].log())[seen]  # (m is one score's value or a rounding away from it)
