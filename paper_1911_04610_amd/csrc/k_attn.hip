@@ -29,12 +29,13 @@ namespace {
 constexpr float LOG2E = 1.44269504088896340736f;
 constexpr float NEG_INF = -__builtin_inff();
 constexpr int ROWS = 128;  // query rows (dk, dv: keys) of a workgroup: 4 waves of 32
-constexpr int QT = 32;     // queries of a step of k_attn_dkv
 
 template <typename T> constexpr int CHUNK = 16 / (int)sizeof(T);
 // keys of a step of the forward, and of k_attn_dq
 template <typename T> constexpr int BN = sizeof(T) == 2 ? 64 : 32;
 template <typename T, int DP> constexpr int BN_DQ = sizeof(T) == 2 && DP == 64 ? 64 : 32;
+// queries of a step of k_attn_dkv
+template <typename T, int DP> constexpr int QT_ = sizeof(T) == 2 && DP == 64 ? 64 : 32;
 // waves of a SIMD that a kernel's registers leave room for: 512 of them a lane, one wave
 // where both operands' columns and the results need more than 256
 template <typename T, int DP> constexpr int WAVES = sizeof(T) == 4 && DP == 128 ? 1 : 2;
@@ -107,15 +108,15 @@ XP_DEV void widen(const u32x4_t& u, float (&v)[CHUNK<T>]) {
 // registers, stored when the step before is done.  Rows are 16-byte aligned, of `dim`
 // elements in whole chunks; a chunk that is not to be read has an offset past the buffer's
 // end, which loads zeros.
-template <typename T, int DP, int N>
+template <typename T, int DP, int N, int THREADS = 256>
 struct Stager {
-  static constexpr int CPR = DP / CHUNK<T>, STEP = 256 / CPR, PER = N / STEP;
+  static constexpr int CPR = DP / CHUNK<T>, STEP = THREADS / CPR, PER = N / STEP;
   static_assert(N % STEP == 0 && PER >= 1, "whole passes");
   u32x4_t r[PER];
   int off;  // of the lane's chunk in the first rows, in bytes; negative behind dim
   int step;
   XP_DEV Stager(int64_t stride, int dim) {
-    const int c = threadIdx.x % CPR, at = threadIdx.x / CPR;
+    const int c = threadIdx.x % CPR, at = threadIdx.x % THREADS / CPR;
     off = c * CHUNK<T> < dim ? (int)((at * stride + c * CHUNK<T>) * (int64_t)sizeof(T)) : -1;
     step = (int)(STEP * stride * (int64_t)sizeof(T));
   }
@@ -127,7 +128,7 @@ struct Stager {
 #pragma unroll
       for (int i = 0; i < PER; ++i) r[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, off < 0 ? off : off + i * step, 0, 0);
     } else {
-      const int at = fresh(threadIdx.x) / CPR;
+      const int at = fresh(threadIdx.x) % THREADS / CPR;
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
         const int row = at + i * STEP;
@@ -138,7 +139,7 @@ struct Stager {
     }
   }
   XP_DEV void store(uint32_t tile) const {
-    const int tid = fresh(threadIdx.x), c = tid & (CPR - 1), at = (tid & 255) / CPR;
+    const int tid = fresh(threadIdx.x), c = tid & (CPR - 1), at = (tid & (THREADS - 1)) / CPR;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int row = at + i * STEP;
@@ -182,6 +183,10 @@ __global__ __launch_bounds__(256) void k_attn_pack(PackArgs a) {
     *reinterpret_cast<u32x4_t*>((T*)a.to[m] + i * CHUNK<T>) = ld_chunk(p, a.dim - c);
   }
 }
+
+// Nothing moves over this line: without it the compiler starts the next product's reads so
+// early that the registers do not hold them.
+XP_DEV void phase() { __builtin_amdgcn_sched_barrier(0); }
 
 // ---------------------------------------------------------------- products
 template <typename T>
@@ -239,6 +244,7 @@ XP_DEV f32x16_t rows_times(uint32_t at, int more, uint32_t col) {
   for (int s = 0; s < DP / CHUNK<T> / 2; ++s) {
     const u32x4_t row = *lds<u32x4_t>((at ^ (s * 32)) + more), mine = *lds<u32x4_t>(col ^ (s * 32));
     c = mma<T>(row, mine, c);
+    if (s % 2 == 1) phase();  // (at most four reads ahead: registers)
   }
   return c;
 }
@@ -298,10 +304,6 @@ XP_DEV void st_column(T* row, int dim, const f32x16_t (&acc)[DP / 32], float f) 
       }
     }
 }
-
-// Nothing moves over this line: without it the compiler starts the next product's reads so
-// early that the registers do not hold them.
-XP_DEV void phase() { __builtin_amdgcn_sched_barrier(0); }
 
 // ---------------------------------------------------------------- halves and waves
 // the larger, and the sum, of a value in lanes l and l ^ 32
@@ -427,7 +429,7 @@ XP_DEV float exp_of(float s, float base, float c1) {
 template <int MODE>
 XP_DEV float log2_of(float d, float c1) { return MODE == PLAIN ? d * c1 : d; }
 
-// Scores of a block of 32 x 32 from its products.  tanh(u) = 1 - 2 r with r = 1 / (1 + exp(2 u)),
+// Scores of a block of 32 x 32 from its products, in their place.  tanh(u) = 1 - 2 r with r = 1 / (1 + exp(2 u)),
 // off by at most 2^-23 of 1 (three roundings of values up to 1, the hardware's exponential and
 // reciprocal), its slope 4 r (1 - r); slope: of the cap (1 without one).  at(r): the bias of register r.
 template <int MODE, bool SLOPE, typename F>
@@ -476,12 +478,60 @@ struct BiasWindow {
 };
 
 // ---------------------------------------------------------------- forward
-// One workgroup per 128 query rows of a head (with pk > 1: of the pk heads that share keys,
-// row r being query r / pk of head r % pk), and part of the keys.
-//
-// The largest score enters the exponentials only when it has grown by more than 8 (base 2)
-// since it last did: P is then at most 2^8, the sums stay in fp32's range, and the results
-// are rarely multiplied.
+// The largest score with those of n blocks, and everything so far multiplied if it has grown by more than 8
+// (base 2) since it last entered the exponentials: P is at most 2^8 then, the sums stay in
+// fp32's range, and the results are rarely multiplied.
+template <int DP, int MODE>
+XP_DEV void softmax_step(const f32x16_t* s, int n, float& m, float& base, float& l, f32x16_t (&acc)[DP / 32], float c1) {
+  float top = s[0][0];
+  for (int i = 0; i < n; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) top = fmaxf(top, s[i][r]);
+  m = fmaxf(m, both_max(top));
+  if (__any(log2_of<MODE>(m - base, c1) > 8.f)) {  // (from -inf on: infinite; while there is no key: NaN)
+    const float keep = m == NEG_INF ? 1.f : exp2_(log2_of<MODE>(base - m, c1));
+    base = m;
+    l *= keep;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[d][r] *= keep;
+  }
+}
+
+// A lane's query row at the end: o and the statistics, or its part of them.
+template <typename T, int DP, int MODE>
+XP_DEV void write_rows(const AttnArgs& a, int b, int head, int i, int split, int kend, float m, float base, float l, f32x16_t (&acc)[DP / 32]) {
+  const float c1 = a.scale * LOG2E;
+  const bool low = (threadIdx.x & 63) < 32;
+  // (a NaN among the scores leaves l NaN, and the row NaN)
+  const float sum = both_sum(l);
+  const bool none = kend == 0 || sum == 0.f;
+  const float fit = exp2_(log2_of<MODE>(base - m, c1));  // (o and l belong to `base`)
+  const float ms = none ? NEG_INF : log2_of<MODE>(m, c1), ls = none ? 0.f : sum * fit;
+  if (a.splits > 1) {  // (a sum of zero leaves the part of o unwritten)
+    const int64_t r = ((int64_t)split * a.batch + b) * a.heads * a.nq + (int64_t)head * a.nq + i;
+    if (low) {
+      a.part_ml[2 * r] = ms;
+      a.part_ml[2 * r + 1] = ls;
+    }
+    st_column<float, DP>(a.part_o + r * DP, none ? 0 : DP, acc, fit);
+    return;
+  }
+  if (a.stats && low) {
+    float* st = a.stats + 2 * (((int64_t)b * a.heads + head) * a.nq + i);
+    st[0] = ms;
+    st[1] = ls;
+  }
+  if (none)
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
+  st_column<T, DP>((T*)a.o.p + b * a.o.b + (int64_t)i * a.o.t + head * a.o.h, a.dim, acc, none ? 0.f : 1.f / sum);
+}
+
+// One workgroup per 128 query rows of a head, and part of the keys.
 template <typename T, int DP, int MODE>
 __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_fwd(AttnArgs a) {
   constexpr int KEYS = BN<T>, NB = KEYS / 32;
@@ -491,25 +541,24 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_fwd(AttnArgs a) {
   __shared__ int sdoc[2][KEYS];
   __shared__ int sh[4][2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int rows = a.nq * a.pk, blocks = (rows + ROWS - 1) / ROWS, units = a.heads / a.pk;
+  const int blocks = (a.nq + ROWS - 1) / ROWS;
   int id = xcd_tile(blockIdx.x, gridDim.x);
   const int split = id % a.splits;
   id /= a.splits;
   const int blk = blocks - 1 - id % blocks;  // (causal: the longest first)
   id /= blocks;
-  const int unit = id % units, b = id / units;
-  const int kvh = unit * a.pk / (a.heads / a.kv_heads);
+  const int head = id % a.heads, b = id / a.heads;
+  const int kvh = head / (a.heads / a.kv_heads);
   const Seq seq(a, b);
 
   // limits of the workgroup's and the wave's rows (of those that count)
-  const int last = min((min(rows, (blk + 1) * ROWS) - 1) / a.pk, seq.ql - 1), first = blk * ROWS / a.pk;
+  const int last = min((blk + 1) * ROWS, min(a.nq, seq.ql)) - 1, first = blk * ROWS;
   const int kmax = first <= last ? seq.kend(last) : 0;
-  const int row0 = blk * ROWS + wave * 32;
-  const int wfirst = row0 / a.pk, wlast = min((row0 + 31) / a.pk, min(a.nq, seq.ql) - 1);
+  const int wfirst = first + wave * 32, wlast = min(wfirst + 31, last);
   const int wmax = wfirst <= wlast ? seq.kend(wlast) : 0, wmin = wfirst <= wlast ? seq.kend(wfirst) : 0;
 
-  const int row = row0 + (lane & 31), i = row / a.pk, head = unit * a.pk + row % a.pk;
-  const bool in = row < rows, live = in && i < seq.ql;
+  const int i = wfirst + (lane & 31);
+  const bool in = i < a.nq, live = in && i < seq.ql;
   const int doc = a.q_doc ? (live ? a.q_doc[(int64_t)b * a.nq + i] : -1) : 0;
   const int kend = live && doc >= 0 ? seq.kend(i) : 0;
   u32x4_t q[DP / CHUNK<T> / 2];
@@ -542,14 +591,14 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_fwd(AttnArgs a) {
     const int32_t* pad = kdoc && walk.tab[t].w ? kdoc + j0 : nullptr;
     ks.load(kp + (int64_t)j0 * a.k.t, seq.kl - j0, pad);
     vs.load(vp + (int64_t)j0 * a.v.t, seq.kl - j0, pad);
-    if (MODE == BIAS && a.pk == 1) window.load(a, unit, low + j0);
+    if constexpr (MODE == BIAS) window.load(a, head, low + j0);
     if (kdoc && threadIdx.x < KEYS) dreg = j0 + (int)threadIdx.x < seq.kl ? kdoc[j0 + threadIdx.x] : -1;
   };
   const uint32_t tile0 = lds_address(tiles_), rplace = row_place<T, DP>() + tile0, cplace = column_place<T, DP>() + tile0;
   auto store = [&](int buf) __attribute__((always_inline)) {
     ks.store(tile0 + buf * 2 * TILE);
     vs.store(tile0 + buf * 2 * TILE + TILE);
-    if (MODE == BIAS && a.pk == 1) window.store(sbias[buf]);
+    if constexpr (MODE == BIAS) window.store(sbias[buf]);
     if (kdoc && threadIdx.x < KEYS) sdoc[buf][threadIdx.x] = dreg;
   };
   int t = walk.next(min(tiles, split * per)), buf = 0;
@@ -577,18 +626,10 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_fwd(AttnArgs a) {
       __builtin_amdgcn_s_setprio(0);
       if constexpr (MODE != PLAIN) {
         float none[16];
-        if (MODE == BIAS && a.pk > 1) {
-          const float* mine = a.bias + (int64_t)min(head, a.heads - 1) * (2 * a.range + 1) + a.range;
-          const int d0 = t * KEYS - i - seq.off;
+        const float* mine = sbias[buf] + ROWS - 1 - (i - first) + 4 * (lane >> 5);
 #pragma unroll
-          for (int n = 0; n < NB; ++n)
-            scores<MODE, false>(s[n], a, none, [&](int r) { return log2_bias(mine[min(max(d0 + n * 32 + row_of(r), -a.range), a.range)]); });
-        } else {
-          const float* mine = sbias[buf] + ROWS - 1 - (row - blk * ROWS) + 4 * (lane >> 5);
-#pragma unroll
-          for (int n = 0; n < NB; ++n)
-            scores<MODE, false>(s[n], a, none, [&](int r) { return mine[n * 32 + 8 * (r >> 2) + (r & 3)]; });
-        }
+        for (int n = 0; n < NB; ++n)
+          scores<MODE, false>(s[n], a, none, [&](int r) { return mine[n * 32 + 8 * (r >> 2) + (r & 3)]; });
       }
       if ((t + 1) * KEYS > wmin)
 #pragma unroll
@@ -596,21 +637,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_fwd(AttnArgs a) {
       if (mixed)
 #pragma unroll
         for (int n = 0; n < NB; ++n) hide_others(s[n], sdoc[buf] + n * 32, doc, NEG_INF);
-      float top = s[0][0];
-#pragma unroll
-      for (int n = 0; n < NB; ++n)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[n][r]);
-      m = fmaxf(m, both_max(top));
-      if (__any(log2_of<MODE>(m - base, c1) > 8.f)) {  // (from -inf on: infinite; while there is no key: NaN)
-        const float keep = m == NEG_INF ? 1.f : exp2_(log2_of<MODE>(base - m, c1));
-        base = m;
-        l *= keep;
-#pragma unroll
-        for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) acc[d][r] *= keep;
-      }
+      softmax_step<DP, MODE>(s, NB, m, base, l, acc, c1);
       const float off = base == NEG_INF ? 0.f : base;
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
@@ -628,41 +655,101 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_fwd(AttnArgs a) {
     t = tn;
   }
 
-  if (!in) return;
-  // (a NaN among the scores leaves l NaN, and the row NaN)
-  const float sum = both_sum(l);
-  const bool none = kend == 0 || sum == 0.f;
-  const float fit = exp2_(log2_of<MODE>(base - m, c1));  // (o and l belong to `base`)
-  const float ms = none ? NEG_INF : log2_of<MODE>(m, c1), ls = none ? 0.f : sum * fit;
-  if (a.splits > 1) {  // (a sum of zero leaves the part of o unwritten)
-    const int64_t r = ((int64_t)split * a.batch + b) * a.heads * a.nq + (int64_t)head * a.nq + i;
-    if (lane < 32) {
-      a.part_ml[2 * r] = ms;
-      a.part_ml[2 * r + 1] = ls;
-    }
-    st_column<float, DP>(a.part_o + r * DP, none ? 0 : DP, acc, fit);
-    return;
-  }
-  if (a.stats && lane < 32) {
-    float* st = a.stats + 2 * (((int64_t)b * a.heads + head) * a.nq + i);
-    st[0] = ms;
-    st[1] = ls;
-  }
-  if (none)
-#pragma unroll
-    for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
-  st_column<T, DP>((T*)a.o.p + b * a.o.b + (int64_t)i * a.o.t + head * a.o.h, a.dim, acc, none ? 0.f : 1.f / sum);
+  if (in) write_rows<T, DP, MODE>(a, b, head, i, split, kend, m, base, l, acc);
 }
 
-// The parts of the keys joined: one wave per query row, a lane a part for the sums.
+// Few query rows (a generation step): a wave takes up to 32 rows of the heads that share keys
+// together, row r being query r / pk of head r % pk, and a part of the keys by itself, 32 at a
+// time through LDS of its own, the next 32 on their way: four times the bytes in flight
+// that the workgroups of k_attn_fwd have, whose other waves would have no rows.
+template <typename T, int DP, int MODE>
+__global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_few(AttnArgs a) {
+  constexpr int TILE = 32 * ROW<T, DP>;
+  __shared__ __attribute__((aligned(1024))) unsigned char tiles_[4 * 2 * TILE];  // of each wave: keys, values
+  __shared__ int sdoc[4][32];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rows = a.nq * a.pk, blocks = (rows + 31) / 32, units = a.kv_heads;
+  // (nothing is read twice: neighbours, the heads of the same keys, go to different XCDs, and so
+  // do the parts of one sequence, which may be the longest)
+  int id = blockIdx.x;
+  const int kvh = id % units;
+  id /= units;
+  const int groups = a.splits / 4, split = id % groups * 4 + wave;
+  id /= groups;
+  const int blk = id % blocks, b = id / blocks;
+  const Seq seq(a, b);
+
+  const int first = blk * 32 / a.pk, last = min((min(rows, (blk + 1) * 32) - 1) / a.pk, seq.ql - 1);
+  const int kmax = first <= last ? seq.kend(last) : 0, kmin = first <= last ? seq.kend(first) : 0;
+  const int row = blk * 32 + (lane & 31), i = row / a.pk, head = kvh * a.pk + row % a.pk;
+  const bool in = row < rows, live = in && i < seq.ql;
+  const int doc = a.q_doc ? (live ? a.q_doc[(int64_t)b * a.nq + i] : -1) : 0;
+  const int kend = live && doc >= 0 ? seq.kend(i) : 0;
+  u32x4_t q[DP / CHUNK<T> / 2];
+  ld_column<T, DP>((const T*)a.q.p + b * a.q.b + (int64_t)i * a.q.t + head * a.q.h, live, a.ldim, q);
+  const T* kp = (const T*)a.k.p + b * a.k.b + kvh * a.k.h;
+  const T* vp = (const T*)a.v.p + b * a.v.b + kvh * a.v.h;
+  const int32_t* kdoc = a.k_doc ? a.k_doc + (int64_t)b * a.nk : nullptr;
+  const float* bias = MODE == BIAS ? a.bias + (int64_t)min(head, a.heads - 1) * (2 * a.range + 1) + a.range : nullptr;
+
+  // (documents: every step is looked at, their tiles have no table here)
+  const int steps = (kmax + 31) / 32, per = (steps + a.splits - 1) / a.splits;
+  const int end = min(steps, (split + 1) * per);
+  const float c1 = a.scale * LOG2E;
+  float m = NEG_INF, base = NEG_INF, l = 0.f;
+  f32x16_t acc[DP / 32];
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
+
+  Stager<T, DP, 32, 64> ks(a.k.t, a.ldim), vs(a.v.t, a.ldim);
+  int dreg = -1;
+  auto load = [&](int t) __attribute__((always_inline)) {
+    const int j0 = t * 32;
+    ks.load(kp + (int64_t)j0 * a.k.t, seq.kl - j0, kdoc ? kdoc + j0 : nullptr);
+    vs.load(vp + (int64_t)j0 * a.v.t, seq.kl - j0, kdoc ? kdoc + j0 : nullptr);
+    if (kdoc) dreg = lane < 32 && j0 + lane < seq.kl ? kdoc[j0 + lane] : -1;
+  };
+  const uint32_t tile = lds_address(tiles_) + wave * 2 * TILE, rplace = row_place<T, DP>() + tile, cplace = column_place<T, DP>() + tile;
+  int t = min(steps, split * per);
+  if (t < end) load(t);
+  for (; t < end; ++t) {
+    ks.store(tile);
+    vs.store(tile + TILE);
+    if (kdoc && lane < 32) sdoc[wave][lane] = dreg;
+    const int next = t + 1;
+    if (next < end) load(next);
+    const int j0 = t * 32;
+    f32x16_t s = rows_times<T, DP>(rplace, 0, q);
+    if constexpr (MODE != PLAIN) {
+      float none[16];
+      const int d0 = j0 - i - seq.off;
+      scores<MODE, false>(s, a, none, [&](int r) { return log2_bias(bias[min(max(d0 + row_of(r), -a.range), a.range)]); });
+    }
+    if (j0 + 32 > kmin || blk == blocks - 1) hide_from(s, kend - j0, NEG_INF);
+    if (kdoc) hide_others(s, sdoc[wave], doc, NEG_INF);
+    float p[16];
+    softmax_step<DP, MODE>(&s, 1, m, base, l, acc, c1);
+    const float off = base == NEG_INF ? 0.f : base;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      p[r] = exp_of<MODE>(s[r], off, c1);
+      l += p[r];
+    }
+    add_transposed<T, DP>(acc, cplace, TILE, p);
+  }
+  if (in) write_rows<T, DP, MODE>(a, b, head, i, split, kend, m, base, l, acc);
+}
+
+// The parts of the keys joined: one workgroup per query row, a lane a part for the sums, a wave
+// every fourth part for o.
 constexpr int MOST_SPLITS = 64;
 template <typename T, int DP>
 __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t rows = (int64_t)a.batch * a.heads * a.nq, r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (r >= rows) return;
+  __shared__ float sh[4][DP];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t rows = (int64_t)a.batch * a.heads * a.nq, r = blockIdx.x;
   const int i = (int)(r % a.nq), head = (int)(r / a.nq % a.heads), b = (int)(r / a.nq / a.heads);
   const bool has = lane < a.splits;
   const float mp = has ? a.part_ml[2 * (lane * rows + r)] : NEG_INF, lp = has ? a.part_ml[2 * (lane * rows + r) + 1] : 0.f;
@@ -675,7 +762,7 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
 #pragma unroll
   for (int d = 0; d < DP / 64; ++d) o[d] = 0.f;
 #pragma unroll 8
-  for (int p = 0; p < a.splits; ++p) {  // (a part whose sum is zero was not written; of one that is NaN, l is)
+  for (int p = wave; p < a.splits; p += 4) {  // (a part whose sum is zero was not written; of one that is NaN, l is)
     const float wp = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), p));
 #pragma unroll
     for (int d = 0; d < DP / 64; ++d) {
@@ -683,15 +770,17 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
       o[d] += wp > 0.f ? wp * v : 0.f;
     }
   }
-  if (a.stats && lane == 0) {
+#pragma unroll
+  for (int d = 0; d < DP / 64; ++d) sh[wave][d * 64 + lane] = o[d];
+  __syncthreads();
+  if (a.stats && threadIdx.x == 0) {
     a.stats[2 * r] = m;
     a.stats[2 * r + 1] = l;
   }
-  T* out = (T*)a.o.p + b * a.o.b + (int64_t)i * a.o.t + head * a.o.h;
-#pragma unroll
-  for (int d = 0; d < DP / 64; ++d) {
-    const int at = d * 64 + lane;
-    if (at < a.dim) std_(out + at, (double)(l == 0.f ? 0.f : o[d] / l));
+  if ((int)threadIdx.x < a.dim) {
+    const int d = threadIdx.x;
+    const float v = (sh[0][d] + sh[1][d]) + (sh[2][d] + sh[3][d]);
+    std_((T*)a.o.p + b * a.o.b + (int64_t)i * a.o.t + head * a.o.h + d, (double)(l == 0.f ? 0.f : v / l));
   }
 }
 
@@ -924,11 +1013,11 @@ __global__ __launch_bounds__(1024) void k_attn_dbias(AttnArgs a) {
 // bf16 rows of 128: the values' columns stay in LDS, for 32 registers less.
 template <typename T, int DP, int MODE, int WHAT>
 __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dkv(AttnArgs a) {
-  constexpr int TILE = QT * ROW<T, DP>;
+  constexpr int QT = QT_<T, DP>, TILE = QT * ROW<T, DP>;
   constexpr bool V_LDS = sizeof(T) == 2 && DP == 128;
   __shared__ __attribute__((aligned(1024))) unsigned char tiles_[4 * TILE + (V_LDS ? ROWS * ROW<T, DP> : 0)];  // q, dout, twice; values
   __shared__ float sbias[2][MODE == BIAS ? ROWS + QT : 1];
-  __shared__ float srow[2][5 * QT];
+  __shared__ float srow[2][5 * QT];  // five values of 32 queries, then of the next 32
   __shared__ int sh[4][2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int blocks = (a.nk + ROWS - 1) / ROWS, group = a.heads / a.kv_heads;
@@ -998,20 +1087,24 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dkv(AttnArgs a) {
   const int row_tiles = (a.nq + ROWS - 1) / ROWS * 4;
   BiasWindow<ROWS + QT> window;
   const int low = k0 - (QT - 1) - seq.off;  // the window's smallest distance, of tile 0
-  float rreg = 0.f;
+  float rreg[QT / 32];
   auto load = [&](int t, int head) __attribute__((always_inline)) {
     const int i0 = t * QT;
     const int32_t* pads = qdoc && walk.tab[t].w ? qdoc + i0 : nullptr;
     qs.load((const T*)a.q.p + b * a.q.b + head * a.q.h + i0 * a.q.t, seq.ql - i0, pads);
     gs.load((const T*)a.dout.p + b * a.dout.b + head * a.dout.h + i0 * a.dout.t, seq.ql - i0, pads);
     if constexpr (MODE == BIAS) window.load(a, head, low - i0);
-    if (threadIdx.x < 5 * QT) rreg = a.rows[(((int64_t)b * a.heads + head) * row_tiles + t) * ROW_INFO + threadIdx.x];
+    if (threadIdx.x < 5 * 32)
+#pragma unroll
+      for (int n = 0; n < QT / 32; ++n) rreg[n] = a.rows[(((int64_t)b * a.heads + head) * row_tiles + t * (QT / 32) + n) * ROW_INFO + threadIdx.x];
   };
   auto store = [&](int buf) __attribute__((always_inline)) {
     qs.store(tile0 + buf * 2 * TILE);
     gs.store(tile0 + buf * 2 * TILE + TILE);
     if constexpr (MODE == BIAS) window.store(sbias[buf]);
-    if (threadIdx.x < 5 * QT) srow[buf][threadIdx.x] = rreg;
+    if (threadIdx.x < 5 * 32)
+#pragma unroll
+      for (int n = 0; n < QT / 32; ++n) srow[buf][n * 5 * 32 + threadIdx.x] = rreg[n];
   };
   int head = h0, t = walk.next(t0), buf = 0;
   const int t_first = t;
@@ -1028,42 +1121,48 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dkv(AttnArgs a) {
     }
     if (hn < h1) load(tn, hn);
     __syncthreads();
-    const int i0 = t * QT, i1 = min(i0 + QT, seq.ql) - 1;
-    bool mixed = false, skip = seq.kend(i1) <= kw;
+    bool mixed = false, other = false;
     if (qdoc) {
       const int4 e = walk.tab[t];
-      skip = skip || e.x > docs.whi || e.y < docs.wlo;
+      other = e.x > docs.whi || e.y < docs.wlo;
       mixed = e.z || pad || docs.wlo != docs.whi;
     }
-    if (!skip) {
+    // (a function called for each block: an unrolled loop of one round leaves more values in registers)
+    auto block = [&](int n) __attribute__((always_inline)) {
+      const int i0 = t * QT + n * 32, i1 = min(i0 + 32, seq.ql) - 1;
+      if (other || i0 >= seq.ql || seq.kend(i1) <= kw) return;
       const uint32_t rat = rplace + buf * 2 * TILE, cat = cplace + buf * 2 * TILE;
-      f32x16_t s = rows_times<T, DP>(rat, 0, kc);
+      f32x16_t s = rows_times<T, DP>(rat, n * 32 * ROW<T, DP>, kc);
       phase();
       float p[16], slope[16];
-      if constexpr (MODE != PLAIN) {  // (register r's place in the window: key - query + 31)
-        const float* mine = sbias[buf] + (j - k0) + 4 - 4 * (lane >> 5);
+      if constexpr (MODE != PLAIN) {  // (register r's place in the window: key - query + QT - 1)
+        const float* mine = sbias[buf] + (MODE == BIAS ? (j - k0) + QT - 28 - 4 * (lane >> 5) - n * 32 : 0);
         scores<MODE, (WHAT & 2) != 0>(s, a, slope, [&](int r) { return mine[27 - 8 * (r >> 2) - (r & 3)]; });
       }
+      auto of = [&](int what, int r) __attribute__((always_inline)) { return srow[buf][n * (5 * 32) + what * 32 + row_of(r)]; };
 #pragma unroll
-      for (int r = 0; r < 16; ++r) p[r] = weight<MODE>(s[r], srow[buf][row_of(r)], MODE == BIAS ? srow[buf][32 + row_of(r)] : 0.f, c1);
-      if (i0 + QT > seq.ql || seq.kend(i0) < kw + 32)
+      for (int r = 0; r < 16; ++r) p[r] = weight<MODE>(s[r], of(0, r), MODE == BIAS ? of(1, r) : 0.f, c1);
+      if (i0 + 32 > seq.ql || seq.kend(i0) < kw + 32)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) p[r] = j >= __float_as_int(srow[buf][96 + row_of(r)]) ? 0.f : p[r];
+        for (int r = 0; r < 16; ++r) p[r] = j >= __float_as_int(of(3, r)) ? 0.f : p[r];
       if (mixed)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) p[r] = __float_as_int(srow[buf][128 + row_of(r)]) != doc ? 0.f : p[r];
+        for (int r = 0; r < 16; ++r) p[r] = __float_as_int(of(4, r)) != doc ? 0.f : p[r];
       if constexpr (WHAT & 1) {
         phase();
-        add_transposed<T, DP>(dv, cat, TILE, p);
+        add_transposed<T, DP>(dv, cat, TILE + n * 32 * ROW<T, DP>, p);
         phase();
       }
       if constexpr (WHAT & 2) {
         f32x16_t dp;
-        if constexpr (V_LDS) dp = rows_times<T, DP>(rat, TILE, (uint32_t)fresh(vplace));
-        else dp = rows_times<T, DP>(rat, TILE, vc);
+        if constexpr (V_LDS) dp = rows_times<T, DP>(rat, TILE + n * 32 * ROW<T, DP>, (uint32_t)fresh(vplace));
+        else dp = rows_times<T, DP>(rat, TILE + n * 32 * ROW<T, DP>, vc);
         phase();
 #pragma unroll
-        for (int r = 0; r < 16; ++r) p[r] *= dp[r] - srow[buf][64 + row_of(r)];
+        for (int r = 0; r < 16; ++r) {
+          p[r] *= dp[r] - of(2, r);
+          if (DP == 128 && r % 4 == 3) phase();
+        }
         if (diag) {
           const int dlow = kw - i0 - 31 - seq.off;  // the block's smallest distance
           if (dlow + 62 <= -a.range || dlow >= a.range) {
@@ -1091,7 +1190,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dkv(AttnArgs a) {
             if (d <= -a.range) left += lo;
             else if (d >= a.range) right += lo;
             const int64_t w = ((int64_t)b * a.heads + head) * wblocks + wblock;
-            a.diag[(w * a.near + (t - near0)) * 64 + lane] = outer ? 0.f : lo;
+            a.diag[(w * a.near + ((i0 >> 5) - near0)) * 64 + lane] = outer ? 0.f : lo;
           }
         }
         if constexpr (MODE != PLAIN) {
@@ -1099,9 +1198,11 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dkv(AttnArgs a) {
           for (int r = 0; r < 16; ++r) p[r] *= slope[r];
         }
         phase();
-        add_transposed<T, DP>(dk, cat, 0, p);
+        add_transposed<T, DP>(dk, cat, n * 32 * ROW<T, DP>, p);
       }
-    }
+    };
+    block(0);
+    if constexpr (QT == 64) block(1);
     if (diag && hn != head) {  // the head's last step
       for (int o = 32; o > 0; o >>= 1) {
         left += __shfl_xor(left, o, 64);
@@ -1157,25 +1258,25 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 int padded_dim(int dim) { return dim <= 64 ? 64 : 128; }
 int keys_of(int dtype) { return dtype == DT_BF16 ? BN<bf16_t> : BN<float>; }
+int q_step_of(int dtype, const AttnArgs& a) { return dtype == DT_BF16 && a.dim <= 64 ? QT_<bf16_t, 64> : 32; }
 int dq_keys_of(int dtype, const AttnArgs& a) { return dtype == DT_BF16 && a.dim <= 64 ? BN_DQ<bf16_t, 64> : 32; }
 
-// Few query rows: those of the heads that share keys go into one workgroup, which then reads
-// the keys once for all of them.
-int rows_packed(const AttnArgs& a) {
-  const int group = a.heads / a.kv_heads;
-  return (int64_t)a.nq * group <= ROWS ? group : 1;
-}
+// Few query rows (k_attn_few): those of the heads that share keys go together, for keys that are
+// read once for all of them.  Up to 64: twice the keys' reads, by then from the L2.
+bool few(const AttnArgs& a) { return (int64_t)a.nq * (a.heads / a.kv_heads) <= 64; }
 
-// Parts of the keys where the rows alone do not fill the card (two workgroups a CU): at
-// least 4 steps each.  Up to 32 rows a workgroup (a generation step) four times as many: what the
-// parts leave is little then, and sequences of different lengths even out (8 of 16384 to
-// 32768 tokens, 8 key heads of 128: 160 us with 512 workgroups).
+// Parts of the keys where the rows alone do not fill the card: for k_attn_fwd two workgroups a
+// CU, at least 4 steps each; for k_attn_few (a wave each, in fours) 16 waves a CU, at least 4
+// steps of 32 keys: what the parts leave is little there, and sequences of different lengths even out.
 int parts(int dtype, const AttnArgs& a) {
-  const int pk = rows_packed(a);
-  const int64_t groups = ceil_div((int64_t)a.nq * pk, ROWS) * (a.heads / pk) * a.batch, steps = ceil_div(a.nk, keys_of(dtype));
+  if (few(a)) {
+    const int64_t groups = ceil_div((int64_t)a.nq * a.pk, 32) * a.kv_heads * a.batch;
+    if (groups == 0) return 4;
+    return (int)std::max<int64_t>(1, std::min<int64_t>({ceil_div(1024, groups), ceil_div(a.nk, 32) / 16, MOST_SPLITS / 4})) * 4;
+  }
+  const int64_t groups = ceil_div(a.nq, ROWS) * a.heads * a.batch, steps = ceil_div(a.nk, keys_of(dtype));
   if (groups == 0 || groups >= 256) return 1;
-  const int64_t want = (int64_t)a.nq * pk <= 32 ? 2048 : 512;
-  return (int)std::max<int64_t>(1, std::min<int64_t>({ceil_div(want, groups), steps / 4, MOST_SPLITS}));
+  return (int)std::max<int64_t>(1, std::min<int64_t>({ceil_div(512, groups), steps / 4, MOST_SPLITS}));
 }
 
 // blocks of 32 queries that hold distances within the range, of 32 keys
@@ -1184,14 +1285,14 @@ int near_blocks(const AttnArgs& a) { return (int)std::min<int64_t>(ceil_div(a.nq
 // Parts of k_attn_dkv where its blocks of keys do not fill the card twice over: heads that share
 // keys first, then runs of at least 8 steps of queries (with grad_bias heads alone: the
 // blocks' diagonals are laid out for one run).
-void cut_dkv(AttnArgs& a, int64_t kgroups) {
+void cut_dkv(int dtype, AttnArgs& a, int64_t kgroups) {
   const int group = a.heads / a.kv_heads;
   a.head_parts = a.q_parts = 1;
   if (kgroups == 0) return;
   for (int d = 1; d <= group && kgroups * a.head_parts < 512; ++d)
     if (group % d == 0) a.head_parts = d;
   const int64_t groups = kgroups * a.head_parts;
-  if (!a.grad_bias && groups < 512) a.q_parts = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(512, groups), ceil_div(a.nq, QT) / 8));
+  if (!a.grad_bias && groups < 512) a.q_parts = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(512, groups), ceil_div(a.nq, q_step_of(dtype, a)) / 8));
 }
 
 // Inputs whose rows are not whole, aligned chunks of 16 bytes are copied to such ones first:
@@ -1216,14 +1317,14 @@ size_t lay_fwd(int dtype, AttnArgs& a, char* base, AttnMat* from) {
   auto take = [&](size_t bytes) { size_t at = n; n += round256(bytes); return base ? base + at : nullptr; };
   AttnMat* m[3] = {&a.q, &a.k, &a.v};
   for (int i = 0; i < 3; ++i) n = lay_packed(dtype, a, *m[i], i ? a.nk : a.nq, i ? a.kv_heads : a.heads, base, n, from[i]);
-  a.pk = rows_packed(a);
+  a.pk = few(a) ? a.heads / a.kv_heads : 1;
   a.splits = parts(dtype, a);
   const int64_t rows = (int64_t)a.batch * a.heads * a.nq;
   if (a.splits > 1) {
     a.part_o = (float*)take((size_t)rows * a.splits * padded_dim(a.dim) * 4);
     a.part_ml = (float*)take((size_t)rows * a.splits * 8);
   }
-  if (a.k_doc) a.k_tab = (int4*)take((size_t)a.batch * ceil_div(a.nk, keys_of(dtype)) * sizeof(int4));
+  if (a.k_doc && !few(a)) a.k_tab = (int4*)take((size_t)a.batch * ceil_div(a.nk, keys_of(dtype)) * sizeof(int4));
   return n;
 }
 size_t lay_bwd(int dtype, AttnArgs& a, char* base, AttnMat* from) {
@@ -1235,13 +1336,13 @@ size_t lay_bwd(int dtype, AttnArgs& a, char* base, AttnMat* from) {
     n = lay_packed(dtype, a, *m[i], keys ? a.nk : a.nq, keys ? a.kv_heads : a.heads, base, n, from[i]);
   }
   const int64_t kgroups = ceil_div(a.nk, ROWS) * a.kv_heads * a.batch;
-  cut_dkv(a, kgroups);
+  cut_dkv(dtype, a, kgroups);
   if (a.head_parts * a.q_parts > 1)
     a.part_kv = (float*)take((size_t)a.batch * a.nk * a.kv_heads * a.head_parts * a.q_parts * 2 * padded_dim(a.dim) * 4);
   a.rows = (float*)take((size_t)a.batch * a.heads * ceil_div(a.nq, ROWS) * 4 * ROW_INFO * 4);
   if (a.k_doc) {
     a.k_tab = (int4*)take((size_t)a.batch * ceil_div(a.nk, dq_keys_of(dtype, a)) * sizeof(int4));
-    a.q_tab = (int4*)take((size_t)a.batch * ceil_div(a.nq, QT) * sizeof(int4));
+    a.q_tab = (int4*)take((size_t)a.batch * ceil_div(a.nq, q_step_of(dtype, a)) * sizeof(int4));
   }
   if (a.grad_bias) {
     const int64_t waves = (int64_t)a.batch * a.heads * ceil_div(a.nk, ROWS) * 4;
@@ -1283,11 +1384,16 @@ void launch_pack(int dtype, const AttnArgs& a, const AttnMat* from, const AttnMa
 template <typename T, int DP, int MODE>
 void fwd(const AttnArgs& a, hipStream_t s) {
   const double flops = 4.0 * a.batch * a.heads * a.nq * (double)a.nk * a.dim;
-  const int64_t groups = ceil_div((int64_t)a.nq * a.pk, ROWS) * (a.heads / a.pk) * a.batch * a.splits;
-  XP_LAUNCH(sizeof(T) == 2 ? "k_attn_fwd<bf16>" : "k_attn_fwd<f32>", flops, (k_attn_fwd<T, DP, MODE>), dim3((unsigned)groups), dim3(256), 0, s, a);
+  if (few(a)) {
+    const int64_t groups = ceil_div((int64_t)a.nq * a.pk, 32) * a.kv_heads * a.batch * (a.splits / 4);
+    XP_LAUNCH(sizeof(T) == 2 ? "k_attn_few<bf16>" : "k_attn_few<f32>", flops, (k_attn_few<T, DP, MODE>), dim3((unsigned)groups), dim3(256), 0, s, a);
+  } else {
+    const int64_t groups = ceil_div(a.nq, ROWS) * a.heads * a.batch * a.splits;
+    XP_LAUNCH(sizeof(T) == 2 ? "k_attn_fwd<bf16>" : "k_attn_fwd<f32>", flops, (k_attn_fwd<T, DP, MODE>), dim3((unsigned)groups), dim3(256), 0, s, a);
+  }
   if (a.splits > 1) {
     const int64_t rows = (int64_t)a.batch * a.heads * a.nq;
-    XP_LAUNCH("k_attn_join", 4.0 * rows * a.splits * DP, (k_attn_join<T, DP>), dim3((unsigned)ceil_div(rows, 4)), dim3(256), 0, s, a);
+    XP_LAUNCH("k_attn_join", 4.0 * rows * a.splits * DP, (k_attn_join<T, DP>), dim3((unsigned)rows), dim3(256), 0, s, a);
   }
 }
 
@@ -1349,7 +1455,7 @@ hipError_t launch_attn_fwd(int dtype, AttnArgs a, void* workspace, hipStream_t s
   lay_fwd(dtype, a, (char*)workspace, from);
   const AttnMat* const to[3] = {&a.q, &a.k, &a.v};
   launch_pack(dtype, a, from, to, 3, s);
-  if (a.k_doc) launch_docs(a.k_doc, a.k_len, a.nk, a.batch, keys_of(dtype), a.k_tab, s);
+  if (a.k_tab) launch_docs(a.k_doc, a.k_len, a.nk, a.batch, keys_of(dtype), a.k_tab, s);
   by_kind(dtype, a, [&](auto t, auto d, auto g) { fwd<decltype(t), decltype(d)::value, decltype(g)::value>(a, s); });
   return hipGetLastError();
 }
@@ -1362,7 +1468,7 @@ hipError_t launch_attn_bwd(int dtype, AttnArgs a, void* workspace, hipStream_t s
   launch_pack(dtype, a, from, to, 4, s);
   if (a.k_doc) {
     launch_docs(a.k_doc, a.k_len, a.nk, a.batch, dq_keys_of(dtype, a), a.k_tab, s);
-    launch_docs(a.q_doc, a.q_len, a.nq, a.batch, QT, a.q_tab, s);
+    launch_docs(a.q_doc, a.q_len, a.nq, a.batch, q_step_of(dtype, a), a.q_tab, s);
   }
   by_kind(dtype, a, [&](auto t, auto d, auto g) { bwd<decltype(t), decltype(d)::value, decltype(g)::value>(a, s); });
   return hipGetLastError();
