@@ -417,8 +417,11 @@ XP_DEV void hide_others(V& s, const int* docs, int doc, float none) {
 // What the scores are, in units of log 2 (the exponential's):
 //   PLAIN  scale q.k; held as the products q.k (c1 = scale log2(e) comes in with the exponential)
 //   CAP    cap tanh(scale q.k / cap)
-//   BIAS   those or scale q.k, plus a bias
-enum { PLAIN = 0, CAP = 1, BIAS = 2 };
+//   BIAS   scale q.k plus a bias
+//   BOTH   CAP plus a bias
+enum { PLAIN = 0, CAP = 1, BIAS = 2, BOTH = 3 };
+constexpr bool has_cap(int mode) { return mode & CAP; }
+constexpr bool has_bias(int mode) { return mode & BIAS; }
 // exp(score - base); c1: as above
 template <int MODE>
 XP_DEV float exp_of(float s, float base, float c1) {
@@ -431,27 +434,22 @@ XP_DEV float log2_of(float d, float c1) { return MODE == PLAIN ? d * c1 : d; }
 
 // Scores of a block of 32 x 32 from its products, in their place.  tanh(u) = 1 - 2 r with r = 1 / (1 + exp(2 u)),
 // off by at most 2^-23 of 1 (three roundings of values up to 1, the hardware's exponential and
-// reciprocal), its slope 4 r (1 - r); slope: of the cap (1 without one).  at(r): the bias of register r.
+// reciprocal), its slope 4 r (1 - r); slope: of the cap.  at(r): the bias of register r.
 template <int MODE, bool SLOPE, typename F>
 XP_DEV void scores(f32x16_t& s, const AttnArgs& a, float (&slope)[16], F&& at) {
-  if (MODE == CAP || (MODE == BIAS && a.cap > 0.f)) {
+  if constexpr (has_cap(MODE)) {
     const float k = 2.f * LOG2E * a.scale / a.cap, top = a.cap * LOG2E;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const float q = __builtin_amdgcn_rcpf(1.f + exp2_(s[r] * k));
       s[r] = top - 2.f * top * q;
       if constexpr (SLOPE) slope[r] = 4.f * q - 4.f * q * q;
+      if constexpr (has_bias(MODE)) s[r] += at(r);
     }
-    if constexpr (MODE == BIAS)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] += at(r);
-  } else if constexpr (MODE == BIAS) {
+  } else if constexpr (has_bias(MODE)) {
     const float c1 = a.scale * LOG2E;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      s[r] = s[r] * c1 + at(r);
-      if constexpr (SLOPE) slope[r] = 1.f;
-    }
+    for (int r = 0; r < 16; ++r) s[r] = s[r] * c1 + at(r);
   }
 }
 
@@ -537,7 +535,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_fwd(AttnArgs a) {
   constexpr int KEYS = BN<T>, NB = KEYS / 32;
   constexpr int TILE = KEYS * ROW<T, DP>;
   __shared__ __attribute__((aligned(1024))) unsigned char tiles_[4 * TILE];  // keys, values, twice
-  __shared__ float sbias[2][MODE == BIAS ? ROWS + KEYS : 1];
+  __shared__ float sbias[2][has_bias(MODE) ? ROWS + KEYS : 1];
   __shared__ int sdoc[2][KEYS];
   __shared__ int sh[4][2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -591,14 +589,14 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_fwd(AttnArgs a) {
     const int32_t* pad = kdoc && walk.tab[t].w ? kdoc + j0 : nullptr;
     ks.load(kp + (int64_t)j0 * a.k.t, seq.kl - j0, pad);
     vs.load(vp + (int64_t)j0 * a.v.t, seq.kl - j0, pad);
-    if constexpr (MODE == BIAS) window.load(a, head, low + j0);
+    if constexpr (has_bias(MODE)) window.load(a, head, low + j0);
     if (kdoc && threadIdx.x < KEYS) dreg = j0 + (int)threadIdx.x < seq.kl ? kdoc[j0 + threadIdx.x] : -1;
   };
   const uint32_t tile0 = lds_address(tiles_), rplace = row_place<T, DP>() + tile0, cplace = column_place<T, DP>() + tile0;
   auto store = [&](int buf) __attribute__((always_inline)) {
     ks.store(tile0 + buf * 2 * TILE);
     vs.store(tile0 + buf * 2 * TILE + TILE);
-    if constexpr (MODE == BIAS) window.store(sbias[buf]);
+    if constexpr (has_bias(MODE)) window.store(sbias[buf]);
     if (kdoc && threadIdx.x < KEYS) sdoc[buf][threadIdx.x] = dreg;
   };
   int t = walk.next(min(tiles, split * per)), buf = 0;
@@ -690,7 +688,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_few(AttnArgs a) {
   const T* kp = (const T*)a.k.p + b * a.k.b + kvh * a.k.h;
   const T* vp = (const T*)a.v.p + b * a.v.b + kvh * a.v.h;
   const int32_t* kdoc = a.k_doc ? a.k_doc + (int64_t)b * a.nk : nullptr;
-  const float* bias = MODE == BIAS ? a.bias + (int64_t)min(head, a.heads - 1) * (2 * a.range + 1) + a.range : nullptr;
+  const float* bias = has_bias(MODE) ? a.bias + (int64_t)min(head, a.heads - 1) * (2 * a.range + 1) + a.range : nullptr;
 
   // (documents: every step is looked at, their tiles have no table here)
   const int steps = (kmax + 31) / 32, per = (steps + a.splits - 1) / a.splits;
@@ -792,7 +790,7 @@ template <int MODE>
 XP_DEV RowStat row_stat(float m, float l) {
   if (l == 0.f) return {__builtin_inff(), 0.f};
   const float log2l = __builtin_amdgcn_logf(l);
-  if constexpr (MODE == BIAS) return {m, log2l};
+  if constexpr (has_bias(MODE)) return {m, log2l};
   else return {m + log2l, 0.f};
 }
 template <int MODE>
@@ -819,7 +817,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dq(AttnArgs a) {
   constexpr int KEYS = BN_DQ<T, DP>, NB = KEYS / 32;
   constexpr int TILE = KEYS * ROW<T, DP>;
   __shared__ __attribute__((aligned(1024))) unsigned char tiles_[4 * TILE];  // keys, values, twice
-  __shared__ float sbias[2][MODE == BIAS ? ROWS + KEYS : 1];
+  __shared__ float sbias[2][has_bias(MODE) ? ROWS + KEYS : 1];
   __shared__ int sdoc[2][KEYS];
   __shared__ int sh[4][2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -889,14 +887,14 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dq(AttnArgs a) {
     const int32_t* pad = kdoc && walk.tab[t].w ? kdoc + j0 : nullptr;
     ks.load(kp + (int64_t)j0 * a.k.t, seq.kl - j0, pad);
     vs.load(vp + (int64_t)j0 * a.v.t, seq.kl - j0, pad);
-    if constexpr (MODE == BIAS) window.load(a, head, low + j0);
+    if constexpr (has_bias(MODE)) window.load(a, head, low + j0);
     if (kdoc && threadIdx.x < KEYS) dreg = j0 + (int)threadIdx.x < seq.kl ? kdoc[j0 + threadIdx.x] : -1;
   };
   const uint32_t tile0 = lds_address(tiles_), rplace = row_place<T, DP>() + tile0, cplace = column_place<T, DP>() + tile0;
   auto store = [&](int buf) __attribute__((always_inline)) {
     ks.store(tile0 + buf * 2 * TILE);
     vs.store(tile0 + buf * 2 * TILE + TILE);
-    if constexpr (MODE == BIAS) window.store(sbias[buf]);
+    if constexpr (has_bias(MODE)) window.store(sbias[buf]);
     if (kdoc && threadIdx.x < KEYS) sdoc[buf][threadIdx.x] = dreg;
   };
   int t = walk.next(0), buf = 0;
@@ -937,7 +935,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dq(AttnArgs a) {
           exact += ds[r] * dp[r];
           ds[r] *= dp[r] - delta;
         }
-        if constexpr (MODE != PLAIN) {
+        if constexpr (has_cap(MODE)) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) ds[r] *= slope[r];
         }
@@ -1016,7 +1014,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dkv(AttnArgs a) {
   constexpr int QT = QT_<T, DP>, TILE = QT * ROW<T, DP>;
   constexpr bool V_LDS = sizeof(T) == 2 && DP == 128;
   __shared__ __attribute__((aligned(1024))) unsigned char tiles_[4 * TILE + (V_LDS ? ROWS * ROW<T, DP> : 0)];  // q, dout, twice; values
-  __shared__ float sbias[2][MODE == BIAS ? ROWS + QT : 1];
+  __shared__ float sbias[2][has_bias(MODE) ? ROWS + QT : 1];
   __shared__ float srow[2][5 * QT];  // five values of 32 queries, then of the next 32
   __shared__ int sh[4][2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -1072,7 +1070,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dkv(AttnArgs a) {
     for (int r = 0; r < 16; ++r) d[r] = 0.f;
   const float c1 = a.scale * LOG2E;
 
-  const bool diag = MODE == BIAS && (WHAT & 2) && a.grad_bias;
+  const bool diag = has_bias(MODE) && (WHAT & 2) && a.grad_bias;
   float left = 0.f, right = 0.f;
   const int near0 = first_near(a, seq, kw);
   const int64_t wblock = blk * 4 + wave, wblocks = blocks * 4;
@@ -1093,7 +1091,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dkv(AttnArgs a) {
     const int32_t* pads = qdoc && walk.tab[t].w ? qdoc + i0 : nullptr;
     qs.load((const T*)a.q.p + b * a.q.b + head * a.q.h + i0 * a.q.t, seq.ql - i0, pads);
     gs.load((const T*)a.dout.p + b * a.dout.b + head * a.dout.h + i0 * a.dout.t, seq.ql - i0, pads);
-    if constexpr (MODE == BIAS) window.load(a, head, low - i0);
+    if constexpr (has_bias(MODE)) window.load(a, head, low - i0);
     if (threadIdx.x < 5 * 32)
 #pragma unroll
       for (int n = 0; n < QT / 32; ++n) rreg[n] = a.rows[(((int64_t)b * a.heads + head) * row_tiles + t * (QT / 32) + n) * ROW_INFO + threadIdx.x];
@@ -1101,7 +1099,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dkv(AttnArgs a) {
   auto store = [&](int buf) __attribute__((always_inline)) {
     qs.store(tile0 + buf * 2 * TILE);
     gs.store(tile0 + buf * 2 * TILE + TILE);
-    if constexpr (MODE == BIAS) window.store(sbias[buf]);
+    if constexpr (has_bias(MODE)) window.store(sbias[buf]);
     if (threadIdx.x < 5 * 32)
 #pragma unroll
       for (int n = 0; n < QT / 32; ++n) srow[buf][n * 5 * 32 + threadIdx.x] = rreg[n];
@@ -1136,12 +1134,12 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dkv(AttnArgs a) {
       phase();
       float p[16], slope[16];
       if constexpr (MODE != PLAIN) {  // (register r's place in the window: key - query + QT - 1)
-        const float* mine = sbias[buf] + (MODE == BIAS ? (j - k0) + QT - 28 - 4 * (lane >> 5) - n * 32 : 0);
+        const float* mine = sbias[buf] + (has_bias(MODE) ? (j - k0) + QT - 28 - 4 * (lane >> 5) - n * 32 : 0);
         scores<MODE, (WHAT & 2) != 0>(s, a, slope, [&](int r) { return mine[27 - 8 * (r >> 2) - (r & 3)]; });
       }
       auto of = [&](int what, int r) __attribute__((always_inline)) { return srow[buf][n * (5 * 32) + what * 32 + row_of(r)]; };
 #pragma unroll
-      for (int r = 0; r < 16; ++r) p[r] = weight<MODE>(s[r], of(0, r), MODE == BIAS ? of(1, r) : 0.f, c1);
+      for (int r = 0; r < 16; ++r) p[r] = weight<MODE>(s[r], of(0, r), has_bias(MODE) ? of(1, r) : 0.f, c1);
       if (i0 + 32 > seq.ql || seq.kend(i0) < kw + 32)
 #pragma unroll
         for (int r = 0; r < 16; ++r) p[r] = j >= __float_as_int(of(3, r)) ? 0.f : p[r];
@@ -1193,7 +1191,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dkv(AttnArgs a) {
             a.diag[(w * a.near + ((i0 >> 5) - near0)) * 64 + lane] = outer ? 0.f : lo;
           }
         }
-        if constexpr (MODE != PLAIN) {
+        if constexpr (has_cap(MODE)) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) p[r] *= slope[r];
         }
@@ -1282,17 +1280,18 @@ int parts(int dtype, const AttnArgs& a) {
 // blocks of 32 queries that hold distances within the range, of 32 keys
 int near_blocks(const AttnArgs& a) { return (int)std::min<int64_t>(ceil_div(a.nq, 32), ceil_div(2 * (int64_t)a.range + 62, 32) + 1); }
 
-// Parts of k_attn_dkv where its blocks of keys do not fill the card twice over: heads that share
-// keys first, then runs of at least 8 steps of queries (with grad_bias heads alone: the
-// blocks' diagonals are laid out for one run).
+// Parts of k_attn_dkv where its blocks of keys do not fill the card twice over (causal, where they
+// differ in length: four times): heads that share keys first, then runs of at least 8 steps
+// of queries (with grad_bias heads alone: the blocks' diagonals are laid out for one run).
 void cut_dkv(int dtype, AttnArgs& a, int64_t kgroups) {
-  const int group = a.heads / a.kv_heads;
+  const int group = a.heads / a.kv_heads, want = a.causal ? 1024 : 512;
   a.head_parts = a.q_parts = 1;
   if (kgroups == 0) return;
-  for (int d = 1; d <= group && kgroups * a.head_parts < 512; ++d)
+  for (int d = 1; d <= group && kgroups * a.head_parts < want; ++d)
     if (group % d == 0) a.head_parts = d;
   const int64_t groups = kgroups * a.head_parts;
-  if (!a.grad_bias && groups < 512) a.q_parts = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(512, groups), ceil_div(a.nq, q_step_of(dtype, a)) / 8));
+  if (!a.grad_bias && groups < want)
+    a.q_parts = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(want, groups), ceil_div(a.nq, q_step_of(dtype, a)) / 8));
 }
 
 // Inputs whose rows are not whole, aligned chunks of 16 bytes are copied to such ones first:
@@ -1425,7 +1424,8 @@ template <typename F>
 void by_kind(int dtype, const AttnArgs& a, F&& f) {
   using std::integral_constant;
   auto with = [&](auto t, auto d) {
-    if (a.bias) f(t, d, integral_constant<int, BIAS>{});
+    if (a.bias && a.cap > 0.f) f(t, d, integral_constant<int, BOTH>{});
+    else if (a.bias) f(t, d, integral_constant<int, BIAS>{});
     else if (a.cap > 0.f) f(t, d, integral_constant<int, CAP>{});
     else f(t, d, integral_constant<int, PLAIN>{});
   };

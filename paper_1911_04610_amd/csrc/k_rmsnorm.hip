@@ -5,9 +5,9 @@
 //   backward: g = dy w;  dx = n (g - h n^2 mean(g h)) + residual;  grad_w += sum over rows of dy h n
 //
 // Bandwidth-bound: a row is read once and held in the registers of the G threads
-// that share it (E elements each), the sums go over those threads.  Sums over a
-// row are fp64 (squares of fp32 values neither overflow nor lose bits there), the
-// rest is fp32, each stored value is rounded once.
+// that share it (E elements each), the sums go over those threads, in fp64 (squares of
+// fp32 values neither overflow nor lose bits there); the rest is fp32, each stored value
+// is rounded once.
 #include "xp_device.h"
 #include "xp_lds.h"
 #include "xp_kernels.h"
@@ -22,20 +22,36 @@ template <typename T> constexpr int CHUNK = 16 / (int)sizeof(T);
 
 // n elements (more than CHUNK: a whole chunk) from p on, which may start anywhere; zeros behind them
 template <typename T>
-XP_DEV void ld_elems(const T* p, int n, float* v) {
+XP_DEV u32x4_t ld_raw(const T* p, int n) {
+  u32x4_t u = {0, 0, 0, 0};
   if (n >= CHUNK<T>) {
-    u32x4_t u;
     __builtin_memcpy(&u, p, 16);
+  } else {
+    uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < CHUNK<T>; ++i) {
-      if constexpr (sizeof(T) == 4) v[i] = __uint_as_float(u[i]);
-      else v[i] = __uint_as_float(i & 1 ? u[i / 2] & 0xffff0000u : u[i / 2] << 16);
+      uint32_t e = 0;
+      if (i < n) {
+        if constexpr (sizeof(T) == 4) e = __float_as_uint(p[i]);
+        else e = p[i];
+      }
+      if constexpr (sizeof(T) == 4) w[i] = e;
+      else w[i / 2] |= e << (16 * (i & 1));
     }
-  } else {
+    u = (u32x4_t){w[0], w[1], w[2], w[3]};
+  }
+  return u;
+}
+template <typename T>
+XP_DEV void unpack(const u32x4_t& u, float* v) {
 #pragma unroll
-    for (int i = 0; i < CHUNK<T>; ++i) v[i] = i < n ? (float)ldd(p + i) : 0.f;
+  for (int i = 0; i < CHUNK<T>; ++i) {
+    if constexpr (sizeof(T) == 4) v[i] = __uint_as_float(u[i]);
+    else v[i] = __uint_as_float(i & 1 ? u[i / 2] & 0xffff0000u : u[i / 2] << 16);
   }
 }
+template <typename T>
+XP_DEV void ld_elems(const T* p, int n, float* v) { unpack<T>(ld_raw(p, n), v); }
 template <typename T>
 XP_DEV void st_elems(T* p, int n, const float* v) {
   if (n >= CHUNK<T>) {
@@ -79,6 +95,44 @@ XP_DEV void row_sums(double (&v)[N], double (*sh)[16], int turn) {
   }
 }
 
+// A thread's part of a row's sums.  In bf16 storage over E elements in fp32 (an fp64 sum takes
+// longer than the row's bytes do: 16384x4096 backward 164 us against 118); a row whose sum of squares leaves the
+// range where that is exact to fp32 is summed again in fp64.
+XP_DEV bool in_range(double squares) { return squares > 1e-20 && squares < 1e36; }
+template <typename T, int E>
+XP_DEV void squares(const float (&h)[E], double& out) {
+  if constexpr (sizeof(T) == 4) {
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < E; ++i) s += (double)h[i] * h[i];
+    out = s;
+  } else {
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < E; ++i) s[i & 3] += h[i] * h[i];
+    out = (double)((s[0] + s[1]) + (s[2] + s[3]));
+  }
+}
+template <typename T, int E>
+XP_DEV void products(const float (&h)[E], const float (&dy)[E], const float (&w)[E], double& out) {
+  if constexpr (sizeof(T) == 4) {
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < E; ++i) s += (double)(dy[i] * w[i]) * h[i];
+    out = s;
+  } else {
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < E; ++i) s[i & 3] += dy[i] * w[i] * h[i];
+    out = (double)((s[0] + s[1]) + (s[2] + s[3]));
+  }
+}
+template <int E>
+XP_DEV void wide_sums(const float (&h)[E], const float (&dy)[E], const float (&w)[E], double (&s)[2]) {
+  squares<float, E>(h, s[0]);
+  products<float, E>(h, dy, w, s[1]);
+}
+
 // No __restrict__: sum and y may be x's or residual's buffer (every element is read
 // by the thread that writes it, before).
 template <typename T, int G, int E>
@@ -112,10 +166,14 @@ __global__ __launch_bounds__(THREADS<G>) void k_rms_fwd(RmsArgs a) {
         for (int i = 0; i < C; ++i) h[j * C + i] += r[i];
       }
     }
-#pragma unroll
-    for (int i = 0; i < E; ++i) ss[0] += (double)h[i] * h[i];
+    squares<T, E>(h, ss[0]);
     row_sums<G, 1>(ss, sh, turn);
     turn ^= 1;
+    if (sizeof(T) == 2 && !in_range(ss[0])) {  // (the row's threads agree)
+      squares<float, E>(h, ss[0]);
+      row_sums<G, 1>(ss, sh, turn);
+      turn ^= 1;
+    }
     const float n = (float)(1.0 / sqrt(ss[0] / a.dim + a.eps));
 #pragma unroll
     for (int j = 0; j < V; ++j) {
@@ -131,44 +189,52 @@ __global__ __launch_bounds__(THREADS<G>) void k_rms_fwd(RmsArgs a) {
 
 // One workgroup's rows: their dx, and its part of grad_w: the sum of its rows' terms in
 // fp32 (at most a few hundred of them), over the ROWS rows at a time in LDS.  The parts
-// are added in fp64 by k_rms_join; a single workgroup adds its own.
+// are added in fp64 by k_rms_join; a single workgroup adds its own.  The next row's
+// h and dy are on their way while this one's sums are joined.
 template <typename T, int G, int E>
 __global__ __launch_bounds__(THREADS<G>) void k_rms_bwd(RmsArgs a) {
   constexpr int C = CHUNK<T>, V = E / C;
   __shared__ double sh[4][16];
   __shared__ float gsum[ROWS<G> > 1 ? G * E * ROWS<G> : 1];
   const int lt = threadIdx.x % G;
-  float acc[E];
+  float acc[E], w[E];
 #pragma unroll
   for (int i = 0; i < E; ++i) acc[i] = 0.f;
+#pragma unroll
+  for (int j = 0; j < V; ++j)
+#pragma unroll
+    for (int p = 0; p < C; p += 4) ld_elems(a.w + (lt + j * G) * C + p, min(4, a.dim - (lt + j * G) * C - p), w + j * C + p);
+  u32x4_t hr[V], dr[V];
+  auto fetch = [&](int64_t row) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const int at = (lt + j * G) * C;
+      hr[j] = ld_raw((const T*)a.x + row * a.ldx + at, a.dim - at);
+      dr[j] = ld_raw((const T*)a.dy + row * a.lddy + at, a.dim - at);
+    }
+  };
   int turn = 0;
-  for (int64_t row = (int64_t)blockIdx.x * ROWS<G> + threadIdx.x / G; row < a.rows; row += (int64_t)gridDim.x * ROWS<G>) {
+  const int64_t step = (int64_t)gridDim.x * ROWS<G>;
+  int64_t row = (int64_t)blockIdx.x * ROWS<G> + threadIdx.x / G;
+  if (row < a.rows) fetch(row);
+  for (; row < a.rows; row += step) {
     float h[E], dy[E];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const int at = (lt + j * G) * C;
-      ld_elems((const T*)a.x + row * a.ldx + at, a.dim - at, h + j * C);
-      ld_elems((const T*)a.dy + row * a.lddy + at, a.dim - at, dy + j * C);
+      unpack<T>(hr[j], h + j * C);
+      unpack<T>(dr[j], dy + j * C);
     }
-    double s[2] = {0.0, 0.0};
-    auto weight = [&](int j, float* w) __attribute__((always_inline)) {
-      const int at = (lt + j * G) * C;
-#pragma unroll
-      for (int p = 0; p < C; p += 4) ld_elems(a.w + at + p, min(4, a.dim - at - p), w + p);
-    };
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      float w[C];
-      weight(j, w);
-#pragma unroll
-      for (int i = 0; i < C; ++i) {
-        const int e = j * C + i;
-        s[0] += (double)h[e] * h[e];
-        s[1] += (double)(dy[e] * w[i]) * h[e];
-      }
-    }
+    if (row + step < a.rows) fetch(row + step);
+    double s[2];
+    squares<T, E>(h, s[0]);
+    products<T, E>(h, dy, w, s[1]);
     row_sums<G, 2>(s, sh, turn);
     turn ^= 1;
+    if (sizeof(T) == 2 && !in_range(s[0])) {  // (the row's threads agree)
+      wide_sums<E>(h, dy, w, s);
+      row_sums<G, 2>(s, sh, turn);
+      turn ^= 1;
+    }
     const double nd = 1.0 / sqrt(s[0] / a.dim + a.eps);
     const float n = (float)nd, c = (float)(nd * nd * s[1] / a.dim);
 #pragma unroll
@@ -177,12 +243,11 @@ __global__ __launch_bounds__(THREADS<G>) void k_rms_bwd(RmsArgs a) {
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const int at = (lt + j * G) * C;
-        float w[C], r[C], dx[C];
-        weight(j, w);
+        float r[C], dx[C];
         if (a.res) ld_elems((const T*)a.res + row * a.ldr + at, a.dim - at, r);
 #pragma unroll
         for (int i = 0; i < C; ++i) {
-          dx[i] = n * (dy[j * C + i] * w[i] - h[j * C + i] * c);
+          dx[i] = n * (dy[j * C + i] * w[j * C + i] - h[j * C + i] * c);
           if (a.res) dx[i] += r[i];
         }
         st_elems((T*)a.y + row * a.ldy + at, a.dim - at, dx);
@@ -236,11 +301,14 @@ __global__ __launch_bounds__(256) void k_rms_join(const float* __restrict__ part
   }
 }
 
-// calls f(threads a row, elements a thread) for rows of dim elements
+// calls f(threads a row, elements a thread) for rows of dim elements: a wave a row where it holds
+// it (8192x2048 backward 30.5 us; 256 threads of 8 elements each 34.8)
 template <typename F>
 void by_size(int dim, F&& f) {
   using std::integral_constant;
   if (dim <= 64) f(integral_constant<int, 8>{}, integral_constant<int, 8>{});
+  else if (dim <= 128) f(integral_constant<int, 16>{}, integral_constant<int, 8>{});
+  else if (dim <= 256) f(integral_constant<int, 32>{}, integral_constant<int, 8>{});
   else if (dim <= 512) f(integral_constant<int, 64>{}, integral_constant<int, 8>{});
   else if (dim <= 1024) f(integral_constant<int, 64>{}, integral_constant<int, 16>{});
   else if (dim <= 2048) f(integral_constant<int, 64>{}, integral_constant<int, 32>{});
@@ -257,7 +325,7 @@ template <typename T>
 hipError_t fwd(const RmsArgs& a, hipStream_t s) {
   by_size(a.dim, [&](auto G, auto E) {
     constexpr int g = decltype(G)::value, e = decltype(E)::value;
-    const int blocks = (int)std::min<int64_t>((a.rows + ROWS<g> - 1) / ROWS<g>, g >= 1024 ? 512 : 2048);
+    const int blocks = (int)std::min<int64_t>((a.rows + ROWS<g> - 1) / ROWS<g>, g <= 64 && e == 8 ? 2048 : 1 << 30);
     const double bytes = (double)sizeof(T) * a.rows * a.dim * (2 + (a.res != nullptr) + (a.out != nullptr));
     XP_LAUNCH(sizeof(T) == 2 ? "k_rms_fwd<bf16>" : "k_rms_fwd<f32>", bytes, (k_rms_fwd<T, g, e>), dim3(blocks),
               dim3(THREADS<g>), 0, s, a);
