@@ -38,7 +38,7 @@ template <typename T, int DP> constexpr int BN_DQ = sizeof(T) == 2 && DP == 64 ?
 template <typename T, int DP> constexpr int QT_ = sizeof(T) == 2 && DP == 64 ? 64 : 32;
 // waves of a SIMD that a kernel's registers leave room for: 512 of them a lane, one wave
 // where both operands' columns and the results need more than 256
-template <typename T, int DP> constexpr int WAVES = sizeof(T) == 4 && DP == 128 ? 1 : 2;
+template <typename T, int DP> constexpr int WAVES = sizeof(T) == 4 && DP > 64 ? 1 : 2;
 
 // ---------------------------------------------------------------- tiles in LDS
 // Rows of DP elements, chunk c of row r at position c ^ swz(r).  Read along rows, 16
@@ -48,11 +48,12 @@ template <typename T, int DP> constexpr int WAVES = sizeof(T) == 4 && DP == 128 
 template <typename T, int DP>
 XP_DEV int swz(int r) {
   if constexpr (sizeof(T) == 4) return ((r >> 2) & 1) << 3 | ((r >> 3) & 1) << 2 | (r & 3);
-  else if constexpr (DP == 128) return (r & 3) << 2 | ((r >> 2) & 3);
+  else if constexpr (DP > 64) return (r & 3) << 2 | ((r >> 2) & 3);
   else return ((r >> 1) & 1) << 2 | ((r >> 2) & 3);
 }
 
-template <typename T, int DP> constexpr int ROW = DP * (int)sizeof(T);  // bytes
+template <int DP> constexpr int PITCH = DP == 64 ? 64 : 128;  // elements: rows of 96 lie as those of 128 do
+template <typename T, int DP> constexpr int ROW = PITCH<DP> * (int)sizeof(T);  // bytes
 // Tiles are named by their byte address in LDS, a multiple of ROW: where a lane's reads differ in
 // the chunk, they then differ by an exclusive or of a constant, and where they differ in the
 // row, by an offset in the instruction.
@@ -110,7 +111,7 @@ XP_DEV void widen(const u32x4_t& u, float (&v)[CHUNK<T>]) {
 // end, which loads zeros.
 template <typename T, int DP, int N, int THREADS = 256>
 struct Stager {
-  static constexpr int CPR = DP / CHUNK<T>, STEP = THREADS / CPR, PER = N / STEP;
+  static constexpr int CPR = PITCH<DP> / CHUNK<T>, STEP = THREADS / CPR, PER = N / STEP;
   static_assert(N % STEP == 0 && PER >= 1, "whole passes");
   u32x4_t r[PER];
   int off;  // of the lane's chunk in the first rows, in bytes; negative behind dim
@@ -359,20 +360,27 @@ struct Walk {
   }
 };
 
-// {smallest, largest document, whether the tile holds several or padding, whether padding} of each tile
-__global__ __launch_bounds__(64) void k_attn_docs(const int32_t* __restrict__ doc, const int32_t* __restrict__ len, int n, int tile,
-                                                   int4* __restrict__ tab) {
-  const int b = blockIdx.y, limit = len ? min(max(len[b], 0), n) : n;
-  const int at = blockIdx.x * tile + threadIdx.x;
+// {smallest, largest document, whether the tile holds several or padding, whether padding} of each
+// tile of keys and of queries
+struct DocArgs {
+  const int32_t* doc[2];
+  const int32_t* len[2];
+  int n[2], tile[2], tiles[2];
+  int4* tab[2];
+};
+__global__ __launch_bounds__(64) void k_attn_docs(DocArgs a) {
+  const int w = (int)blockIdx.x >= a.tiles[0], t = blockIdx.x - (w ? a.tiles[0] : 0), b = blockIdx.y, n = a.n[w], tile = a.tile[w];
+  const int limit = a.len[w] ? min(max(a.len[w][b], 0), n) : n;
+  const int at = t * tile + threadIdx.x;
   const bool in = (int)threadIdx.x < tile && at < limit;
-  const int d = in ? doc[(int64_t)b * n + at] : -1;
+  const int d = in ? a.doc[w][(int64_t)b * n + at] : -1;
   int lo = d >= 0 ? d : INT_MAX, hi = d;
   for (int o = 32; o > 0; o >>= 1) {
     lo = min(lo, __shfl_xor(lo, o, 64));
     hi = max(hi, __shfl_xor(hi, o, 64));
   }
   const bool pad = __any((int)threadIdx.x < tile && d < 0);
-  if (threadIdx.x == 0) tab[(int64_t)b * gridDim.x + blockIdx.x] = make_int4(lo, hi < 0 ? -1 : hi, lo != hi || pad, pad);
+  if (threadIdx.x == 0) a.tab[w][(int64_t)b * a.tiles[w] + t] = make_int4(lo, hi < 0 ? -1 : hi, lo != hi || pad, pad);
 }
 
 // smallest and largest document over a workgroup's rows, and over the wave's; negative ones do not count
@@ -745,7 +753,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_few(AttnArgs a) {
 constexpr int MOST_SPLITS = 64;
 template <typename T, int DP>
 __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
-  __shared__ float sh[4][DP];
+  __shared__ float sh[4][128];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t rows = (int64_t)a.batch * a.heads * a.nq, r = blockIdx.x;
   const int i = (int)(r % a.nq), head = (int)(r / a.nq % a.heads), b = (int)(r / a.nq / a.heads);
@@ -756,20 +764,21 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
   const float w = lp == 0.f ? 0.f : exp2_(mp - m);
   float l = lp * w;
   for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
-  float o[DP / 64];
+  constexpr int N = (DP + 63) / 64;
+  float o[N];
 #pragma unroll
-  for (int d = 0; d < DP / 64; ++d) o[d] = 0.f;
+  for (int d = 0; d < N; ++d) o[d] = 0.f;
 #pragma unroll 8
   for (int p = wave; p < a.splits; p += 4) {  // (a part whose sum is zero was not written; of one that is NaN, l is)
     const float wp = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), p));
 #pragma unroll
-    for (int d = 0; d < DP / 64; ++d) {
-      const float v = a.part_o[(p * rows + r) * DP + d * 64 + lane];
+    for (int d = 0; d < N; ++d) {
+      const float v = d * 64 + lane < DP ? a.part_o[(p * rows + r) * DP + d * 64 + lane] : 0.f;
       o[d] += wp > 0.f ? wp * v : 0.f;
     }
   }
 #pragma unroll
-  for (int d = 0; d < DP / 64; ++d) sh[wave][d * 64 + lane] = o[d];
+  for (int d = 0; d < N; ++d) sh[wave][d * 64 + lane] = o[d];
   __syncthreads();
   if (a.stats && threadIdx.x == 0) {
     a.stats[2 * r] = m;
@@ -1229,12 +1238,13 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dkv(AttnArgs a) {
   if constexpr (WHAT & 2) st_column<T, DP>((T*)a.dk.p + b * a.dk.b + (int64_t)j * a.dk.t + kvh * a.dk.h, a.dim, dk, a.scale);
 }
 
-// The parts' sums of dk and dv added, in their order.
+// The parts' sums of dk and dv added, in their order: four columns a thread.
 template <typename T, int DP>
 __global__ __launch_bounds__(256) void k_attn_dkv_join(AttnArgs a) {
-  const int64_t rows = (int64_t)a.batch * a.nk * a.kv_heads, r = (int64_t)blockIdx.x * (256 / (DP / 2)) + threadIdx.x / (DP / 2);
+  constexpr int PER = 2 * DP / 4;  // threads a row: dk's and dv's columns side by side
+  const int64_t rows = (int64_t)a.batch * a.nk * a.kv_heads, x = (int64_t)blockIdx.x * 256 + threadIdx.x, r = x / PER;
   if (r >= rows) return;
-  const int at = threadIdx.x % (DP / 2) * 4, d = at % DP;  // dk's and dv's columns side by side
+  const int at = (int)(x % PER) * 4, d = at % DP;
   const int parts = a.head_parts * a.q_parts;
   float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
@@ -1254,7 +1264,7 @@ __global__ __launch_bounds__(256) void k_attn_dkv_join(AttnArgs a) {
 // ---------------------------------------------------------------- launches
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
-int padded_dim(int dim) { return dim <= 64 ? 64 : 128; }
+int padded_dim(int dim) { return dim <= 64 ? 64 : dim <= 96 ? 96 : 128; }
 int keys_of(int dtype) { return dtype == DT_BF16 ? BN<bf16_t> : BN<float>; }
 int q_step_of(int dtype, const AttnArgs& a) { return dtype == DT_BF16 && a.dim <= 64 ? QT_<bf16_t, 64> : 32; }
 int dq_keys_of(int dtype, const AttnArgs& a) { return dtype == DT_BF16 && a.dim <= 64 ? BN_DQ<bf16_t, 64> : 32; }
@@ -1352,10 +1362,23 @@ size_t lay_bwd(int dtype, AttnArgs& a, char* base, AttnMat* from) {
   return n;
 }
 
-// documents of the tiles of keys, and of queries
-void launch_docs(const int32_t* doc, const int32_t* len, int n, int batch, int tile, int4* tab, hipStream_t s) {
-  if (n == 0) return;
-  XP_LAUNCH("k_attn_docs", 4.0 * batch * n, k_attn_docs, dim3((unsigned)ceil_div(n, tile), batch), dim3(64), 0, s, doc, len, n, tile, tab);
+// documents of the tiles of keys, and (q_step > 0) of queries
+void launch_docs(const AttnArgs& a, int k_step, int q_step, hipStream_t s) {
+  DocArgs d{};
+  d.doc[0] = a.k_doc;
+  d.len[0] = a.k_len;
+  d.n[0] = a.nk;
+  d.tile[0] = k_step;
+  d.tiles[0] = (int)ceil_div(a.nk, k_step);
+  d.tab[0] = a.k_tab;
+  d.doc[1] = a.q_doc;
+  d.len[1] = a.q_len;
+  d.n[1] = a.nq;
+  d.tile[1] = q_step;
+  d.tiles[1] = q_step > 0 ? (int)ceil_div(a.nq, q_step) : 0;
+  d.tab[1] = a.q_tab;
+  if (d.tiles[0] + d.tiles[1] == 0) return;
+  XP_LAUNCH("k_attn_docs", 4.0 * a.batch * (a.nk + (q_step > 0 ? a.nq : 0)), k_attn_docs, dim3(d.tiles[0] + d.tiles[1], a.batch), dim3(64), 0, s, d);
 }
 
 void launch_pack(int dtype, const AttnArgs& a, const AttnMat* from, const AttnMat* const* to, int n, hipStream_t s) {
@@ -1404,7 +1427,7 @@ void bwd(const AttnArgs& a, hipStream_t s) {
   if (groups > 0)
     XP_LAUNCH(sizeof(T) == 2 ? "k_attn_dq<bf16>" : "k_attn_dq<f32>", 6 * pairs * a.dim, (k_attn_dq<T, DP, MODE>), dim3((unsigned)groups), dim3(256), 0, s, a);
   if (kgroups == 0) return;
-  if constexpr (sizeof(T) == 4 && DP == 128) {
+  if constexpr (sizeof(T) == 4 && DP > 64) {
     XP_LAUNCH("k_attn_dv<f32>", 4 * pairs * a.dim, (k_attn_dkv<T, DP, MODE, 1>), dim3((unsigned)kgroups), dim3(256), 0, s, a);
     XP_LAUNCH("k_attn_dk<f32>", 6 * pairs * a.dim, (k_attn_dkv<T, DP, MODE, 2>), dim3((unsigned)kgroups), dim3(256), 0, s, a);
   } else {
@@ -1413,7 +1436,7 @@ void bwd(const AttnArgs& a, hipStream_t s) {
   }
   if (parts > 1) {
     const int64_t rows = (int64_t)a.batch * a.nk * a.kv_heads;
-    XP_LAUNCH("k_attn_dkv_join", 8.0 * rows * parts * DP, (k_attn_dkv_join<T, DP>), dim3((unsigned)ceil_div(rows, 512 / DP)), dim3(256), 0, s, a);
+    XP_LAUNCH("k_attn_dkv_join", 8.0 * rows * parts * DP, (k_attn_dkv_join<T, DP>), dim3((unsigned)ceil_div(rows * (2 * DP / 4), 256)), dim3(256), 0, s, a);
   }
   if (a.grad_bias && groups > 0)
     XP_LAUNCH("k_attn_dbias", 4.0 * (2 * a.range + 1) * a.heads, k_attn_dbias, dim3((unsigned)ceil_div(2 * (int64_t)a.range + 1, 64), a.heads), dim3(1024), 0, s, a);
@@ -1431,6 +1454,7 @@ void by_kind(int dtype, const AttnArgs& a, F&& f) {
   };
   auto dims = [&](auto t) {
     if (a.dim <= 64) with(t, integral_constant<int, 64>{});
+    else if (a.dim <= 96) with(t, integral_constant<int, 96>{});
     else with(t, integral_constant<int, 128>{});
   };
   if (dtype == DT_BF16) dims(bf16_t{});
@@ -1455,7 +1479,7 @@ hipError_t launch_attn_fwd(int dtype, AttnArgs a, void* workspace, hipStream_t s
   lay_fwd(dtype, a, (char*)workspace, from);
   const AttnMat* const to[3] = {&a.q, &a.k, &a.v};
   launch_pack(dtype, a, from, to, 3, s);
-  if (a.k_tab) launch_docs(a.k_doc, a.k_len, a.nk, a.batch, keys_of(dtype), a.k_tab, s);
+  if (a.k_tab) launch_docs(a, keys_of(dtype), 0, s);
   by_kind(dtype, a, [&](auto t, auto d, auto g) { fwd<decltype(t), decltype(d)::value, decltype(g)::value>(a, s); });
   return hipGetLastError();
 }
@@ -1466,10 +1490,7 @@ hipError_t launch_attn_bwd(int dtype, AttnArgs a, void* workspace, hipStream_t s
   lay_bwd(dtype, a, (char*)workspace, from);
   const AttnMat* const to[4] = {&a.q, &a.k, &a.v, &a.dout};
   launch_pack(dtype, a, from, to, 4, s);
-  if (a.k_doc) {
-    launch_docs(a.k_doc, a.k_len, a.nk, a.batch, dq_keys_of(dtype, a), a.k_tab, s);
-    launch_docs(a.q_doc, a.q_len, a.nq, a.batch, q_step_of(dtype, a), a.q_tab, s);
-  }
+  if (a.k_doc) launch_docs(a, dq_keys_of(dtype, a), q_step_of(dtype, a), s);
   by_kind(dtype, a, [&](auto t, auto d, auto g) { bwd<decltype(t), decltype(d)::value, decltype(g)::value>(a, s); });
   return hipGetLastError();
 }

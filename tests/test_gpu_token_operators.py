@@ -377,6 +377,7 @@ class Case:
 SHAPES = [  # batch, nq, nk, heads, kv_heads, dim
     (1, 1, 1, 1, 1, 1), (2, 1, 5, 2, 1, 64), (1, 3, 33, 4, 4, 8), (2, 31, 64, 2, 2, 33), (1, 65, 65, 6, 2, 128), (3, 77, 77, 4, 1, 40),
     (1, 128, 130, 2, 2, 64), (2, 200, 333, 3, 3, 72), (1, 300, 301, 4, 2, 128), (1, 513, 200, 1, 1, 96), (2, 130, 40, 2, 2, 16),
+    (1, 150, 150, 2, 1, 97), (1, 70, 190, 2, 2, 65),
 ]
 
 
