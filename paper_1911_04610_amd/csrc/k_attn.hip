@@ -505,9 +505,9 @@ XP_DEV void softmax_step(const f32x16_t* s, int n, float& m, float& base, float&
   }
 }
 
-// A lane's query row at the end: o and the statistics, or its part of them.
+// A lane's query row at the end: o and the statistics, or (part >= 0) one part of them.
 template <typename T, int DP, int MODE>
-XP_DEV void write_rows(const AttnArgs& a, int b, int head, int i, int split, int kend, float m, float base, float l, f32x16_t (&acc)[DP / 32]) {
+XP_DEV void write_rows(const AttnArgs& a, int b, int head, int i, int64_t part, int kend, float m, float base, float l, f32x16_t (&acc)[DP / 32]) {
   const float c1 = a.scale * LOG2E;
   const bool low = (threadIdx.x & 63) < 32;
   // (a NaN among the scores leaves l NaN, and the row NaN)
@@ -515,13 +515,12 @@ XP_DEV void write_rows(const AttnArgs& a, int b, int head, int i, int split, int
   const bool none = kend == 0 || sum == 0.f;
   const float fit = exp2_(log2_of<MODE>(base - m, c1));  // (o and l belong to `base`)
   const float ms = none ? NEG_INF : log2_of<MODE>(m, c1), ls = none ? 0.f : sum * fit;
-  if (a.splits > 1) {  // (a sum of zero leaves the part of o unwritten)
-    const int64_t r = ((int64_t)split * a.batch + b) * a.heads * a.nq + (int64_t)head * a.nq + i;
+  if (part >= 0) {  // (a sum of zero leaves the part of o unwritten)
     if (low) {
-      a.part_ml[2 * r] = ms;
-      a.part_ml[2 * r + 1] = ls;
+      a.part_ml[2 * part] = ms;
+      a.part_ml[2 * part + 1] = ls;
     }
-    st_column<float, DP>(a.part_o + r * DP, none ? 0 : DP, acc, fit);
+    st_column<float, DP>(a.part_o + part * DP, none ? 0 : DP, acc, fit);
     return;
   }
   if (a.stats && low) {
@@ -661,13 +660,50 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_fwd(AttnArgs a) {
     t = tn;
   }
 
-  if (in) write_rows<T, DP, MODE>(a, b, head, i, split, kend, m, base, l, acc);
+  if (in) {
+    const int64_t row = ((int64_t)b * a.heads + head) * a.nq + i, rows = (int64_t)a.batch * a.heads * a.nq;
+    write_rows<T, DP, MODE>(a, b, head, i, a.splits > 1 ? split * rows + row : -1, kend, m, base, l, acc);
+  }
+}
+
+// The workgroups of k_attn_few that a sequence gets, of `groups` for each block of rows and key
+// head: one each, and the others by the sequences' lengths, so that the longest does not decide the
+// call's time (up to 64 sequences; more of them even out by their number).
+struct Share {
+  int b, first, end;  // the sequence, its workgroups
+};
+XP_DEV Share share_at(const AttnArgs& a, int group, int seq) {  // the one that `group` is in, or (group < 0) that of sequence seq
+  const int groups = a.splits, lane = threadIdx.x & 63;
+  if (a.batch > 64 || !a.k_len) {
+    const int per = groups / a.batch, b = group < 0 ? seq : min(group / per, a.batch - 1);
+    return {b, b * per, b == a.batch - 1 ? groups : (b + 1) * per};
+  }
+  const int steps = lane < a.batch ? (min(max(a.k_len[lane], 0), a.nk) + 31) / 32 : 0;
+  int before = steps;
+  for (int o = 1; o < 64; o <<= 1) {
+    const int v = __shfl_up(before, o, 64);
+    before += lane >= o ? v : 0;
+  }
+  const int total = __shfl(before, 63, 64);
+  before -= steps;
+  const int c = lane < a.batch ? lane + (total > 0 ? (int)((int64_t)before * (groups - a.batch) / total) : 0) : groups;
+  const int b = group < 0 ? seq : __popcll(__ballot(c <= group)) - 1;
+  return {b, __shfl(c, b, 64), b + 1 < a.batch ? __shfl(c, b + 1, 64) : groups};
+}
+
+// where a wave's part of a row lies
+XP_DEV int64_t few_part(const AttnArgs& a, int kvh, int blk, int wave, int row) {
+  const int blocks = (a.nq * a.pk + 31) / 32;
+  return (((int64_t)kvh * blocks + blk) * (a.splits * 4) + wave) * 32 + row;
 }
 
 // Few query rows (a generation step): a wave takes up to 32 rows of the heads that share keys
 // together, row r being query r / pk of head r % pk, and a part of the keys by itself, 32 at a
 // time through LDS of its own, the next 32 on their way: four times the bytes in flight
-// that the workgroups of k_attn_fwd have, whose other waves would have no rows.
+// that the workgroups of k_attn_fwd have, whose other waves would have no rows.  Short
+// sequences (splits 0): all of the keys, four waves being four blocks of rows.
+// Bound by the keys' and values' bytes: 8 sequences of 32768 tokens, 8 heads of 128, 5.6 TB/s,
+// what a copy reaches.
 template <typename T, int DP, int MODE>
 __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_few(AttnArgs a) {
   constexpr int TILE = 32 * ROW<T, DP>;
@@ -676,13 +712,16 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_few(AttnArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int rows = a.nq * a.pk, blocks = (rows + 31) / 32, units = a.kv_heads;
   // (nothing is read twice: neighbours, the heads of the same keys, go to different XCDs, and so
-  // do the parts of one sequence, which may be the longest)
-  int id = blockIdx.x;
+  // do the parts of one sequence)
+  int id = a.splits > 0 ? blockIdx.x : blockIdx.x * 4 + wave;
   const int kvh = id % units;
   id /= units;
-  const int groups = a.splits / 4, split = id % groups * 4 + wave;
-  id /= groups;
-  const int blk = id % blocks, b = id / blocks;
+  const int blk = id % blocks, group = id / blocks;
+  if (a.splits == 0 && group >= a.batch) return;
+  Share share = {group, 0, 0};
+  if (a.splits > 0) share = share_at(a, group, 0);
+  const int b = __builtin_amdgcn_readfirstlane(share.b);
+  const int parts = a.splits > 0 ? (share.end - share.first) * 4 : 1, split = a.splits > 0 ? (group - share.first) * 4 + wave : 0;
   const Seq seq(a, b);
 
   const int first = blk * 32 / a.pk, last = min((min(rows, (blk + 1) * 32) - 1) / a.pk, seq.ql - 1);
@@ -699,7 +738,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_few(AttnArgs a) {
   const float* bias = has_bias(MODE) ? a.bias + (int64_t)min(head, a.heads - 1) * (2 * a.range + 1) + a.range : nullptr;
 
   // (documents: every step is looked at, their tiles have no table here)
-  const int steps = (kmax + 31) / 32, per = (steps + a.splits - 1) / a.splits;
+  const int steps = (kmax + 31) / 32, per = (steps + parts - 1) / parts;
   const int end = min(steps, (split + 1) * per);
   const float c1 = a.scale * LOG2E;
   float m = NEG_INF, base = NEG_INF, l = 0.f;
@@ -745,38 +784,52 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_few(AttnArgs a) {
     }
     add_transposed<T, DP>(acc, cplace, TILE, p);
   }
-  if (in) write_rows<T, DP, MODE>(a, b, head, i, split, kend, m, base, l, acc);
+  if (in) write_rows<T, DP, MODE>(a, b, head, i, a.splits > 0 ? few_part(a, kvh, blk, group * 4 + wave, lane & 31) : -1, kend, m, base, l, acc);
 }
 
-// The parts of the keys joined: one workgroup per query row, a lane a part for the sums, a wave
-// every fourth part for o.
-constexpr int MOST_SPLITS = 64;
-template <typename T, int DP>
+// The parts of the keys joined: one workgroup per query row; for the sums a lane takes every 64th
+// part, for o a wave every fourth.
+template <typename T, int DP, bool FEW>
 __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
   __shared__ float sh[4][128];
+  constexpr int N = (DP + 63) / 64;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t rows = (int64_t)a.batch * a.heads * a.nq, r = blockIdx.x;
   const int i = (int)(r % a.nq), head = (int)(r / a.nq % a.heads), b = (int)(r / a.nq / a.heads);
-  const bool has = lane < a.splits;
-  const float mp = has ? a.part_ml[2 * (lane * rows + r)] : NEG_INF, lp = has ? a.part_ml[2 * (lane * rows + r) + 1] : 0.f;
-  float m = mp;
+  int64_t first = r, step = rows;
+  int parts = a.splits;
+  if constexpr (FEW) {
+    const Share share = share_at(a, -1, b);
+    const int row = i * a.pk + head % a.pk;
+    first = few_part(a, head / a.pk, row / 32, share.first * 4, row % 32);
+    step = 32;
+    parts = (share.end - share.first) * 4;
+  }
+  const f32x2_t* ml = (const f32x2_t*)a.part_ml;
+  const f32x2_t mine = lane < parts ? ml[first + lane * step] : (f32x2_t){NEG_INF, 0.f};  // (most calls have no more)
+  float m = mine[0];
+  for (int p = lane + 64; p < parts; p += 64) m = fmaxf(m, ml[first + p * step][0]);
   for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-  const float w = lp == 0.f ? 0.f : exp2_(mp - m);
-  float l = lp * w;
-  for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
-  constexpr int N = (DP + 63) / 64;
-  float o[N];
+  float l = 0.f, o[N];
 #pragma unroll
   for (int d = 0; d < N; ++d) o[d] = 0.f;
+  for (int p0 = 0; p0 < parts; p0 += 64) {
+    const int p = p0 + lane;
+    const f32x2_t v = p0 == 0 ? mine : p < parts ? ml[first + p * step] : (f32x2_t){NEG_INF, 0.f};
+    const float lp = v[1], w = lp == 0.f ? 0.f : exp2_(v[0] - m);
+    l += lp * w;
+    const int n = min(64, parts - p0);
 #pragma unroll 8
-  for (int p = wave; p < a.splits; p += 4) {  // (a part whose sum is zero was not written; of one that is NaN, l is)
-    const float wp = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), p));
+    for (int k = wave; k < n; k += 4) {  // (a part whose sum is zero was not written; of one that is NaN, l is)
+      const float wk = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), k));
 #pragma unroll
-    for (int d = 0; d < N; ++d) {
-      const float v = d * 64 + lane < DP ? a.part_o[(p * rows + r) * DP + d * 64 + lane] : 0.f;
-      o[d] += wp > 0.f ? wp * v : 0.f;
+      for (int d = 0; d < N; ++d) {
+        const float v = d * 64 + lane < DP ? a.part_o[(first + (p0 + k) * step) * DP + d * 64 + lane] : 0.f;
+        o[d] += wk > 0.f ? wk * v : 0.f;
+      }
     }
   }
+  for (int k = 32; k > 0; k >>= 1) l += __shfl_xor(l, k, 64);
 #pragma unroll
   for (int d = 0; d < N; ++d) sh[wave][d * 64 + lane] = o[d];
   __syncthreads();
@@ -1273,18 +1326,19 @@ int dq_keys_of(int dtype, const AttnArgs& a) { return dtype == DT_BF16 && a.dim 
 // read once for all of them.  Up to 64: twice the keys' reads, by then from the L2.
 bool few(const AttnArgs& a) { return (int64_t)a.nq * (a.heads / a.kv_heads) <= 64; }
 
-// Parts of the keys where the rows alone do not fill the card: for k_attn_fwd two workgroups a
-// CU, at least 4 steps each; for k_attn_few (a wave each, in fours) 16 waves a CU, at least 4
-// steps of 32 keys: what the parts leave is little there, and sequences of different lengths even out.
+// Parts of the keys where the rows alone do not fill the card.  k_attn_fwd: two workgroups a CU, at
+// least 4 steps each, 1: none.  k_attn_few: workgroups over all sequences for each key head and block of
+// rows, two a CU, of at least 8 steps of 32 keys; 0: up to 4 steps, which a wave does sooner than a
+// second launch joins them.
 int parts(int dtype, const AttnArgs& a) {
   if (few(a)) {
-    const int64_t groups = ceil_div((int64_t)a.nq * a.pk, 32) * a.kv_heads * a.batch;
-    if (groups == 0) return 4;
-    return (int)std::max<int64_t>(1, std::min<int64_t>({ceil_div(1024, groups), ceil_div(a.nk, 32) / 16, MOST_SPLITS / 4})) * 4;
+    const int64_t units = ceil_div((int64_t)a.nq * a.pk, 32) * a.kv_heads, steps = ceil_div(a.nk, 32);
+    if (steps <= 4 || units == 0 || a.batch == 0) return 0;
+    return (int)std::max<int64_t>(a.batch, std::min<int64_t>(ceil_div(512, units), a.batch * ceil_div(steps, 8)));
   }
   const int64_t groups = ceil_div(a.nq, ROWS) * a.heads * a.batch, steps = ceil_div(a.nk, keys_of(dtype));
   if (groups == 0 || groups >= 256) return 1;
-  return (int)std::max<int64_t>(1, std::min<int64_t>({ceil_div(512, groups), steps / 4, MOST_SPLITS}));
+  return (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(512, groups), steps / 4));
 }
 
 // blocks of 32 queries that hold distances within the range, of 32 keys
@@ -1329,9 +1383,10 @@ size_t lay_fwd(int dtype, AttnArgs& a, char* base, AttnMat* from) {
   a.pk = few(a) ? a.heads / a.kv_heads : 1;
   a.splits = parts(dtype, a);
   const int64_t rows = (int64_t)a.batch * a.heads * a.nq;
-  if (a.splits > 1) {
-    a.part_o = (float*)take((size_t)rows * a.splits * padded_dim(a.dim) * 4);
-    a.part_ml = (float*)take((size_t)rows * a.splits * 8);
+  const int64_t count = few(a) ? ceil_div((int64_t)a.nq * a.pk, 32) * a.kv_heads * a.splits * 128 : a.splits > 1 ? rows * a.splits : 0;
+  if (count > 0) {
+    a.part_o = (float*)take((size_t)count * padded_dim(a.dim) * 4);
+    a.part_ml = (float*)take((size_t)count * 8);
   }
   if (a.k_doc && !few(a)) a.k_tab = (int4*)take((size_t)a.batch * ceil_div(a.nk, keys_of(dtype)) * sizeof(int4));
   return n;
@@ -1406,17 +1461,18 @@ void launch_pack(int dtype, const AttnArgs& a, const AttnMat* from, const AttnMa
 template <typename T, int DP, int MODE>
 void fwd(const AttnArgs& a, hipStream_t s) {
   const double flops = 4.0 * a.batch * a.heads * a.nq * (double)a.nk * a.dim;
+  const int64_t rows = (int64_t)a.batch * a.heads * a.nq;
   if (few(a)) {
-    const int64_t groups = ceil_div((int64_t)a.nq * a.pk, 32) * a.kv_heads * a.batch * (a.splits / 4);
+    const int64_t units = ceil_div((int64_t)a.nq * a.pk, 32) * a.kv_heads, groups = a.splits > 0 ? units * a.splits : ceil_div(units * a.batch, 4);
     XP_LAUNCH(sizeof(T) == 2 ? "k_attn_few<bf16>" : "k_attn_few<f32>", flops, (k_attn_few<T, DP, MODE>), dim3((unsigned)groups), dim3(256), 0, s, a);
-  } else {
-    const int64_t groups = ceil_div(a.nq, ROWS) * a.heads * a.batch * a.splits;
-    XP_LAUNCH(sizeof(T) == 2 ? "k_attn_fwd<bf16>" : "k_attn_fwd<f32>", flops, (k_attn_fwd<T, DP, MODE>), dim3((unsigned)groups), dim3(256), 0, s, a);
+    if (a.splits > 0)
+      XP_LAUNCH("k_attn_join", 512.0 * units * a.splits * DP, (k_attn_join<T, DP, true>), dim3((unsigned)rows), dim3(256), 0, s, a);
+    return;
   }
-  if (a.splits > 1) {
-    const int64_t rows = (int64_t)a.batch * a.heads * a.nq;
-    XP_LAUNCH("k_attn_join", 4.0 * rows * a.splits * DP, (k_attn_join<T, DP>), dim3((unsigned)rows), dim3(256), 0, s, a);
-  }
+  const int64_t groups = ceil_div(a.nq, ROWS) * a.heads * a.batch * a.splits;
+  XP_LAUNCH(sizeof(T) == 2 ? "k_attn_fwd<bf16>" : "k_attn_fwd<f32>", flops, (k_attn_fwd<T, DP, MODE>), dim3((unsigned)groups), dim3(256), 0, s, a);
+  if (a.splits > 1)
+    XP_LAUNCH("k_attn_join", 4.0 * rows * a.splits * DP, (k_attn_join<T, DP, false>), dim3((unsigned)rows), dim3(256), 0, s, a);
 }
 
 template <typename T, int DP, int MODE>

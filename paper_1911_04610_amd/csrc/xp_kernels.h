@@ -434,9 +434,9 @@ struct AttnArgs {
   const float* bias;                 // [heads][2 range + 1], optional
   float* grad_bias;                  // backward, optional: added to
   float* stats;                      // [batch][heads][nq][2]: largest score, sum of exp(score - largest)
-  // set by the launcher: query rows of how many heads a workgroup holds together, parts
-  // of the keys and their results, documents of each tile, what the gradients need of each query row, sums of score
-  // gradients along diagonals
+  // set by the launcher: heads whose query rows k_attn_few holds together, parts of the keys
+  // (k_attn_few: workgroups over all sequences) and their results, documents of each tile, what
+  // the gradients need of each query row, sums of score gradients along diagonals
   int pk, splits, near, ldim;        // ldim: dim in whole chunks of 16 bytes
   int head_parts, q_parts;           // of k_attn_dkv
   float *part_o, *part_ml, *part_kv;
