@@ -224,14 +224,17 @@ XP_DEV uint32_t column_place() {
 
 // 32 rows of a tile, `more` bytes from it on, times the lanes' columns; at: row_place + tile
 template <typename T, int DP>
-XP_DEV f32x16_t rows_times(uint32_t at, int more, const u32x4_t (&col)[DP / CHUNK<T> / 2]) {
+XP_DEV f32x16_t rows_times(uint32_t at, int more, const u32x4_t (&col)[DP / CHUNK<T> / 2], int dim) {
   f32x16_t c;
 #pragma unroll
   for (int i = 0; i < 16; ++i) c[i] = 0.f;
 #pragma unroll
   for (int s = 0; s < DP / CHUNK<T> / 2; ++s) {
-    const u32x4_t row = *lds<u32x4_t>((at ^ (s * 32)) + more);
-    c = mma<T>(row, col[s], c);
+    // (fp32 products take 16 times as long as bf16 ones: those of zeros behind dim are left out)
+    if (sizeof(T) == 2 || s * 2 * CHUNK<T> < dim) {
+      const u32x4_t row = *lds<u32x4_t>((at ^ (s * 32)) + more);
+      c = mma<T>(row, col[s], c);
+    }
   }
   return c;
 }
@@ -252,7 +255,7 @@ XP_DEV f32x16_t rows_times(uint32_t at, int more, uint32_t col) {
 
 // acc[d][lane's column] += sum over 32 rows of tile[row][d] w[row]; at: column_place + tile
 template <typename T, int DP>
-XP_DEV void add_transposed(f32x16_t (&acc)[DP / 32], uint32_t at, int more, const float (&w)[16]) {
+XP_DEV void add_transposed(f32x16_t (&acc)[DP / 32], uint32_t at, int more, const float (&w)[16], int dim) {
   if constexpr (sizeof(T) == 2) {
     typedef short v4i16 __attribute__((ext_vector_type(4)));
 #pragma unroll
@@ -266,17 +269,20 @@ XP_DEV void add_transposed(f32x16_t (&acc)[DP / 32], uint32_t at, int more, cons
 #pragma unroll
         for (int k = 0; k < 2; ++k)
           part[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds<v4i16>((at ^ (d * 64 + k * 32)) + (more + (16 * b + 8 * k) * ROW<T, DP>)));
-        acc[d] = mma<T>(__builtin_bit_cast(u32x4_t, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7)), f, acc[d]);
+        const u32x4_t x = __builtin_bit_cast(u32x4_t, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+        acc[d] = mma<T>(x, f, acc[d]);
       }
     }
   } else {
 #pragma unroll
-    for (int r = 0; r < 16; ++r)
+    for (int d = 0; d < DP / 32; ++d) {
+      if (d * 32 < dim)
 #pragma unroll
-      for (int d = 0; d < DP / 32; ++d) {
+      for (int r = 0; r < 16; ++r) {
         const float x = *lds<float>((at ^ (d * 128 + ((r >> 2) & 1) * 64 + (r & 3) * 16)) + (more + (8 * (r >> 2) + (r & 3)) * ROW<T, DP>));
         acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, w[r], acc[d], 0, 0, 0);
       }
+    }
   }
 }
 
@@ -440,19 +446,28 @@ XP_DEV float exp_of(float s, float base, float c1) {
 template <int MODE>
 XP_DEV float log2_of(float d, float c1) { return MODE == PLAIN ? d * c1 : d; }
 
-// Scores of a block of 32 x 32 from its products, in their place.  tanh(u) = 1 - 2 r with r = 1 / (1 + exp(2 u)),
-// off by at most 2^-23 of 1 (three roundings of values up to 1, the hardware's exponential and
-// reciprocal), its slope 4 r (1 - r); slope: of the cap.  at(r): the bias of register r.
-template <int MODE, bool SLOPE, typename F>
+// Scores of a block of 32 x 32 from its products, in their place; slope: of the cap.  at(r): the bias of
+// register r.  For u = scale x / cap, e = exp(-2 |u|): tanh(u) = (1 - e) / (1 + e) with u's sign, good to a
+// few steps of itself but for 1 - e, which is good to half a step of 1; its slope 4 e / (1 + e)^2.
+// Without a bias and in bf16 storage, where nothing but rounded results comes of it, 1 - 2 r and
+// 4 r (1 - r) with r = 1 / (1 + exp(2 u)), off by 2^-23 of 1: three operations less of each score (8192
+// tokens, 16 heads of 128, causal 397 us against 457).
+template <typename T, int MODE, bool SLOPE, typename F>
 XP_DEV void scores(f32x16_t& s, const AttnArgs& a, float (&slope)[16], F&& at) {
   if constexpr (has_cap(MODE)) {
     const float k = 2.f * LOG2E * a.scale / a.cap, top = a.cap * LOG2E;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const float q = __builtin_amdgcn_rcpf(1.f + exp2_(s[r] * k));
-      s[r] = top - 2.f * top * q;
-      if constexpr (SLOPE) slope[r] = 4.f * q - 4.f * q * q;
-      if constexpr (has_bias(MODE)) s[r] += at(r);
+      if constexpr (sizeof(T) == 2 && MODE == CAP) {
+        const float q = __builtin_amdgcn_rcpf(1.f + exp2_(s[r] * k));
+        s[r] = top - 2.f * top * q;
+        if constexpr (SLOPE) slope[r] = 4.f * q - 4.f * q * q;
+      } else {
+        const float u = s[r] * k, e = exp2_(-fabsf(u)), q = __builtin_amdgcn_rcpf(1.f + e);
+        s[r] = copysignf(top * ((1.f - e) * q), u);
+        if constexpr (SLOPE) slope[r] = 4.f * e * q * q;
+        if constexpr (has_bias(MODE)) s[r] += at(r);
+      }
     }
   } else if constexpr (has_bias(MODE)) {
     const float c1 = a.scale * LOG2E;
@@ -627,14 +642,14 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_fwd(AttnArgs a) {
       // (the other wave of the SIMD has its exponentials then)
       __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-      for (int n = 0; n < NB; ++n) s[n] = rows_times<T, DP>(rat, n * 32 * ROW<T, DP>, q);
+      for (int n = 0; n < NB; ++n) s[n] = rows_times<T, DP>(rat, n * 32 * ROW<T, DP>, q, a.ldim);
       __builtin_amdgcn_s_setprio(0);
       if constexpr (MODE != PLAIN) {
         float none[16];
         const float* mine = sbias[buf] + ROWS - 1 - (i - first) + 4 * (lane >> 5);
 #pragma unroll
         for (int n = 0; n < NB; ++n)
-          scores<MODE, false>(s[n], a, none, [&](int r) { return mine[n * 32 + 8 * (r >> 2) + (r & 3)]; });
+          scores<T, MODE, false>(s[n], a, none, [&](int r) { return mine[n * 32 + 8 * (r >> 2) + (r & 3)]; });
       }
       if ((t + 1) * KEYS > wmin)
 #pragma unroll
@@ -652,7 +667,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_fwd(AttnArgs a) {
           p[r] = exp_of<MODE>(s[n][r], off, c1);
           l += p[r];
         }
-        add_transposed<T, DP>(acc, cat, TILE + n * 32 * ROW<T, DP>, p);
+        add_transposed<T, DP>(acc, cat, TILE + n * 32 * ROW<T, DP>, p, a.ldim);
       }
     }
     buf ^= 1;
@@ -766,11 +781,11 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_few(AttnArgs a) {
     const int next = t + 1;
     if (next < end) load(next);
     const int j0 = t * 32;
-    f32x16_t s = rows_times<T, DP>(rplace, 0, q);
+    f32x16_t s = rows_times<T, DP>(rplace, 0, q, a.ldim);
     if constexpr (MODE != PLAIN) {
       float none[16];
       const int d0 = j0 - i - seq.off;
-      scores<MODE, false>(s, a, none, [&](int r) { return log2_bias(bias[min(max(d0 + row_of(r), -a.range), a.range)]); });
+      scores<T, MODE, false>(s, a, none, [&](int r) { return log2_bias(bias[min(max(d0 + row_of(r), -a.range), a.range)]); });
     }
     if (j0 + 32 > kmin || blk == blocks - 1) hide_from(s, kend - j0, NEG_INF);
     if (kdoc) hide_others(s, sdoc[wave], doc, NEG_INF);
@@ -782,7 +797,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_few(AttnArgs a) {
       p[r] = exp_of<MODE>(s[r], off, c1);
       l += p[r];
     }
-    add_transposed<T, DP>(acc, cplace, TILE, p);
+    add_transposed<T, DP>(acc, cplace, TILE, p, a.ldim);
   }
   if (in) write_rows<T, DP, MODE>(a, b, head, i, a.splits > 0 ? few_part(a, kvh, blk, group * 4 + wave, lane & 31) : -1, kend, m, base, l, acc);
 }
@@ -873,7 +888,9 @@ XP_DEV int first_near(const AttnArgs& a, const Seq& seq, int kw) { return max(0,
 // As the forward, a lane a query: scores and dP from the keys' and values' rows, then
 // dq += dX K.  do . o comes from the stored o here (rounded, as dq itself will be); the same
 // sum as P dP in fp32, which the loop makes by the way, is what k_attn_dkv reads: bias
-// gradients are fp32, and a rounded o would show in their sums.
+// gradients are fp32, and a rounded o would show in their sums.  (dX as two bf16 values, for a dq
+// without its rounding, takes this kernel from 331 to 398 us on 2 sequences of 4096 tokens, 16 heads
+// of 128; dq is 2.4e-3 to 2.7e-3 of its 2-norm off without, of which rounding dq itself is 1.7e-3.)
 template <typename T, int DP, int MODE>
 __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dq(AttnArgs a) {
   constexpr int KEYS = BN_DQ<T, DP>, NB = KEYS / 32;
@@ -979,14 +996,14 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dq(AttnArgs a) {
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
         const int k0 = t * KEYS + n * 32;
-        f32x16_t s = rows_times<T, DP>(rat, n * 32 * ROW<T, DP>, q);
+        f32x16_t s = rows_times<T, DP>(rat, n * 32 * ROW<T, DP>, q, a.ldim);
         phase();
-        const f32x16_t dp = rows_times<T, DP>(rat, TILE + n * 32 * ROW<T, DP>, g);
+        const f32x16_t dp = rows_times<T, DP>(rat, TILE + n * 32 * ROW<T, DP>, g, a.ldim);
         phase();
         float slope[16], ds[16];
         if constexpr (MODE != PLAIN) {
           const float* mine = sbias[buf] + ROWS - 1 - (wave * 32 + (lane & 31)) + 4 * (lane >> 5) + n * 32;
-          scores<MODE, true>(s, a, slope, [&](int r) { return mine[8 * (r >> 2) + (r & 3)]; });
+          scores<T, MODE, true>(s, a, slope, [&](int r) { return mine[8 * (r >> 2) + (r & 3)]; });
         }
 #pragma unroll
         for (int r = 0; r < 16; ++r) ds[r] = weight<MODE>(s[r], st.a, st.b, c1);
@@ -1002,7 +1019,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dq(AttnArgs a) {
           for (int r = 0; r < 16; ++r) ds[r] *= slope[r];
         }
         phase();
-        add_transposed<T, DP>(acc, cat, n * 32 * ROW<T, DP>, ds);
+        add_transposed<T, DP>(acc, cat, n * 32 * ROW<T, DP>, ds, a.ldim);
         phase();
       }
     }
@@ -1040,7 +1057,8 @@ __global__ __launch_bounds__(1024) void k_attn_dbias(AttnArgs a) {
       const int64_t at = at0 + w;
       float v0 = 0.f, v1 = 0.f;
       if (outer) {
-        if (x < width) v0 = a.tail[2 * at + (x == 0 ? 0 : 1)];
+        if (x < width)
+          for (int q = 0; q < a.q_parts; ++q) v0 += a.tail[2 * (at * a.q_parts + q) + (x == 0 ? 0 : 1)];
       } else {
         // of block t the distances from w 32 - 32 t - 31 - off on: places u in the two blocks that hold d
         const int near0 = first_near(a, seq, w * 32), from = d - w * 32 + 31 + seq.off, u = from & 31, t = (u - from) >> 5;
@@ -1116,7 +1134,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dkv(AttnArgs a) {
   else if (seq.causal && seq.prefix <= k0) t0 = min(tiles, max(0, k0 - seq.off) / QT);
   const int h0 = kvh * group + part % a.head_parts * (group / a.head_parts), h1 = h0 + group / a.head_parts;
   const int per = (tiles - t0 + a.q_parts - 1) / a.q_parts;
-  t0 = min(tiles, t0 + part / a.head_parts * per);
+  t0 = t0 + part / a.head_parts * per;
   tiles = min(tiles, t0 + per);
   const int tab_tiles = (a.nq + QT - 1) / QT;
   Walk walk(a.q_tab ? a.q_tab + (int64_t)b * tab_tiles : nullptr, tiles, docs.lo, docs.hi);
@@ -1136,12 +1154,16 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dkv(AttnArgs a) {
   float left = 0.f, right = 0.f;
   const int near0 = first_near(a, seq, kw);
   const int64_t wblock = blk * 4 + wave, wblocks = blocks * 4;
-  if (diag)  // blocks that no step reaches
+  const int q_part = part / a.head_parts;
+  if (diag) {  // zeros for blocks that no step reaches: this part's, and what lies before the first's and behind the last's
+    const int n0 = q_part == 0 ? 0 : max(0, t0 * (QT / 32) - near0);
+    const int n1 = q_part == a.q_parts - 1 ? a.near : min(a.near, (t0 + per) * (QT / 32) - near0);
     for (int h = h0; h < h1; ++h) {
       const int64_t w = ((int64_t)b * a.heads + h) * wblocks + wblock;
-      for (int n = 0; n < a.near; ++n) a.diag[(w * a.near + n) * 64 + lane] = 0.f;
-      if (lane < 2) a.tail[2 * w + lane] = 0.f;
+      for (int n = n0; n < n1; ++n) a.diag[(w * a.near + n) * 64 + lane] = 0.f;
+      if (lane < 2) a.tail[2 * (w * a.q_parts + q_part) + lane] = 0.f;
     }
+  }
 
   Stager<T, DP, QT> qs(a.q.t, a.ldim), gs(a.dout.t, a.ldim);
   const int row_tiles = (a.nq + ROWS - 1) / ROWS * 4;
@@ -1192,12 +1214,12 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dkv(AttnArgs a) {
       const int i0 = t * QT + n * 32, i1 = min(i0 + 32, seq.ql) - 1;
       if (other || i0 >= seq.ql || seq.kend(i1) <= kw) return;
       const uint32_t rat = rplace + buf * 2 * TILE, cat = cplace + buf * 2 * TILE;
-      f32x16_t s = rows_times<T, DP>(rat, n * 32 * ROW<T, DP>, kc);
+      f32x16_t s = rows_times<T, DP>(rat, n * 32 * ROW<T, DP>, kc, a.ldim);
       phase();
       float p[16], slope[16];
       if constexpr (MODE != PLAIN) {  // (register r's place in the window: key - query + QT - 1)
         const float* mine = sbias[buf] + (has_bias(MODE) ? (j - k0) + QT - 28 - 4 * (lane >> 5) - n * 32 : 0);
-        scores<MODE, (WHAT & 2) != 0>(s, a, slope, [&](int r) { return mine[27 - 8 * (r >> 2) - (r & 3)]; });
+        scores<T, MODE, (WHAT & 2) != 0>(s, a, slope, [&](int r) { return mine[27 - 8 * (r >> 2) - (r & 3)]; });
       }
       auto of = [&](int what, int r) __attribute__((always_inline)) { return srow[buf][n * (5 * 32) + what * 32 + row_of(r)]; };
 #pragma unroll
@@ -1210,13 +1232,13 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dkv(AttnArgs a) {
         for (int r = 0; r < 16; ++r) p[r] = __float_as_int(of(4, r)) != doc ? 0.f : p[r];
       if constexpr (WHAT & 1) {
         phase();
-        add_transposed<T, DP>(dv, cat, TILE + n * 32 * ROW<T, DP>, p);
+        add_transposed<T, DP>(dv, cat, TILE + n * 32 * ROW<T, DP>, p, a.ldim);
         phase();
       }
       if constexpr (WHAT & 2) {
         f32x16_t dp;
         if constexpr (V_LDS) dp = rows_times<T, DP>(rat, TILE + n * 32 * ROW<T, DP>, (uint32_t)fresh(vplace));
-        else dp = rows_times<T, DP>(rat, TILE + n * 32 * ROW<T, DP>, vc);
+        else dp = rows_times<T, DP>(rat, TILE + n * 32 * ROW<T, DP>, vc, a.ldim);
         phase();
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
@@ -1258,7 +1280,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dkv(AttnArgs a) {
           for (int r = 0; r < 16; ++r) p[r] *= slope[r];
         }
         phase();
-        add_transposed<T, DP>(dk, cat, n * 32 * ROW<T, DP>, p);
+        add_transposed<T, DP>(dk, cat, n * 32 * ROW<T, DP>, p, a.ldim);
       }
     };
     block(0);
@@ -1269,7 +1291,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dkv(AttnArgs a) {
         right += __shfl_xor(right, o, 64);
       }
       if (lane == 0) {
-        float* w = a.tail + 2 * (((int64_t)b * a.heads + head) * wblocks + wblock);
+        float* w = a.tail + 2 * ((((int64_t)b * a.heads + head) * wblocks + wblock) * a.q_parts + q_part);
         w[0] = left;
         w[1] = right;
       }
@@ -1327,7 +1349,7 @@ int dq_keys_of(int dtype, const AttnArgs& a) { return dtype == DT_BF16 && a.dim 
 bool few(const AttnArgs& a) { return (int64_t)a.nq * (a.heads / a.kv_heads) <= 64; }
 
 // Parts of the keys where the rows alone do not fill the card.  k_attn_fwd: two workgroups a CU, at
-// least 4 steps each, 1: none.  k_attn_few: workgroups over all sequences for each key head and block of
+// least 4 steps each (fp32, whose steps are long: 2), 1: none.  k_attn_few: workgroups over all sequences for each key head and block of
 // rows, two a CU, of at least 8 steps of 32 keys; 0: up to 4 steps, which a wave does sooner than a
 // second launch joins them.
 int parts(int dtype, const AttnArgs& a) {
@@ -1338,15 +1360,16 @@ int parts(int dtype, const AttnArgs& a) {
   }
   const int64_t groups = ceil_div(a.nq, ROWS) * a.heads * a.batch, steps = ceil_div(a.nk, keys_of(dtype));
   if (groups == 0 || groups >= 256) return 1;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(512, groups), steps / 4));
+  return (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(512, groups), steps / (dtype == DT_BF16 ? 4 : 2)));
 }
 
 // blocks of 32 queries that hold distances within the range, of 32 keys
 int near_blocks(const AttnArgs& a) { return (int)std::min<int64_t>(ceil_div(a.nq, 32), ceil_div(2 * (int64_t)a.range + 62, 32) + 1); }
 
 // Parts of k_attn_dkv where its blocks of keys do not fill the card twice over (causal, where they
-// differ in length: four times): heads that share keys first, then runs of at least 8 steps
-// of queries (with grad_bias heads alone: the blocks' diagonals are laid out for one run).
+// differ in length: four times): heads that share keys first, then runs of queries, of at least 8 steps
+// (fp32, whose steps are long: 2).  Not with documents: a block's queries are few then, and
+// parts mostly empty (2 x 4096 tokens, 12 heads of 64, documents of 32 to 2048: 147 us without, 172 with).
 void cut_dkv(int dtype, AttnArgs& a, int64_t kgroups) {
   const int group = a.heads / a.kv_heads, want = a.causal ? 1024 : 512;
   a.head_parts = a.q_parts = 1;
@@ -1354,8 +1377,8 @@ void cut_dkv(int dtype, AttnArgs& a, int64_t kgroups) {
   for (int d = 1; d <= group && kgroups * a.head_parts < want; ++d)
     if (group % d == 0) a.head_parts = d;
   const int64_t groups = kgroups * a.head_parts;
-  if (!a.grad_bias && groups < want)
-    a.q_parts = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(want, groups), ceil_div(a.nq, q_step_of(dtype, a)) / 8));
+  if (groups < want && !a.q_doc)
+    a.q_parts = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(want, groups), ceil_div(a.nq, q_step_of(dtype, a)) / (dtype == DT_BF16 ? 8 : 2)));
 }
 
 // Inputs whose rows are not whole, aligned chunks of 16 bytes are copied to such ones first:
@@ -1412,7 +1435,7 @@ size_t lay_bwd(int dtype, AttnArgs& a, char* base, AttnMat* from) {
     const int64_t waves = (int64_t)a.batch * a.heads * ceil_div(a.nk, ROWS) * 4;
     a.near = near_blocks(a);
     a.diag = (float*)take((size_t)waves * a.near * 64 * 4);
-    a.tail = (float*)take((size_t)waves * 8);
+    a.tail = (float*)take((size_t)waves * a.q_parts * 8);
   }
   return n;
 }
