@@ -604,7 +604,7 @@ xpipe_status xpipe_relbias_bwd(const float* dbias, int32_t buckets, int32_t head
  * Layout: [batch][token][head][head_dim], contiguous only in head_dim, aligned to their
  * element, strides in elements: >= 0 for inputs (0 shares them), and such that no two
  * elements fall together for outputs; the token's at most XPIPE_ATTENTION_MAX_STRIDE.
- * head_dim 1 .. 128, batch * heads * (nq / 128 + 1) and the same of keys below 2^27, nq and nk below 2^24,
+ * head_dim 1 .. 128, batch * heads * (nq / 128 + 1) and the same of keys below 2^23, nq and nk below 2^24,
  * bias_range 1 .. 2^20 (beyond: XPIPE_EUNSUPPORTED).  Lengths outside 0 .. nq, 0 .. nk are taken as
  * the nearest of them.  Outputs must not overlap inputs nor one another. */
 #define XPIPE_ATTENTION_MAX_STRIDE ((int64_t)1 << 22)

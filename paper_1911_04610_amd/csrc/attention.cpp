@@ -43,10 +43,14 @@ xpipe_status check_inputs(const xpipe_attention_inputs& q, AttnArgs* a) {
   if (!(q.scale > 0) || !std::isfinite((float)q.scale) || !((float)q.scale > 0)) return fail(XPIPE_EINVAL, "scale must be > 0 and finite");
   if (!(q.cap >= 0) || !std::isfinite((float)q.cap) || (q.cap > 0 && !((float)q.cap > 0)))
     return fail(XPIPE_EINVAL, "cap must be >= 0 and finite");
+  // (factors that a kernel forms of them)
+  if (!std::isfinite(4.f * (float)q.scale) || !std::isfinite(4.f * (float)q.cap) || (q.cap > 0 && !std::isfinite(4.f * (float)q.scale / (float)q.cap)))
+    return fail(XPIPE_EINVAL, "scale, cap or their quotient too large for fp32");
   if (q.head_dim > ATTN_MAX_DIM) return fail(XPIPE_EUNSUPPORTED, "head_dim beyond 128");
-  if (q.nq >= 1 << 24 || q.nk >= 1 << 24 || (int64_t)q.batch * q.heads >= 1 << 27 ||
-      (int64_t)q.batch * q.heads * (q.nq / 128 + 1) >= 1 << 27 || (int64_t)q.batch * q.heads * (q.nk / 128 + 1) >= 1 << 27)
-    return fail(XPIPE_EUNSUPPORTED, "2^24 tokens of a sequence, or 2^27 blocks of 128 rows, or more");
+  // (a launch has less than 2^32 threads)
+  if (q.nq >= 1 << 24 || q.nk >= 1 << 24 || (int64_t)q.batch * q.heads >= 1 << 23 ||
+      (int64_t)q.batch * q.heads * (q.nq / 128 + 1) >= 1 << 23 || (int64_t)q.batch * q.heads * (q.nk / 128 + 1) >= 1 << 23)
+    return fail(XPIPE_EUNSUPPORTED, "2^24 tokens of a sequence, or 2^23 blocks of 128 rows, or more");
   if (q.batch > 65535) return fail(XPIPE_EUNSUPPORTED, "more than 65535 sequences");
   if (q.heads > 65535) return fail(XPIPE_EUNSUPPORTED, "more than 65535 heads");
   if (q.prefix && !q.causal) return fail(XPIPE_EINVAL, "prefix without causal");

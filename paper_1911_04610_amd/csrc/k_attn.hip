@@ -1351,11 +1351,11 @@ bool few(const AttnArgs& a) { return (int64_t)a.nq * (a.heads / a.kv_heads) <= 6
 // Parts of the keys where the rows alone do not fill the card.  k_attn_fwd: two workgroups a CU, at
 // least 4 steps each (fp32, whose steps are long: 2), 1: none.  k_attn_few: workgroups over all sequences for each key head and block of
 // rows, two a CU, of at least 8 steps of 32 keys; 0: up to 4 steps, which a wave does sooner than a
-// second launch joins them.
+// second launch joins them, and where the rows alone are eight waves a CU.
 int parts(int dtype, const AttnArgs& a) {
   if (few(a)) {
     const int64_t units = ceil_div((int64_t)a.nq * a.pk, 32) * a.kv_heads, steps = ceil_div(a.nk, 32);
-    if (steps <= 4 || units == 0 || a.batch == 0) return 0;
+    if (steps <= 4 || units == 0 || units * a.batch >= 2048) return 0;
     return (int)std::max<int64_t>(a.batch, std::min<int64_t>(ceil_div(512, units), a.batch * ceil_div(steps, 8)));
   }
   const int64_t groups = ceil_div(a.nq, ROWS) * a.heads * a.batch, steps = ceil_div(a.nk, keys_of(dtype));

@@ -5,8 +5,8 @@
 // A distance a >= 0 lies in one of n buckets: below n / 2 each has its own, beyond
 // they grow with the logarithm, bucket n / 2 + floor(log(2 a / n) / log(2 far / n) (n - n / 2)),
 // the last one from there on.  In fp64; a distance on a border belongs to the bucket that
-// starts there (the quotient is raised by 1e-10, which is less than the least that whole
-// distances up to 2^20 miss a border by).
+// starts there: the quotient is raised by 2^-44 of itself, a few times what its logarithms and
+// products round by.
 #include "xp_device.h"
 #include "xp_kernels.h"
 
@@ -22,7 +22,7 @@ struct Buckets {
 
 XP_DEV int bucket_of(const Buckets& b, int away) {
   if (away < b.half) return away;
-  const int k = (int)(log((double)away / b.half) * b.scale + 1e-10);
+  const int k = (int)(log((double)away / b.half) * b.scale * (1.0 + 0x1p-44));
   return min(b.n - 1, b.half + k);
 }
 XP_DEV int bucket_at(const Buckets& b, int d) {  // d: key position - query position

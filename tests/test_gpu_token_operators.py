@@ -405,7 +405,8 @@ def test_attention_cap_and_bias(shape, cap, reach, mask, docs, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("shape", [(1, 1, 3000, 4, 2, 128), (3, 1, 1000, 8, 1, 64), (2, 4, 2000, 2, 2, 40), (1, 20, 1500, 8, 2, 128), (2, 1, 257, 1, 1, 128)])
+@pytest.mark.parametrize("shape", [(1, 1, 3000, 4, 2, 128), (3, 1, 1000, 8, 1, 64), (2, 4, 2000, 2, 2, 40), (1, 20, 1500, 8, 2, 128), (2, 1, 257, 1, 1, 128),
+                                   (70, 1, 300, 2, 1, 64), (1, 16, 700, 8, 2, 96), (300, 2, 90, 2, 1, 16), (5, 1, 33, 3, 1, 128)])
 def test_attention_few_queries(shape, dtype):
     """Few rows over many keys: rows of heads that share keys together, the keys in parts."""
     Case(*shape, dtype, mask="causal").check(train=False)
@@ -495,6 +496,7 @@ def test_attention_large_scores():
     for dtype in ("bf16", "f32"):
         Case(1, 64, 200, 2, 1, 64, dtype, spread=30.0).check()
         Case(1, 64, 200, 2, 1, 64, dtype, spread=30.0, cap=50.0, mask="causal").check()
+        Case(1, 64, 200, 2, 1, 64, dtype, spread=3.0, cap=0.5, reach=20).check()
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

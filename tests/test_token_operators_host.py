@@ -129,7 +129,7 @@ def _attn_refused(a, status=xp.EINVAL):
 
 COMMON = [
     dict(batch=-1), dict(nq=-1), dict(nk=-1), dict(heads=0), dict(kv_heads=0), dict(kv_heads=3), dict(head_dim=0), dict(dtype=5), dict(scale=0.0),
-    dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=1e300), dict(scale=1e-300), dict(cap=-1.0), dict(cap=float("inf")), dict(cap=float("nan")), dict(cap=1e-300),
+    dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=1e300), dict(scale=1e-300), dict(cap=-1.0), dict(cap=float("inf")), dict(cap=float("nan")), dict(cap=1e-300), dict(scale=2e38), dict(cap=2e38), dict(scale=1e10, cap=1e-30),
     dict(prefix=10 * P), dict(q_doc=10 * P), dict(k_doc=10 * P), dict(bias=10 * P), dict(bias=10 * P, bias_range=-1), dict(q_len=10 * P + 2),
     dict(bias=10 * P + 1, bias_range=3), dict(q=xp.Heads(None, 1, 1, 1)), dict(k=xp.Heads(None, 1, 1, 1)), dict(v=xp.Heads(3 * P + 1, 15360, 128, 64)),
     dict(q=xp.Heads(P, -1, 256, 64)), dict(q=xp.Heads(P, 25600, -1, 64)), dict(k=xp.Heads(2 * P, 15360, 128, -64)),
@@ -163,7 +163,7 @@ def test_attention_backward_refusals(kw):
 
 
 @pytest.mark.parametrize("kw", [
-    dict(head_dim=129), dict(nq=1 << 24), dict(nk=1 << 24), dict(batch=1 << 20, nq=1 << 20), dict(batch=65536, nq=1, nk=1), dict(bias=10 * P, bias_range=(1 << 20) + 1),
+    dict(head_dim=129), dict(nq=1 << 24), dict(nk=1 << 24), dict(batch=1 << 20, nq=1 << 20), dict(batch=1 << 13, heads=1 << 10, kv_heads=1 << 10, nq=1, nk=1), dict(batch=65536, nq=1, nk=1), dict(bias=10 * P, bias_range=(1 << 20) + 1),
     dict(q=xp.Heads(P, 25600, (1 << 22) + 1, 64)), dict(k=xp.Heads(2 * P, 1 << 41, 128, 64)),
 ])
 def test_attention_unsupported(kw):
