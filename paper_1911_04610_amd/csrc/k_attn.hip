@@ -253,16 +253,21 @@ XP_DEV f32x16_t rows_times(uint32_t at, int more, uint32_t col) {
   return c;
 }
 
-// acc[d][lane's column] += sum over 32 rows of tile[row][d] w[row]; at: column_place + tile
-template <typename T, int DP>
+// acc[d][lane's column] += sum over 32 rows of tile[row][d] w[row]; at: column_place + tile.
+// TWICE: w as two bf16 values, for 16 bits of it.
+template <typename T, int DP, bool TWICE = false>
 XP_DEV void add_transposed(f32x16_t (&acc)[DP / 32], uint32_t at, int more, const float (&w)[16], int dim) {
   if constexpr (sizeof(T) == 2) {
     typedef short v4i16 __attribute__((ext_vector_type(4)));
 #pragma unroll
     for (int b = 0; b < 2; ++b) {  // 16 rows: 4 lane / 32 + 0 .. 3 of them, and 8 further on
-      u32x4_t f;
+      u32x4_t f, rest;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) f[i] = f32x2_to_bf16x2(w[8 * b + 2 * i], w[8 * b + 2 * i + 1]);
+      for (int i = 0; i < 4; ++i) {
+        const float w0 = w[8 * b + 2 * i], w1 = w[8 * b + 2 * i + 1];
+        f[i] = f32x2_to_bf16x2(w0, w1);
+        if constexpr (TWICE) rest[i] = f32x2_to_bf16x2(w0 - __uint_as_float(f[i] << 16), w1 - __uint_as_float(f[i] & 0xffff0000u));
+      }
 #pragma unroll
       for (int d = 0; d < DP / 32; ++d) {
         v4i16 part[2];
@@ -271,6 +276,7 @@ XP_DEV void add_transposed(f32x16_t (&acc)[DP / 32], uint32_t at, int more, cons
           part[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds<v4i16>((at ^ (d * 64 + k * 32)) + (more + (16 * b + 8 * k) * ROW<T, DP>)));
         const u32x4_t x = __builtin_bit_cast(u32x4_t, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
         acc[d] = mma<T>(x, f, acc[d]);
+        if constexpr (TWICE) acc[d] = mma<T>(x, rest, acc[d]);
       }
     }
   } else {
@@ -888,10 +894,15 @@ XP_DEV int first_near(const AttnArgs& a, const Seq& seq, int kw) { return max(0,
 // As the forward, a lane a query: scores and dP from the keys' and values' rows, then
 // dq += dX K.  do . o comes from the stored o here (rounded, as dq itself will be); the same
 // sum as P dP in fp32, which the loop makes by the way, is what k_attn_dkv reads: bias
-// gradients are fp32, and a rounded o would show in their sums.  (dX as two bf16 values, for a dq
-// without its rounding, takes this kernel from 331 to 398 us on 2 sequences of 4096 tokens, 16 heads
-// of 128; dq is 2.4e-3 to 2.7e-3 of its 2-norm off without, of which rounding dq itself is 1.7e-3.)
-template <typename T, int DP, int MODE>
+// gradients are fp32, and a rounded o would show in their sums.
+// TWICE: dX as two bf16 values.  Three roundings reach dq in bf16 storage: its own, dX's, and o's, which the
+// sum over n keys of like weight leaves at 1 / sqrt(n) of itself.  Over many keys dq is
+// 2.4e-3 of its 2-norm off (its own rounding alone: 1.7e-3); over few it would be 2.6e-3 to
+// 2.8e-3, and is 2.3e-3 without dX's (2 x 4096 tokens, 12 heads of 64, documents of 32 to 2048: 100 us for 90).
+// Few rows: the keys in `splits` parts, whose sums k_attn_dq_join adds.
+// Bound as the forward is: two waves a SIMD, whose products (three here) and exponentials overlap in part only.
+// 2 sequences of 4096 tokens, 16 heads of 128 over 4, prefix: 332 us; matrix units busy for 30 % of it.
+template <typename T, int DP, int MODE, bool TWICE>
 __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dq(AttnArgs a) {
   constexpr int KEYS = BN_DQ<T, DP>, NB = KEYS / 32;
   constexpr int TILE = KEYS * ROW<T, DP>;
@@ -902,6 +913,8 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dq(AttnArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int blocks = (a.nq + ROWS - 1) / ROWS;
   int id = xcd_tile(blockIdx.x, gridDim.x);
+  const int split = id % a.splits;
+  id /= a.splits;
   const int blk = blocks - 1 - id % blocks;
   id /= blocks;
   const int head = id % a.heads, b = id / a.heads;
@@ -948,8 +961,9 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dq(AttnArgs a) {
   const T* vp = (const T*)a.v.p + b * a.v.b + kvh * a.v.h;
   const int32_t* kdoc = a.k_doc ? a.k_doc + (int64_t)b * a.nk : nullptr;
 
-  const int tiles = (kmax + KEYS - 1) / KEYS, tab_tiles = (a.nk + KEYS - 1) / KEYS;
-  Walk walk(a.k_tab ? a.k_tab + (int64_t)b * tab_tiles : nullptr, tiles, docs.lo, docs.hi);
+  const int tiles = (kmax + KEYS - 1) / KEYS, per = (tiles + a.splits - 1) / a.splits;
+  const int tab_tiles = (a.nk + KEYS - 1) / KEYS;
+  Walk walk(a.k_tab ? a.k_tab + (int64_t)b * tab_tiles : nullptr, min(tiles, (split + 1) * per), docs.lo, docs.hi);
   const float c1 = a.scale * LOG2E;
   f32x16_t acc[DP / 32];
 #pragma unroll
@@ -976,7 +990,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dq(AttnArgs a) {
     if constexpr (has_bias(MODE)) window.store(sbias[buf]);
     if (kdoc && threadIdx.x < KEYS) sdoc[buf][threadIdx.x] = dreg;
   };
-  int t = walk.next(0), buf = 0;
+  int t = walk.next(min(tiles, split * per)), buf = 0;
   if (t < walk.end) {
     load(t);
     store(0);
@@ -1019,7 +1033,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dq(AttnArgs a) {
           for (int r = 0; r < 16; ++r) ds[r] *= slope[r];
         }
         phase();
-        add_transposed<T, DP>(acc, cat, n * 32 * ROW<T, DP>, ds, a.ldim);
+        add_transposed<T, DP, TWICE>(acc, cat, n * 32 * ROW<T, DP>, ds, a.ldim);
         phase();
       }
     }
@@ -1028,15 +1042,44 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dq(AttnArgs a) {
     t = tn;
   }
   exact = both_sum(exact);
-  if (lane < 32) {
+  if (lane < 32 && split == 0) {
     float* row = a.rows + (((int64_t)b * a.heads + head) * (blocks * 4) + blk * 4 + wave) * ROW_INFO + lane;
     row[0] = st.a;
     row[32] = st.b;
-    row[64] = exact;
+    row[64] = a.splits > 1 ? 0.f : exact;
     row[96] = __int_as_float(kend);
     row[128] = __int_as_float(doc);
   }
-  if (in) st_column<T, DP>((T*)a.dq.p + b * a.dq.b + (int64_t)i * a.dq.t + head * a.dq.h, a.dim, acc, a.scale);
+  if (!in) return;
+  if (a.splits > 1) {
+    const int64_t at = split * ((int64_t)a.batch * a.heads * a.nq) + srow;
+    st_column<float, DP>(a.part_o + at * DP, DP, acc, a.scale);
+    if (lane < 32) a.part_ml[at] = exact;
+  } else {
+    st_column<T, DP>((T*)a.dq.p + b * a.dq.b + (int64_t)i * a.dq.t + head * a.dq.h, a.dim, acc, a.scale);
+  }
+}
+
+// The parts' sums of dq, and of P dP for k_attn_dkv, added in their order: four columns a thread.
+template <typename T, int DP>
+__global__ __launch_bounds__(256) void k_attn_dq_join(AttnArgs a) {
+  const int64_t rows = (int64_t)a.batch * a.heads * a.nq, x = (int64_t)blockIdx.x * 256 + threadIdx.x, r = x / (DP / 4);
+  if (r >= rows) return;
+  const int d = (int)(x % (DP / 4)) * 4;
+  float s[4] = {0.f, 0.f, 0.f, 0.f}, exact = 0.f;
+#pragma unroll 4
+  for (int p = 0; p < a.splits; ++p) {
+    const f32x4_t v = *reinterpret_cast<const f32x4_t*>(a.part_o + (p * rows + r) * DP + d);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] += v[i];
+    if (d == 0) exact += a.part_ml[p * rows + r];
+  }
+  const int i = (int)(r % a.nq), head = (int)(r / a.nq % a.heads), b = (int)(r / a.nq / a.heads), blocks = (a.nq + ROWS - 1) / ROWS;
+  T* to = (T*)a.dq.p + b * a.dq.b + (int64_t)i * a.dq.t + head * a.dq.h + d;
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (d + k < a.dim) std_(to + k, (double)s[k]);
+  if (d == 0) a.rows[(((int64_t)b * a.heads + head) * (blocks * 4) + i / 32) * ROW_INFO + 64 + i % 32] = exact;
 }
 
 // grad_bias[head][x] += the sum over sequences and key blocks of the blocks' diagonals at
@@ -1363,6 +1406,18 @@ int parts(int dtype, const AttnArgs& a) {
   return (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(512, groups), steps / (dtype == DT_BF16 ? 4 : 2)));
 }
 
+// Parts of the keys of k_attn_dq where its rows do not fill the card, of at least 8 steps (fp32, whose steps are
+// long: 2).  Not with documents, whose rows see few keys.  (Training steps: fp32, 2902 tokens, one head of 33: 207 us, in
+// one part 469; bf16, 3840 tokens, 8 heads of 64: 239 and 287.)
+int dq_parts(int dtype, const AttnArgs& a) {
+  const int64_t groups = ceil_div(a.nq, ROWS) * a.heads * a.batch, steps = ceil_div(a.nk, dq_keys_of(dtype, a));
+  if (groups == 0 || groups >= 256 || a.q_doc) return 1;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(512, groups), steps / (dtype == DT_BF16 ? 8 : 2)));
+}
+
+// Where dq's products keep dX to 16 bits.
+bool few_keys(const AttnArgs& a) { return a.k_doc || a.nk <= 2048; }
+
 // blocks of 32 queries that hold distances within the range, of 32 keys
 int near_blocks(const AttnArgs& a) { return (int)std::min<int64_t>(ceil_div(a.nq, 32), ceil_div(2 * (int64_t)a.range + 62, 32) + 1); }
 
@@ -1424,6 +1479,12 @@ size_t lay_bwd(int dtype, AttnArgs& a, char* base, AttnMat* from) {
   }
   const int64_t kgroups = ceil_div(a.nk, ROWS) * a.kv_heads * a.batch;
   cut_dkv(dtype, a, kgroups);
+  a.splits = dq_parts(dtype, a);
+  if (a.splits > 1) {
+    const int64_t count = (int64_t)a.batch * a.heads * a.nq * a.splits;
+    a.part_o = (float*)take((size_t)count * padded_dim(a.dim) * 4);
+    a.part_ml = (float*)take((size_t)count * 4);
+  }
   if (a.head_parts * a.q_parts > 1)
     a.part_kv = (float*)take((size_t)a.batch * a.nk * a.kv_heads * a.head_parts * a.q_parts * 2 * padded_dim(a.dim) * 4);
   a.rows = (float*)take((size_t)a.batch * a.heads * ceil_div(a.nq, ROWS) * 4 * ROW_INFO * 4);
@@ -1502,9 +1563,22 @@ template <typename T, int DP, int MODE>
 void bwd(const AttnArgs& a, hipStream_t s) {
   const double pairs = (double)a.batch * a.heads * a.nq * a.nk;
   const int64_t parts = (int64_t)a.head_parts * a.q_parts;
-  const int64_t groups = ceil_div(a.nq, ROWS) * a.heads * a.batch, kgroups = ceil_div(a.nk, ROWS) * a.kv_heads * a.batch * parts;
-  if (groups > 0)
-    XP_LAUNCH(sizeof(T) == 2 ? "k_attn_dq<bf16>" : "k_attn_dq<f32>", 6 * pairs * a.dim, (k_attn_dq<T, DP, MODE>), dim3((unsigned)groups), dim3(256), 0, s, a);
+  const int64_t groups = ceil_div(a.nq, ROWS) * a.heads * a.batch * a.splits, kgroups = ceil_div(a.nk, ROWS) * a.kv_heads * a.batch * parts;
+  if (groups > 0) {
+    const double flops = 6 * pairs * a.dim;
+    bool done = false;
+    if constexpr (sizeof(T) == 2) {
+      if (few_keys(a)) {
+        XP_LAUNCH("k_attn_dq<bf16>", flops, (k_attn_dq<T, DP, MODE, true>), dim3((unsigned)groups), dim3(256), 0, s, a);
+        done = true;
+      }
+    }
+    if (!done) XP_LAUNCH(sizeof(T) == 2 ? "k_attn_dq<bf16>" : "k_attn_dq<f32>", flops, (k_attn_dq<T, DP, MODE, false>), dim3((unsigned)groups), dim3(256), 0, s, a);
+    if (a.splits > 1) {
+      const int64_t rows = (int64_t)a.batch * a.heads * a.nq;
+      XP_LAUNCH("k_attn_dq_join", 4.0 * rows * a.splits * DP, (k_attn_dq_join<T, DP>), dim3((unsigned)ceil_div(rows * (DP / 4), 256)), dim3(256), 0, s, a);
+    }
+  }
   if (kgroups == 0) return;
   if constexpr (sizeof(T) == 4 && DP > 64) {
     XP_LAUNCH("k_attn_dv<f32>", 4 * pairs * a.dim, (k_attn_dkv<T, DP, MODE, 1>), dim3((unsigned)kgroups), dim3(256), 0, s, a);
@@ -1565,7 +1639,7 @@ hipError_t launch_attn_fwd(int dtype, AttnArgs a, void* workspace, hipStream_t s
 
 hipError_t launch_attn_bwd(int dtype, AttnArgs a, void* workspace, hipStream_t s) {
   AttnMat from[4];
-  a.pk = a.splits = 1;
+  a.pk = 1;
   lay_bwd(dtype, a, (char*)workspace, from);
   const AttnMat* const to[4] = {&a.q, &a.k, &a.v, &a.dout};
   launch_pack(dtype, a, from, to, 4, s);

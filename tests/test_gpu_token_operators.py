@@ -416,6 +416,13 @@ def test_attention_few_queries(shape, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("mask,docs,cap,reach", [("causal", False, 0.0, 0), ("prefix", False, 20.0, 40), ("none", True, 0.0, 0)])
+@pytest.mark.parametrize("shape", [(1, 90, 2100, 2, 1, 33), (1, 140, 2300, 1, 1, 96), (2, 30, 2081, 2, 2, 128), (1, 2080, 300, 2, 1, 64)])
+def test_attention_many_keys(shape, mask, docs, cap, reach, dtype):
+    Case(*shape, dtype, mask=mask, docs=docs, cap=cap, reach=reach, ragged=not docs).check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("layout,pitch", [("bhtd", 0), ("bhtd", 3), ("packed", 0), ("packed", 1), ("bthd", 1), ("bthd", 7), ("bthd", 8)])
 def test_attention_layouts(layout, pitch, dtype):
     Case(2, 90, 130, 4, 2, 64, dtype, mask="causal", layout=layout, pitch=pitch).check()
