@@ -599,7 +599,8 @@ xpipe_status xpipe_relbias_bwd(const float* dbias, int32_t buckets, int32_t head
  * whatever they hold.  (Another value that is not finite can also reach rows that do not see it,
  * those of the same tile: 0 times it is a NaN.)  A -inf in bias masks; a row of which every score is -inf sees nothing.
  * Types: as the linear layers' (products with fp32 sums; in XPIPE_BF16 P and the score
- * gradients are rounded to bf16 as operands of the second products); scores, maxima and
+ * gradients are rounded to bf16 as operands of the second products, for dq over few keys
+ * (documents, or nk up to 2048) to two bf16 values); scores, maxima and
  * sums are fp32, and the order of the sums follows from the sizes and lengths alone.
  * Layout: [batch][token][head][head_dim], contiguous only in head_dim, aligned to their
  * element, strides in elements: >= 0 for inputs (0 shares them), and such that no two
@@ -642,7 +643,9 @@ typedef struct {
 xpipe_status xpipe_attention_fwd_query(const xpipe_attention_fwd_args* args, size_t* workspace_bytes);
 xpipe_status xpipe_attention_bwd_query(const xpipe_attention_bwd_args* args, size_t* workspace_bytes);
 /* workspace: device memory, 256-byte aligned, of at least the query's bytes, free
- * again once the call's work is done (NULL where the query gives 0). */
+ * again once the call's work is done (NULL where the query gives 0).  With grad_bias the
+ * backward's grows as batch heads (nk / 32) min(nq, 2 bias_range) 8 bytes: the sums of dS
+ * along the diagonals of its blocks. */
 xpipe_status xpipe_attention_fwd(const xpipe_attention_fwd_args* args, void* workspace, size_t workspace_bytes, void* hip_stream);
 xpipe_status xpipe_attention_bwd(const xpipe_attention_bwd_args* args, void* workspace, size_t workspace_bytes, void* hip_stream);
 

@@ -31,7 +31,7 @@ XP_DEV int bucket_at(const Buckets& b, int d) {  // d: key position - query posi
 }
 
 // A thread takes one distance and up to 16 heads: the logarithm costs more than the heads'
-// values do.
+// values do.  Bound by that, and by the launch: 65537 distances, 64 heads 6.9 us (16.8 MB, 2.4 TB/s); 257, 12 2.8 us.
 constexpr int HEADS_PER = 16;
 
 __global__ __launch_bounds__(256) void k_relbias_fwd(const float* __restrict__ table, Buckets b, int heads, float* __restrict__ bias) {
@@ -71,6 +71,8 @@ XP_DEV double run_sum(const float* p, int n) {
 // One workgroup per bucket and 4 heads: the bucket's distances are one run of each head's row.
 // Finding its ends costs as much as a short run, so one wave does it for all of them.
 // THREADS: 1024 where runs are long.
+// Bound by the longest run (the bucket of all keys behind the query holds half of a row): 65537
+// distances, 64 heads, 64 buckets 23 us (55 with one head a workgroup); 257 distances, 12 heads 6 us, of which the ends are half.
 constexpr int RUNS = 4;
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void k_relbias_bwd(const float* __restrict__ dbias, Buckets b, int heads, float* __restrict__ grad) {

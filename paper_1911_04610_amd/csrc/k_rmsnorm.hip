@@ -96,7 +96,7 @@ XP_DEV void row_sums(double (&v)[N], double (*sh)[16], int turn) {
 }
 
 // A thread's part of a row's sums.  In bf16 storage over E elements in fp32 (an fp64 sum takes
-// longer than the row's bytes do: 16384x4096 backward 164 us against 118); a row whose sum of squares leaves the
+// longer than the row's bytes do: 16384x4096 backward 118 us with it, 87 without); a row whose sum of squares leaves the
 // range where that is exact to fp32 is summed again in fp64.
 XP_DEV bool in_range(double squares) { return squares > 1e-20 && squares < 1e36; }
 template <typename T, int E>
@@ -133,6 +133,8 @@ XP_DEV void wide_sums(const float (&h)[E], const float (&dy)[E], const float (&w
   products<float, E>(h, dy, w, s[1]);
 }
 
+// 16384x4096 bf16 with residual and sum: 97 us, 5.6 TB/s, of what a copy reaches (5.2 torch's, 6.2 the library's
+// probe); one row: 3 us, a launch.
 // No __restrict__: sum and y may be x's or residual's buffer (every element is read
 // by the thread that writes it, before).
 template <typename T, int G, int E>
@@ -191,6 +193,8 @@ __global__ __launch_bounds__(THREADS<G>) void k_rms_fwd(RmsArgs a) {
 // fp32 (at most a few hundred of them), over the ROWS rows at a time in LDS.  The parts
 // are added in fp64 by k_rms_join; a single workgroup adds its own.  The next row's
 // h and dy are on their way while this one's sums are joined.
+// Bound by the bytes of large calls (16384x4096 bf16: 87 us, 4.6 TB/s for h, dy and dx) and by the two launches of
+// small ones: 8192x2048 with the skip's gradient 36 us (134 MB, 3.7 TB/s) and 5 us for the join, 1001x999 fp32 6.5 and 5.
 template <typename T, int G, int E>
 __global__ __launch_bounds__(THREADS<G>) void k_rms_bwd(RmsArgs a) {
   constexpr int C = CHUNK<T>, V = E / C;
