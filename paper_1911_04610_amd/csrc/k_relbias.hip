@@ -68,12 +68,13 @@ XP_DEV double run_sum(const float* p, int n) {
   return s;
 }
 
-// One workgroup per bucket and 4 heads: the bucket's distances are one run of each head's row.
+// One workgroup per bucket and 2 heads: the bucket's distances are one run of each head's row.
 // Finding its ends costs as much as a short run, so one wave does it for all of them.
 // THREADS: 1024 where runs are long.
 // Bound by the longest run (the bucket of all keys behind the query holds half of a row): 65537
-// distances, 64 heads, 64 buckets 23 us (55 with one head a workgroup); 257 distances, 12 heads 6 us, of which the ends are half.
-constexpr int RUNS = 4;
+// distances, 64 heads, 64 buckets, with the forward: 27.4 us (1 head a workgroup 31.5, 4 heads 29.7); 257 distances,
+// 12 heads 8.8 us (9.7, 9.6), of which the ends are half of the backward's.
+constexpr int RUNS = 2;
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void k_relbias_bwd(const float* __restrict__ dbias, Buckets b, int heads, float* __restrict__ grad) {
   __shared__ double sh[RUNS][THREADS / 64];

@@ -322,6 +322,8 @@ void by_size(int dim, F&& f) {
   else f(integral_constant<int, 1024>{}, integral_constant<int, 32>{});
 }
 
+// Two workgroups a CU (8192x2048 with the skip's gradient 47.2 us, 4096x8192 91.9, 16384x4096 119; three: 50.0,
+// 99.3, 110; four: 53.9, 107, 132).
 template <int G>
 int bwd_blocks(int64_t rows) { return (int)std::min<int64_t>((rows + ROWS<G> - 1) / ROWS<G>, G >= 1024 ? 256 : 512); }
 
