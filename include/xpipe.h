@@ -601,7 +601,8 @@ xpipe_status xpipe_relbias_bwd(const float* dbias, int32_t buckets, int32_t head
  * Types: as the linear layers' (products with fp32 sums; in XPIPE_BF16 P and the score
  * gradients are rounded to bf16 as operands of the second products, for dq over few keys
  * (documents, or nk up to 2048) to two bf16 values); scores, maxima and
- * sums are fp32, and the order of the sums follows from the sizes and lengths alone.
+ * sums are fp32, a capped score good to a few 2^-24 of itself (in XPIPE_BF16 without a bias and up to a cap of 64: of
+ * the cap), and the order of the sums follows from the sizes and lengths alone.
  * Layout: [batch][token][head][head_dim], contiguous only in head_dim, aligned to their
  * element, strides in elements: >= 0 for inputs (0 shares them), and such that no two
  * elements fall together for outputs; the token's at most XPIPE_ATTENTION_MAX_STRIDE.

@@ -455,27 +455,64 @@ template <int MODE>
 XP_DEV float log2_of(float d, float c1) { return MODE == PLAIN ? d * c1 : d; }
 
 // Scores of a block of 32 x 32 from its products, in their place; slope: of the cap.  at(r): the bias of
-// register r.  For u = scale x / cap, e = exp(-2 |u|): tanh(u) = (1 - e) / (1 + e) with u's sign, good to a
-// few steps of itself but for 1 - e, which is good to half a step of 1; its slope 4 e / (1 + e)^2.
-// Without a bias and in bf16 storage, where nothing but rounded results comes of it, 1 - 2 r and
-// 4 r (1 - r) with r = 1 / (1 + exp(2 u)), off by 2^-23 of 1: three operations less of each score (8192
-// tokens, 16 heads of 128, causal 397 us against 457).
-template <typename T, int MODE, bool SLOPE, typename F>
+// register r.  For x = scale q.k / cap the capped score is cap tanh(x), a few steps off itself at most whatever the
+// cap is: below SMALL from tanh(x) / x = 1 + x^2 p(x^2), p of degree 3 with the least relative error over that
+// range (2^-26), times scale q.k, so that a large cap costs no bits; beyond it 1 - 2 q with q = 1 / (1 + exp(2 x)), and
+// the slope 4 q (1 - q), off by 2^-22 of 1.  Which of them a score takes depends on itself alone; a block none of whose
+// scores is beyond SMALL passes the exponentials over (BOTH_WAYS, where the keys' bytes bound: none does, for fewer registers).
+// In bf16 storage, without a bias (whose gradient is fp32) and up to a cap of QUICK_CAP 1 - 2 q alone: the scores are off by
+// 12 * 2^-24 of the cap then, 2^-14 at most, where P itself is rounded by 2^-8.  (16 heads of 8192 tokens, causal, scores
+// of 1: cap 50 404 us, 409 with the polynomial; cap 1, where half of the scores are beyond SMALL, 390 and 552.)
+constexpr float SMALL = 0.5f, QUICK_CAP = 64.f;
+template <typename T, int MODE, bool SLOPE, bool BOTH_WAYS = false, typename F>
 XP_DEV void scores(f32x16_t& s, const AttnArgs& a, float (&slope)[16], F&& at) {
   if constexpr (has_cap(MODE)) {
-    const float k = 2.f * LOG2E * a.scale / a.cap, top = a.cap * LOG2E;
+#pragma clang fp contract(off)  // (the bits of a score do not depend on which way its block goes)
+    const float c1 = a.scale * LOG2E, k = a.scale / a.cap, top = a.cap * LOG2E;
+    auto small = [&](float v, float x, float& d) __attribute__((always_inline)) {
+      const float y = x * x;
+      const float p = fmaf(y, fmaf(y, fmaf(y, fmaf(y, 0.01724149f, -0.05304549f), 0.13325879f), -0.33333144f), 1.f);
+      d = fmaf(-(y * p), p, 1.f);
+      return v * c1 * p;
+    };
+    auto large = [&](float x2, float& d) __attribute__((always_inline)) {  // (2 log2(e) x)
+      const float q = __builtin_amdgcn_rcpf(1.f + exp2_(x2));
+      d = 4.f * fmaf(-q, q, q);
+      return fmaf(-2.f * top, q, top);
+    };
+    float most = 0.f;
+    const bool quick = sizeof(T) == 2 && MODE == CAP && !BOTH_WAYS && a.cap <= QUICK_CAP;
+    if (!quick)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      if constexpr (sizeof(T) == 2 && MODE == CAP) {
-        const float q = __builtin_amdgcn_rcpf(1.f + exp2_(s[r] * k));
-        s[r] = top - 2.f * top * q;
-        if constexpr (SLOPE) slope[r] = 4.f * q - 4.f * q * q;
-      } else {
-        const float u = s[r] * k, e = exp2_(-fabsf(u)), q = __builtin_amdgcn_rcpf(1.f + e);
-        s[r] = copysignf(top * ((1.f - e) * q), u);
-        if constexpr (SLOPE) slope[r] = 4.f * e * q * q;
-        if constexpr (has_bias(MODE)) s[r] += at(r);
+      for (int r = 0; r < 16; ++r) most = fmaxf(most, fabsf(s[r]));
+    if (quick) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        float d;
+        s[r] = large(s[r] * (2.f * LOG2E * k), d);
+        if constexpr (SLOPE) slope[r] = d;
       }
+    } else if (BOTH_WAYS || __any(most * k >= SMALL)) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        float d, dl;
+        const float x = s[r] * k, v = small(s[r], x, d), vl = large(2.f * LOG2E * x, dl);
+        const bool beyond = fabsf(x) >= SMALL;
+        s[r] = beyond ? vl : v;
+        if constexpr (SLOPE) slope[r] = beyond ? dl : d;
+      }
+    } else {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        float d;
+        s[r] = small(s[r], s[r] * k, d);
+        if constexpr (SLOPE) slope[r] = d;
+      }
+    }
+    if constexpr (has_bias(MODE)) {
+      phase();
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] += at(r);
     }
   } else if constexpr (has_bias(MODE)) {
     const float c1 = a.scale * LOG2E;
@@ -798,7 +835,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_few(AttnArgs a) {
     if constexpr (MODE != PLAIN) {
       float none[16];
       const int d0 = j0 - i - seq.off;
-      scores<T, MODE, false>(s, a, none, [&](int r) { return log2_bias(bias[min(max(d0 + row_of(r), -a.range), a.range)]); });
+      scores<T, MODE, false, true>(s, a, none, [&](int r) { return log2_bias(bias[min(max(d0 + row_of(r), -a.range), a.range)]); });
     }
     if (j0 + 32 > kmin || blk == blocks - 1) hide_from(s, kend - j0, NEG_INF);
     if (kdoc) hide_others(s, sdoc[wave], doc, NEG_INF);

@@ -1,0 +1,63 @@
+"""Edges of the operators of token networks on the GPU: values, sizes and places at which
+a formula in 64 bits, or the same call in another layout, has to be met as anywhere else.
+The bounds are those of test_gpu_token_operators.py, or written out at the test."""
+import math
+
+import pytest
+
+import paper_1911_04610_amd as xp
+from test_gpu_token_operators import E24, Case, _close, _d, _dt, _gen, _torch
+
+pytestmark = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------- attention: capped scores
+def _scores(q, cap, **more):
+    """The scores of rows q [n] of one column with one key of 1, as the statistics hold them: their log2(e) multiples."""
+    torch = _torch()
+    n = q.numel()
+    q4, one = q.view(1, n, 1, 1), torch.ones(1, 1, 1, 1, dtype=q.dtype, device="cuda")
+    stats = torch.full((1, 1, n, 2), 7.0, device="cuda")
+    xp.xpipe_attention_fwd(q4, one, one, torch.empty_like(q4), scale=1.0, cap=cap, stats=stats, **more)
+    assert bool(stats[..., 1].eq(1).all())
+    return stats[0, 0, :, 0]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [40, 400])
+@pytest.mark.parametrize("cap", [0.5, 30.0, 1e4, 1e8, 1e30])
+def test_capped_scores_to_their_own_size(cap, rows, dtype):
+    """Every score within 26 * 2^-24 of itself, whatever the cap; in bf16 storage up to a cap of 64, 12 * 2^-24 of the cap.
+    Below half the cap, 1 each for scale log2(e), the product, the polynomial's last step and its multiple, 1 for the
+    rest of it.  Beyond, for q = 1 / (1 + exp(2 x)): 4 * 2^-24 of x, which moves q by 0.9 * 2^-24 at most, 0.5 for the exponential's step,
+    1 for the sum, 2 for the reciprocal; 1 - 2 q doubles that, and 1 for its rounding, 2 for cap log2(e): 12 of the cap, whose
+    0.46th part the score is at least."""
+    torch = _torch()
+    g = _gen(int(math.log2(cap)) + rows)
+    q = cap * torch.exp2(torch.rand(rows, generator=g) * 17 - 12) * torch.sign(torch.randn(rows, generator=g))
+    if cap > 100:
+        q[::2] = torch.randn(rows // 2, generator=g) * 5  # scores of ordinary size under a cap that never binds
+    q = q.to(_dt(dtype)).cuda()
+    want = cap * torch.tanh(_d(q) / cap) / math.log(2)
+    tol = 12 * E24 * cap / math.log(2) if dtype == "bf16" and cap <= 64 else 26 * E24 * want.abs()
+    _close(_scores(q, cap), want, tol, "scores")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_capped_scores_do_not_depend_on_their_neighbours(dtype):
+    torch = _torch()
+    for rows in (40, 400):
+        q = (torch.randn(rows, generator=_gen(rows)) * 2).to(_dt(dtype)).cuda()
+        other = q.clone()
+        other[1::3] = 300.0
+        a, b = _scores(q, 50.0), _scores(other, 50.0)
+        keep = torch.arange(rows) % 3 != 1
+        assert torch.equal(a.cpu()[keep], b.cpu()[keep])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("reach", [0, 20])
+@pytest.mark.parametrize("shape", [(2, 100, 130, 2, 1, 64), (1, 3, 400, 4, 2, 128), (1, 90, 70, 2, 2, 128)])
+def test_a_cap_that_never_binds(shape, reach, dtype):
+    """Under a cap of 1e6 scores below 50 are themselves to 1e-9: results and gradients within the bounds of no cap."""
+    Case(*shape, dtype, mask="causal", reach=reach).check(cap=1e6)
