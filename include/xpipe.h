@@ -528,7 +528,8 @@ xpipe_status xpipe_embedding_bwd(const void* dy, const int32_t* tokens, int64_t 
  * sum receives h (for the next skip connection and the backward); the backward's
  * residual is the gradient that reaches h another way (the skip connection's), and its
  * dx is the gradient of both x and the forward's residual.  weight is the fp32
- * prediction.  A row's sums are fp64, the rest fp32, each stored value is rounded
+ * prediction.  A row's sums are fp64 (in XPIPE_BF16 up to 32 neighbouring terms of them are first
+ * summed in fp32, unless a row's terms leave its range), the rest fp32, each stored value is rounded
  * once (sum is rounded apart; y comes from the unrounded h).  A row's results
  * depend on its own values alone, and the order of grad_weight's sum on the sizes alone.
  * Matrices as for the linear layers; dim at most 32768 (more: XPIPE_EUNSUPPORTED);

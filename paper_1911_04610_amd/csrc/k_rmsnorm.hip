@@ -6,8 +6,8 @@
 //
 // Bandwidth-bound: a row is read once and held in the registers of the G threads
 // that share it (E elements each), the sums go over those threads, in fp64 (squares of
-// fp32 values neither overflow nor lose bits there); the rest is fp32, each stored value
-// is rounded once.
+// fp32 values neither overflow nor lose bits there; in bf16 storage a thread's own elements are
+// summed in fp32 where that holds them); the rest is fp32, each stored value is rounded once.
 #include "xp_device.h"
 #include "xp_lds.h"
 #include "xp_kernels.h"
@@ -96,9 +96,12 @@ XP_DEV void row_sums(double (&v)[N], double (*sh)[16], int turn) {
 }
 
 // A thread's part of a row's sums.  In bf16 storage over E elements in fp32 (an fp64 sum takes
-// longer than the row's bytes do: 16384x4096 backward 118 us with it, 87 without); a row whose sum of squares leaves the
-// range where that is exact to fp32 is summed again in fp64.
+// longer than the row's bytes do: 16384x4096 backward 118 us with it, 87 without); a row whose sums leave the
+// range where that is exact to fp32 is summed again in fp64.  The squares: with a sum between these none has
+// overflowed, and what underflows is below 2^-60 of it.  The products: one that overflowed leaves the row's sum infinite or
+// NaN, and 2^15 that lost 2^-149 each are below 2^-34 of a sum beyond 1e-30 (a row without a gradient is summed twice).
 XP_DEV bool in_range(double squares) { return squares > 1e-20 && squares < 1e36; }
+XP_DEV bool held(double products) { return fabs(products) > 1e-30 && fabs(products) < 1e300; }
 template <typename T, int E>
 XP_DEV void squares(const float (&h)[E], double& out) {
   if constexpr (sizeof(T) == 4) {
@@ -234,7 +237,7 @@ __global__ __launch_bounds__(THREADS<G>) void k_rms_bwd(RmsArgs a) {
     products<T, E>(h, dy, w, s[1]);
     row_sums<G, 2>(s, sh, turn);
     turn ^= 1;
-    if (sizeof(T) == 2 && !in_range(s[0])) {  // (the row's threads agree)
+    if (sizeof(T) == 2 && !(in_range(s[0]) && held(s[1]))) {  // (the row's threads agree)
       wide_sums<E>(h, dy, w, s);
       row_sums<G, 2>(s, sh, turn);
       turn ^= 1;

@@ -6,9 +6,42 @@ import math
 import pytest
 
 import paper_1911_04610_amd as xp
-from test_gpu_token_operators import E24, Case, _close, _d, _dt, _gen, _torch
+from test_gpu_token_operators import E24, Case, _close, _d, _dt, _gen, _half_step, _norm64, _torch
 
 pytestmark = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------- RMS norm
+def _check_norm_backward(dy, h, w, eps, dtype):
+    """dx and grad_weight within the bounds of test_norm_backward, and 3 * 2^-150 n more of dx: dy w, h c and their difference are
+    fp32 values, which below 2^-126 are multiples of 2^-149, each rounded by half of that."""
+    torch = _torch()
+    u, (rows, dim) = _half_step(dtype), h.shape
+    dx, gw = torch.full_like(dy, 7.0), torch.zeros(dim, device="cuda")
+    xp.xpipe_rmsnorm_bwd(dy, h, w, dx, gw, eps=eps)
+    h64, g64 = _d(h), _d(dy) * _d(w)
+    n, _ = _norm64(h64, _d(w), eps)
+    c, mag = n * n * (g64 * h64).mean(1, keepdim=True), n * n * (g64 * h64).abs().mean(1, keepdim=True)
+    want = n * (g64 - h64 * c)
+    tol = 6 * E24 * n * (g64.abs() + h64.abs() * (c.abs() + mag)) + 2 * E24 * want.abs() + 3 * 2.0 ** -150 * n
+    _close(dx, want, u * (want.abs() + tol) + tol, "dx")
+    terms = _d(dy) * h64 * n
+    _close(gw, terms.sum(0), (rows / 256 + 20) * E24 * terms.abs().sum(0), "grad_weight")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dim", [40, 300, 1000, 2047, 4099, 9000, 20000])
+def test_norm_products_that_leave_fp32(dim, dtype):
+    """Rows whose h and dy are in fp32's range and whose products are not, among rows of ordinary size."""
+    torch = _torch()
+    g = _gen(dim)
+    h, dy = torch.randn(9, dim, generator=g), torch.randn(9, dim, generator=g)
+    h[1], dy[1] = h[1] * 1e15, dy[1] * 1e24
+    h[4], dy[4] = h[4] * 1e-9, h[4] * 1e-36 + dy[4] * 1e-37
+    h[5], dy[5] = h[5] * 1e14, h[5].abs() * 1e25 * torch.sign(h[5])
+    dy[7] = 0
+    w = 1 + 0.1 * torch.randn(dim, generator=g)
+    _check_norm_backward(dy.to(_dt(dtype)).cuda(), h.to(_dt(dtype)).cuda(), w.cuda(), 1e-30, dtype)
 
 
 # ---------------------------------------------------------------- attention: capped scores
