@@ -334,7 +334,8 @@ template <typename T>
 hipError_t fwd(const RmsArgs& a, hipStream_t s) {
   by_size(a.dim, [&](auto G, auto E) {
     constexpr int g = decltype(G)::value, e = decltype(E)::value;
-    const int blocks = (int)std::min<int64_t>((a.rows + ROWS<g> - 1) / ROWS<g>, g <= 64 && e == 8 ? 2048 : 1 << 22);  // (a launch has less than 2^32 threads)
+    constexpr int64_t most = g <= 64 && e == 8 ? 2048 : ((int64_t)1 << 31) / THREADS<g>;  // (a launch has less than 2^32 threads)
+    const int blocks = (int)std::min<int64_t>((a.rows + ROWS<g> - 1) / ROWS<g>, most);
     const double bytes = (double)sizeof(T) * a.rows * a.dim * (2 + (a.res != nullptr) + (a.out != nullptr));
     XP_LAUNCH(sizeof(T) == 2 ? "k_rms_fwd<bf16>" : "k_rms_fwd<f32>", bytes, (k_rms_fwd<T, g, e>), dim3(blocks),
               dim3(THREADS<g>), 0, s, a);

@@ -44,6 +44,24 @@ def test_norm_products_that_leave_fp32(dim, dtype):
     _check_norm_backward(dy.to(_dt(dtype)).cuda(), h.to(_dt(dtype)).cuda(), w.cuda(), 1e-30, dtype)
 
 
+def test_norm_of_more_rows_than_a_launch_has_workgroups():
+    """2^22 + 3 rows of 1024 threads each, in place: more threads than a launch may have."""
+    torch = _torch()
+    rows, dim = (1 << 22) + 3, 8200
+    if torch.cuda.mem_get_info()[0] < rows * dim * 2 + (8 << 30):
+        pytest.skip("needs 77 GB of free memory")
+    x = torch.empty(rows, dim, dtype=torch.bfloat16, device="cuda")
+    at = torch.tensor([0, 1, 777, (1 << 21) - 1, 1 << 21, (1 << 21) + 5, rows - 4, rows - 1]).cuda()
+    some, w = torch.randn(8, dim, generator=_gen(8)).bfloat16().cuda(), (1 + 0.1 * torch.randn(dim, generator=_gen(9))).cuda()
+    x[at] = some
+    want = torch.empty_like(some)
+    xp.xpipe_rmsnorm_fwd(some, w, want)
+    xp.xpipe_rmsnorm_fwd(x, w, x)
+    assert torch.equal(x[at], want)
+    del x
+    torch.cuda.empty_cache()
+
+
 # ---------------------------------------------------------------- attention: capped scores
 def _scores(q, cap, **more):
     """The scores of rows q [n] of one column with one key of 1, as the statistics hold them: their log2(e) multiples."""
