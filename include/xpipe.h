@@ -528,10 +528,11 @@ xpipe_status xpipe_embedding_bwd(const void* dy, const int32_t* tokens, int64_t 
  * sum receives h (for the next skip connection and the backward); the backward's
  * residual is the gradient that reaches h another way (the skip connection's), and its
  * dx is the gradient of both x and the forward's residual.  weight is the fp32
- * prediction.  A row's sums are fp64 (in XPIPE_BF16 up to 32 neighbouring terms of them are first
- * summed in fp32, unless a row's terms leave its range), the rest fp32, each stored value is rounded
+ * prediction.  A row's sums are fp64 (in XPIPE_BF16 up to 32 terms at a time are summed
+ * in fp32 first, unless a row's terms leave its range), the rest fp32, each stored value is rounded
  * once (sum is rounded apart; y comes from the unrounded h).  A row's results
- * depend on its own values alone, and the order of grad_weight's sum on the sizes alone.
+ * depend on its own values alone, and the order of grad_weight's sum on the sizes alone (at
+ * most 256 rows' terms, and 32 such sums, are added in fp32, the rest in fp64).
  * Matrices as for the linear layers; dim at most 32768 (more: XPIPE_EUNSUPPORTED);
  * eps > 0; rows >= 0 (0: nothing is done).  y and sum may each be x's or residual's
  * buffer (same pointer and ld), dx may be dy's, h's or residual's; outputs must not

@@ -193,7 +193,7 @@ __global__ __launch_bounds__(THREADS<G>) void k_rms_fwd(RmsArgs a) {
 }
 
 // One workgroup's rows: their dx, and its part of grad_w: the sum of its rows' terms in
-// fp32 (at most a few hundred of them), over the ROWS rows at a time in LDS.  The parts
+// fp32 (MOST_TERMS of them a thread at most: more rows are another launch), over the ROWS rows at a time in LDS.  The parts
 // are added in fp64 by k_rms_join; a single workgroup adds its own.  The next row's
 // h and dy are on their way while this one's sums are joined.
 // Bound by the bytes of large calls (16384x4096 bf16: 87 us, 4.6 TB/s for h, dy and dx) and by the two launches of
@@ -290,14 +290,14 @@ __global__ __launch_bounds__(THREADS<G>) void k_rms_bwd(RmsArgs a) {
 }
 
 // grad[c] += sum of n parts, 16 columns and 16 runs of parts a workgroup
-__global__ __launch_bounds__(256) void k_rms_join(const float* __restrict__ part, int n, int dim, float* __restrict__ grad) {
+__global__ __launch_bounds__(256) void k_rms_join(const float* __restrict__ part, int64_t n, int dim, float* __restrict__ grad) {
   __shared__ double sh[16][17];
   const int c = threadIdx.x & 15, r = threadIdx.x >> 4;
   const int col = blockIdx.x * 16 + c;
   double s = 0.0;
   if (col < dim) {
 #pragma unroll 8
-    for (int i = r; i < n; i += 16) s += (double)part[(int64_t)i * dim + col];
+    for (int64_t i = r; i < n; i += 16) s += (double)part[i * dim + col];
   }
   sh[r][c] = s;
   __syncthreads();
@@ -329,6 +329,15 @@ void by_size(int dim, F&& f) {
 // 99.3, 110; four: 53.9, 107, 132).
 template <int G>
 int bwd_blocks(int64_t rows) { return (int)std::min<int64_t>((rows + ROWS<G> - 1) / ROWS<G>, G >= 1024 ? 256 : 512); }
+// Rows of a launch, and the parts of grad_w that all launches leave.
+constexpr int MOST_TERMS = 256;
+template <int G>
+constexpr int64_t LAUNCH_ROWS = (int64_t)(G >= 1024 ? 256 : 512) * ROWS<G> * MOST_TERMS;
+template <int G>
+int64_t bwd_parts(int64_t rows) {
+  const int last = bwd_blocks<G>(rows % LAUNCH_ROWS<G>);  // (a single workgroup adds its own)
+  return rows / LAUNCH_ROWS<G> * bwd_blocks<G>(LAUNCH_ROWS<G>) + (last > 1 ? last : 0);
+}
 
 template <typename T>
 hipError_t fwd(const RmsArgs& a, hipStream_t s) {
@@ -345,15 +354,26 @@ hipError_t fwd(const RmsArgs& a, hipStream_t s) {
 
 template <typename T>
 hipError_t bwd(RmsArgs a, void* workspace, hipStream_t s) {
-  a.part = (float*)workspace;
+  const auto from = [](const void* p, int64_t row, int64_t ld) { return p ? (char*)p + row * ld * (int64_t)sizeof(T) : nullptr; };
   by_size(a.dim, [&](auto G, auto E) {
     constexpr int g = decltype(G)::value, e = decltype(E)::value;
-    const int blocks = bwd_blocks<g>(a.rows);
-    const double bytes = (double)sizeof(T) * a.rows * a.dim * (2 + (a.y != nullptr) + (a.res != nullptr));
-    XP_LAUNCH(sizeof(T) == 2 ? "k_rms_bwd<bf16>" : "k_rms_bwd<f32>", bytes, (k_rms_bwd<T, g, e>), dim3(blocks),
-              dim3(THREADS<g>), 0, s, a);
-    if (a.grad && blocks > 1)
-      XP_LAUNCH("k_rms_join", 4.0 * blocks * a.dim, k_rms_join, dim3((a.dim + 15) / 16), dim3(256), 0, s, a.part, blocks, a.dim, a.grad);
+    int64_t parts = 0;
+    for (int64_t row = 0; row < a.rows; row += LAUNCH_ROWS<g>) {
+      RmsArgs b = a;
+      b.rows = std::min(a.rows - row, LAUNCH_ROWS<g>);
+      b.dy = from(a.dy, row, a.lddy);
+      b.x = from(a.x, row, a.ldx);
+      b.res = from(a.res, row, a.ldr);
+      b.y = from(a.y, row, a.ldy);
+      b.part = (float*)workspace + parts * a.dim;
+      const int blocks = bwd_blocks<g>(b.rows);
+      const double bytes = (double)sizeof(T) * b.rows * a.dim * (2 + (a.y != nullptr) + (a.res != nullptr));
+      XP_LAUNCH(sizeof(T) == 2 ? "k_rms_bwd<bf16>" : "k_rms_bwd<f32>", bytes, (k_rms_bwd<T, g, e>), dim3(blocks),
+                dim3(THREADS<g>), 0, s, b);
+      if (blocks > 1) parts += blocks;
+    }
+    if (a.grad && parts > 0)
+      XP_LAUNCH("k_rms_join", 4.0 * parts * a.dim, k_rms_join, dim3((a.dim + 15) / 16), dim3(256), 0, s, (const float*)workspace, parts, a.dim, a.grad);
   });
   return hipGetLastError();
 }
@@ -366,10 +386,7 @@ hipError_t launch_rms_fwd(int dtype, const RmsArgs& a, hipStream_t s) {
 
 size_t rms_bwd_bytes(int64_t rows, int dim) {
   size_t n = 0;
-  by_size(dim, [&](auto G, auto) {
-    const int blocks = bwd_blocks<decltype(G)::value>(rows);
-    n = blocks > 1 ? (size_t)blocks * dim * sizeof(float) : 0;
-  });
+  by_size(dim, [&](auto G, auto) { n = (size_t)bwd_parts<decltype(G)::value>(rows) * dim * sizeof(float); });
   return n;
 }
 

@@ -62,6 +62,43 @@ def test_norm_of_more_rows_than_a_launch_has_workgroups():
     torch.cuda.empty_cache()
 
 
+def test_norm_weight_gradient_of_many_rows():
+    """2^21 rows whose first 2048 are 2^24 times as large as the others: each fp32 sum that begins with one of them loses every
+    term that follows, so the gradient is off by about its number of terms over 2^24, 256 + 20 at most."""
+    torch = _torch()
+    rows, dim, large = 1 << 21, 600, 2048
+    h = torch.ones(rows, dim, dtype=torch.bfloat16, device="cuda")
+    dy = torch.ones_like(h)
+    dy[:large] = 2.0 ** 24
+    gw = torch.zeros(dim, device="cuda")
+    xp.xpipe_rmsnorm_bwd(dy, h, torch.ones(dim, device="cuda"), None, gw, eps=1e-12)
+    want = torch.full((dim,), large * 2.0 ** 24 + rows - large, dtype=torch.float64)
+    _close(gw, want, (256 + 20) * E24 * want, "grad_weight")
+
+
+@pytest.mark.parametrize("rows,dim", [((1 << 19) + 1, 520), ((1 << 17) + 700, 2100), ((1 << 16) + 1, 8200)])
+def test_norm_gradients_of_more_rows_than_a_launch_takes(rows, dim):
+    """The rows of a second launch: their dx are those of a call of their own, and grad_weight has all rows' terms."""
+    torch = _torch()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(rows)
+    make = lambda scale: (torch.randn(rows, dim, generator=g, device="cuda") * scale).bfloat16()
+    dy, h, r, w = make(0.1), make(2.0), make(0.1), 1 + 0.1 * torch.randn(dim, generator=g, device="cuda")
+    dx, gw = torch.empty_like(dy), torch.ones(dim, device="cuda")
+    xp.xpipe_rmsnorm_bwd(dy, h, w, dx, gw, eps=1e-5, residual=r)
+    for part in (slice(0, 300), slice(rows - 1000, rows)):
+        alone = torch.empty_like(dx[part])
+        xp.xpipe_rmsnorm_bwd(dy[part], h[part], w, alone, None, eps=1e-5, residual=r[part])
+        assert torch.equal(dx[part], alone)
+    want, size = torch.ones(dim, dtype=torch.float64, device="cuda"), torch.ones(dim, dtype=torch.float64, device="cuda")
+    for i in range(0, rows, 1 << 15):
+        h64 = h[i:i + (1 << 15)].double()
+        terms = dy[i:i + (1 << 15)].double() * h64 / (h64.square().mean(1, keepdim=True) + 1e-5).sqrt()
+        want += terms.sum(0)
+        size += terms.abs().sum(0)
+    _close(gw, _d(want), (256 + 20) * E24 * _d(size), "grad_weight")
+
+
 # ---------------------------------------------------------------- attention: capped scores
 def _scores(q, cap, **more):
     """The scores of rows q [n] of one column with one key of 1, as the statistics hold them: their log2(e) multiples."""
