@@ -625,7 +625,7 @@ typedef struct {
   const int32_t* k_len;                  /* [batch], or NULL: nk */
   const int32_t* prefix;                 /* [batch], or NULL; needs causal */
   const int32_t* q_doc;                  /* [batch][nq], or NULL */
-  const int32_t* k_doc;                  /* [batch][nk]; both or none */
+  const int32_t* k_doc;                  /* [batch][nk]; both or none (where batch, nq or nk is 0 either may be NULL) */
   const float* bias;                     /* [heads][2 bias_range + 1], or NULL */
 } xpipe_attention_inputs;
 typedef struct {

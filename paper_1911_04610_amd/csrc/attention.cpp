@@ -54,7 +54,9 @@ xpipe_status check_inputs(const xpipe_attention_inputs& q, AttnArgs* a) {
   if (q.batch > 65535) return fail(XPIPE_EUNSUPPORTED, "more than 65535 sequences");
   if (q.heads > 65535) return fail(XPIPE_EUNSUPPORTED, "more than 65535 heads");
   if (q.prefix && !q.causal) return fail(XPIPE_EINVAL, "prefix without causal");
-  if ((q.q_doc != nullptr) != (q.k_doc != nullptr)) return fail(XPIPE_EINVAL, "q_doc without k_doc, or k_doc without q_doc");
+  // (documents of nothing may be null; no pair is left to hide then)
+  const bool pairs = (int64_t)q.batch * q.nq > 0 && (int64_t)q.batch * q.nk > 0;
+  if (pairs && (q.q_doc != nullptr) != (q.k_doc != nullptr)) return fail(XPIPE_EINVAL, "q_doc without k_doc, or k_doc without q_doc");
   if (q.bias && q.bias_range < 1) return fail(XPIPE_EINVAL, "bias_range must be >= 1");
   if (q.bias && q.bias_range > 1 << 20) return fail(XPIPE_EUNSUPPORTED, "bias_range beyond 2^20");
   for (const void* p : {(const void*)q.q_len, (const void*)q.k_len, (const void*)q.prefix, (const void*)q.q_doc, (const void*)q.k_doc,
@@ -80,8 +82,8 @@ xpipe_status check_inputs(const xpipe_attention_inputs& q, AttnArgs* a) {
   a->q_len = q.q_len;
   a->k_len = q.k_len;
   a->prefix = q.prefix;
-  a->q_doc = q.q_doc;
-  a->k_doc = q.k_doc;
+  a->q_doc = pairs ? q.q_doc : nullptr;
+  a->k_doc = pairs ? q.k_doc : nullptr;
   a->bias = q.bias;
   return XPIPE_OK;
 }

@@ -149,3 +149,19 @@ def test_capped_scores_do_not_depend_on_their_neighbours(dtype):
 def test_a_cap_that_never_binds(shape, reach, dtype):
     """Under a cap of 1e6 scores below 50 are themselves to 1e-9: results and gradients within the bounds of no cap."""
     Case(*shape, dtype, mask="causal", reach=reach).check(cap=1e6)
+
+
+# ---------------------------------------------------------------- attention: documents
+def test_attention_of_documents_of_nothing():
+    """Queries with documents over no keys, and keys with documents and no queries: zeros, in every result."""
+    torch = _torch()
+    full = lambda *s: torch.full(s, 7.0, device="cuda")
+    docs = lambda n: torch.zeros(2, n, dtype=torch.int32, device="cuda")
+    for nq, nk in ((5, 0), (200, 0), (0, 5)):
+        q, kv, o, st, bias = full(2, nq, 2, 8), full(2, nk, 1, 8), full(2, nq, 2, 8), full(2, 2, nq, 2), torch.ones(2, 9, device="cuda")
+        how = dict(q_doc=docs(nq), k_doc=docs(nk), bias=bias, causal=True)
+        xp.xpipe_attention_fwd(q, kv, kv, o, stats=st, **how)
+        assert bool(o.eq(0).all()) and bool(st[..., 0].eq(-math.inf).all()) and bool(st[..., 1].eq(0).all())
+        dq, dk, dv, gb = full(2, nq, 2, 8), full(2, nk, 1, 8), full(2, nk, 1, 8), torch.ones(2, 9, device="cuda")
+        xp.xpipe_attention_bwd(full(2, nq, 2, 8), q, kv, kv, o, st, dq, dk, dv, gb, **how)
+        assert bool(dq.eq(0).all()) and bool(dk.eq(0).all()) and bool(dv.eq(0).all()) and bool(gb.eq(1).all())

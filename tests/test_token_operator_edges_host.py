@@ -15,3 +15,27 @@ def test_norm_weight_gradient_has_a_part_for_every_256_rows_of_a_thread(rows, di
     need = ctypes.c_size_t()
     assert xp.lib().xpipe_rmsnorm_bwd_query(ctypes.byref(a), ctypes.byref(need)) == xp.OK
     assert need.value >= rows // (256 * shared) * dim * 4
+
+
+def _attention(nq, nk, q_doc, k_doc):
+    """The queries of a forward and a backward call over 2 sequences."""
+    none, some = xp.Heads(None, 0, 0, 0), lambda p, n: xp.Heads(p * P, n * 128, 128, 64)
+    q, k = (some(1, nq) if nq else none), (some(2, nk) if nk else none)
+    f, b, need, got = xp.AttentionFwdArgs(), xp.AttentionBwdArgs(), ctypes.c_size_t(), []
+    for a in (f, b):
+        i = a.in_
+        i.batch, i.nq, i.nk, i.heads, i.kv_heads, i.head_dim, i.dtype, i.scale = 2, nq, nk, 2, 2, 64, xp.BF16, 0.125
+        i.q, i.k, i.v, i.q_doc, i.k_doc = q, k, some(3, nk) if nk else none, q_doc, k_doc
+        a.o = some(4, nq) if nq else none
+    b.dout, b.dq, b.dk, b.dv = (some(p, n) if n else none for p, n in ((5, nq), (6, nq), (7, nk), (8, nk)))
+    b.stats = 9 * P if nq else None
+    L = xp.lib()
+    return L.xpipe_attention_fwd_query(ctypes.byref(f), ctypes.byref(need)), L.xpipe_attention_bwd_query(ctypes.byref(b), ctypes.byref(need))
+
+
+def test_documents_of_nothing_may_be_null():
+    """An empty tensor has no address: where one side is empty, documents of the other alone are no mistake."""
+    ok = (xp.OK, xp.OK)
+    assert _attention(5, 0, 10 * P, None) == ok and _attention(0, 5, None, 10 * P) == ok and _attention(0, 0, None, None) == ok
+    assert _attention(5, 0, 10 * P, 11 * P) == ok and _attention(5, 6, 10 * P, 11 * P) == ok
+    assert _attention(5, 6, 10 * P, None) == _attention(5, 6, None, 10 * P) == (xp.EINVAL, xp.EINVAL)
