@@ -1256,7 +1256,10 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dkv(AttnArgs a) {
     for (int h = h0; h < h1; ++h) {
       const int64_t w = ((int64_t)b * a.heads + h) * wblocks + wblock;
       for (int n = n0; n < n1; ++n) a.diag[(w * a.near + n) * 64 + lane] = 0.f;
-      if (lane < 2) a.tail[2 * (w * a.q_parts + q_part) + lane] = 0.f;
+      if (lane == 0) {  // (the lane that writes them again at the head's end)
+        a.tail[2 * (w * a.q_parts + q_part)] = 0.f;
+        a.tail[2 * (w * a.q_parts + q_part) + 1] = 0.f;
+      }
     }
   }
 

@@ -165,3 +165,15 @@ def test_attention_of_documents_of_nothing():
         dq, dk, dv, gb = full(2, nq, 2, 8), full(2, nk, 1, 8), full(2, nk, 1, 8), torch.ones(2, 9, device="cuda")
         xp.xpipe_attention_bwd(full(2, nq, 2, 8), q, kv, kv, o, st, dq, dk, dv, gb, **how)
         assert bool(dq.eq(0).all()) and bool(dk.eq(0).all()) and bool(dv.eq(0).all()) and bool(gb.eq(1).all())
+
+
+# ---------------------------------------------------------------- attention: results that meet in memory
+@pytest.mark.parametrize("docs", [False, True])
+def test_far_distances_of_heads_that_share_keys(docs):
+    """Bias gradients that are almost all beyond the range: sums that a wave clears first and writes at each head's end."""
+    torch = _torch()
+    c = Case(2, 300, 300, 8, 2, 64, "f32", mask="causal", reach=1, docs=docs)
+    c.check()
+    o, stats = c.forward()
+    first = c.backward(o, stats)[3]
+    assert all(torch.equal(first, c.backward(o, stats)[3]) for _ in range(5))
