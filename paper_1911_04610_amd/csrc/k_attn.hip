@@ -321,6 +321,12 @@ XP_DEV void st_column(T* row, int dim, const f32x16_t (&acc)[DP / 32], float f) 
 }
 
 // ---------------------------------------------------------------- halves and waves
+// What the wave's lanes stored in LDS before, its other lanes read behind this line, and the other way round.  (One
+// wave alone: its LDS operations run in order, so this is for the compiler and costs nothing.)
+XP_DEV void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
 // the larger, and the sum, of a value in lanes l and l ^ 32
 XP_DEV float both_max(float v) {
   const auto u = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -828,6 +834,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_few(AttnArgs a) {
     ks.store(tile);
     vs.store(tile + TILE);
     if (kdoc && lane < 32) sdoc[wave][lane] = dreg;
+    wave_fence();
     const int next = t + 1;
     if (next < end) load(next);
     const int j0 = t * 32;
@@ -848,6 +855,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_few(AttnArgs a) {
       l += p[r];
     }
     add_transposed<T, DP>(acc, cplace, TILE, p, a.ldim);
+    wave_fence();
   }
   if (in) write_rows<T, DP, MODE>(a, b, head, i, a.splits > 0 ? few_part(a, kvh, blk, group * 4 + wave, lane & 31) : -1, kend, m, base, l, acc);
 }

@@ -177,3 +177,14 @@ def test_far_distances_of_heads_that_share_keys(docs):
     o, stats = c.forward()
     first = c.backward(o, stats)[3]
     assert all(torch.equal(first, c.backward(o, stats)[3]) for _ in range(5))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("docs", [False, True])
+def test_few_queries_over_steps_of_one_wave(docs, dtype):
+    """19 steps of the keys through a wave's own LDS, in as many waves as sequences and heads: within the bounds, and the same bits each time."""
+    torch = _torch()
+    c = Case(4, 1, 600, 512, 512, 8, dtype, mask="causal", ragged=True, docs=docs)
+    c.check(train=False)
+    first = c.forward()[0]
+    assert all(torch.equal(first, c.forward()[0]) for _ in range(5))
