@@ -534,7 +534,7 @@ xpipe_status xpipe_embedding_bwd(const void* dy, const int32_t* tokens, int64_t 
  * depend on its own values alone, and the order of grad_weight's sum on the sizes alone (at
  * most 256 rows' terms, and 32 such sums, are added in fp32, the rest in fp64).
  * Matrices as for the linear layers; dim at most 32768 (more: XPIPE_EUNSUPPORTED);
- * eps > 0; rows >= 0 (0: nothing is done).  y and sum may each be x's or residual's
+ * eps at least 2^-252; rows >= 0 (0: nothing is done).  y and sum may each be x's or residual's
  * buffer (same pointer and ld), dx may be dy's, h's or residual's; outputs must not
  * overlap inputs otherwise, nor one another. */
 typedef struct {

@@ -165,6 +165,7 @@ xpipe_status check_rms(int64_t rows, int32_t dim, int32_t dtype, double eps, con
   if (rows < 0 || dim < 1) return fail(XPIPE_EINVAL, "rows must be >= 0, dim >= 1");
   if (!known_dtype(dtype)) return fail(XPIPE_EINVAL, "unknown dtype");
   if (!(eps > 0) || !std::isfinite(eps)) return fail(XPIPE_EINVAL, "eps must be > 0 and finite");
+  if (eps < 0x1p-252) return fail(XPIPE_EINVAL, "eps must be at least 2^-252");  // (the norm of a zero row, 1 / sqrt(eps), is fp32)
   if (dim > RMS_MAX_DIM || rows >= (int64_t)1 << 40) return fail(XPIPE_EUNSUPPORTED, "more than 32768 columns, or 2^40 rows or more");
   if (rows == 0) return XPIPE_OK;
   if (!weight) return fail(XPIPE_EINVAL, "null weight");

@@ -99,6 +99,18 @@ def test_norm_gradients_of_more_rows_than_a_launch_takes(rows, dim):
     _close(gw, _d(want), (256 + 20) * E24 * _d(size), "grad_weight")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_norm_of_zero_rows_under_the_least_epsilon(dtype):
+    """n = 2^126: y is 0 and dx 2^126 dy, exactly."""
+    torch = _torch()
+    for dim in (40, 700, 9000):
+        x, w = torch.zeros(3, dim, dtype=_dt(dtype), device="cuda"), torch.ones(dim, device="cuda")
+        dy, y, dx, gw = torch.full_like(x, 1.5), torch.full_like(x, 7.0), torch.full_like(x, 7.0), torch.zeros(dim, device="cuda")
+        xp.xpipe_rmsnorm_fwd(x, w, y, eps=2.0 ** -252)
+        xp.xpipe_rmsnorm_bwd(dy, x, w, dx, gw, eps=2.0 ** -252)
+        assert bool(y.eq(0).all()) and bool(dx.float().eq(1.5 * 2.0 ** 126).all()) and bool(gw.eq(0).all())
+
+
 # ---------------------------------------------------------------- attention: capped scores
 def _scores(q, cap, **more):
     """The scores of rows q [n] of one column with one key of 1, as the statistics hold them: their log2(e) multiples."""

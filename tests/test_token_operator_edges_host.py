@@ -17,6 +17,17 @@ def test_norm_weight_gradient_has_a_part_for_every_256_rows_of_a_thread(rows, di
     assert need.value >= rows // (256 * shared) * dim * 4
 
 
+def test_norm_epsilon_whose_root_leaves_fp32():
+    """A zero row's n is 1 / sqrt(eps): infinite in fp32 it would make 0 n a NaN."""
+    L, need = xp.lib(), ctypes.c_size_t()
+    for eps, status in ((2.0 ** -252, xp.OK), (2.0 ** -253, xp.EINVAL), (1e-300, xp.EINVAL), (5e-324, xp.EINVAL)):
+        a = xp.RmsnormFwdArgs(rows=4, dim=64, dtype=xp.F32, eps=eps, x=P, ldx=64, weight=2 * P, y=3 * P, ldy=64)
+        if status != xp.OK:
+            assert L.xpipe_rmsnorm_fwd(ctypes.byref(a), None) == status
+        b = xp.RmsnormBwdArgs(rows=4, dim=64, dtype=xp.F32, eps=eps, dy=P, lddy=64, h=2 * P, ldh=64, weight=3 * P, dx=4 * P, lddx=64)
+        assert L.xpipe_rmsnorm_bwd_query(ctypes.byref(b), ctypes.byref(need)) == status
+
+
 def _attention(nq, nk, q_doc, k_doc):
     """The queries of a forward and a backward call over 2 sequences."""
     none, some = xp.Heads(None, 0, 0, 0), lambda p, n: xp.Heads(p * P, n * 128, 128, 64)
