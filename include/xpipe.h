@@ -601,8 +601,8 @@ xpipe_status xpipe_relbias_bwd(const float* dbias, int32_t buckets, int32_t head
  * whatever they hold.  (Another value that is not finite can also reach rows that do not see it,
  * those of the same tile: 0 times it is a NaN.)  A -inf in bias masks; a row of which every score is -inf sees nothing.
  * Types: as the linear layers' (products with fp32 sums; in XPIPE_BF16 P and the score
- * gradients are rounded to bf16 as operands of the second products, for dq over few keys
- * (documents, or nk up to 2048) to two bf16 values); scores, maxima and
+ * gradients are rounded to bf16 as operands of the second products, to two bf16 values P for few queries (nq heads /
+ * kv_heads up to 64) and the score gradients for dq over few keys (documents, or nk up to 2048)); scores, maxima and
  * sums are fp32, a capped score good to a few 2^-24 of itself (in XPIPE_BF16 without a bias and up to a cap of 64: of
  * the cap), and the order of the sums follows from the sizes and lengths alone.
  * Layout: [batch][token][head][head_dim], contiguous only in head_dim, aligned to their

@@ -14,7 +14,10 @@
 // whatever belongs to a query (maximum, sum, limits) is one value a lane.
 //
 // In bf16 storage P and dX are rounded to bf16 for the second products, as every operand of
-// a bf16 product is; scores, sums and statistics are fp32 throughout.
+// a bf16 product is; scores, sums and statistics are fp32 throughout.  That leaves results 2.0e-3 (o) to 2.4e-3 (gradients) of
+// their 2-norm off where their own rounding alone is 1.66e-3.  P and dX as two bf16 values everywhere reach that, for half
+// of the products again: 16 heads of 8192 tokens, causal and capped, 493 us for 370; 2 x 4096 tokens, prefix, training
+// step 1168 for 860.  Two values are taken where they cost little: in k_attn_few, and of dX in k_attn_dq over few keys.
 #include "xp_device.h"
 #include "xp_lds.h"
 #include "xp_kernels.h"
@@ -773,8 +776,8 @@ XP_DEV int64_t few_part(const AttnArgs& a, int kvh, int blk, int wave, int row) 
 // time through LDS of its own, the next 32 on their way: four times the bytes in flight
 // that the workgroups of k_attn_fwd have, whose other waves would have no rows.  Short
 // sequences (splits 0): all of the keys, four waves being four blocks of rows.
-// Bound by the keys' and values' bytes: 8 sequences of 32768 tokens, 8 heads of 128, 5.6 TB/s,
-// what a copy reaches.
+// Bound by the keys' and values' bytes (5.2 TB/s, what a copy reaches), so P is two bf16 values: 8 sequences of up to 32768
+// tokens, 8 heads of 128, 151.4 us for 150.0, and o 1.66e-3 of its 2-norm off, which is its own rounding, for 2.3e-3.
 template <typename T, int DP, int MODE>
 __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_few(AttnArgs a) {
   constexpr int TILE = 32 * ROW<T, DP>;
@@ -854,7 +857,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_few(AttnArgs a) {
       p[r] = exp_of<MODE>(s[r], off, c1);
       l += p[r];
     }
-    add_transposed<T, DP>(acc, cplace, TILE, p, a.ldim);
+    add_transposed<T, DP, true>(acc, cplace, TILE, p, a.ldim);
     wave_fence();
   }
   if (in) write_rows<T, DP, MODE>(a, b, head, i, a.splits > 0 ? few_part(a, kvh, blk, group * 4 + wave, lane & 31) : -1, kend, m, base, l, acc);

@@ -200,3 +200,25 @@ def test_few_queries_over_steps_of_one_wave(docs, dtype):
     c.check(train=False)
     first = c.forward()[0]
     assert all(torch.equal(first, c.forward()[0]) for _ in range(5))
+
+
+# ---------------------------------------------------------------- attention: bits of P
+def _as_f32(c):
+    """The same call's values in fp32 storage: its bounds leave no room for rounded operands."""
+    torch = _torch()
+    d = Case.__new__(Case)
+    d.__dict__.update(c.__dict__, dtype="f32", **{n: getattr(c, n).float() for n in ("q", "k", "v", "do")})
+    return d
+
+
+@pytest.mark.parametrize("cap,reach", [(0.0, 0), (20.0, 30)])
+@pytest.mark.parametrize("shape", [(2, 1, 3000, 8, 2, 128), (1, 4, 900, 8, 1, 64), (40, 1, 200, 64, 64, 96), (3, 1, 40, 4, 4, 33)])
+def test_few_queries_keep_16_bits_of_p(shape, cap, reach):
+    """bf16 storage: within the bounds of fp32 products, o's own rounding, and 2^-16 of P (two bf16 values, the second
+    of what the first leaves)."""
+    c = Case(*shape, "bf16", mask="causal", cap=cap, reach=reach, ragged=True)
+    o, tol = _as_f32(c).exact()["o"]
+    size = _as_f32(c)
+    size.v = size.v.abs()
+    tol = tol + 2.0 ** -16 * size.exact()["o"][0]
+    _close(c.forward()[0].permute(0, 2, 1, 3), o, tol + 2.0 ** -8 * (o.abs() + tol), "o")
