@@ -6,6 +6,7 @@ import math
 import pytest
 
 import paper_1911_04610_amd as xp
+import test_gpu_token_operators as usual
 from test_gpu_token_operators import E24, Case, _close, _d, _dt, _gen, _half_step, _norm64, _torch
 
 pytestmark = pytest.mark.gpu
@@ -109,6 +110,67 @@ def test_norm_of_zero_rows_under_the_least_epsilon(dtype):
         xp.xpipe_rmsnorm_fwd(x, w, y, eps=2.0 ** -252)
         xp.xpipe_rmsnorm_bwd(dy, x, w, dx, gw, eps=2.0 ** -252)
         assert bool(y.eq(0).all()) and bool(dx.float().eq(1.5 * 2.0 ** 126).all()) and bool(gw.eq(0).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,dim", [(8200, 512), (65600, 40), (16390, 100), (8195, 200)])
+def test_norm_of_more_rows_than_workgroups(rows, dim, dtype):
+    """Forward: a workgroup's second round of rows."""
+    usual.test_norm_forward(rows, dim, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,dim", [(300, 9000), (270, 20000), (600, 6000), (20000, 40), (2100, 1500)])
+def test_norm_gradients_of_more_rows_than_workgroups(rows, dim, dtype):
+    usual.test_norm_backward(rows, dim, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dim", [40, 300, 2047, 4099, 9000, 20000])
+def test_norm_extremes_in_every_type_and_width(dim, dtype):
+    """Rows whose squares leave fp32 on either side and zero rows, among ordinary ones; values that are not finite stay in their row."""
+    torch = _torch()
+    u, g = _half_step(dtype), _gen(dim)
+    x, w = torch.randn(11, dim, generator=g), (1 + 0.1 * torch.randn(dim, generator=g)).cuda()
+    for row, by in ((1, 1e25), (2, 1e-30), (3, 0.0), (6, 1e18), (7, 1e-12)):
+        x[row] *= by
+    x[4, dim // 3], x[9, dim - 1] = math.nan, math.inf
+    x, keep = x.to(_dt(dtype)).cuda(), torch.tensor([0, 1, 2, 3, 5, 6, 7, 8, 10])
+    y = torch.full_like(x, 7.0)
+    xp.xpipe_rmsnorm_fwd(x, w, y, eps=1e-30)
+    _, want = _norm64(_d(x)[keep], _d(w), 1e-30)
+    _close(_d(y)[keep], want, 8 * E24 * want.abs() * (1 + u) + u * want.abs(), "y")
+    assert bool(y[3].eq(0).all()) and bool(y[4].isnan().all()) and bool(y[9, dim - 1].isnan())
+    dy = torch.randn(11, dim, generator=g).to(_dt(dtype)).cuda()
+    _check_norm_backward(dy[keep.cuda()], x[keep.cuda()], w, 1e-10, dtype)
+    dx = torch.full_like(x, 7.0)
+    xp.xpipe_rmsnorm_bwd(dy, x, w, dx, None, eps=1e-10)
+    assert bool(_d(dx)[keep].isfinite().all()) and bool(dx[4].isnan().all()) and bool(dx[9].isnan().any())
+
+
+# ---------------------------------------------------------------- relative position bias
+@pytest.mark.parametrize("buckets,heads,far,both", [(64, 5, 4097, False), (32, 3, 4097, True), (64, 64, 32768, False), (64, 2, 32768, True), (5, 1, 9999, False),
+                                                    (128, 2, 1 << 17, True)])
+def test_relative_bias_over_long_distances(buckets, heads, far, both):
+    """grad_table: 300 additions in fp64 one after another and in halves, and as many as distances in the sum that it is held to."""
+    torch = _torch()
+    n = buckets // 2 if both else buckets
+    half, m, one = n // 2, n - n // 2, []
+    for a in range(far + 1):  # (whole numbers; a bucket's first distance is never before the last bucket's)
+        k = one[-1] if one else 0
+        while k + 1 < n and (a > k if k + 1 <= half else a ** m * half ** (k + 1 - half) >= far ** (k + 1 - half) * half ** m):
+            k += 1
+        one.append(k)
+    at = torch.tensor([one[-d] if d <= 0 else one[d] + n if both else 0 for d in range(-far, far + 1)])
+    g = _gen(far + buckets)
+    table, dbias, grad = torch.randn(buckets, heads, generator=g), torch.randn(heads, 2 * far + 1, generator=g), torch.randn(buckets, heads, generator=g)
+    bias, got = torch.full((heads, 2 * far + 1), 7.0, device="cuda"), grad.cuda()
+    xp.xpipe_relbias_fwd(table.cuda(), bias, bidirectional=both)
+    assert torch.equal(bias.cpu(), table[at].t())
+    xp.xpipe_relbias_bwd(dbias.cuda(), got, bidirectional=both)
+    want = grad.double().index_add(0, at, dbias.t().double())
+    size = grad.double().abs().index_add(0, at, dbias.t().double().abs())
+    _close(got, want, E24 * want.abs() + (2 * far + 300) * 2.0 ** -53 * size, "grad_table")
 
 
 # ---------------------------------------------------------------- attention: capped scores
@@ -222,3 +284,31 @@ def test_few_queries_keep_16_bits_of_p(shape, cap, reach):
     size.v = size.v.abs()
     tol = tol + 2.0 ** -16 * size.exact()["o"][0]
     _close(c.forward()[0].permute(0, 2, 1, 3), o, tol + 2.0 ** -8 * (o.abs() + tol), "o")
+
+
+# ---------------------------------------------------------------- attention: far apart in memory
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("odd", [0, 1])
+def test_attention_long_offsets_in_training(odd, dtype):
+    """Rows of every input and output more than 2^31 elements apart give the bits of neighbours (odd: rows that are copied first)."""
+    torch = _torch()
+    n, H, D, stride = 1040, 2, 64, (1 << 21) + odd
+    buf = torch.empty(n * stride, dtype=_dt(dtype), device="cuda")
+    far = lambda slot: buf.as_strided((1, n, H, D), (0, stride, D, 1), slot * 1024)
+    g = _gen(3 + odd)
+    near = [torch.randn(1, n, H, D, generator=g).to(_dt(dtype)).cuda() for _ in range(4)]
+    bias = torch.randn(H, 41, generator=g).cuda()
+    how = dict(causal=True, bias=bias)
+
+    def both(q, k, v, do, o, dq, dk, dv):
+        stats, gb = torch.empty(1, H, n, 2, device="cuda"), torch.zeros_like(bias)
+        xp.xpipe_attention_fwd(q, k, v, o, stats=stats, **how)
+        xp.xpipe_attention_bwd(do, q, k, v, o, stats, dq, dk, dv, gb, **how)
+        return [o, dq, dk, dv, stats, gb]
+    want = both(*near, *[torch.empty_like(near[0]) for _ in range(4)])
+    places = [far(i) for i in range(8)]
+    for to, t in zip(places, near):
+        to.copy_(t)
+    got = both(*places)
+    for a, b, name in zip(want, got, ("o", "dq", "dk", "dv", "stats", "grad_bias")):
+        assert torch.equal(a, b), name
