@@ -450,7 +450,8 @@ XP_DEV void hide_others(V& s, const int* docs, int doc, float none) {
 //   CAP    cap tanh(scale q.k / cap)
 //   BIAS   scale q.k plus a bias
 //   BOTH   CAP plus a bias
-enum { PLAIN = 0, CAP = 1, BIAS = 2, BOTH = 3 };
+//   QUICK  CAP, bf16 storage and a cap up to QUICK_CAP
+enum { PLAIN = 0, CAP = 1, BIAS = 2, BOTH = 3, QUICK = 5 };
 constexpr bool has_cap(int mode) { return mode & CAP; }
 constexpr bool has_bias(int mode) { return mode & BIAS; }
 // exp(score - base); c1: as above
@@ -468,12 +469,13 @@ XP_DEV float log2_of(float d, float c1) { return MODE == PLAIN ? d * c1 : d; }
 // cap is: below SMALL from tanh(x) / x = 1 + x^2 p(x^2), p of degree 3 with the least relative error over that
 // range (2^-26), times scale q.k, so that a large cap costs no bits; beyond it 1 - 2 q with q = 1 / (1 + exp(2 x)), and
 // the slope 4 q (1 - q), off by 2^-22 of 1.  Which of them a score takes depends on itself alone; a block none of whose
-// scores is beyond SMALL passes the exponentials over (BOTH_WAYS, where the keys' bytes bound: none does, for fewer registers).
-// In bf16 storage, without a bias (whose gradient is fp32) and up to a cap of QUICK_CAP 1 - 2 q alone: the scores are off by
-// 12 * 2^-24 of the cap then, 2^-14 at most, where P itself is rounded by 2^-8.  (16 heads of 8192 tokens, causal, scores
-// of 1: cap 50 404 us, 409 with the polynomial; cap 1, where half of the scores are beyond SMALL, 390 and 552.)
+// scores is beyond SMALL passes the exponentials over (BOTH_WAYS, in the forward where the
+// keys' bytes or the fp32 products bound: none does, for fewer registers).
+// QUICK has 1 - 2 q alone: its scores are off by 12 * 2^-24 of the cap, 2^-14 at most, where P itself is rounded by 2^-8;
+// with a bias, whose gradient is fp32, there is no such kind.  (16 heads of 8192 tokens, causal, scores of 1: cap 50 404 us, 409 with
+// the polynomial; cap 1, where half of the scores are beyond SMALL, 390 and 552.)
 constexpr float SMALL = 0.5f, QUICK_CAP = 64.f;
-template <typename T, int MODE, bool SLOPE, bool BOTH_WAYS = false, typename F>
+template <int MODE, bool SLOPE, bool BOTH_WAYS, typename F>
 XP_DEV void scores(f32x16_t& s, const AttnArgs& a, float (&slope)[16], F&& at) {
   if constexpr (has_cap(MODE)) {
 #pragma clang fp contract(off)  // (the bits of a score do not depend on which way its block goes)
@@ -489,19 +491,21 @@ XP_DEV void scores(f32x16_t& s, const AttnArgs& a, float (&slope)[16], F&& at) {
       d = 4.f * fmaf(-q, q, q);
       return fmaf(-2.f * top, q, top);
     };
-    float most = 0.f;
-    const bool quick = sizeof(T) == 2 && MODE == CAP && !BOTH_WAYS && a.cap <= QUICK_CAP;
-    if (!quick)
+    bool any_large = true;
+    if constexpr (MODE != QUICK && !BOTH_WAYS) {
+      float most = 0.f;
 #pragma unroll
       for (int r = 0; r < 16; ++r) most = fmaxf(most, fabsf(s[r]));
-    if (quick) {
+      any_large = __any(most * k >= SMALL);
+    }
+    if constexpr (MODE == QUICK) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         float d;
         s[r] = large(s[r] * (2.f * LOG2E * k), d);
         if constexpr (SLOPE) slope[r] = d;
       }
-    } else if (BOTH_WAYS || __any(most * k >= SMALL)) {
+    } else if (any_large) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         float d, dl;
@@ -708,7 +712,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_fwd(AttnArgs a) {
         const float* mine = sbias[buf] + ROWS - 1 - (i - first) + 4 * (lane >> 5);
 #pragma unroll
         for (int n = 0; n < NB; ++n)
-          scores<T, MODE, false>(s[n], a, none, [&](int r) { return mine[n * 32 + 8 * (r >> 2) + (r & 3)]; });
+          scores<MODE, false, sizeof(T) == 4>(s[n], a, none, [&](int r) { return mine[n * 32 + 8 * (r >> 2) + (r & 3)]; });
       }
       if ((t + 1) * KEYS > wmin)
 #pragma unroll
@@ -845,7 +849,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_few(AttnArgs a) {
     if constexpr (MODE != PLAIN) {
       float none[16];
       const int d0 = j0 - i - seq.off;
-      scores<T, MODE, false, true>(s, a, none, [&](int r) { return log2_bias(bias[min(max(d0 + row_of(r), -a.range), a.range)]); });
+      scores<MODE, false, true>(s, a, none, [&](int r) { return log2_bias(bias[min(max(d0 + row_of(r), -a.range), a.range)]); });
     }
     if (j0 + 32 > kmin || blk == blocks - 1) hide_from(s, kend - j0, NEG_INF);
     if (kdoc) hide_others(s, sdoc[wave], doc, NEG_INF);
@@ -935,7 +939,7 @@ XP_DEV RowStat row_stat(float m, float l) {
 template <int MODE>
 XP_DEV float weight(float s, float a, float b, float c1) {
   if constexpr (MODE == PLAIN) return exp2_(s * c1 - a);
-  else if constexpr (MODE == CAP) return exp2_(s - a);
+  else if constexpr (!has_bias(MODE)) return exp2_(s - a);
   else return exp2_((s - a) - b);
 }
 // What k_attn_dkv needs of 32 query rows: row.a, row.b, sum of P dP, kend, document, 32 each, and
@@ -1073,7 +1077,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dq(AttnArgs a) {
         float slope[16], ds[16];
         if constexpr (MODE != PLAIN) {
           const float* mine = sbias[buf] + ROWS - 1 - (wave * 32 + (lane & 31)) + 4 * (lane >> 5) + n * 32;
-          scores<T, MODE, true>(s, a, slope, [&](int r) { return mine[8 * (r >> 2) + (r & 3)]; });
+          scores<MODE, true, false>(s, a, slope, [&](int r) { return mine[8 * (r >> 2) + (r & 3)]; });
         }
 #pragma unroll
         for (int r = 0; r < 16; ++r) ds[r] = weight<MODE>(s[r], st.a, st.b, c1);
@@ -1328,7 +1332,7 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dkv(AttnArgs a) {
       float p[16], slope[16];
       if constexpr (MODE != PLAIN) {  // (register r's place in the window: key - query + QT - 1)
         const float* mine = sbias[buf] + (has_bias(MODE) ? (j - k0) + QT - 28 - 4 * (lane >> 5) - n * 32 : 0);
-        scores<T, MODE, (WHAT & 2) != 0>(s, a, slope, [&](int r) { return mine[27 - 8 * (r >> 2) - (r & 3)]; });
+        scores<MODE, (WHAT & 2) != 0, false>(s, a, slope, [&](int r) { return mine[27 - 8 * (r >> 2) - (r & 3)]; });
       }
       auto of = [&](int what, int r) __attribute__((always_inline)) { return srow[buf][n * (5 * 32) + what * 32 + row_of(r)]; };
 #pragma unroll
@@ -1669,8 +1673,12 @@ void by_kind(int dtype, const AttnArgs& a, F&& f) {
   auto with = [&](auto t, auto d) {
     if (a.bias && a.cap > 0.f) f(t, d, integral_constant<int, BOTH>{});
     else if (a.bias) f(t, d, integral_constant<int, BIAS>{});
-    else if (a.cap > 0.f) f(t, d, integral_constant<int, CAP>{});
-    else f(t, d, integral_constant<int, PLAIN>{});
+    else if (a.cap > 0.f) {
+      if constexpr (sizeof(t) == 2) {
+        if (a.cap <= QUICK_CAP) return f(t, d, integral_constant<int, QUICK>{});
+      }
+      f(t, d, integral_constant<int, CAP>{});
+    } else f(t, d, integral_constant<int, PLAIN>{});
   };
   auto dims = [&](auto t) {
     if (a.dim <= 64) with(t, integral_constant<int, 64>{});
