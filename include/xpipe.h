@@ -576,7 +576,7 @@ xpipe_status xpipe_rmsnorm_bwd(const xpipe_rmsnorm_bwd_args* args, void* workspa
  * for keys before the query, those after it counting as a = 0; with bidirectional != 0
  * half of them, the upper half for d > 0): a < n / 2 has its own, and further ones share
  * n / 2 + floor(log(a / (n / 2)) / log(max_distance / (n / 2)) (n - n / 2)), at most n - 1, a
- * distance on a border belonging to the bucket that begins there.  All buffers fp32,
+ * distance on a border (to 2^-44 of the quotient) belonging to the bucket that begins there.  All buffers fp32,
  * contiguous, not overlapping; n >= 2, max_distance > n / 2.  At most 1024 buckets, 4096
  * heads and a distance of 2^20 (more: XPIPE_EUNSUPPORTED).  Sums are fp64, in an order that
  * the sizes decide. */
@@ -607,8 +607,9 @@ xpipe_status xpipe_relbias_bwd(const float* dbias, int32_t buckets, int32_t head
  * the cap), and the order of the sums follows from the sizes and lengths alone.
  * Layout: [batch][token][head][head_dim], contiguous only in head_dim, aligned to their
  * element, strides in elements: >= 0 for inputs (0 shares them), and such that no two
- * elements fall together for outputs; the token's at most XPIPE_ATTENTION_MAX_STRIDE.
- * head_dim 1 .. 128, batch * heads * (nq / 128 + 1) and the same of keys below 2^23, nq and nk below 2^24,
+ * elements fall together for outputs (each at least as long as the shorter ones span); the token's at most
+ * XPIPE_ATTENTION_MAX_STRIDE, the others below 2^40.
+ * head_dim 1 .. 128, batch and heads at most 65535, batch * heads * (nq / 128 + 1) and the same of keys below 2^23, nq and nk below 2^24,
  * bias_range 1 .. 2^20 (beyond: XPIPE_EUNSUPPORTED).  Lengths outside 0 .. nq, 0 .. nk are taken as
  * the nearest of them.  Outputs must not overlap inputs nor one another. */
 #define XPIPE_ATTENTION_MAX_STRIDE ((int64_t)1 << 22)
@@ -619,7 +620,7 @@ typedef struct {
 typedef struct {
   int32_t batch, nq, nk, heads, kv_heads, head_dim, dtype;
   int32_t causal, bias_range;
-  double scale, cap;                     /* scale > 0; cap >= 0 */
+  double scale, cap;                     /* scale > 0; cap >= 0; 4 scale, 4 cap and 4 scale / cap finite in fp32 */
   xpipe_heads q, k, v;
   const int32_t* q_len;                  /* [batch] on the device, or NULL: nq */
   const int32_t* k_len;                  /* [batch], or NULL: nk */

@@ -610,11 +610,12 @@ XP_DEV void write_rows(const AttnArgs& a, int b, int head, int i, int64_t part, 
 }
 
 // One workgroup per 128 query rows of a head, and part of the keys.
-// Bound by the matrix units and the exponentials, which two waves a SIMD overlap in part only (a third would
-// need the queries' columns and o in 168 registers).  bf16, dim 128: 16 heads of 8192 tokens 640 us (860
-// Tflop/s), causal 298 us (920); capped and causal 389 us; 2 x 4096 tokens, 16 heads over 4 283 us (970).  dim 64: 2 x
-// 8192 tokens, 16 heads 660 us (830).  No LDS bank conflicts; matrix units busy for 30 % of the time
-// of the causal ones, prologue and uneven ends included.
+// Bound by the matrix units and the vector instructions, 512 cycles and some 690 for a block of 32 x 32 of dim 128 (125
+// instructions, 16 of them exponentials): a SIMD's waves (two; three for bf16 rows of 64 but with both cap and bias) hardly
+// overlap them.  bf16, dim 128: 16 heads of 8192 tokens 564 us (975 Tflop/s), causal 307 us (895); capped and causal
+// 371 us; 2 x 4096 tokens, 16 heads over 4 291 us (945), with a prefix 201 us.  dim 64: 2 x 8192 tokens, 16 heads 657 us (835),
+// causal 359.  fp32, dim 128: 8 heads of 2048 tokens, causal 141 us.  No LDS bank conflicts.  Causal and prefix masks:
+// an XCD takes one head after another, each from its longest block, so the last head's longest blocks start late.
 template <typename T, int DP, int MODE>
 __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_fwd(AttnArgs a) {
   constexpr int KEYS = BN<T>, NB = KEYS / 32;
@@ -746,7 +747,8 @@ __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_fwd(AttnArgs a) {
 
 // The workgroups of k_attn_few that a sequence gets, of `groups` for each block of rows and key
 // head: one each, and the others by the sequences' lengths, so that the longest does not decide the
-// call's time (up to 64 sequences; more of them even out by their number).
+// call's time (up to 64 sequences; more of them even out by their number).  Without lengths equal shares, and the last
+// sequence has what is left over.
 struct Share {
   int b, first, end;  // the sequence, its workgroups
 };
@@ -960,7 +962,7 @@ XP_DEV int first_near(const AttnArgs& a, const Seq& seq, int kw) { return max(0,
 // 2.4e-3 of its 2-norm off (its own rounding alone: 1.7e-3); over few it would be 2.6e-3 to
 // 2.8e-3, and is 2.3e-3 without dX's (2 x 4096 tokens, 12 heads of 64, documents of 32 to 2048: 100 us for 90).
 // Few rows: the keys in `splits` parts, whose sums k_attn_dq_join adds.
-// Bound as the forward is: two waves a SIMD, whose products (three here) and exponentials overlap in part only.
+// Bound as the forward is, with three products a block.
 // 2 sequences of 4096 tokens, 16 heads of 128 over 4, prefix: 332 us; matrix units busy for 30 % of it.
 template <typename T, int DP, int MODE, bool TWICE>
 __global__ __launch_bounds__(256, (WAVES<T, DP>)) void k_attn_dq(AttnArgs a) {
@@ -1478,7 +1480,8 @@ int parts(int dtype, const AttnArgs& a) {
 }
 
 // Parts of the keys of k_attn_dq where its rows do not fill the card, of at least 8 steps (fp32, whose steps are
-// long: 2).  Not with documents, whose rows see few keys.  (Training steps: fp32, 2902 tokens, one head of 33: 207 us, in
+// long: 2).  Not with documents: the parts are cut from all keys, not from those of a block's documents, so most of
+// them would be empty.  (Training steps: fp32, 2902 tokens, one head of 33: 207 us, in
 // one part 469; bf16, 3840 tokens, 8 heads of 64: 239 and 287.)
 int dq_parts(int dtype, const AttnArgs& a) {
   const int64_t groups = ceil_div(a.nq, ROWS) * a.heads * a.batch, steps = ceil_div(a.nk, dq_keys_of(dtype, a));
@@ -1494,8 +1497,8 @@ int near_blocks(const AttnArgs& a) { return (int)std::min<int64_t>(ceil_div(a.nq
 
 // Parts of k_attn_dkv where its blocks of keys do not fill the card twice over (causal, where they
 // differ in length: four times): heads that share keys first, then runs of queries, of at least 8 steps
-// (fp32, whose steps are long: 2).  Not with documents: a block's queries are few then, and
-// parts mostly empty (2 x 4096 tokens, 12 heads of 64, documents of 32 to 2048: 147 us without, 172 with).
+// (fp32, whose steps are long: 2).  Not with documents: the parts are cut from all queries, not from those of a
+// block's documents, so most of them would be empty (2 x 4096 tokens, 12 heads of 64, documents of 32 to 2048: 147 us without, 172 with).
 void cut_dkv(int dtype, AttnArgs& a, int64_t kgroups) {
   const int group = a.heads / a.kv_heads, want = a.causal ? 1024 : 512;
   a.head_parts = a.q_parts = 1;

@@ -6,7 +6,8 @@
 // they grow with the logarithm, bucket n / 2 + floor(log(2 a / n) / log(2 far / n) (n - n / 2)),
 // the last one from there on.  In fp64; a distance on a border belongs to the bucket that
 // starts there: the quotient is raised by 2^-44 of itself, a few times what its logarithms and
-// products round by.
+// products round by, so one that lies below a border by less than that counts as on it (over all max distances up to
+// 2^20: no distance with 8, 16, 32 or 64 buckets a direction, 3 with 128).
 #include "xp_device.h"
 #include "xp_kernels.h"
 
@@ -71,9 +72,10 @@ XP_DEV double run_sum(const float* p, int n) {
 // One workgroup per bucket and 2 heads: the bucket's distances are one run of each head's row.
 // Finding its ends costs as much as a short run, so one wave does it for all of them.
 // THREADS: 1024 where runs are long.
-// Bound by the longest run (the bucket of all keys behind the query holds half of a row): 65537
-// distances, 64 heads, 64 buckets, with the forward: 27.4 us (1 head a workgroup 31.5, 4 heads 29.7); 257 distances,
-// 12 heads 8.8 us (9.7, 9.6), of which the ends are half of the backward's.
+// Bound by the order of the launch and the ends: the bucket of all keys behind the query holds half of a row, and of 2048
+// workgroups of 1024 threads, 512 at a time, the last of that bucket starts in the fourth round; each finds its ends anew by
+// logarithms and an exponential in fp64.  65537 distances, 64 heads, 64 buckets: 21 us, with the forward 27.3 (1 head a workgroup
+// 31.5, 4 heads 29.7); 257 distances, 12 heads 5 us, with the forward 9.5 (9.7, 9.6), of which the ends are half.
 constexpr int RUNS = 2;
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void k_relbias_bwd(const float* __restrict__ dbias, Buckets b, int heads, float* __restrict__ grad) {

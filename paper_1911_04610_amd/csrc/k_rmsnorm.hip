@@ -137,7 +137,7 @@ XP_DEV void wide_sums(const float (&h)[E], const float (&dy)[E], const float (&w
 }
 
 // 16384x4096 bf16 with residual and sum: 97 us, 5.6 TB/s, of what a copy reaches (5.2 torch's, 6.2 the library's
-// probe); one row: 3 us, a launch.
+// probe); 8192x4096 fp32 92 us, 5.8 TB/s; one row: 3 us, a launch.
 // No __restrict__: sum and y may be x's or residual's buffer (every element is read
 // by the thread that writes it, before).
 template <typename T, int G, int E>
@@ -196,8 +196,9 @@ __global__ __launch_bounds__(THREADS<G>) void k_rms_fwd(RmsArgs a) {
 // fp32 (MOST_TERMS of them a thread at most: more rows are another launch), over the ROWS rows at a time in LDS.  The parts
 // are added in fp64 by k_rms_join; a single workgroup adds its own.  The next row's
 // h and dy are on their way while this one's sums are joined.
-// Bound by the bytes of large calls (16384x4096 bf16: 87 us, 4.6 TB/s for h, dy and dx) and by the two launches of
-// small ones: 8192x2048 with the skip's gradient 36 us (134 MB, 3.7 TB/s) and 5 us for the join, 1001x999 fp32 6.5 and 5.
+// Bound by the bytes of large calls (16384x4096 bf16: 84 us with the join, 4.8 TB/s for h, dy and dx; 262144x4096
+// 1230 us, 5.2 TB/s) and by the two launches of small ones: 1001x999 fp32 6.5 us and 5.  The skip's gradient is
+// read behind the next row's h and dy, not ahead, and its wait is a wait for them: 8192x2048 with it 36 us (134 MB, 3.7 TB/s).
 template <typename T, int G, int E>
 __global__ __launch_bounds__(THREADS<G>) void k_rms_bwd(RmsArgs a) {
   constexpr int C = CHUNK<T>, V = E / C;
