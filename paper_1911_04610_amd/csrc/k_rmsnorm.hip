@@ -366,7 +366,7 @@ hipError_t bwd(RmsArgs a, void* workspace, hipStream_t s) {
       b.x = from(a.x, row, a.ldx);
       b.res = from(a.res, row, a.ldr);
       b.y = from(a.y, row, a.ldy);
-      b.part = (float*)workspace + parts * a.dim;
+      b.part = a.grad ? (float*)workspace + parts * a.dim : nullptr;
       const int blocks = bwd_blocks<g>(b.rows);
       const double bytes = (double)sizeof(T) * b.rows * a.dim * (2 + (a.y != nullptr) + (a.res != nullptr));
       XP_LAUNCH(sizeof(T) == 2 ? "k_rms_bwd<bf16>" : "k_rms_bwd<f32>", bytes, (k_rms_bwd<T, g, e>), dim3(blocks),
